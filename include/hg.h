@@ -93,6 +93,10 @@ extern "C" {
 #define HG_THETA_NONE  2147483647
 #define HG_DTYPE_F32   0
 #define HG_DTYPE_BF16  1
+#define HG_ACT_NONE    0   /* z                                             */
+#define HG_ACT_RELU    1   /* max(z, 0)                                     */
+#define HG_ACT_SILU    2   /* z / (1 + exp(-z))                             */
+#define HG_ACT_GELU    3   /* z (1 + erf(z / sqrt 2)) / 2                   */
 #define HG_MAX_REL     255
 #define HG_MAX_NTYPE   255
 
@@ -499,6 +503,82 @@ int hg_mean_agg_bwd(int64_t n_sub, int32_t d, int32_t dtype, const int32_t* l2g,
 int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t* overlap, const int32_t* l2g,
                    const int32_t* home, const int32_t* const* g2l, const void* const* h_parts, void* Y,
                    void* stream);
+
+/* ---- sequence encoder over node histories ---------------------------------
+ * The operators of one block of an encoder over longer histories than the
+ * temporal module's window (the sequences of E12-E13 without the limit on w):
+ *   qkv = hg_linear(x),  q, k = hg_qk_norm_rope(q, k),  o = hg_linattn(q, k, v),
+ *   x' = x + hg_linear(o),  x'' = x' + hg_linear(hg_glu(x'))
+ * Here every matrix of a call, weights and weight gradients too, is stored in
+ * dtype (HG_DTYPE_F32 or HG_DTYPE_BF16); biases, norm weights, decays, states
+ * and their gradients are float32.  Sums are float32 whatever dtype is.
+ *
+ * Linear map with bias, activation and residual in its epilogue (the node
+ * update of E11 with any widths):
+ *   z = X W + b,  Y = act(z) + R
+ * X [n, d_in] with rows ld_x apart, Y [n, d_out] ld_y apart, R ld_r apart,
+ * W [d_in, d_out] contiguous, bias [d_out] (may be NULL = 0), R may be NULL.
+ * Y may be R itself (same address and ld); else Y must not overlap an input.
+ * Base addresses of X, W and dY are multiples of 16 bytes; strides are in
+ * elements and at least the width.  n < 2^31, widths at most 2^20.
+ *
+ * Precision: bfloat16 products enter the MFMA exactly and z, act and the sum
+ * with R are float32, rounded once into Y.  float32 rows follow the row
+ * transforms' split-fp16 rule stated at the top (X by row, W as a whole); a
+ * row that holds an infinity or NaN gives NaN in that row only.  In the
+ * backward dz = dY * act'(z) is formed from float32 z; bfloat16 calls round
+ * it once (when act is not HG_ACT_NONE) as operand of the two products, and
+ * dbias sums it before that.  float32 weight gradients use the three-part
+ * bfloat16 rule. */
+typedef struct hg_linear_desc {
+  int64_t n;
+  int32_t d_in, d_out;
+  int32_t dtype;     /* HG_DTYPE_* of X, W, R, Y and of dY, dX, dW */
+  int32_t act;       /* HG_ACT_* */
+  int64_t ld_x;      /* rows of X */
+  int64_t ld_y;      /* rows of Y; in the backward of dY */
+  int64_t ld_r;      /* rows of R (ignored without R); in the backward of dX */
+} hg_linear_desc;
+
+/* Bytes of workspace; 0 for an invalid descriptor (and where none is needed). */
+size_t hg_linear_fwd_workspace_size(const hg_linear_desc* L);
+size_t hg_linear_bwd_workspace_size(const hg_linear_desc* L);
+int hg_linear_fwd(const hg_linear_desc* L, const void* X, const void* W, const float* bias, const void* R,
+                  void* Y, void* ws, size_t ws_bytes, void* stream);
+/* Backward for dY = dL/dY (z is formed again: nothing is kept between the
+ * calls; dL/dR = dY):
+ *   dz = dY * act'(z),  dX = dz W^T,  dW = X^T dz,  dbias = sum over rows of dz
+ * dX is OVERWRITTEN; dW and dbias are OVERWRITTEN when accumulate = 0 and added
+ * into when accumulate = 1.  Each of dX, dW, dbias may be NULL (not computed).
+ * The outputs must not overlap an input.  Deterministic. */
+int hg_linear_bwd(const hg_linear_desc* L, const void* X, const void* W, const float* bias, const void* dY,
+                  void* dX, void* dW, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Gated product of a feed-forward block: both projections, the activation and
+ * their product in one kernel:
+ *   [a u] = X W + b,  H = act(a) * u
+ * X [n, d] ld_x apart, W [d, 2 f] contiguous (the gate's columns first), bias
+ * [2 f] or NULL, H [n, f] ld_h apart.  Rules and precision are those of
+ * hg_linear_fwd. */
+typedef struct hg_glu_desc {
+  int64_t n;
+  int32_t d, f;
+  int32_t dtype;
+  int32_t act;
+  int64_t ld_x;      /* rows of X */
+  int64_t ld_h;      /* rows of H; in the backward of dH */
+  int64_t ld_dx;     /* rows of dX (backward) */
+} hg_glu_desc;
+size_t hg_glu_fwd_workspace_size(const hg_glu_desc* L);
+size_t hg_glu_bwd_workspace_size(const hg_glu_desc* L);
+int hg_glu_fwd(const hg_glu_desc* L, const void* X, const void* W, const float* bias, void* H, void* ws,
+               size_t ws_bytes, void* stream);
+/* Backward for dH = dL/dH (a and u are formed again):
+ *   da = dH * u * act'(a),  du = dH * act(a),  dX = [da du] W^T,  dW = X^T [da du],
+ *   dbias = sum over rows of [da du]
+ * with the rules of hg_linear_bwd. */
+int hg_glu_bwd(const hg_glu_desc* L, const void* X, const void* W, const float* bias, const void* dH, void* dX,
+               void* dW, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- diagnostics ------------------------------------------------------- */
 const char* hg_status_string(int status);

@@ -29,6 +29,10 @@ HG_KEYDIR_OUT = 0
 HG_THETA_NONE = 2**31 - 1
 HG_DTYPE_F32 = 0
 HG_DTYPE_BF16 = 1
+HG_ACT_NONE = 0
+HG_ACT_RELU = 1
+HG_ACT_SILU = 2
+HG_ACT_GELU = 3
 HG_MAX_REL = 255
 HG_MAX_NTYPE = 255
 HG_MAX_PARTS = 64
@@ -42,6 +46,8 @@ EXPORTS = [
     "hg_mlp_bce_workspace_size", "hg_mlp_bce_fwd_bwd", "hg_adam_step",
     "hg_temporal_fwd", "hg_temporal_bwd_workspace_size", "hg_temporal_bwd",
     "hg_mean_agg_fwd", "hg_mean_agg_bwd", "hg_home_gather",
+    "hg_linear_fwd_workspace_size", "hg_linear_bwd_workspace_size", "hg_linear_fwd", "hg_linear_bwd",
+    "hg_glu_fwd_workspace_size", "hg_glu_bwd_workspace_size", "hg_glu_fwd", "hg_glu_bwd",
     "hg_status_string", "hg_last_error_detail", "hg_timing_enable", "hg_timing_collect",
 ]
 
@@ -105,6 +111,16 @@ class TemporalWeights(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in TEMPORAL_PARAMS]
 
 
+class LinearDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d_in", C.c_int32), ("d_out", C.c_int32), ("dtype", C.c_int32),
+                ("act", C.c_int32), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_r", C.c_int64)]
+
+
+class GluDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("d", C.c_int32), ("f", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32),
+                ("ld_x", C.c_int64), ("ld_h", C.c_int64), ("ld_dx", C.c_int64)]
+
+
 _lib = None
 
 
@@ -149,6 +165,14 @@ def lib() -> C.CDLL:
         "hg_mean_agg_fwd": (C.c_int, [i64, i32, i32, i32, vp, vp, vp, vp, vp]),
         "hg_mean_agg_bwd": (C.c_int, [i64, i32, i32, vp, vp, vp, vp, i32, vp]),
         "hg_home_gather": (C.c_int, [i64, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]),
+        "hg_linear_fwd_workspace_size": (sz, [vp]),
+        "hg_linear_bwd_workspace_size": (sz, [vp]),
+        "hg_linear_fwd": (C.c_int, [vp] * 7 + [sz, vp]),
+        "hg_linear_bwd": (C.c_int, [vp] * 8 + [i32, vp, sz, vp]),
+        "hg_glu_fwd_workspace_size": (sz, [vp]),
+        "hg_glu_bwd_workspace_size": (sz, [vp]),
+        "hg_glu_fwd": (C.c_int, [vp] * 6 + [sz, vp]),
+        "hg_glu_bwd": (C.c_int, [vp] * 8 + [i32, vp, sz, vp]),
         "hg_status_string": (C.c_char_p, [C.c_int]),
         "hg_last_error_detail": (C.c_char_p, []),
         "hg_timing_enable": (C.c_int, [C.c_int]),
@@ -615,6 +639,189 @@ def hg_align_loss_fwd_bwd_noalloc(H, overlap, H_ref, dH, loss3, w=None, lambda_n
                                                _stream(stream)),
            "hg_align_loss_fwd_bwd_noalloc")
     return loss3
+
+
+# ---- sequence encoder -------------------------------------------------------
+
+def _float_code(where: str, t) -> int:
+    if t.dtype == torch.float32:
+        return HG_DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return HG_DTYPE_BF16
+    raise TypeError(f"{where}: {t.dtype} is neither float32 nor bfloat16")
+
+
+def _same(where: str, t, *others):
+    """Every given tensor has the first one's type and device."""
+    for o in others:
+        if o is not None and (o.dtype != t.dtype or o.device != t.device):
+            raise TypeError(f"{where}: {o.dtype} on {o.device} beside {t.dtype} on {t.device}")
+
+
+def _vector(where: str, t, n: int, device, dtype=torch.float32):
+    """A contiguous vector of n values, or None."""
+    if t is not None and (t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{where}: expected {n} contiguous {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on "
+                         f"{t.device}")
+
+
+def _rows(where: str, t, n: int, width: int) -> int:
+    """Checks an [n, width] matrix whose rows are contiguous; returns their distance."""
+    if t.shape != (n, width) or (width > 1 and n > 0 and t.stride(1) != 1):
+        raise ValueError(f"{where}: expected rows [{n}, {width}] with unit column stride, got {tuple(t.shape)} "
+                         f"strides {t.stride()}")
+    return t.stride(0) if n > 1 else max(width, t.stride(0)) if n else width
+
+
+def _matrix(where: str, t, rows: int, cols: int):
+    if t.shape != (rows, cols) or not t.is_contiguous():
+        raise ValueError(f"{where}: expected a contiguous [{rows}, {cols}], got {tuple(t.shape)} strides {t.stride()}")
+
+
+def _ws_for(ws, need: int, device):
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+    return (None, 0) if ws is None else (C.c_void_p(ws.data_ptr()), ws.numel())
+
+
+def _linear_desc(where, x, W, y_cols, act) -> LinearDesc:
+    n, d = x.shape
+    _same(where, x, W)
+    _matrix(where, W, d, y_cols)
+    return LinearDesc(n, d, y_cols, _float_code(where, x), act, _rows(where, x, n, d), y_cols, y_cols)
+
+
+def hg_linear_fwd_workspace_size(n: int, d_in: int, d_out: int, dtype=torch.float32, act: int = HG_ACT_NONE,
+                                 ld_x: Optional[int] = None) -> int:
+    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
+    desc = LinearDesc(n, d_in, d_out, code, act, d_in if ld_x is None else ld_x, d_out, d_out)
+    return int(lib().hg_linear_fwd_workspace_size(C.byref(desc)))
+
+
+def hg_linear_bwd_workspace_size(n: int, d_in: int, d_out: int, dtype=torch.float32, act: int = HG_ACT_NONE,
+                                 ld_x: Optional[int] = None, ld_dy: Optional[int] = None) -> int:
+    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
+    desc = LinearDesc(n, d_in, d_out, code, act, d_in if ld_x is None else ld_x, d_out if ld_dy is None else ld_dy,
+                      d_in)
+    return int(lib().hg_linear_bwd_workspace_size(C.byref(desc)))
+
+
+def hg_linear_fwd(x, W, bias=None, residual=None, act: int = HG_ACT_NONE, y=None, ws=None, stream=None):
+    """y = act(x W + bias) + residual: x [n, d_in], W [d_in, d_out], bias
+    float32 [d_out], residual and y [n, d_out] (y may be the residual); rows
+    may be strided, W is contiguous."""
+    where = "hg_linear_fwd"
+    L = lib()
+    n, m = int(x.shape[0]), int(W.shape[1])
+    desc = _linear_desc(where, x, W, m, act)
+    if y is None:
+        y = torch.empty((n, m), dtype=x.dtype, device=x.device)
+    _same(where, x, y, residual)
+    _vector(where, bias, m, x.device)
+    desc.ld_y = _rows(where, y, n, m)
+    if residual is not None:
+        desc.ld_r = _rows(where, residual, n, m)
+    ref = C.byref(desc)
+    wp, wn = _ws_for(ws, L.hg_linear_fwd_workspace_size(ref), x.device)
+    _check(L.hg_linear_fwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(residual), _ptr(y), wp, wn, _stream(stream)), where)
+    return y
+
+
+def hg_linear_bwd(x, W, bias, dy, act: int = HG_ACT_NONE, dx=None, dW=None, dbias=None, accumulate: bool = False,
+                  want=(True, True, True), ws=None, stream=None):
+    """Returns (dx, dW, dbias) of hg_linear_fwd for dy = dL/dy (the residual's
+    gradient is dy itself); dbias only with a bias.  With accumulate, dW and
+    dbias are added into the given buffers.  want: which of the three to
+    compute where no buffer is given."""
+    where = "hg_linear_bwd"
+    L = lib()
+    n, m = int(x.shape[0]), int(W.shape[1])
+    desc = _linear_desc(where, x, W, m, act)
+    dx, dW, dbias = _linear_grads(where, x, W, bias, dx, dW, dbias, accumulate, want)
+    _same(where, x, dy, dx, dW)
+    desc.ld_y = _rows(where, dy, n, m)
+    if dx is not None:
+        desc.ld_r = _rows(where, dx, n, x.shape[1])
+    ref = C.byref(desc)
+    wp, wn = _ws_for(ws, L.hg_linear_bwd_workspace_size(ref), x.device)
+    _check(L.hg_linear_bwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(dy), _ptr(dx), _ptr(dW), _ptr(dbias),
+                           int(bool(accumulate)), wp, wn, _stream(stream)), where)
+    return dx, dW, dbias
+
+
+def _linear_grads(where, x, W, bias, dx, dW, dbias, accumulate, want):
+    if accumulate and ((dW is None and want[1]) or (dbias is None and want[2] and bias is not None)):
+        raise ValueError(f"{where}: accumulate needs the buffers to add into")
+    if dx is None and want[0]:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if dW is None and want[1]:
+        dW = torch.empty_like(W)
+    if dW is not None:
+        _matrix(where, dW, *W.shape)
+    _vector(where, bias, W.shape[1], x.device)
+    if dbias is None and want[2] and bias is not None:
+        dbias = torch.empty_like(bias)
+    _vector(where, dbias, W.shape[1], x.device)
+    return dx, dW, dbias
+
+
+def _glu_desc(where, x, W, act) -> GluDesc:
+    n, d = x.shape
+    if W.dim() != 2 or W.shape[1] % 2:
+        raise ValueError(f"{where}: W is [d, 2 f], got {tuple(W.shape)}")
+    _same(where, x, W)
+    _matrix(where, W, d, W.shape[1])
+    f = W.shape[1] // 2
+    return GluDesc(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), f, d)
+
+
+def hg_glu_fwd_workspace_size(n: int, d: int, f: int, dtype=torch.float32, ld_x: Optional[int] = None) -> int:
+    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
+    desc = GluDesc(n, d, f, code, HG_ACT_SILU, d if ld_x is None else ld_x, f, d)
+    return int(lib().hg_glu_fwd_workspace_size(C.byref(desc)))
+
+
+def hg_glu_bwd_workspace_size(n: int, d: int, f: int, dtype=torch.float32, ld_x: Optional[int] = None) -> int:
+    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
+    desc = GluDesc(n, d, f, code, HG_ACT_SILU, d if ld_x is None else ld_x, f, d)
+    return int(lib().hg_glu_bwd_workspace_size(C.byref(desc)))
+
+
+def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=None):
+    """h = act(a) * u with [a u] = x W + bias: x [n, d], W [d, 2 f] (the gate's
+    columns first), bias float32 [2 f], h [n, f]."""
+    where = "hg_glu_fwd"
+    L = lib()
+    desc = _glu_desc(where, x, W, act)
+    n, f = int(x.shape[0]), int(desc.f)
+    if h is None:
+        h = torch.empty((n, f), dtype=x.dtype, device=x.device)
+    _same(where, x, h)
+    _vector(where, bias, 2 * f, x.device)
+    desc.ld_h = _rows(where, h, n, f)
+    ref = C.byref(desc)
+    wp, wn = _ws_for(ws, L.hg_glu_fwd_workspace_size(ref), x.device)
+    _check(L.hg_glu_fwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(h), wp, wn, _stream(stream)), where)
+    return h
+
+
+def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=None, accumulate: bool = False,
+               want=(True, True, True), ws=None, stream=None):
+    """Returns (dx, dW, dbias) of hg_glu_fwd for dh = dL/dh, as hg_linear_bwd does."""
+    where = "hg_glu_bwd"
+    L = lib()
+    desc = _glu_desc(where, x, W, act)
+    n, f = int(x.shape[0]), int(desc.f)
+    dx, dW, dbias = _linear_grads(where, x, W, bias, dx, dW, dbias, accumulate, want)
+    _same(where, x, dh, dx, dW)
+    desc.ld_h = _rows(where, dh, n, f)
+    if dx is not None:
+        desc.ld_dx = _rows(where, dx, n, x.shape[1])
+    ref = C.byref(desc)
+    wp, wn = _ws_for(ws, L.hg_glu_bwd_workspace_size(ref), x.device)
+    _check(L.hg_glu_bwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(dh), _ptr(dx), _ptr(dW), _ptr(dbias),
+                        int(bool(accumulate)), wp, wn, _stream(stream)), where)
+    return dx, dW, dbias
 
 
 def hg_timing_enable(on: bool = True):

@@ -1,0 +1,592 @@
+// Tiled matrix product on the 16-bit MFMA with a fused epilogue: the core of
+// the linear map and of the gated product, forward and backward.
+//
+//   Z[m][n] = sum_k A[m][k] B[k][n]
+//
+// Operands are 16-bit matrices of one or more planes (a float32 matrix is a
+// sum of planes, see the product lists below).  Each operand is read as it
+// lies: k contiguous (KM, "rows of k") or k the row index (the rows run over
+// m or n).  That gives the three products of a linear map without a
+// transposition pass:
+//   z  = x W      A = x   KM,      B = W   k-rows
+//   dx = dz W^T   A = dz  KM,      B = W   KM
+//   dW = x^T dz   A = x   k-rows,  B = dz  k-rows
+//
+// A block of waves owns a BM x BN tile of Z and walks k in steps of BK with
+// two LDS buffers: the tile of step t+1 is written to LDS by the loads
+// themselves (buffer_load ... lds, 16 bytes a lane) while the MFMAs of step t
+// run, one barrier a step.  Buffer descriptors carry the bounds: what lies
+// past the last row reads as zero.
+//
+// LDS layouts (a load writes 64 x 16 consecutive bytes, so a swizzle has to be
+// in the global address of the lane):
+//   KM      [row][BK]: the 16-byte chunk ch of row r lies at slot ch ^ (r & 7),
+//           so the 16 rows that one fragment read touches fall on all banks;
+//   k-rows  [k][BM]: the 32-byte granule gr of row k lies at granule
+//           gr ^ g_swz(k), for the transposing 8-byte reads, whose half wave
+//           touches rows 0-3 and 8-11 of one granule.
+//
+// The fragments enter the MFMA as (B, A), so lane (c, g) of the wave holds
+// Z[16 i + c][16 j + 4 g + v], v = 0..3: four consecutive columns of a row.
+#pragma once
+
+#include "hg_mfma.h"
+
+namespace hg {
+
+typedef _Float16 g_f16x8 __attribute__((ext_vector_type(8)));
+typedef short g_s16x4 __attribute__((ext_vector_type(4)));
+
+// The part products that make up one product of two split matrices.
+//   GBf16    one bfloat16 plane a factor, exact
+//   GF16x2   fp16 high part and remainder of both factors, scaled by powers of
+//            two: three of the four products (the split-fp16 row transforms)
+//   GBf16x3  three bfloat16 parts, the six products of order at most two (the
+//            weight gradients: no scales, since the sum runs over rows)
+struct GBf16 {
+  static constexpr int P = 1, NP = 1;
+  static constexpr bool kF16 = false;
+  static constexpr int pa[1] = {0}, pb[1] = {0};
+};
+struct GF16x2 {
+  static constexpr int P = 2, NP = 3;
+  static constexpr bool kF16 = true;
+  static constexpr int pa[3] = {1, 0, 0}, pb[3] = {0, 1, 0};
+};
+struct GBf16x3 {
+  static constexpr int P = 3, NP = 6;
+  static constexpr bool kF16 = false;
+  static constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+};
+
+template <bool kF16>
+__device__ __forceinline__ f32x4 g_mfma(uint4 a, uint4 b, f32x4 c) {
+  if constexpr (kF16) {
+    return mfma_f16(a, b, c);
+  } else {
+    return mfma_bf16(a, b, c);
+  }
+}
+
+// One operand.  KM: `rows` rows (m or n) of K values; else K rows of `cols`
+// values.  ld and plane (the distance of the planes) in elements; p 16-byte
+// aligned, ld, K (KM) or cols multiples of 8.
+struct GOperand {
+  const uint16_t* p;
+  int64_t ld, plane;
+  int64_t rows;  // rows of the matrix as stored
+  int32_t cols;  // valid values of a row
+};
+
+// How Z becomes the output.  Scales undo the operands' powers of two.
+struct GEpi {
+  const float* ua;    // [M] factor of each row, or null
+  const float* ub;    // [1] factor of the whole product, or null
+  const float* bias;  // [N] (gated: [2 F]) or null
+  const void* res;    // residual rows (linear) or upstream gradient rows (backward), or null
+  int64_t ld_res;
+  void* out;
+  int64_t ld_out;
+  int32_t act;
+  int32_t ncol;       // columns that the output has (the tiles may count padding too)
+  int32_t half;       // gated: F; a [., 2 F] result stored in two padded halves: F; else 0
+  int32_t halfp;      // distance of the two halves as the operands hold them
+  int32_t outp;       // gradient of z: padded width of a row (gated: of each half), a multiple of 8
+  int32_t accumulate;
+  float* colsum;      // [tiles of m][ld_colsum] column sums of what a tile wrote, or null
+  int64_t ld_colsum;
+  float* part;        // [splits][M][ld_part] when the k range is split
+  int64_t ld_part;
+};
+
+struct GArgs {
+  GOperand a, b;
+  int64_t M;
+  int32_t N;          // columns of Z as the tiles count them (gated: 2 * halfp)
+  int64_t K;
+  int64_t k_split;    // k range of a split (a multiple of 64), >= K: no split
+  int32_t tiles_m, tiles_n;
+  GEpi e;
+};
+
+__device__ __forceinline__ float g_sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+
+// act(z) and, with G, act'(z); the choice is the same for the whole launch
+template <bool G>
+__device__ __forceinline__ float g_act(int act, float z, float& d) {
+  switch (act) {
+    case HG_ACT_RELU:
+      if (G) d = z > 0.f ? 1.f : (z != z ? z : 0.f);
+      return z > 0.f ? z : (z != z ? z : 0.f);
+    case HG_ACT_SILU: {
+      const float s = g_sigmoid(z);
+      if (G) d = s * (1.f + z * (1.f - s));
+      return z * s;
+    }
+    case HG_ACT_GELU: {
+      const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
+      if (G) d = p + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+      return z * p;
+    }
+    default:
+      if (G) d = 1.f;
+      return z;
+  }
+}
+__device__ __forceinline__ float g_act(int act, float z) {
+  float d;
+  return g_act<false>(act, z, d);
+}
+
+template <class T>
+__device__ __forceinline__ float g_load1(const void* p, int64_t at) {
+  if constexpr (sizeof(T) == 4) {
+    return static_cast<const float*>(p)[at];
+  } else {
+    return bf2f(static_cast<const uint16_t*>(p)[at]);
+  }
+}
+
+// Four consecutive values of a row; `vec`: they are all inside and aligned.
+template <class T>
+__device__ __forceinline__ void g_load4(const void* p, int64_t at, int n, bool vec, float (&v)[4]) {
+  if (vec) {
+    const f32x4 x = Elt<T>::load4(static_cast<const T*>(p) + at);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = x[q];
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = q < n ? g_load1<T>(p, at + q) : 0.f;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void g_store4(void* p, int64_t at, int n, bool vec, const float (&v)[4]) {
+  if constexpr (sizeof(T) == 4) {
+    float* o = static_cast<float*>(p) + at;
+    if (vec) {
+      *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < n) o[q] = v[q];
+    }
+  } else {
+    uint16_t* o = static_cast<uint16_t*>(p) + at;
+    if (vec) {
+      *reinterpret_cast<uint2*>(o) = uint2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < n) o[q] = f2bf(v[q]);
+    }
+  }
+}
+
+// Rows whose four-value groups can be moved at once.
+template <class T>
+__device__ __forceinline__ bool g_vec(const void* p, int64_t ld) {
+  return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
+}
+
+// ---- epilogues: rows m, columns n .. n + 3 of Z --------------------------------
+// Each replaces z by what it wrote (for the column sums).
+
+// out = act(z + bias) + res
+template <class T>
+struct EpiLinear {
+  static constexpr bool kGated = false, kColSum = false;
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4]) {
+    float r[4] = {0.f, 0.f, 0.f, 0.f};
+    if (e.res) g_load4<T>(e.res, m * e.ld_res + n, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float b = e.bias && q < left ? e.bias[n + q] : 0.f;
+      z[q] = g_act(e.act, z[q] + b) + r[q];
+    }
+    g_store4<T>(e.out, m * e.ld_out + n, left, left >= 4 && g_vec<T>(e.out, e.ld_out), z);
+  }
+};
+
+// out = res * act'(z + bias): the gradient of z; the padding of a row is written as zero
+template <class T>
+struct EpiLinearGrad {
+  static constexpr bool kGated = false, kColSum = true;
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4]) {
+    float r[4] = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0) g_load4<T>(e.res, m * e.ld_res + n, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float b = e.bias && q < left ? e.bias[n + q] : 0.f;
+      float d;
+      g_act<true>(e.act, z[q] + b, d);
+      z[q] = q < left ? r[q] * d : 0.f;
+    }
+    const int room = e.outp - n;
+    g_store4<T>(e.out, m * e.ld_out + n, room, room >= 4, z);
+  }
+};
+
+// out = z, or out + z; with half: the columns of two padded halves to [., 2 half]
+template <class T>
+struct EpiSum {
+  static constexpr bool kGated = false, kColSum = false;
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4]) {
+    if (e.half) {
+      // halfp is a multiple of 8, so four columns lie in one half
+      const int up = n >= e.halfp;
+      left = e.half - (n - (up ? e.halfp : 0));
+      n += up ? e.half - e.halfp : 0;
+      if (left <= 0) return;
+    }
+    const bool vec = left >= 4 && g_vec<T>(e.out, e.ld_out) && (n & 3) == 0;
+    if (e.accumulate) {
+      float r[4];
+      g_load4<T>(e.out, m * e.ld_out + n, left, vec, r);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) z[q] += r[q];
+    }
+    g_store4<T>(e.out, m * e.ld_out + n, left, vec, z);
+  }
+};
+
+// out = act(a + bias) * (u + bias), a and u the two halves' products
+template <class T>
+struct EpiGated {
+  static constexpr bool kGated = true, kColSum = false;
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4]) {
+    if (left <= 0) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const bool in = e.bias && q < left;
+      a[q] = g_act(e.act, a[q] + (in ? e.bias[f + q] : 0.f)) * (u[q] + (in ? e.bias[e.half + f + q] : 0.f));
+    }
+    g_store4<T>(e.out, m * e.ld_out + f, left, left >= 4 && g_vec<T>(e.out, e.ld_out), a);
+  }
+};
+
+// da = dh u act'(a), du = dh act(a), side by side; the padding of a half is written as zero
+template <class T>
+struct EpiGatedGrad {
+  static constexpr bool kGated = true, kColSum = true;
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4]) {
+    float r[4] = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0) g_load4<T>(e.res, m * e.ld_res + f, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const bool in = q < left;
+      const float ba = e.bias && in ? e.bias[f + q] : 0.f, bu = e.bias && in ? e.bias[e.half + f + q] : 0.f;
+      float d;
+      const float v = g_act<true>(e.act, a[q] + ba, d);
+      const float w = u[q] + bu;
+      a[q] = in ? r[q] * w * d : 0.f;
+      u[q] = in ? r[q] * v : 0.f;
+    }
+    const int room = e.outp - f;
+    g_store4<T>(e.out, m * e.ld_out + f, room, room >= 4, a);
+    g_store4<T>(e.out, m * e.ld_out + e.outp + f, room, room >= 4, u);
+  }
+};
+
+// ---- tile loads ----------------------------------------------------------------
+// Raw buffer descriptor: an offset at or past `bytes` reads as zero.
+__device__ __forceinline__ u32x4 g_rsrc(const void* base, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xFFFF),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), 0x00020000u};
+}
+
+// 16 bytes a lane from base + voff to LDS address lds + 16 * lane.  Written as
+// an instruction, since the compiler would let every later LDS read wait for
+// it: the caller waits (g_wait_loads) before the barrier that hands the buffer
+// over.  It has no result register.
+__device__ __forceinline__ void g_load_lds(u32x4 rsrc, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
+}
+__device__ __forceinline__ void g_wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ uint32_t g_lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// The granule swizzle of k-row tiles: rows of 256 bytes and more, or of 128
+// (four granules; the parity of the row is then half of the bank already).
+template <int BM>
+__device__ __forceinline__ int g_swz(int k) {
+  if constexpr (BM >= 128) {
+    return (k & 3) | (((k >> 3) & 1) << 2);
+  } else {
+    return ((k >> 1) & 1) | (((k >> 3) & 1) << 1);
+  }
+}
+
+// One operand's share of a step, per wave: PER loads of 1 KB.
+template <int BM, int BK, bool KM, int NW, bool GATED>
+struct GTile {
+  static constexpr int kBytes = BM * BK * 2;
+  static constexpr int INSTR = kBytes / 1024, PER = INSTR / NW;
+  static_assert(INSTR % NW == 0, "whole loads per wave");
+  static_assert(!KM || BK == 64, "the chunk swizzle is made for 128-byte rows");
+  uint32_t voff[PER];  // byte offset of the lane's 16 bytes from the step's base
+  int kch;             // KM: first k of the lane's chunk (the same in every load)
+
+  __device__ __forceinline__ void init(const GOperand& o, int wave, int lane, int upper) {
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int u = wave * PER + q;
+      if constexpr (KM) {
+        const int row = 8 * u + (lane >> 3), ch = (lane & 7) ^ (lane >> 3);
+        voff[q] = (uint32_t)((row * o.ld + ch * 8) * 2);
+        kch = ch * 8;
+      } else {
+        constexpr int SL = BM / 8, RPI = 64 / SL;  // 16-byte slots of a row, rows of a load
+        const int row = RPI * u + lane / SL, slot = lane % SL;
+        const int gr = (slot >> 1) ^ g_swz<BM>(row);
+        const int col = GATED ? (gr >> 1) * 16 + (gr & 1) * upper : gr * 16;
+        voff[q] = (uint32_t)((row * o.ld + col + (slot & 1) * 8) * 2);
+        kch = 0;
+      }
+    }
+  }
+  // base: address of (row0, k0) or (k0, col0); left: bytes from there to the end of the last row
+  __device__ __forceinline__ void issue(const uint16_t* base, int64_t left, int64_t k_left, uint32_t lds, int wave) const {
+    const int64_t most = 0x7FFFFFF0;
+    const u32x4 rsrc = g_rsrc(base, (uint32_t)(left < 0 ? 0 : (left < most ? left : most)));
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const uint32_t v = (KM && kch >= k_left) ? 0x7FFFFFF8u : voff[q];
+      g_load_lds(rsrc, v, lds + (wave * PER + q) * 1024);
+    }
+  }
+  // fragment of rows 16 i + c, k = 32 kb + 8 g .. + 7
+  __device__ static __forceinline__ uint4 frag(const char* lds, int i, int kb, int c, int g) {
+    if constexpr (KM) {
+      const int row = 16 * i + c, ch = (4 * kb + g) ^ (c & 7);
+      return *reinterpret_cast<const uint4*>(lds + row * 128 + ch * 16);
+    } else {
+      typedef __attribute__((address_space(3))) g_s16x4* lds_ptr;
+      const int f = g_swz<BM>(8 * g + (c >> 2));
+      const char* q = lds + (32 * kb + 8 * g + (c >> 2)) * (BM * 2) + ((i ^ f) * 32) + (c & 3) * 8;
+      const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q)));
+      const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(q + 4 * BM * 2)));
+      return uint4{a.x, a.y, b.x, b.y};
+    }
+  }
+};
+
+// XCD-aware order of the tiles: blocks go to the eight XCDs in turn, so each
+// XCD takes one contiguous share of a walk that goes down `group` tile rows
+// before it moves to the next tile column (operand tiles meet in its L2).
+__device__ __forceinline__ void g_tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t group, uint32_t& im,
+                                          uint32_t& in) {
+  const uint32_t n = tm * tn, per = n / 8, more = n % 8;
+  const uint32_t x = id % 8, at = id / 8;
+  const uint32_t i = x * per + (x < more ? x : more) + at;
+  const uint32_t span = group * tn, b = i / span, first = b * group;
+  const uint32_t rows = tm - first < group ? tm - first : group;
+  const uint32_t j = i - b * span;
+  im = first + j % rows;
+  in = j / rows;
+}
+
+// Rows of a tile that the epilogue holds in LDS at a time, and the LDS of a block.
+constexpr int g_slab_rows(int bm, int bn) { return bm * (bn + 4) * 4 <= 70000 ? bm : 64; }
+constexpr size_t g_lds_bytes(int planes, int bm, int bn, int bk) {
+  const size_t a = 2 * (size_t)planes * (bm + bn) * bk * 2, b = (size_t)g_slab_rows(bm, bn) * (bn + 4) * 4;
+  return a > b ? a : b;
+}
+
+// Block of (BM / WM) x (BN / WN) waves.
+template <class F, bool AKM, bool BKM, int BM, int BN, int BK, int WM, int WN, class Epi, bool SPLIT>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
+    k_gemm16(const GArgs p) {
+  constexpr int NWM = BM / WM, NWN = BN / WN, NW = NWM * NWN, MI = WM / 16, NI = WN / 16;
+  constexpr bool GATED = Epi::kGated;
+  typedef GTile<BM, BK, AKM, NW, false> TA;
+  typedef GTile<BN, BK, BKM, NW, GATED> TB;
+  constexpr int kStage = F::P * (TA::kBytes + TB::kBytes);
+  extern __shared__ __align__(1024) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4, wm = wave / NWN, wn = wave % NWN;
+  uint32_t im, in;
+  g_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, 8, im, in);
+  const int64_t m0 = (int64_t)im * BM;
+  const int n0 = (int)in * BN;               // tile column of Z
+  const int bcol = GATED ? (int)in * (BN / 2) : n0;  // first column of B that the tile reads
+  const int64_t k_from = SPLIT ? (int64_t)blockIdx.y * p.k_split : 0;
+  const int64_t k_to = SPLIT ? (k_from + p.k_split < p.K ? k_from + p.k_split : p.K) : p.K;
+  const int steps = (int)((k_to - k_from + BK - 1) / BK);
+
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(g_lds_addr(lds));
+  TA ta;
+  TB tb;
+  ta.init(p.a, wave, lane, 0);
+  tb.init(p.b, wave, lane, p.e.halfp);
+
+  auto issue = [&](int t) {
+    const int64_t k0 = k_from + (int64_t)t * BK, kl = k_to - k0;
+    const uint32_t st = lds0 + (t & 1) * kStage;
+#pragma unroll
+    for (int pl = 0; pl < F::P; ++pl) {
+      const uint16_t* a = p.a.p + pl * p.a.plane;
+      const uint16_t* b = p.b.p + pl * p.b.plane;
+      if constexpr (AKM) {
+        ta.issue(a + m0 * p.a.ld + k0, 2 * ((p.a.rows - m0 - 1) * p.a.ld + p.a.cols - k0), kl, st + pl * TA::kBytes, wave);
+      } else {
+        ta.issue(a + k0 * p.a.ld + m0, 2 * ((kl - 1) * p.a.ld + p.a.cols - m0), kl, st + pl * TA::kBytes, wave);
+      }
+      const uint32_t sb = st + F::P * TA::kBytes + pl * TB::kBytes;
+      if constexpr (BKM) {
+        tb.issue(b + (int64_t)bcol * p.b.ld + k0, 2 * ((p.b.rows - bcol - 1) * p.b.ld + p.b.cols - k0), kl, sb, wave);
+      } else {
+        // rows that B has: its k may end before A's padded one
+        const int64_t rl = (p.b.rows < k_to ? p.b.rows : k_to) - k0;
+        tb.issue(b + k0 * p.b.ld + bcol, 2 * ((rl - 1) * p.b.ld + p.b.cols - bcol), rl, sb, wave);
+      }
+    }
+  };
+
+  f32x4 acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  issue(0);
+  for (int t = 0; t < steps; ++t) {
+    g_wait_loads();  // this wave's share of the step is in LDS
+    __syncthreads();
+    if (t + 1 < steps) issue(t + 1);
+    const char* sa = lds + (t & 1) * kStage;
+    const char* sb = sa + F::P * TA::kBytes;
+#pragma unroll
+    for (int kb = 0; kb < BK / 32; ++kb) {
+      uint4 fa[F::P][MI], fb[F::P][NI];
+#pragma unroll
+      for (int pl = 0; pl < F::P; ++pl) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j) fb[pl][j] = TB::frag(sb + pl * TB::kBytes, wn * NI + j, kb, c, g);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[pl][i] = TA::frag(sa + pl * TA::kBytes, wm * MI + i, kb, c, g);
+      }
+#pragma unroll
+      for (int s = 0; s < F::NP; ++s)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j)
+            acc[i][j] = g_mfma<F::kF16>(fb[F::pb[s]][j], fa[F::pa[s]][i], acc[i][j]);
+    }
+  }
+
+  // ---- epilogue: the tile goes through LDS in slabs of SR rows, so that rows
+  // are read and written whole; a thread keeps its four columns of Z
+  constexpr int SR = g_slab_rows(BM, BN), LDZ = BN + 4, NT = NW * 64;
+  constexpr int TC = GATED ? BN / 8 : BN / 4;  // threads side by side
+  static_assert(NT % TC == 0, "a thread keeps its columns");
+  const GEpi& e = p.e;
+  float* zt = reinterpret_cast<float*>(lds);
+  const float ub = e.ub ? *e.ub : 1.f;
+  const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
+  const int zc = GATED ? (tc >> 2) * 32 + (tc & 3) * 4 : tc * 4;  // column of the tile (gated: of the gate)
+  const int n = GATED ? bcol + tc * 4 : n0 + zc;                  // column of the result (of a half)
+  const bool in_n = n < (GATED ? e.halfp : p.N);
+  float cs[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+  for (int s0 = 0; s0 < BM; s0 += SR) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int row = wm * WM + 16 * i - s0;  // whole 16-row blocks lie in one slab
+      if (row >= 0 && row < SR) {
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+          *reinterpret_cast<f32x4*>(zt + (row + c) * LDZ + wn * WN + 16 * j + 4 * g) = acc[i][j];
+      }
+    }
+    __syncthreads();
+    if (in_n) {
+      for (int r = tr; r < SR; r += NT / TC) {
+        const int64_t m = m0 + s0 + r;
+        if (m >= p.M) break;
+        const float ua = e.ua ? e.ua[m] : 1.f;
+        const f32x4 x = split_unscale4(*reinterpret_cast<const f32x4*>(zt + r * LDZ + zc), ua, ub);
+        if constexpr (SPLIT) {
+          // ld_part and halfp are multiples of 4
+          float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
+          *reinterpret_cast<f32x4*>(part) = x;
+          if constexpr (GATED)
+            *reinterpret_cast<f32x4*>(part + e.halfp) =
+                split_unscale4(*reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16), ua, ub);
+        } else {
+          float z[4] = {x[0], x[1], x[2], x[3]};
+          if constexpr (GATED) {
+            const f32x4 y = split_unscale4(*reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16), ua, ub);
+            float u[4] = {y[0], y[1], y[2], y[3]};
+            Epi::apply(e, m, n, e.half - n, z, u);
+            if constexpr (Epi::kColSum) {
+#pragma unroll
+              for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
+            }
+          } else {
+            Epi::apply(e, m, n, e.ncol - n, z);
+            if constexpr (Epi::kColSum) {
+#pragma unroll
+              for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
+            }
+          }
+        }
+      }
+    }
+  }
+  if constexpr (Epi::kColSum && !SPLIT) {
+    if (e.colsum) {
+      // over the threads that share columns, in order
+      constexpr int H = GATED ? 2 : 1;
+      __syncthreads();
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) zt[tr * (H * TC * 4) + h * TC * 4 + tc * 4 + v] = cs[h][v];
+      __syncthreads();
+      for (int q = threadIdx.x; q < H * TC * 4; q += NT) {
+        float s = 0.f;
+        for (int w = 0; w < NT / TC; ++w) s += zt[w * (H * TC * 4) + q];
+        const int h = q / (TC * 4), col = (GATED ? bcol : n0) + q % (TC * 4);
+        if (col < (GATED ? e.half : e.ncol)) e.colsum[im * e.ld_colsum + col + (GATED ? h * e.half : 0)] = s;
+      }
+    }
+  }
+}
+
+// Sum of the splits in order, then the epilogue; a thread takes four columns of a row.
+template <class Epi>
+__global__ void __launch_bounds__(256) k_gemm16_join(const GArgs p, int splits) {
+  const GEpi& e = p.e;
+  const int cols = Epi::kGated ? e.halfp : p.N, quads = (cols + 3) / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, m = id / quads;
+  if (m >= p.M) return;
+  const int n = (int)(id - m * quads) * 4;
+  auto sum = [&](int at, float (&z)[4]) {
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; ++k) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(e.part + ((int64_t)k * p.M + m) * e.ld_part + at);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) s[v] += x[v];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) z[v] = s[v];
+  };
+  float z[4];
+  sum(n, z);
+  if constexpr (Epi::kGated) {
+    float u[4];
+    sum(e.halfp + n, u);
+    Epi::apply(e, m, n, e.half - n, z, u);
+  } else {
+    Epi::apply(e, m, n, e.ncol - n, z);
+  }
+}
+
+}  // namespace hg

@@ -1,0 +1,845 @@
+// Linear map with bias, activation and residual, and the gated product of a
+// feed-forward block, forward and backward: operand preparation, the choice of
+// tiles and the launches around the product core of hg_gemm.h.
+//
+//   linear   z = X W + b,       Y = act(z) + R
+//   gated    [a u] = X W + b,   H = act(a) * u
+//   backward dz from z and the upstream rows (the forward product once more,
+//            with the gradient in its epilogue), dX = dz W^T, dW = X^T dz
+//
+// The gated product is the same product with the columns of a tile taken by
+// 16 in turn from the gate and from the up projection, so that a lane holds
+// both values of an output and z never leaves the registers.
+//
+// bfloat16 operands are used where they lie when their rows are 16-byte
+// aligned and a multiple of 8 wide; else they are copied once into padded
+// rows.  float32 operands become planes of 16-bit parts first (see the product
+// lists in hg_gemm.h).
+#include <atomic>
+
+#include "hg_gemm.h"
+
+namespace hg {
+namespace {
+
+// One call of either operator.
+struct Prob {
+  int64_t n;
+  int32_t d, f;       // f: width of the output (of one half)
+  int32_t dtype, act;
+  bool gated;
+  int64_t ld_x, ld_y, ld_r;
+  int32_t halves() const { return gated ? 2 : 1; }
+  int32_t cols() const { return halves() * f; }            // columns of W
+  int32_t dp() const { return (d + 7) / 8 * 8; }
+  int32_t fp() const { return (f + 7) / 8 * 8; }
+  int32_t colsp() const { return halves() * fp(); }
+  bool f32() const { return dtype == HG_DTYPE_F32; }
+};
+
+constexpr int32_t kMaxWidth = 1 << 20;
+constexpr int64_t kMaxLd = 1 << 22;   // 256 rows of 16-bit values stay below 2^31 bytes
+constexpr int kAbsBlocks = 256;       // partial maxima of a matrix
+
+bool direct(int32_t width, int64_t ld) { return width % 8 == 0 && ld % 8 == 0 && ld < kMaxLd; }
+
+// ---- preparation -----------------------------------------------------------------
+// A padded row is `halves` halves of Fp values (a multiple of 8), each with F
+// values of the source row side by side; the padding is zero.
+struct RowShape {
+  int32_t F, Fp, halves;
+};
+
+template <class T, class Get>
+__device__ __forceinline__ void p_gather8(const RowShape& r, int j, Get get, float (&v)[8]) {
+  const int h = j >= r.Fp, f = j - h * r.Fp;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = f + q < r.F ? get(h * r.F + f + q) : 0.f;
+}
+
+// bfloat16 rows into padded rows; a thread moves eight values.
+__global__ void __launch_bounds__(256)
+    k_rows_pad(const uint16_t* __restrict__ src, int64_t ld, int64_t rows, RowShape rs, uint16_t* __restrict__ dst) {
+  const int chunks = rs.halves * rs.Fp / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / chunks;
+  if (row >= rows) return;
+  const int j = (int)(id - row * chunks) * 8;
+  const int h = j >= rs.Fp, f = j - h * rs.Fp;
+  const uint16_t* p = src + row * ld + h * rs.F + f;
+  uint16_t v[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = f + q < rs.F ? p[q] : 0;
+  uint4 o;
+  __builtin_memcpy(&o, v, 16);
+  *reinterpret_cast<uint4*>(dst + row * (int64_t)(rs.halves * rs.Fp) + j) = o;
+}
+
+__device__ __forceinline__ float p_mag(float x) {
+  const float m = fabsf(x);
+  return m <= 3.4028234664e38f ? m : 0.f;  // infinities and NaN set no scale
+}
+
+__device__ __forceinline__ void p_store_split(const float (&v)[8], float sc, uint16_t* hi, uint16_t* lo) {
+  float s[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) s[q] = v[q] * sc;
+  uint4 h, l;
+  split8(s, h, l);
+  *reinterpret_cast<uint4*>(hi) = h;
+  *reinterpret_cast<uint4*>(lo) = l;
+}
+
+// float32 rows into fp16 high parts and remainders, each row scaled by the
+// power of two of its largest magnitude; ua undoes it.  A wave takes a row.
+__global__ void __launch_bounds__(256)
+    k_rows_split(const float* __restrict__ src, int64_t ld, int64_t rows, RowShape rs, uint16_t* __restrict__ dst,
+                 int64_t plane, float* __restrict__ ua) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const float* x = src + row * ld;
+  const int wide = rs.halves * rs.F, pad = rs.halves * rs.Fp;
+  float m = 0.f;
+  for (int j = lane; j < wide; j += 64) m = fmaxf(m, p_mag(x[j]));
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  const uint32_t eb = split_exp(m);
+  const float sc = split_scale(eb);
+  for (int j = lane * 8; j < pad; j += 512) {
+    float v[8];
+    p_gather8<float>(rs, j, [&](int at) { return x[at]; }, v);
+    p_store_split(v, sc, dst + row * pad + j, dst + plane + row * pad + j);
+  }
+  if (lane == 0) ua[row] = split_unscale(eb);
+}
+
+__device__ __forceinline__ float p_block_max(float m, float* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
+  __syncthreads();
+  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+
+// Largest magnitude of a contiguous matrix, one value a block.
+__global__ void __launch_bounds__(256) k_absmax(const float* __restrict__ x, int64_t n, float* __restrict__ part) {
+  __shared__ float sh[4];
+  float m = 0.f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
+    m = fmaxf(m, p_mag(x[i]));
+  m = p_block_max(m, sh);
+  if (threadIdx.x == 0) part[blockIdx.x] = m;
+}
+
+// A contiguous float32 matrix into fp16 high parts and remainders under one scale.
+__global__ void __launch_bounds__(256)
+    k_matrix_split(const float* __restrict__ src, int64_t rows, RowShape rs, const float* __restrict__ part, int parts,
+                   uint16_t* __restrict__ dst, int64_t plane, float* __restrict__ ub) {
+  __shared__ float sh[4];
+  const float m = p_block_max((int)threadIdx.x < parts ? part[threadIdx.x] : 0.f, sh);
+  const uint32_t eb = split_exp(m);
+  const float sc = split_scale(eb);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *ub = split_unscale(eb);
+  const int pad = rs.halves * rs.Fp, chunks = pad / 8;
+  const int64_t n = rows * chunks;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < n; id += (int64_t)gridDim.x * 256) {
+    const int64_t row = id / chunks;
+    const int j = (int)(id - row * chunks) * 8;
+    const float* x = src + row * (int64_t)(rs.halves * rs.F);
+    float v[8];
+    p_gather8<float>(rs, j, [&](int at) { return x[at]; }, v);
+    p_store_split(v, sc, dst + row * pad + j, dst + plane + row * pad + j);
+  }
+}
+
+// float32 rows into three bfloat16 parts (each the rounded rest of the ones
+// before; a non-finite value keeps to the first part).
+__global__ void __launch_bounds__(256)
+    k_rows_split3(const float* __restrict__ src, int64_t ld, int64_t rows, RowShape rs, uint16_t* __restrict__ dst,
+                  int64_t plane) {
+  const int pad = rs.halves * rs.Fp, chunks = pad / 8;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / chunks;
+  if (row >= rows) return;
+  const int j = (int)(id - row * chunks) * 8;
+  const float* x = src + row * ld;
+  float v[8];
+  p_gather8<float>(rs, j, [&](int at) { return x[at]; }, v);
+  uint16_t o[3][8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    float r = v[q];
+    const bool fine = fabsf(r) < 3.3e38f;  // above, rounding up to bfloat16 could overflow
+#pragma unroll
+    for (int pl = 0; pl < 3; ++pl) {
+      o[pl][q] = fine || pl == 0 ? f2bf(r) : 0;
+      r -= bf2f(o[pl][q]);
+    }
+  }
+#pragma unroll
+  for (int pl = 0; pl < 3; ++pl) {
+    uint4 w;
+    __builtin_memcpy(&w, o[pl], 16);
+    *reinterpret_cast<uint4*>(dst + pl * plane + row * pad + j) = w;
+  }
+}
+
+// ---- column sums --------------------------------------------------------------------
+constexpr int kSumRows = 256;  // rows that one block sums
+
+template <class T>
+__global__ void __launch_bounds__(256)
+    k_colsum(const void* __restrict__ x, int64_t ld, int64_t rows, int32_t cols, float* __restrict__ part) {
+  __shared__ float sh[4][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int col = blockIdx.y * 64 + lane;
+  const int64_t r0 = (int64_t)blockIdx.x * kSumRows;
+  const int64_t r1 = r0 + kSumRows < rows ? r0 + kSumRows : rows;
+  float s = 0.f;
+  if (col < cols)
+    for (int64_t r = r0 + w; r < r1; r += 4) s += g_load1<T>(x, r * ld + col);
+  sh[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && col < cols) part[blockIdx.x * (int64_t)cols + col] = sh[0][lane] + sh[1][lane] + sh[2][lane] + sh[3][lane];
+}
+
+// Sums of `parts` rows of partial column sums: 16 columns a block, 16 threads a column.
+__global__ void __launch_bounds__(256)
+    k_colsum_join(const float* __restrict__ part, int64_t parts, int32_t cols, float* __restrict__ out, int accumulate) {
+  __shared__ float sh[16][17];
+  const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
+  const int col = blockIdx.x * 16 + cx;
+  float s = 0.f;
+  if (col < cols)
+    for (int64_t r = ry; r < parts; r += 16) s += part[r * cols + col];
+  sh[ry][cx] = s;
+  __syncthreads();
+  if (ry == 0 && col < cols) {
+#pragma unroll
+    for (int q = 1; q < 16; ++q) s += sh[q][cx];
+    out[col] = accumulate ? out[col] + s : s;
+  }
+}
+
+// ---- few rows -------------------------------------------------------------------------
+// Y of NR rows by reading W once: a lane takes 16 bytes of eight consecutive k
+// rows (8 k x VEC columns) and the same eight k of every row of X, so a wave
+// reads 8 x 64 rows' pieces, and the 8 waves of a block split k.  Bound by
+// the bytes of W.  LC lanes side by side cover LC * 16 bytes of a row.
+constexpr int kFewWaves = 8;
+constexpr int kFewRows = 8;
+
+// 16 bytes of a row, n values of them inside.
+template <class T, bool ALIGNED>
+__device__ __forceinline__ typename Elt<T>::rawv_t few_load(const T* p, int n) {
+  if (n >= Elt<T>::EL && ALIGNED) return Elt<T>::rawv(p);
+  typename Elt<T>::rawv_t r = Elt<T>::rawv_zero();
+  if constexpr (!ALIGNED) {
+#pragma unroll
+    for (int q = 0; q < Elt<T>::EL; ++q) {
+      if (q >= n) continue;
+      if constexpr (sizeof(T) == 4) {
+        r[q] = p[q];
+      } else {
+        r[q >> 1] |= (uint32_t)p[q] << (16 * (q & 1));
+      }
+    }
+  }
+  return r;
+}
+
+template <class T, class Epi, int NR, int LC, bool ALIGNED>
+__global__ void __launch_bounds__(kFewWaves * 64)
+    k_few_rows(const T* __restrict__ X, int64_t ld_x, const T* __restrict__ W, int32_t K, int32_t f, int nr,
+               const GEpi e) {
+  constexpr int VEC = Elt<T>::EL, H = Epi::kGated ? 2 : 1, COLS = LC * VEC, KG = 64 / LC;
+  __shared__ float sh[kFewWaves][H][NR][COLS];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lc = lane % LC, kg = lane / LC;
+  const int64_t ldw = (int64_t)H * f;
+  // neighbouring column blocks to one XCD: they share the lines of W
+  const uint32_t nb = gridDim.x, per = nb / 8, x = blockIdx.x % 8, more = nb % 8;
+  const int c0 = (int)(x * per + (x < more ? x : more) + blockIdx.x / 8) * COLS;
+  const int col = c0 + lc * VEC;
+  const int cl = f - col;  // columns left
+  float acc[H][NR][VEC];
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) acc[h][r][q] = 0.f;
+  if (cl > 0) {
+    for (int k = (wave * KG + kg) * 8; k < K; k += kFewWaves * KG * 8) {
+      typename Elt<T>::rawv_t w[H][8], xv[NR][8 / VEC];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+          w[h][j] = few_load<T, ALIGNED>(W + (k + j < K ? k + j : k) * ldw + h * (int64_t)f + col, k + j < K ? cl : 0);
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll
+        for (int j = 0; j < 8; j += VEC)
+          xv[r][j / VEC] = few_load<T, ALIGNED>(X + (r < nr ? r : 0) * ld_x + (k + j < K ? k + j : k), K - k - j);
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int r = 0; r < NR; ++r) {
+            const float xs = Elt<T>::rawv_get(xv[r][j / VEC], j % VEC);
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) acc[h][r][q] = fmaf(xs, Elt<T>::rawv_get(w[h][j], q), acc[h][r][q]);
+          }
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int r = 0; r < NR; ++r)
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) {
+        float s = acc[h][r][q];
+#pragma unroll
+        for (int o = LC; o < 64; o <<= 1) s += __shfl_xor(s, o, 64);
+        if (kg == 0) sh[wave][h][r][lc * VEC + q] = s;
+      }
+  __syncthreads();
+  for (int t = threadIdx.x; t < NR * COLS / 4; t += kFewWaves * 64) {
+    const int r = t / (COLS / 4), cc = t % (COLS / 4) * 4, n = c0 + cc;
+    if (r >= nr || n >= f) continue;
+    float z[H][4];
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) s += sh[w][h][r][cc + q];
+        z[h][q] = s;
+      }
+    if constexpr (Epi::kGated) {
+      Epi::apply(e, r, n, f - n, z[0], z[1]);
+    } else {
+      Epi::apply(e, r, n, f - n, z[0]);
+    }
+  }
+}
+
+template <class T, class Epi, int LC, bool ALIGNED>
+int launch_few(const Prob& p, const T* X, const T* W, const GEpi& e, hipStream_t s) {
+  const unsigned grid = (unsigned)cdiv(p.f, LC * Elt<T>::EL);
+  const int nr = (int)p.n;
+#define HG_FEW(NR_)                                                                                          \
+  HG_LAUNCH("few_rows", (k_few_rows<T, Epi, NR_, LC, ALIGNED>), dim3(grid), dim3(kFewWaves * 64), 0, s, X,   \
+            p.ld_x, W, p.d, p.f, nr, e)
+  if (nr == 1) {
+    HG_FEW(1);
+  } else if (nr == 2) {
+    HG_FEW(2);
+  } else if (nr <= 4) {
+    HG_FEW(4);
+  } else {
+    HG_FEW(8);
+  }
+#undef HG_FEW
+  return HG_OK;
+}
+
+// ---- tiles ----------------------------------------------------------------------------
+struct Tiling {
+  int tile;
+  int64_t tiles_m, tiles_n;
+  int splits;
+  int64_t k_split;
+};
+
+// Tiles of 128 x 128 where they fill half the chip, else 64 x 64; the k range
+// is split over blocks while the tiles do not fill it (never where column
+// sums are formed on the way).
+Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split) {
+  Tiling t{};
+  const int64_t big = cdiv(M, 128) * cdiv(cols, 128);
+  t.tile = big >= 128 || (may_split && big * (K / 512) >= 128) ? 128 : 64;
+  t.tiles_m = cdiv(M, t.tile);
+  t.tiles_n = cdiv(cols, t.tile);
+  const int64_t tiles = t.tiles_m * t.tiles_n;
+  int64_t splits = 1;
+  if (may_split && tiles < 256) splits = std::max<int64_t>(1, std::min(cdiv(512, tiles), K / 256));
+  t.k_split = cdiv(cdiv(std::max<int64_t>(K, 1), splits), 64) * 64;
+  t.splits = (int)std::max<int64_t>(1, cdiv(K, t.k_split));
+  return t;
+}
+
+int64_t part_elems(const Tiling& t, int64_t M, int64_t ld) { return t.splits > 1 ? t.splits * M * ld : 0; }
+
+template <class F, bool AKM, bool BKM, int TILE, class Epi, bool SPLIT>
+int launch_tiles(const char* name, const GArgs& a, const Tiling& t, hipStream_t s) {
+  constexpr int BK = F::P == 3 ? 32 : 64;
+  constexpr size_t lds = g_lds_bytes(F::P, TILE, TILE, BK);
+  auto kern = k_gemm16<F, AKM, BKM, TILE, TILE, BK, TILE / 2, TILE / 2, Epi, SPLIT>;
+  if (lds > 65536) {
+    static std::atomic<bool> attr_set{false};
+    if (!attr_set.load(std::memory_order_relaxed)) {
+      HG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)lds));
+      attr_set.store(true, std::memory_order_relaxed);
+    }
+  }
+  HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(256), lds, s, a);
+  return HG_OK;
+}
+
+// The split launch only forms products: one kernel for every epilogue of a form.
+template <bool GATED>
+struct EpiPart {
+  static constexpr bool kGated = GATED, kColSum = false;
+  __device__ static __forceinline__ void apply(const GEpi&, int64_t, int, int, float (&)[4]) {}
+  __device__ static __forceinline__ void apply(const GEpi&, int64_t, int, int, float (&)[4], float (&)[4]) {}
+};
+
+template <class F, bool AKM, bool BKM, class Epi>
+int launch_product(const char* name, GArgs a, const Tiling& t, float* part, int64_t ld_part, hipStream_t s) {
+  a.tiles_m = (int32_t)t.tiles_m;
+  a.tiles_n = (int32_t)t.tiles_n;
+  a.k_split = t.k_split;
+  if (t.splits == 1) {
+    if (t.tile == 128) return launch_tiles<F, AKM, BKM, 128, Epi, false>(name, a, t, s);
+    return launch_tiles<F, AKM, BKM, 64, Epi, false>(name, a, t, s);
+  }
+  if constexpr (!Epi::kColSum) {
+    typedef EpiPart<Epi::kGated> Part;
+    a.e.part = part;
+    a.e.ld_part = ld_part;
+    if (t.tile == 128) {
+      HG_TRY((launch_tiles<F, AKM, BKM, 128, Part, true>(name, a, t, s)));
+    } else {
+      HG_TRY((launch_tiles<F, AKM, BKM, 64, Part, true>(name, a, t, s)));
+    }
+    const int64_t quads = cdiv(Epi::kGated ? a.e.halfp : a.N, 4);
+    HG_LAUNCH("product_join", k_gemm16_join<Epi>, dim3((unsigned)cdiv(a.M * quads, 256)), dim3(256), 0, s, a, t.splits);
+  }
+  return HG_OK;
+}
+
+// ---- a call's buffers ---------------------------------------------------------------------
+// The same takes size the workspace and hand it out.
+struct Bufs {
+  uint16_t* x16 = nullptr;   // X padded (bf16) or its two fp16 planes (f32)
+  float* ua = nullptr;       // row factors of X
+  uint16_t* w16 = nullptr;   // W padded or its two fp16 planes
+  float* ub = nullptr;       // W's factor
+  float* wpart = nullptr;    // partial maxima of W
+  float* part = nullptr;     // split products
+  // backward
+  void* dz = nullptr;        // gradient of z in dtype, padded rows
+  uint16_t* dz16 = nullptr;  // its two fp16 planes
+  float* uz = nullptr;       // row factors of dz
+  uint16_t* x3 = nullptr;    // three bfloat16 planes of X and of dz
+  uint16_t* dz3 = nullptr;
+  float* colsum = nullptr;
+  int64_t colsum_rows = 0;
+};
+
+bool few(const Prob& p) { return p.n <= kFewRows; }
+Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true); }
+Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false); }
+Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true); }
+Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true); }
+bool x_direct(const Prob& p) { return direct(p.d, p.ld_x); }
+bool w_direct(const Prob& p) { return p.f % 8 == 0; }
+bool has_z(const Prob& p) { return p.gated || p.act != HG_ACT_NONE; }
+// the upstream rows are dz itself and can be read where they lie
+bool dz_direct(const Prob& p) { return !has_z(p) && !p.f32() && direct(p.f, p.ld_y); }
+
+template <class Mem>
+void take_operands(const Prob& p, bool z, Mem& m, Bufs& b) {
+  if (p.f32()) {
+    if (z) {
+      b.x16 = m.template take<uint16_t>(2 * p.n * p.dp());
+      b.ua = m.template take<float>(p.n);
+    }
+    b.w16 = m.template take<uint16_t>(2 * (int64_t)p.d * p.colsp());
+    b.ub = m.template take<float>(1);
+    b.wpart = m.template take<float>(kAbsBlocks);
+  } else {
+    if (!x_direct(p)) b.x16 = m.template take<uint16_t>(p.n * p.dp());
+    if (!w_direct(p)) b.w16 = m.template take<uint16_t>((int64_t)p.d * p.colsp());
+  }
+}
+
+template <class Mem>
+Bufs take_fwd(const Prob& p, Mem& m) {
+  Bufs b;
+  if (p.n == 0 || few(p)) return b;
+  take_operands(p, true, m, b);
+  b.part = m.template take<float>(part_elems(t_fwd(p), p.n, p.colsp()));
+  return b;
+}
+
+template <class Mem>
+Bufs take_bwd(const Prob& p, Mem& m) {
+  Bufs b;
+  if (p.n == 0) return b;
+  take_operands(p, has_z(p), m, b);
+  const int64_t nz = p.n * p.colsp();
+  if (p.f32()) {
+    if (has_z(p)) b.dz = m.template take<float>(nz);
+    b.dz16 = m.template take<uint16_t>(2 * nz);
+    b.uz = m.template take<float>(p.n);
+    b.x3 = m.template take<uint16_t>(3 * p.n * p.dp());
+    b.dz3 = m.template take<uint16_t>(3 * nz);
+  } else if (!dz_direct(p)) {
+    b.dz = m.template take<uint16_t>(nz);
+  }
+  b.colsum_rows = has_z(p) ? t_z(p).tiles_m : cdiv(p.n, kSumRows);
+  b.colsum = m.template take<float>(b.colsum_rows * p.cols());
+  b.part = m.template take<float>(std::max(part_elems(t_dx(p), p.n, p.dp()), part_elems(t_dw(p), p.d, p.colsp())));
+  return b;
+}
+
+// ---- checks -----------------------------------------------------------------------------------
+int check(const Prob& p, const char* what) {
+  if (p.n < 0 || p.d < 1 || p.f < 1) return fail(HG_ERR_ARG, "%s: sizes n=%lld, %d -> %d", what, (long long)p.n, p.d, p.f);
+  if (p.dtype != HG_DTYPE_F32 && p.dtype != HG_DTYPE_BF16) return fail(HG_ERR_ARG, "%s: dtype %d", what, p.dtype);
+  if (p.act < HG_ACT_NONE || p.act > HG_ACT_GELU) return fail(HG_ERR_ARG, "%s: act %d", what, p.act);
+  if (p.n >= (int64_t)1 << 31 || p.d > kMaxWidth || p.f > kMaxWidth)
+    return fail(HG_ERR_UNSUPPORTED, "%s: n=%lld, %d -> %d is too large", what, (long long)p.n, p.d, p.f);
+  // the launches' block counts
+  const int64_t most = ((int64_t)1 << 31) - 1;
+  if (cdiv(p.n, 64) * cdiv(std::max(p.colsp(), p.dp()), 64) > most / 4 || p.n * (int64_t)std::max(p.colsp(), p.dp()) / 4 / 256 > most / 4)
+    return fail(HG_ERR_UNSUPPORTED, "%s: n=%lld rows of %d -> %d are too many", what, (long long)p.n, p.d, p.f);
+  return HG_OK;
+}
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Whether [a, a + na) and [b, b + nb) share a byte.
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  if (!a || !b) return false;
+  const char *x = static_cast<const char*>(a), *y = static_cast<const char*>(b);
+  return x < y + nb && y < x + na;
+}
+
+int64_t span(const Prob& p, int64_t rows, int64_t width, int64_t ld) {
+  return rows > 0 ? ((rows - 1) * ld + width) * (p.f32() ? 4 : 2) : 0;
+}
+
+int check_rows(const Prob& p, const char* what, int64_t ld, int32_t width, const char* name) {
+  if (p.n > 0 && (ld < width || ld > (int64_t)1 << 40))
+    return fail(HG_ERR_ARG, "%s: rows of %s are %lld apart, %d wide", what, name, (long long)ld, width);
+  return HG_OK;
+}
+
+// ---- launches -----------------------------------------------------------------------------------
+int pad_rows(const void* src, int64_t ld, int64_t rows, RowShape rs, uint16_t* dst, hipStream_t s) {
+  HG_LAUNCH("rows_pad", k_rows_pad, dim3((unsigned)cdiv(rows * (rs.halves * rs.Fp / 8), 256)), dim3(256), 0, s,
+            static_cast<const uint16_t*>(src), ld, rows, rs, dst);
+  return HG_OK;
+}
+
+int split_rows(const void* src, int64_t ld, int64_t rows, RowShape rs, uint16_t* dst, float* ua, hipStream_t s) {
+  HG_LAUNCH("rows_split", k_rows_split, dim3((unsigned)cdiv(rows, 4)), dim3(256), 0, s, static_cast<const float*>(src),
+            ld, rows, rs, dst, rows * (int64_t)(rs.halves * rs.Fp), ua);
+  return HG_OK;
+}
+
+int split3_rows(const void* src, int64_t ld, int64_t rows, RowShape rs, uint16_t* dst, hipStream_t s) {
+  HG_LAUNCH("rows_split3", k_rows_split3, dim3((unsigned)cdiv(rows * (rs.halves * rs.Fp / 8), 256)), dim3(256), 0, s,
+            static_cast<const float*>(src), ld, rows, rs, dst, rows * (int64_t)(rs.halves * rs.Fp));
+  return HG_OK;
+}
+
+RowShape x_shape(const Prob& p) { return RowShape{p.d, p.dp(), 1}; }
+RowShape w_shape(const Prob& p) { return RowShape{p.f, p.fp(), p.halves()}; }
+// dz as the gradient epilogues write it: padded already
+RowShape dz_shape(const Prob& p) { return RowShape{p.fp(), p.fp(), p.halves()}; }
+
+// X as rows of k (bfloat16, or fp16 planes) and W, which serves as k rows and as rows of k.
+int operands(const Prob& p, const void* X, const void* W, bool z, const Bufs& b, GOperand& x, GOperand& w, hipStream_t s) {
+  const int64_t wn = (int64_t)p.d * p.colsp();
+  if (p.f32()) {
+    if (z) HG_TRY(split_rows(X, p.ld_x, p.n, x_shape(p), b.x16, b.ua, s));
+    const int64_t total = (int64_t)p.d * p.cols();
+    const int parts = (int)std::min<int64_t>(kAbsBlocks, cdiv(total, 1024));
+    HG_LAUNCH("absmax", k_absmax, dim3(parts), dim3(256), 0, s, static_cast<const float*>(W), total, b.wpart);
+    HG_LAUNCH("matrix_split", k_matrix_split, dim3((unsigned)std::min<int64_t>(2048, cdiv(wn / 8, 256))), dim3(256), 0, s,
+              static_cast<const float*>(W), (int64_t)p.d, w_shape(p), b.wpart, parts, b.w16, wn, b.ub);
+    x = GOperand{b.x16, p.dp(), p.n * p.dp(), p.n, p.dp()};
+    w = GOperand{b.w16, p.colsp(), wn, p.d, p.colsp()};
+    return HG_OK;
+  }
+  x = GOperand{static_cast<const uint16_t*>(X), p.ld_x, 0, p.n, p.dp()};
+  if (!x_direct(p)) {
+    HG_TRY(pad_rows(X, p.ld_x, p.n, x_shape(p), b.x16, s));
+    x.p = b.x16;
+    x.ld = p.dp();
+  }
+  w = GOperand{static_cast<const uint16_t*>(W), p.colsp(), 0, p.d, p.colsp()};
+  if (!w_direct(p)) {
+    HG_TRY(pad_rows(W, p.cols(), p.d, w_shape(p), b.w16, s));
+    w.p = b.w16;
+  }
+  return HG_OK;
+}
+
+GEpi epi_of(const Prob& p, const float* bias, const void* res, int64_t ld_res, void* out, int64_t ld_out) {
+  GEpi e{};
+  e.bias = bias;
+  e.res = res;
+  e.ld_res = ld_res;
+  e.out = out;
+  e.ld_out = ld_out;
+  e.act = p.act;
+  e.ncol = p.f;
+  e.half = p.f;
+  e.halfp = p.fp();
+  e.outp = p.fp();
+  return e;
+}
+
+template <class T, class F, bool GATED>
+int fwd_impl(const Prob& p, const void* X, const void* W, const float* bias, const void* R, void* Y, const Bufs& b,
+             hipStream_t s) {
+  typedef typename std::conditional<GATED, EpiGated<T>, EpiLinear<T>>::type Epi;
+  GArgs a{};
+  a.e = epi_of(p, bias, R, p.ld_r, Y, p.ld_y);
+  if (few(p)) {
+    constexpr int LC = 4;
+    constexpr int V = Elt<T>::EL;
+    const bool al = p.f % V == 0 && p.d % V == 0 && p.ld_x % V == 0;
+    const T *x = static_cast<const T*>(X), *w = static_cast<const T*>(W);
+    return al ? launch_few<T, Epi, LC, true>(p, x, w, a.e, s) : launch_few<T, Epi, LC, false>(p, x, w, a.e, s);
+  }
+  HG_TRY(operands(p, X, W, true, b, a.a, a.b, s));
+  a.M = p.n;
+  a.N = p.colsp();
+  a.K = p.dp();
+  a.e.ua = b.ua;
+  a.e.ub = b.ub;
+  return launch_product<F, true, false, Epi>(GATED ? "glu" : "linear", a, t_fwd(p), b.part, p.colsp(), s);
+}
+
+template <class T, class FR, class FT, bool GATED>
+int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, const void* dY, void* dX, int64_t ld_dx,
+             void* dW, float* dbias, int accumulate, const Bufs& b, hipStream_t s) {
+  typedef typename std::conditional<GATED, EpiGatedGrad<T>, EpiLinearGrad<T>>::type EpiG;
+  constexpr bool kF32 = sizeof(T) == 4;
+  GOperand x{}, w{};
+  HG_TRY(operands(p, X, W, has_z(p), b, x, w, s));
+  // dz, in rows of colsp (or where the upstream rows lie)
+  const void* dz = dY;
+  int64_t ld_dz = p.ld_y;
+  RowShape zs = w_shape(p);
+  if (has_z(p)) {
+    GArgs a{};
+    a.a = x;
+    a.b = w;
+    a.M = p.n;
+    a.N = p.colsp();
+    a.K = p.dp();
+    a.e = epi_of(p, bias, dY, p.ld_y, b.dz, p.colsp());
+    a.e.ua = b.ua;
+    a.e.ub = b.ub;
+    a.e.colsum = dbias ? b.colsum : nullptr;
+    a.e.ld_colsum = p.cols();
+    HG_TRY((launch_product<FR, true, false, EpiG>(GATED ? "glu_dz" : "linear_dz", a, t_z(p), nullptr, 0, s)));
+    dz = b.dz;
+    ld_dz = p.colsp();
+    zs = dz_shape(p);
+  } else if (dbias) {
+    HG_LAUNCH("colsum", k_colsum<T>, dim3((unsigned)b.colsum_rows, (unsigned)cdiv(p.cols(), 64)), dim3(256), 0, s, dY,
+              p.ld_y, p.n, p.cols(), b.colsum);
+  }
+  if (dbias)
+    HG_LAUNCH("colsum_join", k_colsum_join, dim3((unsigned)cdiv(p.cols(), 16)), dim3(256), 0, s, b.colsum, b.colsum_rows,
+              p.cols(), dbias, accumulate);
+  GOperand z{static_cast<const uint16_t*>(dz), ld_dz, 0, p.n, p.colsp()};
+  if (!kF32 && !has_z(p) && !dz_direct(p)) {
+    uint16_t* out = static_cast<uint16_t*>(b.dz);
+    HG_TRY(pad_rows(dY, p.ld_y, p.n, zs, out, s));
+    z.p = out;
+    z.ld = p.colsp();
+  }
+  if (dX) {
+    GArgs a{};
+    a.a = z;
+    a.b = w;
+    if constexpr (kF32) {
+      HG_TRY(split_rows(dz, ld_dz, p.n, zs, b.dz16, b.uz, s));
+      a.a = GOperand{b.dz16, p.colsp(), p.n * p.colsp(), p.n, p.colsp()};
+    }
+    a.M = p.n;
+    a.N = p.d;
+    a.K = p.colsp();
+    a.e.ua = b.uz;
+    a.e.ub = b.ub;
+    a.e.out = dX;
+    a.e.ld_out = ld_dx;
+    a.e.ncol = p.d;
+    HG_TRY((launch_product<FR, true, true, EpiSum<T>>(GATED ? "glu_dx" : "linear_dx", a, t_dx(p), b.part, p.dp(), s)));
+  }
+  if (dW) {
+    GArgs a{};
+    a.a = x;
+    a.b = z;
+    if constexpr (kF32) {
+      HG_TRY(split3_rows(X, p.ld_x, p.n, x_shape(p), b.x3, s));
+      HG_TRY(split3_rows(dz, ld_dz, p.n, zs, b.dz3, s));
+      a.a = GOperand{b.x3, p.dp(), p.n * p.dp(), p.n, p.dp()};
+      a.b = GOperand{b.dz3, p.colsp(), p.n * p.colsp(), p.n, p.colsp()};
+    }
+    a.M = p.d;
+    a.N = p.colsp();
+    a.K = p.n;
+    a.e.out = dW;
+    a.e.ld_out = p.cols();
+    a.e.ncol = p.cols();
+    if (GATED && p.f != p.fp()) {
+      a.e.half = p.f;
+      a.e.halfp = p.fp();
+    }
+    a.e.accumulate = accumulate;
+    HG_TRY((launch_product<FT, false, false, EpiSum<T>>(GATED ? "glu_dw" : "linear_dw", a, t_dw(p), b.part, p.colsp(), s)));
+  }
+  return HG_OK;
+}
+
+__global__ void __launch_bounds__(256) k_zero16(uint16_t* __restrict__ p, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i] = 0;
+}
+
+// Gradients of a call without rows: zero (added: nothing changes).
+int empty_grads(const Prob& p, void* dW, float* dbias, int accumulate, hipStream_t s) {
+  if (accumulate) return HG_OK;
+  const int64_t n = (int64_t)p.d * p.cols();
+  if (dW) {
+    if (p.f32()) {
+      HG_TRY(fill_f32(static_cast<float*>(dW), 0.f, n, s));
+    } else {
+      HG_LAUNCH("zero16", k_zero16, dim3((unsigned)std::min<int64_t>(2048, cdiv(n, 256))), dim3(256), 0, s,
+                static_cast<uint16_t*>(dW), n);
+    }
+  }
+  if (dbias) HG_TRY(fill_f32(dbias, 0.f, p.cols(), s));
+  return HG_OK;
+}
+
+int forward(const Prob& p, const char* what, const void* X, const void* W, const float* bias, const void* R, void* Y,
+            void* ws, size_t ws_bytes, hipStream_t s) {
+  HG_TRY(check(p, what));
+  HG_TRY(check_rows(p, what, p.ld_x, p.d, "X"));
+  HG_TRY(check_rows(p, what, p.ld_y, p.f, "the output"));
+  if (R) HG_TRY(check_rows(p, what, p.ld_r, p.f, "R"));
+  if (p.n == 0) return HG_OK;
+  if (!X || !W || !Y) return fail(HG_ERR_ARG, "%s: null pointer", what);
+  if (!aligned16(X) || !aligned16(W)) return fail(HG_ERR_ARG, "%s: X and W must be 16-byte aligned", what);
+  const int64_t ny = span(p, p.n, p.f, p.ld_y);
+  if (overlap(Y, ny, X, span(p, p.n, p.d, p.ld_x)) || overlap(Y, ny, W, span(p, p.d, p.cols(), p.cols())) ||
+      (R != Y && overlap(Y, ny, R, span(p, p.n, p.f, p.ld_r))) || (R == Y && p.ld_r != p.ld_y))
+    return fail(HG_ERR_ARG, "%s: the output overlaps an input", what);
+  Sizer need;
+  take_fwd(p, need);
+  if (ws_bytes < need.used || (need.used && !ws))
+    return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  Arena m(ws, ws_bytes);
+  const Bufs b = take_fwd(p, m);
+  if (p.f32())
+    return p.gated ? fwd_impl<float, GF16x2, true>(p, X, W, bias, R, Y, b, s)
+                   : fwd_impl<float, GF16x2, false>(p, X, W, bias, R, Y, b, s);
+  return p.gated ? fwd_impl<bf16_t, GBf16, true>(p, X, W, bias, R, Y, b, s)
+                 : fwd_impl<bf16_t, GBf16, false>(p, X, W, bias, R, Y, b, s);
+}
+
+int backward(const Prob& p, const char* what, const void* X, const void* W, const float* bias, const void* dY, void* dX,
+             void* dW, float* dbias, int accumulate, void* ws, size_t ws_bytes, hipStream_t s) {
+  HG_TRY(check(p, what));
+  if (accumulate != 0 && accumulate != 1) return fail(HG_ERR_ARG, "%s: accumulate %d", what, accumulate);
+  HG_TRY(check_rows(p, what, p.ld_x, p.d, "X"));
+  HG_TRY(check_rows(p, what, p.ld_y, p.f, "the upstream gradient"));
+  if (dX) HG_TRY(check_rows(p, what, p.ld_r, p.d, "dX"));
+  if (p.n == 0) return empty_grads(p, dW, dbias, accumulate, s);
+  if (!X || !W || !dY) return fail(HG_ERR_ARG, "%s: null pointer", what);
+  if (!aligned16(X) || !aligned16(W) || !aligned16(dY))
+    return fail(HG_ERR_ARG, "%s: X, W and the upstream gradient must be 16-byte aligned", what);
+  const int64_t nx = span(p, p.n, p.d, p.ld_x), nw = span(p, p.d, p.cols(), p.cols()), ny = span(p, p.n, p.f, p.ld_y);
+  const int64_t ndx = span(p, p.n, p.d, p.ld_r), nb = 4 * (int64_t)p.cols();
+  const struct {
+    const void* p;
+    int64_t n;
+  } out[3] = {{dX, ndx}, {dW, nw}, {dbias, nb}};
+  for (int i = 0; i < 3; ++i) {
+    if (overlap(out[i].p, out[i].n, X, nx) || overlap(out[i].p, out[i].n, W, nw) || overlap(out[i].p, out[i].n, dY, ny) ||
+        overlap(out[i].p, out[i].n, bias, nb))
+      return fail(HG_ERR_ARG, "%s: a gradient overlaps an input", what);
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].n, out[j].p, out[j].n)) return fail(HG_ERR_ARG, "%s: two gradients overlap", what);
+  }
+  Sizer need;
+  take_bwd(p, need);
+  if (ws_bytes < need.used || (need.used && !ws))
+    return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  Arena m(ws, ws_bytes);
+  const Bufs b = take_bwd(p, m);
+  if (p.f32())
+    return p.gated ? bwd_impl<float, GF16x2, GBf16x3, true>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s)
+                   : bwd_impl<float, GF16x2, GBf16x3, false>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s);
+  return p.gated ? bwd_impl<bf16_t, GBf16, GBf16, true>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s)
+                 : bwd_impl<bf16_t, GBf16, GBf16, false>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s);
+}
+
+Prob prob_of(const hg_linear_desc* L) {
+  return Prob{L->n, L->d_in, L->d_out, L->dtype, L->act, false, L->ld_x, L->ld_y, L->ld_r};
+}
+Prob prob_of(const hg_glu_desc* L) { return Prob{L->n, L->d, L->f, L->dtype, L->act, true, L->ld_x, L->ld_h, L->ld_dx}; }
+
+template <class D>
+size_t size_of(const D* L, bool bwd) {
+  if (!L) return 0;
+  const Prob p = prob_of(L);
+  if (check(p, "workspace size") != HG_OK) return 0;
+  Sizer m;
+  if (bwd) {
+    take_bwd(p, m);
+  } else {
+    take_fwd(p, m);
+  }
+  return m.used;
+}
+
+}  // namespace
+}  // namespace hg
+
+using namespace hg;
+
+extern "C" size_t hg_linear_fwd_workspace_size(const hg_linear_desc* L) { return size_of(L, false); }
+extern "C" size_t hg_linear_bwd_workspace_size(const hg_linear_desc* L) { return size_of(L, true); }
+extern "C" size_t hg_glu_fwd_workspace_size(const hg_glu_desc* L) { return size_of(L, false); }
+extern "C" size_t hg_glu_bwd_workspace_size(const hg_glu_desc* L) { return size_of(L, true); }
+
+extern "C" int hg_linear_fwd(const hg_linear_desc* L, const void* X, const void* W, const float* bias, const void* R,
+                             void* Y, void* ws, size_t ws_bytes, void* stream) {
+  if (!L) return fail(HG_ERR_ARG, "hg_linear_fwd: null descriptor");
+  return forward(prob_of(L), "hg_linear_fwd", X, W, bias, R, Y, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int hg_linear_bwd(const hg_linear_desc* L, const void* X, const void* W, const float* bias, const void* dY,
+                             void* dX, void* dW, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes,
+                             void* stream) {
+  if (!L) return fail(HG_ERR_ARG, "hg_linear_bwd: null descriptor");
+  return backward(prob_of(L), "hg_linear_bwd", X, W, bias, dY, dX, dW, dbias, accumulate, ws, ws_bytes,
+                  static_cast<hipStream_t>(stream));
+}
+
+extern "C" int hg_glu_fwd(const hg_glu_desc* L, const void* X, const void* W, const float* bias, void* H, void* ws,
+                          size_t ws_bytes, void* stream) {
+  if (!L) return fail(HG_ERR_ARG, "hg_glu_fwd: null descriptor");
+  return forward(prob_of(L), "hg_glu_fwd", X, W, bias, nullptr, H, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int hg_glu_bwd(const hg_glu_desc* L, const void* X, const void* W, const float* bias, const void* dH, void* dX,
+                          void* dW, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  if (!L) return fail(HG_ERR_ARG, "hg_glu_bwd: null descriptor");
+  return backward(prob_of(L), "hg_glu_bwd", X, W, bias, dH, dX, dW, dbias, accumulate, ws, ws_bytes,
+                  static_cast<hipStream_t>(stream));
+}

@@ -580,6 +580,104 @@ int hg_glu_fwd(const hg_glu_desc* L, const void* X, const void* W, const float* 
 int hg_glu_bwd(const hg_glu_desc* L, const void* X, const void* W, const float* bias, const void* dH, void* dX,
                void* dW, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
 
+/* Rows of heads: element (sequence b, token t, head h, column x) lies at
+ * p[b * batch + t * token + h * head + x] (strides in elements, so heads of a
+ * packed projection are used where they lie).  Addresses and strides are
+ * multiples of 16 bytes. */
+typedef struct hg_heads {
+  void* p;
+  int64_t batch, token, head;
+} hg_heads;
+
+/* Norm of queries and keys for each head, with the position rotation in the
+ * same pass.  Per row x of width d (one head of one token):
+ *   y = x w / sqrt(mean(x^2) + eps)
+ * then the pairs (i, j) of the first rot columns turned by the angle of the
+ * token's position: (y_i cos - y_j sin, y_j cos + y_i sin); pair p is columns
+ * (2 p, 2 p + 1) when interleaved, else (p, p + rot / 2).
+ * q, k: hg_heads with heads and kv_heads heads (batch strides not used;
+ * kv_heads = 0: queries alone); wq, wk float32 [d] (NULL = 1), 16-byte aligned;
+ * pos int32 [n]; table float32 [n_pos, rot], the cosines of a position's rot / 2
+ * pairs, then the sines (hg_rope_table writes one; rot = 0: no rotation, pos
+ * still is given).  A token whose position is outside [0, n_pos) gets NaN rows.
+ * The outputs may be the inputs themselves (same address and strides).
+ * d and rot are multiples of 8, d at most 256.  Norms, rotation and sums are
+ * float32, rounded once.  Asynchronous. */
+typedef struct hg_rope_desc {
+  int64_t n;          /* tokens */
+  int64_t n_pos;      /* rows of the table */
+  int32_t heads, kv_heads, d, rot;
+  int32_t interleaved; /* 0 or 1 */
+  int32_t dtype;      /* of the rows */
+  float eps;          /* >= 0 */
+  int32_t reserved;
+} hg_rope_desc;
+/* Table of n_pos positions: angle = position * step * base^(-2 p / rot), formed
+ * in float64 (step: the time unit of a position). */
+int hg_rope_table(int64_t n_pos, int32_t rot, double base, double step, float* table, void* stream);
+int hg_qk_norm_rope_fwd(const hg_rope_desc* D, const hg_heads* q, const hg_heads* k, const float* wq,
+                        const float* wk, const float* table, const int32_t* pos, const hg_heads* q_out,
+                        const hg_heads* k_out, void* stream);
+/* Backward for the upstream rows dq_out, dk_out (x = q, k as the forward read
+ * them; the norms are formed again): dq, dk are OVERWRITTEN (they may be dq_out,
+ * dk_out themselves); dwq, dwk float32 [d] (each may be NULL) are OVERWRITTEN
+ * when accumulate = 0 and added into when accumulate = 1.  Deterministic. */
+size_t hg_qk_norm_rope_bwd_workspace_size(const hg_rope_desc* D);
+int hg_qk_norm_rope_bwd(const hg_rope_desc* D, const hg_heads* q, const hg_heads* k, const float* wq,
+                        const float* wk, const float* table, const int32_t* pos, const hg_heads* dq_out,
+                        const hg_heads* dk_out, const hg_heads* dq, const hg_heads* dk, float* dwq, float* dwk,
+                        int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* Linear attention with a decay for each head: per sequence and query head h,
+ * with l = exp(log_decay[h]), token by token
+ *   S_t = l S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t
+ * S_{-1} = state (zero if NULL), state_out = the state after the last token (may
+ * be NULL).  q and o have `heads` heads, k and v kv_heads (heads a multiple of
+ * it): query head h uses key head h / (heads / kv_heads).  States are float32
+ * [batch, heads, d, d] (row: column of k, column: column of v), contiguous;
+ * log_decay float32 [heads], at most 0 for a decay (a -infinity forgets all).
+ * lens (may be NULL): int32 [batch] on the device, tokens of each sequence,
+ * taken into [0, t]; rows of o (and of the gradients) past it are written as
+ * zero and the rows of q, k, v and dO past it are not read.
+ * d is a multiple of 8 up to 128.  Outputs must not overlap inputs or each
+ * other; heads of one packed buffer may interleave.
+ * Sums, states and decays are float32; a bfloat16 call holds the weighted
+ * products of a chunk and the copy of the state that multiplies a row to 16
+ * bits, adds k^T v to the state to float32 accuracy and rounds o once.  A k or v
+ * that is not finite reaches every later output of its heads, and one of v may
+ * reach those of up to 15 tokens before it.
+ * Deterministic.  Asynchronous. */
+typedef struct hg_linattn_desc {
+  int64_t t;          /* tokens of a sequence */
+  int32_t batch, heads, kv_heads, d;
+  int32_t dtype;      /* of q, k, v, o and their gradients */
+  float scale;
+} hg_linattn_desc;
+size_t hg_linattn_fwd_workspace_size(const hg_linattn_desc* A);
+size_t hg_linattn_bwd_workspace_size(const hg_linattn_desc* A);
+int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
+                   const float* log_decay, const int32_t* lens, const float* state, const hg_heads* o,
+                   float* state_out, void* ws, size_t ws_bytes, void* stream);
+/* Backward of hg_linattn_fwd for dO = dL/do and dstate_out = dL/dstate_out (zero
+ * if NULL); nothing is kept between the calls.  dq, dk and dv are OVERWRITTEN,
+ * as is dstate = dL/dstate (may be NULL).  With R_t the gradient of S_t,
+ *   R_t = l R_{t+1} + scale q_t^T dO_t  (plus dstate_out at the last token),
+ *   dq_t = scale S_t dO_t,  dk_t = R_t v_t,  dv_t = k_t R_t,  dstate = l R_0;
+ * dk and dv sum over the query heads of a key head.  The decays are constants
+ * of the model: they get no gradient. */
+int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
+                   const float* log_decay, const int32_t* lens, const float* state, const hg_heads* dO,
+                   const float* dstate_out, const hg_heads* dq, const hg_heads* dk, const hg_heads* dv,
+                   float* dstate, void* ws, size_t ws_bytes, void* stream);
+/* One token for each of `batch` rows (A->t = 1; the token strides are not used):
+ * the state of row b is states[slots[b]] of n_slots states [heads, d, d]
+ * (slots NULL: b), UPDATED IN PLACE; the slots of a call are distinct.  A row
+ * whose slot is outside [0, n_slots) gives a zero row of o and changes nothing
+ * (an idle place of a serving batch). */
+int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
+                    const float* log_decay, float* states, const int32_t* slots, int64_t n_slots,
+                    const hg_heads* o, void* stream);
+
 /* ---- diagnostics ------------------------------------------------------- */
 const char* hg_status_string(int status);
 /* Thread-local description of the last error (host memory, valid until the

@@ -48,6 +48,9 @@ EXPORTS = [
     "hg_mean_agg_fwd", "hg_mean_agg_bwd", "hg_home_gather",
     "hg_linear_fwd_workspace_size", "hg_linear_bwd_workspace_size", "hg_linear_fwd", "hg_linear_bwd",
     "hg_glu_fwd_workspace_size", "hg_glu_bwd_workspace_size", "hg_glu_fwd", "hg_glu_bwd",
+    "hg_rope_table", "hg_qk_norm_rope_fwd", "hg_qk_norm_rope_bwd_workspace_size", "hg_qk_norm_rope_bwd",
+    "hg_linattn_fwd_workspace_size", "hg_linattn_bwd_workspace_size", "hg_linattn_fwd", "hg_linattn_bwd",
+    "hg_linattn_step",
     "hg_status_string", "hg_last_error_detail", "hg_timing_enable", "hg_timing_collect",
 ]
 
@@ -121,6 +124,21 @@ class GluDesc(C.Structure):
                 ("ld_x", C.c_int64), ("ld_h", C.c_int64), ("ld_dx", C.c_int64)]
 
 
+class Heads(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("batch", C.c_int64), ("token", C.c_int64), ("head", C.c_int64)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("n", C.c_int64), ("n_pos", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("d", C.c_int32), ("rot", C.c_int32), ("interleaved", C.c_int32), ("dtype", C.c_int32),
+                ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class LinattnDesc(C.Structure):
+    _fields_ = [("t", C.c_int64), ("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("d", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
 _lib = None
 
 
@@ -173,6 +191,15 @@ def lib() -> C.CDLL:
         "hg_glu_bwd_workspace_size": (sz, [vp]),
         "hg_glu_fwd": (C.c_int, [vp] * 6 + [sz, vp]),
         "hg_glu_bwd": (C.c_int, [vp] * 8 + [i32, vp, sz, vp]),
+        "hg_rope_table": (C.c_int, [i64, i32, C.c_double, C.c_double, vp, vp]),
+        "hg_qk_norm_rope_fwd": (C.c_int, [vp] * 10),
+        "hg_qk_norm_rope_bwd_workspace_size": (sz, [vp]),
+        "hg_qk_norm_rope_bwd": (C.c_int, [vp] * 13 + [i32, vp, sz, vp]),
+        "hg_linattn_fwd_workspace_size": (sz, [vp]),
+        "hg_linattn_bwd_workspace_size": (sz, [vp]),
+        "hg_linattn_fwd": (C.c_int, [vp] * 10 + [sz, vp]),
+        "hg_linattn_bwd": (C.c_int, [vp] * 14 + [sz, vp]),
+        "hg_linattn_step": (C.c_int, [vp] * 7 + [i64, vp, vp]),
         "hg_status_string": (C.c_char_p, [C.c_int]),
         "hg_last_error_detail": (C.c_char_p, []),
         "hg_timing_enable": (C.c_int, [C.c_int]),
@@ -822,6 +849,197 @@ def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=N
     _check(L.hg_glu_bwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(dh), _ptr(dx), _ptr(dW), _ptr(dbias),
                         int(bool(accumulate)), wp, wn, _stream(stream)), where)
     return dx, dW, dbias
+
+
+def _stride(t, i: int, unit: int) -> int:
+    """Stride of a dimension; one of a single entry is never walked."""
+    return t.stride(i) if t.shape[i] > 1 else unit
+
+
+def _heads(where: str, name: str, t, shape):
+    """hg_heads of a [tokens, heads, d] or [batch, tokens, heads, d] tensor
+    (or [batch, heads, d] with the token dimension left out of the shape)."""
+    if tuple(t.shape) != tuple(shape) or (shape[-1] > 1 and t.numel() and t.stride(-1) != 1):
+        raise ValueError(f"{where}: expected {name} {tuple(shape)} with unit stride in a head, got {tuple(t.shape)} "
+                         f"strides {t.stride()}")
+    s = [_stride(t, i, 0) for i in range(t.dim() - 1)]
+    return Heads(t.data_ptr() if t.numel() else None, s[0] if len(s) == 3 else 0, s[-2], s[-1])
+
+
+def hg_rope_table(n_pos: int, rot: int, base: float = 10000.0, step: float = 1.0, table=None, device="cuda",
+                  stream=None):
+    """Cosines and sines [n_pos, rot] of position * step * base^(-2 p / rot)."""
+    if table is None:
+        table = torch.empty((n_pos, rot), dtype=torch.float32, device=device)
+    elif tuple(table.shape) != (n_pos, rot) or table.dtype != torch.float32 or not table.is_contiguous():
+        raise ValueError(f"hg_rope_table: expected a contiguous float32 [{n_pos}, {rot}], got {tuple(table.shape)}")
+    _check(lib().hg_rope_table(n_pos, rot, base, step, _ptr(table), _stream(stream)), "hg_rope_table")
+    return table
+
+
+def _rope_desc(where, q, k, wq, wk, table, pos, eps, interleaved):
+    n, hq, d = q.shape
+    _same(where, q, k)
+    _vector(where, wq, d, q.device)
+    _vector(where, wk, d, q.device)
+    _vector(where, pos, n, q.device, torch.int32)
+    if table.dim() != 2 or table.dtype != torch.float32 or table.device != q.device or not table.is_contiguous():
+        raise ValueError(f"{where}: expected a contiguous float32 table [positions, rot], got {tuple(table.shape)}")
+    hk = 0 if k is None else int(k.shape[1])
+    return RopeDesc(n, table.shape[0], hq, hk, d, table.shape[1], int(bool(interleaved)), _float_code(where, q),
+                    eps, 0), (n, hq, d), (n, hk, d)
+
+
+def hg_qk_norm_rope_fwd(q, k, wq, wk, table, pos, eps: float = 1e-6, interleaved: bool = False, q_out=None,
+                        k_out=None, stream=None):
+    """Per-head norm and position rotation: q [n, heads, d], k [n, kv_heads, d]
+    or None (views of a packed projection are used where they lie), wq, wk
+    float32 [d] or None, table [positions, rot] from hg_rope_table, pos int32
+    [n].  Returns (q_out, k_out); they may be q and k themselves."""
+    where = "hg_qk_norm_rope_fwd"
+    desc, qs, ks = _rope_desc(where, q, k, wq, wk, table, pos, eps, interleaved)
+    if q_out is None:
+        q_out = torch.empty(qs, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(ks, dtype=q.dtype, device=q.device)
+    _same(where, q, q_out, k_out)
+    hq, ho = _heads(where, "q", q, qs), _heads(where, "q_out", q_out, qs)
+    hk, hl = (None, None) if k is None else (_heads(where, "k", k, ks), _heads(where, "k_out", k_out, ks))
+    ref = C.byref
+    _check(lib().hg_qk_norm_rope_fwd(ref(desc), ref(hq), hk and ref(hk), _ptr(wq), _ptr(wk), _ptr(table), _ptr(pos),
+                                     ref(ho), hl and ref(hl), _stream(stream)), where)
+    return q_out, k_out
+
+
+def hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps: float = 1e-6, interleaved: bool = False,
+                        dq=None, dk=None, dwq=None, dwk=None, accumulate: bool = False, ws=None, stream=None):
+    """Returns (dq, dk, dwq, dwk) of hg_qk_norm_rope_fwd (q and k as it read
+    them); dwq and dwk for the weights given, added into when accumulate."""
+    where = "hg_qk_norm_rope_bwd"
+    L = lib()
+    desc, qs, ks = _rope_desc(where, q, k, wq, wk, table, pos, eps, interleaved)
+    if accumulate and ((wq is not None and dwq is None) or (wk is not None and dwk is None)):
+        raise ValueError(f"{where}: accumulate needs the buffers to add into")
+    if dq is None:
+        dq = torch.empty(qs, dtype=q.dtype, device=q.device)
+    if k is not None and dk is None:
+        dk = torch.empty(ks, dtype=q.dtype, device=q.device)
+    if dwq is None and wq is not None:
+        dwq = torch.empty_like(wq)
+    if dwk is None and wk is not None:
+        dwk = torch.empty_like(wk)
+    _vector(where, dwq, qs[2], q.device)
+    _vector(where, dwk, qs[2], q.device)
+    _same(where, q, dq_out, dk_out, dq, dk)
+    h = [_heads(where, n, t, s) for n, t, s in (("q", q, qs), ("dq_out", dq_out, qs), ("dq", dq, qs))]
+    g = [None if k is None else _heads(where, n, t, ks) for n, t in (("k", k), ("dk_out", dk_out), ("dk", dk))]
+    ref = C.byref
+    rh, rg = [ref(x) for x in h], [x and ref(x) for x in g]
+    wp, wn = _ws_for(ws, L.hg_qk_norm_rope_bwd_workspace_size(ref(desc)), q.device)
+    _check(L.hg_qk_norm_rope_bwd(ref(desc), rh[0], rg[0], _ptr(wq), _ptr(wk), _ptr(table), _ptr(pos), rh[1], rg[1],
+                                 rh[2], rg[2], _ptr(dwq), _ptr(dwk), int(bool(accumulate)), wp, wn, _stream(stream)),
+           where)
+    return dq, dk, dwq, dwk
+
+
+def _linattn_desc(where, q, k, v, log_decay, scale, lens, states) -> LinattnDesc:
+    b, t, h, d = q.shape
+    _same(where, q, k, v)
+    _vector(where, log_decay, h, q.device)
+    _vector(where, lens, b, q.device, torch.int32)
+    for s in states:
+        if s is not None and (tuple(s.shape) != (b, h, d, d) or s.dtype != torch.float32 or s.device != q.device
+                              or not s.is_contiguous()):
+            raise ValueError(f"{where}: expected a contiguous float32 state [{b}, {h}, {d}, {d}], got "
+                             f"{tuple(s.shape)} {s.dtype}")
+    return LinattnDesc(t, b, h, k.shape[2], d, _float_code(where, q), scale)
+
+
+def hg_linattn_fwd_workspace_size(batch: int, t: int, heads: int, kv_heads: int, d: int, dtype=torch.float32) -> int:
+    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
+    return int(lib().hg_linattn_fwd_workspace_size(C.byref(LinattnDesc(t, batch, heads, kv_heads, d, code, 1.0))))
+
+
+def hg_linattn_bwd_workspace_size(batch: int, t: int, heads: int, kv_heads: int, d: int, dtype=torch.float32) -> int:
+    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
+    return int(lib().hg_linattn_bwd_workspace_size(C.byref(LinattnDesc(t, batch, heads, kv_heads, d, code, 1.0))))
+
+
+def hg_linattn_fwd(q, k, v, log_decay, scale: float = 1.0, lens=None, state=None, o=None, state_out=None,
+                   want_state: bool = False, ws=None, stream=None):
+    """Linear attention with a decay for each head: q [b, t, heads, d], k, v
+    [b, t, kv_heads, d], log_decay float32 [heads], lens int32 [b] or None,
+    state float32 [b, heads, d, d] or None.  Returns (o, state_out); state_out
+    is None unless given or wanted."""
+    where = "hg_linattn_fwd"
+    L = lib()
+    b, t, h, d = q.shape
+    if state_out is None and want_state:
+        state_out = torch.empty((b, h, d, d), dtype=torch.float32, device=q.device)
+    desc = _linattn_desc(where, q, k, v, log_decay, scale, lens, (state, state_out))
+    if o is None:
+        o = torch.empty((b, t, h, d), dtype=q.dtype, device=q.device)
+    _same(where, q, o)
+    kv = (b, t, k.shape[2], d)
+    hq, hk, hv, ho = (_heads(where, n, x, s) for n, x, s in (("q", q, q.shape), ("k", k, kv), ("v", v, kv),
+                                                              ("o", o, q.shape)))
+    ref = C.byref
+    wp, wn = _ws_for(ws, L.hg_linattn_fwd_workspace_size(ref(desc)), q.device)
+    _check(L.hg_linattn_fwd(ref(desc), ref(hq), ref(hk), ref(hv), _ptr(log_decay), _ptr(lens), _ptr(state), ref(ho),
+                            _ptr(state_out), wp, wn, _stream(stream)), where)
+    return o, state_out
+
+
+def hg_linattn_bwd(q, k, v, log_decay, do, scale: float = 1.0, lens=None, state=None, dstate_out=None, dq=None,
+                   dk=None, dv=None, dstate=None, ws=None, stream=None):
+    """Returns (dq, dk, dv, dstate) of hg_linattn_fwd for do = dL/do and
+    dstate_out = dL/dstate_out (or None); dstate is None unless a state or a
+    buffer is given."""
+    where = "hg_linattn_bwd"
+    L = lib()
+    b, t, h, d = q.shape
+    if dstate is None and state is not None:
+        dstate = torch.empty((b, h, d, d), dtype=torch.float32, device=q.device)
+    desc = _linattn_desc(where, q, k, v, log_decay, scale, lens, (state, dstate_out, dstate))
+    kv = (b, t, k.shape[2], d)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(kv, dtype=q.dtype, device=q.device) if dk is None else dk
+    dv = torch.empty(kv, dtype=q.dtype, device=q.device) if dv is None else dv
+    _same(where, q, do, dq, dk, dv)
+    hs = [_heads(where, n, x, s) for n, x, s in (("q", q, q.shape), ("k", k, kv), ("v", v, kv), ("do", do, q.shape),
+                                                 ("dq", dq, q.shape), ("dk", dk, kv), ("dv", dv, kv))]
+    ref = C.byref
+    r = [ref(x) for x in hs]
+    wp, wn = _ws_for(ws, L.hg_linattn_bwd_workspace_size(ref(desc)), q.device)
+    _check(L.hg_linattn_bwd(ref(desc), r[0], r[1], r[2], _ptr(log_decay), _ptr(lens), _ptr(state), r[3],
+                            _ptr(dstate_out), r[4], r[5], r[6], _ptr(dstate), wp, wn, _stream(stream)), where)
+    return dq, dk, dv, dstate
+
+
+def hg_linattn_step(q, k, v, log_decay, states, slots=None, scale: float = 1.0, o=None, stream=None):
+    """One token for each row: q [b, heads, d], k, v [b, kv_heads, d], states
+    float32 [n, heads, d, d] updated in place, slots int32 [b] (None: row b
+    has state b; a slot outside the states: an idle row).  Returns o."""
+    where = "hg_linattn_step"
+    b, h, d = q.shape
+    _same(where, q, k, v)
+    _vector(where, log_decay, h, q.device)
+    _vector(where, slots, b, q.device, torch.int32)
+    if (states.dim() != 4 or tuple(states.shape[1:]) != (h, d, d) or states.dtype != torch.float32
+            or states.device != q.device or not states.is_contiguous()):
+        raise ValueError(f"{where}: expected contiguous float32 states [n, {h}, {d}, {d}], got {tuple(states.shape)}")
+    if o is None:
+        o = torch.empty((b, h, d), dtype=q.dtype, device=q.device)
+    _same(where, q, o)
+    desc = LinattnDesc(1, b, h, k.shape[1], d, _float_code(where, q), scale)
+    hs = []
+    for n, x, s in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape)):
+        y = _heads(where, n, x, (b, s[1], d))
+        hs.append(Heads(y.p, y.token, 0, y.head))  # the rows are sequences
+    ref = C.byref
+    _check(lib().hg_linattn_step(ref(desc), ref(hs[0]), ref(hs[1]), ref(hs[2]), _ptr(log_decay), _ptr(states),
+                                 _ptr(slots), states.shape[0], ref(hs[3]), _stream(stream)), where)
+    return o
 
 
 def hg_timing_enable(on: bool = True):

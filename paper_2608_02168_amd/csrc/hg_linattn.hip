@@ -1,0 +1,819 @@
+// Linear attention with a decay for each head.
+//
+//   S_t = l S_{t-1} + k_t^T v_t,   o_t = scale q_t S_t,   l = exp(log_decay[h])
+//
+// A sequence is walked in chunks of C tokens.  With S the state before a
+// chunk and i, j its tokens,
+//   o_i = sum_{j <= i} l^(i-j) (q_i . k_j) v_j + l^(i+1) q_i S
+//   S'  = l^n S + sum_j l^(n-1-j) k_j^T v_j            (n tokens in the chunk)
+// so everything is matrix products on the MFMA.  Only non-negative powers of
+// l are formed: no decay overflows.
+//
+// The backward is the same walk with the roles changed (R is the gradient of
+// the state, walked from the last token):
+//   dq = scan(q := do, k := v, v := k)        its state is S^T
+//   dk = reverse scan(q := v, k := do, v := q)  its state is R^T
+//   dv = reverse scan(q := k, k := q, v := do)  its state is R
+// A reverse walk adds a token's k^T v before the decay, so its powers are
+// l^i and l^(n-j) instead of l^(i+1) and l^(n-1-j): the `lead` of 1.
+//
+// Work split: a block takes one head of one sequence, or one segment of it
+// when there are too few of those to fill the chip.  Then a first pass forms
+// every segment's sum, a second adds them up along the sequence, and the walk
+// starts each segment from its state.
+//
+// Layout: a wave owns 16 NT columns of v (and of the state and of o) and all
+// rows; q, k and v tiles are shared through LDS.  With the tiles' operands
+// taken as blocks of 16 values, 4 g .. 4 g + 3 in lane group g, every product's
+// result lies as the next product's operand needs it:
+//   P^T = K Q^T       lane (c, g): keys 4 g + v of query c    (operand of V^T P^T)
+//   S  += K^T (w V)   lane (c, g): rows 4 g + v of column c   (operand of S^T Q^T)
+//   O^T = S^T Q^T + V^T P^T   lane (c, g): columns 4 g + v of token c
+// so neither P nor S passes through LDS.
+//
+// Precision: sums, states and decays are float32.  float32 calls use the
+// float32 MFMA.  In bfloat16 calls q, k and v enter exactly, P and the copy of
+// S that multiplies q as a bfloat16 value and the rest of it (2^-17), and the
+// state takes w V in three bfloat16 parts (2^-24): what remains is the one
+// rounding of o.
+#include "hg_mfma.h"
+
+namespace hg {
+namespace {
+
+constexpr int kMaxD = 128;
+
+// One operand: element (sequence b, token t, head h, column x) at
+// p[b * sb + t * st + (h / hdiv) * sh + x].
+struct Role {
+  const void* p;
+  int64_t sb, st, sh;
+  int32_t hdiv;
+};
+
+struct ScanArgs {
+  Role q, k, v, o;
+  const float* log_decay;
+  const int32_t* lens;     // tokens of each sequence, or null
+  const float* s_in;       // [B][H][d][d] state before the walk, or null
+  float* s_out;            // state after it, or null
+  float* seg;              // segment sums, then states before each segment
+  int64_t T;
+  int64_t seg_len;         // a multiple of the chunk
+  int32_t segs, H, d;
+  int32_t reverse;         // walk from the last token; 1: its lead too
+  int32_t s_trans;         // the walk's state is the transpose of s_in and s_out
+  float kv_scale, o_scale;
+};
+
+typedef __bf16 l_bf16x4 __attribute__((ext_vector_type(4)));
+typedef short l_s16x4 __attribute__((ext_vector_type(4)));
+
+// Sixteen values of a contraction, four a lane.
+template <class T>
+struct Blk;
+template <>
+struct Blk<float> {
+  typedef f32x4 type;
+  static __device__ __forceinline__ type zero() { return f32x4{0.f, 0.f, 0.f, 0.f}; }
+  static __device__ __forceinline__ type of(f32x4 x) { return x; }
+};
+template <>
+struct Blk<bf16_t> {
+  typedef uint2 type;
+  static __device__ __forceinline__ type zero() { return uint2{0u, 0u}; }
+  // rounded to nearest
+  static __device__ __forceinline__ type of(f32x4 x) {
+    return __builtin_bit_cast(uint2, __builtin_convertvector(x, l_bf16x4));
+  }
+};
+__device__ __forceinline__ f32x4 wide(f32x4 x) { return x; }
+__device__ __forceinline__ f32x4 wide(uint2 x) {
+  return f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16),
+               __uint_as_float(x.y & 0xFFFF0000u)};
+}
+
+// A float32 factor of a product: as it is, or its bfloat16 value and the rest
+// of it (16 bits in all).
+template <class T>
+struct Factor {
+  static constexpr int N = sizeof(T) == 4 ? 1 : 2;
+  typename Blk<T>::type x[N];
+  __device__ __forceinline__ void set(f32x4 v) {
+    x[0] = Blk<T>::of(v);
+    if constexpr (N == 2) {
+      const f32x4 h = wide(x[0]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = v[i] - h[i];
+      x[1] = Blk<T>::of(v);
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = Blk<T>::zero();
+  }
+};
+
+// acc += A B over 32 values
+__device__ __forceinline__ f32x4 mma32(uint2 a0, uint2 a1, uint2 b0, uint2 b1, f32x4 acc) {
+  return mfma_bf16(uint4{a0.x, a0.y, a1.x, a1.y}, uint4{b0.x, b0.y, b1.x, b1.y}, acc);
+}
+__device__ __forceinline__ f32x4 mma32(f32x4 a0, f32x4 a1, f32x4 b0, f32x4 b1, f32x4 acc) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) acc = mfma4(a0[v], b0[v], acc);
+#pragma unroll
+  for (int v = 0; v < 4; ++v) acc = mfma4(a1[v], b1[v], acc);
+  return acc;
+}
+
+template <class T, int DP>
+struct Tile {
+  static constexpr int EL = Elt<T>::EL;
+  static constexpr int LD = DP + EL;  // 16 bytes more: 16 rows' chunks fall on all banks
+  typedef typename Blk<T>::type B;
+  // 16 columns of row r: lane's four
+  static __device__ __forceinline__ B row4(const T* t, int r, int blk, int g) {
+    return *reinterpret_cast<const B*>(t + r * LD + 16 * blk + 4 * g);
+  }
+  // rows 16 rb + 4 g .. + 3 of column 16 cb + c
+  static __device__ __forceinline__ B col4(const T* t, int rb, int cb, int c, int g) {
+    if constexpr (sizeof(T) == 4) {
+      const T* p = t + (16 * rb + 4 * g) * LD + 16 * cb + c;
+      return f32x4{p[0], p[LD], p[2 * LD], p[3 * LD]};
+    } else {
+      typedef __attribute__((address_space(3))) l_s16x4* lds_ptr;
+      const T* p = t + (16 * rb + 4 * g + (c >> 2)) * LD + 16 * cb + 4 * (c & 3);
+      return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p)));
+    }
+  }
+};
+
+// Tokens of sequence b.
+__device__ __forceinline__ int64_t len_of(const int32_t* lens, int b, int64_t T) {
+  if (!lens) return T;
+  const int64_t l = lens[b];
+  return l < 0 ? 0 : (l > T ? T : l);
+}
+
+// -infinity (a head that keeps nothing) as a number: its powers are 1, 0, 0, ...
+__device__ __forceinline__ float log_of(float x) { return x < -1e30f ? -1e30f : x; }
+
+// Power n >= 0 of the decay: exp(n log l), 1 for n = 0 whatever l is.
+__device__ __forceinline__ float decay(float lg, int64_t n) { return n <= 0 ? 1.f : expf(lg * (float)n); }
+
+// C rows of one operand into LDS: position u of the walk (token u, or last - u
+// in a reverse walk) in row u - u0; positions from u_to on and columns from d on
+// are zero.
+template <class T, int DP, int C, int NT>
+__device__ __forceinline__ void stage(T* lds, const Role& r, const T* base, int64_t u0, int64_t u_to, int64_t last, int d) {
+  constexpr int EL = Elt<T>::EL, CH = DP / EL, N = C * CH / NT;
+  static_assert(C * CH % NT == 0, "whole chunks per thread");
+  typename Elt<T>::rawv_t x[N];
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
+    const int64_t u = u0 + row, t = last >= 0 ? last - u : u;
+    x[q] = u < u_to && col < d ? Elt<T>::rawv(base + t * r.st + col) : Elt<T>::rawv_zero();
+  }
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
+    *reinterpret_cast<typename Elt<T>::rawv_t*>(lds + row * Tile<T, DP>::LD + col) = x[q];
+  }
+}
+
+// v truncated to three bfloat16 parts (24 bits in all), four values a lane
+__device__ __forceinline__ void parts3(f32x4 x, uint2 (&p)[3]) {
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint32_t u[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      u[v] = __float_as_uint(x[v]);
+      if (k < 2) x[v] -= __uint_as_float(u[v] & 0xFFFF0000u);
+    }
+    p[k] = uint2{__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[2], 0x07060302u)};
+  }
+}
+
+template <int DP>
+struct Shape {
+  static constexpr int NT = DP >= 96 ? 2 : 1;  // 16-column blocks of a wave
+  static constexpr int W = DP / 16 / NT, THREADS = 64 * W, NB = DP / 16;
+};
+
+// One head of one sequence, or a segment of it.  SUMS: only the segment's sum.
+template <class T, class TO, int DP, int C, bool SUMS>
+__global__ void __launch_bounds__(Shape<DP>::THREADS) k_linattn_scan(const ScanArgs a) {
+  constexpr int NT = Shape<DP>::NT, NB = Shape<DP>::NB, NTHR = Shape<DP>::THREADS, RB = C / 16;
+  typedef Tile<T, DP> TL;
+  typedef typename Blk<T>::type B;
+  constexpr bool kF32 = sizeof(T) == 4;
+  __shared__ __align__(16) T lk[C * TL::LD];
+  __shared__ __align__(16) T lv[C * TL::LD];
+  __shared__ __align__(16) T lq[SUMS ? 16 : C * TL::LD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int h = blockIdx.x % a.H, b = blockIdx.x / a.H, seg = blockIdx.y;
+  const int d = a.d;
+  const float lg = log_of(a.log_decay[h]);
+  const int64_t L = len_of(a.lens, b, a.T);
+  const int64_t u_from = (int64_t)seg * a.seg_len;
+  const int64_t u_to = u_from + a.seg_len < L ? u_from + a.seg_len : L;
+  const int lead = a.reverse ? 1 : 0;
+  const int64_t last = a.reverse ? L - 1 : -1;
+  const T* kp = static_cast<const T*>(a.k.p) + b * a.k.sb + (h / a.k.hdiv) * a.k.sh;
+  const T* vp = static_cast<const T*>(a.v.p) + b * a.v.sb + (h / a.v.hdiv) * a.v.sh;
+  const T* qp = SUMS ? nullptr : static_cast<const T*>(a.q.p) + b * a.q.sb + (h / a.q.hdiv) * a.q.sh;
+  TO* op = SUMS ? nullptr : static_cast<TO*>(const_cast<void*>(a.o.p)) + b * a.o.sb + (h / a.o.hdiv) * a.o.sh;
+  const int64_t bh = (int64_t)b * a.H + h;
+
+  if constexpr (!SUMS) {
+    // tokens past the sequence's end: zero rows
+    const int64_t z0 = u_from > L ? u_from : L, z1 = u_from + a.seg_len < a.T ? u_from + a.seg_len : a.T;
+    const int ch = d / 4;
+    for (int64_t i = threadIdx.x; i < (z1 - z0) * ch; i += NTHR) {
+      const int64_t t = z0 + i / ch;
+      TO* p = op + t * a.o.st + i % ch * 4;
+      if constexpr (sizeof(TO) == 4) {
+        *reinterpret_cast<f32x4*>(p) = f32x4{0.f, 0.f, 0.f, 0.f};
+      } else {
+        *reinterpret_cast<uint2*>(p) = uint2{0u, 0u};
+      }
+    }
+    if (u_from >= L && seg > 0) return;  // segment 0 of an empty sequence still hands its state on
+  } else {
+    if (u_from >= L) return;
+  }
+
+  // state: rows 16 i + 4 g + v, columns 16 (wave NT + j) + c
+  f32x4 S[NB][NT];
+  float* seg_at = a.seg ? a.seg + ((bh * a.segs + seg) * (NB * NB)) * 256 : nullptr;
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      S[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (!SUMS) {
+        if (a.segs > 1) {
+          S[i][j] = *reinterpret_cast<const f32x4*>(seg_at + (i * NB + wave * NT + j) * 256 + lane * 4);
+        } else if (a.s_in) {
+          const int col = 16 * (wave * NT + j) + c;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int row = 16 * i + 4 * g + v;
+            if (row < d && col < d) S[i][j][v] = a.s_in[bh * d * d + (a.s_trans ? col * d + row : row * d + col)];
+          }
+        }
+      }
+    }
+
+  // powers of the decay that every chunk needs
+  float near0[4], diag[4], tail[4];  // l^(16 + c - 4 g - v), l^(c - 4 g - v) below the diagonal, l^(15 - 4 g - v + lead)
+#pragma unroll
+  for (int v = 0; v < 4; ++v) {
+    const int x = c - 4 * g - v;
+    near0[v] = decay(lg, 16 + x) * a.kv_scale;
+    diag[v] = x >= 0 ? decay(lg, x) * a.kv_scale : 0.f;
+    tail[v] = decay(lg, 15 - 4 * g - v + lead) * a.kv_scale;
+  }
+  const float row0 = decay(lg, c + 1 - lead), p16 = decay(lg, 16), pC = decay(lg, C);
+
+  for (int64_t u0 = u_from; u0 < u_to; u0 += C) {
+    const int n = (int)(u_to - u0 < C ? u_to - u0 : C);
+    __syncthreads();
+    stage<T, DP, C, NTHR>(lk, a.k, kp, u0, u_to, last, d);
+    stage<T, DP, C, NTHR>(lv, a.v, vp, u0, u_to, last, d);
+    if constexpr (!SUMS) stage<T, DP, C, NTHR>(lq, a.q, qp, u0, u_to, last, d);
+    __syncthreads();
+    if constexpr (!SUMS) {
+      Factor<T> Sb[NB + NB % 2][NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int i = 0; i < NB; ++i) Sb[i][j].set(S[i][j]);
+        if constexpr (NB % 2) Sb[NB][j].zero();
+      }
+      float rowp = row0;
+#pragma unroll
+      for (int r = 0; r < RB; ++r, rowp *= p16) {
+        B qf[NB + NB % 2];
+#pragma unroll
+        for (int i = 0; i < NB; ++i) qf[i] = TL::row4(lq, 16 * r + c, i, g);
+        if constexpr (NB % 2) qf[NB] = Blk<T>::zero();
+        f32x4 o[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = Factor<T>::N - 1; x >= 0; --x)
+#pragma unroll
+            for (int i = 0; i < NB; i += 2) o[j] = mma32(Sb[i][j].x[x], Sb[i + 1][j].x[x], qf[i], qf[i + 1], o[j]);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) o[j][v] *= rowp;
+        }
+        Factor<T> pb[RB];
+        if (r + 1 < RB) pb[r + 1].zero();
+        float far = 1.f;
+#pragma unroll
+        for (int kt = r; kt >= 0; --kt) {
+          f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < NB; i += 2)
+            s = mma32(TL::row4(lk, 16 * kt + c, i, g),
+                      i + 1 < NB ? TL::row4(lk, 16 * kt + c, i + 1 < NB ? i + 1 : i, g) : Blk<T>::zero(), qf[i], qf[i + 1], s);
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            s[v] = kt < r ? s[v] * (near0[v] * far) : c >= 4 * g + v ? s[v] * diag[v] : 0.f;
+          if (kt < r) far *= p16;
+          pb[kt].set(s);
+        }
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+#pragma unroll
+          for (int kt = 0; kt <= r; kt += 2) {
+            const B v0 = TL::col4(lv, kt, wave * NT + j, c, g);
+            const B v1 = kt + 1 <= r ? TL::col4(lv, kt + 1, wave * NT + j, c, g) : Blk<T>::zero();
+#pragma unroll
+            for (int x = Factor<T>::N - 1; x >= 0; --x) o[j] = mma32(v0, v1, pb[kt].x[x], pb[kt + 1].x[x], o[j]);
+          }
+          const int64_t u = u0 + 16 * r + c, t = last >= 0 ? last - u : u;
+          const int col = 16 * (wave * NT + j) + 4 * g;
+          if (u < u_to && col < d) {
+            TO* p = op + t * a.o.st + col;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[j][v] *= a.o_scale;
+            if constexpr (sizeof(TO) == 4) {
+              *reinterpret_cast<f32x4*>(p) = o[j];
+            } else {
+              *reinterpret_cast<uint2*>(p) = Blk<bf16_t>::of(o[j]);
+            }
+          }
+        }
+      }
+    }
+
+    // state
+    const float dn = n == C ? pC : decay(lg, n);
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) S[i][j][v] *= dn;
+    // w V of this wave's columns: token 16 tb + 4 g + v
+    f32x4 wv[RB][NT];
+    float far = 1.f;
+#pragma unroll
+    for (int tb = RB - 1; tb >= 0; --tb, far *= p16) {
+      float w[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        w[v] = n == C ? tail[v] * far : decay(lg, n - 1 - (16 * tb + 4 * g + v) + lead) * a.kv_scale;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        wv[tb][j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
+#pragma unroll
+        for (int v = 0; v < 4; ++v) wv[tb][j][v] *= w[v];
+      }
+    }
+#pragma unroll
+    for (int tb = 0; tb < RB; tb += 2) {
+      uint2 p0[NT][3], p1[NT][3];
+      if constexpr (!kF32) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          parts3(wv[tb][j], p0[j]);
+          parts3(wv[tb + 1][j], p1[j]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const B k0 = TL::col4(lk, tb, i, c, g), k1 = TL::col4(lk, tb + 1, i, c, g);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          if constexpr (kF32) {
+            S[i][j] = mma32(k0, k1, wv[tb][j], wv[tb + 1][j], S[i][j]);
+          } else {
+#pragma unroll
+            for (int x = 2; x >= 0; --x) S[i][j] = mma32(k0, k1, p0[j][x], p1[j][x], S[i][j]);
+          }
+        }
+      }
+    }
+  }
+
+  if constexpr (SUMS) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        *reinterpret_cast<f32x4*>(seg_at + (i * NB + wave * NT + j) * 256 + lane * 4) = S[i][j];
+  } else if (a.segs == 1 && a.s_out) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const int col = 16 * (wave * NT + j) + c;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int row = 16 * i + 4 * g + v;
+          if (row < d && col < d) a.s_out[bh * d * d + (a.s_trans ? col * d + row : row * d + col)] = S[i][j][v];
+        }
+      }
+  }
+}
+
+// The segments' sums added up along each sequence: each becomes the state
+// before its segment, the last one's successor the state after the walk.  A
+// thread takes four elements (a lane's share of one 16 x 16 block).
+template <int DP>
+__global__ void __launch_bounds__(256) k_linattn_join(const ScanArgs a, int64_t bhs) {
+  constexpr int NB = DP / 16, Q = NB * NB * 64;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, bh = id / Q;
+  if (bh >= bhs) return;
+  const int q = (int)(id - bh * Q), blk = q >> 6, lane = q & 63, c = lane & 15, g = lane >> 4;
+  const int h = (int)(bh % a.H), b = (int)(bh / a.H), d = a.d;
+  const int64_t L = len_of(a.lens, b, a.T);
+  const float lg = log_of(a.log_decay[h]), whole = decay(lg, a.seg_len);
+  const int col = 16 * (blk % NB) + c, row = 16 * (blk / NB) + 4 * g;
+  f32x4 S{0.f, 0.f, 0.f, 0.f};
+  auto at = [&](int v) { return bh * d * d + (a.s_trans ? col * d + row + v : (row + v) * d + col); };
+  if (a.s_in && col < d) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      if (row + v < d) S[v] = a.s_in[at(v)];
+  }
+  float* p = a.seg + bh * a.segs * (int64_t)(NB * NB * 256) + (int64_t)q * 4;
+  const int live = (int)((L + a.seg_len - 1) / a.seg_len);
+  for (int s = 0; s < live; ++s, p += NB * NB * 256) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p);
+    *reinterpret_cast<f32x4*>(p) = S;
+    const int64_t left = L - s * a.seg_len;
+    const float f = left >= a.seg_len ? whole : decay(lg, left);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) S[v] = S[v] * f + x[v];
+  }
+  if (a.s_out && col < d) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      if (row + v < d) a.s_out[at(v)] = S[v];
+  }
+}
+
+// Sum over the query heads of a key head, in order: x [rows][hk][group][d] -> out
+template <class T>
+__global__ void __launch_bounds__(256)
+    k_group_sum(const float* __restrict__ x, int64_t B, int64_t T_, int hk, int group, int d, Role o) {
+  const int ch = d / 4;
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t r = id / ch;  // (b, t, head)
+  if (r >= B * T_ * hk) return;
+  const int col = (int)(id - r * ch) * 4;
+  f32x4 s{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < group; ++i) {
+    const f32x4 y = *reinterpret_cast<const f32x4*>(x + (r * group + i) * d + col);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) s[v] += y[v];
+  }
+  const int h = (int)(r % hk);
+  const int64_t bt = r / hk, b = bt / T_, t = bt - b * T_;
+  T* p = static_cast<T*>(const_cast<void*>(o.p)) + b * o.sb + t * o.st + h * o.sh + col;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4*>(p) = s;
+  } else {
+    *reinterpret_cast<uint2*>(p) = Blk<bf16_t>::of(s);
+  }
+}
+
+// One token: S' = l S + k^T v in place, o = scale q S'.  A block takes a head
+// of a row, or some columns of it; a thread four columns of every RG-th row of
+// the state.  Bound by the state, read and written once.
+template <class T, int NTHR>
+__global__ void __launch_bounds__(NTHR)
+    k_linattn_step(Role q, Role k, Role v, Role o, const float* __restrict__ log_decay, float* __restrict__ state,
+                   const int32_t* __restrict__ slots, int64_t n_slots, int H, int d, int width, float scale) {
+  __shared__ float lq[kMaxD], lk[kMaxD];
+  __shared__ f32x4 part[NTHR];
+  const int h = blockIdx.x % H, b = blockIdx.x / H;
+  const int c0 = blockIdx.y * width, wide = d - c0 < width ? d - c0 : width;
+  const int lc = wide / 4, rg = NTHR / lc;
+  const int x = threadIdx.x % lc, y = threadIdx.x / lc;
+  T* op = static_cast<T*>(const_cast<void*>(o.p)) + b * o.sb + (h / o.hdiv) * o.sh + c0;
+  const int64_t slot = slots ? slots[b] : b;
+  const bool live = slot >= 0 && slot < n_slots;
+  if (live) {
+    const T* qp = static_cast<const T*>(q.p) + b * q.sb + (h / q.hdiv) * q.sh;
+    const T* kp = static_cast<const T*>(k.p) + b * k.sb + (h / k.hdiv) * k.sh;
+    for (int i = threadIdx.x; i < d; i += NTHR) {
+      lq[i] = Elt<T>::get(qp + i) * scale;
+      lk[i] = Elt<T>::get(kp + i);
+    }
+  }
+  __syncthreads();
+  f32x4 s{0.f, 0.f, 0.f, 0.f};
+  if (live && y < rg) {
+    const float l = expf(log_decay[h]);
+    const f32x4 vv = Elt<T>::load4(static_cast<const T*>(v.p) + b * v.sb + (h / v.hdiv) * v.sh + c0 + 4 * x);
+    float* p = state + (slot * H + h) * (int64_t)d * d + c0 + 4 * x;
+#pragma unroll 8
+    for (int r = y; r < d; r += rg) {
+      f32x4 w = *reinterpret_cast<const f32x4*>(p + r * d);
+      const float kr = lk[r], qr = lq[r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        w[i] = fmaf(l, w[i], kr * vv[i]);
+        s[i] = fmaf(qr, w[i], s[i]);
+      }
+      *reinterpret_cast<f32x4*>(p + r * d) = w;
+    }
+  }
+  part[threadIdx.x] = s;
+  __syncthreads();
+  if (y == 0) {
+    for (int i = 1; i < rg; ++i) {
+      const f32x4 w = part[i * lc + x];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] += w[j];
+    }
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<f32x4*>(op + 4 * x) = s;
+    } else {
+      *reinterpret_cast<uint2*>(op + 4 * x) = Blk<bf16_t>::of(s);
+    }
+  }
+}
+
+// ---- host ---------------------------------------------------------------------------
+int pad_d(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
+int chunk_of(int dtype, int64_t T) { return dtype == HG_DTYPE_F32 || T <= 32 ? 32 : 64; }
+
+// Segments of a walk: none while the heads fill the chip (a block per CU);
+// else enough for two blocks per CU, of at least four chunks each.
+struct Segs {
+  int n;
+  int64_t len;
+};
+Segs segs_of(const hg_linattn_desc* A) {
+  const int64_t C = chunk_of(A->dtype, A->t), heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads);
+  int64_t n = 1;
+  if (heads < 256) n = std::max<int64_t>(1, std::min(cdiv(512, heads), A->t / (4 * C)));
+  const int64_t len = cdiv(cdiv(std::max<int64_t>(A->t, 1), n), C) * C;
+  return {(int)std::max<int64_t>(1, cdiv(A->t, len)), len};
+}
+
+int64_t seg_elems(const hg_linattn_desc* A) {
+  const Segs s = segs_of(A);
+  const int64_t dp = pad_d(A->d);
+  return s.n > 1 ? (int64_t)A->batch * A->heads * s.n * dp * dp : 0;
+}
+
+template <class T, class TO, int DP, int C>
+int launch_scan(const char* name, ScanArgs a, int64_t B, hipStream_t s) {
+  const int64_t bhs = B * a.H;
+  const dim3 grid((unsigned)bhs, (unsigned)a.segs), block(Shape<DP>::THREADS);
+  if (a.segs > 1) {
+    HG_LAUNCH("linattn_sums", (k_linattn_scan<T, TO, DP, C, true>), grid, block, 0, s, a);
+    HG_LAUNCH("linattn_join", (k_linattn_join<DP>), dim3((unsigned)cdiv(bhs * (DP / 16) * (DP / 16) * 64, 256)), dim3(256),
+              0, s, a, bhs);
+  }
+  HG_LAUNCH(name, (k_linattn_scan<T, TO, DP, C, false>), grid, block, 0, s, a);
+  return HG_OK;
+}
+
+template <class T, class TO, int C>
+int scan_d(const char* name, const ScanArgs& a, int64_t B, hipStream_t s) {
+  switch (pad_d(a.d)) {
+    case 16: return launch_scan<T, TO, 16, C>(name, a, B, s);
+    case 32: return launch_scan<T, TO, 32, C>(name, a, B, s);
+    case 64: return launch_scan<T, TO, 64, C>(name, a, B, s);
+    case 96: return launch_scan<T, TO, 96, C>(name, a, B, s);
+    default: return launch_scan<T, TO, 128, C>(name, a, B, s);
+  }
+}
+
+// f32_out: o is float32 whatever dtype is
+int scan(const char* name, const hg_linattn_desc* A, const ScanArgs& a, bool f32_out, hipStream_t s) {
+  if (A->dtype == HG_DTYPE_F32) return scan_d<float, float, 32>(name, a, A->batch, s);
+  const bool small = chunk_of(A->dtype, A->t) == 32;
+  if (f32_out)
+    return small ? scan_d<bf16_t, float, 32>(name, a, A->batch, s) : scan_d<bf16_t, float, 64>(name, a, A->batch, s);
+  return small ? scan_d<bf16_t, bf16_t, 32>(name, a, A->batch, s) : scan_d<bf16_t, bf16_t, 64>(name, a, A->batch, s);
+}
+
+int check(const hg_linattn_desc* A, const char* what) {
+  if (!A) return fail(HG_ERR_ARG, "%s: null descriptor", what);
+  if (A->t < 0 || A->batch < 0 || A->heads < 1 || A->kv_heads < 1 || A->d < 1)
+    return fail(HG_ERR_ARG, "%s: batch=%d t=%lld heads=%d kv_heads=%d d=%d", what, A->batch, (long long)A->t, A->heads,
+                A->kv_heads, A->d);
+  if (A->heads % A->kv_heads) return fail(HG_ERR_ARG, "%s: %d heads on %d key heads", what, A->heads, A->kv_heads);
+  if (A->dtype != HG_DTYPE_F32 && A->dtype != HG_DTYPE_BF16) return fail(HG_ERR_ARG, "%s: dtype %d", what, A->dtype);
+  if (A->d % 8 || A->d > kMaxD) return fail(HG_ERR_UNSUPPORTED, "%s: d=%d is not a multiple of 8 up to %d", what, A->d, kMaxD);
+  if ((int64_t)A->batch * A->heads >= (int64_t)1 << 24 || A->t >= (int64_t)1 << 31 ||
+      A->t * A->batch > ((int64_t)1 << 36) / A->heads)
+    return fail(HG_ERR_UNSUPPORTED, "%s: %d sequences of %lld tokens and %d heads are too many", what, A->batch,
+                (long long)A->t, A->heads);
+  return HG_OK;
+}
+
+// A strided operand: 16-byte aligned rows (null only where there are none).
+int check_heads(const hg_linattn_desc* A, const char* what, const hg_heads* x, const char* name) {
+  if (!x || (!x->p && A->t > 0 && A->batch > 0)) return fail(HG_ERR_ARG, "%s: null %s", what, name);
+  const int64_t e = A->dtype == HG_DTYPE_F32 ? 4 : 8;
+  if ((reinterpret_cast<uintptr_t>(x->p) & 15) || x->batch % e || x->token % e || x->head % e)
+    return fail(HG_ERR_ARG, "%s: rows of %s are not 16-byte aligned", what, name);
+  return HG_OK;
+}
+
+Role role(const hg_heads* x, int hdiv) { return Role{x->p, x->batch, x->token, x->head, hdiv}; }
+
+ScanArgs args_of(const hg_linattn_desc* A, const float* log_decay, const int32_t* lens, float* seg) {
+  const Segs sg = segs_of(A);
+  ScanArgs a{};
+  a.log_decay = log_decay;
+  a.lens = lens;
+  a.seg = sg.n > 1 ? seg : nullptr;
+  a.T = A->t;
+  a.seg_len = sg.len;
+  a.segs = sg.n;
+  a.H = A->heads;
+  a.d = A->d;
+  a.kv_scale = a.o_scale = 1.f;
+  return a;
+}
+
+struct Bufs {
+  float* seg = nullptr;
+  float* part = nullptr;  // gradients of k and v for each query head
+};
+
+template <class Mem>
+Bufs take(const hg_linattn_desc* A, bool bwd, Mem& m) {
+  Bufs b;
+  b.seg = m.template take<float>(seg_elems(A));
+  if (bwd && A->heads != A->kv_heads) b.part = m.template take<float>((int64_t)A->batch * A->t * A->heads * A->d);
+  return b;
+}
+
+int sum_groups(const hg_linattn_desc* A, const float* part, const hg_heads* o, hipStream_t s) {
+  const int64_t rows = (int64_t)A->batch * A->t * A->kv_heads;
+  if (rows == 0) return HG_OK;
+  const dim3 grid((unsigned)cdiv(rows * (A->d / 4), 256));
+  const int group = A->heads / A->kv_heads;
+  if (A->dtype == HG_DTYPE_F32) {
+    HG_LAUNCH("group_sum", k_group_sum<float>, grid, dim3(256), 0, s, part, (int64_t)A->batch, A->t, A->kv_heads, group,
+              A->d, role(o, 1));
+  } else {
+    HG_LAUNCH("group_sum", k_group_sum<bf16_t>, grid, dim3(256), 0, s, part, (int64_t)A->batch, A->t, A->kv_heads, group,
+              A->d, role(o, 1));
+  }
+  return HG_OK;
+}
+
+}  // namespace
+}  // namespace hg
+
+using namespace hg;
+
+extern "C" size_t hg_linattn_fwd_workspace_size(const hg_linattn_desc* A) {
+  if (check(A, "workspace size") != HG_OK) return 0;
+  Sizer m;
+  take(A, false, m);
+  return m.used;
+}
+
+extern "C" size_t hg_linattn_bwd_workspace_size(const hg_linattn_desc* A) {
+  if (check(A, "workspace size") != HG_OK) return 0;
+  Sizer m;
+  take(A, true, m);
+  return m.used;
+}
+
+extern "C" int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
+                              const float* log_decay, const int32_t* lens, const float* state, const hg_heads* o,
+                              float* state_out, void* ws, size_t ws_bytes, void* stream) {
+  const char* what = "hg_linattn_fwd";
+  HG_TRY(check(A, what));
+  HG_TRY(check_heads(A, what, q, "q"));
+  HG_TRY(check_heads(A, what, k, "k"));
+  HG_TRY(check_heads(A, what, v, "v"));
+  HG_TRY(check_heads(A, what, o, "o"));
+  if (A->batch == 0) return HG_OK;
+  if (!log_decay) return fail(HG_ERR_ARG, "%s: null log_decay", what);
+  if (A->t > 0 && (o->p == q->p || o->p == k->p || o->p == v->p)) return fail(HG_ERR_ARG, "%s: o is an input", what);
+  if (state && state == state_out) return fail(HG_ERR_ARG, "%s: state_out is state", what);
+  Sizer need;
+  take(A, false, need);
+  if (ws_bytes < need.used || (need.used && !ws))
+    return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  Arena m(ws, ws_bytes);
+  const Bufs b = take(A, false, m);
+  ScanArgs a = args_of(A, log_decay, lens, b.seg);
+  const int group = A->heads / A->kv_heads;
+  a.q = role(q, 1);
+  a.k = role(k, group);
+  a.v = role(v, group);
+  a.o = role(o, 1);
+  a.s_in = state;
+  a.s_out = state_out;
+  a.o_scale = A->scale;
+  return scan("linattn", A, a, false, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
+                              const float* log_decay, const int32_t* lens, const float* state, const hg_heads* d_o,
+                              const float* dstate_out, const hg_heads* dq, const hg_heads* dk, const hg_heads* dv,
+                              float* dstate, void* ws, size_t ws_bytes, void* stream) {
+  const char* what = "hg_linattn_bwd";
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  HG_TRY(check(A, what));
+  const hg_heads* all[7] = {q, k, v, d_o, dq, dk, dv};
+  const char* names[7] = {"q", "k", "v", "dO", "dq", "dk", "dv"};
+  for (int i = 0; i < 7; ++i) HG_TRY(check_heads(A, what, all[i], names[i]));
+  if (A->batch == 0) return HG_OK;
+  if (!log_decay) return fail(HG_ERR_ARG, "%s: null log_decay", what);
+  for (int i = 4; i < 7 && A->t > 0; ++i)
+    for (int j = 0; j < i; ++j)
+      if (all[i]->p == all[j]->p) return fail(HG_ERR_ARG, "%s: %s is %s", what, names[i], names[j]);
+  if (dstate && (dstate == state || dstate == dstate_out)) return fail(HG_ERR_ARG, "%s: dstate is an input", what);
+  Sizer need;
+  take(A, true, need);
+  if (ws_bytes < need.used || (need.used && !ws))
+    return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  Arena m(ws, ws_bytes);
+  const Bufs b = take(A, true, m);
+  const int group = A->heads / A->kv_heads;
+  ScanArgs a = args_of(A, log_decay, lens, b.seg);
+  // dq: its state is the transpose of the forward's
+  a.q = role(d_o, 1);
+  a.k = role(v, group);
+  a.v = role(k, group);
+  a.o = role(dq, 1);
+  a.s_in = state;
+  a.s_trans = 1;
+  a.o_scale = A->scale;
+  HG_TRY(scan("linattn_dq", A, a, false, s));
+  // dk and dv: from the last token, for each query head
+  const int64_t H = A->heads, d = A->d;
+  const Role part{b.part, A->t * H * d, H * d, d, 1};
+  a.reverse = 1;
+  a.kv_scale = A->scale;
+  a.o_scale = 1.f;
+  a.s_in = dstate_out;
+  a.q = role(v, group);
+  a.k = role(d_o, 1);
+  a.v = role(q, 1);
+  a.o = group > 1 ? part : role(dk, 1);
+  HG_TRY(scan("linattn_dk", A, a, group > 1, s));
+  if (group > 1) HG_TRY(sum_groups(A, b.part, dk, s));
+  a.s_trans = 0;
+  a.s_out = dstate;
+  a.q = role(k, group);
+  a.k = role(q, 1);
+  a.v = role(d_o, 1);
+  a.o = group > 1 ? part : role(dv, 1);
+  HG_TRY(scan("linattn_dv", A, a, group > 1, s));
+  if (group > 1) HG_TRY(sum_groups(A, b.part, dv, s));
+  return HG_OK;
+}
+
+extern "C" int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
+                               const float* log_decay, float* state, const int32_t* slots, int64_t n_slots,
+                               const hg_heads* o, void* stream) {
+  const char* what = "hg_linattn_step";
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  HG_TRY(check(A, what));
+  if (A->t != 1) return fail(HG_ERR_ARG, "%s: t=%lld, one token a row", what, (long long)A->t);
+  HG_TRY(check_heads(A, what, q, "q"));
+  HG_TRY(check_heads(A, what, k, "k"));
+  HG_TRY(check_heads(A, what, v, "v"));
+  HG_TRY(check_heads(A, what, o, "o"));
+  if (n_slots < 0 || (!slots && n_slots < A->batch))
+    return fail(HG_ERR_ARG, "%s: %lld states for %d rows", what, (long long)n_slots, A->batch);
+  if (A->batch == 0) return HG_OK;
+  if (!log_decay || (!state && n_slots > 0)) return fail(HG_ERR_ARG, "%s: null pointer", what);
+  if (reinterpret_cast<uintptr_t>(state) & 15) return fail(HG_ERR_ARG, "%s: the states are not 16-byte aligned", what);
+  // whole heads while there are two blocks per CU of them, else columns of a
+  // head, at least 16 (64 bytes of a row of the state)
+  const int64_t heads = (int64_t)A->batch * A->heads;
+  int width = A->d;
+  while (width > 16 && heads * cdiv(A->d, width) < 512) width = std::max(16, (int)cdiv(width / 2, 8) * 8);
+  const int group = A->heads / A->kv_heads;
+  const dim3 grid((unsigned)heads, (unsigned)cdiv(A->d, width));
+#define HG_STEP(T_, N_)                                                                                              \
+  HG_LAUNCH("linattn_step", (k_linattn_step<T_, N_>), grid, dim3(N_), 0, s, role(q, 1), role(k, group), role(v, group), \
+            role(o, 1), log_decay, state, slots, n_slots, A->heads, A->d, width, A->scale)
+  const bool small = A->d <= 32;
+  if (A->dtype == HG_DTYPE_F32) {
+    if (small) {
+      HG_STEP(float, 64);
+    } else {
+      HG_STEP(float, 256);
+    }
+  } else if (small) {
+    HG_STEP(bf16_t, 64);
+  } else {
+    HG_STEP(bf16_t, 256);
+  }
+#undef HG_STEP
+  return HG_OK;
+}

@@ -522,14 +522,14 @@ int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t
  * Base addresses of X, W and dY are multiples of 16 bytes; strides are in
  * elements and at least the width.  n < 2^31, widths at most 2^20.
  *
- * Precision: bfloat16 products enter the MFMA exactly and z, act and the sum
- * with R are float32, rounded once into Y.  float32 rows follow the row
- * transforms' split-fp16 rule stated at the top (X by row, W as a whole); a
- * row that holds an infinity or NaN gives NaN in that row only.  In the
- * backward dz = dY * act'(z) is formed from float32 z; bfloat16 calls round
- * it once (when act is not HG_ACT_NONE) as operand of the two products, and
- * dbias sums it before that.  float32 weight gradients use the three-part
- * bfloat16 rule. */
+ * Precision: bfloat16 values enter the MFMA exactly and z, act and the sum
+ * with R are float32, rounded once into Y.  float32 values are taken in three
+ * bfloat16 parts with the six part products of order at most two (the weight
+ * gradients' rule stated at the top, here for all three products), each product
+ * term within about 2^-22 of itself; a row that holds an infinity or NaN gives
+ * NaN in that row only.  In the backward dz = dY * act'(z) is formed from
+ * float32 z; bfloat16 calls round it once (when act is not HG_ACT_NONE) as
+ * operand of the two products, and dbias sums it before that. */
 typedef struct hg_linear_desc {
   int64_t n;
   int32_t d_in, d_out;

@@ -1,11 +1,9 @@
-// Tiled matrix product on the 16-bit MFMA with a fused epilogue: the core of
+// Tiled matrix product on the bfloat16 MFMA with a fused epilogue: the core of
 // the linear map and of the gated product, forward and backward.
 //
 //   Z[m][n] = sum_k A[m][k] B[k][n]
 //
-// Operands are 16-bit matrices of one or more planes (a float32 matrix is a
-// sum of planes, see the product lists below).  Each operand is read as it
-// lies: k contiguous (KM, "rows of k") or k the row index (the rows run over
+// Each operand is read as it lies: k contiguous (KM, "rows of k") or k the row index (the rows run over
 // m or n).  That gives the three products of a linear map without a
 // transposition pass:
 //   z  = x W      A = x   KM,      B = W   k-rows
@@ -34,54 +32,21 @@
 
 namespace hg {
 
-typedef _Float16 g_f16x8 __attribute__((ext_vector_type(8)));
 typedef short g_s16x4 __attribute__((ext_vector_type(4)));
 
-// The part products that make up one product of two split matrices.
-//   GBf16    one bfloat16 plane a factor, exact
-//   GF16x2   fp16 high part and remainder of both factors, scaled by powers of
-//            two: three of the four products (the split-fp16 row transforms)
-//   GBf16x3  three bfloat16 parts, the six products of order at most two (the
-//            weight gradients: no scales, since the sum runs over rows)
-struct GBf16 {
-  static constexpr int P = 1, NP = 1;
-  static constexpr bool kF16 = false;
-  static constexpr int pa[1] = {0}, pb[1] = {0};
-};
-struct GF16x2 {
-  static constexpr int P = 2, NP = 3;
-  static constexpr bool kF16 = true;
-  static constexpr int pa[3] = {1, 0, 0}, pb[3] = {0, 1, 0};
-};
-struct GBf16x3 {
-  static constexpr int P = 3, NP = 6;
-  static constexpr bool kF16 = false;
-  static constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
-};
-
-template <bool kF16>
-__device__ __forceinline__ f32x4 g_mfma(uint4 a, uint4 b, f32x4 c) {
-  if constexpr (kF16) {
-    return mfma_f16(a, b, c);
-  } else {
-    return mfma_bf16(a, b, c);
-  }
-}
-
 // One operand.  KM: `rows` rows (m or n) of K values; else K rows of `cols`
-// values.  ld and plane (the distance of the planes) in elements; p 16-byte
-// aligned, ld, K (KM) or cols multiples of 8.
+// values.  ld in elements.  bfloat16: p 16-byte aligned, ld, K (KM) or cols
+// multiples of 8.
+template <class T>
 struct GOperand {
-  const uint16_t* p;
-  int64_t ld, plane;
+  const T* p;
+  int64_t ld;
   int64_t rows;  // rows of the matrix as stored
   int32_t cols;  // valid values of a row
 };
 
-// How Z becomes the output.  Scales undo the operands' powers of two.
+// How Z becomes the output.
 struct GEpi {
-  const float* ua;    // [M] factor of each row, or null
-  const float* ub;    // [1] factor of the whole product, or null
   const float* bias;  // [N] (gated: [2 F]) or null
   const void* res;    // residual rows (linear) or upstream gradient rows (backward), or null
   int64_t ld_res;
@@ -91,22 +56,26 @@ struct GEpi {
   int32_t ncol;       // columns that the output has (the tiles may count padding too)
   int32_t half;       // gated: F; a [., 2 F] result stored in two padded halves: F; else 0
   int32_t halfp;      // distance of the two halves as the operands hold them
-  int32_t outp;       // gradient of z: padded width of a row (gated: of each half), a multiple of 8
+  int32_t outp;       // gradient of z: width of a row (gated: of each half) with its padding
   int32_t accumulate;
   float* colsum;      // [tiles of m][ld_colsum] column sums of what a tile wrote, or null
   int64_t ld_colsum;
   float* part;        // [splits][M][ld_part] when the k range is split
-  int64_t ld_part;
+  int64_t ld_part;    // a multiple of 4
+  int32_t parth;      // distance of the two halves in it, a multiple of 4
 };
 
-struct GArgs {
-  GOperand a, b;
+struct GShape {
   int64_t M;
   int32_t N;          // columns of Z as the tiles count them (gated: 2 * halfp)
   int64_t K;
   int64_t k_split;    // k range of a split (a multiple of 64), >= K: no split
   int32_t tiles_m, tiles_n;
   GEpi e;
+};
+template <class T>
+struct GArgs : GShape {
+  GOperand<T> a, b;
 };
 
 __device__ __forceinline__ float g_sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
@@ -223,7 +192,7 @@ struct EpiLinearGrad {
       z[q] = q < left ? r[q] * d : 0.f;
     }
     const int room = e.outp - n;
-    g_store4<T>(e.out, m * e.ld_out + n, room, room >= 4, z);
+    g_store4<T>(e.out, m * e.ld_out + n, room, room >= 4 && g_vec<T>(e.out, e.ld_out), z);
   }
 };
 
@@ -283,8 +252,9 @@ struct EpiGatedGrad {
       u[q] = in ? r[q] * v : 0.f;
     }
     const int room = e.outp - f;
-    g_store4<T>(e.out, m * e.ld_out + f, room, room >= 4, a);
-    g_store4<T>(e.out, m * e.ld_out + e.outp + f, room, room >= 4, u);
+    const bool vec = room >= 4 && g_vec<T>(e.out, e.ld_out) && (e.outp & 3) == 0;
+    g_store4<T>(e.out, m * e.ld_out + f, room, vec, a);
+    g_store4<T>(e.out, m * e.ld_out + e.outp + f, room, vec, u);
   }
 };
 
@@ -331,7 +301,7 @@ struct GTile {
   uint32_t voff[PER];  // byte offset of the lane's 16 bytes from the step's base
   int kch;             // KM: first k of the lane's chunk (the same in every load)
 
-  __device__ __forceinline__ void init(const GOperand& o, int wave, int lane, int upper) {
+  __device__ __forceinline__ void init(const GOperand<uint16_t>& o, int wave, int lane, int upper) {
 #pragma unroll
     for (int q = 0; q < PER; ++q) {
       const int u = wave * PER + q;
@@ -392,102 +362,23 @@ __device__ __forceinline__ void g_tile_of(uint32_t id, uint32_t tm, uint32_t tn,
 
 // Rows of a tile that the epilogue holds in LDS at a time, and the LDS of a block.
 constexpr int g_slab_rows(int bm, int bn) { return bm * (bn + 4) * 4 <= 70000 ? bm : 64; }
-constexpr size_t g_lds_bytes(int planes, int bm, int bn, int bk) {
-  const size_t a = 2 * (size_t)planes * (bm + bn) * bk * 2, b = (size_t)g_slab_rows(bm, bn) * (bn + 4) * 4;
+constexpr size_t g_lds_bytes(int stages, int bm, int bn, int bk) {
+  const size_t a = (size_t)stages * (bm + bn) * bk * 2, b = (size_t)g_slab_rows(bm, bn) * (bn + 4) * 4;
   return a > b ? a : b;
 }
 
-// Block of (BM / WM) x (BN / WN) waves.
-template <class F, bool AKM, bool BKM, int BM, int BN, int BK, int WM, int WN, class Epi, bool SPLIT>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
-    k_gemm16(const GArgs p) {
-  constexpr int NWM = BM / WM, NWN = BN / WN, NW = NWM * NWN, MI = WM / 16, NI = WN / 16;
+// The tile of Z in the waves' accumulators to the output.  zt: the block's LDS.
+template <int BM, int BN, int WM, int WN, class Epi, bool SPLIT>
+__device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[WM / 16][WN / 16], float* zt, uint32_t im,
+                                           int64_t m0, int n0, int bcol, int wm, int wn, int c, int g) {
   constexpr bool GATED = Epi::kGated;
-  typedef GTile<BM, BK, AKM, NW, false> TA;
-  typedef GTile<BN, BK, BKM, NW, GATED> TB;
-  constexpr int kStage = F::P * (TA::kBytes + TB::kBytes);
-  extern __shared__ __align__(1024) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, g = lane >> 4, wm = wave / NWN, wn = wave % NWN;
-  uint32_t im, in;
-  g_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, 8, im, in);
-  const int64_t m0 = (int64_t)im * BM;
-  const int n0 = (int)in * BN;               // tile column of Z
-  const int bcol = GATED ? (int)in * (BN / 2) : n0;  // first column of B that the tile reads
-  const int64_t k_from = SPLIT ? (int64_t)blockIdx.y * p.k_split : 0;
-  const int64_t k_to = SPLIT ? (k_from + p.k_split < p.K ? k_from + p.k_split : p.K) : p.K;
-  const int steps = (int)((k_to - k_from + BK - 1) / BK);
-
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(g_lds_addr(lds));
-  TA ta;
-  TB tb;
-  ta.init(p.a, wave, lane, 0);
-  tb.init(p.b, wave, lane, p.e.halfp);
-
-  auto issue = [&](int t) {
-    const int64_t k0 = k_from + (int64_t)t * BK, kl = k_to - k0;
-    const uint32_t st = lds0 + (t & 1) * kStage;
-#pragma unroll
-    for (int pl = 0; pl < F::P; ++pl) {
-      const uint16_t* a = p.a.p + pl * p.a.plane;
-      const uint16_t* b = p.b.p + pl * p.b.plane;
-      if constexpr (AKM) {
-        ta.issue(a + m0 * p.a.ld + k0, 2 * ((p.a.rows - m0 - 1) * p.a.ld + p.a.cols - k0), kl, st + pl * TA::kBytes, wave);
-      } else {
-        ta.issue(a + k0 * p.a.ld + m0, 2 * ((kl - 1) * p.a.ld + p.a.cols - m0), kl, st + pl * TA::kBytes, wave);
-      }
-      const uint32_t sb = st + F::P * TA::kBytes + pl * TB::kBytes;
-      if constexpr (BKM) {
-        tb.issue(b + (int64_t)bcol * p.b.ld + k0, 2 * ((p.b.rows - bcol - 1) * p.b.ld + p.b.cols - k0), kl, sb, wave);
-      } else {
-        // rows that B has: its k may end before A's padded one
-        const int64_t rl = (p.b.rows < k_to ? p.b.rows : k_to) - k0;
-        tb.issue(b + k0 * p.b.ld + bcol, 2 * ((rl - 1) * p.b.ld + p.b.cols - bcol), rl, sb, wave);
-      }
-    }
-  };
-
-  f32x4 acc[MI][NI];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  issue(0);
-  for (int t = 0; t < steps; ++t) {
-    g_wait_loads();  // this wave's share of the step is in LDS
-    __syncthreads();
-    if (t + 1 < steps) issue(t + 1);
-    const char* sa = lds + (t & 1) * kStage;
-    const char* sb = sa + F::P * TA::kBytes;
-#pragma unroll
-    for (int kb = 0; kb < BK / 32; ++kb) {
-      uint4 fa[F::P][MI], fb[F::P][NI];
-#pragma unroll
-      for (int pl = 0; pl < F::P; ++pl) {
-#pragma unroll
-        for (int j = 0; j < NI; ++j) fb[pl][j] = TB::frag(sb + pl * TB::kBytes, wn * NI + j, kb, c, g);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) fa[pl][i] = TA::frag(sa + pl * TA::kBytes, wm * MI + i, kb, c, g);
-      }
-#pragma unroll
-      for (int s = 0; s < F::NP; ++s)
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-          for (int j = 0; j < NI; ++j)
-            acc[i][j] = g_mfma<F::kF16>(fb[F::pb[s]][j], fa[F::pa[s]][i], acc[i][j]);
-    }
-  }
-
+  constexpr int MI = WM / 16, NI = WN / 16, NW = (BM / WM) * (BN / WN);
   // ---- epilogue: the tile goes through LDS in slabs of SR rows, so that rows
   // are read and written whole; a thread keeps its four columns of Z
   constexpr int SR = g_slab_rows(BM, BN), LDZ = BN + 4, NT = NW * 64;
   constexpr int TC = GATED ? BN / 8 : BN / 4;  // threads side by side
   static_assert(NT % TC == 0, "a thread keeps its columns");
   const GEpi& e = p.e;
-  float* zt = reinterpret_cast<float*>(lds);
-  const float ub = e.ub ? *e.ub : 1.f;
   const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
   const int zc = GATED ? (tc >> 2) * 32 + (tc & 3) * 4 : tc * 4;  // column of the tile (gated: of the gate)
   const int n = GATED ? bcol + tc * 4 : n0 + zc;                  // column of the result (of a half)
@@ -510,19 +401,16 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
       for (int r = tr; r < SR; r += NT / TC) {
         const int64_t m = m0 + s0 + r;
         if (m >= p.M) break;
-        const float ua = e.ua ? e.ua[m] : 1.f;
-        const f32x4 x = split_unscale4(*reinterpret_cast<const f32x4*>(zt + r * LDZ + zc), ua, ub);
+        const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
         if constexpr (SPLIT) {
-          // ld_part and halfp are multiples of 4
           float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
           *reinterpret_cast<f32x4*>(part) = x;
           if constexpr (GATED)
-            *reinterpret_cast<f32x4*>(part + e.halfp) =
-                split_unscale4(*reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16), ua, ub);
+            *reinterpret_cast<f32x4*>(part + e.parth) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
         } else {
           float z[4] = {x[0], x[1], x[2], x[3]};
           if constexpr (GATED) {
-            const f32x4 y = split_unscale4(*reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16), ua, ub);
+            const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
             float u[4] = {y[0], y[1], y[2], y[3]};
             Epi::apply(e, m, n, e.half - n, z, u);
             if constexpr (Epi::kColSum) {
@@ -560,29 +448,262 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
   }
 }
 
-// Sum of the splits in order, then the epilogue; a thread takes four columns of a row.
-template <class Epi>
-__global__ void __launch_bounds__(256) k_gemm16_join(const GArgs p, int splits) {
+// Block of (BM / WM) x (BN / WN) waves.
+template <bool AKM, bool BKM, int BM, int BN, int BK, int WM, int WN, class Epi, bool SPLIT>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
+    k_gemm16(const GArgs<uint16_t> p) {
+  constexpr int NWM = BM / WM, NWN = BN / WN, NW = NWM * NWN, MI = WM / 16, NI = WN / 16;
+  constexpr bool GATED = Epi::kGated;
+  typedef GTile<BM, BK, AKM, NW, false> TA;
+  typedef GTile<BN, BK, BKM, NW, GATED> TB;
+  constexpr int kStage = TA::kBytes + TB::kBytes;
+  extern __shared__ __align__(1024) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4, wm = wave / NWN, wn = wave % NWN;
+  uint32_t im, in;
+  g_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, 8, im, in);
+  const int64_t m0 = (int64_t)im * BM;
+  const int n0 = (int)in * BN;               // tile column of Z
+  const int bcol = GATED ? (int)in * (BN / 2) : n0;  // first column of B that the tile reads
+  const int64_t k_from = SPLIT ? (int64_t)blockIdx.y * p.k_split : 0;
+  const int64_t k_to = SPLIT ? (k_from + p.k_split < p.K ? k_from + p.k_split : p.K) : p.K;
+  const int steps = (int)((k_to - k_from + BK - 1) / BK);
+
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(g_lds_addr(lds));
+  TA ta;
+  TB tb;
+  ta.init(p.a, wave, lane, 0);
+  tb.init(p.b, wave, lane, p.e.halfp);
+
+  auto issue = [&](int t) {
+    const int64_t k0 = k_from + (int64_t)t * BK, kl = k_to - k0;
+    const uint32_t st = lds0 + (t & 1) * kStage;
+    const uint32_t sb = st + TA::kBytes;
+    if constexpr (AKM) {
+      ta.issue(p.a.p + m0 * p.a.ld + k0, 2 * ((p.a.rows - m0 - 1) * p.a.ld + p.a.cols - k0), kl, st, wave);
+    } else {
+      ta.issue(p.a.p + k0 * p.a.ld + m0, 2 * ((kl - 1) * p.a.ld + p.a.cols - m0), kl, st, wave);
+    }
+    if constexpr (BKM) {
+      tb.issue(p.b.p + (int64_t)bcol * p.b.ld + k0, 2 * ((p.b.rows - bcol - 1) * p.b.ld + p.b.cols - k0), kl, sb, wave);
+    } else {
+      // rows that B has: its k may end before A's padded one
+      const int64_t rl = (p.b.rows < k_to ? p.b.rows : k_to) - k0;
+      tb.issue(p.b.p + k0 * p.b.ld + bcol, 2 * ((rl - 1) * p.b.ld + p.b.cols - bcol), rl, sb, wave);
+    }
+  };
+
+  f32x4 acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  issue(0);
+  for (int t = 0; t < steps; ++t) {
+    g_wait_loads();  // this wave's share of the step is in LDS
+    __syncthreads();
+    if (t + 1 < steps) issue(t + 1);
+    const char* sa = lds + (t & 1) * kStage;
+    const char* sb = sa + TA::kBytes;
+#pragma unroll
+    for (int kb = 0; kb < BK / 32; ++kb) {
+      uint4 fa[MI], fb[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) fb[j] = TB::frag(sb, wn * NI + j, kb, c, g);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fa[i] = TA::frag(sa, wm * MI + i, kb, c, g);
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = mfma_bf16(fb[j], fa[i], acc[i][j]);
+    }
+  }
+  g_epilogue<BM, BN, WM, WN, Epi, SPLIT>(p, acc, reinterpret_cast<float*>(lds), im, m0, n0, bcol, wm, wn, c, g);
+}
+
+// ---- float32 operands ------------------------------------------------------------
+// The same product with each float32 value as the sum of three bfloat16 parts
+// (its leading 8 bits, the next 8, the rest) and the six part products of order
+// at most two, so a product term is exact to about 2^-23 of itself.  The parts
+// are made on the way to LDS: a step's tile is loaded into registers while the
+// MFMAs of the step before run.  No scales: any exponent, whatever lies beside
+// it.  Three planes of 32 k a step.  VEC: rows are 16-byte aligned and whole
+// multiples of four values.
+constexpr int kG32K = 32;
+
+// Four values truncated to three parts.
+__device__ __forceinline__ void g_parts3(f32x4 x, uint2 (&p)[3]) {
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    uint32_t u[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      u[v] = __float_as_uint(x[v]);
+      if (k < 2) x[v] -= __uint_as_float(u[v] & 0xFFFF0000u);
+    }
+    p[k] = uint2{__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[2], 0x07060302u)};
+  }
+}
+
+template <int BM, bool KM, int NT, bool GATED, bool VEC>
+struct GTile32 {
+  static constexpr int kPlane = BM * kG32K * 2;      // bytes
+  static constexpr int PER = BM * kG32K / 4 / NT;    // groups of four a thread
+  static constexpr int ACROSS = KM ? kG32K / 4 : BM / 4;
+  static_assert(BM * kG32K / 4 % NT == 0, "whole groups a thread");
+  f32x4 x[PER];
+
+  // first: first row (KM) or column; rows and cols as stored; k0, k_to: the step's range
+  __device__ __forceinline__ void load(const GOperand<float>& o, int64_t first, int64_t k0, int64_t k_to, int upper,
+                                       int half) {
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int id = threadIdx.x + q * NT, r = id / ACROSS, s = id % ACROSS * 4;
+      int64_t row, col, to;
+      if constexpr (KM) {
+        row = first + r;
+        col = k0 + s;
+        to = row < o.rows ? (k_to < o.cols ? k_to : o.cols) : 0;
+      } else {
+        const int gr = s >> 4;
+        row = k0 + r;
+        // gated: 16 columns of each half in turn; `half` columns in each
+        const int64_t f = first + (GATED ? (gr >> 1) * 16 + (s & 15) : s);
+        col = f + (GATED ? (gr & 1) * upper : 0);
+        const int64_t wide = GATED ? half + (gr & 1) * upper : o.cols;
+        to = row < k_to && row < o.rows ? wide : 0;
+      }
+      const float* p = o.p + row * o.ld + col;
+      if (VEC) {
+        x[q] = col < to ? *reinterpret_cast<const f32x4*>(p) : f32x4{0.f, 0.f, 0.f, 0.f};
+      } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x[q][v] = col + v < to ? p[v] : 0.f;
+      }
+    }
+  }
+  // LDS: KM [row][32], the 16-byte chunk ch of row r at ch ^ ((r >> 1) & 3); k rows as in GTile
+  __device__ __forceinline__ void store(char* lds) const {
+#pragma unroll
+    for (int q = 0; q < PER; ++q) {
+      const int id = threadIdx.x + q * NT, r = id / ACROSS, s = id % ACROSS;
+      uint2 p[3];
+      g_parts3(x[q], p);
+      char* at = KM ? lds + r * 64 + (((s >> 1) ^ ((r >> 1) & 3)) * 16) + (s & 1) * 8
+                    : lds + r * (BM * 2) + (((s >> 2) ^ g_swz<BM>(r)) * 32) + (s & 3) * 8;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(at + k * kPlane) = p[k];
+    }
+  }
+  __device__ static __forceinline__ uint4 frag(const char* lds, int i, int c, int g) {
+    if constexpr (KM) {
+      const int row = 16 * i + c;
+      return *reinterpret_cast<const uint4*>(lds + row * 64 + ((g ^ ((c >> 1) & 3)) * 16));
+    } else {
+      return GTile<BM, kG32K, false, 1, false>::frag(lds, i, 0, c, g);
+    }
+  }
+};
+
+template <bool AKM, bool BKM, int BM, int BN, int WM, int WN, class Epi, bool SPLIT, bool VEC>
+__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
+    k_gemm32(const GArgs<float> p) {
+  constexpr int NWN = BN / WN, NT = (BM / WM) * NWN * 64, MI = WM / 16, NI = WN / 16;
+  constexpr bool GATED = Epi::kGated;
+  typedef GTile32<BM, AKM, NT, false, VEC> TA;
+  typedef GTile32<BN, BKM, NT, GATED, VEC> TB;
+  extern __shared__ __align__(1024) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4, wm = wave / NWN, wn = wave % NWN;
+  uint32_t im, in;
+  g_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, 8, im, in);
+  const int64_t m0 = (int64_t)im * BM;
+  const int n0 = (int)in * BN, bcol = GATED ? (int)in * (BN / 2) : n0;
+  const int64_t k_from = SPLIT ? (int64_t)blockIdx.y * p.k_split : 0;
+  const int64_t k_to = SPLIT ? (k_from + p.k_split < p.K ? k_from + p.k_split : p.K) : p.K;
+  f32x4 acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  TA ta;
+  TB tb;
+  ta.load(p.a, m0, k_from, k_to, 0, 0);
+  tb.load(p.b, bcol, k_from, k_to, p.e.halfp, p.e.half);
+  for (int64_t k0 = k_from; k0 < k_to; k0 += kG32K) {
+    __syncthreads();
+    ta.store(lds);
+    tb.store(lds + 3 * TA::kPlane);
+    __syncthreads();
+    if (k0 + kG32K < k_to) {
+      ta.load(p.a, m0, k0 + kG32K, k_to, 0, 0);
+      tb.load(p.b, bcol, k0 + kG32K, k_to, p.e.halfp, p.e.half);
+    }
+    uint4 fa[3][MI], fb[3][NI];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fa[k][i] = TA::frag(lds + k * TA::kPlane, wm * MI + i, c, g);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) fb[k][j] = TB::frag(lds + 3 * TA::kPlane + k * TB::kPlane, wn * NI + j, c, g);
+    }
+    // the smallest part products first
+    constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+    for (int s = 0; s < 6; ++s)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = mfma_bf16(fb[pb[s]][j], fa[pa[s]][i], acc[i][j]);
+  }
+  g_epilogue<BM, BN, WM, WN, Epi, SPLIT>(p, acc, reinterpret_cast<float*>(lds), im, m0, n0, bcol, wm, wn, c, g);
+}
+
+// Sum of the splits, then the epilogue.  SL threads share the splits of four
+// columns of a row (each every SL-th in order, then the SL sums in order).
+template <class Epi, int SL>
+__global__ void __launch_bounds__(256) k_product_join(const GShape p, int splits) {
+  constexpr int QB = 256 / SL, H = Epi::kGated ? 2 : 1;
+  __shared__ f32x4 sh[SL > 1 ? SL : 1][H][SL > 1 ? QB : 1];
   const GEpi& e = p.e;
   const int cols = Epi::kGated ? e.halfp : p.N, quads = (cols + 3) / 4;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, m = id / quads;
-  if (m >= p.M) return;
+  const int q = threadIdx.x % QB, sl = threadIdx.x / QB;
+  const int64_t id = (int64_t)blockIdx.x * QB + q, m = id / quads;
+  const bool in = m < p.M;
   const int n = (int)(id - m * quads) * 4;
-  auto sum = [&](int at, float (&z)[4]) {
-    f32x4 s{0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < splits; ++k) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(e.part + ((int64_t)k * p.M + m) * e.ld_part + at);
+  f32x4 s[H];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) s[v] += x[v];
+  for (int h = 0; h < H; ++h) {
+    s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!in) continue;
+    const float* at = e.part + m * e.ld_part + n + h * e.parth;
+#pragma unroll 8
+    for (int k = sl; k < splits; k += SL) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(at + (int64_t)k * p.M * e.ld_part);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) s[h][v] += x[v];
     }
+  }
+  if constexpr (SL > 1) {
 #pragma unroll
-    for (int v = 0; v < 4; ++v) z[v] = s[v];
-  };
-  float z[4];
-  sum(n, z);
+    for (int h = 0; h < H; ++h) sh[sl][h][q] = s[h];
+    __syncthreads();
+    if (sl > 0) return;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int k = 1; k < SL; ++k) {
+        const f32x4 x = sh[k][h][q];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) s[h][v] += x[v];
+      }
+  }
+  if (!in) return;
+  float z[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
   if constexpr (Epi::kGated) {
-    float u[4];
-    sum(e.halfp + n, u);
+    float u[4] = {s[H - 1][0], s[H - 1][1], s[H - 1][2], s[H - 1][3]};
     Epi::apply(e, m, n, e.half - n, z, u);
   } else {
     Epi::apply(e, m, n, e.ncol - n, z);

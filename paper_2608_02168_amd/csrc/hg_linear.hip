@@ -13,8 +13,8 @@
 //
 // bfloat16 operands are used where they lie when their rows are 16-byte
 // aligned and a multiple of 8 wide; else they are copied once into padded
-// rows.  float32 operands become planes of 16-bit parts first (see the product
-// lists in hg_gemm.h).
+// rows.  float32 operands are always used where they lie (split into parts on
+// the way to LDS).
 #include <atomic>
 
 #include "hg_gemm.h"
@@ -32,14 +32,15 @@ struct Prob {
   int32_t halves() const { return gated ? 2 : 1; }
   int32_t cols() const { return halves() * f; }            // columns of W
   int32_t dp() const { return (d + 7) / 8 * 8; }
-  int32_t fp() const { return (f + 7) / 8 * 8; }
+  int32_t fp() const { return f32() ? f : (f + 7) / 8 * 8; }  // width of a half in operands and in dz
   int32_t colsp() const { return halves() * fp(); }
   bool f32() const { return dtype == HG_DTYPE_F32; }
+  int32_t parth() const { return (fp() + 3) / 4 * 4; }
+  int64_t ld_part() const { return (int64_t)halves() * parth(); }
 };
 
 constexpr int32_t kMaxWidth = 1 << 20;
 constexpr int64_t kMaxLd = 1 << 22;   // 256 rows of 16-bit values stay below 2^31 bytes
-constexpr int kAbsBlocks = 256;       // partial maxima of a matrix
 
 bool direct(int32_t width, int64_t ld) { return width % 8 == 0 && ld % 8 == 0 && ld < kMaxLd; }
 
@@ -49,13 +50,6 @@ bool direct(int32_t width, int64_t ld) { return width % 8 == 0 && ld % 8 == 0 &&
 struct RowShape {
   int32_t F, Fp, halves;
 };
-
-template <class T, class Get>
-__device__ __forceinline__ void p_gather8(const RowShape& r, int j, Get get, float (&v)[8]) {
-  const int h = j >= r.Fp, f = j - h * r.Fp;
-#pragma unroll
-  for (int q = 0; q < 8; ++q) v[q] = f + q < r.F ? get(h * r.F + f + q) : 0.f;
-}
 
 // bfloat16 rows into padded rows; a thread moves eight values.
 __global__ void __launch_bounds__(256)
@@ -72,115 +66,6 @@ __global__ void __launch_bounds__(256)
   uint4 o;
   __builtin_memcpy(&o, v, 16);
   *reinterpret_cast<uint4*>(dst + row * (int64_t)(rs.halves * rs.Fp) + j) = o;
-}
-
-__device__ __forceinline__ float p_mag(float x) {
-  const float m = fabsf(x);
-  return m <= 3.4028234664e38f ? m : 0.f;  // infinities and NaN set no scale
-}
-
-__device__ __forceinline__ void p_store_split(const float (&v)[8], float sc, uint16_t* hi, uint16_t* lo) {
-  float s[8];
-#pragma unroll
-  for (int q = 0; q < 8; ++q) s[q] = v[q] * sc;
-  uint4 h, l;
-  split8(s, h, l);
-  *reinterpret_cast<uint4*>(hi) = h;
-  *reinterpret_cast<uint4*>(lo) = l;
-}
-
-// float32 rows into fp16 high parts and remainders, each row scaled by the
-// power of two of its largest magnitude; ua undoes it.  A wave takes a row.
-__global__ void __launch_bounds__(256)
-    k_rows_split(const float* __restrict__ src, int64_t ld, int64_t rows, RowShape rs, uint16_t* __restrict__ dst,
-                 int64_t plane, float* __restrict__ ua) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const float* x = src + row * ld;
-  const int wide = rs.halves * rs.F, pad = rs.halves * rs.Fp;
-  float m = 0.f;
-  for (int j = lane; j < wide; j += 64) m = fmaxf(m, p_mag(x[j]));
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  const uint32_t eb = split_exp(m);
-  const float sc = split_scale(eb);
-  for (int j = lane * 8; j < pad; j += 512) {
-    float v[8];
-    p_gather8<float>(rs, j, [&](int at) { return x[at]; }, v);
-    p_store_split(v, sc, dst + row * pad + j, dst + plane + row * pad + j);
-  }
-  if (lane == 0) ua[row] = split_unscale(eb);
-}
-
-__device__ __forceinline__ float p_block_max(float m, float* sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
-  __syncthreads();
-  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
-}
-
-// Largest magnitude of a contiguous matrix, one value a block.
-__global__ void __launch_bounds__(256) k_absmax(const float* __restrict__ x, int64_t n, float* __restrict__ part) {
-  __shared__ float sh[4];
-  float m = 0.f;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256)
-    m = fmaxf(m, p_mag(x[i]));
-  m = p_block_max(m, sh);
-  if (threadIdx.x == 0) part[blockIdx.x] = m;
-}
-
-// A contiguous float32 matrix into fp16 high parts and remainders under one scale.
-__global__ void __launch_bounds__(256)
-    k_matrix_split(const float* __restrict__ src, int64_t rows, RowShape rs, const float* __restrict__ part, int parts,
-                   uint16_t* __restrict__ dst, int64_t plane, float* __restrict__ ub) {
-  __shared__ float sh[4];
-  const float m = p_block_max((int)threadIdx.x < parts ? part[threadIdx.x] : 0.f, sh);
-  const uint32_t eb = split_exp(m);
-  const float sc = split_scale(eb);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *ub = split_unscale(eb);
-  const int pad = rs.halves * rs.Fp, chunks = pad / 8;
-  const int64_t n = rows * chunks;
-  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < n; id += (int64_t)gridDim.x * 256) {
-    const int64_t row = id / chunks;
-    const int j = (int)(id - row * chunks) * 8;
-    const float* x = src + row * (int64_t)(rs.halves * rs.F);
-    float v[8];
-    p_gather8<float>(rs, j, [&](int at) { return x[at]; }, v);
-    p_store_split(v, sc, dst + row * pad + j, dst + plane + row * pad + j);
-  }
-}
-
-// float32 rows into three bfloat16 parts (each the rounded rest of the ones
-// before; a non-finite value keeps to the first part).
-__global__ void __launch_bounds__(256)
-    k_rows_split3(const float* __restrict__ src, int64_t ld, int64_t rows, RowShape rs, uint16_t* __restrict__ dst,
-                  int64_t plane) {
-  const int pad = rs.halves * rs.Fp, chunks = pad / 8;
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, row = id / chunks;
-  if (row >= rows) return;
-  const int j = (int)(id - row * chunks) * 8;
-  const float* x = src + row * ld;
-  float v[8];
-  p_gather8<float>(rs, j, [&](int at) { return x[at]; }, v);
-  uint16_t o[3][8];
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    float r = v[q];
-    const bool fine = fabsf(r) < 3.3e38f;  // above, rounding up to bfloat16 could overflow
-#pragma unroll
-    for (int pl = 0; pl < 3; ++pl) {
-      o[pl][q] = fine || pl == 0 ? f2bf(r) : 0;
-      r -= bf2f(o[pl][q]);
-    }
-  }
-#pragma unroll
-  for (int pl = 0; pl < 3; ++pl) {
-    uint4 w;
-    __builtin_memcpy(&w, o[pl], 16);
-    *reinterpret_cast<uint4*>(dst + pl * plane + row * pad + j) = w;
-  }
 }
 
 // ---- column sums --------------------------------------------------------------------
@@ -210,6 +95,7 @@ __global__ void __launch_bounds__(256)
   const int col = blockIdx.x * 16 + cx;
   float s = 0.f;
   if (col < cols)
+#pragma unroll 8
     for (int64_t r = ry; r < parts; r += 16) s += part[r * cols + col];
   sh[ry][cx] = s;
   __syncthreads();
@@ -373,11 +259,8 @@ Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split) {
 
 int64_t part_elems(const Tiling& t, int64_t M, int64_t ld) { return t.splits > 1 ? t.splits * M * ld : 0; }
 
-template <class F, bool AKM, bool BKM, int TILE, class Epi, bool SPLIT>
-int launch_tiles(const char* name, const GArgs& a, const Tiling& t, hipStream_t s) {
-  constexpr int BK = F::P == 3 ? 32 : 64;
-  constexpr size_t lds = g_lds_bytes(F::P, TILE, TILE, BK);
-  auto kern = k_gemm16<F, AKM, BKM, TILE, TILE, BK, TILE / 2, TILE / 2, Epi, SPLIT>;
+template <auto kern>
+int allow_lds(size_t lds) {
   if (lds > 65536) {
     static std::atomic<bool> attr_set{false};
     if (!attr_set.load(std::memory_order_relaxed)) {
@@ -386,8 +269,37 @@ int launch_tiles(const char* name, const GArgs& a, const Tiling& t, hipStream_t 
       attr_set.store(true, std::memory_order_relaxed);
     }
   }
+  return HG_OK;
+}
+
+template <bool AKM, bool BKM, int TILE, class Epi, bool SPLIT>
+int launch_tiles(const char* name, const GArgs<uint16_t>& a, const Tiling& t, hipStream_t s) {
+  constexpr size_t lds = g_lds_bytes(2, TILE, TILE, 64);
+  constexpr auto kern = k_gemm16<AKM, BKM, TILE, TILE, 64, TILE / 2, TILE / 2, Epi, SPLIT>;
+  HG_TRY((allow_lds<kern>(lds)));
   HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(256), lds, s, a);
   return HG_OK;
+}
+
+template <bool AKM, bool BKM, int TILE, class Epi, bool SPLIT, bool VEC>
+int launch_tiles32(const char* name, const GArgs<float>& a, const Tiling& t, hipStream_t s) {
+  constexpr size_t lds = g_lds_bytes(3, TILE, TILE, kG32K);
+  constexpr auto kern = k_gemm32<AKM, BKM, TILE, TILE, TILE / 2, TILE / 2, Epi, SPLIT, VEC>;
+  HG_TRY((allow_lds<kern>(lds)));
+  HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(256), lds, s, a);
+  return HG_OK;
+}
+
+// Whether every group of four values of a float32 operand is 16-byte aligned.
+bool vec4(const GOperand<float>& o) {
+  return (reinterpret_cast<uintptr_t>(o.p) & 15) == 0 && o.ld % 4 == 0 && o.cols % 4 == 0;
+}
+
+template <bool AKM, bool BKM, int TILE, class Epi, bool SPLIT>
+int launch_tiles(const char* name, const GArgs<float>& a, const Tiling& t, hipStream_t s) {
+  if (vec4(a.a) && vec4(a.b) && (!Epi::kGated || a.e.half % 4 == 0))
+    return launch_tiles32<AKM, BKM, TILE, Epi, SPLIT, true>(name, a, t, s);
+  return launch_tiles32<AKM, BKM, TILE, Epi, SPLIT, false>(name, a, t, s);
 }
 
 // The split launch only forms products: one kernel for every epilogue of a form.
@@ -398,26 +310,31 @@ struct EpiPart {
   __device__ static __forceinline__ void apply(const GEpi&, int64_t, int, int, float (&)[4], float (&)[4]) {}
 };
 
-template <class F, bool AKM, bool BKM, class Epi>
-int launch_product(const char* name, GArgs a, const Tiling& t, float* part, int64_t ld_part, hipStream_t s) {
+template <bool AKM, bool BKM, class Epi, class T>
+int launch_product(const char* name, GArgs<T> a, const Tiling& t, float* part, int32_t parth, hipStream_t s) {
   a.tiles_m = (int32_t)t.tiles_m;
   a.tiles_n = (int32_t)t.tiles_n;
   a.k_split = t.k_split;
   if (t.splits == 1) {
-    if (t.tile == 128) return launch_tiles<F, AKM, BKM, 128, Epi, false>(name, a, t, s);
-    return launch_tiles<F, AKM, BKM, 64, Epi, false>(name, a, t, s);
+    if (t.tile == 128) return launch_tiles<AKM, BKM, 128, Epi, false>(name, a, t, s);
+    return launch_tiles<AKM, BKM, 64, Epi, false>(name, a, t, s);
   }
   if constexpr (!Epi::kColSum) {
     typedef EpiPart<Epi::kGated> Part;
     a.e.part = part;
-    a.e.ld_part = ld_part;
+    a.e.parth = parth;
+    a.e.ld_part = (Epi::kGated ? 2 : 1) * (int64_t)parth;
     if (t.tile == 128) {
-      HG_TRY((launch_tiles<F, AKM, BKM, 128, Part, true>(name, a, t, s)));
+      HG_TRY((launch_tiles<AKM, BKM, 128, Part, true>(name, a, t, s)));
     } else {
-      HG_TRY((launch_tiles<F, AKM, BKM, 64, Part, true>(name, a, t, s)));
+      HG_TRY((launch_tiles<AKM, BKM, 64, Part, true>(name, a, t, s)));
     }
-    const int64_t quads = cdiv(Epi::kGated ? a.e.halfp : a.N, 4);
-    HG_LAUNCH("product_join", k_gemm16_join<Epi>, dim3((unsigned)cdiv(a.M * quads, 256)), dim3(256), 0, s, a, t.splits);
+    const int64_t quads = a.M * cdiv(Epi::kGated ? a.e.halfp : a.N, 4);
+    if (t.splits > 8) {
+      HG_LAUNCH("product_join", (k_product_join<Epi, 8>), dim3((unsigned)cdiv(quads, 32)), dim3(256), 0, s, a, t.splits);
+    } else {
+      HG_LAUNCH("product_join", (k_product_join<Epi, 1>), dim3((unsigned)cdiv(quads, 256)), dim3(256), 0, s, a, t.splits);
+    }
   }
   return HG_OK;
 }
@@ -425,18 +342,10 @@ int launch_product(const char* name, GArgs a, const Tiling& t, float* part, int6
 // ---- a call's buffers ---------------------------------------------------------------------
 // The same takes size the workspace and hand it out.
 struct Bufs {
-  uint16_t* x16 = nullptr;   // X padded (bf16) or its two fp16 planes (f32)
-  float* ua = nullptr;       // row factors of X
-  uint16_t* w16 = nullptr;   // W padded or its two fp16 planes
-  float* ub = nullptr;       // W's factor
-  float* wpart = nullptr;    // partial maxima of W
-  float* part = nullptr;     // split products
-  // backward
-  void* dz = nullptr;        // gradient of z in dtype, padded rows
-  uint16_t* dz16 = nullptr;  // its two fp16 planes
-  float* uz = nullptr;       // row factors of dz
-  uint16_t* x3 = nullptr;    // three bfloat16 planes of X and of dz
-  uint16_t* dz3 = nullptr;
+  uint16_t* x16 = nullptr;  // X and W in padded rows (bfloat16 whose rows cannot be used where they lie)
+  uint16_t* w16 = nullptr;
+  void* dz = nullptr;       // gradient of z in dtype
+  float* part = nullptr;    // split products
   float* colsum = nullptr;
   int64_t colsum_rows = 0;
 };
@@ -446,55 +355,44 @@ Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true); }
 Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false); }
 Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true); }
 Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true); }
-bool x_direct(const Prob& p) { return direct(p.d, p.ld_x); }
-bool w_direct(const Prob& p) { return p.f % 8 == 0; }
+bool x_direct(const Prob& p) { return p.f32() || direct(p.d, p.ld_x); }
+bool w_direct(const Prob& p) { return p.f32() || p.f % 8 == 0; }
 bool has_z(const Prob& p) { return p.gated || p.act != HG_ACT_NONE; }
 // the upstream rows are dz itself and can be read where they lie
-bool dz_direct(const Prob& p) { return !has_z(p) && !p.f32() && direct(p.f, p.ld_y); }
+bool dz_direct(const Prob& p) { return !has_z(p) && (p.f32() || direct(p.f, p.ld_y)); }
 
 template <class Mem>
-void take_operands(const Prob& p, bool z, Mem& m, Bufs& b) {
-  if (p.f32()) {
-    if (z) {
-      b.x16 = m.template take<uint16_t>(2 * p.n * p.dp());
-      b.ua = m.template take<float>(p.n);
-    }
-    b.w16 = m.template take<uint16_t>(2 * (int64_t)p.d * p.colsp());
-    b.ub = m.template take<float>(1);
-    b.wpart = m.template take<float>(kAbsBlocks);
-  } else {
-    if (!x_direct(p)) b.x16 = m.template take<uint16_t>(p.n * p.dp());
-    if (!w_direct(p)) b.w16 = m.template take<uint16_t>((int64_t)p.d * p.colsp());
-  }
+void take_operands(const Prob& p, Mem& m, Bufs& b) {
+  if (!x_direct(p)) b.x16 = m.template take<uint16_t>(p.n * p.dp());
+  if (!w_direct(p)) b.w16 = m.template take<uint16_t>((int64_t)p.d * p.colsp());
 }
 
 template <class Mem>
 Bufs take_fwd(const Prob& p, Mem& m) {
   Bufs b;
   if (p.n == 0 || few(p)) return b;
-  take_operands(p, true, m, b);
-  b.part = m.template take<float>(part_elems(t_fwd(p), p.n, p.colsp()));
+  take_operands(p, m, b);
+  b.part = m.template take<float>(part_elems(t_fwd(p), p.n, p.ld_part()));
   return b;
 }
+
+int64_t pad4(int64_t x) { return (x + 3) / 4 * 4; }
 
 template <class Mem>
 Bufs take_bwd(const Prob& p, Mem& m) {
   Bufs b;
   if (p.n == 0) return b;
-  take_operands(p, has_z(p), m, b);
-  const int64_t nz = p.n * p.colsp();
-  if (p.f32()) {
-    if (has_z(p)) b.dz = m.template take<float>(nz);
-    b.dz16 = m.template take<uint16_t>(2 * nz);
-    b.uz = m.template take<float>(p.n);
-    b.x3 = m.template take<uint16_t>(3 * p.n * p.dp());
-    b.dz3 = m.template take<uint16_t>(3 * nz);
-  } else if (!dz_direct(p)) {
-    b.dz = m.template take<uint16_t>(nz);
+  take_operands(p, m, b);
+  if (!dz_direct(p)) {
+    if (p.f32()) {
+      b.dz = m.template take<float>(p.n * p.colsp());
+    } else {
+      b.dz = m.template take<uint16_t>(p.n * p.colsp());
+    }
   }
   b.colsum_rows = has_z(p) ? t_z(p).tiles_m : cdiv(p.n, kSumRows);
   b.colsum = m.template take<float>(b.colsum_rows * p.cols());
-  b.part = m.template take<float>(std::max(part_elems(t_dx(p), p.n, p.dp()), part_elems(t_dw(p), p.d, p.colsp())));
+  b.part = m.template take<float>(std::max(part_elems(t_dx(p), p.n, pad4(p.d)), part_elems(t_dw(p), p.d, pad4(p.colsp()))));
   return b;
 }
 
@@ -538,44 +436,25 @@ int pad_rows(const void* src, int64_t ld, int64_t rows, RowShape rs, uint16_t* d
   return HG_OK;
 }
 
-int split_rows(const void* src, int64_t ld, int64_t rows, RowShape rs, uint16_t* dst, float* ua, hipStream_t s) {
-  HG_LAUNCH("rows_split", k_rows_split, dim3((unsigned)cdiv(rows, 4)), dim3(256), 0, s, static_cast<const float*>(src),
-            ld, rows, rs, dst, rows * (int64_t)(rs.halves * rs.Fp), ua);
-  return HG_OK;
-}
-
-int split3_rows(const void* src, int64_t ld, int64_t rows, RowShape rs, uint16_t* dst, hipStream_t s) {
-  HG_LAUNCH("rows_split3", k_rows_split3, dim3((unsigned)cdiv(rows * (rs.halves * rs.Fp / 8), 256)), dim3(256), 0, s,
-            static_cast<const float*>(src), ld, rows, rs, dst, rows * (int64_t)(rs.halves * rs.Fp));
-  return HG_OK;
-}
-
 RowShape x_shape(const Prob& p) { return RowShape{p.d, p.dp(), 1}; }
 RowShape w_shape(const Prob& p) { return RowShape{p.f, p.fp(), p.halves()}; }
-// dz as the gradient epilogues write it: padded already
-RowShape dz_shape(const Prob& p) { return RowShape{p.fp(), p.fp(), p.halves()}; }
 
-// X as rows of k (bfloat16, or fp16 planes) and W, which serves as k rows and as rows of k.
-int operands(const Prob& p, const void* X, const void* W, bool z, const Bufs& b, GOperand& x, GOperand& w, hipStream_t s) {
-  const int64_t wn = (int64_t)p.d * p.colsp();
-  if (p.f32()) {
-    if (z) HG_TRY(split_rows(X, p.ld_x, p.n, x_shape(p), b.x16, b.ua, s));
-    const int64_t total = (int64_t)p.d * p.cols();
-    const int parts = (int)std::min<int64_t>(kAbsBlocks, cdiv(total, 1024));
-    HG_LAUNCH("absmax", k_absmax, dim3(parts), dim3(256), 0, s, static_cast<const float*>(W), total, b.wpart);
-    HG_LAUNCH("matrix_split", k_matrix_split, dim3((unsigned)std::min<int64_t>(2048, cdiv(wn / 8, 256))), dim3(256), 0, s,
-              static_cast<const float*>(W), (int64_t)p.d, w_shape(p), b.wpart, parts, b.w16, wn, b.ub);
-    x = GOperand{b.x16, p.dp(), p.n * p.dp(), p.n, p.dp()};
-    w = GOperand{b.w16, p.colsp(), wn, p.d, p.colsp()};
-    return HG_OK;
-  }
-  x = GOperand{static_cast<const uint16_t*>(X), p.ld_x, 0, p.n, p.dp()};
+// X as rows of k, and W, which serves as k rows and as rows of k.
+int operands(const Prob& p, const void* X, const void* W, const Bufs&, GOperand<float>& x, GOperand<float>& w, hipStream_t) {
+  x = GOperand<float>{static_cast<const float*>(X), p.ld_x, p.n, p.d};
+  w = GOperand<float>{static_cast<const float*>(W), p.cols(), p.d, p.cols()};
+  return HG_OK;
+}
+
+int operands(const Prob& p, const void* X, const void* W, const Bufs& b, GOperand<bf16_t>& x, GOperand<bf16_t>& w,
+             hipStream_t s) {
+  x = GOperand<bf16_t>{static_cast<const bf16_t*>(X), p.ld_x, p.n, p.dp()};
   if (!x_direct(p)) {
     HG_TRY(pad_rows(X, p.ld_x, p.n, x_shape(p), b.x16, s));
     x.p = b.x16;
     x.ld = p.dp();
   }
-  w = GOperand{static_cast<const uint16_t*>(W), p.colsp(), 0, p.d, p.colsp()};
+  w = GOperand<bf16_t>{static_cast<const bf16_t*>(W), p.colsp(), p.d, p.colsp()};
   if (!w_direct(p)) {
     HG_TRY(pad_rows(W, p.cols(), p.d, w_shape(p), b.w16, s));
     w.p = b.w16;
@@ -598,11 +477,11 @@ GEpi epi_of(const Prob& p, const float* bias, const void* res, int64_t ld_res, v
   return e;
 }
 
-template <class T, class F, bool GATED>
+template <class T, bool GATED>
 int fwd_impl(const Prob& p, const void* X, const void* W, const float* bias, const void* R, void* Y, const Bufs& b,
              hipStream_t s) {
   typedef typename std::conditional<GATED, EpiGated<T>, EpiLinear<T>>::type Epi;
-  GArgs a{};
+  GArgs<T> a{};
   a.e = epi_of(p, bias, R, p.ld_r, Y, p.ld_y);
   if (few(p)) {
     constexpr int LC = 4;
@@ -611,84 +490,62 @@ int fwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
     const T *x = static_cast<const T*>(X), *w = static_cast<const T*>(W);
     return al ? launch_few<T, Epi, LC, true>(p, x, w, a.e, s) : launch_few<T, Epi, LC, false>(p, x, w, a.e, s);
   }
-  HG_TRY(operands(p, X, W, true, b, a.a, a.b, s));
+  HG_TRY(operands(p, X, W, b, a.a, a.b, s));
   a.M = p.n;
   a.N = p.colsp();
-  a.K = p.dp();
-  a.e.ua = b.ua;
-  a.e.ub = b.ub;
-  return launch_product<F, true, false, Epi>(GATED ? "glu" : "linear", a, t_fwd(p), b.part, p.colsp(), s);
+  a.K = a.a.cols;
+  return launch_product<true, false, Epi>(GATED ? "glu" : "linear", a, t_fwd(p), b.part, p.parth(), s);
 }
 
-template <class T, class FR, class FT, bool GATED>
+template <class T, bool GATED>
 int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, const void* dY, void* dX, int64_t ld_dx,
              void* dW, float* dbias, int accumulate, const Bufs& b, hipStream_t s) {
   typedef typename std::conditional<GATED, EpiGatedGrad<T>, EpiLinearGrad<T>>::type EpiG;
-  constexpr bool kF32 = sizeof(T) == 4;
-  GOperand x{}, w{};
-  HG_TRY(operands(p, X, W, has_z(p), b, x, w, s));
+  GOperand<T> x{}, w{};
+  HG_TRY(operands(p, X, W, b, x, w, s));
   // dz, in rows of colsp (or where the upstream rows lie)
-  const void* dz = dY;
-  int64_t ld_dz = p.ld_y;
-  RowShape zs = w_shape(p);
+  GOperand<T> z{static_cast<const T*>(b.dz), p.colsp(), p.n, p.colsp()};
   if (has_z(p)) {
-    GArgs a{};
+    GArgs<T> a{};
     a.a = x;
     a.b = w;
     a.M = p.n;
     a.N = p.colsp();
-    a.K = p.dp();
+    a.K = x.cols;
     a.e = epi_of(p, bias, dY, p.ld_y, b.dz, p.colsp());
-    a.e.ua = b.ua;
-    a.e.ub = b.ub;
     a.e.colsum = dbias ? b.colsum : nullptr;
     a.e.ld_colsum = p.cols();
-    HG_TRY((launch_product<FR, true, false, EpiG>(GATED ? "glu_dz" : "linear_dz", a, t_z(p), nullptr, 0, s)));
-    dz = b.dz;
-    ld_dz = p.colsp();
-    zs = dz_shape(p);
-  } else if (dbias) {
-    HG_LAUNCH("colsum", k_colsum<T>, dim3((unsigned)b.colsum_rows, (unsigned)cdiv(p.cols(), 64)), dim3(256), 0, s, dY,
-              p.ld_y, p.n, p.cols(), b.colsum);
+    HG_TRY((launch_product<true, false, EpiG>(GATED ? "glu_dz" : "linear_dz", a, t_z(p), nullptr, 0, s)));
+  } else {
+    if (dbias)
+      HG_LAUNCH("colsum", k_colsum<T>, dim3((unsigned)b.colsum_rows, (unsigned)cdiv(p.cols(), 64)), dim3(256), 0, s, dY,
+                p.ld_y, p.n, p.cols(), b.colsum);
+    if (dz_direct(p)) {
+      z.p = static_cast<const T*>(dY);
+      z.ld = p.ld_y;
+    } else {
+      HG_TRY(pad_rows(dY, p.ld_y, p.n, w_shape(p), static_cast<uint16_t*>(b.dz), s));
+    }
   }
   if (dbias)
     HG_LAUNCH("colsum_join", k_colsum_join, dim3((unsigned)cdiv(p.cols(), 16)), dim3(256), 0, s, b.colsum, b.colsum_rows,
               p.cols(), dbias, accumulate);
-  GOperand z{static_cast<const uint16_t*>(dz), ld_dz, 0, p.n, p.colsp()};
-  if (!kF32 && !has_z(p) && !dz_direct(p)) {
-    uint16_t* out = static_cast<uint16_t*>(b.dz);
-    HG_TRY(pad_rows(dY, p.ld_y, p.n, zs, out, s));
-    z.p = out;
-    z.ld = p.colsp();
-  }
   if (dX) {
-    GArgs a{};
+    GArgs<T> a{};
     a.a = z;
     a.b = w;
-    if constexpr (kF32) {
-      HG_TRY(split_rows(dz, ld_dz, p.n, zs, b.dz16, b.uz, s));
-      a.a = GOperand{b.dz16, p.colsp(), p.n * p.colsp(), p.n, p.colsp()};
-    }
     a.M = p.n;
     a.N = p.d;
     a.K = p.colsp();
-    a.e.ua = b.uz;
-    a.e.ub = b.ub;
     a.e.out = dX;
     a.e.ld_out = ld_dx;
     a.e.ncol = p.d;
-    HG_TRY((launch_product<FR, true, true, EpiSum<T>>(GATED ? "glu_dx" : "linear_dx", a, t_dx(p), b.part, p.dp(), s)));
+    HG_TRY((launch_product<true, true, EpiSum<T>>(GATED ? "glu_dx" : "linear_dx", a, t_dx(p), b.part, (int32_t)pad4(p.d), s)));
   }
   if (dW) {
-    GArgs a{};
+    GArgs<T> a{};
     a.a = x;
     a.b = z;
-    if constexpr (kF32) {
-      HG_TRY(split3_rows(X, p.ld_x, p.n, x_shape(p), b.x3, s));
-      HG_TRY(split3_rows(dz, ld_dz, p.n, zs, b.dz3, s));
-      a.a = GOperand{b.x3, p.dp(), p.n * p.dp(), p.n, p.dp()};
-      a.b = GOperand{b.dz3, p.colsp(), p.n * p.colsp(), p.n, p.colsp()};
-    }
     a.M = p.d;
     a.N = p.colsp();
     a.K = p.n;
@@ -700,7 +557,8 @@ int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
       a.e.halfp = p.fp();
     }
     a.e.accumulate = accumulate;
-    HG_TRY((launch_product<FT, false, false, EpiSum<T>>(GATED ? "glu_dw" : "linear_dw", a, t_dw(p), b.part, p.colsp(), s)));
+    HG_TRY((launch_product<false, false, EpiSum<T>>(GATED ? "glu_dw" : "linear_dw", a, t_dw(p), b.part,
+                                                    (int32_t)pad4(p.colsp()), s)));
   }
   return HG_OK;
 }
@@ -745,10 +603,10 @@ int forward(const Prob& p, const char* what, const void* X, const void* W, const
   Arena m(ws, ws_bytes);
   const Bufs b = take_fwd(p, m);
   if (p.f32())
-    return p.gated ? fwd_impl<float, GF16x2, true>(p, X, W, bias, R, Y, b, s)
-                   : fwd_impl<float, GF16x2, false>(p, X, W, bias, R, Y, b, s);
-  return p.gated ? fwd_impl<bf16_t, GBf16, true>(p, X, W, bias, R, Y, b, s)
-                 : fwd_impl<bf16_t, GBf16, false>(p, X, W, bias, R, Y, b, s);
+    return p.gated ? fwd_impl<float, true>(p, X, W, bias, R, Y, b, s)
+                   : fwd_impl<float, false>(p, X, W, bias, R, Y, b, s);
+  return p.gated ? fwd_impl<bf16_t, true>(p, X, W, bias, R, Y, b, s)
+                 : fwd_impl<bf16_t, false>(p, X, W, bias, R, Y, b, s);
 }
 
 int backward(const Prob& p, const char* what, const void* X, const void* W, const float* bias, const void* dY, void* dX,
@@ -782,10 +640,10 @@ int backward(const Prob& p, const char* what, const void* X, const void* W, cons
   Arena m(ws, ws_bytes);
   const Bufs b = take_bwd(p, m);
   if (p.f32())
-    return p.gated ? bwd_impl<float, GF16x2, GBf16x3, true>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s)
-                   : bwd_impl<float, GF16x2, GBf16x3, false>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s);
-  return p.gated ? bwd_impl<bf16_t, GBf16, GBf16, true>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s)
-                 : bwd_impl<bf16_t, GBf16, GBf16, false>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s);
+    return p.gated ? bwd_impl<float, true>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s)
+                   : bwd_impl<float, false>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s);
+  return p.gated ? bwd_impl<bf16_t, true>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s)
+                 : bwd_impl<bf16_t, false>(p, X, W, bias, dY, dX, p.ld_r, dW, dbias, accumulate, b, s);
 }
 
 Prob prob_of(const hg_linear_desc* L) {

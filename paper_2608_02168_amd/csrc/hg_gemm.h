@@ -78,7 +78,7 @@ struct GArgs : GShape {
   GOperand<T> a, b;
 };
 
-__device__ __forceinline__ float g_sigmoid(float z) { return 1.f / (1.f + expf(-z)); }
+__device__ __forceinline__ float g_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + expf(-z)); }
 
 // act(z) and, with G, act'(z); the choice is the same for the whole launch
 template <bool G>
@@ -159,15 +159,24 @@ __device__ __forceinline__ bool g_vec(const void* p, int64_t ld) {
 }
 
 // ---- epilogues: rows m, columns n .. n + 3 of Z --------------------------------
-// Each replaces z by what it wrote (for the column sums).
+// `load` reads what a row's output needs beside z, `apply` writes the
+// output and replaces z by what it wrote (for the column sums).
+template <class T>
+__device__ __forceinline__ void g_load_res(const GEpi& e, int64_t m, int n, int left, float (&r)[4]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) r[q] = 0.f;
+  if (left > 0) g_load4<T>(e.res, m * e.ld_res + n, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+}
 
 // out = act(z + bias) + res
 template <class T>
 struct EpiLinear {
   static constexpr bool kGated = false, kColSum = false;
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4]) {
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-    if (e.res) g_load4<T>(e.res, m * e.ld_res + n, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+  __device__ static __forceinline__ void load(const GEpi& e, int64_t m, int n, int left, float (&r)[4]) {
+    g_load_res<T>(e, m, n, e.res ? left : 0, r);
+  }
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4],
+                                               const float (&r)[4]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float b = e.bias && q < left ? e.bias[n + q] : 0.f;
@@ -181,9 +190,11 @@ struct EpiLinear {
 template <class T>
 struct EpiLinearGrad {
   static constexpr bool kGated = false, kColSum = true;
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4]) {
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-    if (left > 0) g_load4<T>(e.res, m * e.ld_res + n, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+  __device__ static __forceinline__ void load(const GEpi& e, int64_t m, int n, int left, float (&r)[4]) {
+    g_load_res<T>(e, m, n, left, r);
+  }
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4],
+                                               const float (&r)[4]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float b = e.bias && q < left ? e.bias[n + q] : 0.f;
@@ -200,7 +211,9 @@ struct EpiLinearGrad {
 template <class T>
 struct EpiSum {
   static constexpr bool kGated = false, kColSum = false;
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4]) {
+  __device__ static __forceinline__ void load(const GEpi&, int64_t, int, int, float (&)[4]) {}
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4],
+                                               const float (&)[4]) {
     if (e.half) {
       // halfp is a multiple of 8, so four columns lie in one half
       const int up = n >= e.halfp;
@@ -223,7 +236,9 @@ struct EpiSum {
 template <class T>
 struct EpiGated {
   static constexpr bool kGated = true, kColSum = false;
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4]) {
+  __device__ static __forceinline__ void load(const GEpi&, int64_t, int, int, float (&)[4]) {}
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4],
+                                               const float (&)[4]) {
     if (left <= 0) return;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -238,9 +253,11 @@ struct EpiGated {
 template <class T>
 struct EpiGatedGrad {
   static constexpr bool kGated = true, kColSum = true;
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4]) {
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-    if (left > 0) g_load4<T>(e.res, m * e.ld_res + f, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+  __device__ static __forceinline__ void load(const GEpi& e, int64_t m, int f, int left, float (&r)[4]) {
+    g_load_res<T>(e, m, f, left, r);
+  }
+  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4],
+                                               const float (&r)[4]) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const bool in = q < left;
@@ -398,30 +415,45 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
     }
     __syncthreads();
     if (in_n) {
-      for (int r = tr; r < SR; r += NT / TC) {
-        const int64_t m = m0 + s0 + r;
-        if (m >= p.M) break;
-        const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
-        if constexpr (SPLIT) {
-          float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
-          *reinterpret_cast<f32x4*>(part) = x;
-          if constexpr (GATED)
-            *reinterpret_cast<f32x4*>(part + e.parth) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
-        } else {
-          float z[4] = {x[0], x[1], x[2], x[3]};
-          if constexpr (GATED) {
-            const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
-            float u[4] = {y[0], y[1], y[2], y[3]};
-            Epi::apply(e, m, n, e.half - n, z, u);
-            if constexpr (Epi::kColSum) {
+      // four rows at a time: what they need beside z is in flight together
+      constexpr int STEP = NT / TC, U = SR / STEP < 4 ? SR / STEP : 4;
+      const int left = GATED ? e.half - n : e.ncol - n;
+      for (int r0 = tr; r0 < SR; r0 += U * STEP) {
+        float res[U][4];
+        if constexpr (!SPLIT) {
 #pragma unroll
-              for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
-            }
+          for (int i = 0; i < U; ++i) {
+            const int64_t m = m0 + s0 + r0 + i * STEP;
+            Epi::load(e, m < p.M ? m : p.M - 1, n, left, res[i]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const int r = r0 + i * STEP;
+          const int64_t m = m0 + s0 + r;
+          if (m >= p.M) break;
+          const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
+          if constexpr (SPLIT) {
+            float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
+            *reinterpret_cast<f32x4*>(part) = x;
+            if constexpr (GATED)
+              *reinterpret_cast<f32x4*>(part + e.parth) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
           } else {
-            Epi::apply(e, m, n, e.ncol - n, z);
-            if constexpr (Epi::kColSum) {
+            float z[4] = {x[0], x[1], x[2], x[3]};
+            if constexpr (GATED) {
+              const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
+              float u[4] = {y[0], y[1], y[2], y[3]};
+              Epi::apply(e, m, n, left, z, u, res[i]);
+              if constexpr (Epi::kColSum) {
 #pragma unroll
-              for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
+                for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
+              }
+            } else {
+              Epi::apply(e, m, n, left, z, res[i]);
+              if constexpr (Epi::kColSum) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
+              }
             }
           }
         }
@@ -701,12 +733,14 @@ __global__ void __launch_bounds__(256) k_product_join(const GShape p, int splits
       }
   }
   if (!in) return;
-  float z[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
+  float z[4] = {s[0][0], s[0][1], s[0][2], s[0][3]}, r[4];
+  const int left = Epi::kGated ? e.half - n : e.ncol - n;
+  Epi::load(e, m, n, left, r);
   if constexpr (Epi::kGated) {
     float u[4] = {s[H - 1][0], s[H - 1][1], s[H - 1][2], s[H - 1][3]};
-    Epi::apply(e, m, n, e.half - n, z, u);
+    Epi::apply(e, m, n, left, z, u, r);
   } else {
-    Epi::apply(e, m, n, e.ncol - n, z);
+    Epi::apply(e, m, n, left, z, r);
   }
 }
 

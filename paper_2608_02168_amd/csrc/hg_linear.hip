@@ -204,10 +204,12 @@ __global__ void __launch_bounds__(kFewWaves * 64)
         for (int w = 0; w < kFewWaves; ++w) s += sh[w][h][r][cc + q];
         z[h][q] = s;
       }
+    float res[4];
+    Epi::load(e, r, n, f - n, res);
     if constexpr (Epi::kGated) {
-      Epi::apply(e, r, n, f - n, z[0], z[1]);
+      Epi::apply(e, r, n, f - n, z[0], z[1], res);
     } else {
-      Epi::apply(e, r, n, f - n, z[0]);
+      Epi::apply(e, r, n, f - n, z[0], res);
     }
   }
 }
@@ -243,9 +245,13 @@ struct Tiling {
 // Tiles of 128 x 128 where they fill half the chip, else 64 x 64; the k range
 // is split over blocks while the tiles do not fill it (never where column
 // sums are formed on the way).
-Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split) {
+Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32) {
   Tiling t{};
   const int64_t big = cdiv(M, 128) * cdiv(cols, 128);
+  if (!f32 && cdiv(M, 256) * cdiv(cols, 256) >= 192) {
+    t = Tiling{256, cdiv(M, 256), cdiv(cols, 256), 1, cdiv(std::max<int64_t>(K, 1), 64) * 64};
+    return t;
+  }
   t.tile = big >= 128 || (may_split && big * (K / 512) >= 128) ? 128 : 64;
   t.tiles_m = cdiv(M, t.tile);
   t.tiles_n = cdiv(cols, t.tile);
@@ -275,9 +281,10 @@ int allow_lds(size_t lds) {
 template <bool AKM, bool BKM, int TILE, class Epi, bool SPLIT>
 int launch_tiles(const char* name, const GArgs<uint16_t>& a, const Tiling& t, hipStream_t s) {
   constexpr size_t lds = g_lds_bytes(2, TILE, TILE, 64);
-  constexpr auto kern = k_gemm16<AKM, BKM, TILE, TILE, 64, TILE / 2, TILE / 2, Epi, SPLIT>;
+  constexpr int WN = TILE == 256 ? 64 : TILE / 2, NT = 2 * (TILE / WN) * 64;
+  constexpr auto kern = k_gemm16<AKM, BKM, TILE, TILE, 64, TILE / 2, WN, Epi, SPLIT>;
   HG_TRY((allow_lds<kern>(lds)));
-  HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(256), lds, s, a);
+  HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(NT), lds, s, a);
   return HG_OK;
 }
 
@@ -306,8 +313,6 @@ int launch_tiles(const char* name, const GArgs<float>& a, const Tiling& t, hipSt
 template <bool GATED>
 struct EpiPart {
   static constexpr bool kGated = GATED, kColSum = false;
-  __device__ static __forceinline__ void apply(const GEpi&, int64_t, int, int, float (&)[4]) {}
-  __device__ static __forceinline__ void apply(const GEpi&, int64_t, int, int, float (&)[4], float (&)[4]) {}
 };
 
 template <bool AKM, bool BKM, class Epi, class T>
@@ -316,6 +321,8 @@ int launch_product(const char* name, GArgs<T> a, const Tiling& t, float* part, i
   a.tiles_n = (int32_t)t.tiles_n;
   a.k_split = t.k_split;
   if (t.splits == 1) {
+    if constexpr (sizeof(T) == 2)
+      if (t.tile == 256) return launch_tiles<AKM, BKM, 256, Epi, false>(name, a, t, s);
     if (t.tile == 128) return launch_tiles<AKM, BKM, 128, Epi, false>(name, a, t, s);
     return launch_tiles<AKM, BKM, 64, Epi, false>(name, a, t, s);
   }
@@ -351,10 +358,10 @@ struct Bufs {
 };
 
 bool few(const Prob& p) { return p.n <= kFewRows; }
-Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true); }
-Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false); }
-Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true); }
-Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true); }
+Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true, p.f32()); }
+Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false, p.f32()); }
+Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true, p.f32()); }
+Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true, p.f32()); }
 bool x_direct(const Prob& p) { return p.f32() || direct(p.d, p.ld_x); }
 bool w_direct(const Prob& p) { return p.f32() || p.f % 8 == 0; }
 bool has_z(const Prob& p) { return p.gated || p.act != HG_ACT_NONE; }

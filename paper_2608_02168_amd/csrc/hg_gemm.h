@@ -33,6 +33,7 @@
 namespace hg {
 
 typedef short g_s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 g_bf16x4 __attribute__((ext_vector_type(4)));
 
 // One operand.  KM: `rows` rows (m or n) of K values; else K rows of `cols`
 // values.  ld in elements.  bfloat16: p 16-byte aligned, ld, K (KM) or cols
@@ -78,33 +79,70 @@ struct GArgs : GShape {
   GOperand<T> a, b;
 };
 
-__device__ __forceinline__ float g_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + expf(-z)); }
-
-// act(z) and, with G, act'(z); the choice is the same for the whole launch
-template <bool G>
-__device__ __forceinline__ float g_act(int act, float z, float& d) {
-  switch (act) {
-    case HG_ACT_RELU:
-      if (G) d = z > 0.f ? 1.f : (z != z ? z : 0.f);
-      return z > 0.f ? z : (z != z ? z : 0.f);
-    case HG_ACT_SILU: {
-      const float s = g_sigmoid(z);
-      if (G) d = s * (1.f + z * (1.f - s));
-      return z * s;
-    }
-    case HG_ACT_GELU: {
-      const float p = 0.5f * (1.f + erff(z * 0.70710678118654752f));
-      if (G) d = p + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-      return z * p;
-    }
-    default:
-      if (G) d = 1.f;
-      return z;
+// exp, the sigmoid and Phi(z) = (1 + erf(z / sqrt 2)) / 2 with e = exp(-z^2 / 2).
+// float32 results take the library functions; results that are rounded to
+// bfloat16 take the hardware's exponential (relative error below 2^-18 for
+// |x| <= 32) and erf by the rational approximation 7.1.26 of Abramowitz and
+// Stegun (absolute error 1.5e-7): a float32 epilogue of 256 x 256 values cost
+// 35 us of a tile's time, this one 9.
+template <class T>
+__device__ __forceinline__ float g_exp(float x) {
+  if constexpr (sizeof(T) == 4) {
+    return expf(x);
+  } else {
+    return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
   }
 }
-__device__ __forceinline__ float g_act(int act, float z) {
-  float d;
-  return g_act<false>(act, z, d);
+
+template <class T>
+__device__ __forceinline__ float g_sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.f + g_exp<T>(-z));
+}
+
+template <class T>
+__device__ __forceinline__ float g_phi(float z, float e) {
+  if constexpr (sizeof(T) == 4) {
+    return 0.5f * (1.f + erff(z * 0.70710678118654752f));
+  } else {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * q * e;  // (1 - erf(|z| / sqrt 2)) / 2
+    return z < 0.f ? tail : 1.f - tail;
+  }
+}
+
+// act of four values and, with G, its slopes; the choice is the same for the whole launch
+template <class T, bool G>
+__device__ __forceinline__ void g_act4(int act, const float (&z)[4], float (&f)[4], float (&d)[4]) {
+  if (act == HG_ACT_SILU) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float s = g_sigmoid<T>(z[q]);
+      f[q] = z[q] * s;
+      if (G) d[q] = fmaf(f[q], 1.f - s, s);
+    }
+  } else if (act == HG_ACT_GELU) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float e = sizeof(T) == 2 || G ? g_exp<T>(-0.5f * z[q] * z[q]) : 0.f, p = g_phi<T>(z[q], e);
+      f[q] = z[q] * p;
+      if (G) d[q] = fmaf(z[q] * e, 0.39894228040143268f, p);
+    }
+  } else if (act == HG_ACT_RELU) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const bool nan = z[q] != z[q];
+      f[q] = z[q] > 0.f || nan ? z[q] : 0.f;
+      if (G) d[q] = nan ? z[q] : z[q] > 0.f ? 1.f : 0.f;
+    }
+  } else {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      f[q] = z[q];
+      if (G) d[q] = 1.f;
+    }
+  }
 }
 
 template <class T>
@@ -143,7 +181,7 @@ __device__ __forceinline__ void g_store4(void* p, int64_t at, int n, bool vec, c
   } else {
     uint16_t* o = static_cast<uint16_t*>(p) + at;
     if (vec) {
-      *reinterpret_cast<uint2*>(o) = uint2{pack2bf(v[0], v[1]), pack2bf(v[2], v[3])};
+      *reinterpret_cast<uint2*>(o) = __builtin_bit_cast(uint2, __builtin_convertvector((f32x4{v[0], v[1], v[2], v[3]}), g_bf16x4));
     } else {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
@@ -159,30 +197,55 @@ __device__ __forceinline__ bool g_vec(const void* p, int64_t ld) {
 }
 
 // ---- epilogues: rows m, columns n .. n + 3 of Z --------------------------------
-// `load` reads what a row's output needs beside z, `apply` writes the
-// output and replaces z by what it wrote (for the column sums).
+// `cols` is made once for a thread's columns; `load` reads what a row's output
+// needs beside z; `apply` writes the output and replaces z by what it wrote (for
+// the column sums).
+struct GCols {
+  int n, left;       // first column, columns from there on that exist
+  int out;           // column of the output
+  bool vr, vo, vo2;  // groups of four of res and of the output (of both halves) can be moved at once
+  float b[4], b2[4];
+};
+
 template <class T>
-__device__ __forceinline__ void g_load_res(const GEpi& e, int64_t m, int n, int left, float (&r)[4]) {
+__device__ __forceinline__ GCols g_cols(const GEpi& e, int n, int left, bool gated) {
+  GCols c;
+  c.n = c.out = n;
+  c.left = left;
+  c.vr = left >= 4 && g_vec<T>(e.res, e.ld_res);
+  c.vo = left >= 4 && g_vec<T>(e.out, e.ld_out);
+  c.vo2 = false;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    c.b[q] = e.bias && q < left ? e.bias[n + q] : 0.f;
+    c.b2[q] = gated && e.bias && q < left ? e.bias[e.half + n + q] : 0.f;
+  }
+  return c;
+}
+
+template <class T>
+__device__ __forceinline__ void g_load_res(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) r[q] = 0.f;
-  if (left > 0) g_load4<T>(e.res, m * e.ld_res + n, left, left >= 4 && g_vec<T>(e.res, e.ld_res), r);
+  if (e.res) g_load4<T>(e.res, m * e.ld_res + c.n, c.left, c.vr, r);
 }
 
 // out = act(z + bias) + res
 template <class T>
 struct EpiLinear {
   static constexpr bool kGated = false, kColSum = false;
-  __device__ static __forceinline__ void load(const GEpi& e, int64_t m, int n, int left, float (&r)[4]) {
-    g_load_res<T>(e, m, n, e.res ? left : 0, r);
+  __device__ static __forceinline__ GCols cols(const GEpi& e, int n) { return g_cols<T>(e, n, e.ncol - n, false); }
+  __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
+    g_load_res<T>(e, c, m, r);
   }
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4],
-                                               const float (&r)[4]) {
+  __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&z)[4], const float (&r)[4]) {
+    float f[4], d[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float b = e.bias && q < left ? e.bias[n + q] : 0.f;
-      z[q] = g_act(e.act, z[q] + b) + r[q];
-    }
-    g_store4<T>(e.out, m * e.ld_out + n, left, left >= 4 && g_vec<T>(e.out, e.ld_out), z);
+    for (int q = 0; q < 4; ++q) z[q] += c.b[q];
+    g_act4<T, false>(e.act, z, f, d);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f[q] += r[q];
+    g_store4<T>(e.out, m * e.ld_out + c.n, c.left, c.vo, f);
   }
 };
 
@@ -190,20 +253,22 @@ struct EpiLinear {
 template <class T>
 struct EpiLinearGrad {
   static constexpr bool kGated = false, kColSum = true;
-  __device__ static __forceinline__ void load(const GEpi& e, int64_t m, int n, int left, float (&r)[4]) {
-    g_load_res<T>(e, m, n, left, r);
+  __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
+    GCols c = g_cols<T>(e, n, e.ncol - n, false);
+    c.vo = e.outp - n >= 4 && g_vec<T>(e.out, e.ld_out);
+    return c;
   }
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4],
-                                               const float (&r)[4]) {
+  __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
+    g_load_res<T>(e, c, m, r);
+  }
+  __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&z)[4], const float (&r)[4]) {
+    float f[4], d[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float b = e.bias && q < left ? e.bias[n + q] : 0.f;
-      float d;
-      g_act<true>(e.act, z[q] + b, d);
-      z[q] = q < left ? r[q] * d : 0.f;
-    }
-    const int room = e.outp - n;
-    g_store4<T>(e.out, m * e.ld_out + n, room, room >= 4 && g_vec<T>(e.out, e.ld_out), z);
+    for (int q = 0; q < 4; ++q) z[q] += c.b[q];
+    g_act4<T, true>(e.act, z, f, d);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) z[q] = q < c.left ? r[q] * d[q] : 0.f;
+    g_store4<T>(e.out, m * e.ld_out + c.n, e.outp - c.n, c.vo, z);
   }
 };
 
@@ -211,24 +276,29 @@ struct EpiLinearGrad {
 template <class T>
 struct EpiSum {
   static constexpr bool kGated = false, kColSum = false;
-  __device__ static __forceinline__ void load(const GEpi&, int64_t, int, int, float (&)[4]) {}
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int n, int left, float (&z)[4],
-                                               const float (&)[4]) {
+  __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
+    GCols c;
+    c.n = c.out = n;
+    c.left = e.ncol - n;
     if (e.half) {
       // halfp is a multiple of 8, so four columns lie in one half
-      const int up = n >= e.halfp;
-      left = e.half - (n - (up ? e.halfp : 0));
-      n += up ? e.half - e.halfp : 0;
-      if (left <= 0) return;
+      const bool up = n >= e.halfp;
+      c.left = e.half - (n - (up ? e.halfp : 0));
+      c.out = n + (up ? e.half - e.halfp : 0);
     }
-    const bool vec = left >= 4 && g_vec<T>(e.out, e.ld_out) && (n & 3) == 0;
+    c.vo = c.left >= 4 && g_vec<T>(e.out, e.ld_out) && (c.out & 3) == 0;
+    return c;
+  }
+  __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
+    if (e.accumulate) g_load4<T>(e.out, m * e.ld_out + c.out, c.left, c.vo, r);
+  }
+  __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&z)[4], const float (&r)[4]) {
+    if (c.left <= 0) return;
     if (e.accumulate) {
-      float r[4];
-      g_load4<T>(e.out, m * e.ld_out + n, left, vec, r);
 #pragma unroll
       for (int q = 0; q < 4; ++q) z[q] += r[q];
     }
-    g_store4<T>(e.out, m * e.ld_out + n, left, vec, z);
+    g_store4<T>(e.out, m * e.ld_out + c.out, c.left, c.vo, z);
   }
 };
 
@@ -236,16 +306,18 @@ struct EpiSum {
 template <class T>
 struct EpiGated {
   static constexpr bool kGated = true, kColSum = false;
-  __device__ static __forceinline__ void load(const GEpi&, int64_t, int, int, float (&)[4]) {}
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4],
+  __device__ static __forceinline__ GCols cols(const GEpi& e, int n) { return g_cols<T>(e, n, e.half - n, true); }
+  __device__ static __forceinline__ void load(const GEpi&, const GCols&, int64_t, float (&)[4]) {}
+  __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&a)[4], float (&u)[4],
                                                const float (&)[4]) {
-    if (left <= 0) return;
+    if (c.left <= 0) return;
+    float f[4], d[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const bool in = e.bias && q < left;
-      a[q] = g_act(e.act, a[q] + (in ? e.bias[f + q] : 0.f)) * (u[q] + (in ? e.bias[e.half + f + q] : 0.f));
-    }
-    g_store4<T>(e.out, m * e.ld_out + f, left, left >= 4 && g_vec<T>(e.out, e.ld_out), a);
+    for (int q = 0; q < 4; ++q) a[q] += c.b[q];
+    g_act4<T, false>(e.act, a, f, d);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f[q] *= u[q] + c.b2[q];
+    g_store4<T>(e.out, m * e.ld_out + c.n, c.left, c.vo, f);
   }
 };
 
@@ -253,25 +325,29 @@ struct EpiGated {
 template <class T>
 struct EpiGatedGrad {
   static constexpr bool kGated = true, kColSum = true;
-  __device__ static __forceinline__ void load(const GEpi& e, int64_t m, int f, int left, float (&r)[4]) {
-    g_load_res<T>(e, m, f, left, r);
+  __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
+    GCols c = g_cols<T>(e, n, e.half - n, true);
+    c.vo = e.outp - n >= 4 && g_vec<T>(e.out, e.ld_out) && (e.outp & 3) == 0;
+    return c;
   }
-  __device__ static __forceinline__ void apply(const GEpi& e, int64_t m, int f, int left, float (&a)[4], float (&u)[4],
+  __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
+    g_load_res<T>(e, c, m, r);
+  }
+  __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&a)[4], float (&u)[4],
                                                const float (&r)[4]) {
+    float f[4], d[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) a[q] += c.b[q];
+    g_act4<T, true>(e.act, a, f, d);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const bool in = q < left;
-      const float ba = e.bias && in ? e.bias[f + q] : 0.f, bu = e.bias && in ? e.bias[e.half + f + q] : 0.f;
-      float d;
-      const float v = g_act<true>(e.act, a[q] + ba, d);
-      const float w = u[q] + bu;
-      a[q] = in ? r[q] * w * d : 0.f;
-      u[q] = in ? r[q] * v : 0.f;
+      const bool in = q < c.left;
+      a[q] = in ? r[q] * (u[q] + c.b2[q]) * d[q] : 0.f;
+      u[q] = in ? r[q] * f[q] : 0.f;
     }
-    const int room = e.outp - f;
-    const bool vec = room >= 4 && g_vec<T>(e.out, e.ld_out) && (e.outp & 3) == 0;
-    g_store4<T>(e.out, m * e.ld_out + f, room, vec, a);
-    g_store4<T>(e.out, m * e.ld_out + e.outp + f, room, vec, u);
+    const int64_t at = m * e.ld_out + c.n;
+    g_store4<T>(e.out, at, e.outp - c.n, c.vo, a);
+    g_store4<T>(e.out, at + e.outp, e.outp - c.n, c.vo, u);
   }
 };
 
@@ -400,6 +476,8 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
   const int zc = GATED ? (tc >> 2) * 32 + (tc & 3) * 4 : tc * 4;  // column of the tile (gated: of the gate)
   const int n = GATED ? bcol + tc * 4 : n0 + zc;                  // column of the result (of a half)
   const bool in_n = n < (GATED ? e.halfp : p.N);
+  GCols ec;
+  if constexpr (!SPLIT) ec = Epi::cols(e, in_n ? n : 0);
   float cs[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
   for (int s0 = 0; s0 < BM; s0 += SR) {
@@ -417,14 +495,13 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
     if (in_n) {
       // four rows at a time: what they need beside z is in flight together
       constexpr int STEP = NT / TC, U = SR / STEP < 4 ? SR / STEP : 4;
-      const int left = GATED ? e.half - n : e.ncol - n;
       for (int r0 = tr; r0 < SR; r0 += U * STEP) {
         float res[U][4];
         if constexpr (!SPLIT) {
 #pragma unroll
           for (int i = 0; i < U; ++i) {
             const int64_t m = m0 + s0 + r0 + i * STEP;
-            Epi::load(e, m < p.M ? m : p.M - 1, n, left, res[i]);
+            Epi::load(e, ec, m < p.M ? m : p.M - 1, res[i]);
           }
         }
 #pragma unroll
@@ -443,13 +520,13 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
             if constexpr (GATED) {
               const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
               float u[4] = {y[0], y[1], y[2], y[3]};
-              Epi::apply(e, m, n, left, z, u, res[i]);
+              Epi::apply(e, ec, m, z, u, res[i]);
               if constexpr (Epi::kColSum) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
               }
             } else {
-              Epi::apply(e, m, n, left, z, res[i]);
+              Epi::apply(e, ec, m, z, res[i]);
               if constexpr (Epi::kColSum) {
 #pragma unroll
                 for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
@@ -734,13 +811,13 @@ __global__ void __launch_bounds__(256) k_product_join(const GShape p, int splits
   }
   if (!in) return;
   float z[4] = {s[0][0], s[0][1], s[0][2], s[0][3]}, r[4];
-  const int left = Epi::kGated ? e.half - n : e.ncol - n;
-  Epi::load(e, m, n, left, r);
+  const GCols ec = Epi::cols(e, n);
+  Epi::load(e, ec, m, r);
   if constexpr (Epi::kGated) {
     float u[4] = {s[H - 1][0], s[H - 1][1], s[H - 1][2], s[H - 1][3]};
-    Epi::apply(e, m, n, left, z, u, r);
+    Epi::apply(e, ec, m, z, u, r);
   } else {
-    Epi::apply(e, m, n, left, z, r);
+    Epi::apply(e, ec, m, z, r);
   }
 }
 

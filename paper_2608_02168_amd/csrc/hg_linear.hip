@@ -205,11 +205,12 @@ __global__ void __launch_bounds__(kFewWaves * 64)
         z[h][q] = s;
       }
     float res[4];
-    Epi::load(e, r, n, f - n, res);
+    const GCols ec = Epi::cols(e, n);
+    Epi::load(e, ec, r, res);
     if constexpr (Epi::kGated) {
-      Epi::apply(e, r, n, f - n, z[0], z[1], res);
+      Epi::apply(e, ec, r, z[0], z[1], res);
     } else {
-      Epi::apply(e, r, n, f - n, z[0], res);
+      Epi::apply(e, ec, r, z[0], res);
     }
   }
 }

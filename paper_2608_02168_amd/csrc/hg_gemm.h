@@ -479,6 +479,21 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
   GCols ec;
   if constexpr (!SPLIT) ec = Epi::cols(e, in_n ? n : 0);
   float cs[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  // what a slab needs beside z is in flight while the slab before is written
+  constexpr int STEP = NT / TC, RPT = SR / STEP;  // a thread's rows of a slab
+  float res[RPT][4];
+  auto load = [&](int s0) {
+    if constexpr (!SPLIT) {
+      if (in_n) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          const int64_t m = m0 + s0 + tr + i * STEP;
+          Epi::load(e, ec, m < p.M ? m : p.M - 1, res[i]);
+        }
+      }
+    }
+  };
+  load(0);
 #pragma unroll
   for (int s0 = 0; s0 < BM; s0 += SR) {
     __syncthreads();
@@ -491,46 +506,40 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
           *reinterpret_cast<f32x4*>(zt + (row + c) * LDZ + wn * WN + 16 * j + 4 * g) = acc[i][j];
       }
     }
+    float cur[RPT][4];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) cur[i][v] = res[i][v];
+    if (s0 + SR < BM) load(s0 + SR);
     __syncthreads();
     if (in_n) {
-      // four rows at a time: what they need beside z is in flight together
-      constexpr int STEP = NT / TC, U = SR / STEP < 4 ? SR / STEP : 4;
-      for (int r0 = tr; r0 < SR; r0 += U * STEP) {
-        float res[U][4];
-        if constexpr (!SPLIT) {
 #pragma unroll
-          for (int i = 0; i < U; ++i) {
-            const int64_t m = m0 + s0 + r0 + i * STEP;
-            Epi::load(e, ec, m < p.M ? m : p.M - 1, res[i]);
-          }
-        }
+      for (int i = 0; i < RPT; ++i) {
+        const int r = tr + i * STEP;
+        const int64_t m = m0 + s0 + r;
+        if (m >= p.M) break;
+        const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
+        if constexpr (SPLIT) {
+          float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
+          *reinterpret_cast<f32x4*>(part) = x;
+          if constexpr (GATED)
+            *reinterpret_cast<f32x4*>(part + e.parth) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
+        } else {
+          float z[4] = {x[0], x[1], x[2], x[3]};
+          if constexpr (GATED) {
+            const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
+            float u[4] = {y[0], y[1], y[2], y[3]};
+            Epi::apply(e, ec, m, z, u, cur[i]);
+            if constexpr (Epi::kColSum) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int r = r0 + i * STEP;
-          const int64_t m = m0 + s0 + r;
-          if (m >= p.M) break;
-          const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
-          if constexpr (SPLIT) {
-            float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
-            *reinterpret_cast<f32x4*>(part) = x;
-            if constexpr (GATED)
-              *reinterpret_cast<f32x4*>(part + e.parth) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
+              for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
+            }
           } else {
-            float z[4] = {x[0], x[1], x[2], x[3]};
-            if constexpr (GATED) {
-              const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
-              float u[4] = {y[0], y[1], y[2], y[3]};
-              Epi::apply(e, ec, m, z, u, res[i]);
-              if constexpr (Epi::kColSum) {
+            Epi::apply(e, ec, m, z, cur[i]);
+            if constexpr (Epi::kColSum) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
-              }
-            } else {
-              Epi::apply(e, ec, m, z, res[i]);
-              if constexpr (Epi::kColSum) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
-              }
+              for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
             }
           }
         }

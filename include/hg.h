@@ -639,8 +639,9 @@ int hg_qk_norm_rope_bwd(const hg_rope_desc* D, const hg_heads* q, const hg_heads
  * lens (may be NULL): int32 [batch] on the device, tokens of each sequence,
  * taken into [0, t]; rows of o (and of the gradients) past it are written as
  * zero and the rows of q, k, v and dO past it are not read.
- * d is a multiple of 8 up to 128.  Outputs must not overlap inputs or each
- * other; heads of one packed buffer may interleave.
+ * d is a multiple of 8 up to 128; the tokens of a sequence are between d and
+ * 2^22 elements apart.  Outputs must not overlap inputs or each other; heads of
+ * one packed buffer may interleave.
  * Sums, states and decays are float32; a bfloat16 call holds the weighted
  * products of a chunk and the copy of the state that multiplies a row to 16
  * bits, adds k^T v to the state to float32 accuracy and rounds o once.  A k or v

@@ -22,14 +22,15 @@
 // every segment's sum, a second adds them up along the sequence, and the walk
 // starts each segment from its state.
 //
-// Layout: a wave owns 16 NT columns of v (and of the state and of o) and all
-// rows; q, k and v tiles are shared through LDS.  With the tiles' operands
+// Layout: a wave owns 32 columns (16 up to d = 32) of v, of the state and of o
+// and all rows;
+// q, k and v tiles and P, whose blocks the waves share out, pass through LDS.  With the tiles' operands
 // taken as blocks of 16 values, 4 g .. 4 g + 3 in lane group g, every product's
 // result lies as the next product's operand needs it:
 //   P^T = K Q^T       lane (c, g): keys 4 g + v of query c    (operand of V^T P^T)
 //   S  += K^T (w V)   lane (c, g): rows 4 g + v of column c   (operand of S^T Q^T)
 //   O^T = S^T Q^T + V^T P^T   lane (c, g): columns 4 g + v of token c
-// so neither P nor S passes through LDS.
+// so S never leaves the wave's registers.
 //
 // Precision: sums, states and decays are float32.  float32 calls use the
 // float32 MFMA.  In bfloat16 calls q, k and v enter exactly, P and the copy of
@@ -42,6 +43,7 @@ namespace hg {
 namespace {
 
 constexpr int kMaxD = 128;
+constexpr int64_t kMaxToken = 1 << 22;  // token stride: a chunk of 64 stays below 2^31 bytes
 
 // One operand: element (sequence b, token t, head h, column x) at
 // p[b * sb + t * st + (h / hdiv) * sh + x].
@@ -159,28 +161,44 @@ __device__ __forceinline__ int64_t len_of(const int32_t* lens, int b, int64_t T)
 __device__ __forceinline__ float log_of(float x) { return x < -1e30f ? -1e30f : x; }
 
 // Power n >= 0 of the decay: exp(n log l), 1 for n = 0 whatever l is.
-__device__ __forceinline__ float decay(float lg, int64_t n) { return n <= 0 ? 1.f : expf(lg * (float)n); }
+__device__ __forceinline__ float decay(float lg, int n) { return n <= 0 ? 1.f : expf(lg * (float)n); }
 
-// C rows of one operand into LDS: position u of the walk (token u, or last - u
-// in a reverse walk) in row u - u0; positions from u_to on and columns from d on
-// are zero.
+// C rows of one operand: row i holds position u0 + i of the walk (token u0 + i,
+// or last - u0 - i in a reverse walk); rows from n on and columns from d on are
+// zero.  `load` starts the loads of a chunk, `store` puts it into LDS: the next
+// chunk's rows are in flight while the MFMAs of this one run.  Buffer loads: the
+// descriptor starts at the chunk's first token and ends with its last, what lies
+// outside reads as zero, so no branch holds a load back.
 template <class T, int DP, int C, int NT>
-__device__ __forceinline__ void stage(T* lds, const Role& r, const T* base, int64_t u0, int64_t u_to, int64_t last, int d) {
-  constexpr int EL = Elt<T>::EL, CH = DP / EL, N = C * CH / NT;
+struct Rows {
+  static constexpr int EL = Elt<T>::EL, CH = DP / EL, N = C * CH / NT;
   static_assert(C * CH % NT == 0, "whole chunks per thread");
-  typename Elt<T>::rawv_t x[N];
+  u32x4 x[N];
+  int off[N];
+  __device__ __forceinline__ void init(int64_t st, int d, bool reverse) {
 #pragma unroll
-  for (int q = 0; q < N; ++q) {
-    const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
-    const int64_t u = u0 + row, t = last >= 0 ? last - u : u;
-    x[q] = u < u_to && col < d ? Elt<T>::rawv(base + t * r.st + col) : Elt<T>::rawv_zero();
+    for (int q = 0; q < N; ++q) {
+      const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
+      off[q] = col < d ? ((reverse ? C - 1 - row : row) * (int)st + col) * (int)sizeof(T) : 0x7FFFFF00;
+    }
   }
+  // first: the chunk's first token in memory
+  __device__ __forceinline__ void load(const T* first, int64_t st, int n, int d, bool reverse) {
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(first), 0,
+                                                        (int)(((n - 1) * (int)st + d) * (int)sizeof(T)), 0x00020000);
+    // a reverse walk's missing rows lie before the first token
+    const int back = reverse ? (C - n) * (int)st * (int)sizeof(T) : 0;
 #pragma unroll
-  for (int q = 0; q < N; ++q) {
-    const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
-    *reinterpret_cast<typename Elt<T>::rawv_t*>(lds + row * Tile<T, DP>::LD + col) = x[q];
+    for (int q = 0; q < N; ++q) x[q] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[q] - back, 0, 0);
   }
-}
+  __device__ __forceinline__ void store(T* lds) const {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
+      *reinterpret_cast<u32x4*>(lds + row * Tile<T, DP>::LD + col) = x[q];
+    }
+  }
+};
 
 // v truncated to three bfloat16 parts (24 bits in all), four values a lane
 __device__ __forceinline__ void parts3(f32x4 x, uint2 (&p)[3]) {
@@ -198,21 +216,24 @@ __device__ __forceinline__ void parts3(f32x4 x, uint2 (&p)[3]) {
 
 template <int DP>
 struct Shape {
-  static constexpr int NT = DP >= 96 ? 2 : 1;  // 16-column blocks of a wave
-  static constexpr int W = DP / 16 / NT, THREADS = 64 * W, NB = DP / 16;
+  static constexpr int NB = DP / 16;          // 16-column blocks of a row
+  static constexpr int NT = 1;                 // of a wave
+  static constexpr int W = NB / NT, THREADS = 64 * W;
 };
 
 // One head of one sequence, or a segment of it.  SUMS: only the segment's sum.
 template <class T, class TO, int DP, int C, bool SUMS>
-__global__ void __launch_bounds__(Shape<DP>::THREADS) k_linattn_scan(const ScanArgs a) {
-  constexpr int NT = Shape<DP>::NT, NB = Shape<DP>::NB, NTHR = Shape<DP>::THREADS, RB = C / 16;
+__global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const ScanArgs a) {
+  constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, RB = C / 16;
   typedef Tile<T, DP> TL;
   typedef typename Blk<T>::type B;
   constexpr bool kF32 = sizeof(T) == 4;
+  constexpr int NP = RB * (RB + 1) / 2;  // 16 x 16 blocks of P on and below the diagonal
   __shared__ __align__(16) T lk[C * TL::LD];
   __shared__ __align__(16) T lv[C * TL::LD];
   __shared__ __align__(16) T lq[SUMS ? 16 : C * TL::LD];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  __shared__ __align__(16) Factor<T> lp[SUMS ? 1 : NP][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const int h = blockIdx.x % a.H, b = blockIdx.x / a.H, seg = blockIdx.y;
   const int d = a.d;
   const float lg = log_of(a.log_decay[h]);
@@ -272,83 +293,141 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS) k_linattn_scan(const ScanA
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const int x = c - 4 * g - v;
-    near0[v] = decay(lg, 16 + x) * a.kv_scale;
-    diag[v] = x >= 0 ? decay(lg, x) * a.kv_scale : 0.f;
+    near0[v] = decay(lg, 16 + x) * a.kv_scale * a.o_scale;
+    diag[v] = decay(lg, x) * a.kv_scale * a.o_scale;
     tail[v] = decay(lg, 15 - 4 * g - v + lead) * a.kv_scale;
   }
-  const float row0 = decay(lg, c + 1 - lead), p16 = decay(lg, 16), pC = decay(lg, C);
+  const float row0 = decay(lg, c + 1 - lead) * a.o_scale, p16 = decay(lg, 16), pC = decay(lg, C);
 
+  Rows<T, DP, C, NTHR> rk, rv, rq;
+  rk.init(a.k.st, d, a.reverse);
+  rv.init(a.v.st, d, a.reverse);
+  if constexpr (!SUMS) rq.init(a.q.st, d, a.reverse);
+  auto load = [&](int64_t u0) {
+    const int n = (int)(u_to - u0 < C ? u_to - u0 : C);
+    const int64_t t = a.reverse ? L - n - u0 : u0;
+    rk.load(kp + t * a.k.st, a.k.st, n, d, a.reverse);
+    rv.load(vp + t * a.v.st, a.v.st, n, d, a.reverse);
+    if constexpr (!SUMS) rq.load(qp + t * a.q.st, a.q.st, n, d, a.reverse);
+  };
+  // this lane's columns of o in row c of a block of 16
+  const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave * NT + 4 * g) * (int)sizeof(TO));
+
+  if (u_from < u_to) load(u_from);
   for (int64_t u0 = u_from; u0 < u_to; u0 += C) {
     const int n = (int)(u_to - u0 < C ? u_to - u0 : C);
     __syncthreads();
-    stage<T, DP, C, NTHR>(lk, a.k, kp, u0, u_to, last, d);
-    stage<T, DP, C, NTHR>(lv, a.v, vp, u0, u_to, last, d);
-    if constexpr (!SUMS) stage<T, DP, C, NTHR>(lq, a.q, qp, u0, u_to, last, d);
+    rk.store(lk);
+    rv.store(lv);
+    if constexpr (!SUMS) rq.store(lq);
     __syncthreads();
+    if (u0 + C < u_to) load(u0 + C);
     if constexpr (!SUMS) {
-      Factor<T> Sb[NB + NB % 2][NT];
+      // P, its blocks shared out over the waves
+      for (int pr = wave; pr < NP; pr += Shape<DP>::W) {
+        const int r = pr >= 6 ? 3 : pr >= 3 ? 2 : pr >= 1 ? 1 : 0, kt = pr - r * (r + 1) / 2;
+        f32x4 s{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
+        for (int i = 0; i < NB; i += 2) {
+          const bool two = i + 1 < NB;
+          const B k0 = TL::row4(lk, 16 * kt + c, i, g), q0 = TL::row4(lq, 16 * r + c, i, g);
+          const B k1 = two ? TL::row4(lk, 16 * kt + c, two ? i + 1 : i, g) : Blk<T>::zero();
+          const B q1 = two ? TL::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
+          f32x4& acc = (i & 2) ? s1 : s;  // two chains
+          acc = mma32(k0, k1, q0, q1, acc);
+        }
 #pragma unroll
-        for (int i = 0; i < NB; ++i) Sb[i][j].set(S[i][j]);
-        if constexpr (NB % 2) Sb[NB][j].zero();
+        for (int v = 0; v < 4; ++v) s[v] += s1[v];
+        if (kt == r) {
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s[v] = c >= 4 * g + v ? s[v] * diag[v] : 0.f;
+        } else {
+          const float far = r - kt == 1 ? 1.f : r - kt == 2 ? p16 : p16 * p16;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s[v] *= near0[v] * far;
+        }
+        Factor<T> f;
+        f.set(s);
+        lp[pr][lane] = f;
+      }
+      // q S, the chains of the rows and columns side by side
+      f32x4 o[RB][NT];
+#pragma unroll
+      for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) o[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NB; i += 2) {
+        const bool two = i + 1 < NB;
+        B q0[RB], q1[RB];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          q0[r] = TL::row4(lq, 16 * r + c, i, g);
+          q1[r] = two ? TL::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
+        }
+        Factor<T> s0[NT], s1[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          s0[j].set(S[i][j]);
+          if (two) {
+            s1[j].set(S[two ? i + 1 : i][j]);
+          } else {
+            s1[j].zero();
+          }
+        }
+#pragma unroll
+        for (int x = Factor<T>::N - 1; x >= 0; --x)
+#pragma unroll
+          for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) o[r][j] = mma32(s0[j].x[x], s1[j].x[x], q0[r], q1[r], o[r][j]);
       }
       float rowp = row0;
 #pragma unroll
-      for (int r = 0; r < RB; ++r, rowp *= p16) {
-        B qf[NB + NB % 2];
+      for (int r = 0; r < RB; ++r, rowp *= p16)
 #pragma unroll
-        for (int i = 0; i < NB; ++i) qf[i] = TL::row4(lq, 16 * r + c, i, g);
-        if constexpr (NB % 2) qf[NB] = Blk<T>::zero();
-        f32x4 o[NT];
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) o[r][j][v] *= rowp;
+      __syncthreads();
+      // P v
+#pragma unroll
+      for (int kt = 0; kt < RB; kt += 2) {
+        B v0[NT], v1[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          v0[j] = TL::col4(lv, kt, wave * NT + j, c, g);
+          v1[j] = TL::col4(lv, kt + 1, wave * NT + j, c, g);
+        }
+#pragma unroll
+        for (int r = kt; r < RB; ++r) {
+          const Factor<T> p0 = lp[r * (r + 1) / 2 + kt][lane];
+          Factor<T> p1;
+          if (r > kt) {
+            p1 = lp[r * (r + 1) / 2 + kt + 1][lane];
+          } else {
+            p1.zero();
+          }
 #pragma unroll
           for (int x = Factor<T>::N - 1; x >= 0; --x)
 #pragma unroll
-            for (int i = 0; i < NB; i += 2) o[j] = mma32(Sb[i][j].x[x], Sb[i + 1][j].x[x], qf[i], qf[i + 1], o[j]);
-#pragma unroll
-          for (int v = 0; v < 4; ++v) o[j][v] *= rowp;
+            for (int j = 0; j < NT; ++j)
+              o[r][j] = mma32(v0[j], r > kt ? v1[j] : Blk<T>::zero(), p0.x[x], p1.x[x], o[r][j]);
         }
-        Factor<T> pb[RB];
-        if (r + 1 < RB) pb[r + 1].zero();
-        float far = 1.f;
+      }
 #pragma unroll
-        for (int kt = r; kt >= 0; --kt) {
-          f32x4 s{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < RB; ++r) {
+        const int64_t t = a.reverse ? last - u0 - 16 * r - 15 : u0 + 16 * r;  // token of row 0, or of row 15
+        char* p = reinterpret_cast<char*>(op + t * a.o.st);
 #pragma unroll
-          for (int i = 0; i < NB; i += 2)
-            s = mma32(TL::row4(lk, 16 * kt + c, i, g),
-                      i + 1 < NB ? TL::row4(lk, 16 * kt + c, i + 1 < NB ? i + 1 : i, g) : Blk<T>::zero(), qf[i], qf[i + 1], s);
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            s[v] = kt < r ? s[v] * (near0[v] * far) : c >= 4 * g + v ? s[v] * diag[v] : 0.f;
-          if (kt < r) far *= p16;
-          pb[kt].set(s);
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-#pragma unroll
-          for (int kt = 0; kt <= r; kt += 2) {
-            const B v0 = TL::col4(lv, kt, wave * NT + j, c, g);
-            const B v1 = kt + 1 <= r ? TL::col4(lv, kt + 1, wave * NT + j, c, g) : Blk<T>::zero();
-#pragma unroll
-            for (int x = Factor<T>::N - 1; x >= 0; --x) o[j] = mma32(v0, v1, pb[kt].x[x], pb[kt + 1].x[x], o[j]);
-          }
-          const int64_t u = u0 + 16 * r + c, t = last >= 0 ? last - u : u;
-          const int col = 16 * (wave * NT + j) + 4 * g;
-          if (u < u_to && col < d) {
-            TO* p = op + t * a.o.st + col;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) o[j][v] *= a.o_scale;
+        for (int j = 0; j < NT; ++j)
+          if (16 * (wave * NT + j) + 4 * g < d && 16 * r + c < n) {
             if constexpr (sizeof(TO) == 4) {
-              *reinterpret_cast<f32x4*>(p) = o[j];
+              *reinterpret_cast<f32x4*>(p + o_off + 64 * j) = o[r][j];
             } else {
-              *reinterpret_cast<uint2*>(p) = Blk<bf16_t>::of(o[j]);
+              *reinterpret_cast<uint2*>(p + o_off + 32 * j) = Blk<bf16_t>::of(o[r][j]);
             }
           }
-        }
       }
     }
 
@@ -360,44 +439,64 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS) k_linattn_scan(const ScanA
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) S[i][j][v] *= dn;
-    // w V of this wave's columns: token 16 tb + 4 g + v
-    f32x4 wv[RB][NT];
     float far = 1.f;
 #pragma unroll
-    for (int tb = RB - 1; tb >= 0; --tb, far *= p16) {
-      float w[4];
+    for (int tb = RB - 2; tb >= 0; tb -= 2, far *= p16 * p16) {
+      // w v of this wave's columns: tokens 16 tb + 4 g + v and 16 more
+      f32x4 w0[NT], w1[NT];
+      float x0[4], x1[4];
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-        w[v] = n == C ? tail[v] * far : decay(lg, n - 1 - (16 * tb + 4 * g + v) + lead) * a.kv_scale;
+      for (int v = 0; v < 4; ++v) {
+        if (n == C) {
+          x1[v] = tail[v] * far;
+          x0[v] = x1[v] * p16;
+        } else {
+          const int at = n - 1 - (16 * tb + 4 * g + v) + lead;
+          x0[v] = decay(lg, at) * a.kv_scale;
+          x1[v] = decay(lg, at - 16) * a.kv_scale;
+        }
+      }
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        wv[tb][j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
+        w0[j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
+        w1[j] = wide(TL::col4(lv, tb + 1, wave * NT + j, c, g));
 #pragma unroll
-        for (int v = 0; v < 4; ++v) wv[tb][j][v] *= w[v];
+        for (int v = 0; v < 4; ++v) {
+          w0[j][v] *= x0[v];
+          w1[j][v] *= x1[v];
+        }
       }
-    }
-#pragma unroll
-    for (int tb = 0; tb < RB; tb += 2) {
       uint2 p0[NT][3], p1[NT][3];
       if constexpr (!kF32) {
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          parts3(wv[tb][j], p0[j]);
-          parts3(wv[tb + 1][j], p1[j]);
+          parts3(w0[j], p0[j]);
+          parts3(w1[j], p1[j]);
         }
       }
+      // chains side by side, at most U blocks' operands at a time
+      constexpr int U = NB < 4 ? NB : kF32 ? 2 : 4;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const B k0 = TL::col4(lk, tb, i, c, g), k1 = TL::col4(lk, tb + 1, i, c, g);
+      for (int i0 = 0; i0 < NB; i0 += U) {
+        B k0[U], k1[U];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          if constexpr (kF32) {
-            S[i][j] = mma32(k0, k1, wv[tb][j], wv[tb + 1][j], S[i][j]);
-          } else {
-#pragma unroll
-            for (int x = 2; x >= 0; --x) S[i][j] = mma32(k0, k1, p0[j][x], p1[j][x], S[i][j]);
-          }
+        for (int i = 0; i < U && i0 + i < NB; ++i) {
+          k0[i] = TL::col4(lk, tb, i0 + i, c, g);
+          k1[i] = TL::col4(lk, tb + 1, i0 + i, c, g);
         }
+#pragma unroll
+        for (int x = kF32 ? 0 : 2; x >= 0; --x)
+#pragma unroll
+          for (int i = 0; i < U && i0 + i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              f32x4& s = S[i0 + i][j];
+              if constexpr (kF32) {
+                s = mma32(k0[i], k1[i], w0[j], w1[j], s);
+              } else {
+                s = mma32(k0[i], k1[i], p0[j][x], p1[j][x], s);
+              }
+            }
       }
     }
   }
@@ -434,7 +533,7 @@ __global__ void __launch_bounds__(256) k_linattn_join(const ScanArgs a, int64_t 
   const int q = (int)(id - bh * Q), blk = q >> 6, lane = q & 63, c = lane & 15, g = lane >> 4;
   const int h = (int)(bh % a.H), b = (int)(bh / a.H), d = a.d;
   const int64_t L = len_of(a.lens, b, a.T);
-  const float lg = log_of(a.log_decay[h]), whole = decay(lg, a.seg_len);
+  const float lg = log_of(a.log_decay[h]), whole = decay(lg, (int)a.seg_len);
   const int col = 16 * (blk % NB) + c, row = 16 * (blk / NB) + 4 * g;
   f32x4 S{0.f, 0.f, 0.f, 0.f};
   auto at = [&](int v) { return bh * d * d + (a.s_trans ? col * d + row + v : (row + v) * d + col); };
@@ -449,7 +548,7 @@ __global__ void __launch_bounds__(256) k_linattn_join(const ScanArgs a, int64_t 
     const f32x4 x = *reinterpret_cast<const f32x4*>(p);
     *reinterpret_cast<f32x4*>(p) = S;
     const int64_t left = L - s * a.seg_len;
-    const float f = left >= a.seg_len ? whole : decay(lg, left);
+    const float f = left >= a.seg_len ? whole : decay(lg, (int)left);
 #pragma unroll
     for (int v = 0; v < 4; ++v) S[v] = S[v] * f + x[v];
   }
@@ -621,10 +720,17 @@ int check_heads(const hg_linattn_desc* A, const char* what, const hg_heads* x, c
   const int64_t e = A->dtype == HG_DTYPE_F32 ? 4 : 8;
   if ((reinterpret_cast<uintptr_t>(x->p) & 15) || x->batch % e || x->token % e || x->head % e)
     return fail(HG_ERR_ARG, "%s: rows of %s are not 16-byte aligned", what, name);
+  if (A->t > 1 && x->token < A->d)
+    return fail(HG_ERR_ARG, "%s: tokens of %s are %lld apart, %d wide", what, name, (long long)x->token, A->d);
+  if (A->t > 1 && x->token > kMaxToken)
+    return fail(HG_ERR_UNSUPPORTED, "%s: tokens of %s are %lld apart", what, name, (long long)x->token);
   return HG_OK;
 }
 
-Role role(const hg_heads* x, int hdiv) { return Role{x->p, x->batch, x->token, x->head, hdiv}; }
+// A single token's stride is never walked: any that keeps rows apart does.
+Role role(const hg_linattn_desc* A, const hg_heads* x, int hdiv) {
+  return Role{x->p, x->batch, A->t > 1 ? x->token : A->d, x->head, hdiv};
+}
 
 ScanArgs args_of(const hg_linattn_desc* A, const float* log_decay, const int32_t* lens, float* seg) {
   const Segs sg = segs_of(A);
@@ -661,10 +767,10 @@ int sum_groups(const hg_linattn_desc* A, const float* part, const hg_heads* o, h
   const int group = A->heads / A->kv_heads;
   if (A->dtype == HG_DTYPE_F32) {
     HG_LAUNCH("group_sum", k_group_sum<float>, grid, dim3(256), 0, s, part, (int64_t)A->batch, A->t, A->kv_heads, group,
-              A->d, role(o, 1));
+              A->d, role(A, o, 1));
   } else {
     HG_LAUNCH("group_sum", k_group_sum<bf16_t>, grid, dim3(256), 0, s, part, (int64_t)A->batch, A->t, A->kv_heads, group,
-              A->d, role(o, 1));
+              A->d, role(A, o, 1));
   }
   return HG_OK;
 }
@@ -709,10 +815,10 @@ extern "C" int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const
   const Bufs b = take(A, false, m);
   ScanArgs a = args_of(A, log_decay, lens, b.seg);
   const int group = A->heads / A->kv_heads;
-  a.q = role(q, 1);
-  a.k = role(k, group);
-  a.v = role(v, group);
-  a.o = role(o, 1);
+  a.q = role(A, q, 1);
+  a.k = role(A, k, group);
+  a.v = role(A, v, group);
+  a.o = role(A, o, 1);
   a.s_in = state;
   a.s_out = state_out;
   a.o_scale = A->scale;
@@ -744,10 +850,10 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
   const int group = A->heads / A->kv_heads;
   ScanArgs a = args_of(A, log_decay, lens, b.seg);
   // dq: its state is the transpose of the forward's
-  a.q = role(d_o, 1);
-  a.k = role(v, group);
-  a.v = role(k, group);
-  a.o = role(dq, 1);
+  a.q = role(A, d_o, 1);
+  a.k = role(A, v, group);
+  a.v = role(A, k, group);
+  a.o = role(A, dq, 1);
   a.s_in = state;
   a.s_trans = 1;
   a.o_scale = A->scale;
@@ -759,18 +865,18 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
   a.kv_scale = A->scale;
   a.o_scale = 1.f;
   a.s_in = dstate_out;
-  a.q = role(v, group);
-  a.k = role(d_o, 1);
-  a.v = role(q, 1);
-  a.o = group > 1 ? part : role(dk, 1);
+  a.q = role(A, v, group);
+  a.k = role(A, d_o, 1);
+  a.v = role(A, q, 1);
+  a.o = group > 1 ? part : role(A, dk, 1);
   HG_TRY(scan("linattn_dk", A, a, group > 1, s));
   if (group > 1) HG_TRY(sum_groups(A, b.part, dk, s));
   a.s_trans = 0;
   a.s_out = dstate;
-  a.q = role(k, group);
-  a.k = role(q, 1);
-  a.v = role(d_o, 1);
-  a.o = group > 1 ? part : role(dv, 1);
+  a.q = role(A, k, group);
+  a.k = role(A, q, 1);
+  a.v = role(A, d_o, 1);
+  a.o = group > 1 ? part : role(A, dv, 1);
   HG_TRY(scan("linattn_dv", A, a, group > 1, s));
   if (group > 1) HG_TRY(sum_groups(A, b.part, dv, s));
   return HG_OK;
@@ -800,8 +906,8 @@ extern "C" int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, cons
   const int group = A->heads / A->kv_heads;
   const dim3 grid((unsigned)heads, (unsigned)cdiv(A->d, width));
 #define HG_STEP(T_, N_)                                                                                              \
-  HG_LAUNCH("linattn_step", (k_linattn_step<T_, N_>), grid, dim3(N_), 0, s, role(q, 1), role(k, group), role(v, group), \
-            role(o, 1), log_decay, state, slots, n_slots, A->heads, A->d, width, A->scale)
+  HG_LAUNCH("linattn_step", (k_linattn_step<T_, N_>), grid, dim3(N_), 0, s, role(A, q, 1), role(A, k, group), role(A, v, group), \
+            role(A, o, 1), log_decay, state, slots, n_slots, A->heads, A->d, width, A->scale)
   const bool small = A->d <= 32;
   if (A->dtype == HG_DTYPE_F32) {
     if (small) {

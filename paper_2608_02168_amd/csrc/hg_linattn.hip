@@ -20,7 +20,8 @@
 // Work split: a block takes one head of one sequence, or one segment of it
 // when there are too few of those to fill the chip.  Then a first pass forms
 // every segment's sum, a second adds them up along the sequence, and the walk
-// starts each segment from its state.
+// starts each segment from its state.  The backward's three walks are one
+// launch; dk takes dv's segment states transposed.
 //
 // Layout: a wave owns 32 columns (16 up to d = 32) of v, of the state and of o
 // and all rows;
@@ -43,6 +44,7 @@ namespace hg {
 namespace {
 
 constexpr int kMaxD = 128;
+constexpr int64_t kBlocks = 512;  // two for each CU
 constexpr int64_t kMaxToken = 1 << 22;  // token stride: a chunk of 64 stays below 2^31 bytes
 
 // One operand: element (sequence b, token t, head h, column x) at
@@ -53,7 +55,7 @@ struct Role {
   int32_t hdiv;
 };
 
-struct ScanArgs {
+struct Walk {
   Role q, k, v, o;
   const float* log_decay;
   const int32_t* lens;     // tokens of each sequence, or null
@@ -65,7 +67,14 @@ struct ScanArgs {
   int32_t segs, H, d;
   int32_t reverse;         // walk from the last token; 1: its lead too
   int32_t s_trans;         // the walk's state is the transpose of s_in and s_out
+  int32_t seg_trans;       // ... and of seg (another walk's)
+  int32_t f32_out;         // o is float32 whatever the operands are
   float kv_scale, o_scale;
+};
+
+// The walks of a call, one a blockIdx.z.
+struct Walks {
+  Walk w[3];
 };
 
 typedef __bf16 l_bf16x4 __attribute__((ext_vector_type(4)));
@@ -222,8 +231,9 @@ struct Shape {
 };
 
 // One head of one sequence, or a segment of it.  SUMS: only the segment's sum.
-template <class T, class TO, int DP, int C, bool SUMS>
-__global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const ScanArgs a) {
+template <class T, int DP, int C, bool SUMS>
+__global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Walks walks) {
+  const Walk& a = walks.w[blockIdx.z];
   constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, RB = C / 16;
   typedef Tile<T, DP> TL;
   typedef typename Blk<T>::type B;
@@ -237,25 +247,24 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Sc
   const int h = blockIdx.x % a.H, b = blockIdx.x / a.H, seg = blockIdx.y;
   const int d = a.d;
   const float lg = log_of(a.log_decay[h]);
-  const int64_t L = len_of(a.lens, b, a.T);
-  const int64_t u_from = (int64_t)seg * a.seg_len;
-  const int64_t u_to = u_from + a.seg_len < L ? u_from + a.seg_len : L;
+  // positions fit 32 bits (T < 2^31); addresses are formed in 64
+  const int L = (int)len_of(a.lens, b, a.T);
+  const int u_from = (int)((int64_t)seg * a.seg_len), u_end = (int)(u_from + a.seg_len < a.T ? u_from + a.seg_len : a.T);
+  const int u_to = u_end < L ? u_end : L;
   const int lead = a.reverse ? 1 : 0;
-  const int64_t last = a.reverse ? L - 1 : -1;
   const T* kp = static_cast<const T*>(a.k.p) + b * a.k.sb + (h / a.k.hdiv) * a.k.sh;
   const T* vp = static_cast<const T*>(a.v.p) + b * a.v.sb + (h / a.v.hdiv) * a.v.sh;
   const T* qp = SUMS ? nullptr : static_cast<const T*>(a.q.p) + b * a.q.sb + (h / a.q.hdiv) * a.q.sh;
-  TO* op = SUMS ? nullptr : static_cast<TO*>(const_cast<void*>(a.o.p)) + b * a.o.sb + (h / a.o.hdiv) * a.o.sh;
+  const int osz = kF32 || a.f32_out ? 4 : 2;
+  char* op = SUMS ? nullptr : static_cast<char*>(const_cast<void*>(a.o.p)) + (b * a.o.sb + (h / a.o.hdiv) * a.o.sh) * osz;
   const int64_t bh = (int64_t)b * a.H + h;
 
   if constexpr (!SUMS) {
     // tokens past the sequence's end: zero rows
-    const int64_t z0 = u_from > L ? u_from : L, z1 = u_from + a.seg_len < a.T ? u_from + a.seg_len : a.T;
-    const int ch = d / 4;
-    for (int64_t i = threadIdx.x; i < (z1 - z0) * ch; i += NTHR) {
-      const int64_t t = z0 + i / ch;
-      TO* p = op + t * a.o.st + i % ch * 4;
-      if constexpr (sizeof(TO) == 4) {
+    const int z0 = u_from > L ? u_from : L, ch = d / 4;
+    for (int64_t i = threadIdx.x; i < (int64_t)(u_end - z0) * ch; i += NTHR) {
+      char* p = op + ((z0 + i / ch) * a.o.st + i % ch * 4) * osz;
+      if (osz == 4) {
         *reinterpret_cast<f32x4*>(p) = f32x4{0.f, 0.f, 0.f, 0.f};
       } else {
         *reinterpret_cast<uint2*>(p) = uint2{0u, 0u};
@@ -276,7 +285,14 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Sc
       S[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (!SUMS) {
         if (a.segs > 1) {
-          S[i][j] = *reinterpret_cast<const f32x4*>(seg_at + (i * NB + wave * NT + j) * 256 + lane * 4);
+          if (!a.seg_trans) {
+            S[i][j] = *reinterpret_cast<const f32x4*>(seg_at + (i * NB + wave * NT + j) * 256 + lane * 4);
+          } else {
+            // element (r, c) of the block lies where (c, r) of the mirrored block does
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              S[i][j][v] = seg_at[((wave * NT + j) * NB + i) * 256 + ((c >> 2) * 16 + 4 * g + v) * 4 + (c & 3)];
+          }
         } else if (a.s_in) {
           const int col = 16 * (wave * NT + j) + c;
 #pragma unroll
@@ -289,33 +305,40 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Sc
     }
 
   // powers of the decay that every chunk needs
-  float near0[4], diag[4], tail[4];  // l^(16 + c - 4 g - v), l^(c - 4 g - v) below the diagonal, l^(15 - 4 g - v + lead)
+  float near0[4], diag[4];  // l^(16 + c - 4 g - v), l^(c - 4 g - v) on and below the diagonal
+  float w[RB][4];           // of token 16 tb + 4 g + v in the state after a chunk
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
     const int x = c - 4 * g - v;
     near0[v] = decay(lg, 16 + x) * a.kv_scale * a.o_scale;
     diag[v] = decay(lg, x) * a.kv_scale * a.o_scale;
-    tail[v] = decay(lg, 15 - 4 * g - v + lead) * a.kv_scale;
   }
-  const float row0 = decay(lg, c + 1 - lead) * a.o_scale, p16 = decay(lg, 16), pC = decay(lg, C);
+  const float row0 = decay(lg, c + 1 - lead) * a.o_scale, p16 = decay(lg, 16), p32 = p16 * p16;
+  float dn = decay(lg, C);  // of the state over a chunk
+#pragma unroll
+  for (int v = 0; v < 4; ++v) w[RB - 1][v] = decay(lg, 15 - 4 * g - v + lead) * a.kv_scale;
+#pragma unroll
+  for (int tb = RB - 2; tb >= 0; --tb)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) w[tb][v] = w[tb + 1][v] * p16;
 
   Rows<T, DP, C, NTHR> rk, rv, rq;
   rk.init(a.k.st, d, a.reverse);
   rv.init(a.v.st, d, a.reverse);
   if constexpr (!SUMS) rq.init(a.q.st, d, a.reverse);
-  auto load = [&](int64_t u0) {
-    const int n = (int)(u_to - u0 < C ? u_to - u0 : C);
+  auto load = [&](int u0) {
+    const int n = u_to - u0 < C ? u_to - u0 : C;
     const int64_t t = a.reverse ? L - n - u0 : u0;
     rk.load(kp + t * a.k.st, a.k.st, n, d, a.reverse);
     rv.load(vp + t * a.v.st, a.v.st, n, d, a.reverse);
     if constexpr (!SUMS) rq.load(qp + t * a.q.st, a.q.st, n, d, a.reverse);
   };
   // this lane's columns of o in row c of a block of 16
-  const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave * NT + 4 * g) * (int)sizeof(TO));
+  const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave * NT + 4 * g) * osz);
 
   if (u_from < u_to) load(u_from);
-  for (int64_t u0 = u_from; u0 < u_to; u0 += C) {
-    const int n = (int)(u_to - u0 < C ? u_to - u0 : C);
+  for (int u0 = u_from; u0 < u_to; u0 += C) {
+    const int n = u_to - u0 < C ? u_to - u0 : C;
     __syncthreads();
     rk.store(lk);
     rv.store(lv);
@@ -342,7 +365,7 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Sc
 #pragma unroll
           for (int v = 0; v < 4; ++v) s[v] = c >= 4 * g + v ? s[v] * diag[v] : 0.f;
         } else {
-          const float far = r - kt == 1 ? 1.f : r - kt == 2 ? p16 : p16 * p16;
+          const float far = r - kt == 1 ? 1.f : r - kt == 2 ? p16 : p32;
 #pragma unroll
           for (int v = 0; v < 4; ++v) s[v] *= near0[v] * far;
         }
@@ -417,53 +440,46 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Sc
       }
 #pragma unroll
       for (int r = 0; r < RB; ++r) {
-        const int64_t t = a.reverse ? last - u0 - 16 * r - 15 : u0 + 16 * r;  // token of row 0, or of row 15
-        char* p = reinterpret_cast<char*>(op + t * a.o.st);
+        const int64_t t = a.reverse ? L - 1 - u0 - 16 * r - 15 : u0 + 16 * r;  // token of row 0, or of row 15
+        char* p = op + t * a.o.st * osz + o_off;
 #pragma unroll
         for (int j = 0; j < NT; ++j)
           if (16 * (wave * NT + j) + 4 * g < d && 16 * r + c < n) {
-            if constexpr (sizeof(TO) == 4) {
-              *reinterpret_cast<f32x4*>(p + o_off + 64 * j) = o[r][j];
+            if (osz == 4) {
+              *reinterpret_cast<f32x4*>(p + 64 * j) = o[r][j];
             } else {
-              *reinterpret_cast<uint2*>(p + o_off + 32 * j) = Blk<bf16_t>::of(o[r][j]);
+              *reinterpret_cast<uint2*>(p + 32 * j) = Blk<bf16_t>::of(o[r][j]);
             }
           }
       }
     }
 
     // state
-    const float dn = n == C ? pC : decay(lg, n);
+    if (n < C) {  // the last chunk of a segment
+      dn = decay(lg, n);
+#pragma unroll
+      for (int tb = 0; tb < RB; ++tb)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) w[tb][v] = decay(lg, n - 1 - (16 * tb + 4 * g + v) + lead) * a.kv_scale;
+    }
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
         for (int v = 0; v < 4; ++v) S[i][j][v] *= dn;
-    float far = 1.f;
 #pragma unroll
-    for (int tb = RB - 2; tb >= 0; tb -= 2, far *= p16 * p16) {
-      // w v of this wave's columns: tokens 16 tb + 4 g + v and 16 more
+    for (int tb = 0; tb < RB; tb += 2) {
+      // w v of this wave's columns
       f32x4 w0[NT], w1[NT];
-      float x0[4], x1[4];
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (n == C) {
-          x1[v] = tail[v] * far;
-          x0[v] = x1[v] * p16;
-        } else {
-          const int at = n - 1 - (16 * tb + 4 * g + v) + lead;
-          x0[v] = decay(lg, at) * a.kv_scale;
-          x1[v] = decay(lg, at - 16) * a.kv_scale;
-        }
-      }
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
         w0[j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
         w1[j] = wide(TL::col4(lv, tb + 1, wave * NT + j, c, g));
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          w0[j][v] *= x0[v];
-          w1[j][v] *= x1[v];
+          w0[j][v] *= w[tb][v];
+          w1[j][v] *= w[tb + 1][v];
         }
       }
       uint2 p0[NT][3], p1[NT][3];
@@ -526,7 +542,8 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Sc
 // before its segment, the last one's successor the state after the walk.  A
 // thread takes four elements (a lane's share of one 16 x 16 block).
 template <int DP>
-__global__ void __launch_bounds__(256) k_linattn_join(const ScanArgs a, int64_t bhs) {
+__global__ void __launch_bounds__(256) k_linattn_join(const Walks walks, int64_t bhs) {
+  const Walk& a = walks.w[blockIdx.z];
   constexpr int NB = DP / 16, Q = NB * NB * 64;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, bh = id / Q;
   if (bh >= bhs) return;
@@ -544,13 +561,21 @@ __global__ void __launch_bounds__(256) k_linattn_join(const ScanArgs a, int64_t 
   }
   float* p = a.seg + bh * a.segs * (int64_t)(NB * NB * 256) + (int64_t)q * 4;
   const int live = (int)((L + a.seg_len - 1) / a.seg_len);
-  for (int s = 0; s < live; ++s, p += NB * NB * 256) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(p);
-    *reinterpret_cast<f32x4*>(p) = S;
-    const int64_t left = L - s * a.seg_len;
-    const float f = left >= a.seg_len ? whole : decay(lg, (int)left);
+  constexpr int U = 8;  // sums in flight
+  for (int s0 = 0; s0 < live; s0 += U) {
+    f32x4 x[U];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) S[v] = S[v] * f + x[v];
+    for (int i = 0; i < U; ++i) x[i] = *reinterpret_cast<const f32x4*>(p + (s0 + i < live ? s0 + i : s0) * (int64_t)(NB * NB * 256));
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int s = s0 + i;
+      if (s >= live) break;
+      *reinterpret_cast<f32x4*>(p + s * (int64_t)(NB * NB * 256)) = S;
+      const int64_t left = L - s * a.seg_len;
+      const float f = left >= a.seg_len ? whole : decay(lg, (int)left);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) S[v] = S[v] * f + x[i][v];
+    }
   }
   if (a.s_out && col < d) {
 #pragma unroll
@@ -562,7 +587,10 @@ __global__ void __launch_bounds__(256) k_linattn_join(const ScanArgs a, int64_t 
 // Sum over the query heads of a key head, in order: x [rows][hk][group][d] -> out
 template <class T>
 __global__ void __launch_bounds__(256)
-    k_group_sum(const float* __restrict__ x, int64_t B, int64_t T_, int hk, int group, int d, Role o) {
+    k_group_sum(const float* __restrict__ xk, const float* __restrict__ xv, int64_t B, int64_t T_, int hk, int group, int d,
+                Role ok, Role ov) {
+  const float* x = blockIdx.y ? xv : xk;
+  const Role& o = blockIdx.y ? ov : ok;
   const int ch = d / 4;
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t r = id / ch;  // (b, t, head)
@@ -646,57 +674,57 @@ __global__ void __launch_bounds__(NTHR)
 int pad_d(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 int chunk_of(int dtype, int64_t T) { return dtype == HG_DTYPE_F32 || T <= 32 ? 32 : 64; }
 
-// Segments of a walk: none while the heads fill the chip (a block per CU);
-// else enough for two blocks per CU, of at least four chunks each.
+// Segments of the walks: none while their heads give two blocks per CU; else
+// enough for that, of at least four chunks each.
 struct Segs {
   int n;
   int64_t len;
 };
-Segs segs_of(const hg_linattn_desc* A) {
-  const int64_t C = chunk_of(A->dtype, A->t), heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads);
+Segs segs_of(const hg_linattn_desc* A, int walks) {
+  const int64_t C = chunk_of(A->dtype, A->t), heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads * walks);
   int64_t n = 1;
-  if (heads < 256) n = std::max<int64_t>(1, std::min(cdiv(512, heads), A->t / (4 * C)));
+  if (heads < kBlocks) n = std::max<int64_t>(1, std::min(cdiv(kBlocks, heads), A->t / (4 * C)));
   const int64_t len = cdiv(cdiv(std::max<int64_t>(A->t, 1), n), C) * C;
   return {(int)std::max<int64_t>(1, cdiv(A->t, len)), len};
 }
 
-int64_t seg_elems(const hg_linattn_desc* A) {
-  const Segs s = segs_of(A);
+// of one walk's states
+int64_t seg_elems(const hg_linattn_desc* A, int walks) {
+  const Segs s = segs_of(A, walks);
   const int64_t dp = pad_d(A->d);
   return s.n > 1 ? (int64_t)A->batch * A->heads * s.n * dp * dp : 0;
 }
 
-template <class T, class TO, int DP, int C>
-int launch_scan(const char* name, ScanArgs a, int64_t B, hipStream_t s) {
-  const int64_t bhs = B * a.H;
-  const dim3 grid((unsigned)bhs, (unsigned)a.segs), block(Shape<DP>::THREADS);
-  if (a.segs > 1) {
-    HG_LAUNCH("linattn_sums", (k_linattn_scan<T, TO, DP, C, true>), grid, block, 0, s, a);
-    HG_LAUNCH("linattn_join", (k_linattn_join<DP>), dim3((unsigned)cdiv(bhs * (DP / 16) * (DP / 16) * 64, 256)), dim3(256),
-              0, s, a, bhs);
+// `sums` of the n walks, the first ones, form their own segment sums.
+template <class T, int DP, int C>
+int launch_scan(const char* name, const Walks& w, int sums, int n, int64_t B, hipStream_t s) {
+  const int64_t bhs = B * w.w[0].H;
+  const unsigned segs = (unsigned)w.w[0].segs;
+  if (segs > 1) {
+    HG_LAUNCH("linattn_sums", (k_linattn_scan<T, DP, C, true>), dim3((unsigned)bhs, segs, sums), dim3(Shape<DP>::THREADS), 0,
+              s, w);
+    HG_LAUNCH("linattn_join", (k_linattn_join<DP>),
+              dim3((unsigned)cdiv(bhs * (DP / 16) * (DP / 16) * 64, 256), 1, sums), dim3(256), 0, s, w, bhs);
   }
-  HG_LAUNCH(name, (k_linattn_scan<T, TO, DP, C, false>), grid, block, 0, s, a);
+  HG_LAUNCH(name, (k_linattn_scan<T, DP, C, false>), dim3((unsigned)bhs, segs, n), dim3(Shape<DP>::THREADS), 0, s, w);
   return HG_OK;
 }
 
-template <class T, class TO, int C>
-int scan_d(const char* name, const ScanArgs& a, int64_t B, hipStream_t s) {
-  switch (pad_d(a.d)) {
-    case 16: return launch_scan<T, TO, 16, C>(name, a, B, s);
-    case 32: return launch_scan<T, TO, 32, C>(name, a, B, s);
-    case 64: return launch_scan<T, TO, 64, C>(name, a, B, s);
-    case 96: return launch_scan<T, TO, 96, C>(name, a, B, s);
-    default: return launch_scan<T, TO, 128, C>(name, a, B, s);
+template <class T, int C>
+int scan_d(const char* name, const Walks& w, int sums, int n, int64_t B, hipStream_t s) {
+  switch (pad_d(w.w[0].d)) {
+    case 16: return launch_scan<T, 16, C>(name, w, sums, n, B, s);
+    case 32: return launch_scan<T, 32, C>(name, w, sums, n, B, s);
+    case 64: return launch_scan<T, 64, C>(name, w, sums, n, B, s);
+    case 96: return launch_scan<T, 96, C>(name, w, sums, n, B, s);
+    default: return launch_scan<T, 128, C>(name, w, sums, n, B, s);
   }
 }
 
-// f32_out: o is float32 whatever dtype is
-int scan(const char* name, const hg_linattn_desc* A, const ScanArgs& a, bool f32_out, hipStream_t s) {
-  if (A->dtype == HG_DTYPE_F32) return scan_d<float, float, 32>(name, a, A->batch, s);
-  const bool small = chunk_of(A->dtype, A->t) == 32;
-  if (f32_out)
-    return small ? scan_d<bf16_t, float, 32>(name, a, A->batch, s) : scan_d<bf16_t, float, 64>(name, a, A->batch, s);
-  return small ? scan_d<bf16_t, bf16_t, 32>(name, a, A->batch, s) : scan_d<bf16_t, bf16_t, 64>(name, a, A->batch, s);
+int scan(const char* name, const hg_linattn_desc* A, const Walks& w, int sums, int n, hipStream_t s) {
+  if (A->dtype == HG_DTYPE_F32) return scan_d<float, 32>(name, w, sums, n, A->batch, s);
+  if (chunk_of(A->dtype, A->t) == 32) return scan_d<bf16_t, 32>(name, w, sums, n, A->batch, s);
+  return scan_d<bf16_t, 64>(name, w, sums, n, A->batch, s);
 }
 
 int check(const hg_linattn_desc* A, const char* what) {
@@ -732,12 +760,11 @@ Role role(const hg_linattn_desc* A, const hg_heads* x, int hdiv) {
   return Role{x->p, x->batch, A->t > 1 ? x->token : A->d, x->head, hdiv};
 }
 
-ScanArgs args_of(const hg_linattn_desc* A, const float* log_decay, const int32_t* lens, float* seg) {
-  const Segs sg = segs_of(A);
-  ScanArgs a{};
+Walk walk_of(const hg_linattn_desc* A, int walks, const float* log_decay, const int32_t* lens) {
+  const Segs sg = segs_of(A, walks);
+  Walk a{};
   a.log_decay = log_decay;
   a.lens = lens;
-  a.seg = sg.n > 1 ? seg : nullptr;
   a.T = A->t;
   a.seg_len = sg.len;
   a.segs = sg.n;
@@ -748,29 +775,35 @@ ScanArgs args_of(const hg_linattn_desc* A, const float* log_decay, const int32_t
 }
 
 struct Bufs {
-  float* seg = nullptr;
-  float* part = nullptr;  // gradients of k and v for each query head
+  float *seg0 = nullptr, *seg1 = nullptr;    // states of the segments: S, and in the backward R
+  float *partk = nullptr, *partv = nullptr;  // gradients of k and v for each query head
 };
 
 template <class Mem>
 Bufs take(const hg_linattn_desc* A, bool bwd, Mem& m) {
   Bufs b;
-  b.seg = m.template take<float>(seg_elems(A));
-  if (bwd && A->heads != A->kv_heads) b.part = m.template take<float>((int64_t)A->batch * A->t * A->heads * A->d);
+  const int walks = bwd ? 3 : 1;
+  b.seg0 = m.template take<float>(seg_elems(A, walks));
+  if (bwd) b.seg1 = m.template take<float>(seg_elems(A, walks));
+  if (bwd && A->heads != A->kv_heads) {
+    const int64_t n = (int64_t)A->batch * A->t * A->heads * A->d;
+    b.partk = m.template take<float>(n);
+    b.partv = m.template take<float>(n);
+  }
   return b;
 }
 
-int sum_groups(const hg_linattn_desc* A, const float* part, const hg_heads* o, hipStream_t s) {
+int sum_groups(const hg_linattn_desc* A, const Bufs& b, const hg_heads* dk, const hg_heads* dv, hipStream_t s) {
   const int64_t rows = (int64_t)A->batch * A->t * A->kv_heads;
   if (rows == 0) return HG_OK;
-  const dim3 grid((unsigned)cdiv(rows * (A->d / 4), 256));
+  const dim3 grid((unsigned)cdiv(rows * (A->d / 4), 256), 2);
   const int group = A->heads / A->kv_heads;
   if (A->dtype == HG_DTYPE_F32) {
-    HG_LAUNCH("group_sum", k_group_sum<float>, grid, dim3(256), 0, s, part, (int64_t)A->batch, A->t, A->kv_heads, group,
-              A->d, role(A, o, 1));
+    HG_LAUNCH("group_sum", k_group_sum<float>, grid, dim3(256), 0, s, b.partk, b.partv, (int64_t)A->batch, A->t,
+              A->kv_heads, group, A->d, role(A, dk, 1), role(A, dv, 1));
   } else {
-    HG_LAUNCH("group_sum", k_group_sum<bf16_t>, grid, dim3(256), 0, s, part, (int64_t)A->batch, A->t, A->kv_heads, group,
-              A->d, role(A, o, 1));
+    HG_LAUNCH("group_sum", k_group_sum<bf16_t>, grid, dim3(256), 0, s, b.partk, b.partv, (int64_t)A->batch, A->t,
+              A->kv_heads, group, A->d, role(A, dk, 1), role(A, dv, 1));
   }
   return HG_OK;
 }
@@ -813,7 +846,9 @@ extern "C" int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const
     return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
   Arena m(ws, ws_bytes);
   const Bufs b = take(A, false, m);
-  ScanArgs a = args_of(A, log_decay, lens, b.seg);
+  Walks ws_{};
+  Walk& a = ws_.w[0];
+  a = walk_of(A, 1, log_decay, lens);
   const int group = A->heads / A->kv_heads;
   a.q = role(A, q, 1);
   a.k = role(A, k, group);
@@ -821,8 +856,9 @@ extern "C" int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const
   a.o = role(A, o, 1);
   a.s_in = state;
   a.s_out = state_out;
+  a.seg = b.seg0;
   a.o_scale = A->scale;
-  return scan("linattn", A, a, false, static_cast<hipStream_t>(stream));
+  return scan("linattn", A, ws_, 1, 1, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
@@ -848,37 +884,41 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
   Arena m(ws, ws_bytes);
   const Bufs b = take(A, true, m);
   const int group = A->heads / A->kv_heads;
-  ScanArgs a = args_of(A, log_decay, lens, b.seg);
-  // dq: its state is the transpose of the forward's
-  a.q = role(A, d_o, 1);
-  a.k = role(A, v, group);
-  a.v = role(A, k, group);
-  a.o = role(A, dq, 1);
-  a.s_in = state;
-  a.s_trans = 1;
-  a.o_scale = A->scale;
-  HG_TRY(scan("linattn_dq", A, a, false, s));
-  // dk and dv: from the last token, for each query head
   const int64_t H = A->heads, d = A->d;
-  const Role part{b.part, A->t * H * d, H * d, d, 1};
-  a.reverse = 1;
-  a.kv_scale = A->scale;
-  a.o_scale = 1.f;
-  a.s_in = dstate_out;
-  a.q = role(A, v, group);
-  a.k = role(A, d_o, 1);
-  a.v = role(A, q, 1);
-  a.o = group > 1 ? part : role(A, dk, 1);
-  HG_TRY(scan("linattn_dk", A, a, group > 1, s));
-  if (group > 1) HG_TRY(sum_groups(A, b.part, dk, s));
-  a.s_trans = 0;
-  a.s_out = dstate;
-  a.q = role(A, k, group);
-  a.k = role(A, q, 1);
-  a.v = role(A, d_o, 1);
-  a.o = group > 1 ? part : role(A, dv, 1);
-  HG_TRY(scan("linattn_dv", A, a, group > 1, s));
-  if (group > 1) HG_TRY(sum_groups(A, b.part, dv, s));
+  Walks w{};
+  Walk &wq = w.w[0], &wv = w.w[1], &wk = w.w[2];
+  wq = wv = walk_of(A, 3, log_decay, lens);
+  // dq: its state is the transpose of the forward's
+  wq.q = role(A, d_o, 1);
+  wq.k = role(A, v, group);
+  wq.v = role(A, k, group);
+  wq.o = role(A, dq, 1);
+  wq.s_in = state;
+  wq.s_trans = 1;
+  wq.seg = b.seg0;
+  wq.o_scale = A->scale;
+  // dv: from the last token, for each query head
+  wv.reverse = 1;
+  wv.kv_scale = A->scale;
+  wv.q = role(A, k, group);
+  wv.k = role(A, q, 1);
+  wv.v = role(A, d_o, 1);
+  wv.o = group > 1 ? Role{b.partv, A->t * H * d, H * d, d, 1} : role(A, dv, 1);
+  wv.f32_out = group > 1;
+  wv.s_in = dstate_out;
+  wv.s_out = dstate;
+  wv.seg = b.seg1;
+  // dk: its state is the transpose of dv's
+  wk = wv;
+  wk.q = role(A, v, group);
+  wk.k = role(A, d_o, 1);
+  wk.v = role(A, q, 1);
+  wk.o = group > 1 ? Role{b.partk, A->t * H * d, H * d, d, 1} : role(A, dk, 1);
+  wk.s_trans = 1;
+  wk.seg_trans = 1;
+  wk.s_out = nullptr;
+  HG_TRY(scan("linattn_bwd", A, w, 2, 3, s));
+  if (group > 1) HG_TRY(sum_groups(A, b, dk, dv, s));
   return HG_OK;
 }
 

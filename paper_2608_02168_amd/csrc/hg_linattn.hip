@@ -44,7 +44,6 @@ namespace hg {
 namespace {
 
 constexpr int kMaxD = 128;
-constexpr int64_t kBlocks = 512;  // two for each CU
 constexpr int64_t kMaxToken = 1 << 22;  // token stride: a chunk of 64 stays below 2^31 bytes
 
 // One operand: element (sequence b, token t, head h, column x) at
@@ -137,14 +136,37 @@ __device__ __forceinline__ f32x4 mma32(f32x4 a0, f32x4 a1, f32x4 b0, f32x4 b1, f
   return acc;
 }
 
+// acc += A B over 16 values
+__device__ __forceinline__ f32x4 mma16(uint2 a, uint2 b, f32x4 acc) {
+  return mma32(a, uint2{0u, 0u}, b, uint2{0u, 0u}, acc);
+}
+__device__ __forceinline__ f32x4 mma16(f32x4 a, f32x4 b, f32x4 acc) {
+#pragma unroll
+  for (int v = 0; v < 4; ++v) acc = mfma4(a[v], b[v], acc);
+  return acc;
+}
+
 template <class T, int DP>
 struct Tile {
   static constexpr int EL = Elt<T>::EL;
-  static constexpr int LD = DP + EL;  // 16 bytes more: 16 rows' chunks fall on all banks
+  // 16 bytes more than the row (bfloat16: 32, for the transposing reads of 4 rows
+  // a lane group): the rows that one read touches fall on all banks
+  static constexpr int LD = DP + (sizeof(T) == 4 ? 4 : 16);
   typedef typename Blk<T>::type B;
   // 16 columns of row r: lane's four
   static __device__ __forceinline__ B row4(const T* t, int r, int blk, int g) {
     return *reinterpret_cast<const B*>(t + r * LD + 16 * blk + 4 * g);
+  }
+  // 32 columns of row r: lane's eight, 8 g .. (float32: four and four of two blocks)
+  static __device__ __forceinline__ void row8(const T* t, int r, int blk, int g, B& x, B& y) {
+    if constexpr (sizeof(T) == 2) {
+      const uint4 w = *reinterpret_cast<const uint4*>(t + r * LD + 16 * blk + 8 * g);
+      x = uint2{w.x, w.y};
+      y = uint2{w.z, w.w};
+    } else {
+      x = row4(t, r, blk, g);
+      y = row4(t, r, blk + 1, g);
+    }
   }
   // rows 16 rb + 4 g .. + 3 of column 16 cb + c
   static __device__ __forceinline__ B col4(const T* t, int rb, int cb, int c, int g) {
@@ -352,12 +374,17 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Wa
         f32x4 s{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NB; i += 2) {
-          const bool two = i + 1 < NB;
-          const B k0 = TL::row4(lk, 16 * kt + c, i, g), q0 = TL::row4(lq, 16 * r + c, i, g);
-          const B k1 = two ? TL::row4(lk, 16 * kt + c, two ? i + 1 : i, g) : Blk<T>::zero();
-          const B q1 = two ? TL::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
+          B k0, k1, q0, q1;
+          if (i + 1 < NB) {
+            TL::row8(lk, 16 * kt + c, i, g, k0, k1);
+            TL::row8(lq, 16 * r + c, i, g, q0, q1);
+          } else {
+            k0 = TL::row4(lk, 16 * kt + c, i, g);
+            q0 = TL::row4(lq, 16 * r + c, i, g);
+            k1 = q1 = Blk<T>::zero();
+          }
           f32x4& acc = (i & 2) ? s1 : s;  // two chains
-          acc = mma32(k0, k1, q0, q1, acc);
+          acc = i + 1 < NB ? mma32(k0, k1, q0, q1, acc) : mma16(k0, q0, acc);
         }
 #pragma unroll
         for (int v = 0; v < 4; ++v) s[v] += s1[v];
@@ -403,7 +430,8 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Wa
 #pragma unroll
           for (int r = 0; r < RB; ++r)
 #pragma unroll
-            for (int j = 0; j < NT; ++j) o[r][j] = mma32(s0[j].x[x], s1[j].x[x], q0[r], q1[r], o[r][j]);
+            for (int j = 0; j < NT; ++j)
+              o[r][j] = two ? mma32(s0[j].x[x], s1[j].x[x], q0[r], q1[r], o[r][j]) : mma16(s0[j].x[x], q0[r], o[r][j]);
       }
       float rowp = row0;
 #pragma unroll
@@ -425,17 +453,13 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Wa
 #pragma unroll
         for (int r = kt; r < RB; ++r) {
           const Factor<T> p0 = lp[r * (r + 1) / 2 + kt][lane];
-          Factor<T> p1;
-          if (r > kt) {
-            p1 = lp[r * (r + 1) / 2 + kt + 1][lane];
-          } else {
-            p1.zero();
-          }
+          Factor<T> p1 = p0;
+          if (r > kt) p1 = lp[r * (r + 1) / 2 + kt + 1][lane];
 #pragma unroll
           for (int x = Factor<T>::N - 1; x >= 0; --x)
 #pragma unroll
             for (int j = 0; j < NT; ++j)
-              o[r][j] = mma32(v0[j], r > kt ? v1[j] : Blk<T>::zero(), p0.x[x], p1.x[x], o[r][j]);
+              o[r][j] = r > kt ? mma32(v0[j], v1[j], p0.x[x], p1.x[x], o[r][j]) : mma16(v0[j], p0.x[x], o[r][j]);
         }
       }
 #pragma unroll
@@ -674,8 +698,12 @@ __global__ void __launch_bounds__(NTHR)
 int pad_d(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
 int chunk_of(int dtype, int64_t T) { return dtype == HG_DTYPE_F32 || T <= 32 ? 32 : 64; }
 
-// Segments of the walks: none while their heads give two blocks per CU; else
-// enough for that, of at least four chunks each.
+// Segments of the walks: none while their heads fill the chip; else enough for
+// that, of at least four chunks each.  Full is a block a CU from d = 96 on (eight
+// waves of 200 registers are what fits: 144 us at 256 blocks, 162 at 512 for
+// 16 heads of 16381 tokens, d = 128), 4096 waves below (backward of 128 heads,
+// 2048 tokens, d = 64: 134 us at 1024 blocks, 143 at 512).
+int64_t full_blocks(int d) { return pad_d(d) >= 96 ? 256 : 4096 / (pad_d(d) / 16); }
 struct Segs {
   int n;
   int64_t len;
@@ -683,7 +711,8 @@ struct Segs {
 Segs segs_of(const hg_linattn_desc* A, int walks) {
   const int64_t C = chunk_of(A->dtype, A->t), heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads * walks);
   int64_t n = 1;
-  if (heads < kBlocks) n = std::max<int64_t>(1, std::min(cdiv(kBlocks, heads), A->t / (4 * C)));
+  const int64_t full = full_blocks(A->d);
+  if (heads < full) n = std::max<int64_t>(1, std::min(cdiv(full, heads), A->t / (4 * C)));
   const int64_t len = cdiv(cdiv(std::max<int64_t>(A->t, 1), n), C) * C;
   return {(int)std::max<int64_t>(1, cdiv(A->t, len)), len};
 }

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import Optional
 
@@ -669,35 +670,49 @@ def hg_align_loss_fwd_bwd_noalloc(H, overlap, H_ref, dH, loss3, w=None, lambda_n
 
 
 # ---- sequence encoder -------------------------------------------------------
+# These calls are made for single tokens too, so their marshalling is kept
+# short: descriptors are packed bytes (the layouts of LinearDesc, GluDesc,
+# RopeDesc, LinattnDesc and Heads), devices are compared by index.
+
+_pack_linear = struct.Struct("@qiiiiqqq").pack
+_pack_glu = struct.Struct("@qiiiiqqq").pack
+_pack_rope = struct.Struct("@qqiiiiiifi").pack
+_pack_linattn = struct.Struct("@qiiiiif").pack
+_pack_heads = struct.Struct("@Pqqq").pack
+_DTYPES = {torch.float32: HG_DTYPE_F32, torch.bfloat16: HG_DTYPE_BF16}
+
 
 def _float_code(where: str, t) -> int:
-    if t.dtype == torch.float32:
-        return HG_DTYPE_F32
-    if t.dtype == torch.bfloat16:
-        return HG_DTYPE_BF16
-    raise TypeError(f"{where}: {t.dtype} is neither float32 nor bfloat16")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{where}: {t.dtype} is neither float32 nor bfloat16")
+    return code
 
 
 def _same(where: str, t, *others):
     """Every given tensor has the first one's type and device."""
+    dtype, dev = t.dtype, t.get_device()
     for o in others:
-        if o is not None and (o.dtype != t.dtype or o.device != t.device):
+        if o is not None and (o.dtype is not dtype or o.get_device() != dev):
             raise TypeError(f"{where}: {o.dtype} on {o.device} beside {t.dtype} on {t.device}")
 
 
-def _vector(where: str, t, n: int, device, dtype=torch.float32):
-    """A contiguous vector of n values, or None."""
-    if t is not None and (t.dtype != dtype or t.device != device or t.numel() != n or not t.is_contiguous()):
-        raise ValueError(f"{where}: expected {n} contiguous {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on "
+def _vector(where: str, t, n: int, like, dtype=torch.float32):
+    """A contiguous vector of n values on like's device, or None; its address."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{where}: expected {n} contiguous {dtype} on {like.device}, got {tuple(t.shape)} {t.dtype} on "
                          f"{t.device}")
+    return t.data_ptr()
 
 
 def _rows(where: str, t, n: int, width: int) -> int:
     """Checks an [n, width] matrix whose rows are contiguous; returns their distance."""
-    if t.shape != (n, width) or (width > 1 and n > 0 and t.stride(1) != 1):
-        raise ValueError(f"{where}: expected rows [{n}, {width}] with unit column stride, got {tuple(t.shape)} "
-                         f"strides {t.stride()}")
-    return t.stride(0) if n > 1 else max(width, t.stride(0)) if n else width
+    s = t.stride()
+    if t.shape != (n, width) or (s[1] != 1 and width > 1 and n > 0):
+        raise ValueError(f"{where}: expected rows [{n}, {width}] with unit column stride, got {tuple(t.shape)} strides {s}")
+    return s[0] if n > 1 else width
 
 
 def _matrix(where: str, t, rows: int, cols: int):
@@ -705,32 +720,62 @@ def _matrix(where: str, t, rows: int, cols: int):
         raise ValueError(f"{where}: expected a contiguous [{rows}, {cols}], got {tuple(t.shape)} strides {t.stride()}")
 
 
-def _ws_for(ws, need: int, device):
-    if ws is None and need:
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    return (None, 0) if ws is None else (C.c_void_p(ws.data_ptr()), ws.numel())
+def _heads(where: str, name: str, t, shape, single=False) -> bytes:
+    """hg_heads of a [tokens, heads, d] or [batch, tokens, heads, d] tensor.  The
+    stride of a dimension with one entry is never walked."""
+    s = t.stride()
+    if t.shape != shape or (s[-1] != 1 and t.numel()):
+        raise ValueError(f"{where}: expected {name} {tuple(shape)} with unit stride in a head, got {tuple(t.shape)} "
+                         f"strides {s}")
+    if len(s) == 3:  # tokens, or with `single` sequences of one token
+        n, h, _ = shape
+        st, sh = s[0] if n > 1 else 0, s[1] if h > 1 else 0
+        return _pack_heads(t.data_ptr(), st, 0, sh) if single else _pack_heads(t.data_ptr(), 0, st, sh)
+    b, n, h, _ = shape
+    return _pack_heads(t.data_ptr(), s[0] if b > 1 else 0, s[1] if n > 1 else 0, s[2] if h > 1 else 0)
 
 
-def _linear_desc(where, x, W, y_cols, act) -> LinearDesc:
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(ws, need: int, like):
+    """(buffer kept alive by the caller, its address, its size)"""
+    if ws is None:
+        if not need:
+            return None, None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return ws, ws.data_ptr(), ws.numel()
+
+
+def _raw_stream(like, stream):
+    """The given stream, or the current one of the tensor's device."""
+    if stream is None:
+        return torch.cuda.current_stream(like.device).cuda_stream if _current_raw is None else \
+            _current_raw(like.get_device())
+    return stream.cuda_stream
+
+
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _linear_sizes(where, x, W):
     n, d = x.shape
-    _same(where, x, W)
-    _matrix(where, W, d, y_cols)
-    return LinearDesc(n, d, y_cols, _float_code(where, x), act, _rows(where, x, n, d), y_cols, y_cols)
+    m = W.shape[1]
+    _matrix(where, W, d, m)
+    return n, d, m
 
 
 def hg_linear_fwd_workspace_size(n: int, d_in: int, d_out: int, dtype=torch.float32, act: int = HG_ACT_NONE,
                                  ld_x: Optional[int] = None) -> int:
-    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
-    desc = LinearDesc(n, d_in, d_out, code, act, d_in if ld_x is None else ld_x, d_out, d_out)
-    return int(lib().hg_linear_fwd_workspace_size(C.byref(desc)))
+    return int(lib().hg_linear_fwd_workspace_size(_pack_linear(
+        n, d_in, d_out, _DTYPES[dtype], act, d_in if ld_x is None else ld_x, d_out, d_out)))
 
 
 def hg_linear_bwd_workspace_size(n: int, d_in: int, d_out: int, dtype=torch.float32, act: int = HG_ACT_NONE,
                                  ld_x: Optional[int] = None, ld_dy: Optional[int] = None) -> int:
-    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
-    desc = LinearDesc(n, d_in, d_out, code, act, d_in if ld_x is None else ld_x, d_out if ld_dy is None else ld_dy,
-                      d_in)
-    return int(lib().hg_linear_bwd_workspace_size(C.byref(desc)))
+    return int(lib().hg_linear_bwd_workspace_size(_pack_linear(
+        n, d_in, d_out, _DTYPES[dtype], act, d_in if ld_x is None else ld_x, d_out if ld_dy is None else ld_dy, d_in)))
 
 
 def hg_linear_fwd(x, W, bias=None, residual=None, act: int = HG_ACT_NONE, y=None, ws=None, stream=None):
@@ -739,18 +784,20 @@ def hg_linear_fwd(x, W, bias=None, residual=None, act: int = HG_ACT_NONE, y=None
     may be strided, W is contiguous."""
     where = "hg_linear_fwd"
     L = lib()
-    n, m = int(x.shape[0]), int(W.shape[1])
-    desc = _linear_desc(where, x, W, m, act)
+    n, d, m = _linear_sizes(where, x, W)
     if y is None:
         y = torch.empty((n, m), dtype=x.dtype, device=x.device)
-    _same(where, x, y, residual)
-    _vector(where, bias, m, x.device)
-    desc.ld_y = _rows(where, y, n, m)
-    if residual is not None:
-        desc.ld_r = _rows(where, residual, n, m)
-    ref = C.byref(desc)
-    wp, wn = _ws_for(ws, L.hg_linear_fwd_workspace_size(ref), x.device)
-    _check(L.hg_linear_fwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(residual), _ptr(y), wp, wn, _stream(stream)), where)
+        ld_y = m
+    else:
+        ld_y = _rows(where, y, n, m)
+    _same(where, x, W, y, residual)
+    desc = _pack_linear(n, d, m, _float_code(where, x), act, _rows(where, x, n, d), ld_y,
+                        m if residual is None else _rows(where, residual, n, m))
+    ws, wp, wn = _workspace(ws, L.hg_linear_fwd_workspace_size(desc), x)
+    st = L.hg_linear_fwd(desc, x.data_ptr(), W.data_ptr(), _vector(where, bias, m, x), _addr(residual), y.data_ptr(), wp,
+                         wn, _raw_stream(x, stream))
+    if st:
+        _check(st, where)
     return y
 
 
@@ -762,17 +809,16 @@ def hg_linear_bwd(x, W, bias, dy, act: int = HG_ACT_NONE, dx=None, dW=None, dbia
     compute where no buffer is given."""
     where = "hg_linear_bwd"
     L = lib()
-    n, m = int(x.shape[0]), int(W.shape[1])
-    desc = _linear_desc(where, x, W, m, act)
+    n, d, m = _linear_sizes(where, x, W)
     dx, dW, dbias = _linear_grads(where, x, W, bias, dx, dW, dbias, accumulate, want)
-    _same(where, x, dy, dx, dW)
-    desc.ld_y = _rows(where, dy, n, m)
-    if dx is not None:
-        desc.ld_r = _rows(where, dx, n, x.shape[1])
-    ref = C.byref(desc)
-    wp, wn = _ws_for(ws, L.hg_linear_bwd_workspace_size(ref), x.device)
-    _check(L.hg_linear_bwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(dy), _ptr(dx), _ptr(dW), _ptr(dbias),
-                           int(bool(accumulate)), wp, wn, _stream(stream)), where)
+    _same(where, x, W, dy, dx, dW)
+    desc = _pack_linear(n, d, m, _float_code(where, x), act, _rows(where, x, n, d), _rows(where, dy, n, m),
+                        d if dx is None else _rows(where, dx, n, d))
+    ws, wp, wn = _workspace(ws, L.hg_linear_bwd_workspace_size(desc), x)
+    st = L.hg_linear_bwd(desc, x.data_ptr(), W.data_ptr(), _addr(bias), dy.data_ptr(), _addr(dx), _addr(dW), _addr(dbias),
+                         1 if accumulate else 0, wp, wn, _raw_stream(x, stream))
+    if st:
+        _check(st, where)
     return dx, dW, dbias
 
 
@@ -782,36 +828,32 @@ def _linear_grads(where, x, W, bias, dx, dW, dbias, accumulate, want):
     if dx is None and want[0]:
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     if dW is None and want[1]:
-        dW = torch.empty_like(W)
-    if dW is not None:
+        dW = torch.empty(W.shape, dtype=W.dtype, device=W.device)
+    elif dW is not None:
         _matrix(where, dW, *W.shape)
-    _vector(where, bias, W.shape[1], x.device)
+    _vector(where, bias, W.shape[1], x)
     if dbias is None and want[2] and bias is not None:
         dbias = torch.empty_like(bias)
-    _vector(where, dbias, W.shape[1], x.device)
+    _vector(where, dbias, W.shape[1], x)
     return dx, dW, dbias
 
 
-def _glu_desc(where, x, W, act) -> GluDesc:
+def _glu_sizes(where, x, W):
     n, d = x.shape
     if W.dim() != 2 or W.shape[1] % 2:
         raise ValueError(f"{where}: W is [d, 2 f], got {tuple(W.shape)}")
-    _same(where, x, W)
     _matrix(where, W, d, W.shape[1])
-    f = W.shape[1] // 2
-    return GluDesc(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), f, d)
+    return n, d, W.shape[1] // 2
 
 
 def hg_glu_fwd_workspace_size(n: int, d: int, f: int, dtype=torch.float32, ld_x: Optional[int] = None) -> int:
-    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
-    desc = GluDesc(n, d, f, code, HG_ACT_SILU, d if ld_x is None else ld_x, f, d)
-    return int(lib().hg_glu_fwd_workspace_size(C.byref(desc)))
+    return int(lib().hg_glu_fwd_workspace_size(_pack_glu(n, d, f, _DTYPES[dtype], HG_ACT_SILU,
+                                                         d if ld_x is None else ld_x, f, d)))
 
 
 def hg_glu_bwd_workspace_size(n: int, d: int, f: int, dtype=torch.float32, ld_x: Optional[int] = None) -> int:
-    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
-    desc = GluDesc(n, d, f, code, HG_ACT_SILU, d if ld_x is None else ld_x, f, d)
-    return int(lib().hg_glu_bwd_workspace_size(C.byref(desc)))
+    return int(lib().hg_glu_bwd_workspace_size(_pack_glu(n, d, f, _DTYPES[dtype], HG_ACT_SILU,
+                                                         d if ld_x is None else ld_x, f, d)))
 
 
 def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=None):
@@ -819,16 +861,19 @@ def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=
     columns first), bias float32 [2 f], h [n, f]."""
     where = "hg_glu_fwd"
     L = lib()
-    desc = _glu_desc(where, x, W, act)
-    n, f = int(x.shape[0]), int(desc.f)
+    n, d, f = _glu_sizes(where, x, W)
     if h is None:
         h = torch.empty((n, f), dtype=x.dtype, device=x.device)
-    _same(where, x, h)
-    _vector(where, bias, 2 * f, x.device)
-    desc.ld_h = _rows(where, h, n, f)
-    ref = C.byref(desc)
-    wp, wn = _ws_for(ws, L.hg_glu_fwd_workspace_size(ref), x.device)
-    _check(L.hg_glu_fwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(h), wp, wn, _stream(stream)), where)
+        ld_h = f
+    else:
+        ld_h = _rows(where, h, n, f)
+    _same(where, x, W, h)
+    desc = _pack_glu(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), ld_h, d)
+    ws, wp, wn = _workspace(ws, L.hg_glu_fwd_workspace_size(desc), x)
+    st = L.hg_glu_fwd(desc, x.data_ptr(), W.data_ptr(), _vector(where, bias, 2 * f, x), h.data_ptr(), wp, wn,
+                      _raw_stream(x, stream))
+    if st:
+        _check(st, where)
     return h
 
 
@@ -837,33 +882,17 @@ def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=N
     """Returns (dx, dW, dbias) of hg_glu_fwd for dh = dL/dh, as hg_linear_bwd does."""
     where = "hg_glu_bwd"
     L = lib()
-    desc = _glu_desc(where, x, W, act)
-    n, f = int(x.shape[0]), int(desc.f)
+    n, d, f = _glu_sizes(where, x, W)
     dx, dW, dbias = _linear_grads(where, x, W, bias, dx, dW, dbias, accumulate, want)
-    _same(where, x, dh, dx, dW)
-    desc.ld_h = _rows(where, dh, n, f)
-    if dx is not None:
-        desc.ld_dx = _rows(where, dx, n, x.shape[1])
-    ref = C.byref(desc)
-    wp, wn = _ws_for(ws, L.hg_glu_bwd_workspace_size(ref), x.device)
-    _check(L.hg_glu_bwd(ref, _ptr(x), _ptr(W), _ptr(bias), _ptr(dh), _ptr(dx), _ptr(dW), _ptr(dbias),
-                        int(bool(accumulate)), wp, wn, _stream(stream)), where)
+    _same(where, x, W, dh, dx, dW)
+    desc = _pack_glu(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), _rows(where, dh, n, f),
+                     d if dx is None else _rows(where, dx, n, d))
+    ws, wp, wn = _workspace(ws, L.hg_glu_bwd_workspace_size(desc), x)
+    st = L.hg_glu_bwd(desc, x.data_ptr(), W.data_ptr(), _addr(bias), dh.data_ptr(), _addr(dx), _addr(dW), _addr(dbias),
+                      1 if accumulate else 0, wp, wn, _raw_stream(x, stream))
+    if st:
+        _check(st, where)
     return dx, dW, dbias
-
-
-def _stride(t, i: int, unit: int) -> int:
-    """Stride of a dimension; one of a single entry is never walked."""
-    return t.stride(i) if t.shape[i] > 1 else unit
-
-
-def _heads(where: str, name: str, t, shape):
-    """hg_heads of a [tokens, heads, d] or [batch, tokens, heads, d] tensor
-    (or [batch, heads, d] with the token dimension left out of the shape)."""
-    if tuple(t.shape) != tuple(shape) or (shape[-1] > 1 and t.numel() and t.stride(-1) != 1):
-        raise ValueError(f"{where}: expected {name} {tuple(shape)} with unit stride in a head, got {tuple(t.shape)} "
-                         f"strides {t.stride()}")
-    s = [_stride(t, i, 0) for i in range(t.dim() - 1)]
-    return Heads(t.data_ptr() if t.numel() else None, s[0] if len(s) == 3 else 0, s[-2], s[-1])
 
 
 def hg_rope_table(n_pos: int, rot: int, base: float = 10000.0, step: float = 1.0, table=None, device="cuda",
@@ -873,21 +902,19 @@ def hg_rope_table(n_pos: int, rot: int, base: float = 10000.0, step: float = 1.0
         table = torch.empty((n_pos, rot), dtype=torch.float32, device=device)
     elif tuple(table.shape) != (n_pos, rot) or table.dtype != torch.float32 or not table.is_contiguous():
         raise ValueError(f"hg_rope_table: expected a contiguous float32 [{n_pos}, {rot}], got {tuple(table.shape)}")
-    _check(lib().hg_rope_table(n_pos, rot, base, step, _ptr(table), _stream(stream)), "hg_rope_table")
+    _check(lib().hg_rope_table(n_pos, rot, base, step, table.data_ptr(), _raw_stream(table, stream)), "hg_rope_table")
     return table
 
 
-def _rope_desc(where, q, k, wq, wk, table, pos, eps, interleaved):
+def _rope_desc(where, q, k, table, eps, interleaved):
     n, hq, d = q.shape
-    _same(where, q, k)
-    _vector(where, wq, d, q.device)
-    _vector(where, wk, d, q.device)
-    _vector(where, pos, n, q.device, torch.int32)
-    if table.dim() != 2 or table.dtype != torch.float32 or table.device != q.device or not table.is_contiguous():
+    hk = 0 if k is None else k.shape[1]
+    if (table.dim() != 2 or table.dtype is not torch.float32 or table.get_device() != q.get_device()
+            or not table.is_contiguous()):
         raise ValueError(f"{where}: expected a contiguous float32 table [positions, rot], got {tuple(table.shape)}")
-    hk = 0 if k is None else int(k.shape[1])
-    return RopeDesc(n, table.shape[0], hq, hk, d, table.shape[1], int(bool(interleaved)), _float_code(where, q),
-                    eps, 0), (n, hq, d), (n, hk, d)
+    n_pos, rot = table.shape
+    return _pack_rope(n, n_pos, hq, hk, d, rot, 1 if interleaved else 0, _float_code(where, q), eps, 0), \
+        (n, hq, d), (n, hk, d)
 
 
 def hg_qk_norm_rope_fwd(q, k, wq, wk, table, pos, eps: float = 1e-6, interleaved: bool = False, q_out=None,
@@ -897,17 +924,19 @@ def hg_qk_norm_rope_fwd(q, k, wq, wk, table, pos, eps: float = 1e-6, interleaved
     float32 [d] or None, table [positions, rot] from hg_rope_table, pos int32
     [n].  Returns (q_out, k_out); they may be q and k themselves."""
     where = "hg_qk_norm_rope_fwd"
-    desc, qs, ks = _rope_desc(where, q, k, wq, wk, table, pos, eps, interleaved)
+    desc, qs, ks = _rope_desc(where, q, k, table, eps, interleaved)
     if q_out is None:
         q_out = torch.empty(qs, dtype=q.dtype, device=q.device)
     if k is not None and k_out is None:
         k_out = torch.empty(ks, dtype=q.dtype, device=q.device)
-    _same(where, q, q_out, k_out)
-    hq, ho = _heads(where, "q", q, qs), _heads(where, "q_out", q_out, qs)
+    _same(where, q, k, q_out, k_out)
     hk, hl = (None, None) if k is None else (_heads(where, "k", k, ks), _heads(where, "k_out", k_out, ks))
-    ref = C.byref
-    _check(lib().hg_qk_norm_rope_fwd(ref(desc), ref(hq), hk and ref(hk), _ptr(wq), _ptr(wk), _ptr(table), _ptr(pos),
-                                     ref(ho), hl and ref(hl), _stream(stream)), where)
+    st = lib().hg_qk_norm_rope_fwd(desc, _heads(where, "q", q, qs), hk, _vector(where, wq, qs[2], q),
+                                   _vector(where, wk, qs[2], q), table.data_ptr(),
+                                   _vector(where, pos, qs[0], q, torch.int32), _heads(where, "q_out", q_out, qs), hl,
+                                   _raw_stream(q, stream))
+    if st:
+        _check(st, where)
     return q_out, k_out
 
 
@@ -917,7 +946,7 @@ def hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps: float = 1
     them); dwq and dwk for the weights given, added into when accumulate."""
     where = "hg_qk_norm_rope_bwd"
     L = lib()
-    desc, qs, ks = _rope_desc(where, q, k, wq, wk, table, pos, eps, interleaved)
+    desc, qs, ks = _rope_desc(where, q, k, table, eps, interleaved)
     if accumulate and ((wq is not None and dwq is None) or (wk is not None and dwk is None)):
         raise ValueError(f"{where}: accumulate needs the buffers to add into")
     if dq is None:
@@ -928,41 +957,34 @@ def hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps: float = 1
         dwq = torch.empty_like(wq)
     if dwk is None and wk is not None:
         dwk = torch.empty_like(wk)
-    _vector(where, dwq, qs[2], q.device)
-    _vector(where, dwk, qs[2], q.device)
-    _same(where, q, dq_out, dk_out, dq, dk)
-    h = [_heads(where, n, t, s) for n, t, s in (("q", q, qs), ("dq_out", dq_out, qs), ("dq", dq, qs))]
+    _same(where, q, k, dq_out, dk_out, dq, dk)
+    h = [_heads(where, n, t, qs) for n, t in (("q", q), ("dq_out", dq_out), ("dq", dq))]
     g = [None if k is None else _heads(where, n, t, ks) for n, t in (("k", k), ("dk_out", dk_out), ("dk", dk))]
-    ref = C.byref
-    rh, rg = [ref(x) for x in h], [x and ref(x) for x in g]
-    wp, wn = _ws_for(ws, L.hg_qk_norm_rope_bwd_workspace_size(ref(desc)), q.device)
-    _check(L.hg_qk_norm_rope_bwd(ref(desc), rh[0], rg[0], _ptr(wq), _ptr(wk), _ptr(table), _ptr(pos), rh[1], rg[1],
-                                 rh[2], rg[2], _ptr(dwq), _ptr(dwk), int(bool(accumulate)), wp, wn, _stream(stream)),
-           where)
+    ws, wp, wn = _workspace(ws, L.hg_qk_norm_rope_bwd_workspace_size(desc), q)
+    d = qs[2]
+    st = L.hg_qk_norm_rope_bwd(desc, h[0], g[0], _vector(where, wq, d, q), _vector(where, wk, d, q), table.data_ptr(),
+                               _vector(where, pos, qs[0], q, torch.int32), h[1], g[1], h[2], g[2],
+                               _vector(where, dwq, d, q), _vector(where, dwk, d, q), 1 if accumulate else 0, wp, wn,
+                               _raw_stream(q, stream))
+    if st:
+        _check(st, where)
     return dq, dk, dwq, dwk
 
 
-def _linattn_desc(where, q, k, v, log_decay, scale, lens, states) -> LinattnDesc:
-    b, t, h, d = q.shape
-    _same(where, q, k, v)
-    _vector(where, log_decay, h, q.device)
-    _vector(where, lens, b, q.device, torch.int32)
-    for s in states:
-        if s is not None and (tuple(s.shape) != (b, h, d, d) or s.dtype != torch.float32 or s.device != q.device
-                              or not s.is_contiguous()):
-            raise ValueError(f"{where}: expected a contiguous float32 state [{b}, {h}, {d}, {d}], got "
-                             f"{tuple(s.shape)} {s.dtype}")
-    return LinattnDesc(t, b, h, k.shape[2], d, _float_code(where, q), scale)
+def _state(where, s, shape, like):
+    if s is None:
+        return None
+    if s.shape != shape or s.dtype is not torch.float32 or s.get_device() != like.get_device() or not s.is_contiguous():
+        raise ValueError(f"{where}: expected a contiguous float32 state {tuple(shape)}, got {tuple(s.shape)} {s.dtype}")
+    return s.data_ptr()
 
 
 def hg_linattn_fwd_workspace_size(batch: int, t: int, heads: int, kv_heads: int, d: int, dtype=torch.float32) -> int:
-    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
-    return int(lib().hg_linattn_fwd_workspace_size(C.byref(LinattnDesc(t, batch, heads, kv_heads, d, code, 1.0))))
+    return int(lib().hg_linattn_fwd_workspace_size(_pack_linattn(t, batch, heads, kv_heads, d, _DTYPES[dtype], 1.0)))
 
 
 def hg_linattn_bwd_workspace_size(batch: int, t: int, heads: int, kv_heads: int, d: int, dtype=torch.float32) -> int:
-    code = HG_DTYPE_BF16 if dtype == torch.bfloat16 else HG_DTYPE_F32
-    return int(lib().hg_linattn_bwd_workspace_size(C.byref(LinattnDesc(t, batch, heads, kv_heads, d, code, 1.0))))
+    return int(lib().hg_linattn_bwd_workspace_size(_pack_linattn(t, batch, heads, kv_heads, d, _DTYPES[dtype], 1.0)))
 
 
 def hg_linattn_fwd(q, k, v, log_decay, scale: float = 1.0, lens=None, state=None, o=None, state_out=None,
@@ -973,20 +995,22 @@ def hg_linattn_fwd(q, k, v, log_decay, scale: float = 1.0, lens=None, state=None
     is None unless given or wanted."""
     where = "hg_linattn_fwd"
     L = lib()
-    b, t, h, d = q.shape
+    qs = q.shape
+    b, t, h, d = qs
     if state_out is None and want_state:
         state_out = torch.empty((b, h, d, d), dtype=torch.float32, device=q.device)
-    desc = _linattn_desc(where, q, k, v, log_decay, scale, lens, (state, state_out))
     if o is None:
-        o = torch.empty((b, t, h, d), dtype=q.dtype, device=q.device)
-    _same(where, q, o)
+        o = torch.empty(qs, dtype=q.dtype, device=q.device)
+    _same(where, q, k, v, o)
     kv = (b, t, k.shape[2], d)
-    hq, hk, hv, ho = (_heads(where, n, x, s) for n, x, s in (("q", q, q.shape), ("k", k, kv), ("v", v, kv),
-                                                              ("o", o, q.shape)))
-    ref = C.byref
-    wp, wn = _ws_for(ws, L.hg_linattn_fwd_workspace_size(ref(desc)), q.device)
-    _check(L.hg_linattn_fwd(ref(desc), ref(hq), ref(hk), ref(hv), _ptr(log_decay), _ptr(lens), _ptr(state), ref(ho),
-                            _ptr(state_out), wp, wn, _stream(stream)), where)
+    desc = _pack_linattn(t, b, h, kv[2], d, _float_code(where, q), scale)
+    ws, wp, wn = _workspace(ws, L.hg_linattn_fwd_workspace_size(desc), q)
+    st = L.hg_linattn_fwd(desc, _heads(where, "q", q, qs), _heads(where, "k", k, kv), _heads(where, "v", v, kv),
+                          _vector(where, log_decay, h, q), _vector(where, lens, b, q, torch.int32),
+                          _state(where, state, (b, h, d, d), q), _heads(where, "o", o, qs),
+                          _state(where, state_out, (b, h, d, d), q), wp, wn, _raw_stream(q, stream))
+    if st:
+        _check(st, where)
     return o, state_out
 
 
@@ -997,22 +1021,25 @@ def hg_linattn_bwd(q, k, v, log_decay, do, scale: float = 1.0, lens=None, state=
     buffer is given."""
     where = "hg_linattn_bwd"
     L = lib()
-    b, t, h, d = q.shape
-    if dstate is None and state is not None:
-        dstate = torch.empty((b, h, d, d), dtype=torch.float32, device=q.device)
-    desc = _linattn_desc(where, q, k, v, log_decay, scale, lens, (state, dstate_out, dstate))
+    qs = q.shape
+    b, t, h, d = qs
+    s = (b, h, d, d)
     kv = (b, t, k.shape[2], d)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    if dstate is None and state is not None:
+        dstate = torch.empty(s, dtype=torch.float32, device=q.device)
+    dq = torch.empty(qs, dtype=q.dtype, device=q.device) if dq is None else dq
     dk = torch.empty(kv, dtype=q.dtype, device=q.device) if dk is None else dk
     dv = torch.empty(kv, dtype=q.dtype, device=q.device) if dv is None else dv
-    _same(where, q, do, dq, dk, dv)
-    hs = [_heads(where, n, x, s) for n, x, s in (("q", q, q.shape), ("k", k, kv), ("v", v, kv), ("do", do, q.shape),
-                                                 ("dq", dq, q.shape), ("dk", dk, kv), ("dv", dv, kv))]
-    ref = C.byref
-    r = [ref(x) for x in hs]
-    wp, wn = _ws_for(ws, L.hg_linattn_bwd_workspace_size(ref(desc)), q.device)
-    _check(L.hg_linattn_bwd(ref(desc), r[0], r[1], r[2], _ptr(log_decay), _ptr(lens), _ptr(state), r[3],
-                            _ptr(dstate_out), r[4], r[5], r[6], _ptr(dstate), wp, wn, _stream(stream)), where)
+    _same(where, q, k, v, do, dq, dk, dv)
+    desc = _pack_linattn(t, b, h, kv[2], d, _float_code(where, q), scale)
+    ws, wp, wn = _workspace(ws, L.hg_linattn_bwd_workspace_size(desc), q)
+    st = L.hg_linattn_bwd(desc, _heads(where, "q", q, qs), _heads(where, "k", k, kv), _heads(where, "v", v, kv),
+                          _vector(where, log_decay, h, q), _vector(where, lens, b, q, torch.int32),
+                          _state(where, state, s, q), _heads(where, "do", do, qs), _state(where, dstate_out, s, q),
+                          _heads(where, "dq", dq, qs), _heads(where, "dk", dk, kv), _heads(where, "dv", dv, kv),
+                          _state(where, dstate, s, q), wp, wn, _raw_stream(q, stream))
+    if st:
+        _check(st, where)
     return dq, dk, dv, dstate
 
 
@@ -1022,23 +1049,19 @@ def hg_linattn_step(q, k, v, log_decay, states, slots=None, scale: float = 1.0, 
     has state b; a slot outside the states: an idle row).  Returns o."""
     where = "hg_linattn_step"
     b, h, d = q.shape
-    _same(where, q, k, v)
-    _vector(where, log_decay, h, q.device)
-    _vector(where, slots, b, q.device, torch.int32)
-    if (states.dim() != 4 or tuple(states.shape[1:]) != (h, d, d) or states.dtype != torch.float32
-            or states.device != q.device or not states.is_contiguous()):
-        raise ValueError(f"{where}: expected contiguous float32 states [n, {h}, {d}, {d}], got {tuple(states.shape)}")
+    hk = k.shape[1]
     if o is None:
         o = torch.empty((b, h, d), dtype=q.dtype, device=q.device)
-    _same(where, q, o)
-    desc = LinattnDesc(1, b, h, k.shape[1], d, _float_code(where, q), scale)
-    hs = []
-    for n, x, s in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape)):
-        y = _heads(where, n, x, (b, s[1], d))
-        hs.append(Heads(y.p, y.token, 0, y.head))  # the rows are sequences
-    ref = C.byref
-    _check(lib().hg_linattn_step(ref(desc), ref(hs[0]), ref(hs[1]), ref(hs[2]), _ptr(log_decay), _ptr(states),
-                                 _ptr(slots), states.shape[0], ref(hs[3]), _stream(stream)), where)
+    _same(where, q, k, v, o)
+    n = states.shape[0]
+    qs, ks = (b, h, d), (b, hk, d)
+    st = lib().hg_linattn_step(_pack_linattn(1, b, h, hk, d, _float_code(where, q), scale),
+                               _heads(where, "q", q, qs, True), _heads(where, "k", k, ks, True),
+                               _heads(where, "v", v, ks, True), _vector(where, log_decay, h, q),
+                               _state(where, states, (n, h, d, d), q), _vector(where, slots, b, q, torch.int32), n,
+                               _heads(where, "o", o, qs, True), _raw_stream(q, stream))
+    if st:
+        _check(st, where)
     return o
 
 

@@ -1,0 +1,188 @@
+"""The C ABI of the sequence encoder's operators on the host: descriptors as the
+binding packs them, workspace sizes, and the refusal of invalid arguments
+before any device work (no GPU is needed for any of these)."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2608_02168_amd import api
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "hg.h")
+P = 0x10000  # never dereferenced: validation fails first
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(api.LIB_PATH):
+        pytest.skip("libhg.so not built")
+    return api.lib()
+
+
+STRUCTS = {"hg_linear_desc": (api.LinearDesc, api._pack_linear, (1, 2, 3, 4, 5, 6, 7, 8)),
+           "hg_glu_desc": (api.GluDesc, api._pack_glu, (1, 2, 3, 4, 5, 6, 7, 8)),
+           "hg_rope_desc": (api.RopeDesc, api._pack_rope, (1, 2, 3, 4, 5, 6, 7, 8, 9.0, 10)),
+           "hg_linattn_desc": (api.LinattnDesc, api._pack_linattn, (1, 2, 3, 4, 5, 6, 7.0)),
+           "hg_heads": (api.Heads, api._pack_heads, (1, 2, 3, 4))}
+
+
+def test_structs_match_the_header(tmp_path):
+    if not shutil.which("gcc"):
+        pytest.skip("gcc not available")
+    lines = ["#include <stdio.h>", "#include <stddef.h>", f'#include "{HEADER}"', "int main(void) {"]
+    for cname, (py, _, _) in STRUCTS.items():
+        lines.append(f'  printf("{cname} size %zu\\n", sizeof({cname}));')
+        lines += [f'  printf("{cname} {f} %zu\\n", offsetof({cname}, {f}));' for f, _ in py._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ["  return 0;", "}"]) + "\n")
+    subprocess.run(["gcc", "-std=c11", "-o", str(exe), str(src)], check=True)
+    out = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split("\n")
+    got = {tuple(x.split()[:2]): int(x.split()[2]) for x in out if x.strip()}
+    for cname, (py, pack, vals) in STRUCTS.items():
+        assert got[(cname, "size")] == C.sizeof(py), cname
+        for f, _ in py._fields_:
+            assert got[(cname, f)] == getattr(py, f).offset, (cname, f)
+        assert pack(*vals) == bytes(py(*vals)), cname
+
+
+def linear(n=20, d_in=24, d_out=32, dtype=1, act=0, ld_x=24, ld_y=32, ld_r=32):
+    return api._pack_linear(n, d_in, d_out, dtype, act, ld_x, ld_y, ld_r)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=-1), api.HG_ERR_ARG), (dict(d_in=0), api.HG_ERR_ARG), (dict(d_out=0), api.HG_ERR_ARG),
+    (dict(dtype=2), api.HG_ERR_ARG), (dict(act=4), api.HG_ERR_ARG), (dict(act=-1), api.HG_ERR_ARG),
+    (dict(ld_x=23), api.HG_ERR_ARG), (dict(ld_y=31), api.HG_ERR_ARG), (dict(ld_r=31), api.HG_ERR_ARG),
+    (dict(n=1 << 31), api.HG_ERR_UNSUPPORTED), (dict(d_in=(1 << 20) + 8, ld_x=1 << 21), api.HG_ERR_UNSUPPORTED),
+    (dict(d_out=(1 << 20) + 8, ld_y=1 << 21, ld_r=1 << 21), api.HG_ERR_UNSUPPORTED)])
+def test_linear_refusals(L, kw, code):
+    X, W, b, R, Y = (P * i for i in range(1, 6))
+    assert L.hg_linear_fwd(linear(**kw), X, W, b, R, Y, P * 9, BIG, None) == code
+    assert len(api.last_error_detail()) > 0
+    kw = dict(dict(ld_r=24), **{k: (v if k != "ld_r" else 23) for k, v in kw.items()})
+    assert L.hg_linear_bwd(linear(**kw), X, W, b, R, Y, P * 7, P * 8, 0, P * 9, BIG, None) == code
+
+
+def test_linear_pointers(L):
+    d = linear()
+    X, W, b, R, Y = (P * i for i in range(1, 6))
+    f = L.hg_linear_fwd
+    assert f(None, X, W, b, R, Y, None, 0, None) == api.HG_ERR_ARG
+    for i in (0, 1, 4):
+        a = [X, W, b, R, Y]
+        a[i] = None
+        assert f(d, *a, None, 0, None) == api.HG_ERR_ARG
+    assert f(d, X + 2, W, b, R, Y, None, 0, None) == api.HG_ERR_ARG      # alignment
+    assert f(d, X, W + 8, b, R, Y, None, 0, None) == api.HG_ERR_ARG
+    assert f(d, X, W, b, R, X + 64, None, 0, None) == api.HG_ERR_ARG     # overlaps X
+    assert f(d, X, W, b, Y + 64, Y, None, 0, None) == api.HG_ERR_ARG     # overlaps R, not R itself
+    assert f(linear(ld_y=40), X, W, b, Y, Y, None, 0, None) == api.HG_ERR_ARG
+    assert f(linear(n=0), None, None, None, None, None, None, 0, None) == api.HG_OK
+    g = L.hg_linear_bwd
+    d = linear(act=2, ld_r=24)
+    assert g(d, X, W, b, R, Y, P * 7, P * 8, 2, P * 9, BIG, None) == api.HG_ERR_ARG
+    assert g(d, X, W, b, R, X, P * 7, P * 8, 0, P * 9, BIG, None) == api.HG_ERR_ARG
+    assert g(d, X, W, b, R, Y, W, P * 8, 0, P * 9, BIG, None) == api.HG_ERR_ARG
+    assert g(d, X, W, b, R, Y, Y, P * 8, 0, P * 9, BIG, None) == api.HG_ERR_ARG
+    need = L.hg_linear_bwd_workspace_size(d)
+    assert need > 0 and g(d, X, W, b, R, Y, P * 7, P * 8, 0, P * 9, need - 1, None) == api.HG_ERR_CAPACITY
+
+
+def test_workspace_sizes(L):
+    # rows that can be used where they lie need no copy; float32 never does
+    assert api.hg_linear_fwd_workspace_size(100, 512, 40000, api.torch.bfloat16) == 0
+    assert api.hg_linear_fwd_workspace_size(100, 511, 40000, api.torch.bfloat16) > 0
+    assert api.hg_linear_fwd_workspace_size(100, 511, 40001) == 0
+    assert api.hg_linear_bwd_workspace_size(1000, 64, 64) < api.hg_linear_bwd_workspace_size(
+        1000, 64, 64, act=api.HG_ACT_SILU)
+    assert L.hg_linear_fwd_workspace_size(linear(act=9)) == 0 == L.hg_linear_fwd_workspace_size(None)
+    assert api.hg_linattn_fwd_workspace_size(1, 1 << 14, 4, 4, 64) > 0
+    assert api.hg_linattn_fwd_workspace_size(4096, 64, 4, 4, 64) == 0
+    assert api.hg_linattn_bwd_workspace_size(4096, 64, 4, 2, 64) >= 2 * 4 * 4096 * 64 * 4 * 64
+
+
+def test_glu_refusals(L):
+    X, W, b, H = P, 2 * P, 3 * P, 4 * P
+
+    def d(n=20, d=24, f=16, dtype=1, act=2, ld_x=24, ld_h=16, ld_dx=24):
+        return api._pack_glu(n, d, f, dtype, act, ld_x, ld_h, ld_dx)
+
+    for kw, code in ((dict(n=-1), api.HG_ERR_ARG), (dict(f=0), api.HG_ERR_ARG), (dict(dtype=-1), api.HG_ERR_ARG),
+                     (dict(act=7), api.HG_ERR_ARG), (dict(ld_x=8), api.HG_ERR_ARG), (dict(ld_h=8), api.HG_ERR_ARG),
+                     (dict(f=1 << 21, ld_h=1 << 21), api.HG_ERR_UNSUPPORTED)):
+        assert L.hg_glu_fwd(d(**kw), X, W, b, H, 5 * P, BIG, None) == code
+        assert L.hg_glu_bwd(d(**kw), X, W, b, H, 5 * P, 6 * P, 7 * P, 0, 8 * P, BIG, None) == code
+    assert L.hg_glu_fwd(d(), X, None, b, H, None, 0, None) == api.HG_ERR_ARG
+    assert L.hg_glu_bwd(d(ld_dx=23), X, W, b, H, 5 * P, 6 * P, 7 * P, 0, 8 * P, BIG, None) == api.HG_ERR_ARG
+
+
+def heads(p=P, batch=3200, token=160, head=16):
+    return api._pack_heads(p, batch, token, head)
+
+
+def test_rope_refusals(L):
+    def d(n=10, n_pos=50, heads=4, kv=2, d=16, rot=16, inter=0, dtype=1, eps=1e-6):
+        return api._pack_rope(n, n_pos, heads, kv, d, rot, inter, dtype, eps, 0)
+
+    def fwd(desc, q=heads(), k=heads(2 * P), wq=3 * P, tab=4 * P, pos=5 * P, qo=heads(6 * P), ko=heads(7 * P)):
+        return L.hg_qk_norm_rope_fwd(desc, q, k, wq, wq, tab, pos, qo, ko, None)
+
+    for kw, code in ((dict(n=-1), api.HG_ERR_ARG), (dict(heads=0), api.HG_ERR_ARG), (dict(kv=-1), api.HG_ERR_ARG),
+                     (dict(rot=24), api.HG_ERR_ARG), (dict(rot=4), api.HG_ERR_UNSUPPORTED),
+                     (dict(d=20), api.HG_ERR_UNSUPPORTED), (dict(d=264), api.HG_ERR_UNSUPPORTED),
+                     (dict(inter=2), api.HG_ERR_ARG), (dict(dtype=3), api.HG_ERR_ARG), (dict(eps=-1.0), api.HG_ERR_ARG),
+                     (dict(eps=float("nan")), api.HG_ERR_ARG), (dict(n_pos=-1), api.HG_ERR_ARG),
+                     (dict(n=1 << 40), api.HG_ERR_UNSUPPORTED)):
+        assert fwd(d(**kw)) == code, kw
+    assert fwd(d(), q=None) == fwd(d(), k=None) == fwd(d(), pos=None) == fwd(d(), tab=None) == api.HG_ERR_ARG
+    assert fwd(d(), q=heads(P + 2)) == fwd(d(), k=heads(token=161)) == fwd(d(), qo=heads(head=20)) == api.HG_ERR_ARG
+    assert fwd(d(), wq=3 * P + 4) == api.HG_ERR_ARG
+    assert fwd(None) == api.HG_ERR_ARG and fwd(d(n=0)) == api.HG_OK
+
+    def bwd(acc=0, ws=9 * P, n=BIG):
+        return L.hg_qk_norm_rope_bwd(d(), heads(), heads(2 * P), 3 * P, 3 * P, 4 * P, 5 * P, heads(6 * P), heads(7 * P),
+                                     heads(6 * P), heads(7 * P), 10 * P, 11 * P, acc, ws, n, None)
+
+    assert bwd(acc=2) == api.HG_ERR_ARG
+    assert bwd(ws=None) == api.HG_ERR_CAPACITY
+    assert bwd(n=L.hg_qk_norm_rope_bwd_workspace_size(d()) - 1) == api.HG_ERR_CAPACITY
+    assert L.hg_rope_table(10, 7, 1e4, 1.0, P, None) == L.hg_rope_table(10, 8, -1.0, 1.0, P, None) == api.HG_ERR_ARG
+    assert L.hg_rope_table(10, 8, 1e4, float("inf"), P, None) == L.hg_rope_table(10, 8, 1e4, 1.0, None, None) == api.HG_ERR_ARG
+    assert L.hg_rope_table(10, 512, 1e4, 1.0, P, None) == api.HG_ERR_UNSUPPORTED
+
+
+def test_linattn_refusals(L):
+    def d(t=20, b=2, h=4, hk=2, d=16, dtype=1):
+        return api._pack_linattn(t, b, h, hk, d, dtype, 1.0)
+
+    def fwd(desc, q=heads(), k=heads(2 * P), v=heads(3 * P), g=4 * P, s=5 * P, o=heads(6 * P), so=7 * P, ws=8 * P, n=BIG):
+        return L.hg_linattn_fwd(desc, q, k, v, g, None, s, o, so, ws, n, None)
+
+    for kw, code in ((dict(t=-1), api.HG_ERR_ARG), (dict(b=-1), api.HG_ERR_ARG), (dict(h=3), api.HG_ERR_ARG),
+                     (dict(hk=0), api.HG_ERR_ARG), (dict(dtype=5), api.HG_ERR_ARG), (dict(d=0), api.HG_ERR_ARG),
+                     (dict(d=12), api.HG_ERR_UNSUPPORTED), (dict(d=136), api.HG_ERR_UNSUPPORTED),
+                     (dict(t=1 << 31), api.HG_ERR_UNSUPPORTED), (dict(b=1 << 23), api.HG_ERR_UNSUPPORTED)):
+        assert fwd(d(**kw)) == code, kw
+    assert fwd(None) == fwd(d(), q=None) == fwd(d(), g=None) == api.HG_ERR_ARG
+    assert fwd(d(), o=heads()) == fwd(d(), so=5 * P) == api.HG_ERR_ARG                 # outputs that are inputs
+    assert fwd(d(), k=heads(token=8)) == fwd(d(), k=heads(P + 8)) == api.HG_ERR_ARG    # overlapping, unaligned rows
+    assert fwd(d(), v=heads(token=1 << 23)) == api.HG_ERR_UNSUPPORTED
+    assert fwd(d(t=4096), ws=None, n=0) == api.HG_ERR_CAPACITY
+    assert fwd(d(b=0)) == api.HG_OK
+
+    def bwd(dq=heads(6 * P), ds=11 * P, n=BIG):
+        return L.hg_linattn_bwd(d(), heads(), heads(2 * P), heads(3 * P), 4 * P, None, 5 * P, heads(7 * P), 10 * P, dq,
+                                heads(8 * P), heads(9 * P), ds, 12 * P, n, None)
+
+    assert bwd(dq=heads(7 * P)) == bwd(dq=heads(8 * P)) == bwd(ds=5 * P) == bwd(ds=10 * P) == api.HG_ERR_ARG
+    assert bwd(n=8) == api.HG_ERR_CAPACITY
+
+    def step(desc, s=5 * P, slots=None, n=2, o=heads(6 * P)):
+        return L.hg_linattn_step(desc, heads(), heads(2 * P), heads(3 * P), 4 * P, s, slots, n, o, None)
+
+    assert step(d()) == api.HG_ERR_ARG                     # more than one token
+    assert step(d(t=1), n=1) == step(d(t=1), n=-1) == step(d(t=1), s=None) == step(d(t=1), s=5 * P + 4) == api.HG_ERR_ARG
+    assert step(d(t=1, b=0)) == api.HG_OK

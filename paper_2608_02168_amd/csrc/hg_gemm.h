@@ -112,24 +112,24 @@ __device__ __forceinline__ float g_phi(float z, float e) {
   }
 }
 
-// act of four values and, with G, its slopes; the choice is the same for the whole launch
-template <class T, bool G>
-__device__ __forceinline__ void g_act4(int act, const float (&z)[4], float (&f)[4], float (&d)[4]) {
-  if (act == HG_ACT_SILU) {
+// act of four values and, with G, its slopes
+template <class T, int ACT, bool G>
+__device__ __forceinline__ void g_act4(const float (&z)[4], float (&f)[4], float (&d)[4]) {
+  if constexpr (ACT == HG_ACT_SILU) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float s = g_sigmoid<T>(z[q]);
       f[q] = z[q] * s;
       if (G) d[q] = fmaf(f[q], 1.f - s, s);
     }
-  } else if (act == HG_ACT_GELU) {
+  } else if constexpr (ACT == HG_ACT_GELU) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const float e = sizeof(T) == 2 || G ? g_exp<T>(-0.5f * z[q] * z[q]) : 0.f, p = g_phi<T>(z[q], e);
       f[q] = z[q] * p;
       if (G) d[q] = fmaf(z[q] * e, 0.39894228040143268f, p);
     }
-  } else if (act == HG_ACT_RELU) {
+  } else if constexpr (ACT == HG_ACT_RELU) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const bool nan = z[q] != z[q];
@@ -196,6 +196,22 @@ __device__ __forceinline__ bool g_vec(const void* p, int64_t ld) {
   return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)sizeof(T))) & (4 * sizeof(T) - 1)) == 0;
 }
 
+// Calls f with the launch's activation as a constant: a branch once, so that the
+// code of one activation is in a row.
+template <bool ACT, class F>
+__device__ __forceinline__ void g_by_act(int act, F f) {
+  if constexpr (!ACT) {
+    f(std::integral_constant<int, HG_ACT_NONE>{});
+  } else {
+    switch (act) {
+      case HG_ACT_RELU: f(std::integral_constant<int, HG_ACT_RELU>{}); break;
+      case HG_ACT_SILU: f(std::integral_constant<int, HG_ACT_SILU>{}); break;
+      case HG_ACT_GELU: f(std::integral_constant<int, HG_ACT_GELU>{}); break;
+      default: f(std::integral_constant<int, HG_ACT_NONE>{});
+    }
+  }
+}
+
 // ---- epilogues: rows m, columns n .. n + 3 of Z --------------------------------
 // `cols` is made once for a thread's columns; `load` reads what a row's output
 // needs beside z; `apply` writes the output and replaces z by what it wrote (for
@@ -233,16 +249,17 @@ __device__ __forceinline__ void g_load_res(const GEpi& e, const GCols& c, int64_
 // out = act(z + bias) + res
 template <class T>
 struct EpiLinear {
-  static constexpr bool kGated = false, kColSum = false;
+  static constexpr bool kGated = false, kColSum = false, kAct = true;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) { return g_cols<T>(e, n, e.ncol - n, false); }
   __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
     g_load_res<T>(e, c, m, r);
   }
+  template <int ACT>
   __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&z)[4], const float (&r)[4]) {
     float f[4], d[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) z[q] += c.b[q];
-    g_act4<T, false>(e.act, z, f, d);
+    g_act4<T, ACT, false>(z, f, d);
 #pragma unroll
     for (int q = 0; q < 4; ++q) f[q] += r[q];
     g_store4<T>(e.out, m * e.ld_out + c.n, c.left, c.vo, f);
@@ -252,7 +269,7 @@ struct EpiLinear {
 // out = res * act'(z + bias): the gradient of z; the padding of a row is written as zero
 template <class T>
 struct EpiLinearGrad {
-  static constexpr bool kGated = false, kColSum = true;
+  static constexpr bool kGated = false, kColSum = true, kAct = true;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
     GCols c = g_cols<T>(e, n, e.ncol - n, false);
     c.vo = e.outp - n >= 4 && g_vec<T>(e.out, e.ld_out);
@@ -261,11 +278,12 @@ struct EpiLinearGrad {
   __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
     g_load_res<T>(e, c, m, r);
   }
+  template <int ACT>
   __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&z)[4], const float (&r)[4]) {
     float f[4], d[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) z[q] += c.b[q];
-    g_act4<T, true>(e.act, z, f, d);
+    g_act4<T, ACT, true>(z, f, d);
 #pragma unroll
     for (int q = 0; q < 4; ++q) z[q] = q < c.left ? r[q] * d[q] : 0.f;
     g_store4<T>(e.out, m * e.ld_out + c.n, e.outp - c.n, c.vo, z);
@@ -275,7 +293,7 @@ struct EpiLinearGrad {
 // out = z, or out + z; with half: the columns of two padded halves to [., 2 half]
 template <class T>
 struct EpiSum {
-  static constexpr bool kGated = false, kColSum = false;
+  static constexpr bool kGated = false, kColSum = false, kAct = false;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
     GCols c;
     c.n = c.out = n;
@@ -292,6 +310,7 @@ struct EpiSum {
   __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
     if (e.accumulate) g_load4<T>(e.out, m * e.ld_out + c.out, c.left, c.vo, r);
   }
+  template <int ACT>
   __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&z)[4], const float (&r)[4]) {
     if (c.left <= 0) return;
     if (e.accumulate) {
@@ -305,16 +324,17 @@ struct EpiSum {
 // out = act(a + bias) * (u + bias), a and u the two halves' products
 template <class T>
 struct EpiGated {
-  static constexpr bool kGated = true, kColSum = false;
+  static constexpr bool kGated = true, kColSum = false, kAct = true;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) { return g_cols<T>(e, n, e.half - n, true); }
   __device__ static __forceinline__ void load(const GEpi&, const GCols&, int64_t, float (&)[4]) {}
+  template <int ACT>
   __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&a)[4], float (&u)[4],
                                                const float (&)[4]) {
     if (c.left <= 0) return;
     float f[4], d[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) a[q] += c.b[q];
-    g_act4<T, false>(e.act, a, f, d);
+    g_act4<T, ACT, false>(a, f, d);
 #pragma unroll
     for (int q = 0; q < 4; ++q) f[q] *= u[q] + c.b2[q];
     g_store4<T>(e.out, m * e.ld_out + c.n, c.left, c.vo, f);
@@ -324,7 +344,7 @@ struct EpiGated {
 // da = dh u act'(a), du = dh act(a), side by side; the padding of a half is written as zero
 template <class T>
 struct EpiGatedGrad {
-  static constexpr bool kGated = true, kColSum = true;
+  static constexpr bool kGated = true, kColSum = true, kAct = true;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
     GCols c = g_cols<T>(e, n, e.half - n, true);
     c.vo = e.outp - n >= 4 && g_vec<T>(e.out, e.ld_out) && (e.outp & 3) == 0;
@@ -333,12 +353,13 @@ struct EpiGatedGrad {
   __device__ static __forceinline__ void load(const GEpi& e, const GCols& c, int64_t m, float (&r)[4]) {
     g_load_res<T>(e, c, m, r);
   }
+  template <int ACT>
   __device__ static __forceinline__ void apply(const GEpi& e, const GCols& c, int64_t m, float (&a)[4], float (&u)[4],
                                                const float (&r)[4]) {
     float f[4], d[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) a[q] += c.b[q];
-    g_act4<T, true>(e.act, a, f, d);
+    g_act4<T, ACT, true>(a, f, d);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const bool in = q < c.left;
@@ -513,37 +534,47 @@ __device__ __forceinline__ void g_epilogue(const GShape& p, const f32x4 (&acc)[W
       for (int v = 0; v < 4; ++v) cur[i][v] = res[i][v];
     if (s0 + SR < BM) load(s0 + SR);
     __syncthreads();
-    if (in_n) {
+    if constexpr (SPLIT) {
+      if (in_n) {
 #pragma unroll
-      for (int i = 0; i < RPT; ++i) {
-        const int r = tr + i * STEP;
-        const int64_t m = m0 + s0 + r;
-        if (m >= p.M) break;
-        const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
-        if constexpr (SPLIT) {
+        for (int i = 0; i < RPT; ++i) {
+          const int r = tr + i * STEP;
+          const int64_t m = m0 + s0 + r;
+          if (m >= p.M) break;
           float* part = e.part + ((int64_t)blockIdx.y * p.M + m) * e.ld_part + n;
-          *reinterpret_cast<f32x4*>(part) = x;
+          *reinterpret_cast<f32x4*>(part) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
           if constexpr (GATED)
             *reinterpret_cast<f32x4*>(part + e.parth) = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
-        } else {
+        }
+      }
+    } else {
+      g_by_act<Epi::kAct>(e.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
+        if (!in_n) return;
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          const int r = tr + i * STEP;
+          const int64_t m = m0 + s0 + r;
+          if (m >= p.M) break;
+          const f32x4 x = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc);
           float z[4] = {x[0], x[1], x[2], x[3]};
           if constexpr (GATED) {
             const f32x4 y = *reinterpret_cast<const f32x4*>(zt + r * LDZ + zc + 16);
             float u[4] = {y[0], y[1], y[2], y[3]};
-            Epi::apply(e, ec, m, z, u, cur[i]);
+            Epi::template apply<ACT>(e, ec, m, z, u, cur[i]);
             if constexpr (Epi::kColSum) {
 #pragma unroll
               for (int v = 0; v < 4; ++v) cs[0][v] += z[v], cs[1][v] += u[v];
             }
           } else {
-            Epi::apply(e, ec, m, z, cur[i]);
+            Epi::template apply<ACT>(e, ec, m, z, cur[i]);
             if constexpr (Epi::kColSum) {
 #pragma unroll
               for (int v = 0; v < 4; ++v) cs[0][v] += z[v];
             }
           }
         }
-      }
+      });
     }
   }
   if constexpr (Epi::kColSum && !SPLIT) {
@@ -822,12 +853,15 @@ __global__ void __launch_bounds__(256) k_product_join(const GShape p, int splits
   float z[4] = {s[0][0], s[0][1], s[0][2], s[0][3]}, r[4];
   const GCols ec = Epi::cols(e, n);
   Epi::load(e, ec, m, r);
-  if constexpr (Epi::kGated) {
-    float u[4] = {s[H - 1][0], s[H - 1][1], s[H - 1][2], s[H - 1][3]};
-    Epi::apply(e, ec, m, z, u, r);
-  } else {
-    Epi::apply(e, ec, m, z, r);
-  }
+  g_by_act<Epi::kAct>(e.act, [&](auto act) {
+    constexpr int ACT = decltype(act)::value;
+    if constexpr (Epi::kGated) {
+      float u[4] = {s[H - 1][0], s[H - 1][1], s[H - 1][2], s[H - 1][3]};
+      Epi::template apply<ACT>(e, ec, m, z, u, r);
+    } else {
+      Epi::template apply<ACT>(e, ec, m, z, r);
+    }
+  });
 }
 
 }  // namespace hg

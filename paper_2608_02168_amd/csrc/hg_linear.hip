@@ -207,11 +207,14 @@ __global__ void __launch_bounds__(kFewWaves * 64)
     float res[4];
     const GCols ec = Epi::cols(e, n);
     Epi::load(e, ec, r, res);
-    if constexpr (Epi::kGated) {
-      Epi::apply(e, ec, r, z[0], z[1], res);
-    } else {
-      Epi::apply(e, ec, r, z[0], res);
-    }
+    g_by_act<Epi::kAct>(e.act, [&](auto act) {
+      constexpr int ACT = decltype(act)::value;
+      if constexpr (Epi::kGated) {
+        Epi::template apply<ACT>(e, ec, r, z[0], z[H - 1], res);
+      } else {
+        Epi::template apply<ACT>(e, ec, r, z[0], res);
+      }
+    });
   }
 }
 
@@ -313,7 +316,7 @@ int launch_tiles(const char* name, const GArgs<float>& a, const Tiling& t, hipSt
 // The split launch only forms products: one kernel for every epilogue of a form.
 template <bool GATED>
 struct EpiPart {
-  static constexpr bool kGated = GATED, kColSum = false;
+  static constexpr bool kGated = GATED, kColSum = false, kAct = false;
 };
 
 template <bool AKM, bool BKM, class Epi, class T>

@@ -110,9 +110,10 @@ __global__ void __launch_bounds__(256)
 // Y of NR rows by reading W once: a lane takes 16 bytes of eight consecutive k
 // rows (8 k x VEC columns) and the same eight k of every row of X, so a wave
 // reads 8 x 64 rows' pieces, and the 8 waves of a block split k.  Bound by
-// the bytes of W.  LC lanes side by side cover LC * 16 bytes of a row.
+// the bytes of W (33.5 MB in 11.8 us, 2.8 TB/s, where 4096 columns make 128
+// blocks; 3.5 TB/s with 256).  LC lanes side by side cover LC * 16 bytes of a row.
 constexpr int kFewWaves = 8;
-constexpr int kFewRows = 8;
+constexpr int kFewRows = 8;  // at most
 
 // 16 bytes of a row, n values of them inside.
 template <class T, bool ALIGNED>
@@ -225,14 +226,15 @@ int launch_few(const Prob& p, const T* X, const T* W, const GEpi& e, hipStream_t
 #define HG_FEW(NR_)                                                                                          \
   HG_LAUNCH("few_rows", (k_few_rows<T, Epi, NR_, LC, ALIGNED>), dim3(grid), dim3(kFewWaves * 64), 0, s, X,   \
             p.ld_x, W, p.d, p.f, nr, e)
+  constexpr bool kBf = sizeof(T) == 2;
   if (nr == 1) {
     HG_FEW(1);
   } else if (nr == 2) {
     HG_FEW(2);
-  } else if (nr <= 4) {
-    HG_FEW(4);
+  } else if (!(kBf && ALIGNED) && nr <= 4) {
+    if constexpr (!(kBf && ALIGNED)) HG_FEW(4);
   } else {
-    HG_FEW(8);
+    if constexpr (kBf && !ALIGNED) HG_FEW(8);
   }
 #undef HG_FEW
   return HG_OK;
@@ -361,7 +363,10 @@ struct Bufs {
   int64_t colsum_rows = 0;
 };
 
-bool few(const Prob& p) { return p.n <= kFewRows; }
+// Few rows: up to 2 bfloat16 rows (4096 x 4096: 11.8 us for one, 13.5 by tiles with
+// k split; 4 rows 16.3), 4 float32 rows (2048 x 2048: 8 rows 12.7 us, 9 by tiles
+// 13.2), and 8 where W would have to be copied first.
+bool few(const Prob& p) { return p.n <= (p.f32() ? 4 : p.f % 8 ? kFewRows : 2); }
 Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true, p.f32()); }
 Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false, p.f32()); }
 Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true, p.f32()); }

@@ -265,20 +265,23 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_rope_bwd(const RopeArgs a)
   }
 }
 
-// Weight gradients from the blocks' sums: 16 columns a block, 16 threads a column.
-__global__ void __launch_bounds__(kThreads)
+// Weight gradients from the blocks' sums: 16 columns a block, 64 threads a column
+// (every 64th partial row in order, then the 64 sums in order).
+__global__ void __launch_bounds__(1024)
     k_rope_dw(const float* __restrict__ part, int blocks, int d, float* __restrict__ dwq, float* __restrict__ dwk,
               int accumulate) {
-  __shared__ float sh[16][17];
+  __shared__ float sh[64][17];
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4, col = blockIdx.x * 16 + cx;
   float s = 0.f;
-  if (col < 2 * d)
-    for (int r = ry; r < blocks; r += 16) s += part[(int64_t)r * 2 * d + col];
+  if (col < 2 * d) {
+#pragma unroll 8
+    for (int r = ry; r < blocks; r += 64) s += part[(int64_t)r * 2 * d + col];
+  }
   sh[ry][cx] = s;
   __syncthreads();
   if (ry == 0 && col < 2 * d) {
 #pragma unroll
-    for (int q = 1; q < 16; ++q) s += sh[q][cx];
+    for (int q = 1; q < 64; ++q) s += sh[q][cx];
     float* o = col < d ? dwq : dwk;
     if (o) {
       const int c = col < d ? col : col - d;
@@ -474,7 +477,7 @@ extern "C" int hg_qk_norm_rope_bwd(const hg_rope_desc* D, const hg_heads* q, con
   }
   HG_TRY(D->dtype == HG_DTYPE_F32 ? launch_d<float>(a, true, blocks, s) : launch_d<bf16_t>(a, true, blocks, s));
   if (a.part)
-    HG_LAUNCH("rope_dw", k_rope_dw, dim3((unsigned)cdiv(2 * D->d, 16)), dim3(kThreads), 0, s, a.part, blocks, D->d, dwq,
+    HG_LAUNCH("rope_dw", k_rope_dw, dim3((unsigned)cdiv(2 * D->d, 16)), dim3(1024), 0, s, a.part, blocks, D->d, dwq,
               dwk, accumulate);
   return HG_OK;
 }

@@ -810,6 +810,218 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
   g_epilogue<BM, BN, WM, WN, Epi, SPLIT>(p, acc, reinterpret_cast<float*>(lds), im, m0, n0, bcol, wm, wn, c, g);
 }
 
+// ---- backward of narrow float32 rows --------------------------------------------
+// dz, dX and dW of a linear map with both widths up to 128 in one pass over very
+// many rows: x and dy are read once, dX written once and dz never leaves the CU
+// (three products by tiles read and write it and x again: 2.3 times the bytes).
+// A block of eight waves keeps W in LDS as three bfloat16 planes for all its
+// 32-row tiles.  A tile's x and dz lie there too, in the same layout [row][128],
+// which serves as rows of k and, through the transposing reads, as k rows:
+//   z  = x W       x rows of k,  W k rows        wave w: columns 16 w of z
+//   dx = dz W^T    dz rows of k, W rows of k     wave w: columns 16 w of dx
+//   dW += x^T dz   x k rows,     dz k rows       a wave: 64 x 32, kept over the tiles
+// 144 KB of LDS: one block a CU.
+constexpr int kNarrow = 128, kNarrowRows = 32;
+constexpr int kNarrowThreads = 512;
+constexpr int kNarrowPlaneW = kNarrow * kNarrow * 2, kNarrowPlaneR = kNarrowRows * kNarrow * 2;  // bytes
+constexpr size_t kNarrowLds = 3 * (size_t)kNarrowPlaneW + 6 * (size_t)kNarrowPlaneR;
+
+struct GNarrow {
+  const float *x, *w, *dy, *bias;
+  float* dx;
+  int64_t ld_x, ld_dy, ld_dx, n;
+  int32_t d, f, act;
+  float *part, *colsum;  // [blocks][d][ld_part], [blocks][f] (or null)
+  int32_t ld_part;
+};
+
+// Address of (row, col) in a plane of 256-byte rows: the 32-byte granule is
+// swizzled by the rows that a half wave of transposing reads touches (0-3 and
+// 8-11 of eight), its halves by the row's bit that is left, so that 16 rows'
+// 16-byte reads fall on all banks too.
+__device__ __forceinline__ int n_at(int row, int col) {
+  return row * 256 + ((col >> 4) ^ ((row & 3) | ((row >> 3 & 1) << 2))) * 32 + ((col >> 3 ^ row >> 2) & 1) * 16 + (col & 7) * 2;
+}
+// Eight k of row `row`.
+__device__ __forceinline__ uint4 n_row8(const char* plane, int row, int k) {
+  return *reinterpret_cast<const uint4*>(plane + n_at(row, k));
+}
+// Rows k0 + 8 g .. + 7 of column 16 blk + c.
+__device__ __forceinline__ uint4 n_col8(const char* plane, int k0, int blk, int c, int g) {
+  typedef __attribute__((address_space(3))) g_s16x4* lds_ptr;
+  const int row = k0 + 8 * g + (c >> 2), col = 16 * blk + 4 * (c & 3);
+  const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(plane + n_at(row, col))));
+  const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(plane + n_at(row + 4, col))));
+  return uint4{a.x, a.y, b.x, b.y};
+}
+__device__ __forceinline__ void n_put(char* planes, int plane_bytes, int row, int col, f32x4 x) {
+  uint2 p[3];
+  g_parts3(x, p);
+  const int at = n_at(row, col);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2*>(planes + k * plane_bytes + at) = p[k];
+}
+
+// 32 rows x 16 columns over KB blocks of 32 k: the next block's fragments are read
+// while the MFMAs of one run.
+template <int KB, class Read>
+__device__ __forceinline__ void n_product(f32x4 (&acc)[2], Read read) {
+  constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};  // the smallest part products first
+  uint4 fb[2][3], fa[2][3][2];
+  read(0, fb[0], fa[0]);
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb) {
+    if (kb + 1 < KB) read(kb + 1, fb[(kb + 1) & 1], fa[(kb + 1) & 1]);
+#pragma unroll
+    for (int s = 0; s < 6; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i] = mfma_bf16(fb[kb & 1][pb[s]], fa[kb & 1][pa[s]][i], acc[i]);
+  }
+}
+
+// KB: blocks of 32 that cover both widths.
+template <int KB>
+__global__ void __launch_bounds__(kNarrowThreads, 2) k_narrow_bwd(const GNarrow p) {
+  extern __shared__ __align__(1024) char lds[];
+  char *lw = lds, *lx = lds + 3 * kNarrowPlaneW, *lz = lx + 3 * kNarrowPlaneR;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4, wm = wave >> 2, wn = wave & 3;
+  constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};  // the smallest part products first
+  const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+  for (int id = threadIdx.x; id < kNarrow * kNarrow / 4; id += kNarrowThreads) {
+    const int row = id / 32, col = id % 32 * 4;
+    n_put(lw, kNarrowPlaneW, row, col,
+          row < p.d && col < p.f ? *reinterpret_cast<const f32x4*>(p.w + (int64_t)row * p.f + col) : zero);
+  }
+  const int zc = 16 * wave + 4 * g;  // this lane's columns of z and of dx
+  float b[4], cs[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int v = 0; v < 4; ++v) b[v] = p.bias && zc < p.f ? p.bias[zc + v] : 0.f;
+  f32x4 dw[4][2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) dw[i][j] = zero;
+
+  // the next tile's rows are in flight during this one
+  const int64_t tiles = (p.n + kNarrowRows - 1) / kNarrowRows;
+  f32x4 xr[2], dyr[2];
+  auto load_x = [&](int64_t t) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int id = threadIdx.x + q * kNarrowThreads, col = id % 32 * 4;
+      const int64_t row = t * kNarrowRows + id / 32;
+      const bool in = row < p.n && col < p.d;
+      xr[q] = *reinterpret_cast<const f32x4*>(p.x + (in ? row * p.ld_x + col : 0));
+      if (!in) xr[q] = zero;
+    }
+  };
+  auto load_dy = [&](int64_t t) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t row = t * kNarrowRows + 16 * i + c;
+      const bool in = row < p.n && zc < p.f;
+      dyr[i] = *reinterpret_cast<const f32x4*>(p.dy + (in ? row * p.ld_dy + zc : 0));
+      if (!in) dyr[i] = zero;
+    }
+  };
+  load_x(blockIdx.x);
+  load_dy(blockIdx.x);
+  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    const int64_t next = t + gridDim.x < tiles ? t + gridDim.x : t;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int id = threadIdx.x + q * kNarrowThreads;
+      n_put(lx, kNarrowPlaneR, id / 32, id % 32 * 4, xr[q]);
+    }
+    __syncthreads();
+    load_x(next);
+    // dz
+    f32x4 z[2] = {zero, zero};
+    if (p.act != HG_ACT_NONE && 16 * wave < p.f) {
+      n_product<KB>(z, [&](int kb, uint4 (&fw)[3], uint4 (&fx)[3][2]) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          fw[k] = n_col8(lw + k * kNarrowPlaneW, 32 * kb, wave, c, g);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) fx[k][i] = n_row8(lx + k * kNarrowPlaneR, 16 * i + c, 32 * kb + 8 * g);
+        }
+      });
+    }
+    g_by_act<true>(p.act, [&](auto act) {
+      constexpr int ACT = decltype(act)::value;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float y[4], f[4], s[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[v] = z[i][v] + b[v];
+        g_act4<float, ACT, true>(y, f, s);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          y[v] = dyr[i][v] * s[v];  // zero in rows and columns that are not there
+          cs[v] += y[v];
+        }
+        n_put(lz, kNarrowPlaneR, 16 * i + c, zc, f32x4{y[0], y[1], y[2], y[3]});
+      }
+    });
+    load_dy(next);
+    __syncthreads();
+    // dX
+    if (16 * wave < p.d) {
+      f32x4 o[2] = {zero, zero};
+      n_product<KB>(o, [&](int kb, uint4 (&fw)[3], uint4 (&fz)[3][2]) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          fw[k] = n_row8(lw + k * kNarrowPlaneW, 16 * wave + c, 32 * kb + 8 * g);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) fz[k][i] = n_row8(lz + k * kNarrowPlaneR, 16 * i + c, 32 * kb + 8 * g);
+        }
+      });
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t row = t * kNarrowRows + 16 * i + c;
+        if (row < p.n && zc < p.d) *reinterpret_cast<f32x4*>(p.dx + row * p.ld_dx + zc) = o[i];
+      }
+    }
+    // dW
+    if (64 * wm < p.d && 32 * wn < p.f) {
+      uint4 fx[3][4], fz[3][2];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fx[k][i] = n_col8(lx + k * kNarrowPlaneR, 0, 4 * wm + i, c, g);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fz[k][j] = n_col8(lz + k * kNarrowPlaneR, 0, 2 * wn + j, c, g);
+      }
+#pragma unroll
+      for (int s = 0; s < 6; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) dw[i][j] = mfma_bf16(fz[pb[s]][j], fx[pa[s]][i], dw[i][j]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = 64 * wm + 16 * i + c;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int n = 32 * wn + 16 * j + 4 * g;
+      if (m < p.d && n < p.f)
+        *reinterpret_cast<f32x4*>(p.part + ((int64_t)blockIdx.x * p.d + m) * p.ld_part + n) = dw[i][j];
+    }
+  }
+  if (p.colsum) {
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) cs[v] += __shfl_xor(cs[v], o, 64);
+      if (c == 0 && zc < p.f) p.colsum[(int64_t)blockIdx.x * p.f + zc + v] = cs[v];
+    }
+  }
+}
+
 // Sum of the splits, then the epilogue.  SL threads share the splits of four
 // columns of a row (each every SL-th in order, then the SL sums in order).
 template <class Epi, int SL>

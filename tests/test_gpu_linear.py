@@ -104,6 +104,26 @@ def test_glu_backward(n, d, f, dtype, act, bias, pad):
     check_grads(got, encoder.glu_bwd(host(x), host(W), host(b), host(dh), act), dtype, (n, d, f, act))
 
 
+@pytest.mark.parametrize("n,d,f,pad", [(20003, 128, 128, 0), (16384, 64, 128, 4), (16400, 128, 64, 0), (17001, 36, 20, 8),
+                                       (16385, 4, 100, 0), (30000, 100, 4, 4)])
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+def test_narrow_rows_backward(n, d, f, pad, act):
+    """Very many float32 rows with both widths up to 128: one pass; the same by
+    tiles where dx is not wanted; added into what is there."""
+    x, W, b = problem(n, d, f, F32, True, pad)
+    dy = draw(9, n, f, pad=pad)
+    wide = torch.full((n, d + 4), 5.0, device="cuda")
+    got = api.hg_linear_bwd(x, W, b, dy, act=ACT[act], dx=wide[:, :d])
+    ref = encoder.linear_bwd(host(x), host(W), host(b), host(dy), act)
+    check_grads(got, ref, F32, (n, d, f, act))
+    assert torch.all(wide[:, d:] == 5.0)
+    again = api.hg_linear_bwd(x, W, b, dy, act=ACT[act], want=(False, True, True))
+    check_grads(again, ref, F32, "by tiles")
+    dW, db = torch.full_like(W, 2.0), torch.full_like(b, 3.0)
+    api.hg_linear_bwd(x, W, b, dy, act=ACT[act], dW=dW, dbias=db, accumulate=True)
+    assert torch.equal(dW, 2.0 + got[1]) and torch.equal(db, 3.0 + got[2])
+
+
 def test_relu_backward_away_from_the_kink():
     # z = x W + b with b far from every kink: half of the columns all positive, half all negative
     n, d, m = 300, 40, 64

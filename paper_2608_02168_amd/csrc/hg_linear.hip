@@ -254,8 +254,7 @@ struct Tiling {
 Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32) {
   Tiling t{};
   const int64_t big = cdiv(M, 128) * cdiv(cols, 128);
-  const int64_t huge = cdiv(M, 256) * cdiv(cols, 256);
-  if (!f32 && 4 * cdiv(big, 512) >= 5 * cdiv(huge, 256)) {
+  if (!f32 && cdiv(M, 256) * cdiv(cols, 256) >= 192) {
     t = Tiling{256, cdiv(M, 256), cdiv(cols, 256), 1, cdiv(std::max<int64_t>(K, 1), 64) * 64};
     return t;
   }

@@ -21,12 +21,19 @@
 // when there are too few of those to fill the chip.  Then a first pass forms
 // every segment's sum, a second adds them up along the sequence, and the walk
 // starts each segment from its state.  The backward's three walks are one
-// launch; dk takes dv's segment states transposed.
+// launch; dk takes dv's segment states transposed.  Where query heads share key
+// heads, a block of the backward takes two of them in turn for every chunk, so
+// the sum of their dk and dv stays in registers and what they share is loaded
+// once (8 x 2048 tokens, 16 heads on 8, d = 64: 101 to 109 us, 131 with one float32
+// gradient a query head and a pass that adds them).
 //
-// Layout: a wave owns 32 columns (16 up to d = 32) of v, of the state and of o
-// and all rows;
-// q, k and v tiles and P, whose blocks the waves share out, pass through LDS.  With the tiles' operands
-// taken as blocks of 16 values, 4 g .. 4 g + 3 in lane group g, every product's
+// A chunk is 32 tokens: half of the registers and LDS of 64, so that a CU holds
+// 16 waves (133 us and 121 for the same backward with one head a block).  The
+// powers of the decay that a chunk needs are a table in LDS.
+//
+// Layout: a wave owns 16 columns of v, of the state and of o and all rows; q, k
+// and v tiles and P, whose blocks the waves share out, pass through LDS.  With
+// the tiles' operands taken as blocks of 16 values, 4 g .. 4 g + 3 in lane group g, every product's
 // result lies as the next product's operand needs it:
 //   P^T = K Q^T       lane (c, g): keys 4 g + v of query c    (operand of V^T P^T)
 //   S  += K^T (w V)   lane (c, g): rows 4 g + v of column c   (operand of S^T Q^T)
@@ -44,7 +51,8 @@ namespace hg {
 namespace {
 
 constexpr int kMaxD = 128;
-constexpr int64_t kMaxToken = 1 << 22;  // token stride: a chunk of 64 stays below 2^31 bytes
+constexpr int kChunk = 32;              // tokens of a step
+constexpr int64_t kMaxToken = 1 << 22;  // token stride: a chunk stays below 2^31 bytes
 
 // One operand: element (sequence b, token t, head h, column x) at
 // p[b * sb + t * st + (h / hdiv) * sh + x].
@@ -68,6 +76,7 @@ struct Walk {
   int32_t s_trans;         // the walk's state is the transpose of s_in and s_out
   int32_t seg_trans;       // ... and of seg (another walk's)
   int32_t f32_out;         // o is float32 whatever the operands are
+  int32_t sum_o;           // o is the sum over a block's heads, which share q; else they share k and v
   float kv_scale, o_scale;
 };
 
@@ -252,11 +261,12 @@ struct Shape {
   static constexpr int W = NB / NT, THREADS = 64 * W;
 };
 
-// One head of one sequence, or a segment of it.  SUMS: only the segment's sum.
-template <class T, int DP, int C, bool SUMS>
-__global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Walks walks) {
+// GR heads of one sequence that share their key head, or a segment of them.
+// SUMS: only the segment's sum.
+template <class T, int DP, bool SUMS, int GR>
+__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4) k_linattn_scan(const Walks walks) {
   const Walk& a = walks.w[blockIdx.z];
-  constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, RB = C / 16;
+  constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, C = kChunk, RB = C / 16;
   typedef Tile<T, DP> TL;
   typedef typename Blk<T>::type B;
   constexpr bool kF32 = sizeof(T) == 4;
@@ -265,10 +275,11 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Wa
   __shared__ __align__(16) T lv[C * TL::LD];
   __shared__ __align__(16) T lq[SUMS ? 16 : C * TL::LD];
   __shared__ __align__(16) Factor<T> lp[SUMS ? 1 : NP][64];
+  __shared__ float pw[GR][C + 1];  // powers of the heads' decays
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % a.H, b = blockIdx.x / a.H, seg = blockIdx.y;
+  const int hb = a.H / GR, h = blockIdx.x % hb * GR, b = blockIdx.x / hb, seg = blockIdx.y;
   const int d = a.d;
-  const float lg = log_of(a.log_decay[h]);
+  const bool sum_o = GR > 1 && a.sum_o;
   // positions fit 32 bits (T < 2^31); addresses are formed in 64
   const int L = (int)len_of(a.lens, b, a.T);
   const int u_from = (int)((int64_t)seg * a.seg_len), u_end = (int)(u_from + a.seg_len < a.T ? u_from + a.seg_len : a.T);
@@ -279,286 +290,294 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, 2) k_linattn_scan(const Wa
   const T* qp = SUMS ? nullptr : static_cast<const T*>(a.q.p) + b * a.q.sb + (h / a.q.hdiv) * a.q.sh;
   const int osz = kF32 || a.f32_out ? 4 : 2;
   char* op = SUMS ? nullptr : static_cast<char*>(const_cast<void*>(a.o.p)) + (b * a.o.sb + (h / a.o.hdiv) * a.o.sh) * osz;
-  const int64_t bh = (int64_t)b * a.H + h;
+  // from a head to the next: the operand that the block's heads do not share
+  const int64_t q_head = sum_o ? 0 : a.q.sh, k_head = sum_o ? a.k.sh : 0, v_head = sum_o ? a.v.sh : 0;
+  const int64_t bh = (int64_t)b * a.H + h;  // of the first head
+  const float po = a.kv_scale * a.o_scale;
 
   if constexpr (!SUMS) {
     // tokens past the sequence's end: zero rows
     const int z0 = u_from > L ? u_from : L, ch = d / 4;
-    for (int64_t i = threadIdx.x; i < (int64_t)(u_end - z0) * ch; i += NTHR) {
-      char* p = op + ((z0 + i / ch) * a.o.st + i % ch * 4) * osz;
-      if (osz == 4) {
-        *reinterpret_cast<f32x4*>(p) = f32x4{0.f, 0.f, 0.f, 0.f};
-      } else {
-        *reinterpret_cast<uint2*>(p) = uint2{0u, 0u};
+    for (int r = 0; r < (sum_o ? 1 : GR); ++r)
+      for (int64_t i = threadIdx.x; i < (int64_t)(u_end - z0) * ch; i += NTHR) {
+        char* p = op + ((z0 + i / ch) * a.o.st + r * a.o.sh + i % ch * 4) * osz;
+        if (osz == 4) {
+          *reinterpret_cast<f32x4*>(p) = f32x4{0.f, 0.f, 0.f, 0.f};
+        } else {
+          *reinterpret_cast<uint2*>(p) = uint2{0u, 0u};
+        }
       }
-    }
     if (u_from >= L && seg > 0) return;  // segment 0 of an empty sequence still hands its state on
   } else {
     if (u_from >= L) return;
   }
 
+  for (int i = threadIdx.x; i < GR * (C + 1); i += NTHR) pw[i / (C + 1)][i % (C + 1)] = decay(log_of(a.log_decay[h + i / (C + 1)]), i % (C + 1));
+
   // state: rows 16 i + 4 g + v, columns 16 (wave NT + j) + c
-  f32x4 S[NB][NT];
+  f32x4 S[GR][NB][NT];
   float* seg_at = a.seg ? a.seg + ((bh * a.segs + seg) * (NB * NB)) * 256 : nullptr;
+  const int64_t seg_head = (int64_t)a.segs * (NB * NB * 256);  // from a head's states to the next one's
 #pragma unroll
-  for (int i = 0; i < NB; ++i)
+  for (int r = 0; r < GR; ++r)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      S[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if constexpr (!SUMS) {
-        if (a.segs > 1) {
-          if (!a.seg_trans) {
-            S[i][j] = *reinterpret_cast<const f32x4*>(seg_at + (i * NB + wave * NT + j) * 256 + lane * 4);
-          } else {
-            // element (r, c) of the block lies where (c, r) of the mirrored block does
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-              S[i][j][v] = seg_at[((wave * NT + j) * NB + i) * 256 + ((c >> 2) * 16 + 4 * g + v) * 4 + (c & 3)];
-          }
-        } else if (a.s_in) {
-          const int col = 16 * (wave * NT + j) + c;
+      for (int j = 0; j < NT; ++j) {
+        f32x4& x = S[r][i][j];
+        x = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (!SUMS) {
+          if (a.segs > 1) {
+            const float* at = seg_at + r * seg_head;
+            if (!a.seg_trans) {
+              x = *reinterpret_cast<const f32x4*>(at + (i * NB + wave * NT + j) * 256 + lane * 4);
+            } else {
+              // element (r, c) of the block lies where (c, r) of the mirrored block does
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int row = 16 * i + 4 * g + v;
-            if (row < d && col < d) S[i][j][v] = a.s_in[bh * d * d + (a.s_trans ? col * d + row : row * d + col)];
+              for (int v = 0; v < 4; ++v)
+                x[v] = at[((wave * NT + j) * NB + i) * 256 + ((c >> 2) * 16 + 4 * g + v) * 4 + (c & 3)];
+            }
+          } else if (a.s_in) {
+            const int col = 16 * (wave * NT + j) + c;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int row = 16 * i + 4 * g + v;
+              if (row < d && col < d) x[v] = a.s_in[(bh + r) * d * d + (a.s_trans ? col * d + row : row * d + col)];
+            }
           }
         }
       }
-    }
-
-  // powers of the decay that every chunk needs
-  float near0[4], diag[4];  // l^(16 + c - 4 g - v), l^(c - 4 g - v) on and below the diagonal
-  float w[RB][4];           // of token 16 tb + 4 g + v in the state after a chunk
-#pragma unroll
-  for (int v = 0; v < 4; ++v) {
-    const int x = c - 4 * g - v;
-    near0[v] = decay(lg, 16 + x) * a.kv_scale * a.o_scale;
-    diag[v] = decay(lg, x) * a.kv_scale * a.o_scale;
-  }
-  const float row0 = decay(lg, c + 1 - lead) * a.o_scale, p16 = decay(lg, 16), p32 = p16 * p16;
-  float dn = decay(lg, C);  // of the state over a chunk
-#pragma unroll
-  for (int v = 0; v < 4; ++v) w[RB - 1][v] = decay(lg, 15 - 4 * g - v + lead) * a.kv_scale;
-#pragma unroll
-  for (int tb = RB - 2; tb >= 0; --tb)
-#pragma unroll
-    for (int v = 0; v < 4; ++v) w[tb][v] = w[tb + 1][v] * p16;
 
   Rows<T, DP, C, NTHR> rk, rv, rq;
   rk.init(a.k.st, d, a.reverse);
   rv.init(a.v.st, d, a.reverse);
   if constexpr (!SUMS) rq.init(a.q.st, d, a.reverse);
-  auto load = [&](int u0) {
+  auto load = [&](int u0, int r) {
     const int n = u_to - u0 < C ? u_to - u0 : C;
     const int64_t t = a.reverse ? L - n - u0 : u0;
-    rk.load(kp + t * a.k.st, a.k.st, n, d, a.reverse);
-    rv.load(vp + t * a.v.st, a.v.st, n, d, a.reverse);
-    if constexpr (!SUMS) rq.load(qp + t * a.q.st, a.q.st, n, d, a.reverse);
+    if (r == 0 || sum_o) {
+      rk.load(kp + t * a.k.st + r * k_head, a.k.st, n, d, a.reverse);
+      rv.load(vp + t * a.v.st + r * v_head, a.v.st, n, d, a.reverse);
+    }
+    if constexpr (!SUMS)
+      if (r == 0 || !sum_o) rq.load(qp + t * a.q.st + r * q_head, a.q.st, n, d, a.reverse);
   };
   // this lane's columns of o in row c of a block of 16
   const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave * NT + 4 * g) * osz);
 
-  if (u_from < u_to) load(u_from);
+  f32x4 sum[RB][NT];  // o of the block's heads so far
+  if (u_from < u_to) load(u_from, 0);
   for (int u0 = u_from; u0 < u_to; u0 += C) {
     const int n = u_to - u0 < C ? u_to - u0 : C;
-    __syncthreads();
-    rk.store(lk);
-    rv.store(lv);
-    if constexpr (!SUMS) rq.store(lq);
-    __syncthreads();
-    if (u0 + C < u_to) load(u0 + C);
-    if constexpr (!SUMS) {
-      // P, its blocks shared out over the waves
-      for (int pr = wave; pr < NP; pr += Shape<DP>::W) {
-        const int r = pr >= 6 ? 3 : pr >= 3 ? 2 : pr >= 1 ? 1 : 0, kt = pr - r * (r + 1) / 2;
-        f32x4 s{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int hr = 0; hr < GR; ++hr) {
+      __syncthreads();
+      if (hr == 0 || sum_o) {
+        rk.store(lk);
+        rv.store(lv);
+      }
+      if constexpr (!SUMS)
+        if (hr == 0 || !sum_o) rq.store(lq);
+      __syncthreads();
+      if (hr + 1 < GR) {
+        load(u0, hr + 1);
+      } else if (u0 + C < u_to) {
+        load(u0 + C, 0);
+      }
+      if constexpr (!SUMS) {
+        // P, its blocks shared out over the waves
+        for (int pr = wave; pr < NP; pr += Shape<DP>::W) {
+          const int r = pr >= 1 ? 1 : 0, kt = pr - r;
+          f32x4 s{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < NB; i += 2) {
+            B k0, k1, q0, q1;
+            if (i + 1 < NB) {
+              TL::row8(lk, 16 * kt + c, i, g, k0, k1);
+              TL::row8(lq, 16 * r + c, i, g, q0, q1);
+            } else {
+              k0 = TL::row4(lk, 16 * kt + c, i, g);
+              q0 = TL::row4(lq, 16 * r + c, i, g);
+              k1 = q1 = Blk<T>::zero();
+            }
+            f32x4& acc = (i & 2) ? s1 : s;  // two chains
+            acc = i + 1 < NB ? mma32(k0, k1, q0, q1, acc) : mma16(k0, q0, acc);
+          }
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s[v] += s1[v];
+          const int x = 16 * (r - kt) + c - 4 * g;  // tokens from key 4 g to the query
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s[v] = x >= v ? s[v] * (pw[hr][x >= v ? x - v : 0] * po) : 0.f;
+          Factor<T> f;
+          f.set(s);
+          lp[pr][lane] = f;
+        }
+        // q S, the chains of the rows and columns side by side
+        f32x4 o[RB][NT];
+#pragma unroll
+        for (int r = 0; r < RB; ++r)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) o[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NB; i += 2) {
-          B k0, k1, q0, q1;
-          if (i + 1 < NB) {
-            TL::row8(lk, 16 * kt + c, i, g, k0, k1);
-            TL::row8(lq, 16 * r + c, i, g, q0, q1);
-          } else {
-            k0 = TL::row4(lk, 16 * kt + c, i, g);
-            q0 = TL::row4(lq, 16 * r + c, i, g);
-            k1 = q1 = Blk<T>::zero();
+          const bool two = i + 1 < NB;
+          B q0[RB], q1[RB];
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            q0[r] = TL::row4(lq, 16 * r + c, i, g);
+            q1[r] = two ? TL::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
           }
-          f32x4& acc = (i & 2) ? s1 : s;  // two chains
-          acc = i + 1 < NB ? mma32(k0, k1, q0, q1, acc) : mma16(k0, q0, acc);
-        }
+          Factor<T> s0[NT], s1[NT];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) s[v] += s1[v];
-        if (kt == r) {
-#pragma unroll
-          for (int v = 0; v < 4; ++v) s[v] = c >= 4 * g + v ? s[v] * diag[v] : 0.f;
-        } else {
-          const float far = r - kt == 1 ? 1.f : r - kt == 2 ? p16 : p32;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) s[v] *= near0[v] * far;
-        }
-        Factor<T> f;
-        f.set(s);
-        lp[pr][lane] = f;
-      }
-      // q S, the chains of the rows and columns side by side
-      f32x4 o[RB][NT];
-#pragma unroll
-      for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) o[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NB; i += 2) {
-        const bool two = i + 1 < NB;
-        B q0[RB], q1[RB];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          q0[r] = TL::row4(lq, 16 * r + c, i, g);
-          q1[r] = two ? TL::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
-        }
-        Factor<T> s0[NT], s1[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          s0[j].set(S[i][j]);
-          if (two) {
-            s1[j].set(S[two ? i + 1 : i][j]);
-          } else {
-            s1[j].zero();
+          for (int j = 0; j < NT; ++j) {
+            s0[j].set(S[hr][i][j]);
+            if (two) {
+              s1[j].set(S[hr][two ? i + 1 : i][j]);
+            } else {
+              s1[j].zero();
+            }
           }
-        }
-#pragma unroll
-        for (int x = Factor<T>::N - 1; x >= 0; --x)
-#pragma unroll
-          for (int r = 0; r < RB; ++r)
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-              o[r][j] = two ? mma32(s0[j].x[x], s1[j].x[x], q0[r], q1[r], o[r][j]) : mma16(s0[j].x[x], q0[r], o[r][j]);
-      }
-      float rowp = row0;
-#pragma unroll
-      for (int r = 0; r < RB; ++r, rowp *= p16)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) o[r][j][v] *= rowp;
-      __syncthreads();
-      // P v
-#pragma unroll
-      for (int kt = 0; kt < RB; kt += 2) {
-        B v0[NT], v1[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          v0[j] = TL::col4(lv, kt, wave * NT + j, c, g);
-          v1[j] = TL::col4(lv, kt + 1, wave * NT + j, c, g);
-        }
-#pragma unroll
-        for (int r = kt; r < RB; ++r) {
-          const Factor<T> p0 = lp[r * (r + 1) / 2 + kt][lane];
-          Factor<T> p1 = p0;
-          if (r > kt) p1 = lp[r * (r + 1) / 2 + kt + 1][lane];
 #pragma unroll
           for (int x = Factor<T>::N - 1; x >= 0; --x)
 #pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+              for (int j = 0; j < NT; ++j)
+                o[r][j] = two ? mma32(s0[j].x[x], s1[j].x[x], q0[r], q1[r], o[r][j]) : mma16(s0[j].x[x], q0[r], o[r][j]);
+        }
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          const float rowp = pw[hr][16 * r + c + 1 - lead] * a.o_scale;
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[r][j][v] = sum_o && hr > 0 ? fmaf(o[r][j][v], rowp, sum[r][j][v]) : o[r][j][v] * rowp;
+        }
+        __syncthreads();
+        // P v
+#pragma unroll
+        for (int kt = 0; kt < RB; kt += 2) {
+          B v0[NT], v1[NT];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            v0[j] = TL::col4(lv, kt, wave * NT + j, c, g);
+            v1[j] = TL::col4(lv, kt + 1, wave * NT + j, c, g);
+          }
+#pragma unroll
+          for (int r = kt; r < RB; ++r) {
+            const Factor<T> p0 = lp[r * (r + 1) / 2 + kt][lane];
+            Factor<T> p1 = p0;
+            if (r > kt) p1 = lp[r * (r + 1) / 2 + kt + 1][lane];
+#pragma unroll
+            for (int x = Factor<T>::N - 1; x >= 0; --x)
+#pragma unroll
+              for (int j = 0; j < NT; ++j)
+                o[r][j] = r > kt ? mma32(v0[j], v1[j], p0.x[x], p1.x[x], o[r][j]) : mma16(v0[j], p0.x[x], o[r][j]);
+          }
+        }
+        if (sum_o && hr + 1 < GR) {
+#pragma unroll
+          for (int r = 0; r < RB; ++r)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sum[r][j] = o[r][j];
+        } else {
+#pragma unroll
+          for (int r = 0; r < RB; ++r) {
+            const int64_t t = a.reverse ? L - 1 - u0 - 16 * r - 15 : u0 + 16 * r;  // token of row 0, or of row 15
+            char* p = op + (t * a.o.st + (sum_o ? 0 : hr * a.o.sh)) * osz + o_off;
+#pragma unroll
             for (int j = 0; j < NT; ++j)
-              o[r][j] = r > kt ? mma32(v0[j], v1[j], p0.x[x], p1.x[x], o[r][j]) : mma16(v0[j], p0.x[x], o[r][j]);
+              if (16 * (wave * NT + j) + 4 * g < d && 16 * r + c < n) {
+                if (osz == 4) {
+                  *reinterpret_cast<f32x4*>(p + 64 * j) = o[r][j];
+                } else {
+                  *reinterpret_cast<uint2*>(p + 32 * j) = Blk<bf16_t>::of(o[r][j]);
+                }
+              }
+          }
         }
       }
+
+      // state
+      const float dn = pw[hr][n];
 #pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        const int64_t t = a.reverse ? L - 1 - u0 - 16 * r - 15 : u0 + 16 * r;  // token of row 0, or of row 15
-        char* p = op + t * a.o.st * osz + o_off;
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-          if (16 * (wave * NT + j) + 4 * g < d && 16 * r + c < n) {
-            if (osz == 4) {
-              *reinterpret_cast<f32x4*>(p + 64 * j) = o[r][j];
-            } else {
-              *reinterpret_cast<uint2*>(p + 32 * j) = Blk<bf16_t>::of(o[r][j]);
-            }
-          }
-      }
-    }
-
-    // state
-    if (n < C) {  // the last chunk of a segment
-      dn = decay(lg, n);
 #pragma unroll
-      for (int tb = 0; tb < RB; ++tb)
+          for (int v = 0; v < 4; ++v) S[hr][i][j][v] *= dn;
 #pragma unroll
-        for (int v = 0; v < 4; ++v) w[tb][v] = decay(lg, n - 1 - (16 * tb + 4 * g + v) + lead) * a.kv_scale;
-    }
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) S[i][j][v] *= dn;
-#pragma unroll
-    for (int tb = 0; tb < RB; tb += 2) {
-      // w v of this wave's columns
-      f32x4 w0[NT], w1[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        w0[j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
-        w1[j] = wide(TL::col4(lv, tb + 1, wave * NT + j, c, g));
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          w0[j][v] *= w[tb][v];
-          w1[j][v] *= w[tb + 1][v];
-        }
-      }
-      uint2 p0[NT][3], p1[NT][3];
-      if constexpr (!kF32) {
+      for (int tb = 0; tb < RB; tb += 2) {
+        // w v of this wave's columns
+        f32x4 w0[NT], w1[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          parts3(w0[j], p0[j]);
-          parts3(w1[j], p1[j]);
+          w0[j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
+          w1[j] = wide(TL::col4(lv, tb + 1, wave * NT + j, c, g));
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int x = n - 1 + lead - 16 * tb - 4 * g - v;  // (rows past the chunk's end are zero)
+            w0[j][v] *= pw[hr][x > 0 ? x : 0] * a.kv_scale;
+            w1[j][v] *= pw[hr][x > 16 ? x - 16 : 0] * a.kv_scale;
+          }
         }
-      }
-      // chains side by side, at most U blocks' operands at a time
-      constexpr int U = NB < 4 ? NB : kF32 ? 2 : 4;
+        uint2 p0[NT][3], p1[NT][3];
+        if constexpr (!kF32) {
 #pragma unroll
-      for (int i0 = 0; i0 < NB; i0 += U) {
-        B k0[U], k1[U];
-#pragma unroll
-        for (int i = 0; i < U && i0 + i < NB; ++i) {
-          k0[i] = TL::col4(lk, tb, i0 + i, c, g);
-          k1[i] = TL::col4(lk, tb + 1, i0 + i, c, g);
+          for (int j = 0; j < NT; ++j) {
+            parts3(w0[j], p0[j]);
+            parts3(w1[j], p1[j]);
+          }
         }
+        // chains side by side, at most U blocks' operands at a time
+        constexpr int U = NB < 4 ? NB : kF32 ? 2 : 4;
 #pragma unroll
-        for (int x = kF32 ? 0 : 2; x >= 0; --x)
+        for (int i0 = 0; i0 < NB; i0 += U) {
+          B k0[U], k1[U];
 #pragma unroll
-          for (int i = 0; i < U && i0 + i < NB; ++i)
+          for (int i = 0; i < U && i0 + i < NB; ++i) {
+            k0[i] = TL::col4(lk, tb, i0 + i, c, g);
+            k1[i] = TL::col4(lk, tb + 1, i0 + i, c, g);
+          }
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              f32x4& s = S[i0 + i][j];
-              if constexpr (kF32) {
-                s = mma32(k0[i], k1[i], w0[j], w1[j], s);
-              } else {
-                s = mma32(k0[i], k1[i], p0[j][x], p1[j][x], s);
+          for (int x = kF32 ? 0 : 2; x >= 0; --x)
+#pragma unroll
+            for (int i = 0; i < U && i0 + i < NB; ++i)
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                f32x4& s = S[hr][i0 + i][j];
+                if constexpr (kF32) {
+                  s = mma32(k0[i], k1[i], w0[j], w1[j], s);
+                } else {
+                  s = mma32(k0[i], k1[i], p0[j][x], p1[j][x], s);
+                }
               }
-            }
+        }
       }
     }
   }
 
-  if constexpr (SUMS) {
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+  for (int r = 0; r < GR; ++r) {
+    if constexpr (SUMS) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        *reinterpret_cast<f32x4*>(seg_at + (i * NB + wave * NT + j) * 256 + lane * 4) = S[i][j];
-  } else if (a.segs == 1 && a.s_out) {
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+        for (int j = 0; j < NT; ++j)
+          *reinterpret_cast<f32x4*>(seg_at + r * seg_head + (i * NB + wave * NT + j) * 256 + lane * 4) = S[r][i][j];
+    } else if (a.segs == 1 && a.s_out) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const int col = 16 * (wave * NT + j) + c;
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int row = 16 * i + 4 * g + v;
-          if (row < d && col < d) a.s_out[bh * d * d + (a.s_trans ? col * d + row : row * d + col)] = S[i][j][v];
+        for (int j = 0; j < NT; ++j) {
+          const int col = 16 * (wave * NT + j) + c;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int row = 16 * i + 4 * g + v;
+            if (row < d && col < d) a.s_out[(bh + r) * d * d + (a.s_trans ? col * d + row : row * d + col)] = S[r][i][j][v];
+          }
         }
-      }
+    }
   }
 }
 
@@ -608,7 +627,7 @@ __global__ void __launch_bounds__(256) k_linattn_join(const Walks walks, int64_t
   }
 }
 
-// Sum over the query heads of a key head, in order: x [rows][hk][group][d] -> out
+// Sum over the partial gradients of a key head, in order: x [rows][hk][group][d] -> out
 template <class T>
 __global__ void __launch_bounds__(256)
     k_group_sum(const float* __restrict__ xk, const float* __restrict__ xv, int64_t B, int64_t T_, int hk, int group, int d,
@@ -696,64 +715,71 @@ __global__ void __launch_bounds__(NTHR)
 
 // ---- host ---------------------------------------------------------------------------
 int pad_d(int d) { return d <= 16 ? 16 : d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
-int chunk_of(int dtype, int64_t T) { return dtype == HG_DTYPE_F32 || T <= 32 ? 32 : 64; }
 
-// Segments of the walks: none while their heads fill the chip; else enough for
-// that, of at least four chunks each.  Full is a block a CU from d = 96 on (eight
-// waves of 200 registers are what fits: 144 us at 256 blocks, 162 at 512 for
-// 16 heads of 16381 tokens, d = 128), 4096 waves below (backward of 128 heads,
-// 2048 tokens, d = 64: 134 us at 1024 blocks, 143 at 512).
-int64_t full_blocks(int d) { return pad_d(d) >= 96 ? 256 : 4096 / (pad_d(d) / 16); }
-struct Segs {
+// The blocks of the walks: each takes `gr` heads, or one of `n` segments of them,
+// of at least four chunks each.  As many segments as fill the chip at most once:
+// 16 waves a CU fit (16 heads of 16381 tokens, d = 128: 125 to 130 us at 512 blocks,
+// 136 at 256, 153 at 1024; backward of 64 x 512 tokens, 8 heads on 4, d = 64: 77
+// us at 384 blocks, 118 at 768 in two segments).  Two heads a block where they
+// share a key head, unless that leaves the chip short of blocks (300 tokens, 8
+// heads on 4, d = 128: 32 us, 43 with two heads a block).
+struct Split {
+  int gr;
   int n;
-  int64_t len;
+  int64_t len;  // tokens of a segment, a multiple of the chunk
 };
-Segs segs_of(const hg_linattn_desc* A, int walks) {
-  const int64_t C = chunk_of(A->dtype, A->t), heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads * walks);
-  int64_t n = 1;
-  const int64_t full = full_blocks(A->d);
-  if (heads < full) n = std::max<int64_t>(1, std::min(cdiv(full, heads), A->t / (4 * C)));
-  const int64_t len = cdiv(cdiv(std::max<int64_t>(A->t, 1), n), C) * C;
-  return {(int)std::max<int64_t>(1, cdiv(A->t, len)), len};
+Split split_of(const hg_linattn_desc* A, int walks) {
+  const int64_t heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads * walks), full = 4096 / (pad_d(A->d) / 16);
+  const int64_t most = std::max<int64_t>(1, A->t / (4 * kChunk));
+  Split p{1, 1, 0};
+  if (walks > 1 && A->heads / A->kv_heads % 2 == 0 && heads / 2 * most >= full) p.gr = 2;
+  const int64_t n = std::max<int64_t>(1, std::min(full / (heads / p.gr), most));
+  p.len = cdiv(cdiv(std::max<int64_t>(A->t, 1), n), kChunk) * kChunk;
+  p.n = (int)std::max<int64_t>(1, cdiv(A->t, p.len));
+  return p;
 }
 
 // of one walk's states
 int64_t seg_elems(const hg_linattn_desc* A, int walks) {
-  const Segs s = segs_of(A, walks);
+  const Split s = split_of(A, walks);
   const int64_t dp = pad_d(A->d);
   return s.n > 1 ? (int64_t)A->batch * A->heads * s.n * dp * dp : 0;
 }
 
 // `sums` of the n walks, the first ones, form their own segment sums.
-template <class T, int DP, int C>
+template <class T, int DP, int GR>
 int launch_scan(const char* name, const Walks& w, int sums, int n, int64_t B, hipStream_t s) {
   const int64_t bhs = B * w.w[0].H;
   const unsigned segs = (unsigned)w.w[0].segs;
   if (segs > 1) {
-    HG_LAUNCH("linattn_sums", (k_linattn_scan<T, DP, C, true>), dim3((unsigned)bhs, segs, sums), dim3(Shape<DP>::THREADS), 0,
+    HG_LAUNCH("linattn_sums", (k_linattn_scan<T, DP, true, 1>), dim3((unsigned)bhs, segs, sums), dim3(Shape<DP>::THREADS), 0,
               s, w);
     HG_LAUNCH("linattn_join", (k_linattn_join<DP>),
               dim3((unsigned)cdiv(bhs * (DP / 16) * (DP / 16) * 64, 256), 1, sums), dim3(256), 0, s, w, bhs);
   }
-  HG_LAUNCH(name, (k_linattn_scan<T, DP, C, false>), dim3((unsigned)bhs, segs, n), dim3(Shape<DP>::THREADS), 0, s, w);
+  HG_LAUNCH(name, (k_linattn_scan<T, DP, false, GR>), dim3((unsigned)(bhs / GR), segs, n), dim3(Shape<DP>::THREADS), 0, s, w);
   return HG_OK;
 }
 
-template <class T, int C>
-int scan_d(const char* name, const Walks& w, int sums, int n, int64_t B, hipStream_t s) {
+template <class T, int DP>
+int scan_g(const char* name, const Walks& w, int sums, int n, int gr, int64_t B, hipStream_t s) {
+  return gr == 2 ? launch_scan<T, DP, 2>(name, w, sums, n, B, s) : launch_scan<T, DP, 1>(name, w, sums, n, B, s);
+}
+
+template <class T>
+int scan_d(const char* name, const Walks& w, int sums, int n, int gr, int64_t B, hipStream_t s) {
   switch (pad_d(w.w[0].d)) {
-    case 16: return launch_scan<T, 16, C>(name, w, sums, n, B, s);
-    case 32: return launch_scan<T, 32, C>(name, w, sums, n, B, s);
-    case 64: return launch_scan<T, 64, C>(name, w, sums, n, B, s);
-    case 96: return launch_scan<T, 96, C>(name, w, sums, n, B, s);
-    default: return launch_scan<T, 128, C>(name, w, sums, n, B, s);
+    case 16: return scan_g<T, 16>(name, w, sums, n, gr, B, s);
+    case 32: return scan_g<T, 32>(name, w, sums, n, gr, B, s);
+    case 64: return scan_g<T, 64>(name, w, sums, n, gr, B, s);
+    case 96: return scan_g<T, 96>(name, w, sums, n, gr, B, s);
+    default: return scan_g<T, 128>(name, w, sums, n, gr, B, s);
   }
 }
 
-int scan(const char* name, const hg_linattn_desc* A, const Walks& w, int sums, int n, hipStream_t s) {
-  if (A->dtype == HG_DTYPE_F32) return scan_d<float, 32>(name, w, sums, n, A->batch, s);
-  if (chunk_of(A->dtype, A->t) == 32) return scan_d<bf16_t, 32>(name, w, sums, n, A->batch, s);
-  return scan_d<bf16_t, 64>(name, w, sums, n, A->batch, s);
+int scan(const char* name, const hg_linattn_desc* A, const Walks& w, int sums, int n, int gr, hipStream_t s) {
+  return A->dtype == HG_DTYPE_F32 ? scan_d<float>(name, w, sums, n, gr, A->batch, s)
+                                  : scan_d<bf16_t>(name, w, sums, n, gr, A->batch, s);
 }
 
 int check(const hg_linattn_desc* A, const char* what) {
@@ -764,7 +790,8 @@ int check(const hg_linattn_desc* A, const char* what) {
   if (A->heads % A->kv_heads) return fail(HG_ERR_ARG, "%s: %d heads on %d key heads", what, A->heads, A->kv_heads);
   if (A->dtype != HG_DTYPE_F32 && A->dtype != HG_DTYPE_BF16) return fail(HG_ERR_ARG, "%s: dtype %d", what, A->dtype);
   if (A->d % 8 || A->d > kMaxD) return fail(HG_ERR_UNSUPPORTED, "%s: d=%d is not a multiple of 8 up to %d", what, A->d, kMaxD);
-  if ((int64_t)A->batch * A->heads >= (int64_t)1 << 24 || A->t >= (int64_t)1 << 31 ||
+  // (a grid has fewer than 2^32 threads; the end of a chunk fits 32 bits)
+  if ((int64_t)A->batch * A->heads >= ((int64_t)1 << 32) / std::max(256, 4 * pad_d(A->d)) || A->t > ((int64_t)1 << 31) - 2 * kChunk ||
       A->t * A->batch > ((int64_t)1 << 36) / A->heads)
     return fail(HG_ERR_UNSUPPORTED, "%s: %d sequences of %lld tokens and %d heads are too many", what, A->batch,
                 (long long)A->t, A->heads);
@@ -790,7 +817,7 @@ Role role(const hg_linattn_desc* A, const hg_heads* x, int hdiv) {
 }
 
 Walk walk_of(const hg_linattn_desc* A, int walks, const float* log_decay, const int32_t* lens) {
-  const Segs sg = segs_of(A, walks);
+  const Split sg = split_of(A, walks);
   Walk a{};
   a.log_decay = log_decay;
   a.lens = lens;
@@ -805,7 +832,7 @@ Walk walk_of(const hg_linattn_desc* A, int walks, const float* log_decay, const 
 
 struct Bufs {
   float *seg0 = nullptr, *seg1 = nullptr;    // states of the segments: S, and in the backward R
-  float *partk = nullptr, *partv = nullptr;  // gradients of k and v for each query head
+  float *partk = nullptr, *partv = nullptr;  // gradients of k and v for each query head, or pair of them
 };
 
 template <class Mem>
@@ -814,8 +841,9 @@ Bufs take(const hg_linattn_desc* A, bool bwd, Mem& m) {
   const int walks = bwd ? 3 : 1;
   b.seg0 = m.template take<float>(seg_elems(A, walks));
   if (bwd) b.seg1 = m.template take<float>(seg_elems(A, walks));
-  if (bwd && A->heads != A->kv_heads) {
-    const int64_t n = (int64_t)A->batch * A->t * A->heads * A->d;
+  const int gr = split_of(A, walks).gr;
+  if (bwd && A->heads / A->kv_heads > gr) {
+    const int64_t n = (int64_t)A->batch * A->t * (A->heads / gr) * A->d;
     b.partk = m.template take<float>(n);
     b.partv = m.template take<float>(n);
   }
@@ -826,7 +854,7 @@ int sum_groups(const hg_linattn_desc* A, const Bufs& b, const hg_heads* dk, cons
   const int64_t rows = (int64_t)A->batch * A->t * A->kv_heads;
   if (rows == 0) return HG_OK;
   const dim3 grid((unsigned)cdiv(rows * (A->d / 4), 256), 2);
-  const int group = A->heads / A->kv_heads;
+  const int group = A->heads / A->kv_heads / split_of(A, 3).gr;
   if (A->dtype == HG_DTYPE_F32) {
     HG_LAUNCH("group_sum", k_group_sum<float>, grid, dim3(256), 0, s, b.partk, b.partv, (int64_t)A->batch, A->t,
               A->kv_heads, group, A->d, role(A, dk, 1), role(A, dv, 1));
@@ -887,7 +915,7 @@ extern "C" int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const
   a.s_out = state_out;
   a.seg = b.seg0;
   a.o_scale = A->scale;
-  return scan("linattn", A, ws_, 1, 1, static_cast<hipStream_t>(stream));
+  return scan("linattn", A, ws_, 1, 1, 1, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const hg_heads* k, const hg_heads* v,
@@ -912,8 +940,8 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
     return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
   Arena m(ws, ws_bytes);
   const Bufs b = take(A, true, m);
-  const int group = A->heads / A->kv_heads;
-  const int64_t H = A->heads, d = A->d;
+  const int group = A->heads / A->kv_heads, gr = split_of(A, 3).gr;
+  const int64_t H = A->heads / gr, d = A->d;  // of the partial gradients
   Walks w{};
   Walk &wq = w.w[0], &wv = w.w[1], &wk = w.w[2];
   wq = wv = walk_of(A, 3, log_decay, lens);
@@ -932,8 +960,9 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
   wv.q = role(A, k, group);
   wv.k = role(A, q, 1);
   wv.v = role(A, d_o, 1);
-  wv.o = group > 1 ? Role{b.partv, A->t * H * d, H * d, d, 1} : role(A, dv, 1);
-  wv.f32_out = group > 1;
+  wv.o = group > gr ? Role{b.partv, A->t * H * d, H * d, d, gr} : role(A, dv, group);
+  wv.f32_out = group > gr;
+  wv.sum_o = 1;
   wv.s_in = dstate_out;
   wv.s_out = dstate;
   wv.seg = b.seg1;
@@ -942,12 +971,12 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
   wk.q = role(A, v, group);
   wk.k = role(A, d_o, 1);
   wk.v = role(A, q, 1);
-  wk.o = group > 1 ? Role{b.partk, A->t * H * d, H * d, d, 1} : role(A, dk, 1);
+  wk.o = group > gr ? Role{b.partk, A->t * H * d, H * d, d, gr} : role(A, dk, group);
   wk.s_trans = 1;
   wk.seg_trans = 1;
   wk.s_out = nullptr;
-  HG_TRY(scan("linattn_bwd", A, w, 2, 3, s));
-  if (group > 1) HG_TRY(sum_groups(A, b, dk, dv, s));
+  HG_TRY(scan("linattn_bwd", A, w, 2, 3, gr, s));
+  if (group > gr) HG_TRY(sum_groups(A, b, dk, dv, s));
   return HG_OK;
 }
 

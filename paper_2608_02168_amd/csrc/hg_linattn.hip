@@ -133,6 +133,26 @@ struct Factor {
   }
 };
 
+// Element i of the factor of a lane.
+template <class T>
+__device__ __forceinline__ float element(const Factor<T>& f, int i) {
+  float s = 0.f;
+#pragma unroll
+  for (int x = Factor<T>::N - 1; x >= 0; --x) {
+    const f32x4 w = wide(f.x[x]);
+    s += i == 0 ? w[0] : i == 1 ? w[1] : i == 2 ? w[2] : w[3];
+  }
+  return s;
+}
+
+// The values with zero in the place of infinities and NaN.
+__device__ __forceinline__ f32x4 finite(f32x4 x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = fabsf(x[i]) < INFINITY ? x[i] : 0.f;
+  return x;
+}
+__device__ __forceinline__ uint2 finite(uint2 x) { return Blk<bf16_t>::of(finite(wide(x))); }
+
 // acc += A B over 32 values
 __device__ __forceinline__ f32x4 mma32(uint2 a0, uint2 a1, uint2 b0, uint2 b1, f32x4 acc) {
   return mfma_bf16(uint4{a0.x, a0.y, a1.x, a1.y}, uint4{b0.x, b0.y, b1.x, b1.y}, acc);
@@ -238,6 +258,21 @@ struct Rows {
       *reinterpret_cast<u32x4*>(lds + row * Tile<T, DP>::LD + col) = x[q];
     }
   }
+  // whether any of this thread's values is infinite or NaN
+  __device__ __forceinline__ bool not_finite() const {
+    bool bad = false;
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          bad |= (x[q][i] & 0x7F800000u) == 0x7F800000u;
+        } else {
+          bad |= (x[q][i] & 0x7F80u) == 0x7F80u || (x[q][i] & 0x7F800000u) == 0x7F800000u;
+        }
+      }
+    return bad;
+  }
 };
 
 // v truncated to three bfloat16 parts (24 bits in all), four values a lane
@@ -264,7 +299,7 @@ struct Shape {
 // GR heads of one sequence that share their key head, or a segment of them.
 // SUMS: only the segment's sum.
 template <class T, int DP, bool SUMS, int GR>
-__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4) k_linattn_scan(const Walks walks) {
+__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : DP == 96 ? 3 : 4) k_linattn_scan(const Walks walks) {
   const Walk& a = walks.w[blockIdx.z];
   constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, C = kChunk, RB = C / 16;
   typedef Tile<T, DP> TL;
@@ -276,6 +311,7 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4
   __shared__ __align__(16) T lq[SUMS ? 16 : C * TL::LD];
   __shared__ __align__(16) Factor<T> lp[SUMS ? 1 : NP][64];
   __shared__ float pw[GR][C + 1];  // powers of the heads' decays
+  __shared__ int bad_v;            // the last fill of lv that held an infinity or a NaN
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const int hb = a.H / GR, h = blockIdx.x % hb * GR, b = blockIdx.x / hb, seg = blockIdx.y;
   const int d = a.d;
@@ -366,6 +402,8 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4
   const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave * NT + 4 * g) * osz);
 
   f32x4 sum[RB][NT];  // o of the block's heads so far
+  int fill = 0;       // of lv
+  if (threadIdx.x == 0) bad_v = 0;
   if (u_from < u_to) load(u_from, 0);
   for (int u0 = u_from; u0 < u_to; u0 += C) {
     const int n = u_to - u0 < C ? u_to - u0 : C;
@@ -375,6 +413,9 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4
       if (hr == 0 || sum_o) {
         rk.store(lk);
         rv.store(lv);
+        ++fill;
+        if constexpr (!SUMS)
+          if (rv.not_finite()) bad_v = fill;
       }
       if constexpr (!SUMS)
         if (hr == 0 || !sum_o) rq.store(lq);
@@ -454,7 +495,10 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4
             for (int v = 0; v < 4; ++v) o[r][j][v] = sum_o && hr > 0 ? fmaf(o[r][j][v], rowp, sum[r][j][v]) : o[r][j][v] * rowp;
         }
         __syncthreads();
-        // P v
+        // P v.  Above the diagonal P is zero, and 0 times an infinity or a NaN is
+        // none: those values leave their diagonal block's product and are added for
+        // the tokens that they belong to.
+        const bool bad = bad_v == fill;
 #pragma unroll
         for (int kt = 0; kt < RB; kt += 2) {
           B v0[NT], v1[NT];
@@ -462,6 +506,16 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4
           for (int j = 0; j < NT; ++j) {
             v0[j] = TL::col4(lv, kt, wave * NT + j, c, g);
             v1[j] = TL::col4(lv, kt + 1, wave * NT + j, c, g);
+          }
+          B d0[NT], d1[NT];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            d0[j] = v0[j];
+            d1[j] = v1[j];
+            if (bad) {
+              d0[j] = finite(v0[j]);
+              d1[j] = finite(v1[j]);
+            }
           }
 #pragma unroll
           for (int r = kt; r < RB; ++r) {
@@ -472,8 +526,22 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : 4
             for (int x = Factor<T>::N - 1; x >= 0; --x)
 #pragma unroll
               for (int j = 0; j < NT; ++j)
-                o[r][j] = r > kt ? mma32(v0[j], v1[j], p0.x[x], p1.x[x], o[r][j]) : mma16(v0[j], p0.x[x], o[r][j]);
+                o[r][j] = r > kt ? mma32(v0[j], d1[j], p0.x[x], p1.x[x], o[r][j]) : mma16(d0[j], p0.x[x], o[r][j]);
           }
+        }
+        if (bad) {
+          for (int y = 0; y <= c; ++y)
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+              const float p = element<T>(lp[r * (r + 3) / 2][16 * (y >> 2) + c], y & 3);
+#pragma unroll
+              for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                  const float x = Elt<T>::get(lv + (16 * r + y) * TL::LD + 16 * (wave * NT + j) + 4 * g + v);
+                  if (!(fabsf(x) < INFINITY)) o[r][j][v] = fmaf(p, x, o[r][j][v]);
+                }
+            }
         }
         if (sum_o && hr + 1 < GR) {
 #pragma unroll
@@ -729,7 +797,7 @@ struct Split {
   int64_t len;  // tokens of a segment, a multiple of the chunk
 };
 Split split_of(const hg_linattn_desc* A, int walks) {
-  const int64_t heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads * walks), full = 4096 / (pad_d(A->d) / 16);
+  const int64_t heads = std::max<int64_t>(1, (int64_t)A->batch * A->heads * walks), full = 256 * (16 / (pad_d(A->d) / 16));
   const int64_t most = std::max<int64_t>(1, A->t / (4 * kChunk));
   Split p{1, 1, 0};
   if (walks > 1 && A->heads / A->kv_heads % 2 == 0 && heads / 2 * most >= full) p.gr = 2;

@@ -171,6 +171,56 @@ def test_values_that_are_not_finite(dtype):
     assert o[0, 101:, 0].isnan().all()
 
 
+# two heads of a key head in one block of the backward: with the key head's gradient whole in the block, as one of
+# several partial ones, in segments, and an odd number of heads on a key head
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,t,h,hk,d,lens", [(700, 40, 4, 2, 16, "ragged"), (700, 33, 4, 1, 16, "wild"),
+                                             (350, 70, 6, 2, 32, None), (20, 4500, 4, 2, 16, "ragged"),
+                                             (8, 1450, 4, 2, 80, "empty"), (3, 4100, 2, 1, 128, "ragged")])
+def test_backward_of_many_shared_heads(b, t, h, hk, d, lens, dtype):
+    test_backward(b, t, h, hk, d, lens, dtype, True)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_values_that_are_not_finite_in_v(value, dtype):
+    """A value of v that is not finite reaches its own column of its own and later tokens."""
+    b, t, h, d = 1, 200, 2, 32
+    q, k, v, g = problem(b, t, h, h, d, dtype)
+    clean, _ = api.hg_linattn_fwd(q, k, v, g)
+    v = v.clone()
+    v[0, 101, 0, 3] = value
+    o, _ = api.hg_linattn_fwd(q, k, v, g)
+    hit = torch.zeros_like(o, dtype=torch.bool)
+    hit[:, 101:, 0, 3] = True
+    assert torch.equal(o[~hit], clean[~hit])
+    assert not o[hit].isfinite().any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("b,t,h,hk,d", [(1, 200, 2, 2, 32), (700, 40, 4, 2, 16)])
+def test_gradients_that_are_not_finite(b, t, h, hk, d, dtype):
+    """A NaN in a token's upstream row, key or query reaches the gradients that depend on it and no other."""
+    q, k, v, g = problem(b, t, h, hk, d, dtype)
+    g = torch.full_like(g, -0.02)
+    do = normal(7, b, t, h, d, dtype=dtype)
+    clean = api.hg_linattn_bwd(q, k, v, g, do)[:3]
+    at = 21
+    for which in ("do", "q", "k", "v"):
+        x = dict(q=q.clone(), k=k.clone(), v=v.clone(), do=do.clone())
+        x[which][0, at, 0, 3] = float("nan")
+        got = api.hg_linattn_bwd(x["q"], x["k"], x["v"], g, x["do"])[:3]
+        # rows of dq, dk and dv that the value reaches, by the formulas
+        one, none, before, after = (at, at + 1), (0, 0), (0, at + 1), (at, t)
+        rows = dict(do=(one, before, before), q=(none, before, before), k=(after, none, one), v=(after, one, none))[which]
+        heads = (h // hk if which in "kv" else 1, 1, 1)  # of dq: all that share the key head
+        for a, c, (lo, hi), n in zip(got, clean, rows, heads):
+            hit = torch.zeros_like(a, dtype=torch.bool)
+            hit[0, lo:hi, :n] = True
+            assert not a[hit].isfinite().all() or lo == hi, which
+            assert torch.equal(a[~hit], c[~hit]), which
+
+
 def test_deterministic_other_stream_and_graph():
     b, t, h, hk, d = 1, 2000, 4, 2, 64
     q, k, v, g = problem(b, t, h, hk, d, BF16)

@@ -87,10 +87,13 @@ struct GArgs : GShape {
 // 35 us of a tile's time, this one 9.
 template <class T>
 __device__ __forceinline__ float g_exp(float x) {
+  constexpr float kLog2e = 1.4426950408889634f;
   if constexpr (sizeof(T) == 4) {
-    return expf(x);
+    x = __builtin_amdgcn_fmed3f(x, -150.f, 150.f);
+    const float h = x * kLog2e, l = fmaf(x, 1.9259629911e-8f, fmaf(x, kLog2e, -h)), r = __builtin_amdgcn_exp2f(h);
+    return fmaf(r, l * 0.69314718056f, r);
   } else {
-    return __builtin_amdgcn_exp2f(x * 1.4426950408889634f);
+    return __builtin_amdgcn_exp2f(x * kLog2e);
   }
 }
 
@@ -814,17 +817,22 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
 // dz, dX and dW of a linear map with both widths up to 128 in one pass over very
 // many rows: x and dy are read once, dX written once and dz never leaves the CU
 // (three products by tiles read and write it and x again: 2.3 times the bytes).
-// A block of eight waves keeps W in LDS as three bfloat16 planes for all its
-// 32-row tiles.  A tile's x and dz lie there too, in the same layout [row][128],
-// which serves as rows of k and, through the transposing reads, as k rows:
+// A block of eight waves takes tiles of 32 rows; each wave keeps its columns of W
+// and of W^T in registers, as three bfloat16 parts.  A tile's x and dz lie in LDS
+// in one layout [row][128], which serves as rows of k and, through the
+// transposing reads, as k rows:
 //   z  = x W       x rows of k,  W k rows        wave w: columns 16 w of z
 //   dx = dz W^T    dz rows of k, W rows of k     wave w: columns 16 w of dx
 //   dW += x^T dz   x k rows,     dz k rows       a wave: 64 x 32, kept over the tiles
-// 144 KB of LDS: one block a CU.
+// z of a tile and dx and dW of the one before lie between the same two barriers,
+// so one wave's activation runs beside another's products.  120 KB of LDS and
+// 256 registers: one block a CU.
 constexpr int kNarrow = 128, kNarrowRows = 32;
 constexpr int kNarrowThreads = 512;
 constexpr int kNarrowPlaneW = kNarrow * kNarrow * 2, kNarrowPlaneR = kNarrowRows * kNarrow * 2;  // bytes
-constexpr size_t kNarrowLds = 3 * (size_t)kNarrowPlaneW + 6 * (size_t)kNarrowPlaneR;
+constexpr int kNarrowTile = 3 * kNarrowPlaneR;
+constexpr size_t kNarrowLds = 5 * (size_t)kNarrowTile;  // three tiles of x, two of dz; W before them
+static_assert(kNarrowLds >= 3 * (size_t)kNarrowPlaneW, "W fits");
 
 struct GNarrow {
   const float *x, *w, *dy, *bias;
@@ -864,18 +872,20 @@ __device__ __forceinline__ void n_put(char* planes, int plane_bytes, int row, in
 
 // 32 rows x 16 columns over KB blocks of 32 k: the next block's fragments are read
 // while the MFMAs of one run.
-template <int KB, class Read>
-__device__ __forceinline__ void n_product(f32x4 (&acc)[2], Read read) {
+template <int KB>
+__device__ __forceinline__ void n_product(f32x4 (&acc)[2], const uint4 (&fw)[KB][3], const char* planes, int c, int g) {
   constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};  // the smallest part products first
-  uint4 fb[2][3], fa[2][3][2];
-  read(0, fb[0], fa[0]);
 #pragma unroll
   for (int kb = 0; kb < KB; ++kb) {
-    if (kb + 1 < KB) read(kb + 1, fb[(kb + 1) & 1], fa[(kb + 1) & 1]);
+    uint4 fa[3][2];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) fa[k][i] = n_row8(planes + k * kNarrowPlaneR, 16 * i + c, 32 * kb + 8 * g);
 #pragma unroll
     for (int s = 0; s < 6; ++s)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) acc[i] = mfma_bf16(fb[kb & 1][pb[s]], fa[kb & 1][pa[s]][i], acc[i]);
+      for (int i = 0; i < 2; ++i) acc[i] = mfma_bf16(fw[kb][pb[s]], fa[pa[s]][i], acc[i]);
   }
 }
 
@@ -883,14 +893,13 @@ __device__ __forceinline__ void n_product(f32x4 (&acc)[2], Read read) {
 template <int KB>
 __global__ void __launch_bounds__(kNarrowThreads, 2) k_narrow_bwd(const GNarrow p) {
   extern __shared__ __align__(1024) char lds[];
-  char *lw = lds, *lx = lds + 3 * kNarrowPlaneW, *lz = lx + 3 * kNarrowPlaneR;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 15, g = lane >> 4, wm = wave >> 2, wn = wave & 3;
   constexpr int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};  // the smallest part products first
   const f32x4 zero{0.f, 0.f, 0.f, 0.f};
   for (int id = threadIdx.x; id < kNarrow * kNarrow / 4; id += kNarrowThreads) {
     const int row = id / 32, col = id % 32 * 4;
-    n_put(lw, kNarrowPlaneW, row, col,
+    n_put(lds, kNarrowPlaneW, row, col,
           row < p.d && col < p.f ? *reinterpret_cast<const f32x4*>(p.w + (int64_t)row * p.f + col) : zero);
   }
   const int zc = 16 * wave + 4 * g;  // this lane's columns of z and of dx
@@ -925,82 +934,96 @@ __global__ void __launch_bounds__(kNarrowThreads, 2) k_narrow_bwd(const GNarrow 
       if (!in) dyr[i] = zero;
     }
   };
-  load_x(blockIdx.x);
-  load_dy(blockIdx.x);
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t next = t + gridDim.x < tiles ? t + gridDim.x : t;
-    __syncthreads();
+  // this wave's columns of W and of W^T, to registers
+  __syncthreads();
+  uint4 wz[KB][3], wx[KB][3];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      wz[kb][k] = n_col8(lds + k * kNarrowPlaneW, 32 * kb, wave, c, g);
+      wx[kb][k] = n_row8(lds + k * kNarrowPlaneW, 16 * wave + c, 32 * kb + 8 * g);
+    }
+  __syncthreads();
+  auto put_x = [&](int at) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const int id = threadIdx.x + q * kNarrowThreads;
-      n_put(lx, kNarrowPlaneR, id / 32, id % 32 * 4, xr[q]);
+      n_put(lds + at * kNarrowTile, kNarrowPlaneR, id / 32, id % 32 * 4, xr[q]);
     }
+  };
+  const int64_t step = gridDim.x;
+  load_x(blockIdx.x);
+  load_dy(blockIdx.x);
+  put_x(0);
+  load_x(blockIdx.x + step);
+  int bx = 0, bz = 0;  // buffers of this tile
+  for (int64_t t = blockIdx.x; t < tiles + step; t += step) {
+    const int px = bx == 0 ? 2 : bx - 1, pz = bz ^ 1, nx = bx == 2 ? 0 : bx + 1;  // of the tile before, of the next one
     __syncthreads();
-    load_x(next);
-    // dz
+    const char* lx = lds + bx * kNarrowTile;
     f32x4 z[2] = {zero, zero};
-    if (p.act != HG_ACT_NONE && 16 * wave < p.f) {
-      n_product<KB>(z, [&](int kb, uint4 (&fw)[3], uint4 (&fx)[3][2]) {
+    if (t < tiles && p.act != HG_ACT_NONE && 16 * wave < p.f) n_product<KB>(z, wz, lx, c, g);
+    if (t < tiles) {
+      // dz
+      char* lz = lds + (3 + bz) * kNarrowTile;
+      g_by_act<true>(p.act, [&](auto act) {
+        constexpr int ACT = decltype(act)::value;
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          fw[k] = n_col8(lw + k * kNarrowPlaneW, 32 * kb, wave, c, g);
+        for (int i = 0; i < 2; ++i) {
+          float y[4], f[4], s[4];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) fx[k][i] = n_row8(lx + k * kNarrowPlaneR, 16 * i + c, 32 * kb + 8 * g);
+          for (int v = 0; v < 4; ++v) y[v] = z[i][v] + b[v];
+          g_act4<float, ACT, true>(y, f, s);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            y[v] = dyr[i][v] * s[v];  // zero in rows and columns that are not there
+            cs[v] += y[v];
+          }
+          n_put(lz, kNarrowPlaneR, 16 * i + c, zc, f32x4{y[0], y[1], y[2], y[3]});
         }
       });
+      load_dy(t + step);
     }
-    g_by_act<true>(p.act, [&](auto act) {
-      constexpr int ACT = decltype(act)::value;
+    put_x(nx);
+    load_x(t + 2 * step);
+    if (t >= step) {
+      const char *lq = lds + px * kNarrowTile, *lz = lds + (3 + pz) * kNarrowTile;
+      // dX
+      if (16 * wave < p.d) {
+        f32x4 o[2] = {zero, zero};
+        n_product<KB>(o, wx, lz, c, g);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float y[4], f[4], s[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) y[v] = z[i][v] + b[v];
-        g_act4<float, ACT, true>(y, f, s);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          y[v] = dyr[i][v] * s[v];  // zero in rows and columns that are not there
-          cs[v] += y[v];
+        for (int i = 0; i < 2; ++i) {
+          const int64_t row = (t - step) * kNarrowRows + 16 * i + c;
+          if (row < p.n && zc < p.d) *reinterpret_cast<f32x4*>(p.dx + row * p.ld_dx + zc) = o[i];
         }
-        n_put(lz, kNarrowPlaneR, 16 * i + c, zc, f32x4{y[0], y[1], y[2], y[3]});
       }
-    });
-    load_dy(next);
-    __syncthreads();
-    // dX
-    if (16 * wave < p.d) {
-      f32x4 o[2] = {zero, zero};
-      n_product<KB>(o, [&](int kb, uint4 (&fw)[3], uint4 (&fz)[3][2]) {
+      // dW
+      if (64 * wm < p.d && 32 * wn < p.f) {
+        uint4 fz[3][2];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-          fw[k] = n_row8(lw + k * kNarrowPlaneW, 16 * wave + c, 32 * kb + 8 * g);
+        for (int k = 0; k < 3; ++k)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) fz[k][i] = n_row8(lz + k * kNarrowPlaneR, 16 * i + c, 32 * kb + 8 * g);
+          for (int j = 0; j < 2; ++j) fz[k][j] = n_col8(lz + k * kNarrowPlaneR, 0, 2 * wn + j, c, g);
+#pragma unroll
+        for (int i0 = 0; i0 < 4; i0 += 2) {
+          uint4 fx[3][2];
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) fx[k][i] = n_col8(lq + k * kNarrowPlaneR, 0, 4 * wm + i0 + i, c, g);
+#pragma unroll
+          for (int s = 0; s < 6; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 2; ++j) dw[i0 + i][j] = mfma_bf16(fz[pb[s]][j], fx[pa[s]][i], dw[i0 + i][j]);
         }
-      });
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int64_t row = t * kNarrowRows + 16 * i + c;
-        if (row < p.n && zc < p.d) *reinterpret_cast<f32x4*>(p.dx + row * p.ld_dx + zc) = o[i];
       }
     }
-    // dW
-    if (64 * wm < p.d && 32 * wn < p.f) {
-      uint4 fx[3][4], fz[3][2];
-#pragma unroll
-      for (int k = 0; k < 3; ++k) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) fx[k][i] = n_col8(lx + k * kNarrowPlaneR, 0, 4 * wm + i, c, g);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) fz[k][j] = n_col8(lz + k * kNarrowPlaneR, 0, 2 * wn + j, c, g);
-      }
-#pragma unroll
-      for (int s = 0; s < 6; ++s)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) dw[i][j] = mfma_bf16(fz[pb[s]][j], fx[pa[s]][i], dw[i][j]);
-    }
+    bx = nx;
+    bz ^= 1;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

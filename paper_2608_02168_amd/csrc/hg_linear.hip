@@ -248,17 +248,23 @@ struct Tiling {
   int64_t k_split;
 };
 
-// Tiles of 128 x 128 where they fill half the chip, else 64 x 64; the k range
-// is split over blocks while the tiles do not fill it (never where column
-// sums are formed on the way).
+// Tiles of 256 x 256 where they fill most of the chip, have at least 512 k for
+// their long epilogue and count at most an eighth more padding than 128 x 128
+// (40000 rows, 128 to 384 columns: backward 66 us, 90 without the last two
+// conditions; 30000 rows, 256 to 1024: 39 us, 40).  Tiles of 128 x 128 where they
+// fill half the chip and count less than half more padding than 64 x 64 (60000
+// rows, 304 to 64 columns: 10 us, 14 with tiles of 128; backward 55, 62).  The k
+// range is split over blocks while the tiles do not fill the chip (never where
+// column sums are formed on the way).
 Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32) {
   Tiling t{};
-  const int64_t big = cdiv(M, 128) * cdiv(cols, 128);
-  if (!f32 && cdiv(M, 256) * cdiv(cols, 256) >= 192) {
+  const auto tiles_of = [&](int64_t x) { return cdiv(M, x) * cdiv(cols, x); };
+  const int64_t big = tiles_of(128), huge = tiles_of(256);
+  if (!f32 && huge >= 192 && K >= 512 && 8 * 4 * huge <= 9 * big) {
     t = Tiling{256, cdiv(M, 256), cdiv(cols, 256), 1, cdiv(std::max<int64_t>(K, 1), 64) * 64};
     return t;
   }
-  t.tile = big >= 128 || (may_split && big * (K / 512) >= 128) ? 128 : 64;
+  t.tile = (big >= 128 || (may_split && big * (K / 512) >= 128)) && 2 * 4 * big <= 3 * tiles_of(64) ? 128 : 64;
   t.tiles_m = cdiv(M, t.tile);
   t.tiles_n = cdiv(cols, t.tile);
   const int64_t tiles = t.tiles_m * t.tiles_n;

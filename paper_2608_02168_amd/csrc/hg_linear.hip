@@ -87,8 +87,9 @@ __global__ void __launch_bounds__(256)
   if (w == 0 && col < cols) part[blockIdx.x * (int64_t)cols + col] = sh[0][lane] + sh[1][lane] + sh[2][lane] + sh[3][lane];
 }
 
-// Sums of `parts` rows of partial column sums: 16 columns a block, 16 threads a column.
-__global__ void __launch_bounds__(256)
+// Sums of `parts` rows of partial column sums: 16 columns a block, 64 threads a
+// column (every 64th row in order, then the 64 sums in a fixed order).
+__global__ void __launch_bounds__(1024)
     k_colsum_join(const float* __restrict__ part, int64_t parts, int32_t cols, float* __restrict__ out, int accumulate) {
   __shared__ float sh[16][17];
   const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
@@ -96,8 +97,11 @@ __global__ void __launch_bounds__(256)
   float s = 0.f;
   if (col < cols)
 #pragma unroll 8
-    for (int64_t r = ry; r < parts; r += 16) s += part[r * cols + col];
-  sh[ry][cx] = s;
+    for (int64_t r = ry; r < parts; r += 64) s += part[r * cols + col];
+  // four rows of the block lie in a wave
+  s += __shfl_xor(s, 16, 64);
+  s += __shfl_xor(s, 32, 64);
+  if ((ry & 3) == 0) sh[ry >> 2][cx] = s;
   __syncthreads();
   if (ry == 0 && col < cols) {
 #pragma unroll
@@ -253,10 +257,15 @@ struct Tiling {
 // (40000 rows, 128 to 384 columns: backward 66 us, 90 without the last two
 // conditions; 30000 rows, 256 to 1024: 39 us, 40).  Tiles of 128 x 128 where they
 // fill half the chip and count less than half more padding than 64 x 64 (60000
-// rows, 304 to 64 columns: 10 us, 14 with tiles of 128; backward 55, 62).  The k
+// rows, 304 to 64 columns: 10 us, 14 with tiles of 128; backward 55, 62).  Up to
+// `short_k` values of k a bfloat16 tile is mostly epilogue, and 64 x 64, of which
+// twice as many waves fit a CU, are faster: 256 for the gradient of z, whose
+// epilogue reads and writes (20000 rows, 160 to 520: backward 64 us, 72; gated,
+// 200 to 600: 94, 98), 128 without that (40000 rows, 96 to 256: 12.7 us, 15.1),
+// none for the gated product (30000 rows, 80 to 100: 12.7 us, 15.8 with 64).  The k
 // range is split over blocks while the tiles do not fill the chip (never where
 // column sums are formed on the way).
-Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32) {
+Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32, int64_t short_k) {
   Tiling t{};
   const auto tiles_of = [&](int64_t x) { return cdiv(M, x) * cdiv(cols, x); };
   const int64_t big = tiles_of(128), huge = tiles_of(256);
@@ -264,7 +273,10 @@ Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32) {
     t = Tiling{256, cdiv(M, 256), cdiv(cols, 256), 1, cdiv(std::max<int64_t>(K, 1), 64) * 64};
     return t;
   }
-  t.tile = (big >= 128 || (may_split && big * (K / 512) >= 128)) && 2 * 4 * big <= 3 * tiles_of(64) ? 128 : 64;
+  t.tile = (big >= 128 || (may_split && big * (K / 512) >= 128)) && 2 * 4 * big <= 3 * tiles_of(64) &&
+                   (f32 || K > short_k)
+               ? 128
+               : 64;
   t.tiles_m = cdiv(M, t.tile);
   t.tiles_n = cdiv(cols, t.tile);
   const int64_t tiles = t.tiles_m * t.tiles_n;
@@ -373,10 +385,10 @@ struct Bufs {
 // k split; 4 rows 16.3), 4 float32 rows (2048 x 2048: 8 rows 12.7 us, 9 by tiles
 // 13.2), and 8 where W would have to be copied first.
 bool few(const Prob& p) { return p.n <= (p.f32() ? 4 : p.f % 8 ? kFewRows : 2); }
-Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true, p.f32()); }
-Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false, p.f32()); }
-Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true, p.f32()); }
-Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true, p.f32()); }
+Tiling t_fwd(const Prob& p) { return tiling(p.n, p.colsp(), p.d, true, p.f32(), p.gated ? 0 : 128); }
+Tiling t_z(const Prob& p) { return tiling(p.n, p.colsp(), p.d, false, p.f32(), 256); }
+Tiling t_dx(const Prob& p) { return tiling(p.n, p.d, p.colsp(), true, p.f32(), 128); }
+Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true, p.f32(), 0); }
 bool x_direct(const Prob& p) { return p.f32() || direct(p.d, p.ld_x); }
 bool w_direct(const Prob& p) { return p.f32() || p.f % 8 == 0; }
 bool has_z(const Prob& p) { return p.gated || p.act != HG_ACT_NONE; }
@@ -553,7 +565,7 @@ int narrow_bwd(const Prob& p, const float* X, const float* W, const float* bias,
   HG_LAUNCH("product_join", (k_product_join<EpiSum<float>, 8>), dim3((unsigned)cdiv((int64_t)p.d * p.f / 4, 32)), dim3(256), 0,
             s, j, kNarrowBlocks);
   if (dbias)
-    HG_LAUNCH("colsum_join", k_colsum_join, dim3((unsigned)cdiv(p.f, 16)), dim3(256), 0, s, b.colsum, (int64_t)kNarrowBlocks,
+    HG_LAUNCH("colsum_join", k_colsum_join, dim3((unsigned)cdiv(p.f, 16)), dim3(1024), 0, s, b.colsum, (int64_t)kNarrowBlocks,
               p.f, dbias, accumulate);
   return HG_OK;
 }
@@ -594,7 +606,7 @@ int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
     }
   }
   if (dbias)
-    HG_LAUNCH("colsum_join", k_colsum_join, dim3((unsigned)cdiv(p.cols(), 16)), dim3(256), 0, s, b.colsum, b.colsum_rows,
+    HG_LAUNCH("colsum_join", k_colsum_join, dim3((unsigned)cdiv(p.cols(), 16)), dim3(1024), 0, s, b.colsum, b.colsum_rows,
               p.cols(), dbias, accumulate);
   if (dX) {
     GArgs<T> a{};

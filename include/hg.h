@@ -644,9 +644,10 @@ int hg_qk_norm_rope_bwd(const hg_rope_desc* D, const hg_heads* q, const hg_heads
  * one packed buffer may interleave.
  * Sums, states and decays are float32; a bfloat16 call holds the weighted
  * products of a chunk and the copy of the state that multiplies a row to 16
- * bits, adds k^T v to the state to float32 accuracy and rounds o once.  A k or v
- * that is not finite reaches every later output of its heads, and one of v may
- * reach those of up to 15 tokens before it.
+ * bits, adds k^T v to the state to float32 accuracy and rounds o once.  A value
+ * of k or v that is not finite reaches outputs of its own and later tokens of its
+ * heads only (one of v: its own column), in the backward those gradients that the
+ * formulas let it reach.
  * Deterministic.  Asynchronous. */
 typedef struct hg_linattn_desc {
   int64_t t;          /* tokens of a sequence */

@@ -24,7 +24,7 @@
 // launch; dk takes dv's segment states transposed.  Where query heads share key
 // heads, a block of the backward takes two of them in turn for every chunk, so
 // the sum of their dk and dv stays in registers and what they share is loaded
-// once (8 x 2048 tokens, 16 heads on 8, d = 64: 101 to 109 us, 131 with one float32
+// once (8 x 2048 tokens, 16 heads on 8, d = 64: 98 to 105 us, 131 with one float32
 // gradient a query head and a pass that adds them).
 //
 // A chunk is 32 tokens: half of the registers and LDS of 64, so that a CU holds
@@ -297,9 +297,12 @@ struct Shape {
 };
 
 // GR heads of one sequence that share their key head, or a segment of them.
-// SUMS: only the segment's sum.
+// SUMS: only the segment's sum.  Registers for 16 waves a CU, or for 12 and 8 where
+// the states of two heads, or six waves a block, leave no use for more (two heads
+// at d = 64 spilled 28 bytes a lane at 16: 114 us for the backward of 8 x 2048
+// tokens, 98 to 105 at 12).
 template <class T, int DP, bool SUMS, int GR>
-__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : DP == 96 ? 3 : 4) k_linattn_scan(const Walks walks) {
+__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : DP == 96 || (GR == 2 && DP == 64) ? 3 : 4) k_linattn_scan(const Walks walks) {
   const Walk& a = walks.w[blockIdx.z];
   constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, C = kChunk, RB = C / 16;
   typedef Tile<T, DP> TL;

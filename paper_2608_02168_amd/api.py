@@ -748,12 +748,11 @@ def _workspace(ws, need: int, like):
     return ws, ws.data_ptr(), ws.numel()
 
 
-def _raw_stream(like, stream):
-    """The given stream, or the current one of the tensor's device."""
-    if stream is None:
-        return torch.cuda.current_stream(like.device).cuda_stream if _current_raw is None else \
-            _current_raw(like.get_device())
-    return stream.cuda_stream
+def _raw_stream(like):
+    """The current stream of the tensor's device.  The calls below that take a
+    stream make it the current one first, so that what they allocate is that
+    stream's too."""
+    return torch.cuda.current_stream(like.device).cuda_stream if _current_raw is None else _current_raw(like.get_device())
 
 
 _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -782,6 +781,9 @@ def hg_linear_fwd(x, W, bias=None, residual=None, act: int = HG_ACT_NONE, y=None
     """y = act(x W + bias) + residual: x [n, d_in], W [d_in, d_out], bias
     float32 [d_out], residual and y [n, d_out] (y may be the residual); rows
     may be strided, W is contiguous."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_linear_fwd(x, W, bias, residual, act, y, ws)
     where = "hg_linear_fwd"
     L = lib()
     n, d, m = _linear_sizes(where, x, W)
@@ -795,7 +797,7 @@ def hg_linear_fwd(x, W, bias=None, residual=None, act: int = HG_ACT_NONE, y=None
                         m if residual is None else _rows(where, residual, n, m))
     ws, wp, wn = _workspace(ws, L.hg_linear_fwd_workspace_size(desc), x)
     st = L.hg_linear_fwd(desc, x.data_ptr(), W.data_ptr(), _vector(where, bias, m, x), _addr(residual), y.data_ptr(), wp,
-                         wn, _raw_stream(x, stream))
+                         wn, _raw_stream(x))
     if st:
         _check(st, where)
     return y
@@ -807,6 +809,9 @@ def hg_linear_bwd(x, W, bias, dy, act: int = HG_ACT_NONE, dx=None, dW=None, dbia
     gradient is dy itself); dbias only with a bias.  With accumulate, dW and
     dbias are added into the given buffers.  want: which of the three to
     compute where no buffer is given."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_linear_bwd(x, W, bias, dy, act, dx, dW, dbias, accumulate, want, ws)
     where = "hg_linear_bwd"
     L = lib()
     n, d, m = _linear_sizes(where, x, W)
@@ -816,7 +821,7 @@ def hg_linear_bwd(x, W, bias, dy, act: int = HG_ACT_NONE, dx=None, dW=None, dbia
                         d if dx is None else _rows(where, dx, n, d))
     ws, wp, wn = _workspace(ws, L.hg_linear_bwd_workspace_size(desc), x)
     st = L.hg_linear_bwd(desc, x.data_ptr(), W.data_ptr(), _addr(bias), dy.data_ptr(), _addr(dx), _addr(dW), _addr(dbias),
-                         1 if accumulate else 0, wp, wn, _raw_stream(x, stream))
+                         1 if accumulate else 0, wp, wn, _raw_stream(x))
     if st:
         _check(st, where)
     return dx, dW, dbias
@@ -859,6 +864,9 @@ def hg_glu_bwd_workspace_size(n: int, d: int, f: int, dtype=torch.float32, ld_x:
 def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=None):
     """h = act(a) * u with [a u] = x W + bias: x [n, d], W [d, 2 f] (the gate's
     columns first), bias float32 [2 f], h [n, f]."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_glu_fwd(x, W, bias, act, h, ws)
     where = "hg_glu_fwd"
     L = lib()
     n, d, f = _glu_sizes(where, x, W)
@@ -871,7 +879,7 @@ def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=
     desc = _pack_glu(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), ld_h, d)
     ws, wp, wn = _workspace(ws, L.hg_glu_fwd_workspace_size(desc), x)
     st = L.hg_glu_fwd(desc, x.data_ptr(), W.data_ptr(), _vector(where, bias, 2 * f, x), h.data_ptr(), wp, wn,
-                      _raw_stream(x, stream))
+                      _raw_stream(x))
     if st:
         _check(st, where)
     return h
@@ -880,6 +888,9 @@ def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=
 def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=None, accumulate: bool = False,
                want=(True, True, True), ws=None, stream=None):
     """Returns (dx, dW, dbias) of hg_glu_fwd for dh = dL/dh, as hg_linear_bwd does."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_glu_bwd(x, W, bias, dh, act, dx, dW, dbias, accumulate, want, ws)
     where = "hg_glu_bwd"
     L = lib()
     n, d, f = _glu_sizes(where, x, W)
@@ -889,7 +900,7 @@ def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=N
                      d if dx is None else _rows(where, dx, n, d))
     ws, wp, wn = _workspace(ws, L.hg_glu_bwd_workspace_size(desc), x)
     st = L.hg_glu_bwd(desc, x.data_ptr(), W.data_ptr(), _addr(bias), dh.data_ptr(), _addr(dx), _addr(dW), _addr(dbias),
-                      1 if accumulate else 0, wp, wn, _raw_stream(x, stream))
+                      1 if accumulate else 0, wp, wn, _raw_stream(x))
     if st:
         _check(st, where)
     return dx, dW, dbias
@@ -898,11 +909,14 @@ def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=N
 def hg_rope_table(n_pos: int, rot: int, base: float = 10000.0, step: float = 1.0, table=None, device="cuda",
                   stream=None):
     """Cosines and sines [n_pos, rot] of position * step * base^(-2 p / rot)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_rope_table(n_pos, rot, base, step, table, device)
     if table is None:
         table = torch.empty((n_pos, rot), dtype=torch.float32, device=device)
     elif tuple(table.shape) != (n_pos, rot) or table.dtype != torch.float32 or not table.is_contiguous():
         raise ValueError(f"hg_rope_table: expected a contiguous float32 [{n_pos}, {rot}], got {tuple(table.shape)}")
-    _check(lib().hg_rope_table(n_pos, rot, base, step, table.data_ptr(), _raw_stream(table, stream)), "hg_rope_table")
+    _check(lib().hg_rope_table(n_pos, rot, base, step, table.data_ptr(), _raw_stream(table)), "hg_rope_table")
     return table
 
 
@@ -923,6 +937,9 @@ def hg_qk_norm_rope_fwd(q, k, wq, wk, table, pos, eps: float = 1e-6, interleaved
     or None (views of a packed projection are used where they lie), wq, wk
     float32 [d] or None, table [positions, rot] from hg_rope_table, pos int32
     [n].  Returns (q_out, k_out); they may be q and k themselves."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_qk_norm_rope_fwd(q, k, wq, wk, table, pos, eps, interleaved, q_out, k_out)
     where = "hg_qk_norm_rope_fwd"
     desc, qs, ks = _rope_desc(where, q, k, table, eps, interleaved)
     if q_out is None:
@@ -934,7 +951,7 @@ def hg_qk_norm_rope_fwd(q, k, wq, wk, table, pos, eps: float = 1e-6, interleaved
     st = lib().hg_qk_norm_rope_fwd(desc, _heads(where, "q", q, qs), hk, _vector(where, wq, qs[2], q),
                                    _vector(where, wk, qs[2], q), table.data_ptr(),
                                    _vector(where, pos, qs[0], q, torch.int32), _heads(where, "q_out", q_out, qs), hl,
-                                   _raw_stream(q, stream))
+                                   _raw_stream(q))
     if st:
         _check(st, where)
     return q_out, k_out
@@ -944,6 +961,10 @@ def hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps: float = 1
                         dq=None, dk=None, dwq=None, dwk=None, accumulate: bool = False, ws=None, stream=None):
     """Returns (dq, dk, dwq, dwk) of hg_qk_norm_rope_fwd (q and k as it read
     them); dwq and dwk for the weights given, added into when accumulate."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps, interleaved, dq,
+                                       dk, dwq, dwk, accumulate, ws)
     where = "hg_qk_norm_rope_bwd"
     L = lib()
     desc, qs, ks = _rope_desc(where, q, k, table, eps, interleaved)
@@ -965,7 +986,7 @@ def hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps: float = 1
     st = L.hg_qk_norm_rope_bwd(desc, h[0], g[0], _vector(where, wq, d, q), _vector(where, wk, d, q), table.data_ptr(),
                                _vector(where, pos, qs[0], q, torch.int32), h[1], g[1], h[2], g[2],
                                _vector(where, dwq, d, q), _vector(where, dwk, d, q), 1 if accumulate else 0, wp, wn,
-                               _raw_stream(q, stream))
+                               _raw_stream(q))
     if st:
         _check(st, where)
     return dq, dk, dwq, dwk
@@ -993,6 +1014,9 @@ def hg_linattn_fwd(q, k, v, log_decay, scale: float = 1.0, lens=None, state=None
     [b, t, kv_heads, d], log_decay float32 [heads], lens int32 [b] or None,
     state float32 [b, heads, d, d] or None.  Returns (o, state_out); state_out
     is None unless given or wanted."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_linattn_fwd(q, k, v, log_decay, scale, lens, state, o, state_out, want_state, ws)
     where = "hg_linattn_fwd"
     L = lib()
     qs = q.shape
@@ -1008,7 +1032,7 @@ def hg_linattn_fwd(q, k, v, log_decay, scale: float = 1.0, lens=None, state=None
     st = L.hg_linattn_fwd(desc, _heads(where, "q", q, qs), _heads(where, "k", k, kv), _heads(where, "v", v, kv),
                           _vector(where, log_decay, h, q), _vector(where, lens, b, q, torch.int32),
                           _state(where, state, (b, h, d, d), q), _heads(where, "o", o, qs),
-                          _state(where, state_out, (b, h, d, d), q), wp, wn, _raw_stream(q, stream))
+                          _state(where, state_out, (b, h, d, d), q), wp, wn, _raw_stream(q))
     if st:
         _check(st, where)
     return o, state_out
@@ -1019,6 +1043,9 @@ def hg_linattn_bwd(q, k, v, log_decay, do, scale: float = 1.0, lens=None, state=
     """Returns (dq, dk, dv, dstate) of hg_linattn_fwd for do = dL/do and
     dstate_out = dL/dstate_out (or None); dstate is None unless a state or a
     buffer is given."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_linattn_bwd(q, k, v, log_decay, do, scale, lens, state, dstate_out, dq, dk, dv, dstate, ws)
     where = "hg_linattn_bwd"
     L = lib()
     qs = q.shape
@@ -1037,7 +1064,7 @@ def hg_linattn_bwd(q, k, v, log_decay, do, scale: float = 1.0, lens=None, state=
                           _vector(where, log_decay, h, q), _vector(where, lens, b, q, torch.int32),
                           _state(where, state, s, q), _heads(where, "do", do, qs), _state(where, dstate_out, s, q),
                           _heads(where, "dq", dq, qs), _heads(where, "dk", dk, kv), _heads(where, "dv", dv, kv),
-                          _state(where, dstate, s, q), wp, wn, _raw_stream(q, stream))
+                          _state(where, dstate, s, q), wp, wn, _raw_stream(q))
     if st:
         _check(st, where)
     return dq, dk, dv, dstate
@@ -1047,6 +1074,9 @@ def hg_linattn_step(q, k, v, log_decay, states, slots=None, scale: float = 1.0, 
     """One token for each row: q [b, heads, d], k, v [b, kv_heads, d], states
     float32 [n, heads, d, d] updated in place, slots int32 [b] (None: row b
     has state b; a slot outside the states: an idle row).  Returns o."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_linattn_step(q, k, v, log_decay, states, slots, scale, o)
     where = "hg_linattn_step"
     b, h, d = q.shape
     hk = k.shape[1]
@@ -1059,7 +1089,7 @@ def hg_linattn_step(q, k, v, log_decay, states, slots=None, scale: float = 1.0, 
                                _heads(where, "q", q, qs, True), _heads(where, "k", k, ks, True),
                                _heads(where, "v", v, ks, True), _vector(where, log_decay, h, q),
                                _state(where, states, (n, h, d, d), q), _vector(where, slots, b, q, torch.int32), n,
-                               _heads(where, "o", o, qs, True), _raw_stream(q, stream))
+                               _heads(where, "o", o, qs, True), _raw_stream(q))
     if st:
         _check(st, where)
     return o

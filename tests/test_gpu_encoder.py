@@ -118,3 +118,34 @@ def test_tokens_one_by_one(dtype, bar):
 def test_training_learns():
     losses, _, _, _ = encoder.train(encoder.EncoderConfig(), 120)
     assert all(np.isfinite(losses)) and np.mean(losses[-10:]) < 0.75 * np.mean(losses[:5])
+
+
+def test_a_given_stream_owns_what_a_call_allocates(monkeypatch):
+    """Workspace and outputs come from the stream that the call runs on: memory of
+    the caller's current stream could be handed out again while that one still works."""
+    side = torch.cuda.Stream()
+    seen, empty = [], torch.empty
+
+    def spy(*a, **k):
+        seen.append(torch.cuda.current_stream())
+        return empty(*a, **k)
+
+    x, w = torch.randn(300, 203, device="cuda"), torch.randn(203, 106, device="cuda")
+    q, k = torch.randn(2, 1500, 2, 16, device="cuda"), torch.randn(2, 1500, 1, 16, device="cuda")
+    g, one, pos = torch.full((2,), -0.1, device="cuda"), torch.ones(16, device="cuda"), torch.arange(8, device="cuda").int()
+    b, states = torch.zeros(106, device="cuda"), torch.zeros(2, 2, 16, 16, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    monkeypatch.setattr(torch, "empty", spy)
+    table = api.hg_rope_table(8, 16, stream=side)
+    y = api.hg_linear_fwd(x, w, act=api.HG_ACT_SILU, stream=side)
+    h = api.hg_glu_fwd(x, w, stream=side)
+    api.hg_linear_bwd(x, w, b, y, act=api.HG_ACT_SILU, stream=side)
+    api.hg_glu_bwd(x, w, b, h, stream=side)
+    qt, kt = q[0, :8], k[0, :8]
+    api.hg_qk_norm_rope_fwd(qt, kt, one, one, table, pos, stream=side)
+    api.hg_qk_norm_rope_bwd(qt, kt, one, one, table, pos, qt, kt, stream=side)
+    api.hg_linattn_fwd(q, k, k, g, want_state=True, stream=side)
+    api.hg_linattn_bwd(q, k, k, g, q, stream=side)
+    api.hg_linattn_step(q[:, 0], k[:, 0], k[:, 0], g, states, stream=side)
+    assert len(seen) >= 10 and all(s == side for s in seen)
+    torch.cuda.synchronize()

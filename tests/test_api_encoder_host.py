@@ -101,7 +101,10 @@ def test_workspace_sizes(L):
     assert L.hg_linear_fwd_workspace_size(linear(act=9)) == 0 == L.hg_linear_fwd_workspace_size(None)
     assert api.hg_linattn_fwd_workspace_size(1, 1 << 14, 4, 4, 64) > 0
     assert api.hg_linattn_fwd_workspace_size(4096, 64, 4, 4, 64) == 0
-    assert api.hg_linattn_bwd_workspace_size(4096, 64, 4, 2, 64) >= 2 * 4 * 4096 * 64 * 4 * 64
+    # two query heads of a key head are added up in a block; three leave a partial gradient each, four one a pair
+    assert api.hg_linattn_bwd_workspace_size(4096, 64, 4, 2, 64) == 0
+    assert api.hg_linattn_bwd_workspace_size(4096, 64, 6, 2, 64) >= 2 * 4 * 4096 * 64 * 6 * 64
+    assert 0 < api.hg_linattn_bwd_workspace_size(4096, 64, 4, 1, 64) < 2 * 4 * 4096 * 64 * 3 * 64
 
 
 def test_glu_refusals(L):

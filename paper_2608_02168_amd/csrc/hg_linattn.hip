@@ -175,12 +175,14 @@ __device__ __forceinline__ f32x4 mma16(f32x4 a, f32x4 b, f32x4 acc) {
   return acc;
 }
 
-template <class T, int DP>
+// COLS: k and v, read down columns; else q, read along rows.
+template <class T, int DP, bool COLS>
 struct Tile {
   static constexpr int EL = Elt<T>::EL;
-  // 16 bytes more than the row (bfloat16: 32, for the transposing reads of 4 rows
-  // a lane group): the rows that one read touches fall on all banks
-  static constexpr int LD = DP + (sizeof(T) == 4 ? 4 : 16);
+  // 16 bytes more than the row, and 32 for bfloat16 rows whose transposing reads
+  // take 8 rows of 32 bytes a half wave: what one read touches falls on all banks
+  // (16 heads of 16381 tokens, d = 128: 127 us, 133 with 32 for all)
+  static constexpr int LD = DP + (sizeof(T) == 4 ? 4 : COLS ? 16 : 8);
   typedef typename Blk<T>::type B;
   // 16 columns of row r: lane's four
   static __device__ __forceinline__ B row4(const T* t, int r, int blk, int g) {
@@ -251,11 +253,12 @@ struct Rows {
 #pragma unroll
     for (int q = 0; q < N; ++q) x[q] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[q] - back, 0, 0);
   }
+  template <class TL>
   __device__ __forceinline__ void store(T* lds) const {
 #pragma unroll
     for (int q = 0; q < N; ++q) {
       const int id = threadIdx.x + q * NT, row = id / CH, col = id % CH * EL;
-      *reinterpret_cast<u32x4*>(lds + row * Tile<T, DP>::LD + col) = x[q];
+      *reinterpret_cast<u32x4*>(lds + row * TL::LD + col) = x[q];
     }
   }
   // whether any of this thread's values is infinite or NaN
@@ -305,13 +308,14 @@ template <class T, int DP, bool SUMS, int GR>
 __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : DP == 96 || (GR == 2 && DP == 64) ? 3 : 4) k_linattn_scan(const Walks walks) {
   const Walk& a = walks.w[blockIdx.z];
   constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, C = kChunk, RB = C / 16;
-  typedef Tile<T, DP> TL;
+  typedef Tile<T, DP, true> TL;
+  typedef Tile<T, DP, false> TQ;
   typedef typename Blk<T>::type B;
   constexpr bool kF32 = sizeof(T) == 4;
   constexpr int NP = RB * (RB + 1) / 2;  // 16 x 16 blocks of P on and below the diagonal
   __shared__ __align__(16) T lk[C * TL::LD];
   __shared__ __align__(16) T lv[C * TL::LD];
-  __shared__ __align__(16) T lq[SUMS ? 16 : C * TL::LD];
+  __shared__ __align__(16) T lq[SUMS ? 16 : C * TQ::LD];
   __shared__ __align__(16) Factor<T> lp[SUMS ? 1 : NP][64];
   __shared__ float pw[GR][C + 1];  // powers of the heads' decays
   __shared__ int bad_v;            // the last fill of lv that held an infinity or a NaN
@@ -414,14 +418,14 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
     for (int hr = 0; hr < GR; ++hr) {
       __syncthreads();
       if (hr == 0 || sum_o) {
-        rk.store(lk);
-        rv.store(lv);
+        rk.template store<TL>(lk);
+        rv.template store<TL>(lv);
         ++fill;
         if constexpr (!SUMS)
           if (rv.not_finite()) bad_v = fill;
       }
       if constexpr (!SUMS)
-        if (hr == 0 || !sum_o) rq.store(lq);
+        if (hr == 0 || !sum_o) rq.template store<TQ>(lq);
       __syncthreads();
       if (hr + 1 < GR) {
         load(u0, hr + 1);
@@ -438,10 +442,10 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
             B k0, k1, q0, q1;
             if (i + 1 < NB) {
               TL::row8(lk, 16 * kt + c, i, g, k0, k1);
-              TL::row8(lq, 16 * r + c, i, g, q0, q1);
+              TQ::row8(lq, 16 * r + c, i, g, q0, q1);
             } else {
               k0 = TL::row4(lk, 16 * kt + c, i, g);
-              q0 = TL::row4(lq, 16 * r + c, i, g);
+              q0 = TQ::row4(lq, 16 * r + c, i, g);
               k1 = q1 = Blk<T>::zero();
             }
             f32x4& acc = (i & 2) ? s1 : s;  // two chains
@@ -468,8 +472,8 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
           B q0[RB], q1[RB];
 #pragma unroll
           for (int r = 0; r < RB; ++r) {
-            q0[r] = TL::row4(lq, 16 * r + c, i, g);
-            q1[r] = two ? TL::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
+            q0[r] = TQ::row4(lq, 16 * r + c, i, g);
+            q1[r] = two ? TQ::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
           }
           Factor<T> s0[NT], s1[NT];
 #pragma unroll

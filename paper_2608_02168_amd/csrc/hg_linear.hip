@@ -396,7 +396,7 @@ bool has_z(const Prob& p) { return p.gated || p.act != HG_ACT_NONE; }
 bool dz_direct(const Prob& p) { return !has_z(p) && (p.f32() || direct(p.f, p.ld_y)); }
 
 // Narrow float32 rows whose backward is one pass: groups of four aligned, and
-// several tiles for every block (200003 rows of 128: 170 us, 215 by tiles).
+// several tiles for every block (200003 rows of 128: 142 us, 198 by tiles).
 bool narrow(const Prob& p) {
   return p.f32() && !p.gated && p.d <= kNarrow && p.f <= kNarrow && p.n >= 16384 && p.d % 4 == 0 && p.f % 4 == 0 &&
          p.ld_x % 4 == 0 && p.ld_y % 4 == 0 && p.ld_r % 4 == 0;

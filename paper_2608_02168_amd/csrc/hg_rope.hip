@@ -7,7 +7,9 @@
 // backward, with g the upstream row turned back:
 //   dw = sum over rows of g x r,   dx = r (g w - x r mean(g w x r))
 //
-// One read and one write of every row: bound by HBM.  A head's row is taken by
+// One read and one write of every row: bound by HBM (32768 tokens of 40 heads of
+// 128, bfloat16: 138 us, 5.0 TB/s; backward of 20011 tokens of 24 heads of 64,
+// float32: 76 us, 4.9 TB/s; a large copy reaches 4.9).  A head's row is taken by
 // G lanes (a power of two), eight columns a lane, in two groups of four so
 // chosen that both columns of every pair are in one lane: columns 4 u .. and
 // rot / 2 + 4 u .. for pairs (p, p + rot / 2), columns 8 u .. + 7 for adjacent

@@ -703,6 +703,8 @@ __device__ __forceinline__ void g_parts3(f32x4 x, uint2 (&p)[3]) {
   }
 }
 
+__device__ const float g_zeros[4] = {0.f, 0.f, 0.f, 0.f};
+
 template <int BM, bool KM, int NT, bool GATED, bool VEC>
 struct GTile32 {
   static constexpr int kPlane = BM * kG32K * 2;      // bytes
@@ -714,8 +716,8 @@ struct GTile32 {
   // first: first row (KM) or column; rows and cols as stored; k0, k_to: the step's range
   __device__ __forceinline__ void load(const GOperand<float>& o, int64_t first, int64_t k0, int64_t k_to, int upper,
                                        int half) {
-#pragma unroll
-    for (int q = 0; q < PER; ++q) {
+    // group q: its address and how many of its values exist
+    auto at = [&](int q, int64_t& left) {
       const int id = threadIdx.x + q * NT, r = id / ACROSS, s = id % ACROSS * 4;
       int64_t row, col, to;
       if constexpr (KM) {
@@ -731,12 +733,31 @@ struct GTile32 {
         const int64_t wide = GATED ? half + (gr & 1) * upper : o.cols;
         to = row < k_to && row < o.rows ? wide : 0;
       }
-      const float* p = o.p + row * o.ld + col;
-      if (VEC) {
-        x[q] = col < to ? *reinterpret_cast<const f32x4*>(p) : f32x4{0.f, 0.f, 0.f, 0.f};
-      } else {
+      left = to - col;
+      return o.p + row * o.ld + col;
+    };
 #pragma unroll
-        for (int v = 0; v < 4; ++v) x[q][v] = col + v < to ? p[v] : 0.f;
+    for (int q = 0; q < PER; ++q) {
+      int64_t left;
+      const float* p = at(q, left);
+      if (VEC) {
+        x[q] = left > 0 ? *reinterpret_cast<const f32x4*>(p) : f32x4{0.f, 0.f, 0.f, 0.f};
+      } else {
+        // a load of 16 bytes needs 4-byte alignment only; all are issued before the
+        // groups at an edge are looked at (glu_odd: 15.8 us with single floats)
+        __builtin_memcpy(&x[q], left >= 4 ? p : g_zeros, 16);
+      }
+    }
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int q = 0; q < PER; ++q) {
+        int64_t left;
+        const float* p = at(q, left);
+        if (left > 0 && left < 4) {
+#pragma unroll
+          for (int v = 0; v < 3; ++v)
+            if (v < left) x[q][v] = p[v];
+        }
       }
     }
   }

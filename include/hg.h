@@ -529,7 +529,8 @@ int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t
  * term within about 2^-22 of itself; a row that holds an infinity or NaN gives
  * NaN in that row only.  In the backward dz = dY * act'(z) is formed from
  * float32 z; bfloat16 calls round it once (when act is not HG_ACT_NONE) as
- * operand of the two products, and dbias sums it before that. */
+ * operand of the two products, to 16 bits where dX or dW has fewer than 4096 values
+ * and to 8 else, and dbias sums it before that. */
 typedef struct hg_linear_desc {
   int64_t n;
   int32_t d_in, d_out;

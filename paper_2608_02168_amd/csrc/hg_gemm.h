@@ -69,6 +69,7 @@ struct GEpi {
   float* part;        // [splits][M][ld_part] when the k range is split
   int64_t ld_part;    // a multiple of 4
   int32_t parth;      // distance of the two halves in it, a multiple of 4
+  int64_t lo;         // gradient of z in two bfloat16 parts: values from out to the second
 };
 
 struct GShape {
@@ -82,6 +83,10 @@ struct GShape {
 template <class T>
 struct GArgs : GShape {
   GOperand<T> a, b;
+  // split bfloat16 products whose A or B is the sum of two planes: values from the
+  // first to the second, and the split from which on the second is taken (0: one plane)
+  int64_t lo_a, lo_b;
+  uint32_t lo_from;
 };
 
 // exp, the sigmoid and Phi(z) = (1 + erf(z / sqrt 2)) / 2 with e = exp(-z^2 / 2).
@@ -198,6 +203,15 @@ __device__ __forceinline__ void g_store4(void* p, int64_t at, int n, bool vec, c
   }
 }
 
+// What bfloat16 rounding took from the values, into the second plane.
+template <class T>
+__device__ __forceinline__ void g_store_lo(const GEpi& e, int64_t at, int n, bool vec, const float (&v)[4]) {
+  float l[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) l[q] = v[q] - bf2f(f2bf(v[q]));
+  g_store4<T>(e.out, at + e.lo, n, vec, l);
+}
+
 // Rows whose four-value groups can be moved at once.
 template <class T>
 __device__ __forceinline__ bool g_vec(const void* p, int64_t ld) {
@@ -275,8 +289,9 @@ struct EpiLinear {
 };
 
 // out = res * act'(z + bias): the gradient of z; the padding of a row is written as zero
-template <class T>
+template <class T, bool LO>
 struct EpiLinearGrad {
+  static constexpr bool kLo = LO;  // in two parts
   static constexpr bool kGated = false, kColSum = true, kAct = true;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
     GCols c = g_cols<T>(e, n, e.ncol - n, false);
@@ -295,6 +310,7 @@ struct EpiLinearGrad {
 #pragma unroll
     for (int q = 0; q < 4; ++q) z[q] = q < c.left ? r[q] * d[q] : 0.f;
     g_store4<T>(e.out, m * e.ld_out + c.n, e.outp - c.n, c.vo, z);
+    if constexpr (LO) g_store_lo<T>(e, m * e.ld_out + c.n, e.outp - c.n, c.vo, z);
   }
 };
 
@@ -350,8 +366,9 @@ struct EpiGated {
 };
 
 // da = dh u act'(a), du = dh act(a), side by side; the padding of a half is written as zero
-template <class T>
+template <class T, bool LO>
 struct EpiGatedGrad {
+  static constexpr bool kLo = LO;  // in two parts
   static constexpr bool kGated = true, kColSum = true, kAct = true;
   __device__ static __forceinline__ GCols cols(const GEpi& e, int n) {
     GCols c = g_cols<T>(e, n, e.half - n, true);
@@ -377,6 +394,8 @@ struct EpiGatedGrad {
     const int64_t at = m * e.ld_out + c.n;
     g_store4<T>(e.out, at, e.outp - c.n, c.vo, a);
     g_store4<T>(e.out, at + e.outp, e.outp - c.n, c.vo, u);
+    if constexpr (LO) g_store_lo<T>(e, at, e.outp - c.n, c.vo, a);
+    if constexpr (LO) g_store_lo<T>(e, at + e.outp, e.outp - c.n, c.vo, u);
   }
 };
 
@@ -622,7 +641,14 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
   const int64_t m0 = (int64_t)im * BM;
   const int n0 = (int)in * BN;               // tile column of Z
   const int bcol = GATED ? (int)in * (BN / 2) : n0;  // first column of B that the tile reads
-  const int64_t k_from = SPLIT ? (int64_t)blockIdx.y * p.k_split : 0;
+  const uint16_t *ap = p.a.p, *bp = p.b.p;
+  uint32_t split = SPLIT ? blockIdx.y : 0;
+  if (SPLIT && p.lo_from && split >= p.lo_from) {
+    split -= p.lo_from;
+    ap += p.lo_a;
+    bp += p.lo_b;
+  }
+  const int64_t k_from = SPLIT ? (int64_t)split * p.k_split : 0;
   const int64_t k_to = SPLIT ? (k_from + p.k_split < p.K ? k_from + p.k_split : p.K) : p.K;
   const int steps = (int)((k_to - k_from + BK - 1) / BK);
 
@@ -637,16 +663,16 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64)
     const uint32_t st = lds0 + (t & 1) * kStage;
     const uint32_t sb = st + TA::kBytes;
     if constexpr (AKM) {
-      ta.issue(p.a.p + m0 * p.a.ld + k0, 2 * ((p.a.rows - m0 - 1) * p.a.ld + p.a.cols - k0), kl, st, wave);
+      ta.issue(ap + m0 * p.a.ld + k0, 2 * ((p.a.rows - m0 - 1) * p.a.ld + p.a.cols - k0), kl, st, wave);
     } else {
-      ta.issue(p.a.p + k0 * p.a.ld + m0, 2 * ((kl - 1) * p.a.ld + p.a.cols - m0), kl, st, wave);
+      ta.issue(ap + k0 * p.a.ld + m0, 2 * ((kl - 1) * p.a.ld + p.a.cols - m0), kl, st, wave);
     }
     if constexpr (BKM) {
-      tb.issue(p.b.p + (int64_t)bcol * p.b.ld + k0, 2 * ((p.b.rows - bcol - 1) * p.b.ld + p.b.cols - k0), kl, sb, wave);
+      tb.issue(bp + (int64_t)bcol * p.b.ld + k0, 2 * ((p.b.rows - bcol - 1) * p.b.ld + p.b.cols - k0), kl, sb, wave);
     } else {
       // rows that B has: its k may end before A's padded one
       const int64_t rl = (p.b.rows < k_to ? p.b.rows : k_to) - k0;
-      tb.issue(p.b.p + k0 * p.b.ld + bcol, 2 * ((rl - 1) * p.b.ld + p.b.cols - bcol), rl, sb, wave);
+      tb.issue(bp + k0 * p.b.ld + bcol, 2 * ((rl - 1) * p.b.ld + p.b.cols - bcol), rl, sb, wave);
     }
   };
 

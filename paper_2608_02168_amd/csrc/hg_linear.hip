@@ -287,7 +287,9 @@ Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32, int6
   return t;
 }
 
-int64_t part_elems(const Tiling& t, int64_t M, int64_t ld) { return t.splits > 1 ? t.splits * M * ld : 0; }
+int64_t part_elems(const Tiling& t, int64_t M, int64_t ld, int planes = 1) {
+  return t.splits * planes > 1 ? (int64_t)t.splits * planes * M * ld : 0;
+}
 
 template <auto kern>
 int allow_lds(size_t lds) {
@@ -339,13 +341,25 @@ struct EpiPart {
   static constexpr bool kGated = GATED, kColSum = false, kAct = false;
 };
 
+// Whether an epilogue writes a gradient in two parts (tiles of 128 at most).
+template <class Epi>
+constexpr bool two_parts() {
+  if constexpr (Epi::kColSum) return Epi::kLo;
+  return false;
+}
+
 template <bool AKM, bool BKM, class Epi, class T>
 int launch_product(const char* name, GArgs<T> a, const Tiling& t, float* part, int32_t parth, hipStream_t s) {
   a.tiles_m = (int32_t)t.tiles_m;
   a.tiles_n = (int32_t)t.tiles_n;
   a.k_split = t.k_split;
-  if (t.splits == 1) {
-    if constexpr (sizeof(T) == 2)
+  Tiling u = t;  // the blocks of both planes
+  if (a.lo_a || a.lo_b) {
+    a.lo_from = (uint32_t)t.splits;
+    u.splits = 2 * t.splits;
+  }
+  if (u.splits == 1) {
+    if constexpr (sizeof(T) == 2 && !two_parts<Epi>())
       if (t.tile == 256) return launch_tiles<AKM, BKM, 256, Epi, false>(name, a, t, s);
     if (t.tile == 128) return launch_tiles<AKM, BKM, 128, Epi, false>(name, a, t, s);
     return launch_tiles<AKM, BKM, 64, Epi, false>(name, a, t, s);
@@ -356,15 +370,15 @@ int launch_product(const char* name, GArgs<T> a, const Tiling& t, float* part, i
     a.e.parth = parth;
     a.e.ld_part = (Epi::kGated ? 2 : 1) * (int64_t)parth;
     if (t.tile == 128) {
-      HG_TRY((launch_tiles<AKM, BKM, 128, Part, true>(name, a, t, s)));
+      HG_TRY((launch_tiles<AKM, BKM, 128, Part, true>(name, a, u, s)));
     } else {
-      HG_TRY((launch_tiles<AKM, BKM, 64, Part, true>(name, a, t, s)));
+      HG_TRY((launch_tiles<AKM, BKM, 64, Part, true>(name, a, u, s)));
     }
     const int64_t quads = a.M * cdiv(Epi::kGated ? a.e.halfp : a.N, 4);
-    if (t.splits > 8) {
-      HG_LAUNCH("product_join", (k_product_join<Epi, 8>), dim3((unsigned)cdiv(quads, 32)), dim3(256), 0, s, a, t.splits);
+    if (u.splits > 8) {
+      HG_LAUNCH("product_join", (k_product_join<Epi, 8>), dim3((unsigned)cdiv(quads, 32)), dim3(256), 0, s, a, u.splits);
     } else {
-      HG_LAUNCH("product_join", (k_product_join<Epi, 1>), dim3((unsigned)cdiv(quads, 256)), dim3(256), 0, s, a, t.splits);
+      HG_LAUNCH("product_join", (k_product_join<Epi, 1>), dim3((unsigned)cdiv(quads, 256)), dim3(256), 0, s, a, u.splits);
     }
   }
   return HG_OK;
@@ -392,6 +406,18 @@ Tiling t_dw(const Prob& p) { return tiling(p.d, p.colsp(), p.n, true, p.f32(), 0
 bool x_direct(const Prob& p) { return p.f32() || direct(p.d, p.ld_x); }
 bool w_direct(const Prob& p) { return p.f32() || p.f % 8 == 0; }
 bool has_z(const Prob& p) { return p.gated || p.act != HG_ACT_NONE; }
+// Parts (bfloat16 values) that a bfloat16 gradient of z is kept in.  One adds as much
+// to the error of dX and dW as their own rounding (together 0.0023 of the norm,
+// 0.0017 without; 0.0025 met among results of some hundred values, whose error
+// varies most).  Two where a result has few values and the products are bound by
+// their launches (10 rows, 24 to 1448: 33 us, 27 with one part; 60000 rows, 64 to
+// 64, keep one: 30 us, 47 with two).  Never with tiles of 256.
+int planes(const Prob& p) {
+  return !p.f32() && has_z(p) && p.d * std::min<int64_t>(p.n, p.cols()) < 4096 &&
+                 p.n * p.d <= ((int64_t)1 << 28) / p.cols()
+             ? 2
+             : 1;
+}
 // the upstream rows are dz itself and can be read where they lie
 bool dz_direct(const Prob& p) { return !has_z(p) && (p.f32() || direct(p.f, p.ld_y)); }
 
@@ -429,14 +455,15 @@ Bufs take_bwd(const Prob& p, Mem& m) {
     if (p.f32()) {
       b.dz = m.template take<float>(p.n * p.colsp());
     } else {
-      b.dz = m.template take<uint16_t>(p.n * p.colsp());
+      b.dz = m.template take<uint16_t>(planes(p) * p.n * p.colsp());
     }
   }
   b.colsum_rows = has_z(p) ? t_z(p).tiles_m : cdiv(p.n, kSumRows);
   // (a narrow call may still go by tiles: without dX, or to rows that are not aligned)
   const int64_t blocks = narrow(p) ? kNarrowBlocks : 0;
   b.colsum = m.template take<float>(std::max(b.colsum_rows, blocks) * p.cols());
-  b.part = m.template take<float>(std::max({part_elems(t_dx(p), p.n, pad4(p.d)), part_elems(t_dw(p), p.d, pad4(p.colsp())),
+  b.part = m.template take<float>(std::max({part_elems(t_dx(p), p.n, pad4(p.d), planes(p)),
+                                            part_elems(t_dw(p), p.d, pad4(p.colsp()), planes(p)),
                                             blocks * p.d * p.f}));
   return b;
 }
@@ -573,7 +600,8 @@ int narrow_bwd(const Prob& p, const float* X, const float* W, const float* bias,
 template <class T, bool GATED>
 int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, const void* dY, void* dX, int64_t ld_dx,
              void* dW, float* dbias, int accumulate, const Bufs& b, hipStream_t s) {
-  typedef typename std::conditional<GATED, EpiGatedGrad<T>, EpiLinearGrad<T>>::type EpiG;
+  typedef typename std::conditional<GATED, EpiGatedGrad<T, false>, EpiLinearGrad<T, false>>::type EpiG;
+  typedef typename std::conditional<GATED, EpiGatedGrad<T, true>, EpiLinearGrad<T, true>>::type EpiG2;
   if constexpr (sizeof(T) == 4 && !GATED) {
     if (narrow(p) && dX && dW && aligned16(dX))
       return narrow_bwd(p, static_cast<const float*>(X), static_cast<const float*>(W), bias, static_cast<const float*>(dY),
@@ -581,7 +609,8 @@ int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
   }
   GOperand<T> x{}, w{};
   HG_TRY(operands(p, X, W, b, x, w, s));
-  // dz, in rows of colsp (or where the upstream rows lie)
+  // dz, in rows of colsp (or where the upstream rows lie); its second part
+  const int64_t lo = planes(p) == 2 ? p.n * p.colsp() : 0;
   GOperand<T> z{static_cast<const T*>(b.dz), p.colsp(), p.n, p.colsp()};
   if (has_z(p)) {
     GArgs<T> a{};
@@ -593,7 +622,14 @@ int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
     a.e = epi_of(p, bias, dY, p.ld_y, b.dz, p.colsp());
     a.e.colsum = dbias ? b.colsum : nullptr;
     a.e.ld_colsum = p.cols();
-    HG_TRY((launch_product<true, false, EpiG>(GATED ? "glu_dz" : "linear_dz", a, t_z(p), nullptr, 0, s)));
+    a.e.lo = lo;
+    const char* name = GATED ? "glu_dz" : "linear_dz";
+    bool two = false;
+    if constexpr (sizeof(T) == 2) {
+      two = lo > 0;
+      if (two) HG_TRY((launch_product<true, false, EpiG2>(name, a, t_z(p), nullptr, 0, s)));
+    }
+    if (!two) HG_TRY((launch_product<true, false, EpiG>(name, a, t_z(p), nullptr, 0, s)));
   } else {
     if (dbias)
       HG_LAUNCH("colsum", k_colsum<T>, dim3((unsigned)b.colsum_rows, (unsigned)cdiv(p.cols(), 64)), dim3(256), 0, s, dY,
@@ -618,6 +654,7 @@ int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
     a.e.out = dX;
     a.e.ld_out = ld_dx;
     a.e.ncol = p.d;
+    a.lo_a = lo;
     HG_TRY((launch_product<true, true, EpiSum<T>>(GATED ? "glu_dx" : "linear_dx", a, t_dx(p), b.part, (int32_t)pad4(p.d), s)));
   }
   if (dW) {
@@ -635,6 +672,7 @@ int bwd_impl(const Prob& p, const void* X, const void* W, const float* bias, con
       a.e.halfp = p.fp();
     }
     a.e.accumulate = accumulate;
+    a.lo_b = lo;
     HG_TRY((launch_product<false, false, EpiSum<T>>(GATED ? "glu_dw" : "linear_dw", a, t_dw(p), b.part,
                                                     (int32_t)pad4(p.colsp()), s)));
   }

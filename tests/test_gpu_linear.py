@@ -291,3 +291,22 @@ def test_refusals():
         api.hg_glu_fwd(x, W[:, :31].contiguous())
     with pytest.raises(ValueError):
         api.hg_linear_bwd(x, W, b, torch.empty(20, 32, dtype=BF16, device="cuda"), accumulate=True)
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("n,d,f", [(10, 24, 1448), (1, 100, 37), (300, 13, 260)])
+def test_small_bf16_gradients_keep_their_precision(n, d, f, gated):
+    """Where a result has few values, dz enters the products with 16 bits: the
+    gradients are off by their own rounding, at most 2^-9 of each value and so of the
+    norm, and 1% more for dz and the sums."""
+    x, w = normal(1, n, d, dtype=BF16), normal(2, d, 2 * f if gated else f, dtype=BF16, scale=d ** -0.5)
+    b, up = normal(3, w.shape[1]), normal(4, n, f, dtype=BF16)
+    if gated:
+        got = api.hg_glu_bwd(x, w, b, up, act=api.HG_ACT_SILU)
+    else:
+        got = api.hg_linear_bwd(x, w, b, up, act=api.HG_ACT_SILU)
+    X, W = x.double().requires_grad_(), w.double().requires_grad_()
+    z = X @ W + b.double()
+    y = torch.nn.functional.silu(z[:, :f]) * z[:, f:] if gated else torch.nn.functional.silu(z)
+    for g, r in zip(got, torch.autograd.grad(y, (X, W), up.double())):
+        assert float((g.double() - r).norm() / r.norm()) <= 1.01 * 2.0 ** -9

@@ -299,8 +299,8 @@ def test_small_bf16_gradients_keep_their_precision(n, d, f, gated):
     """Where a result has few values, dz enters the products with 16 bits: the
     gradients are off by their own rounding, at most 2^-9 of each value and so of the
     norm, and 1% more for dz and the sums."""
-    x, w = normal(1, n, d, dtype=BF16), normal(2, d, 2 * f if gated else f, dtype=BF16, scale=d ** -0.5)
-    b, up = normal(3, w.shape[1]), normal(4, n, f, dtype=BF16)
+    x, w = draw(1, n, d, dtype=BF16), draw(2, d, 2 * f if gated else f, dtype=BF16, scale=d ** -0.5)
+    b, up = draw(3, w.shape[1]), draw(4, n, f, dtype=BF16)
     if gated:
         got = api.hg_glu_bwd(x, w, b, up, act=api.HG_ACT_SILU)
     else:

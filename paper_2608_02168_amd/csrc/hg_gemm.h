@@ -770,7 +770,8 @@ struct GTile32 {
         x[q] = left > 0 ? *reinterpret_cast<const f32x4*>(p) : f32x4{0.f, 0.f, 0.f, 0.f};
       } else {
         // a load of 16 bytes needs 4-byte alignment only; all are issued before the
-        // groups at an edge are looked at (glu_odd: 15.8 us with single floats)
+        // groups at an edge are looked at (gated, 1777 rows, 200 to 2 x 517: 13.0 us,
+        // 15.8 with single floats)
         __builtin_memcpy(&x[q], left >= 4 ? p : g_zeros, 16);
       }
     }

@@ -411,9 +411,14 @@ __device__ __forceinline__ u32x4 g_rsrc(const void* base, uint32_t bytes) {
 // 16 bytes a lane from base + voff to LDS address lds + 16 * lane.  Written as
 // an instruction, since the compiler would let every later LDS read wait for
 // it: the caller waits (g_wait_loads) before the barrier that hands the buffer
-// over.  It has no result register.
+// over.  It has no result register.  The compiler does not look into the block
+// for what has to lie apart, so the block keeps it apart itself: one wait state
+// from the write of m0 to the load that takes its LDS address from it, five from
+// a vector instruction's write of a scalar register to a load that reads it (the
+// descriptor's words may come from v_readfirstlane).
 __device__ __forceinline__ void g_load_lds(u32x4 rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(voff), "s"(rsrc)
+               : "memory");
 }
 __device__ __forceinline__ void g_wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 

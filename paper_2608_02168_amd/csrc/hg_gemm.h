@@ -89,29 +89,21 @@ struct GArgs : GShape {
   uint32_t lo_from;
 };
 
-// exp, the sigmoid and Phi(z) = (1 + erf(z / sqrt 2)) / 2 with e = exp(-z^2 / 2).
-// float32 results take the library functions; results that are rounded to
-// bfloat16 take the hardware's exponential (relative error below 2^-18 for
-// |x| <= 32) and erf by the rational approximation 7.1.26 of Abramowitz and
-// Stegun (absolute error 1.5e-7): a float32 epilogue of 256 x 256 values cost
-// 35 us of a tile's time, this one 9.
-template <class T>
+// exp: 2^h of the rounded h = x log2 e from the hardware, corrected by the factor
+// 1 + l ln 2 for what the rounding left (as a factor, since 2^h is infinite from
+// x = 88.72 on, and adding l ln 2 times it would be NaN); relative error below 2^-22.
 __device__ __forceinline__ float g_exp(float x) {
   constexpr float kLog2e = 1.4426950408889634f;
-  if constexpr (sizeof(T) == 4) {
-    x = __builtin_amdgcn_fmed3f(x, -150.f, 150.f);
-    const float h = x * kLog2e, l = fmaf(x, 1.9259629911e-8f, fmaf(x, kLog2e, -h)), r = __builtin_amdgcn_exp2f(h);
-    return fmaf(r, l * 0.69314718056f, r);
-  } else {
-    return __builtin_amdgcn_exp2f(x * kLog2e);
-  }
+  x = __builtin_amdgcn_fmed3f(x, -150.f, 150.f);  // (so that l is a number)
+  const float h = x * kLog2e, l = fmaf(x, 1.9259629911e-8f, fmaf(x, kLog2e, -h));
+  return __builtin_amdgcn_exp2f(h) * fmaf(l, 0.69314718056f, 1.f);
 }
 
-template <class T>
-__device__ __forceinline__ float g_sigmoid(float z) {
-  return __builtin_amdgcn_rcpf(1.f + g_exp<T>(-z));
-}
+__device__ __forceinline__ float g_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + g_exp(-z)); }
 
+// Phi(z) = (1 + erf(z / sqrt 2)) / 2 with e = exp(-z^2 / 2).  float32 results take the
+// library's erf; results that are rounded to bfloat16 the rational approximation
+// 7.1.26 of Abramowitz and Stegun (absolute error 1.5e-7).
 template <class T>
 __device__ __forceinline__ float g_phi(float z, float e) {
   if constexpr (sizeof(T) == 4) {
@@ -131,14 +123,14 @@ __device__ __forceinline__ void g_act4(const float (&z)[4], float (&f)[4], float
   if constexpr (ACT == HG_ACT_SILU) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float s = g_sigmoid<T>(z[q]);
+      const float s = g_sigmoid(z[q]);
       f[q] = z[q] * s;
       if (G) d[q] = fmaf(f[q], 1.f - s, s);
     }
   } else if constexpr (ACT == HG_ACT_GELU) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      const float e = sizeof(T) == 2 || G ? g_exp<T>(-0.5f * z[q] * z[q]) : 0.f, p = g_phi<T>(z[q], e);
+      const float e = sizeof(T) == 2 || G ? g_exp(-0.5f * z[q] * z[q]) : 0.f, p = g_phi<T>(z[q], e);
       f[q] = z[q] * p;
       if (G) d[q] = fmaf(z[q] * e, 0.39894228040143268f, p);
     }

@@ -9,9 +9,11 @@ the sums of dz over the rows, and dX is dz W^T.
 
 Bounds.  SiLU is z s(z): the exponential, 1 + e, the reciprocal and the product
 are each off by at most 2^-22 relative, 2^-20 together; where s falls below the
-smallest normal number 2^-126 it may be zero.  GELU in float32 is z (1 + erf) / 2
-with 1 + erf formed to 2^-22.  bfloat16 results add one rounding: 8 bits, 2^-8 of
+smallest normal number 2^-126 it may be zero.  GELU is z Phi(z), with
+Phi formed to 2^-22 (the last test holds negative z to their own size).  bfloat16 results add one rounding: 8 bits, 2^-8 of
 a value just above a power of two."""
+import math
+
 import numpy as np
 import pytest
 
@@ -129,3 +131,20 @@ def test_infinities_stay_in_their_column(n, d, act, dtype):
     _, cW, cb = api.hg_linear_bwd(x, W, clean, up, act=ACT[act], want=(False, True, True))
     keep = torch.from_numpy(fin).cuda()
     assert torch.equal(dW[:, keep], cW[:, keep]) and torch.equal(db[keep], cb[keep])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d", ROWS)
+def test_gelu_keeps_its_digits_below_zero(n, d, dtype):
+    """z Phi(z) for z = -13 .. 0 to its own size: the tail and the products to 2^-20, exp(-z^2 / 2) to z^2 2^-24 for
+    the rounding of z^2, one rounding of the result."""
+    z = np.linspace(-13, 0, 800).astype(np.float32)
+    z64 = z.astype(np.float64)
+    ref = z64 * 0.5 * np.vectorize(math.erfc)(-z64 / math.sqrt(2))
+    rel = 2.0 ** -20 + z64 ** 2 * 2.0 ** -24 + (2.0 ** -8 if dtype == BF16 else 0)
+    x, W, b, _ = problem(n, d, z, dtype, False)
+    err = np.abs(host(api.hg_linear_fwd(x, W, bias=b, act=api.HG_ACT_GELU)) - ref)
+    assert np.all(err <= rel * np.abs(ref) + 13 * 2.0 ** -125)
+    x, W, b, _ = problem(n, d, z, dtype, True)
+    err = np.abs(host(api.hg_glu_fwd(x, W, bias=b, act=api.HG_ACT_GELU)) - 1.5 * ref)
+    assert np.all(err <= (rel * np.abs(ref) + 13 * 2.0 ** -125) * 1.5)

@@ -512,6 +512,7 @@ int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t
  * Here every matrix of a call, weights and weight gradients too, is stored in
  * dtype (HG_DTYPE_F32 or HG_DTYPE_BF16); biases, norm weights, decays, states
  * and their gradients are float32.  Sums are float32 whatever dtype is.
+ * Workspaces are 16-byte aligned.
  *
  * Linear map with bias, activation and residual in its epilogue (the node
  * update of E11 with any widths):

@@ -690,11 +690,18 @@ def _float_code(where: str, t) -> int:
 
 
 def _same(where: str, t, *others):
-    """Every given tensor has the first one's type and device."""
+    """Every given tensor has the first one's type and device, which is a GPU."""
     dtype, dev = t.dtype, t.get_device()
+    _on_gpu(where, t)
     for o in others:
         if o is not None and (o.dtype is not dtype or o.get_device() != dev):
             raise TypeError(f"{where}: {o.dtype} on {o.device} beside {t.dtype} on {t.device}")
+
+
+def _on_gpu(where: str, t):
+    """The library takes device addresses only: a host address would fault in a kernel."""
+    if t.get_device() < 0:
+        raise TypeError(f"{where}: a tensor on {t.device}, expected one on a GPU")
 
 
 def _vector(where: str, t, n: int, like, dtype=torch.float32):
@@ -739,13 +746,15 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _workspace(ws, need: int, like):
+def _workspace(where: str, ws, need: int, like):
     """(buffer kept alive by the caller, its address, its size)"""
     if ws is None:
         if not need:
             return None, None, 0
         ws = torch.empty(need, dtype=torch.uint8, device=like.device)
-    return ws, ws.data_ptr(), ws.numel()
+    elif ws.get_device() != like.get_device() or not ws.is_contiguous():
+        raise ValueError(f"{where}: expected a contiguous workspace on {like.device}, got strides {ws.stride()} on {ws.device}")
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _raw_stream(like):
@@ -795,7 +804,7 @@ def hg_linear_fwd(x, W, bias=None, residual=None, act: int = HG_ACT_NONE, y=None
     _same(where, x, W, y, residual)
     desc = _pack_linear(n, d, m, _float_code(where, x), act, _rows(where, x, n, d), ld_y,
                         m if residual is None else _rows(where, residual, n, m))
-    ws, wp, wn = _workspace(ws, L.hg_linear_fwd_workspace_size(desc), x)
+    ws, wp, wn = _workspace(where, ws, L.hg_linear_fwd_workspace_size(desc), x)
     st = L.hg_linear_fwd(desc, x.data_ptr(), W.data_ptr(), _vector(where, bias, m, x), _addr(residual), y.data_ptr(), wp,
                          wn, _raw_stream(x))
     if st:
@@ -819,7 +828,7 @@ def hg_linear_bwd(x, W, bias, dy, act: int = HG_ACT_NONE, dx=None, dW=None, dbia
     _same(where, x, W, dy, dx, dW)
     desc = _pack_linear(n, d, m, _float_code(where, x), act, _rows(where, x, n, d), _rows(where, dy, n, m),
                         d if dx is None else _rows(where, dx, n, d))
-    ws, wp, wn = _workspace(ws, L.hg_linear_bwd_workspace_size(desc), x)
+    ws, wp, wn = _workspace(where, ws, L.hg_linear_bwd_workspace_size(desc), x)
     st = L.hg_linear_bwd(desc, x.data_ptr(), W.data_ptr(), _addr(bias), dy.data_ptr(), _addr(dx), _addr(dW), _addr(dbias),
                          1 if accumulate else 0, wp, wn, _raw_stream(x))
     if st:
@@ -877,7 +886,7 @@ def hg_glu_fwd(x, W, bias=None, act: int = HG_ACT_SILU, h=None, ws=None, stream=
         ld_h = _rows(where, h, n, f)
     _same(where, x, W, h)
     desc = _pack_glu(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), ld_h, d)
-    ws, wp, wn = _workspace(ws, L.hg_glu_fwd_workspace_size(desc), x)
+    ws, wp, wn = _workspace(where, ws, L.hg_glu_fwd_workspace_size(desc), x)
     st = L.hg_glu_fwd(desc, x.data_ptr(), W.data_ptr(), _vector(where, bias, 2 * f, x), h.data_ptr(), wp, wn,
                       _raw_stream(x))
     if st:
@@ -898,7 +907,7 @@ def hg_glu_bwd(x, W, bias, dh, act: int = HG_ACT_SILU, dx=None, dW=None, dbias=N
     _same(where, x, W, dh, dx, dW)
     desc = _pack_glu(n, d, f, _float_code(where, x), act, _rows(where, x, n, d), _rows(where, dh, n, f),
                      d if dx is None else _rows(where, dx, n, d))
-    ws, wp, wn = _workspace(ws, L.hg_glu_bwd_workspace_size(desc), x)
+    ws, wp, wn = _workspace(where, ws, L.hg_glu_bwd_workspace_size(desc), x)
     st = L.hg_glu_bwd(desc, x.data_ptr(), W.data_ptr(), _addr(bias), dh.data_ptr(), _addr(dx), _addr(dW), _addr(dbias),
                       1 if accumulate else 0, wp, wn, _raw_stream(x))
     if st:
@@ -916,6 +925,7 @@ def hg_rope_table(n_pos: int, rot: int, base: float = 10000.0, step: float = 1.0
         table = torch.empty((n_pos, rot), dtype=torch.float32, device=device)
     elif tuple(table.shape) != (n_pos, rot) or table.dtype != torch.float32 or not table.is_contiguous():
         raise ValueError(f"hg_rope_table: expected a contiguous float32 [{n_pos}, {rot}], got {tuple(table.shape)}")
+    _on_gpu("hg_rope_table", table)
     _check(lib().hg_rope_table(n_pos, rot, base, step, table.data_ptr(), _raw_stream(table)), "hg_rope_table")
     return table
 
@@ -981,7 +991,7 @@ def hg_qk_norm_rope_bwd(q, k, wq, wk, table, pos, dq_out, dk_out, eps: float = 1
     _same(where, q, k, dq_out, dk_out, dq, dk)
     h = [_heads(where, n, t, qs) for n, t in (("q", q), ("dq_out", dq_out), ("dq", dq))]
     g = [None if k is None else _heads(where, n, t, ks) for n, t in (("k", k), ("dk_out", dk_out), ("dk", dk))]
-    ws, wp, wn = _workspace(ws, L.hg_qk_norm_rope_bwd_workspace_size(desc), q)
+    ws, wp, wn = _workspace(where, ws, L.hg_qk_norm_rope_bwd_workspace_size(desc), q)
     d = qs[2]
     st = L.hg_qk_norm_rope_bwd(desc, h[0], g[0], _vector(where, wq, d, q), _vector(where, wk, d, q), table.data_ptr(),
                                _vector(where, pos, qs[0], q, torch.int32), h[1], g[1], h[2], g[2],
@@ -1028,7 +1038,7 @@ def hg_linattn_fwd(q, k, v, log_decay, scale: float = 1.0, lens=None, state=None
     _same(where, q, k, v, o)
     kv = (b, t, k.shape[2], d)
     desc = _pack_linattn(t, b, h, kv[2], d, _float_code(where, q), scale)
-    ws, wp, wn = _workspace(ws, L.hg_linattn_fwd_workspace_size(desc), q)
+    ws, wp, wn = _workspace(where, ws, L.hg_linattn_fwd_workspace_size(desc), q)
     st = L.hg_linattn_fwd(desc, _heads(where, "q", q, qs), _heads(where, "k", k, kv), _heads(where, "v", v, kv),
                           _vector(where, log_decay, h, q), _vector(where, lens, b, q, torch.int32),
                           _state(where, state, (b, h, d, d), q), _heads(where, "o", o, qs),
@@ -1059,7 +1069,7 @@ def hg_linattn_bwd(q, k, v, log_decay, do, scale: float = 1.0, lens=None, state=
     dv = torch.empty(kv, dtype=q.dtype, device=q.device) if dv is None else dv
     _same(where, q, k, v, do, dq, dk, dv)
     desc = _pack_linattn(t, b, h, kv[2], d, _float_code(where, q), scale)
-    ws, wp, wn = _workspace(ws, L.hg_linattn_bwd_workspace_size(desc), q)
+    ws, wp, wn = _workspace(where, ws, L.hg_linattn_bwd_workspace_size(desc), q)
     st = L.hg_linattn_bwd(desc, _heads(where, "q", q, qs), _heads(where, "k", k, kv), _heads(where, "v", v, kv),
                           _vector(where, log_decay, h, q), _vector(where, lens, b, q, torch.int32),
                           _state(where, state, s, q), _heads(where, "do", do, qs), _state(where, dstate_out, s, q),

@@ -977,6 +977,7 @@ extern "C" int hg_linattn_fwd(const hg_linattn_desc* A, const hg_heads* q, const
   take(A, false, need);
   if (ws_bytes < need.used || (need.used && !ws))
     return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(HG_ERR_ARG, "%s: the workspace is not 16-byte aligned", what);
   Arena m(ws, ws_bytes);
   const Bufs b = take(A, false, m);
   Walks ws_{};
@@ -1014,6 +1015,7 @@ extern "C" int hg_linattn_bwd(const hg_linattn_desc* A, const hg_heads* q, const
   take(A, true, need);
   if (ws_bytes < need.used || (need.used && !ws))
     return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(HG_ERR_ARG, "%s: the workspace is not 16-byte aligned", what);
   Arena m(ws, ws_bytes);
   const Bufs b = take(A, true, m);
   const int group = A->heads / A->kv_heads, gr = split_of(A, 3).gr;

@@ -716,6 +716,7 @@ int forward(const Prob& p, const char* what, const void* X, const void* W, const
   take_fwd(p, need);
   if (ws_bytes < need.used || (need.used && !ws))
     return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  if (!aligned16(ws)) return fail(HG_ERR_ARG, "%s: the workspace is not 16-byte aligned", what);
   Arena m(ws, ws_bytes);
   const Bufs b = take_fwd(p, m);
   if (p.f32())
@@ -753,6 +754,7 @@ int backward(const Prob& p, const char* what, const void* X, const void* W, cons
   take_bwd(p, need);
   if (ws_bytes < need.used || (need.used && !ws))
     return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+  if (!aligned16(ws)) return fail(HG_ERR_ARG, "%s: the workspace is not 16-byte aligned", what);
   Arena m(ws, ws_bytes);
   const Bufs b = take_bwd(p, m);
   if (p.f32())

@@ -474,6 +474,7 @@ extern "C" int hg_qk_norm_rope_bwd(const hg_rope_desc* D, const hg_heads* q, con
     need.take<float>((int64_t)blocks * 2 * D->d);
     if (!ws || ws_bytes < need.used)
       return fail(HG_ERR_CAPACITY, "%s: workspace of %zu bytes, %zu needed", what, ws_bytes, need.used);
+    if (reinterpret_cast<uintptr_t>(ws) & 15) return fail(HG_ERR_ARG, "%s: the workspace is not 16-byte aligned", what);
     Arena m(ws, ws_bytes);
     a.part = m.take<float>((int64_t)blocks * 2 * D->d);
   }

@@ -1,0 +1,92 @@
+"""Where the tensors of the sequence encoder's calls lie (no GPU is needed): host
+tensors, whose addresses would fault in a kernel, and workspaces on another
+device, with gaps or not aligned are refused before anything reaches the library."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import os
+
+from paper_2608_02168_amd import api
+
+P = 0x10000  # never dereferenced: validation fails first
+
+
+class Library:
+    """Answers the workspace sizes and fails a test that launches."""
+
+    def __getattr__(self, name):
+        if name.endswith("_workspace_size"):
+            return lambda *a: 4096
+        return lambda *a: pytest.fail(f"{name} was called")
+
+
+@pytest.fixture
+def no_launch(monkeypatch):
+    monkeypatch.setattr(api, "lib", Library)
+    monkeypatch.setattr(api, "_current_raw", lambda device: 0)
+
+
+def calls():
+    x, W, b, y = torch.randn(3, 8), torch.randn(8, 16), torch.randn(16), torch.randn(3, 16)
+    q, k, one = torch.randn(3, 2, 8), torch.randn(3, 1, 8), torch.ones(8)
+    table, pos = torch.randn(5, 8), torch.zeros(3, dtype=torch.int32)
+    q4, k4, g, S = torch.randn(2, 3, 2, 8), torch.randn(2, 3, 1, 8), torch.zeros(2), torch.zeros(3, 2, 8, 8)
+    return {
+        "linear_fwd": lambda: api.hg_linear_fwd(x, W, bias=b),
+        "linear_bwd": lambda: api.hg_linear_bwd(x, W, b, y),
+        "glu_fwd": lambda: api.hg_glu_fwd(x, W, bias=b),
+        "glu_bwd": lambda: api.hg_glu_bwd(x, W, b, y[:, :8].contiguous()),
+        "table": lambda: api.hg_rope_table(5, 8, device="cpu"),
+        "given table": lambda: api.hg_rope_table(5, 8, table=table),
+        "rope_fwd": lambda: api.hg_qk_norm_rope_fwd(q, k, one, one, table, pos),
+        "rope_bwd": lambda: api.hg_qk_norm_rope_bwd(q, k, one, one, table, pos, q, k),
+        "linattn_fwd": lambda: api.hg_linattn_fwd(q4, k4, k4, g),
+        "linattn_bwd": lambda: api.hg_linattn_bwd(q4, k4, k4, g, q4),
+        "linattn_step": lambda: api.hg_linattn_step(q, k, k, g, S),
+    }
+
+
+@pytest.mark.parametrize("name", list(calls()))
+def test_host_tensors_are_refused(no_launch, name):
+    with pytest.raises(TypeError, match="GPU"):
+        calls()[name]()
+
+
+class OnDevice:
+    """What the workspace check asks of a tensor, as if it lay on a device."""
+    dtype, device = torch.uint8, "cuda:0"
+
+    def __init__(self, index, contiguous=True, n=64, size=1):
+        self.get_device, self.is_contiguous = lambda: index, lambda: contiguous
+        self.numel, self.element_size, self.data_ptr, self.stride = (lambda: n), (lambda: size), (lambda: P), (lambda: (1,))
+
+
+def test_workspaces_of_other_places_are_refused():
+    like = OnDevice(0)
+    assert api._workspace("call", OnDevice(0), 64, like)[1:] == (P, 64)
+    assert api._workspace("call", OnDevice(0, size=4), 64, like)[1:] == (P, 256)  # its size in bytes
+    assert api._workspace("call", None, 0, like) == (None, None, 0)
+    for ws in (torch.empty(64, dtype=torch.uint8), OnDevice(1), OnDevice(0, contiguous=False)):
+        with pytest.raises(ValueError, match="call"):
+            api._workspace("call", ws, 64, like)
+
+
+@pytest.mark.skipif(not os.path.exists(api.LIB_PATH), reason="libhg.so not built")
+def test_unaligned_workspaces_are_refused():
+    L = api.lib()
+    ws, big = 9 * P + 8, 1 << 40
+    linear = api._pack_linear(20, 23, 31, 1, 2, 23, 31, 23)
+    glu = api._pack_glu(20, 23, 31, 1, 2, 23, 31, 23)
+    rope = api._pack_rope(10, 50, 4, 2, 16, 16, 0, 1, 1e-6, 0)
+    attn = api._pack_linattn(4096, 1, 4, 2, 16, 1, 1.0)
+    heads = [api._pack_heads(i * P, 1 << 20, 160, 16) for i in range(1, 8)]
+    X, W, b, Y, dX, dW, db = (i * P for i in range(1, 8))
+    got = [L.hg_linear_fwd(linear, X, W, b, None, Y, ws, big, None),
+           L.hg_linear_bwd(linear, X, W, b, Y, dX, dW, db, 0, ws, big, None),
+           L.hg_glu_fwd(glu, X, W, b, Y, ws, big, None),
+           L.hg_glu_bwd(glu, X, W, b, Y, dX, dW, db, 0, ws, big, None),
+           L.hg_qk_norm_rope_bwd(rope, *heads[:2], P, P, P, P, *heads[2:4], *heads[4:6], P, P, 0, ws, big, None),
+           L.hg_linattn_fwd(attn, *heads[:3], P, None, None, heads[3], None, ws, big, None),
+           L.hg_linattn_bwd(attn, *heads[:3], P, None, None, heads[3], None, *heads[4:7], None, ws, big, None)]
+    assert got == [api.HG_ERR_ARG] * 7

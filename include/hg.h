@@ -521,7 +521,9 @@ int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t
  * W [d_in, d_out] contiguous, bias [d_out] (may be NULL = 0), R may be NULL.
  * Y may be R itself (same address and ld); else Y must not overlap an input.
  * Base addresses of X, W and dY are multiples of 16 bytes; strides are in
- * elements and at least the width.  n < 2^31, widths at most 2^20.
+ * elements and at least the width.  n < 2^31, widths at most 2^20, and the product
+ * of two of n and the widths, each rounded up to a multiple of 64, below 2^35 (what is
+ * larger is HG_ERR_UNSUPPORTED where a launch would need 2^32 threads).
  *
  * Precision: bfloat16 values enter the MFMA exactly and z, act and the sum
  * with R are float32, rounded once into Y.  float32 values are taken in three
@@ -603,8 +605,8 @@ typedef struct hg_heads {
  * pairs, then the sines (hg_rope_table writes one; rot = 0: no rotation, pos
  * still is given).  A token whose position is outside [0, n_pos) gets NaN rows.
  * The outputs may be the inputs themselves (same address and strides).
- * d and rot are multiples of 8, d at most 256.  Norms, rotation and sums are
- * float32, rounded once.  Asynchronous. */
+ * d and rot are multiples of 8, d at most 256, n (heads + kv_heads) d below 2^34.
+ * Norms, rotation and sums are float32, rounded once.  Asynchronous. */
 typedef struct hg_rope_desc {
   int64_t n;          /* tokens */
   int64_t n_pos;      /* rows of the table */
@@ -615,7 +617,7 @@ typedef struct hg_rope_desc {
   int32_t reserved;
 } hg_rope_desc;
 /* Table of n_pos positions: angle = position * step * base^(-2 p / rot), formed
- * in float64 (step: the time unit of a position). */
+ * in float64 (step: the time unit of a position).  n_pos rot is below 2^33. */
 int hg_rope_table(int64_t n_pos, int32_t rot, double base, double step, float* table, void* stream);
 int hg_qk_norm_rope_fwd(const hg_rope_desc* D, const hg_heads* q, const hg_heads* k, const float* wq,
                         const float* wk, const float* table, const int32_t* pos, const hg_heads* q_out,

@@ -469,15 +469,27 @@ Bufs take_bwd(const Prob& p, Mem& m) {
 }
 
 // ---- checks -----------------------------------------------------------------------------------
-int check(const Prob& p, const char* what) {
+// A grid has fewer than 2^32 threads in x: of the tiles, and of the copies into padded
+// rows, a thread for eight values.  (Joins and column sums have fewer: the k range is
+// split only where there are few tiles.)
+bool launchable(const Tiling& t) { return t.tiles_m * t.tiles_n * (t.tile == 256 ? 512 : 256) < (int64_t)1 << 32; }
+bool launchable_pad(int64_t rows, int64_t width) { return rows * (width / 8) <= ((int64_t)1 << 32) - 256; }
+
+bool launchable(const Prob& p, bool bwd) {
+  if (p.n == 0 || (!bwd && few(p))) return true;
+  if ((!x_direct(p) && !launchable_pad(p.n, p.dp())) || (!w_direct(p) && !launchable_pad(p.d, p.colsp()))) return false;
+  if (!bwd) return launchable(t_fwd(p));
+  if (!has_z(p) && !dz_direct(p) && !launchable_pad(p.n, p.colsp())) return false;
+  return (!has_z(p) || launchable(t_z(p))) && launchable(t_dx(p)) && launchable(t_dw(p));
+}
+
+int check(const Prob& p, const char* what, bool bwd) {
   if (p.n < 0 || p.d < 1 || p.f < 1) return fail(HG_ERR_ARG, "%s: sizes n=%lld, %d -> %d", what, (long long)p.n, p.d, p.f);
   if (p.dtype != HG_DTYPE_F32 && p.dtype != HG_DTYPE_BF16) return fail(HG_ERR_ARG, "%s: dtype %d", what, p.dtype);
   if (p.act < HG_ACT_NONE || p.act > HG_ACT_GELU) return fail(HG_ERR_ARG, "%s: act %d", what, p.act);
   if (p.n >= (int64_t)1 << 31 || p.d > kMaxWidth || p.f > kMaxWidth)
     return fail(HG_ERR_UNSUPPORTED, "%s: n=%lld, %d -> %d is too large", what, (long long)p.n, p.d, p.f);
-  // the launches' block counts
-  const int64_t most = ((int64_t)1 << 31) - 1;
-  if (cdiv(p.n, 64) * cdiv(std::max(p.colsp(), p.dp()), 64) > most / 4 || p.n * (int64_t)std::max(p.colsp(), p.dp()) / 4 / 256 > most / 4)
+  if (!launchable(p, bwd))
     return fail(HG_ERR_UNSUPPORTED, "%s: n=%lld rows of %d -> %d are too many", what, (long long)p.n, p.d, p.f);
   return HG_OK;
 }
@@ -701,7 +713,7 @@ int empty_grads(const Prob& p, void* dW, float* dbias, int accumulate, hipStream
 
 int forward(const Prob& p, const char* what, const void* X, const void* W, const float* bias, const void* R, void* Y,
             void* ws, size_t ws_bytes, hipStream_t s) {
-  HG_TRY(check(p, what));
+  HG_TRY(check(p, what, false));
   HG_TRY(check_rows(p, what, p.ld_x, p.d, "X"));
   HG_TRY(check_rows(p, what, p.ld_y, p.f, "the output"));
   if (R) HG_TRY(check_rows(p, what, p.ld_r, p.f, "R"));
@@ -728,7 +740,7 @@ int forward(const Prob& p, const char* what, const void* X, const void* W, const
 
 int backward(const Prob& p, const char* what, const void* X, const void* W, const float* bias, const void* dY, void* dX,
              void* dW, float* dbias, int accumulate, void* ws, size_t ws_bytes, hipStream_t s) {
-  HG_TRY(check(p, what));
+  HG_TRY(check(p, what, true));
   if (accumulate != 0 && accumulate != 1) return fail(HG_ERR_ARG, "%s: accumulate %d", what, accumulate);
   HG_TRY(check_rows(p, what, p.ld_x, p.d, "X"));
   HG_TRY(check_rows(p, what, p.ld_y, p.f, "the upstream gradient"));
@@ -773,7 +785,7 @@ template <class D>
 size_t size_of(const D* L, bool bwd) {
   if (!L) return 0;
   const Prob p = prob_of(L);
-  if (check(p, "workspace size") != HG_OK) return 0;
+  if (check(p, "workspace size", bwd) != HG_OK) return 0;
   Sizer m;
   if (bwd) {
     take_bwd(p, m);

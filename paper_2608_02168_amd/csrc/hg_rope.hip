@@ -362,6 +362,9 @@ int check_vectors(const hg_rope_desc* D, const char* what, const float* wq, cons
   return HG_OK;
 }
 
+// A grid has fewer than 2^32 threads.
+bool launchable(int64_t groups, int lanes) { return groups <= (((int64_t)1 << 32) - kThreads) / lanes; }
+
 RopeArgs args_of(const hg_rope_desc* D, const hg_heads* q, const hg_heads* k, const float* wq, const float* wk,
                  const float* table, const int32_t* pos) {
   RopeArgs a{};
@@ -413,7 +416,8 @@ using namespace hg;
 extern "C" int hg_rope_table(int64_t n_pos, int32_t rot, double base, double step, float* table, void* stream) {
   if (n_pos < 0 || rot < 0 || rot % 2 || !(base > 0) || !std::isfinite(base) || !std::isfinite(step))
     return fail(HG_ERR_ARG, "hg_rope_table: n_pos=%lld rot=%d base=%g step=%g", (long long)n_pos, rot, base, step);
-  if (rot > kMaxD || n_pos > (int64_t)1 << 31) return fail(HG_ERR_UNSUPPORTED, "hg_rope_table: n_pos=%lld rot=%d", (long long)n_pos, rot);
+  if (rot > kMaxD || n_pos > (int64_t)1 << 31 || (rot > 0 && !launchable(n_pos, rot / 2)))
+    return fail(HG_ERR_UNSUPPORTED, "hg_rope_table: n_pos=%lld rot=%d", (long long)n_pos, rot);
   if (n_pos == 0 || rot == 0) return HG_OK;
   if (!table) return fail(HG_ERR_ARG, "hg_rope_table: null pointer");
   HG_LAUNCH("rope_table", k_rope_table, dim3((unsigned)cdiv(n_pos * (rot / 2), kThreads)), dim3(kThreads), 0,
@@ -433,6 +437,9 @@ extern "C" int hg_qk_norm_rope_fwd(const hg_rope_desc* D, const hg_heads* q, con
   if (D->n == 0) return HG_OK;
   HG_TRY(check_vectors(D, what, wq, wk, table, pos));
   RopeArgs a = args_of(D, q, k, wq, wk, table, pos);
+  if (!launchable(a.n * a.slots, lanes_of(D->d)))
+    return fail(HG_ERR_UNSUPPORTED, "%s: n=%lld tokens of %d heads are too many", what, (long long)D->n,
+                D->heads + D->kv_heads);
   a.oq = heads(q_out);
   a.ok = heads(D->kv_heads ? k_out : nullptr);
   hipStream_t s = static_cast<hipStream_t>(stream);

@@ -90,3 +90,35 @@ def test_unaligned_workspaces_are_refused():
            L.hg_linattn_fwd(attn, *heads[:3], P, None, None, heads[3], None, ws, big, None),
            L.hg_linattn_bwd(attn, *heads[:3], P, None, None, heads[3], None, *heads[4:7], None, ws, big, None)]
     assert got == [api.HG_ERR_ARG] * 7
+
+
+@pytest.mark.skipif(not os.path.exists(api.LIB_PATH), reason="libhg.so not built")
+def test_calls_of_too_many_threads_are_refused():
+    """A grid of 2^32 threads cannot be launched: refused like every size before any device work."""
+    L, big = api.lib(), 1 << 62
+    X, W, b, Y, dX, dW, db = (i << 56 for i in range(1, 8))
+
+    def linear(n, d, m, dtype=1, act=2, ld_x=None, ld_y=None):
+        return api._pack_linear(n, d, m, dtype, act, ld_x or d, ld_y or m, m), \
+            api._pack_linear(n, d, m, dtype, act, ld_x or d, ld_y or m, d)
+
+    # 2^24 tiles; X to be copied into padded rows; only the backward's tiles
+    for n, d, m, ld_x in ((1 << 30, 8, 8, 8), ((1 << 31) - 64, 17, 16, 17), (1 << 26, 513, 8, 513)):
+        fwd, bwd = linear(n, d, m, ld_x=ld_x)
+        assert L.hg_linear_fwd(fwd, X, W, b, None, Y, 1 << 48, big, None) == api.HG_ERR_UNSUPPORTED
+        assert L.hg_linear_bwd(bwd, X, W, b, Y, dX, dW, db, 0, 1 << 48, big, None) == api.HG_ERR_UNSUPPORTED
+        assert L.hg_linear_fwd_workspace_size(fwd) == L.hg_linear_bwd_workspace_size(bwd) == 0
+    # the forward's tiles are few, those of dX too many
+    _, bwd = linear(1 << 24, 1 << 14, 8)
+    assert L.hg_linear_bwd(bwd, X, W, b, Y, dX, dW, db, 0, 1 << 48, big, None) == api.HG_ERR_UNSUPPORTED
+    glu = api._pack_glu(1 << 30, 8, 8, 0, 2, 8, 8, 8)
+    assert L.hg_glu_fwd(glu, X, W, b, Y, 1 << 48, big, None) == api.HG_ERR_UNSUPPORTED
+    assert L.hg_glu_bwd(glu, X, W, b, Y, dX, dW, db, 0, 1 << 48, big, None) == api.HG_ERR_UNSUPPORTED
+    # what can be launched has a workspace still
+    fwd, bwd = linear((1 << 29) - 64, 8, 8)
+    assert L.hg_linear_bwd_workspace_size(bwd) > 0 == L.hg_linear_fwd_workspace_size(fwd)
+    rope = api._pack_rope(1 << 31, 50, 4, 4, 64, 64, 0, 1, 1e-6, 0)
+    heads = [api._pack_heads(i << 56, 0, 512, 64) for i in range(1, 5)]
+    assert L.hg_qk_norm_rope_fwd(rope, *heads[:2], P, P, P, P, *heads[2:], None) == api.HG_ERR_UNSUPPORTED
+    assert L.hg_rope_table(1 << 30, 16, 1e4, 1.0, P, None) == api.HG_ERR_UNSUPPORTED
+    assert L.hg_rope_table(1 << 30, 0, 1e4, 1.0, P, None) == api.HG_OK

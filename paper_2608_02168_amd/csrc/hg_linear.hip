@@ -291,14 +291,19 @@ int64_t part_elems(const Tiling& t, int64_t M, int64_t ld, int planes = 1) {
   return t.splits * planes > 1 ? (int64_t)t.splits * planes * M * ld : 0;
 }
 
+// More than 64 KB of LDS for a kernel: an attribute of its copy on each device, set
+// before its first launch there (a device past the 64th sets it every time).
 template <auto kern>
 int allow_lds(size_t lds) {
   if (lds > 65536) {
-    static std::atomic<bool> attr_set{false};
-    if (!attr_set.load(std::memory_order_relaxed)) {
+    static std::atomic<uint64_t> set_on{0};
+    int dev = 0;
+    HG_HIP_TRY(hipGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(set_on.load(std::memory_order_relaxed) & bit)) {
       HG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                      (int)lds));
-      attr_set.store(true, std::memory_order_relaxed);
+      set_on.fetch_or(bit, std::memory_order_relaxed);
     }
   }
   return HG_OK;

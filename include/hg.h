@@ -533,7 +533,8 @@ int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t
  * NaN in that row only.  In the backward dz = dY * act'(z) is formed from
  * float32 z; bfloat16 calls round it once (when act is not HG_ACT_NONE) as
  * operand of the two products, to 16 bits where dX or dW has fewer than 4096 values
- * and to 8 else, and dbias sums it before that. */
+ * and n d_in d_out (gated: n d 2 f) is at most 2^28, to 8 else, and dbias sums it
+ * before that. */
 typedef struct hg_linear_desc {
   int64_t n;
   int32_t d_in, d_out;

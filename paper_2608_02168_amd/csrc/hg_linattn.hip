@@ -1074,6 +1074,8 @@ extern "C" int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, cons
   if (A->batch == 0) return HG_OK;
   if (!log_decay || (!state && n_slots > 0)) return fail(HG_ERR_ARG, "%s: null pointer", what);
   if (reinterpret_cast<uintptr_t>(state) & 15) return fail(HG_ERR_ARG, "%s: the states are not 16-byte aligned", what);
+  // (blocks of the same row, and of heads that share k and v, read their inputs while another writes o)
+  if (o->p == q->p || o->p == k->p || o->p == v->p) return fail(HG_ERR_ARG, "%s: o is an input", what);
   // whole heads while there are two blocks per CU of them, else columns of a
   // head, at least 16 (64 bytes of a row of the state)
   const int64_t heads = (int64_t)A->batch * A->heads;

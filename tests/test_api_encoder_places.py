@@ -122,3 +122,13 @@ def test_calls_of_too_many_threads_are_refused():
     assert L.hg_qk_norm_rope_fwd(rope, *heads[:2], P, P, P, P, *heads[2:], None) == api.HG_ERR_UNSUPPORTED
     assert L.hg_rope_table(1 << 30, 16, 1e4, 1.0, P, None) == api.HG_ERR_UNSUPPORTED
     assert L.hg_rope_table(1 << 30, 0, 1e4, 1.0, P, None) == api.HG_OK
+
+
+@pytest.mark.skipif(not os.path.exists(api.LIB_PATH), reason="libhg.so not built")
+def test_a_step_does_not_write_its_inputs():
+    L = api.lib()
+    A = api._pack_linattn(1, 2, 4, 2, 16, 1, 1.0)
+    q, k, v = (api._pack_heads(i * P, 160, 0, 16) for i in (1, 2, 3))
+    for o in (q, k, v):
+        assert L.hg_linattn_step(A, q, k, v, 4 * P, 5 * P, None, 2, o, None) == api.HG_ERR_ARG
+        assert "o is an input" in api.last_error_detail()

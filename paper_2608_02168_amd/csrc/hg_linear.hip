@@ -727,6 +727,7 @@ int forward(const Prob& p, const char* what, const void* X, const void* W, const
   if (!aligned16(X) || !aligned16(W)) return fail(HG_ERR_ARG, "%s: X and W must be 16-byte aligned", what);
   const int64_t ny = span(p, p.n, p.f, p.ld_y);
   if (overlap(Y, ny, X, span(p, p.n, p.d, p.ld_x)) || overlap(Y, ny, W, span(p, p.d, p.cols(), p.cols())) ||
+      overlap(Y, ny, bias, 4 * (int64_t)p.cols()) ||
       (R != Y && overlap(Y, ny, R, span(p, p.n, p.f, p.ld_r))) || (R == Y && p.ld_r != p.ld_y))
     return fail(HG_ERR_ARG, "%s: the output overlaps an input", what);
   Sizer need;

@@ -132,3 +132,14 @@ def test_a_step_does_not_write_its_inputs():
     for o in (q, k, v):
         assert L.hg_linattn_step(A, q, k, v, 4 * P, 5 * P, None, 2, o, None) == api.HG_ERR_ARG
         assert "o is an input" in api.last_error_detail()
+
+
+@pytest.mark.skipif(not os.path.exists(api.LIB_PATH), reason="libhg.so not built")
+def test_a_product_does_not_write_its_bias():
+    L = api.lib()
+    X, W, Y = P, 2 * P, 4 * P
+    for at in (0, 60, 20 * 32 * 2 - 4):
+        assert L.hg_linear_fwd(api._pack_linear(20, 24, 32, 1, 0, 24, 32, 32), X, W, Y + at, None, Y, None, 0, None) == api.HG_ERR_ARG
+        assert "overlaps" in api.last_error_detail()
+    assert L.hg_glu_fwd(api._pack_glu(20, 24, 16, 1, 2, 24, 16, 24), X, W, Y - 64, Y, None, 0, None) == api.HG_ERR_ARG
+    assert "overlaps" in api.last_error_detail()

@@ -70,8 +70,8 @@ def make_plan(cfg: EncoderConfig, device="cuda") -> dict:
 
 def _split(cfg: EncoderConfig, qkv):
     """Views of the heads in a packed projection [n, d_qkv]."""
-    x = qkv.view(qkv.shape[0], -1, cfg.d_head)
     h, k = cfg.heads, cfg.kv_heads
+    x = qkv.view(qkv.shape[0], h + 2 * k, cfg.d_head)
     return x[:, :h], x[:, h:h + k], x[:, h + k:]
 
 
@@ -116,7 +116,7 @@ def backward(cfg: EncoderConfig, params: list, plan: dict, saved: dict, dz, grad
         dqkv = torch.empty_like(s["qkv"])
         dq, dk, dv = _split(cfg, dqkv)
         q4, k4, v4, do4, dq4, dk4, dv4 = (y.unflatten(0, (b, t)) for y in
-                                          (s["qr"], s["kr"], v, do.view(b * t, cfg.heads, -1), dq, dk, dv))
+                                          (s["qr"], s["kr"], v, do.view(b * t, cfg.heads, cfg.d_head), dq, dk, dv))
         api.hg_linattn_bwd(q4, k4, v4, plan["log_decay"], do4, scale=plan["scale"], lens=lens, dq=dq4, dk=dk4, dv=dv4)
         api.hg_qk_norm_rope_bwd(q, k, p["w_q"], p["w_k"], plan["table"], pos, dq, dk, dq=dq, dk=dk, dwq=w["w_q"],
                                 dwk=w["w_k"], accumulate=add)

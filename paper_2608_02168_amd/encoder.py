@@ -36,6 +36,14 @@ class EncoderConfig:
     n_pos: int = 4096       # positions (time steps) of the rotation table
     dtype: torch.dtype = torch.float32
 
+    def __post_init__(self):
+        if min(self.heads, self.kv_heads, self.f) < 1 or min(self.blocks, self.n_pos) < 0:
+            raise ValueError(f"{self}: heads and widths are at least 1")
+        if self.heads % self.kv_heads:
+            raise ValueError(f"{self}: {self.heads} heads on {self.kv_heads} key heads")
+        if self.d % self.heads or self.d_head % 8 or not 8 <= self.d_head <= 128:
+            raise ValueError(f"{self}: d is not heads of a multiple of 8 up to 128 columns")
+
     @property
     def d_head(self) -> int:
         return self.d // self.heads

@@ -294,20 +294,20 @@ __device__ __forceinline__ void parts3(f32x4 x, uint2 (&p)[3]) {
 
 template <int DP>
 struct Shape {
-  static constexpr int NB = DP / 16;          // 16-column blocks of a row
-  static constexpr int NT = 1;                 // of a wave
-  static constexpr int W = NB / NT, THREADS = 64 * W;
+  static constexpr int NB = DP / 16;        // 16-column blocks of a row, a wave each
+  static constexpr int THREADS = 64 * NB;
 };
 
 // GR heads of one sequence that share their key head, or a segment of them.
 // SUMS: only the segment's sum.  Registers for 16 waves a CU, or for 12 and 8 where
 // the states of two heads, or six waves a block, leave no use for more (two heads
 // at d = 64 spilled 28 bytes a lane at 16: 114 us for the backward of 8 x 2048
-// tokens, 98 to 105 at 12).
+// tokens, 98 to 105 at 12; float32 at d = 32 eight registers: 64 x 512 tokens, 8
+// heads on 4, 112 us, 101 at 12).
 template <class T, int DP, bool SUMS, int GR>
-__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : DP == 96 || (GR == 2 && DP == 64) ? 3 : 4) k_linattn_scan(const Walks walks) {
+__global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : DP == 96 || (GR == 2 && DP * sizeof(T) >= 128) ? 3 : 4) k_linattn_scan(const Walks walks) {
   const Walk& a = walks.w[blockIdx.z];
-  constexpr int NB = Shape<DP>::NB, NT = Shape<DP>::NT, NTHR = Shape<DP>::THREADS, C = kChunk, RB = C / 16;
+  constexpr int NB = Shape<DP>::NB, NTHR = Shape<DP>::THREADS, C = kChunk, RB = C / 16;
   typedef Tile<T, DP, true> TL;
   typedef Tile<T, DP, false> TQ;
   typedef typename Blk<T>::type B;
@@ -357,39 +357,37 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
 
   for (int i = threadIdx.x; i < GR * (C + 1); i += NTHR) pw[i / (C + 1)][i % (C + 1)] = decay(log_of(a.log_decay[h + i / (C + 1)]), i % (C + 1));
 
-  // state: rows 16 i + 4 g + v, columns 16 (wave NT + j) + c
-  f32x4 S[GR][NB][NT];
+  // state: rows 16 i + 4 g + v, columns 16 wave + c
+  f32x4 S[GR][NB];
   float* seg_at = a.seg ? a.seg + ((bh * a.segs + seg) * (NB * NB)) * 256 : nullptr;
   const int64_t seg_head = (int64_t)a.segs * (NB * NB * 256);  // from a head's states to the next one's
 #pragma unroll
   for (int r = 0; r < GR; ++r)
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+    for (int i = 0; i < NB; ++i) {
+      f32x4& x = S[r][i];
+      x = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (!SUMS) {
+        if (a.segs > 1) {
+          const float* at = seg_at + r * seg_head;
+          if (!a.seg_trans) {
+            x = *reinterpret_cast<const f32x4*>(at + (i * NB + wave) * 256 + lane * 4);
+          } else {
+            // element (r, c) of the block lies where (c, r) of the mirrored block does
 #pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        f32x4& x = S[r][i][j];
-        x = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (!SUMS) {
-          if (a.segs > 1) {
-            const float* at = seg_at + r * seg_head;
-            if (!a.seg_trans) {
-              x = *reinterpret_cast<const f32x4*>(at + (i * NB + wave * NT + j) * 256 + lane * 4);
-            } else {
-              // element (r, c) of the block lies where (c, r) of the mirrored block does
+            for (int v = 0; v < 4; ++v)
+              x[v] = at[(wave * NB + i) * 256 + ((c >> 2) * 16 + 4 * g + v) * 4 + (c & 3)];
+          }
+        } else if (a.s_in) {
+          const int col = 16 * wave + c;
 #pragma unroll
-              for (int v = 0; v < 4; ++v)
-                x[v] = at[((wave * NT + j) * NB + i) * 256 + ((c >> 2) * 16 + 4 * g + v) * 4 + (c & 3)];
-            }
-          } else if (a.s_in) {
-            const int col = 16 * (wave * NT + j) + c;
-#pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              const int row = 16 * i + 4 * g + v;
-              if (row < d && col < d) x[v] = a.s_in[(bh + r) * d * d + (a.s_trans ? col * d + row : row * d + col)];
-            }
+          for (int v = 0; v < 4; ++v) {
+            const int row = 16 * i + 4 * g + v;
+            if (row < d && col < d) x[v] = a.s_in[(bh + r) * d * d + (a.s_trans ? col * d + row : row * d + col)];
           }
         }
       }
+    }
 
   Rows<T, DP, C, NTHR> rk, rv, rq;
   rk.init(a.k.st, d, a.reverse);
@@ -406,10 +404,10 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
       if (r == 0 || !sum_o) rq.load(qp + t * a.q.st + r * q_head, a.q.st, n, d, a.reverse);
   };
   // this lane's columns of o in row c of a block of 16
-  const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave * NT + 4 * g) * osz);
+  const uint32_t o_off = SUMS ? 0 : (uint32_t)(((a.reverse ? 15 - c : c) * (int)a.o.st + 16 * wave + 4 * g) * osz);
 
-  f32x4 sum[RB][NT];  // o of the block's heads so far
-  int fill = 0;       // of lv
+  f32x4 sum[RB];  // o of the block's heads so far
+  int fill = 0;   // of lv
   if (threadIdx.x == 0) bad_v = 0;
   if (u_from < u_to) load(u_from, 0);
   for (int u0 = u_from; u0 < u_to; u0 += C) {
@@ -434,7 +432,7 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
       }
       if constexpr (!SUMS) {
         // P, its blocks shared out over the waves
-        for (int pr = wave; pr < NP; pr += Shape<DP>::W) {
+        for (int pr = wave; pr < NP; pr += NB) {
           const int r = pr >= 1 ? 1 : 0, kt = pr - r;
           f32x4 s{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -460,12 +458,10 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
           f.set(s);
           lp[pr][lane] = f;
         }
-        // q S, the chains of the rows and columns side by side
-        f32x4 o[RB][NT];
+        // q S, the chains of the rows side by side
+        f32x4 o[RB];
 #pragma unroll
-        for (int r = 0; r < RB; ++r)
-#pragma unroll
-          for (int j = 0; j < NT; ++j) o[r][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int r = 0; r < RB; ++r) o[r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NB; i += 2) {
           const bool two = i + 1 < NB;
@@ -475,31 +471,24 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
             q0[r] = TQ::row4(lq, 16 * r + c, i, g);
             q1[r] = two ? TQ::row4(lq, 16 * r + c, two ? i + 1 : i, g) : Blk<T>::zero();
           }
-          Factor<T> s0[NT], s1[NT];
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            s0[j].set(S[hr][i][j]);
-            if (two) {
-              s1[j].set(S[hr][two ? i + 1 : i][j]);
-            } else {
-              s1[j].zero();
-            }
+          Factor<T> s0, s1;
+          s0.set(S[hr][i]);
+          if (two) {
+            s1.set(S[hr][two ? i + 1 : i]);
+          } else {
+            s1.zero();
           }
 #pragma unroll
           for (int x = Factor<T>::N - 1; x >= 0; --x)
 #pragma unroll
             for (int r = 0; r < RB; ++r)
-#pragma unroll
-              for (int j = 0; j < NT; ++j)
-                o[r][j] = two ? mma32(s0[j].x[x], s1[j].x[x], q0[r], q1[r], o[r][j]) : mma16(s0[j].x[x], q0[r], o[r][j]);
+              o[r] = two ? mma32(s0.x[x], s1.x[x], q0[r], q1[r], o[r]) : mma16(s0.x[x], q0[r], o[r]);
         }
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
           const float rowp = pw[hr][16 * r + c + 1 - lead] * a.o_scale;
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) o[r][j][v] = sum_o && hr > 0 ? fmaf(o[r][j][v], rowp, sum[r][j][v]) : o[r][j][v] * rowp;
+          for (int v = 0; v < 4; ++v) o[r][v] = sum_o && hr > 0 ? fmaf(o[r][v], rowp, sum[r][v]) : o[r][v] * rowp;
         }
         __syncthreads();
         // P v.  Above the diagonal P is zero, and 0 times an infinity or a NaN is
@@ -508,21 +497,11 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
         const bool bad = bad_v == fill;
 #pragma unroll
         for (int kt = 0; kt < RB; kt += 2) {
-          B v0[NT], v1[NT];
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            v0[j] = TL::col4(lv, kt, wave * NT + j, c, g);
-            v1[j] = TL::col4(lv, kt + 1, wave * NT + j, c, g);
-          }
-          B d0[NT], d1[NT];
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            d0[j] = v0[j];
-            d1[j] = v1[j];
-            if (bad) {
-              d0[j] = finite(v0[j]);
-              d1[j] = finite(v1[j]);
-            }
+          const B v0 = TL::col4(lv, kt, wave, c, g), v1 = TL::col4(lv, kt + 1, wave, c, g);
+          B d0 = v0, d1 = v1;
+          if (bad) {
+            d0 = finite(v0);
+            d1 = finite(v1);
           }
 #pragma unroll
           for (int r = kt; r < RB; ++r) {
@@ -531,9 +510,7 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
             if (r > kt) p1 = lp[r * (r + 1) / 2 + kt + 1][lane];
 #pragma unroll
             for (int x = Factor<T>::N - 1; x >= 0; --x)
-#pragma unroll
-              for (int j = 0; j < NT; ++j)
-                o[r][j] = r > kt ? mma32(v0[j], d1[j], p0.x[x], p1.x[x], o[r][j]) : mma16(d0[j], p0.x[x], o[r][j]);
+              o[r] = r > kt ? mma32(v0, d1, p0.x[x], p1.x[x], o[r]) : mma16(d0, p0.x[x], o[r]);
           }
         }
         if (bad) {
@@ -542,33 +519,27 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
             for (int r = 0; r < RB; ++r) {
               const float p = element<T>(lp[r * (r + 3) / 2][16 * (y >> 2) + c], y & 3);
 #pragma unroll
-              for (int j = 0; j < NT; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                  const float x = Elt<T>::get(lv + (16 * r + y) * TL::LD + 16 * (wave * NT + j) + 4 * g + v);
-                  if (!(fabsf(x) < INFINITY)) o[r][j][v] = fmaf(p, x, o[r][j][v]);
-                }
+              for (int v = 0; v < 4; ++v) {
+                const float x = Elt<T>::get(lv + (16 * r + y) * TL::LD + 16 * wave + 4 * g + v);
+                if (!(fabsf(x) < INFINITY)) o[r][v] = fmaf(p, x, o[r][v]);
+              }
             }
         }
         if (sum_o && hr + 1 < GR) {
 #pragma unroll
-          for (int r = 0; r < RB; ++r)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) sum[r][j] = o[r][j];
+          for (int r = 0; r < RB; ++r) sum[r] = o[r];
         } else {
 #pragma unroll
           for (int r = 0; r < RB; ++r) {
             const int64_t t = a.reverse ? L - 1 - u0 - 16 * r - 15 : u0 + 16 * r;  // token of row 0, or of row 15
             char* p = op + (t * a.o.st + (sum_o ? 0 : hr * a.o.sh)) * osz + o_off;
-#pragma unroll
-            for (int j = 0; j < NT; ++j)
-              if (16 * (wave * NT + j) + 4 * g < d && 16 * r + c < n) {
-                if (osz == 4) {
-                  *reinterpret_cast<f32x4*>(p + 64 * j) = o[r][j];
-                } else {
-                  *reinterpret_cast<uint2*>(p + 32 * j) = Blk<bf16_t>::of(o[r][j]);
-                }
+            if (16 * wave + 4 * g < d && 16 * r + c < n) {
+              if (osz == 4) {
+                *reinterpret_cast<f32x4*>(p) = o[r];
+              } else {
+                *reinterpret_cast<uint2*>(p) = Blk<bf16_t>::of(o[r]);
               }
+            }
           }
         }
       }
@@ -578,31 +549,21 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) S[hr][i][j][v] *= dn;
+        for (int v = 0; v < 4; ++v) S[hr][i][v] *= dn;
 #pragma unroll
       for (int tb = 0; tb < RB; tb += 2) {
         // w v of this wave's columns
-        f32x4 w0[NT], w1[NT];
+        f32x4 w0 = wide(TL::col4(lv, tb, wave, c, g)), w1 = wide(TL::col4(lv, tb + 1, wave, c, g));
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          w0[j] = wide(TL::col4(lv, tb, wave * NT + j, c, g));
-          w1[j] = wide(TL::col4(lv, tb + 1, wave * NT + j, c, g));
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int x = n - 1 + lead - 16 * tb - 4 * g - v;  // (rows past the chunk's end are zero)
-            w0[j][v] *= pw[hr][x > 0 ? x : 0] * a.kv_scale;
-            w1[j][v] *= pw[hr][x > 16 ? x - 16 : 0] * a.kv_scale;
-          }
+        for (int v = 0; v < 4; ++v) {
+          const int x = n - 1 + lead - 16 * tb - 4 * g - v;  // (rows past the chunk's end are zero)
+          w0[v] *= pw[hr][x > 0 ? x : 0] * a.kv_scale;
+          w1[v] *= pw[hr][x > 16 ? x - 16 : 0] * a.kv_scale;
         }
-        uint2 p0[NT][3], p1[NT][3];
+        uint2 p0[3], p1[3];
         if constexpr (!kF32) {
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            parts3(w0[j], p0[j]);
-            parts3(w1[j], p1[j]);
-          }
+          parts3(w0, p0);
+          parts3(w1, p1);
         }
         // chains side by side, at most U blocks' operands at a time
         constexpr int U = NB < 4 ? NB : kF32 ? 2 : 4;
@@ -617,16 +578,14 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
 #pragma unroll
           for (int x = kF32 ? 0 : 2; x >= 0; --x)
 #pragma unroll
-            for (int i = 0; i < U && i0 + i < NB; ++i)
-#pragma unroll
-              for (int j = 0; j < NT; ++j) {
-                f32x4& s = S[hr][i0 + i][j];
-                if constexpr (kF32) {
-                  s = mma32(k0[i], k1[i], w0[j], w1[j], s);
-                } else {
-                  s = mma32(k0[i], k1[i], p0[j][x], p1[j][x], s);
-                }
+            for (int i = 0; i < U && i0 + i < NB; ++i) {
+              f32x4& s = S[hr][i0 + i];
+              if constexpr (kF32) {
+                s = mma32(k0[i], k1[i], w0, w1, s);
+              } else {
+                s = mma32(k0[i], k1[i], p0[x], p1[x], s);
               }
+            }
         }
       }
     }
@@ -637,21 +596,17 @@ __global__ void __launch_bounds__(Shape<DP>::THREADS, GR == 2 && DP > 64 ? 2 : D
     if constexpr (SUMS) {
 #pragma unroll
       for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          *reinterpret_cast<f32x4*>(seg_at + r * seg_head + (i * NB + wave * NT + j) * 256 + lane * 4) = S[r][i][j];
+        *reinterpret_cast<f32x4*>(seg_at + r * seg_head + (i * NB + wave) * 256 + lane * 4) = S[r][i];
     } else if (a.segs == 1 && a.s_out) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+      for (int i = 0; i < NB; ++i) {
+        const int col = 16 * wave + c;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const int col = 16 * (wave * NT + j) + c;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int row = 16 * i + 4 * g + v;
-            if (row < d && col < d) a.s_out[(bh + r) * d * d + (a.s_trans ? col * d + row : row * d + col)] = S[r][i][j][v];
-          }
+        for (int v = 0; v < 4; ++v) {
+          const int row = 16 * i + 4 * g + v;
+          if (row < d && col < d) a.s_out[(bh + r) * d * d + (a.s_trans ? col * d + row : row * d + col)] = S[r][i][v];
         }
+      }
     }
   }
 }

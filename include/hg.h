@@ -530,7 +530,7 @@ int hg_home_gather(int64_t m, int32_t d, int32_t dtype, int32_t K, const int32_t
  * bfloat16 parts with the six part products of order at most two (the weight
  * gradients' rule stated at the top, here for all three products), each product
  * term within about 2^-22 of itself; a row that holds an infinity or NaN gives
- * NaN in that row only.  In the backward dz = dY * act'(z) is formed from
+ * values that are not finite (NaN where it was split) in that row only.  In the backward dz = dY * act'(z) is formed from
  * float32 z; bfloat16 calls round it once (when act is not HG_ACT_NONE) as
  * operand of the two products, to 16 bits where dX or dW has fewer than 4096 values
  * and n d_in d_out (gated: n d 2 f) is at most 2^28, to 8 else, and dbias sums it
@@ -604,7 +604,8 @@ typedef struct hg_heads {
  * kv_heads = 0: queries alone); wq, wk float32 [d] (NULL = 1), 16-byte aligned;
  * pos int32 [n]; table float32 [n_pos, rot], the cosines of a position's rot / 2
  * pairs, then the sines (hg_rope_table writes one; rot = 0: no rotation, pos
- * still is given).  A token whose position is outside [0, n_pos) gets NaN rows.
+ * still is given).  A token whose position is outside [0, n_pos) gets NaN rows, and
+ * in the backward makes dwq and dwk NaN: padding takes any position inside.
  * The outputs may be the inputs themselves (same address and strides).
  * d and rot are multiples of 8, d at most 256, n (heads + kv_heads) d below 2^34.
  * Norms, rotation and sums are float32, rounded once.  Asynchronous. */

@@ -25,7 +25,7 @@
 //           touches rows 0-3 and 8-11 of one granule.
 //
 // Bound by the MFMA where k is long: the backward of the gated product of 8192
-// rows, 2048 to 2 x 8192, runs its three products at 1.11 PFLOP/s (1486 us); large
+// rows, 2048 to 2 x 8192, runs its three products at 1.10 PFLOP/s (1500 us); large
 // products of the library reach 1.24 to 1.35 on this card.  With less than some
 // hundred k the epilogue's rows bound it.
 //
@@ -768,8 +768,8 @@ struct GTile32 {
         x[q] = left > 0 ? *reinterpret_cast<const f32x4*>(p) : f32x4{0.f, 0.f, 0.f, 0.f};
       } else {
         // a load of 16 bytes needs 4-byte alignment only; all are issued before the
-        // groups at an edge are looked at (gated, 1777 rows, 200 to 2 x 517: 13.0 us,
-        // 15.8 with single floats)
+        // groups at an edge are looked at (gated, 1777 rows, 200 to 2 x 517: 12.4 us,
+        // 2.8 more with single floats)
         __builtin_memcpy(&x[q], left >= 4 ? p : g_zeros, 16);
       }
     }

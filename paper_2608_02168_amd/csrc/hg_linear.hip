@@ -254,15 +254,16 @@ struct Tiling {
 
 // Tiles of 256 x 256 where they fill most of the chip, have at least 512 k for
 // their long epilogue and count at most an eighth more padding than 128 x 128
-// (40000 rows, 128 to 384 columns: backward 66 us, 90 without the last two
-// conditions; 30000 rows, 256 to 1024: 39 us, 40).  Tiles of 128 x 128 where they
-// fill half the chip and count less than half more padding than 64 x 64 (60000
-// rows, 304 to 64 columns: 10 us, 14 with tiles of 128; backward 55, 62).  Up to
-// `short_k` values of k a bfloat16 tile is mostly epilogue, and 64 x 64, of which
-// twice as many waves fit a CU, are faster: 256 for the gradient of z, whose
-// epilogue reads and writes (20000 rows, 160 to 520: backward 64 us, 72; gated,
-// 200 to 600: 94, 98), 128 without that (40000 rows, 96 to 256: 12.7 us, 15.1),
-// none for the gated product (30000 rows, 80 to 100: 12.7 us, 15.8 with 64).  The k
+// (SiLU, 40000 rows, 128 to 384 columns: backward 60 us, 91 without the last two
+// conditions; 30000 rows, 256 to 1024: backward 123 us, 138 without the one on k,
+// forward 41, 42; the gated forward of 256 to 2 x 512 loses by it, 34 us, 32).  Tiles of
+// 128 x 128 where they fill half the chip and count less than half more padding than
+// 64 x 64 (60000 rows, 304 to 64 columns: 11.3 us, 13.5 with tiles of 128; backward
+// with SiLU 50, 58).  Up to `short_k` values of k a bfloat16 tile is mostly epilogue,
+// and 64 x 64, of which twice as many waves fit a CU, are faster: 256 for the gradient of z, whose
+// epilogue reads and writes (20000 rows, 160 to 520: backward 61 us, 73; gated,
+// 200 to 600: 94, 101), 128 without that (40000 rows, 96 to 256: 12.1 us, 14.2),
+// none for the gated product (30000 rows, 80 to 100: 13.6 us, 15.8 with 64).  The k
 // range is split over blocks while the tiles do not fill the chip (never where
 // column sums are formed on the way).
 Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32, int64_t short_k) {
@@ -427,7 +428,14 @@ int planes(const Prob& p) {
 bool dz_direct(const Prob& p) { return !has_z(p) && (p.f32() || direct(p.f, p.ld_y)); }
 
 // Narrow float32 rows whose backward is one pass: groups of four aligned, and
-// several tiles for every block (200003 rows of 128: 142 us, 198 by tiles).
+// several tiles for every block.  With SiLU in us, and by tiles:
+//            16384 rows          200003 rows
+//   128 -> 128    34 (48)            134 (202)
+//    64 -> 64     22 (29)             75 (93)
+//     4 -> 100    22 (34)             86 (107)
+//    16 -> 16     21 (26)             67 (60)
+// (the planes in LDS are 128 wide whatever the widths are: up to 32 wide very many rows
+// lose a tenth, and 65536 are even).
 bool narrow(const Prob& p) {
   return p.f32() && !p.gated && p.d <= kNarrow && p.f <= kNarrow && p.n >= 16384 && p.d % 4 == 0 && p.f % 4 == 0 &&
          p.ld_x % 4 == 0 && p.ld_y % 4 == 0 && p.ld_r % 4 == 0;

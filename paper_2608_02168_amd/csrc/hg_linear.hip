@@ -260,9 +260,9 @@ struct Tiling {
 // 128 x 128 where they fill half the chip and count less than half more padding than
 // 64 x 64 (60000 rows, 304 to 64 columns: 11.3 us, 13.5 with tiles of 128; backward
 // with SiLU 50, 58).  Up to `short_k` values of k a bfloat16 tile is mostly epilogue,
-// and 64 x 64, of which twice as many waves fit a CU, are faster: 256 for the gradient of z, whose
-// epilogue reads and writes (20000 rows, 160 to 520: backward 61 us, 73; gated,
-// 200 to 600: 94, 101), 128 without that (40000 rows, 96 to 256: 12.1 us, 14.2),
+// and 64 x 64, of which twice as many waves fit a CU, are faster: 256 for the gradient
+// of z, whose epilogue reads and writes (20000 rows, 160 to 520: backward 61 us, 73;
+// gated, 200 to 600: 94, 101), 128 without that (40000 rows, 96 to 256: 12.1 us, 14.2),
 // none for the gated product (30000 rows, 80 to 100: 13.6 us, 15.8 with 64).  The k
 // range is split over blocks while the tiles do not fill the chip (never where
 // column sums are formed on the way).

@@ -9,9 +9,9 @@ the sums of dz over the rows, and dX is dz W^T.
 
 Bounds.  SiLU is z s(z): the exponential, 1 + e, the reciprocal and the product
 are each off by at most 2^-22 relative, 2^-20 together; where s falls below the
-smallest normal number 2^-126 it may be zero.  GELU is z Phi(z), with
-Phi formed to 2^-22 (the last test holds negative z to their own size).  bfloat16 results add one rounding: 8 bits, 2^-8 of
-a value just above a power of two."""
+smallest normal number 2^-126 it may be zero.  GELU is z Phi(z), with Phi formed
+to 2^-22 (the last test holds negative z to their own size).  bfloat16 results add
+one rounding: 8 bits, 2^-8 of a value just above a power of two."""
 import math
 
 import numpy as np

@@ -686,6 +686,125 @@ int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, const hg_heads*
                     const float* log_decay, float* states, const int32_t* slots, int64_t n_slots,
                     const hg_heads* o, void* stream);
 
+/* ---- recurrent block and its training ---------------------------------------
+ * What a block of the sequence encoder has in place of attention, and the update
+ * of its matrices:
+ *   [x r i] = hg_linear(rows),  h = hg_recur(x, r, i),  y = hg_group_norm(h),
+ *   rows' = rows + hg_linear(y);   W = hg_muon_step(W, dW)
+ * Rows of these operators need no alignment but their values' own: an element
+ * (sequence b, token t, channel c) lies at p[b * batch + t * token + c] of an
+ * hg_heads whose head stride is not used.  Strides are at least 0 and below 2^40,
+ * those of outputs keep the rows apart.  Outputs must not overlap inputs or each
+ * other; views of one packed buffer may interleave.  Workspaces are 16-byte
+ * aligned.  Asynchronous and deterministic.
+ *
+ * Gated linear recurrence: the GRU of E13 without its products with the state,
+ * so that a history is a scan.  Per channel c with l_c = -rate softplus(decay[c]),
+ * token by token
+ *   a_t = exp(l_c sigmoid(r_t)),   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t
+ * width is at least 4.  h_{-1} = state (zero if NULL), state_out = h after the last token (may be NULL):
+ * float32 [batch, width], contiguous; decay float32 [width].  lens (may be NULL):
+ * int32 [batch] on the device, tokens of each sequence, taken into [0, t]; rows of
+ * h (and of the gradients) past it are written as zero and those of the inputs are
+ * not read.  All arithmetic is float32 (1 - a^2 by a series where a is near 1),
+ * each written row rounded once.  A value that is not finite stays in its
+ * sequence's channel, and there in the tokens that the formulas let it reach. */
+typedef struct hg_recur_desc {
+  int64_t t;          /* tokens of a sequence */
+  int32_t batch, width;
+  int32_t dtype;      /* of x, r, i, h and their gradients */
+  float rate;         /* > 0, finite */
+} hg_recur_desc;
+size_t hg_recur_fwd_workspace_size(const hg_recur_desc* A);
+size_t hg_recur_bwd_workspace_size(const hg_recur_desc* A);
+int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_heads* r, const hg_heads* i, const float* decay,
+                 const int32_t* lens, const float* state, const hg_heads* h, float* state_out, void* ws,
+                 size_t ws_bytes, void* stream);
+/* Backward for dh = dL/dh and dstate_out = dL/dstate_out (zero if NULL), with h
+ * as the forward wrote it.  With g_t the gradient of h_t, q_t = sqrt(1 - a_t^2),
+ *   g_t = dh_t + a_{t+1} g_{t+1}  (plus dstate_out at the last token),
+ *   dx_t = g_t q_t sigmoid(i_t),  di_t = g_t q_t x_t sigmoid'(i_t),
+ *   dlog_t = g_t (a_t h_{t-1} - sigmoid(i_t) x_t a_t^2 / q_t),
+ *   dr_t = dlog_t l_c sigmoid'(r_t),  ddecay[c] = -rate softplus'(decay[c]) sum dlog_t sigmoid(r_t),
+ *   dstate = a_0 g_0
+ * (dr and ddecay's term are 0, their limit, where l_c sigmoid(r_t) = 0).  dx, dr, di
+ * and dstate [batch, width] (may be NULL) are OVERWRITTEN; ddecay [width] (may be
+ * NULL) is OVERWRITTEN when accumulate = 0 and added into when accumulate = 1. */
+int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_heads* r, const hg_heads* i, const float* decay,
+                 const int32_t* lens, const float* state, const hg_heads* h, const hg_heads* dh,
+                 const float* dstate_out, const hg_heads* dx, const hg_heads* dr, const hg_heads* di, float* ddecay,
+                 float* dstate, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+/* One token for each of `batch` rows (A->t = 1; the token strides are not used):
+ * the state of row b is states[slots[b]] of n_slots states [width] (slots NULL: b),
+ * UPDATED IN PLACE; the slots of a call are distinct.  A row whose slot is outside
+ * [0, n_slots) gives a zero row of h and changes nothing. */
+int hg_recur_step(const hg_recur_desc* A, const hg_heads* x, const hg_heads* r, const hg_heads* i, const float* decay,
+                  float* states, const int32_t* slots, int64_t n_slots, const hg_heads* h, void* stream);
+
+/* Group norm with an activation over rows of channels.  The width is cut into
+ * `groups` groups of adjacent channels; per sequence b and group, over its lens[b]
+ * tokens (all t if lens is NULL; taken into [0, t]) and its channels,
+ *   z = w (x - mean) / sqrt(var + eps) + b,   y = act(z)
+ * with var the mean of (x - mean)^2.  t = 1 normalises every row by itself.
+ * x, y: hg_heads; w, b float32 [width] (NULL = 1, 0).  Rows of y past lens[b] are
+ * written as zero and those of x are not read.  stats (may be NULL) float32
+ * [batch, groups, 2]: mean and 1 / sqrt(var + eps), zeros for an empty sequence.
+ * A group has up to 1024 channels, 4096 where they are a multiple of 4, 8192 in
+ * bfloat16 where they are one of 8.  Sums are float32, squares are taken about the
+ * mean, parts of a long sequence are joined in float64; y is rounded once. */
+typedef struct hg_group_norm_desc {
+  int64_t t;          /* tokens of a sequence */
+  int32_t batch, width;
+  int32_t groups;     /* divides width */
+  int32_t dtype;      /* of x, y and their gradients */
+  int32_t act;        /* HG_ACT_* */
+  float eps;          /* > 0, finite */
+} hg_group_norm_desc;
+size_t hg_group_norm_fwd_workspace_size(const hg_group_norm_desc* A);
+size_t hg_group_norm_bwd_workspace_size(const hg_group_norm_desc* A);
+int hg_group_norm_fwd(const hg_group_norm_desc* A, const hg_heads* x, const float* w, const float* b,
+                      const int32_t* lens, const hg_heads* y, float* stats, void* ws, size_t ws_bytes, void* stream);
+/* Backward for dy = dL/dy with the forward's stats: with u = (x - mean) rstd,
+ * dz = dy act'(z), and means over the tokens and channels of a group,
+ *   dx = rstd (w dz - mean(w dz) - u mean(w dz u)),   dw = sum dz u,   db = sum dz
+ * dx is OVERWRITTEN; dw and db [width] (each may be NULL) are OVERWRITTEN when
+ * accumulate = 0 and added into when accumulate = 1. */
+int hg_group_norm_bwd(const hg_group_norm_desc* A, const hg_heads* x, const float* w, const float* b,
+                      const int32_t* lens, const float* stats, const hg_heads* dy, const hg_heads* dx, float* dw,
+                      float* db, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* One update of `count` matrices of the same shape along the orthogonalised
+ * momentum, in place.  Per matrix W with gradient G and momentum M:
+ *   M = mu M + G,   U = G + mu M (nesterov) or M,   X = U / max(|U|, eps)
+ * with |U| the root of the sum of squares, then `steps` times, with the smaller
+ * Gram matrix A (X X^T; X^T X where rows > cols, and the factor on the right),
+ *   X = 3.4445 X + (-4.7750 A + 2.0315 A A) X
+ * which brings every singular value of X near 1, and
+ *   W = (1 - lr weight_decay) W - lr scale X
+ * W and G [count, rows, cols] in dtype, M float32, contiguous; W, G and M do not
+ * overlap.  M = 0 before the first update.
+ * Precision: |U| is summed in float64 and every product in float32.  float32
+ * matrices enter the products as two fp16 parts of each value, three part
+ * products (the row transforms' rule stated at the top, with one scale for the
+ * whole of X, whose entries are at most 1.21): float32 accuracy.  bfloat16 matrices
+ * enter as the fp16 high part alone (X, A and B are rounded to 11 bits a step: X is
+ * off by some 2^-9 of its norm, up to 2^-7 where noise lies far below a gradient's
+ * strong directions).  A matrix whose U holds a value
+ * that is not finite becomes NaN as a whole; the others of the call do not.
+ * rows and cols are at most 2^15, count rows cols is below 2^32 and count times the
+ * 64 x 64 tiles of a matrix below 2^22. */
+typedef struct hg_muon_desc {
+  int32_t count, rows, cols;
+  int32_t dtype;      /* of W and G */
+  int32_t steps;      /* 0 .. 32; 0: along U / max(|U|, eps) */
+  int32_t nesterov;   /* 0 or 1 */
+  float lr, mu, weight_decay, scale;
+  float eps;          /* > 0 */
+  int32_t reserved;
+} hg_muon_desc;
+size_t hg_muon_workspace_size(const hg_muon_desc* A);
+int hg_muon_step(const hg_muon_desc* A, void* W, const void* G, float* M, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- diagnostics ------------------------------------------------------- */
 const char* hg_status_string(int status);
 /* Thread-local description of the last error (host memory, valid until the

@@ -32,6 +32,9 @@ reordering beyond what the definition states:
 * ``kway``    -- K overlapping subgraphs of one graph, MeanAgg of their
   embeddings, and their joint step with the alignment to the home copies
   (Algorithm 1 on K workers).
+* ``encoder``, ``recurrent`` -- the operators of the sequence encoder over node
+  histories and of its recurrent block, forward and backward, and the update of
+  matrices along their orthogonalised momentum.
 * ``splitmix`` -- the SplitMix64 mixer used as the seeded tie-break of the
   budgeted sampling.
 

@@ -52,6 +52,9 @@ EXPORTS = [
     "hg_rope_table", "hg_qk_norm_rope_fwd", "hg_qk_norm_rope_bwd_workspace_size", "hg_qk_norm_rope_bwd",
     "hg_linattn_fwd_workspace_size", "hg_linattn_bwd_workspace_size", "hg_linattn_fwd", "hg_linattn_bwd",
     "hg_linattn_step",
+    "hg_recur_fwd_workspace_size", "hg_recur_bwd_workspace_size", "hg_recur_fwd", "hg_recur_bwd", "hg_recur_step",
+    "hg_group_norm_fwd_workspace_size", "hg_group_norm_bwd_workspace_size", "hg_group_norm_fwd", "hg_group_norm_bwd",
+    "hg_muon_workspace_size", "hg_muon_step",
     "hg_status_string", "hg_last_error_detail", "hg_timing_enable", "hg_timing_collect",
 ]
 
@@ -140,6 +143,22 @@ class LinattnDesc(C.Structure):
                 ("d", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
 
 
+class RecurDesc(C.Structure):
+    _fields_ = [("t", C.c_int64), ("batch", C.c_int32), ("width", C.c_int32), ("dtype", C.c_int32),
+                ("rate", C.c_float)]
+
+
+class GroupNormDesc(C.Structure):
+    _fields_ = [("t", C.c_int64), ("batch", C.c_int32), ("width", C.c_int32), ("groups", C.c_int32),
+                ("dtype", C.c_int32), ("act", C.c_int32), ("eps", C.c_float)]
+
+
+class MuonDesc(C.Structure):
+    _fields_ = [("count", C.c_int32), ("rows", C.c_int32), ("cols", C.c_int32), ("dtype", C.c_int32),
+                ("steps", C.c_int32), ("nesterov", C.c_int32), ("lr", C.c_float), ("mu", C.c_float),
+                ("weight_decay", C.c_float), ("scale", C.c_float), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -201,6 +220,17 @@ def lib() -> C.CDLL:
         "hg_linattn_fwd": (C.c_int, [vp] * 10 + [sz, vp]),
         "hg_linattn_bwd": (C.c_int, [vp] * 14 + [sz, vp]),
         "hg_linattn_step": (C.c_int, [vp] * 7 + [i64, vp, vp]),
+        "hg_recur_fwd_workspace_size": (sz, [vp]),
+        "hg_recur_bwd_workspace_size": (sz, [vp]),
+        "hg_recur_fwd": (C.c_int, [vp] * 10 + [sz, vp]),
+        "hg_recur_bwd": (C.c_int, [vp] * 15 + [i32, vp, sz, vp]),
+        "hg_recur_step": (C.c_int, [vp] * 7 + [i64, vp, vp]),
+        "hg_group_norm_fwd_workspace_size": (sz, [vp]),
+        "hg_group_norm_bwd_workspace_size": (sz, [vp]),
+        "hg_group_norm_fwd": (C.c_int, [vp] * 8 + [sz, vp]),
+        "hg_group_norm_bwd": (C.c_int, [vp] * 10 + [i32, vp, sz, vp]),
+        "hg_muon_workspace_size": (sz, [vp]),
+        "hg_muon_step": (C.c_int, [vp] * 5 + [sz, vp]),
         "hg_status_string": (C.c_char_p, [C.c_int]),
         "hg_last_error_detail": (C.c_char_p, []),
         "hg_timing_enable": (C.c_int, [C.c_int]),
@@ -672,13 +702,17 @@ def hg_align_loss_fwd_bwd_noalloc(H, overlap, H_ref, dH, loss3, w=None, lambda_n
 # ---- sequence encoder -------------------------------------------------------
 # These calls are made for single tokens too, so their marshalling is kept
 # short: descriptors are packed bytes (the layouts of LinearDesc, GluDesc,
-# RopeDesc, LinattnDesc and Heads), devices are compared by index.
+# RopeDesc, LinattnDesc, RecurDesc, GroupNormDesc, MuonDesc and Heads), devices
+# are compared by index.
 
 _pack_linear = struct.Struct("@qiiiiqqq").pack
 _pack_glu = struct.Struct("@qiiiiqqq").pack
 _pack_rope = struct.Struct("@qqiiiiiifi").pack
 _pack_linattn = struct.Struct("@qiiiiif").pack
 _pack_heads = struct.Struct("@Pqqq").pack
+_pack_recur = struct.Struct("@qiiif").pack
+_pack_group_norm = struct.Struct("@qiiiiif").pack
+_pack_muon = struct.Struct("@iiiiiifffffi").pack
 _DTYPES = {torch.float32: HG_DTYPE_F32, torch.bfloat16: HG_DTYPE_BF16}
 
 
@@ -1103,6 +1137,222 @@ def hg_linattn_step(q, k, v, log_decay, states, slots=None, scale: float = 1.0, 
     if st:
         _check(st, where)
     return o
+
+
+# ---- recurrent block and its training -----------------------------------------
+
+def _channels(where: str, name: str, t, shape) -> bytes:
+    """hg_heads of [batch, tokens, width] rows, or of [n, width] ones (a token
+    each).  The stride of a dimension with one entry is never walked."""
+    s = t.stride()
+    if t.shape != shape or (s[-1] != 1 and shape[-1] > 1 and t.numel()):
+        raise ValueError(f"{where}: expected {name} {tuple(shape)} with unit column stride, got {tuple(t.shape)} strides {s}")
+    if len(s) == 2:
+        return _pack_heads(t.data_ptr(), s[0] if shape[0] > 1 else 0, 0, 0)
+    return _pack_heads(t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, 0)
+
+
+def hg_recur_fwd_workspace_size(batch: int, t: int, width: int, dtype=torch.float32) -> int:
+    return int(lib().hg_recur_fwd_workspace_size(_pack_recur(t, batch, width, _DTYPES[dtype], 1.0)))
+
+
+def hg_recur_bwd_workspace_size(batch: int, t: int, width: int, dtype=torch.float32) -> int:
+    return int(lib().hg_recur_bwd_workspace_size(_pack_recur(t, batch, width, _DTYPES[dtype], 1.0)))
+
+
+def hg_recur_fwd(x, r, i, decay, rate: float = 8.0, lens=None, state=None, h=None, state_out=None,
+                 want_state: bool = False, ws=None, stream=None):
+    """Gated linear recurrence: x and its gates r and i [b, t, width] (views of a
+    packed projection are used where they lie), decay float32 [width], lens int32
+    [b] or None, state float32 [b, width] or None.  Returns (h, state_out);
+    state_out is None unless given or wanted."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_recur_fwd(x, r, i, decay, rate, lens, state, h, state_out, want_state, ws)
+    where = "hg_recur_fwd"
+    L = lib()
+    xs = x.shape
+    b, t, w = xs
+    if state_out is None and want_state:
+        state_out = torch.empty((b, w), dtype=torch.float32, device=x.device)
+    if h is None:
+        h = torch.empty(xs, dtype=x.dtype, device=x.device)
+    _same(where, x, r, i, h)
+    desc = _pack_recur(t, b, w, _float_code(where, x), rate)
+    ws, wp, wn = _workspace(where, ws, L.hg_recur_fwd_workspace_size(desc), x)
+    st = L.hg_recur_fwd(desc, _channels(where, "x", x, xs), _channels(where, "r", r, xs), _channels(where, "i", i, xs),
+                        _vector(where, decay, w, x), _vector(where, lens, b, x, torch.int32),
+                        _state(where, state, (b, w), x), _channels(where, "h", h, xs),
+                        _state(where, state_out, (b, w), x), wp, wn, _raw_stream(x))
+    if st:
+        _check(st, where)
+    return h, state_out
+
+
+def hg_recur_bwd(x, r, i, decay, h, dh, rate: float = 8.0, lens=None, state=None, dstate_out=None, dx=None, dr=None,
+                 di=None, ddecay=None, dstate=None, accumulate: bool = False, ws=None, stream=None):
+    """Returns (dx, dr, di, ddecay, dstate) of hg_recur_fwd, whose output h was,
+    for dh = dL/dh and dstate_out = dL/dstate_out (or None); ddecay is added into
+    the given buffer when accumulate; dstate is None unless a state or a buffer
+    is given."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_recur_bwd(x, r, i, decay, h, dh, rate, lens, state, dstate_out, dx, dr, di, ddecay, dstate,
+                                accumulate, ws)
+    where = "hg_recur_bwd"
+    L = lib()
+    xs = x.shape
+    b, t, w = xs
+    if accumulate and ddecay is None:
+        raise ValueError(f"{where}: accumulate needs the buffer to add into")
+    if dstate is None and state is not None:
+        dstate = torch.empty((b, w), dtype=torch.float32, device=x.device)
+    dx, dr, di = (torch.empty(xs, dtype=x.dtype, device=x.device) if g is None else g for g in (dx, dr, di))
+    if ddecay is None:
+        ddecay = torch.empty_like(decay)
+    _same(where, x, r, i, h, dh, dx, dr, di)
+    desc = _pack_recur(t, b, w, _float_code(where, x), rate)
+    ws, wp, wn = _workspace(where, ws, L.hg_recur_bwd_workspace_size(desc), x)
+    ch = [_channels(where, n, v, xs) for n, v in (("x", x), ("r", r), ("i", i), ("h", h), ("dh", dh), ("dx", dx),
+                                                  ("dr", dr), ("di", di))]
+    st = L.hg_recur_bwd(desc, *ch[:3], _vector(where, decay, w, x), _vector(where, lens, b, x, torch.int32),
+                        _state(where, state, (b, w), x), *ch[3:5], _state(where, dstate_out, (b, w), x), *ch[5:],
+                        _vector(where, ddecay, w, x), _state(where, dstate, (b, w), x), 1 if accumulate else 0, wp, wn,
+                        _raw_stream(x))
+    if st:
+        _check(st, where)
+    return dx, dr, di, ddecay, dstate
+
+
+def hg_recur_step(x, r, i, decay, states, slots=None, rate: float = 8.0, h=None, stream=None):
+    """One token for each row: x, r, i [b, width], states float32 [n, width]
+    updated in place, slots int32 [b] (None: row b has state b; a slot outside
+    the states: an idle row).  Returns h."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_recur_step(x, r, i, decay, states, slots, rate, h)
+    where = "hg_recur_step"
+    xs = x.shape
+    b, w = xs
+    if h is None:
+        h = torch.empty(xs, dtype=x.dtype, device=x.device)
+    _same(where, x, r, i, h)
+    n = states.shape[0]
+    st = lib().hg_recur_step(_pack_recur(1, b, w, _float_code(where, x), rate), _channels(where, "x", x, xs),
+                             _channels(where, "r", r, xs), _channels(where, "i", i, xs), _vector(where, decay, w, x),
+                             _state(where, states, (n, w), x), _vector(where, slots, b, x, torch.int32), n,
+                             _channels(where, "h", h, xs), _raw_stream(x))
+    if st:
+        _check(st, where)
+    return h
+
+
+def hg_group_norm_fwd_workspace_size(batch: int, t: int, width: int, groups: int, dtype=torch.float32) -> int:
+    return int(lib().hg_group_norm_fwd_workspace_size(_pack_group_norm(t, batch, width, groups, _DTYPES[dtype], 0, 1.0)))
+
+
+def hg_group_norm_bwd_workspace_size(batch: int, t: int, width: int, groups: int, dtype=torch.float32) -> int:
+    return int(lib().hg_group_norm_bwd_workspace_size(_pack_group_norm(t, batch, width, groups, _DTYPES[dtype], 0, 1.0)))
+
+
+def _group_norm_desc(where, x, groups, act, eps):
+    if x.dim() not in (2, 3):
+        raise ValueError(f"{where}: rows are [batch, t, width] or [n, width], got {tuple(x.shape)}")
+    b, w = x.shape[0], x.shape[-1]
+    return _pack_group_norm(x.shape[1] if x.dim() == 3 else 1, b, w, groups, _float_code(where, x), act, eps), b, w
+
+
+def hg_group_norm_fwd(x, groups: int, w=None, b=None, act: int = HG_ACT_NONE, eps: float = 1e-5, lens=None, y=None,
+                      stats=None, want_stats: bool = False, ws=None, stream=None):
+    """act(w (x - mean) / sqrt(var + eps) + b) over the tokens and the channels of
+    each group: x [batch, t, width], or [n, width] for every row by itself; w, b
+    float32 [width] or None, lens int32 [batch] or None.  Returns (y, stats):
+    stats float32 [batch, groups, 2] for the backward, None unless given or
+    wanted."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_group_norm_fwd(x, groups, w, b, act, eps, lens, y, stats, want_stats, ws)
+    where = "hg_group_norm_fwd"
+    L = lib()
+    desc, n, width = _group_norm_desc(where, x, groups, act, eps)
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if stats is None and want_stats:
+        stats = torch.empty((n, groups, 2), dtype=torch.float32, device=x.device)
+    _same(where, x, y)
+    ws, wp, wn = _workspace(where, ws, L.hg_group_norm_fwd_workspace_size(desc), x)
+    st = L.hg_group_norm_fwd(desc, _channels(where, "x", x, x.shape), _vector(where, w, width, x),
+                             _vector(where, b, width, x), _vector(where, lens, n, x, torch.int32),
+                             _channels(where, "y", y, x.shape), _state(where, stats, (n, groups, 2), x), wp, wn,
+                             _raw_stream(x))
+    if st:
+        _check(st, where)
+    return y, stats
+
+
+def hg_group_norm_bwd(x, groups: int, w, b, stats, dy, act: int = HG_ACT_NONE, eps: float = 1e-5, lens=None, dx=None,
+                      dw=None, db=None, accumulate: bool = False, ws=None, stream=None):
+    """Returns (dx, dw, db) of hg_group_norm_fwd, whose stats these are, for dy =
+    dL/dy; dw and db for the vectors given, added into when accumulate."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_group_norm_bwd(x, groups, w, b, stats, dy, act, eps, lens, dx, dw, db, accumulate, ws)
+    where = "hg_group_norm_bwd"
+    L = lib()
+    desc, n, width = _group_norm_desc(where, x, groups, act, eps)
+    if accumulate and ((w is not None and dw is None) or (b is not None and db is None)):
+        raise ValueError(f"{where}: accumulate needs the buffers to add into")
+    if dx is None:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if dw is None and w is not None:
+        dw = torch.empty_like(w)
+    if db is None and b is not None:
+        db = torch.empty_like(b)
+    _same(where, x, dy, dx)
+    ws, wp, wn = _workspace(where, ws, L.hg_group_norm_bwd_workspace_size(desc), x)
+    st = L.hg_group_norm_bwd(desc, _channels(where, "x", x, x.shape), _vector(where, w, width, x),
+                             _vector(where, b, width, x), _vector(where, lens, n, x, torch.int32),
+                             _state(where, stats, (n, groups, 2), x), _channels(where, "dy", dy, x.shape),
+                             _channels(where, "dx", dx, x.shape), _vector(where, dw, width, x),
+                             _vector(where, db, width, x), 1 if accumulate else 0, wp, wn, _raw_stream(x))
+    if st:
+        _check(st, where)
+    return dx, dw, db
+
+
+def hg_muon_workspace_size(count: int, rows: int, cols: int, dtype=torch.float32, steps: int = 5) -> int:
+    return int(lib().hg_muon_workspace_size(_pack_muon(count, rows, cols, _DTYPES[dtype], steps, 1, 0.0, 0.0, 0.0, 1.0,
+                                                       1.0, 0)))
+
+
+def hg_muon_step(param, grad, momentum, lr: float, mu: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+                 steps: int = 5, scale: Optional[float] = None, eps: float = 1e-7, ws=None, stream=None):
+    """One update of matrices along their orthogonalised momentum, in place on
+    param and momentum: param and grad [rows, cols] or [count, rows, cols],
+    float32 or bfloat16, momentum float32.  scale None: sqrt(max(1, rows / cols))."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return hg_muon_step(param, grad, momentum, lr, mu, weight_decay, nesterov, steps, scale, eps, ws)
+    where = "hg_muon_step"
+    L = lib()
+    shape = param.shape
+    if param.dim() not in (2, 3):
+        raise ValueError(f"{where}: matrices are [rows, cols] or [count, rows, cols], got {tuple(shape)}")
+    _same(where, param, grad)
+    if grad.shape != shape or not grad.is_contiguous() or not param.is_contiguous():
+        raise ValueError(f"{where}: expected contiguous {tuple(shape)}, got param strides {param.stride()}, grad "
+                         f"{tuple(grad.shape)} strides {grad.stride()}")
+    count = shape[0] if len(shape) == 3 else 1
+    rows, cols = shape[-2:]
+    if scale is None:
+        scale = max(1.0, rows / max(1, cols)) ** 0.5
+    desc = _pack_muon(count, rows, cols, _float_code(where, param), steps, 1 if nesterov else 0, lr, mu, weight_decay,
+                      scale, eps, 0)
+    ws, wp, wn = _workspace(where, ws, L.hg_muon_workspace_size(desc), param)
+    st = L.hg_muon_step(desc, param.data_ptr(), grad.data_ptr(), _state(where, momentum, shape, param), wp, wn,
+                        _raw_stream(param))
+    if st:
+        _check(st, where)
 
 
 def hg_timing_enable(on: bool = True):

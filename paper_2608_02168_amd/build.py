@@ -20,7 +20,7 @@ ARCH = os.environ.get("HG_OFFLOAD_ARCH", "gfx950")
 
 SOURCES = ["hg_api.hip", "hg_scan.hip", "hg_build.hip", "hg_layer.hip", "hg_hgt.hip", "hg_align.hip", "hg_objective.hip",
            "hg_temporal.hip", "hg_kway.hip", "hg_linear.hip", "hg_rope.hip",
-           "hg_linattn.hip"]
+           "hg_linattn.hip", "hg_recur.hip", "hg_norm.hip", "hg_muon.hip"]
 CEILING_SOURCES = ["hg_ceiling.hip"]
 
 FLAGS = [

@@ -33,6 +33,8 @@
 // Z[16 i + c][16 j + 4 g + v], v = 0..3: four consecutive columns of a row.
 #pragma once
 
+#include <atomic>
+
 #include "hg_mfma.h"
 
 namespace hg {
@@ -1148,6 +1150,24 @@ __global__ void __launch_bounds__(256) k_product_join(const GShape p, int splits
       Epi::template apply<ACT>(e, ec, m, z, r);
     }
   });
+}
+
+// More than 64 KB of LDS for a kernel: an attribute of its copy on each device, set
+// before its first launch there (a device past the 64th sets it every time).
+template <auto kern>
+int allow_lds(size_t lds) {
+  if (lds > 65536) {
+    static std::atomic<uint64_t> set_on{0};
+    int dev = 0;
+    HG_HIP_TRY(hipGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+    if (!(set_on.load(std::memory_order_relaxed) & bit)) {
+      HG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                     (int)lds));
+      set_on.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  return HG_OK;
 }
 
 }  // namespace hg

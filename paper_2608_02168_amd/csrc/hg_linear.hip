@@ -15,7 +15,6 @@
 // aligned and a multiple of 8 wide; else they are copied once into padded
 // rows.  float32 operands are always used where they lie (split into parts on
 // the way to LDS).
-#include <atomic>
 
 #include "hg_gemm.h"
 
@@ -290,24 +289,6 @@ Tiling tiling(int64_t M, int64_t cols, int64_t K, bool may_split, bool f32, int6
 
 int64_t part_elems(const Tiling& t, int64_t M, int64_t ld, int planes = 1) {
   return t.splits * planes > 1 ? (int64_t)t.splits * planes * M * ld : 0;
-}
-
-// More than 64 KB of LDS for a kernel: an attribute of its copy on each device, set
-// before its first launch there (a device past the 64th sets it every time).
-template <auto kern>
-int allow_lds(size_t lds) {
-  if (lds > 65536) {
-    static std::atomic<uint64_t> set_on{0};
-    int dev = 0;
-    HG_HIP_TRY(hipGetDevice(&dev));
-    const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
-    if (!(set_on.load(std::memory_order_relaxed) & bit)) {
-      HG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)lds));
-      set_on.fetch_or(bit, std::memory_order_relaxed);
-    }
-  }
-  return HG_OK;
 }
 
 template <bool AKM, bool BKM, int TILE, class Epi, bool SPLIT>

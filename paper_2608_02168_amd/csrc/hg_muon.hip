@@ -33,118 +33,215 @@ constexpr float pow2(int e) { return e >= 0 ? (float)(1ll << e) : 1.f / (float)(
 
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
-// One stored matrix [rows][ld] (ld a multiple of 8; columns past cols are zero), a
-// plane or two of them, `step` values from one matrix of the call to the next.
-struct Planes {
+// One stored matrix of rows x cols values, `step` 16-bit values from one matrix of
+// the call to the next.  A row holds its columns up to a multiple of 8 (with LO of
+// 32), zeros from cols on; with LO each 32 high parts are followed by their low
+// parts, so that a tile's 128-byte rows are 32 columns in two parts, or 64 in one.
+struct Stored {
   uint16_t* p;
-  int64_t step, lo;
-  int32_t rows, cols, ld;
+  int64_t step;
+  int32_t rows, cols;
+  int32_t pad;  // columns with their padding
+  int32_t ld;   // values of a row
 };
+template <bool LO>
+__device__ __forceinline__ int64_t spot(const Stored& o, int r, int c) {
+  return (int64_t)r * o.ld + (LO ? (c >> 5) * 64 + (c & 31) : c);
+}
 
 struct MuonArgs {
-  Planes a, b;          // operands
-  Planes c;             // what the epilogue adds: A for B, X for the next X
-  Planes o;             // what it writes
+  Stored a, b;          // operands
+  Stored c;             // what the epilogue adds: A for B, X for the next X
+  Stored o;             // what it writes
   void* W;              // or the update of W [count][M][N]
   int32_t M, N, K;      // of the product
   int32_t tiles_m, tiles_n, tiles;  // tiles of one matrix
+  uint32_t full;        // tiles of the call that one block takes; of the others, each `pieces` blocks a part of k
+  int32_t pieces;
+  float* part;          // [blocks of parts][BM BN] their sums
   float zs, cs;         // out = zs z + cs c
   float ws, us;         // W = ws W - us (zs z + cs c)
 };
 
 enum { kEpiSym = 0, kEpiSymAdd = 1, kEpiAdd = 2, kEpiUpdate = 3 };
 
-// fp16 parts of four values; the low parts only with LO.
+// The parts of four adjacent values (of the first of them) of a row.
 template <bool LO>
-__device__ __forceinline__ void put4(const Planes& o, int64_t at, int left, const float (&v)[4]) {
+__device__ __forceinline__ void put4(uint16_t* p, const float (&v)[4]) {
   f16x4 h, l;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     h[q] = (_Float16)v[q];
     l[q] = (_Float16)(v[q] - (float)h[q]);
   }
-  if (left >= 4) {
-    *reinterpret_cast<f16x4*>(o.p + at) = h;
-    if (LO) *reinterpret_cast<f16x4*>(o.p + o.lo + at) = l;
-  } else {
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (q < left) {
-        o.p[at + q] = __builtin_bit_cast(uint16_t, h[q]);
-        if (LO) o.p[o.lo + at + q] = __builtin_bit_cast(uint16_t, l[q]);
-      }
-  }
+  *reinterpret_cast<f16x4*>(p) = h;
+  if (LO) *reinterpret_cast<f16x4*>(p + 32) = l;
 }
 template <bool LO>
-__device__ __forceinline__ void get4(const Planes& c, int64_t at, float (&v)[4]) {
-  const f16x4 h = *reinterpret_cast<const f16x4*>(c.p + at);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] = (float)h[q];
-  if (LO) {
-    const f16x4 l = *reinterpret_cast<const f16x4*>(c.p + c.lo + at);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] += (float)l[q];
-  }
+__device__ __forceinline__ void put1(uint16_t* p, float v) {
+  const _Float16 h = (_Float16)v;
+  *p = __builtin_bit_cast(uint16_t, h);
+  if (LO) p[32] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
-
-// Tile (row, column) of tile id of the lower triangle.
-__device__ __forceinline__ void tri_of(uint32_t id, uint32_t& im, uint32_t& in) {
+// Tile (row, column) of tile id of the lower triangle of tm tile rows, in the order
+// of g_tile_of: each XCD takes one contiguous share of a walk that goes down eight
+// tile rows before it moves to the next tile column.
+__device__ __forceinline__ uint32_t row_of_tri(uint32_t id) {
   uint32_t i = (uint32_t)((sqrtf(8.f * (float)id + 1.f) - 1.f) * 0.5f);
   while ((i + 1) * (i + 2) / 2 <= id) ++i;
   while (i * (i + 1) / 2 > id) --i;
-  im = i;
-  in = id - i * (i + 1) / 2;
+  return i;
+}
+__device__ __forceinline__ void tri_of(uint32_t id, uint32_t tm, uint32_t& im, uint32_t& in) {
+  const uint32_t n = tm * (tm + 1) / 2, per = n / 8, more = n % 8, x = id % 8;
+  const uint32_t i = x * per + (x < more ? x : more) + id / 8;
+  // rows 8 b .. of a band: 8 b whole columns, then a triangle; the bands before have 32 b^2 + 4 b tiles
+  uint32_t b = (uint32_t)((sqrtf(16.f + 128.f * (float)i) - 4.f) / 64.f);
+  while (32 * (b + 1) * (b + 1) + 4 * (b + 1) <= i) ++b;
+  while (32 * b * b + 4 * b > i) --b;
+  const uint32_t r = i - (32 * b * b + 4 * b), rows = tm - 8 * b < 8 ? tm - 8 * b : 8;
+  if (r < rows * 8 * b) {
+    im = 8 * b + r % rows;
+    in = r / rows;
+  } else {
+    const uint32_t t = r - rows * 8 * b, y = row_of_tri(t);
+    im = 8 * b + y;
+    in = 8 * b + t - y * (y + 1) / 2;
+  }
 }
 
-template <bool AKM, bool BKM, int BM, int BN, int WM, int WN, bool LO, int EPI, class TW>
-__global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_muon_product(const MuonArgs p) {
-  constexpr int BK = 64, NWN = BN / WN, NW = (BM / WM) * NWN, MI = WM / 16, NI = WN / 16, PL = LO ? 2 : 1;
-  typedef GTile<BM, BK, AKM, NW, false> TA;
-  typedef GTile<BN, BK, BKM, NW, false> TB;
-  constexpr int kStage = PL * (TA::kBytes + TB::kBytes);
-  extern __shared__ __align__(1024) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c = lane & 15, g = lane >> 4, wm = wave / NWN, wn = wave % NWN;
-  const uint32_t mat = blockIdx.x / (uint32_t)p.tiles, id = blockIdx.x - mat * (uint32_t)p.tiles;
-  constexpr bool SYM = EPI == kEpiSym || EPI == kEpiSymAdd;
-  uint32_t im, in;
-  if constexpr (SYM) {
-    tri_of(id, im, in);
+// A tile of the call: its matrix, row and column.
+template <int EPI>
+__device__ __forceinline__ void tile_of(const MuonArgs& p, uint32_t tile, uint32_t& mat, uint32_t& im, uint32_t& in) {
+  mat = tile / (uint32_t)p.tiles;
+  const uint32_t id = tile - mat * (uint32_t)p.tiles;
+  if constexpr (EPI <= kEpiSymAdd) {
+    tri_of(id, p.tiles_m, im, in);
   } else {
     g_tile_of(id, p.tiles_m, p.tiles_n, 8, im, in);
   }
+}
+
+// What the epilogue of columns n .. n + 3 of row m reads: of X or A, and of W.  All
+// of a row of blocks is loaded before the first is written: the compiler keeps loads
+// behind stores that may be to the same place, and would wait for each.
+template <bool LO, int EPI, class T>
+struct Beside {
+  f16x4 h, l;
+  typename Vec<T, 4>::raw w;
+  __device__ __forceinline__ void load(const MuonArgs& p, uint32_t mat, int m, int n) {
+    if constexpr (EPI != kEpiSym) {
+      if (m < p.M && n < p.c.pad) {
+        const uint16_t* x = p.c.p + mat * p.c.step + spot<LO>(p.c, m, n);
+        h = *reinterpret_cast<const f16x4*>(x);
+        if (LO) l = *reinterpret_cast<const f16x4*>(x + 32);
+      }
+    }
+    if constexpr (EPI == kEpiUpdate)
+      if (m < p.M && n + 4 <= p.N) w = Vec<T, 4>::load(static_cast<const T*>(p.W) + ((int64_t)mat * p.M + m) * p.N + n);
+  }
+};
+
+// The epilogue of columns n .. n + 3 of row m; mirror: below the diagonal of a
+// symmetric result, whose transpose is written too.
+template <bool LO, int EPI, class T>
+__device__ __forceinline__ void finish(const MuonArgs& p, uint32_t mat, int m, int n, bool mirror, const f32x4& z,
+                                       const Beside<LO, EPI, T>& x) {
+  constexpr bool SYM = EPI <= kEpiSymAdd;
+  const bool row = m < p.M;
+  const int left = p.N - n;
+  // A stored row is read up to its padding, so the padding is written too: that of a
+  // symmetric matrix's upper rows by the mirrored tiles, from rows past M.
+  if (EPI == kEpiUpdate ? !row || left <= 0 : n >= p.o.pad || !(row || (SYM && m < p.o.pad))) return;
+  float v[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    v[q] = row ? p.zs * z[q] : 0.f;
+    if (EPI != kEpiSym && row) v[q] = fmaf(p.cs, LO ? (float)x.h[q] + (float)x.l[q] : (float)x.h[q], v[q]);
+  }
+  if constexpr (EPI == kEpiUpdate) {
+    T* w = static_cast<T*>(p.W) + ((int64_t)mat * p.M + m) * p.N + n;
+    if (left >= 4) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = fmaf(-p.us, v[q], p.ws * Vec<T, 4>::get(x.w, q));
+      Vec<T, 4>::put(w, v);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < left) {
+          const float y[1] = {fmaf(-p.us, v[q], p.ws * Elt<T>::get(w + q))};
+          Vec<T, 1>::put(w + q, y);
+        }
+    }
+  } else {
+    uint16_t* o = p.o.p + mat * p.o.step;
+    if (row) put4<LO>(o + spot<LO>(p.o, m, n), v);
+    if (SYM && mirror) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (q < left) put1<LO>(o + spot<LO>(p.o, n + q, m), v[q]);
+    }
+  }
+}
+
+// Tiles of a block and of a wave, and stages of k in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int ST_>
+struct Tile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, ST = ST_;
+  static constexpr int NWN = BN / WN, NW = (BM / WM) * NWN, NT = NW * 64, MI = WM / 16, NI = WN / 16;
+  static constexpr size_t kLds = (size_t)ST * (BM + BN) * 128;
+};
+
+// Waits until at most N loads of this wave are in flight.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+template <class TL, bool AKM, bool BKM, bool LO, int EPI, class T>
+__global__ void __launch_bounds__(TL::NT) k_muon_product(const MuonArgs p) {
+  constexpr int BM = TL::BM, BN = TL::BN, MI = TL::MI, NI = TL::NI, NW = TL::NW, ST = TL::ST;
+  constexpr int PL = LO ? 2 : 1, BK = 64 / PL;  // k of a stage
+  // by rows of k: 64 values, in two parts those of 32; with k as the row: BK rows of the tile's columns in their parts
+  typedef GTile<AKM ? BM : BM * PL, AKM ? 64 : BK, AKM, NW, false> TA;
+  typedef GTile<BKM ? BN : BN * PL, BKM ? 64 : BK, BKM, NW, false> TB;
+  constexpr int kStage = TA::kBytes + TB::kBytes, kLoads = TA::PER + TB::PER;
+  static_assert((size_t)ST * kStage == TL::kLds && kLoads * (ST - 1) < 64, "the stages fit LDS and the counter");
+  extern __shared__ __align__(1024) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 15, g = lane >> 4, wm = wave / TL::NWN, wn = wave % TL::NWN;
+  // a tile, or one of the parts of its k
+  uint32_t tile = blockIdx.x, piece = 0, pieces = 1;
+  if (tile >= p.full) {
+    pieces = p.pieces;
+    piece = (blockIdx.x - p.full) % pieces;
+    tile = p.full + (blockIdx.x - p.full) / pieces;
+  }
+  uint32_t mat, im, in;
+  tile_of<EPI>(p, tile, mat, im, in);
   const int m0 = (int)im * BM, n0 = (int)in * BN;
   const uint16_t *ap = p.a.p + mat * p.a.step, *bp = p.b.p + mat * p.b.step;
-  const int steps = (p.K + BK - 1) / BK;
+  const uint32_t whole = (uint32_t)(p.K + BK - 1) / BK;
+  const int from = (int)(whole * piece / pieces), to = (int)(whole * (piece + 1) / pieces);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(g_lds_addr(lds));
   TA ta;
   TB tb;
-  ta.init(GOperand<uint16_t>{ap, p.a.ld, p.a.rows, p.a.cols}, wave, lane, 0);
-  tb.init(GOperand<uint16_t>{bp, p.b.ld, p.b.rows, p.b.cols}, wave, lane, 0);
+  ta.init(GOperand<uint16_t>{ap, p.a.ld, p.a.rows, p.a.ld}, wave, lane, 0);
+  tb.init(GOperand<uint16_t>{bp, p.b.ld, p.b.rows, p.b.ld}, wave, lane, 0);
 
-  // (a stored row ends at ld, with zeros from cols on)
+  // (rows past the last and values past a row's padding read as zero)
   auto issue = [&](int t) {
-    const int64_t k0 = (int64_t)t * BK, kl = p.K - k0;
-    uint32_t st = lds0 + (t & 1) * kStage;
-#pragma unroll
-    for (int q = 0; q < PL; ++q) {
-      const uint16_t* s = ap + q * p.a.lo;
-      if constexpr (AKM) {
-        ta.issue(s + (int64_t)m0 * p.a.ld + k0, 2 * ((int64_t)(p.a.rows - m0) * p.a.ld - k0), kl, st, wave);
-      } else {
-        ta.issue(s + k0 * p.a.ld + m0, 2 * (kl * p.a.ld - m0), kl, st, wave);
-      }
-      st += TA::kBytes;
+    const uint32_t st = lds0 + (uint32_t)(t % ST) * kStage;
+    const int64_t kv = (int64_t)t * 64, kr = (int64_t)t * BK;
+    if constexpr (AKM) {
+      ta.issue(ap + (int64_t)m0 * p.a.ld + kv, 2 * ((int64_t)(p.a.rows - m0) * p.a.ld - kv), p.a.ld - kv, st, wave);
+    } else {
+      ta.issue(ap + kr * p.a.ld + m0 * PL, 2 * ((p.a.rows - kr) * p.a.ld - m0 * PL), p.K - kr, st, wave);
     }
-#pragma unroll
-    for (int q = 0; q < PL; ++q) {
-      const uint16_t* s = bp + q * p.b.lo;
-      if constexpr (BKM) {
-        tb.issue(s + (int64_t)n0 * p.b.ld + k0, 2 * ((int64_t)(p.b.rows - n0) * p.b.ld - k0), kl, st, wave);
-      } else {
-        tb.issue(s + k0 * p.b.ld + n0, 2 * (kl * p.b.ld - n0), kl, st, wave);
-      }
-      st += TB::kBytes;
+    if constexpr (BKM) {
+      tb.issue(bp + (int64_t)n0 * p.b.ld + kv, 2 * ((int64_t)(p.b.rows - n0) * p.b.ld - kv), p.b.ld - kv, st + TA::kBytes, wave);
+    } else {
+      tb.issue(bp + kr * p.b.ld + n0 * PL, 2 * ((p.b.rows - kr) * p.b.ld - n0 * PL), p.K - kr, st + TA::kBytes, wave);
     }
   };
 
@@ -154,111 +251,152 @@ __global__ void __launch_bounds__((BM / WM) * (BN / WN) * 64) k_muon_product(con
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  issue(0);
-  for (int t = 0; t < steps; ++t) {
-    g_wait_loads();  // this wave's share of the step is in LDS
+#pragma unroll
+  for (int q = 0; q < ST - 1; ++q)
+    if (from + q < to) issue(from + q);
+  for (int t = from; t < to; ++t) {
+    // this wave's share of the stage is in LDS, later stages may be under way
+    if (to - t >= ST - 1) {
+      wait_loads<kLoads*(ST - 2)>();
+    } else {
+      wait_loads<0>();
+    }
     __syncthreads();
-    if (t + 1 < steps) issue(t + 1);
-    const char* sa = lds + (t & 1) * kStage;
-    const char* sb = sa + PL * TA::kBytes;
+    if (t + ST - 1 < to) issue(t + ST - 1);
+    const char* sa = lds + (t % ST) * kStage;
+    const char* sb = sa + TA::kBytes;
+    // fragment (i, part or half of the stage's k)
+    auto fa_of = [&](int i, int h) { return AKM || !LO ? TA::frag(sa, i, h, c, g) : TA::frag(sa, (i >> 1) * 4 + (i & 1) + 2 * h, 0, c, g); };
+    auto fb_of = [&](int i, int h) { return BKM || !LO ? TB::frag(sb, i, h, c, g) : TB::frag(sb, (i >> 1) * 4 + (i & 1) + 2 * h, 0, c, g); };
+    if constexpr (LO) {
+      uint4 fa[2][MI], fb[2][NI];
 #pragma unroll
-    for (int kb = 0; kb < BK / 32; ++kb) {
-      uint4 fa[PL][MI], fb[PL][NI];
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int q = 0; q < PL; ++q) {
+        for (int j = 0; j < NI; ++j) fb[h][j] = fb_of(wn * NI + j, h);
 #pragma unroll
-        for (int j = 0; j < NI; ++j) fb[q][j] = TB::frag(sb + q * TB::kBytes, wn * NI + j, kb, c, g);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) fa[q][i] = TA::frag(sa + q * TA::kBytes, wm * MI + i, kb, c, g);
+        for (int i = 0; i < MI; ++i) fa[h][i] = fa_of(wm * MI + i, h);
       }
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
+      for (int h = 0; h < 3; ++h)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          if constexpr (LO) {
-            acc[i][j] = mfma_f16(fb[0][j], fa[1][i], acc[i][j]);
-            acc[i][j] = mfma_f16(fb[1][j], fa[0][i], acc[i][j]);
-          }
-          acc[i][j] = mfma_f16(fb[0][j], fa[0][i], acc[i][j]);
-        }
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = mfma_f16(fb[h == 1][j], fa[h == 2][i], acc[i][j]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint4 fa[MI], fb[NI];
+#pragma unroll
+        for (int j = 0; j < NI; ++j) fb[j] = fb_of(wn * NI + j, h);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[i] = fa_of(wm * MI + i, h);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = mfma_f16(fb[j], fa[i], acc[i][j]);
+      }
     }
   }
 
+  if (pieces > 1) {
+    float* mine = p.part + (int64_t)(blockIdx.x - p.full) * BM * BN + threadIdx.x * 4;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j) *reinterpret_cast<f32x4*>(mine + (i * NI + j) * TL::NT * 4) = acc[i][j];
+    return;
+  }
   // lane (c, g) holds columns 16 j + 4 g .. + 3 of row 16 i + c
+  const int mr = m0 + wm * TL::WM + c, nc = n0 + wn * TL::WN + 4 * g;
+  Beside<LO, EPI, T> x[2][NI];
+#pragma unroll
+  for (int j = 0; j < NI; ++j) x[0][j].load(p, mat, mr, nc + 16 * j);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
-    const int m = m0 + wm * WM + 16 * i + c;
-    const bool row = m < p.M;
-    // (a symmetric matrix's columns from M to ld are zeros that its mirrored tiles write)
-    if (!row && !(SYM && m < p.o.ld)) continue;
+    if (i + 1 < MI)
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int n = n0 + wn * WN + 16 * j + 4 * g, left = p.N - n;
-      // (the padding of a written row is written too: a row is read up to ld)
-      if (EPI == kEpiUpdate ? left <= 0 : n >= p.o.ld) continue;
-      float v[4];
+      for (int j = 0; j < NI; ++j) x[(i + 1) & 1][j].load(p, mat, mr + 16 * (i + 1), nc + 16 * j);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = row ? p.zs * acc[i][j][q] : 0.f;
-      if constexpr (EPI != kEpiSym) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};  // (within the row: ld is a multiple of 8)
-        if (row) get4<LO>(p.c, mat * p.c.step + (int64_t)m * p.c.ld + n, x);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = fmaf(p.cs, x[q], v[q]);
-      }
-      if constexpr (EPI == kEpiUpdate) {
-        TW* w = static_cast<TW*>(p.W) + ((int64_t)mat * p.M + m) * p.N + n;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (q < left) {
-            const float y = fmaf(-p.us, v[q], p.ws * Elt<TW>::get(w + q));
-            if constexpr (sizeof(TW) == 4) {
-              w[q] = y;
-            } else {
-              w[q] = f2bf(y);
-            }
-          }
-      } else {
-        // (columns from N to ld are zero: the operands' columns there are)
-        if (row) put4<LO>(p.o, mat * p.o.step + (int64_t)m * p.o.ld + n, p.o.ld - n, v);
-      }
-      if constexpr (SYM) {
-        if (im != in) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (q < left) {
-              const float s[4] = {v[q], 0.f, 0.f, 0.f};
-              put4<LO>(p.o, mat * p.o.step + (int64_t)(n + q) * p.o.ld + m, 1, s);
-            }
-        }
-      }
-    }
+    for (int j = 0; j < NI; ++j) finish<LO, EPI, T>(p, mat, mr + 16 * i, nc + 16 * j, im != in, acc[i][j], x[i & 1][j]);
   }
+}
+
+// Tiles whose k was cut: their parts added in order, then the epilogue.  A block has
+// one of the MI NI groups of 16 x 16 of each of a tile's waves.
+template <class TL, bool LO, int EPI, class T>
+__global__ void __launch_bounds__(TL::NT) k_muon_join(const MuonArgs p) {
+  constexpr int G = TL::MI * TL::NI;
+  const uint32_t cut = blockIdx.x / G, ij = blockIdx.x - cut * G;
+  uint32_t mat, im, in;
+  tile_of<EPI>(p, p.full + cut, mat, im, in);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4, i = (int)ij / TL::NI, j = (int)ij % TL::NI;
+  const float* all = p.part + (int64_t)cut * p.pieces * TL::BM * TL::BN + (int64_t)ij * TL::NT * 4 + threadIdx.x * 4;
+  const int m = (int)im * TL::BM + (wave / TL::NWN) * TL::WM + 16 * i + c;
+  const int n = (int)in * TL::BN + (wave % TL::NWN) * TL::WN + 16 * j + 4 * g;
+  Beside<LO, EPI, T> x;
+  x.load(p, mat, m, n);
+  f32x4 z{0.f, 0.f, 0.f, 0.f};
+  for (int q0 = 0; q0 < p.pieces; q0 += 8) {
+    f32x4 y[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q0 + q < p.pieces) y[q] = *reinterpret_cast<const f32x4*>(all + (int64_t)(q0 + q) * TL::BM * TL::BN);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (q0 + q < p.pieces)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z[v] += y[q][v];
+  }
+  finish<LO, EPI, T>(p, mat, m, n, im != in, z, x);
 }
 
 // ---- momentum, norm, first X ------------------------------------------------------
-constexpr int kNormBlocks = 256;  // blocks of a matrix at most
+constexpr int kNormBlocks = 2048;  // blocks of a matrix at most
 
-// Four values from at on of n (fewer at the end).
-template <class T>
-__device__ __forceinline__ f32x4 take4(const T* p, int64_t left) {
-  if (left >= 4) return Elt<T>::load4(p);
-  f32x4 v{0.f, 0.f, 0.f, 0.f};
-  for (int q = 0; q < left; ++q) v[q] = Elt<T>::get(p + q);
-  return v;
-}
-
-// M = mu M + G and the blocks' sums of U^2.
+// M = mu M + G and the blocks' sums of U^2: four values at a time, the last ones
+// (and all of a matrix whose four would reach into the next) one by one.
 template <class T>
 __global__ void __launch_bounds__(256)
     k_muon_momentum(const T* __restrict__ G, float* __restrict__ M, int64_t n, float mu, int nesterov, double* __restrict__ part) {
   __shared__ double sh[256];
-  const int64_t base = (int64_t)blockIdx.y * n;
+  const T* g = G + (int64_t)blockIdx.y * n;
+  float* m = M + (int64_t)blockIdx.y * n;
   double s = 0;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const float g = Elt<T>::get(G + base + i), m = fmaf(mu, M[base + i], g);
-    M[base + i] = m;
-    const double u = nesterov ? fmaf(mu, m, g) : m;
-    s += u * u;
+  const int64_t step = (int64_t)gridDim.x * 1024;
+  for (int64_t i0 = (int64_t)blockIdx.x * 1024 + threadIdx.x * 4; i0 < n; i0 += 4 * step) {
+    typename Vec<T, 4>::raw a[4];
+    typename Vec<float, 4>::raw b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i0 + k * step + 4 <= n) {
+        a[k] = Vec<T, 4>::load(g + i0 + k * step);
+        b[k] = Vec<float, 4>::load(m + i0 + k * step);
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t i = i0 + k * step;
+      if (i + 4 <= n) {
+        float v[4];
+        double w = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float x = Vec<T, 4>::get(a[k], q);
+          v[q] = fmaf(mu, b[k][q], x);
+          const double u = nesterov ? fmaf(mu, v[q], x) : v[q];
+          w += u * u;
+        }
+        s += w;
+        Vec<float, 4>::put(m + i, v);
+      } else {
+        for (int64_t q = i; q < n; ++q) {
+          const float x = Elt<T>::get(g + q), v = fmaf(mu, m[q], x);
+          m[q] = v;
+          const double u = nesterov ? fmaf(mu, v, x) : v;
+          s += u * u;
+        }
+      }
+    }
   }
   sh[threadIdx.x] = s;
   __syncthreads();
@@ -269,85 +407,451 @@ __global__ void __launch_bounds__(256)
   if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sh[0];
 }
 
+// 1 / max(size, eps) as f 2^e (so that neither it nor a scaled value leaves float32's
+// range); NaN if the size is not finite.
+struct Inverse {
+  float f;
+  int e;
+};
+__device__ __forceinline__ Inverse inverse_of(double size, float eps) {
+  int e;
+  const double f = frexp(1.0 / (size > (double)eps ? size : (double)eps), &e);
+  return std::isfinite(size) ? Inverse{(float)f, e} : Inverse{__builtin_nanf(""), 0};
+}
+__device__ __forceinline__ float scaled(float u, const Inverse& i, int more) {
+  return __builtin_amdgcn_ldexpf(u * i.f, i.e + more);
+}
+
 // X = U / max(|U|, eps) in its parts, or with steps = 0 the update of W.
 template <class T, bool LO, bool UPDATE>
 __global__ void __launch_bounds__(256)
     k_muon_first(const T* __restrict__ G, const float* __restrict__ M, int32_t rows, int32_t cols, float mu, int nesterov,
-                 const double* __restrict__ part, int parts, float eps, Planes o, T* __restrict__ W, float ws, float us) {
-  __shared__ double sh[kNormBlocks];
+                 const double* __restrict__ part, int parts, float eps, Stored o, T* __restrict__ W, float ws, float us) {
+  __shared__ double sh[256];
   const int64_t mat = blockIdx.y, base = mat * rows * cols;
-  sh[threadIdx.x] = (int)threadIdx.x < parts ? part[mat * parts + threadIdx.x] : 0.0;
+  {
+    double s = 0;
+    for (int q = threadIdx.x; q < parts; q += 256) s += part[mat * parts + q];
+    sh[threadIdx.x] = s;
+  }
   __syncthreads();
-  for (int q = kNormBlocks / 2; q > 0; q /= 2) {
+  for (int q = 128; q > 0; q /= 2) {
     if ((int)threadIdx.x < q) sh[threadIdx.x] += sh[threadIdx.x + q];
     __syncthreads();
   }
-  const double size = sqrt(sh[0]);
-  const double inv = std::isfinite(size) ? 1.0 / (size > (double)eps ? size : (double)eps) : (double)__builtin_nanf("");
-  const int per = o.ld / 4;
+  const Inverse inv = inverse_of(sqrt(sh[0]), eps);
+  const int per = o.pad / 4;
   const int64_t n = (int64_t)rows * per;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / per), c = (int)(i - (int64_t)r * per) * 4;
+    const int64_t at = base + (int64_t)r * cols + c;
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, g[4], m[4], w[4];
+    const int left = cols - c;
+    if (left >= 4) {
+      const auto a = Vec<T, 4>::load(G + at);
+      const auto b = Vec<float, 4>::load(M + at);
+      if constexpr (UPDATE) {
+        const auto d = Vec<T, 4>::load(W + at);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = Vec<T, 4>::get(d, q);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) g[q] = Vec<T, 4>::get(a, q), m[q] = b[q];
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        g[q] = q < left ? Elt<T>::get(G + at + q) : 0.f;
+        m[q] = q < left ? M[at + q] : 0.f;
+        if (UPDATE) w[q] = q < left ? Elt<T>::get(W + at + q) : 0.f;
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q >= left) break;
+      const float x = scaled(nesterov ? fmaf(mu, m[q], g[q]) : m[q], inv, UPDATE ? 0 : kXe);
+      v[q] = UPDATE ? fmaf(-us, x, ws * w[q]) : x;
+    }
+    if constexpr (!UPDATE) {
+      put4<LO>(o.p + mat * o.step + spot<LO>(o, r, c), v);
+    } else if (left >= 4) {
+      Vec<T, 4>::put(W + at, v);
+    } else {
+      for (int q = 0; q < left; ++q) {
+        const float y[1] = {v[q]};
+        Vec<T, 1>::put(W + at + q, y);
+      }
+    }
+  }
+}
+
+// ---- small matrices -----------------------------------------------------------------
+// A matrix whose smaller side is at most MP and whose X and A fit LDS: one block does
+// the whole update.  X [MP][pad of the larger side] and A [MP][MP] lie in LDS in
+// panels of 128-byte rows (the stored rows' order), the 16-byte chunk ch of row r at
+// ch ^ (r & 7).  A panel is a tile by rows of k (the Gram product, A A, B), or with
+// transposing reads one with k as the row (B X).  A tall matrix is worked on as its
+// transpose.  A product's sums stay in registers until all waves have read, so A A
+// overwrites A, and B X overwrites X.
+struct SmallArgs {
+  const void* G;
+  float* M;
+  void* W;
+  int32_t rows, cols;   // as the caller has them
+  int32_t m, n, panels; // the smaller side, the larger, panels of X
+  int32_t steps, nesterov;
+  float mu, eps, ws, us;
+};
+
+constexpr int kSmallWaves = 16;
+constexpr int kFlight = 4;  // times four values of a thread in flight
+
+// fragment of rows 16 i + c of a panel, k = 32 kb + 8 g ..
+__device__ __forceinline__ uint4 panel_rows(const char* panel, int i, int kb, int c, int g) {
+  return *reinterpret_cast<const uint4*>(panel + (16 * i + c) * 128 + (((4 * kb + g) ^ (c & 7)) * 16));
+}
+// fragment of columns 16 j + c of a panel (16-bit values of its rows), k = rows 32 kb + 8 g ..
+__device__ __forceinline__ uint4 panel_cols(const char* panel, int j, int kb, int c, int g) {
+  typedef __attribute__((address_space(3))) g_s16x4* lds_ptr;
+  const int r = 32 * kb + 8 * g + (c >> 2), ch = 2 * j + ((c & 3) >> 1);
+  const char* a = panel + r * 128 + ((ch ^ (r & 7)) * 16) + (c & 1) * 8;
+  const char* b = panel + (r + 4) * 128 + ((ch ^ ((r + 4) & 7)) * 16) + (c & 1) * 8;
+  const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)a));
+  const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)b));
+  return uint4{x.x, x.y, y.x, y.y};
+}
+// the high part of value (r, col) of panels of MP rows
+template <bool LO, int MP>
+__device__ __forceinline__ uint16_t* panel_at(char* panels, int r, int col) {
+  const int panel = LO ? col >> 5 : col >> 6, v = LO ? col & 31 : col & 63;
+  return reinterpret_cast<uint16_t*>(panels + panel * MP * 128 + r * 128 + (((v >> 3) ^ (r & 7)) * 16)) + (v & 7);
+}
+// (the low part's chunk is four from the high part's, before the exchange by r & 7)
+template <bool LO, int MP>
+__device__ __forceinline__ void panel_put4(char* panels, int r, int col, const float (&v)[4]) {
+  f16x4 h, l;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    h[q] = (_Float16)v[q];
+    l[q] = (_Float16)(v[q] - (float)h[q]);
+  }
+  uint16_t* p = panel_at<LO, MP>(panels, r, col);
+  *reinterpret_cast<f16x4*>(p) = h;
+  if (LO) *reinterpret_cast<f16x4*>(reinterpret_cast<uint16_t*>(reinterpret_cast<uintptr_t>(p) ^ 64)) = l;
+}
+template <bool LO, int MP>
+__device__ __forceinline__ void panel_get4(const char* panels, int r, int col, float (&v)[4]) {
+  const uint16_t* p = panel_at<LO, MP>(const_cast<char*>(panels), r, col);
+  const f16x4 h = *reinterpret_cast<const f16x4*>(p);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) v[q] = (float)h[q];
+  if (LO) {
+    const f16x4 l = *reinterpret_cast<const f16x4*>(reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(p) ^ 64));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] += (float)l[q];
+  }
+}
+
+// One stage of k (a panel's 128-byte rows) into acc: hi hi and, with LO, the cross products.
+template <bool LO, int MI, int NI, class FA, class FB>
+__device__ __forceinline__ void stage(f32x4 (&acc)[MI][NI], FA fa_of, FB fb_of) {
+  uint4 fa[2][MI], fb[2][NI];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) fb[h][j] = fb_of(j, h);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fa[h][i] = fa_of(i, h);
+  }
+#pragma unroll
+  for (int h = 0; h < (LO ? 3 : 2); ++h)
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+        acc[i][j] = mfma_f16(fb[LO ? h == 1 : h][j], fa[LO ? h == 2 : h][i], acc[i][j]);
+}
+template <int MI, int NI>
+__device__ __forceinline__ void clear(f32x4 (&acc)[MI][NI]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+}
+
+template <class T, int MP>
+__global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs p) {
+  constexpr bool LO = sizeof(T) == 4;
+  constexpr int NT = kSmallWaves * 64, kPanel = MP * 128, AP = (LO ? 2 : 1) * MP / 64 > 0 ? (LO ? 2 : 1) * MP / 64 : 1;
+  constexpr int CP = LO ? 32 : 64;                 // columns of a panel
+  constexpr int WR = MP / 16 < 4 ? MP / 16 : 4, WC = WR;  // waves of A
+  constexpr int MI = MP / 16 / WR, NI = MP / 16 / WC;
+  constexpr int XR = MP / 32, XI = MP / 16 / XR;  // row parts of a panel of X, their 16-row blocks
+  constexpr int XJ = CP / 16;
+  extern __shared__ __align__(1024) char lds[];
+  __shared__ double sh[NT];
+  char *xs = lds, *as = lds + p.panels * kPanel;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
+  const int64_t size = (int64_t)p.rows * p.cols, base = blockIdx.x * size;
+  const T* G = static_cast<const T*>(p.G) + base;
+  float* M = p.M + base;
+  T* W = static_cast<T*>(p.W) + base;
+  const bool tall = p.rows > p.cols;
+
+  // four values a thread, kFlight times in flight; the matrix's last ones by one thread
+  const int n4 = (int)(size / 4) * 4, left = (int)size - n4;
+  const auto pass = [&](auto f) {
+    for (int i0 = threadIdx.x * 4; i0 < n4; i0 += NT * 4 * kFlight) {
+      typename Vec<T, 4>::raw x[kFlight];
+      typename Vec<float, 4>::raw m[kFlight];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k)
+        if (i0 + k * NT * 4 < n4) {
+          x[k] = Vec<T, 4>::load(G + i0 + k * NT * 4);
+          m[k] = Vec<float, 4>::load(M + i0 + k * NT * 4);
+        }
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k)
+        if (i0 + k * NT * 4 < n4) {
+          const float xs4[4] = {Vec<T, 4>::get(x[k], 0), Vec<T, 4>::get(x[k], 1), Vec<T, 4>::get(x[k], 2), Vec<T, 4>::get(x[k], 3)};
+          const float ms4[4] = {m[k][0], m[k][1], m[k][2], m[k][3]};
+          f(i0 + k * NT * 4, xs4, ms4, 4);
+        }
+    }
+    if ((int)threadIdx.x < left) {
+      const float x1[4] = {Elt<T>::get(G + n4 + threadIdx.x), 0.f, 0.f, 0.f}, m1[4] = {M[n4 + threadIdx.x], 0.f, 0.f, 0.f};
+      f(n4 + (int)threadIdx.x, x1, m1, 1);
+    }
+  };
+  double s = 0;
+  pass([&](int i, const float (&x)[4], const float (&m)[4], int n) {
     float v[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      v[q] = 0.f;
-      if (c + q < cols) {
-        const int64_t at = base + (int64_t)r * cols + c + q;
-        const float m = M[at], u = nesterov ? fmaf(mu, m, Elt<T>::get(G + at)) : m;
-        const double x = (double)u * inv;
-        if constexpr (UPDATE) {
-          const float y = fmaf(-us, (float)x, ws * Elt<T>::get(W + at));
-          if constexpr (sizeof(T) == 4) {
-            W[at] = y;
-          } else {
-            W[at] = f2bf(y);
-          }
-        } else {
-          v[q] = (float)(x * (double)pow2(kXe));
-        }
-      }
+      v[q] = fmaf(p.mu, m[q], x[q]);
+      const double u = p.nesterov ? fmaf(p.mu, v[q], x[q]) : v[q];
+      if (q < n) s += u * u;
     }
-    if constexpr (!UPDATE) put4<LO>(o, mat * o.step + (int64_t)r * o.ld + c, 4, v);
+    if (n == 4) {
+      Vec<float, 4>::put(M + i, v);
+    } else {
+      M[i] = v[0];
+    }
+  });
+  sh[threadIdx.x] = s;
+  // (X's padding and rows past m are zero, and what no product writes of A's panels)
+  for (int i = threadIdx.x; i < (p.panels + AP) * kPanel / 16; i += NT) reinterpret_cast<uint4*>(xs)[i] = uint4{0u, 0u, 0u, 0u};
+  __syncthreads();
+  for (int o = NT / 2; o > 0; o /= 2) {
+    if ((int)threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
+    __syncthreads();
+  }
+  const Inverse inv = inverse_of(sqrt(sh[0]), p.eps);
+  // (a thread reads again what it wrote)
+  pass([&](int i, const float (&x)[4], const float (&m)[4], int n) {
+    int r = i / p.cols, q = i - r * p.cols;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k >= n) break;
+      const float y = scaled(p.nesterov ? fmaf(p.mu, m[k], x[k]) : m[k], inv, kXe);
+      uint16_t* o = panel_at<LO, MP>(xs, tall ? q : r, tall ? r : q);
+      const _Float16 h = (_Float16)y;
+      *o = __builtin_bit_cast(uint16_t, h);
+      if (LO) *reinterpret_cast<uint16_t*>(reinterpret_cast<uintptr_t>(o) ^ 64) = __builtin_bit_cast(uint16_t, (_Float16)(y - (float)h));
+      if (++q == p.cols) q = 0, ++r;
+    }
+  });
+  __syncthreads();
+
+  const int wr = wave / WC, wc = wave % WC;
+  const bool mine = wave < WR * WC;
+  const int units = p.panels * XR;
+  for (int it = 0; it < p.steps; ++it) {
+    f32x4 acc[MI][NI];
+    // A = X X^T
+    clear(acc);
+    if (mine)
+      for (int q = 0; q < p.panels; ++q) {
+        const char* x = xs + q * kPanel;
+        stage<LO>(acc, [&](int i, int h) { return panel_rows(x, wr * MI + i, h, c, g); },
+                  [&](int j, int h) { return panel_rows(x, wc * NI + j, h, c, g); });
+      }
+    auto store = [&](float zs) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          const int r = 16 * (wr * MI + i) + c, col = 16 * (wc * NI + j) + 4 * g;
+          float v[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[k] = zs * acc[i][j][k];
+          panel_put4<LO, MP>(as, r, col, v);
+        }
+    };
+    if (mine) store(pow2(kAe - 2 * kXe));
+    __syncthreads();
+    // B = q A + s A A, over A
+    clear(acc);
+    if (mine) {
+#pragma unroll
+      for (int q = 0; q < AP; ++q) {
+        const char* x = as + q * kPanel;
+        stage<LO>(acc, [&](int i, int h) { return panel_rows(x, wr * MI + i, h, c, g); },
+                  [&](int j, int h) { return panel_rows(x, wc * NI + j, h, c, g); });
+      }
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          float v[4];
+          panel_get4<LO, MP>(as, 16 * (wr * MI + i) + c, 16 * (wc * NI + j) + 4 * g, v);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            acc[i][j][k] = fmaf(kQ * pow2(kBe - kAe), v[k], kS * pow2(kBe - 2 * kAe) * acc[i][j][k]);
+        }
+    }
+    __syncthreads();
+    if (mine) store(1.f);
+    __syncthreads();
+    // X = p X + B X: a wave has a panel's columns, and of those 32 rows
+    for (int u0 = 0; u0 < units; u0 += kSmallWaves) {
+      const int u = u0 + wave, panel = u / XR, part = u - panel * XR;
+      char* x = xs + panel * kPanel;
+      f32x4 z[XI][XJ];
+      clear(z);
+      if (u < units) {
+#pragma unroll
+        for (int q = 0; q < MP / 32; ++q) {
+          // rows of B: 32 of its columns in two parts, or one half of a panel's 64
+          const char* bq = as + (LO ? q : q / 2) * kPanel;
+          uint4 fa[2][XI], fb[2][XJ];
+#pragma unroll
+          for (int h = 0; h < (LO ? 2 : 1); ++h) {
+#pragma unroll
+            for (int i = 0; i < XI; ++i) fa[h][i] = panel_rows(bq, part * XI + i, LO ? h : q & 1, c, g);
+#pragma unroll
+            for (int j = 0; j < XJ; ++j) fb[h][j] = panel_cols(x, LO ? j + 2 * h : j, q, c, g);
+          }
+#pragma unroll
+          for (int h = 0; h < (LO ? 3 : 1); ++h)
+#pragma unroll
+            for (int i = 0; i < XI; ++i)
+#pragma unroll
+              for (int j = 0; j < XJ; ++j) z[i][j] = mfma_f16(fb[h == 1][j], fa[h == 2][i], z[i][j]);
+        }
+#pragma unroll
+        for (int i = 0; i < XI; ++i)
+#pragma unroll
+          for (int j = 0; j < XJ; ++j) {
+            float v[4];
+            panel_get4<LO, MP>(x, 16 * (part * XI + i) + c, 16 * j + 4 * g, v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[i][j][k] = fmaf(kP, v[k], pow2(-kBe) * z[i][j][k]);
+          }
+      }
+      if (XR > 1) __syncthreads();  // (the other rows' wave of the panel has read it)
+      if (u < units)
+#pragma unroll
+        for (int i = 0; i < XI; ++i)
+#pragma unroll
+          for (int j = 0; j < XJ; ++j) {
+            const float v[4] = {z[i][j][0], z[i][j][1], z[i][j][2], z[i][j][3]};
+            panel_put4<LO, MP>(xs, 16 * (part * XI + i) + c, panel * CP + 16 * j + 4 * g, v);
+          }
+    }
+    __syncthreads();
+  }
+
+  // W along X, in W's order (a lane's values of the last product lie in 16 rows: 13 us
+  // more for 128 x 128 float32)
+  const auto x_at = [&](int r, int q) {
+    const uint16_t* o = panel_at<LO, MP>(xs, tall ? q : r, tall ? r : q);
+    float v = (float)__builtin_bit_cast(_Float16, *o);
+    if (LO) v += (float)__builtin_bit_cast(_Float16, *reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(o) ^ 64));
+    return v;
+  };
+  for (int i0 = threadIdx.x * 4; i0 < n4; i0 += NT * 4 * kFlight) {
+    typename Vec<T, 4>::raw w[kFlight];
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k)
+      if (i0 + k * NT * 4 < n4) w[k] = Vec<T, 4>::load(W + i0 + k * NT * 4);
+#pragma unroll
+    for (int k = 0; k < kFlight; ++k) {
+      const int i = i0 + k * NT * 4;
+      if (i >= n4) break;
+      int r = i / p.cols, q = i - r * p.cols;
+      float v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = fmaf(-p.us, x_at(r, q), p.ws * Vec<T, 4>::get(w[k], j));
+        if (++q == p.cols) q = 0, ++r;
+      }
+      Vec<T, 4>::put(W + i, v);
+    }
+  }
+  if ((int)threadIdx.x < left) {
+    const int i = n4 + (int)threadIdx.x, r = i / p.cols;
+    const float y[1] = {fmaf(-p.us, x_at(r, i - r * p.cols), p.ws * Elt<T>::get(W + i))};
+    Vec<T, 1>::put(W + i, y);
   }
 }
 
 // ---- host ---------------------------------------------------------------------------
-int32_t pad8(int32_t n) { return (n + 7) / 8 * 8; }
+// Blocks of a launch's last round whose tiles are cut along k, and their parts.
+constexpr int kParts = 512;       // blocks of parts at most
+// Stages of k of a part at least (1024 x 5632 float32: 507 us with 8, 522 with 4, 519 with
+// 16; 1024 x 1024 bfloat16 222, 233, 243; 512 x 2048 float32 203, 197, 192).
+constexpr int kLeastSteps = 8;
+// Sides from which symmetric products take 128 x 128 tiles (512 x 2048 float32: 203 us
+// with 64 x 64, 229 with 128; 1024 x 5632: 315 of 510 us with 64, 302 of 523 with 128).
+constexpr int kSym128 = 1024;
 
 struct Bufs {
   double* part = nullptr;
-  Planes x0{}, x1{}, a{}, b{};
+  float* sums = nullptr;
+  Stored x0{}, x1{}, a{}, b{};
   int parts = 0;
 };
 
+// The rows that a block holds a small matrix in, or 0; its LDS.
+int small_of(const hg_muon_desc* A, size_t* bytes) {
+  const bool lo = A->dtype == HG_DTYPE_F32;
+  const int32_t m = std::min(A->rows, A->cols), n = std::max(A->rows, A->cols);
+  if (A->steps == 0 || m > 128) return 0;
+  const int mp = m <= 32 ? 32 : m <= 64 ? 64 : 128, cp = lo ? 32 : 64;
+  const size_t panels = (size_t)(cdiv(n, cp) + cdiv(mp, cp)), need = panels * mp * 128;
+  if (need > 152 * 1024) return 0;  // (and 4 KB for the norm)
+  *bytes = need;
+  return mp;
+}
+
 template <class Mem>
-Planes planes(const hg_muon_desc* A, int32_t rows, int32_t cols, Mem& m) {
-  Planes p{};
+Stored stored(const hg_muon_desc* A, int32_t rows, int32_t cols, bool memory, Mem& m) {
+  Stored p{};
+  const bool lo = A->dtype == HG_DTYPE_F32;
   p.rows = rows;
   p.cols = cols;
-  p.ld = pad8(cols);
+  p.pad = lo ? (cols + 31) / 32 * 32 : (cols + 7) / 8 * 8;
+  p.ld = lo ? 2 * p.pad : p.pad;
   p.step = (int64_t)rows * p.ld;
-  p.lo = p.step * A->count;
-  p.p = m.template take<uint16_t>(p.lo * (A->dtype == HG_DTYPE_F32 ? 2 : 1));
+  if (memory) p.p = m.template take<uint16_t>(p.step * A->count);
   return p;
 }
 
 template <class Mem>
 Bufs take(const hg_muon_desc* A, Mem& m) {
   Bufs b;
+  size_t bytes = 0;
+  if (small_of(A, &bytes)) return b;
   const int64_t n = (int64_t)A->rows * A->cols;
   const int32_t k = std::min(A->rows, A->cols);
   b.parts = (int)std::min<int64_t>(kNormBlocks, std::max<int64_t>(1, cdiv(n, 1024)));
   b.part = m.template take<double>((int64_t)A->count * b.parts);
-  if (A->steps == 0) {
-    b.x0.ld = pad8(A->cols);
-    return b;
-  }
-  b.x0 = planes(A, A->rows, A->cols, m);
-  if (A->steps > 1) b.x1 = planes(A, A->rows, A->cols, m);
-  b.a = planes(A, k, k, m);
-  b.b = planes(A, k, k, m);
+  const bool any = A->steps > 0;
+  b.sums = m.template take<float>(any ? (int64_t)kParts * 128 * 128 : 0);
+  b.x0 = stored(A, A->rows, A->cols, any, m);
+  b.x1 = stored(A, A->rows, A->cols, A->steps > 1, m);
+  b.a = stored(A, k, k, any, m);
+  b.b = stored(A, k, k, any, m);
   return b;
 }
 
@@ -368,36 +872,68 @@ int check(const hg_muon_desc* A, const char* what) {
   return HG_OK;
 }
 
-template <bool AKM, bool BKM, int BM, int BN, int WM, int WN, bool LO, int EPI, class TW>
+template <class TL, bool AKM, bool BKM, bool LO, int EPI, class T>
 int product(const char* name, MuonArgs a, int count, hipStream_t s) {
-  constexpr size_t bytes = 2 * (LO ? 2 : 1) * (size_t)(BM + BN) * 64 * 2;
-  a.tiles_m = (a.M + BM - 1) / BM;
-  a.tiles_n = (a.N + BN - 1) / BN;
+  a.tiles_m = (a.M + TL::BM - 1) / TL::BM;
+  a.tiles_n = (a.N + TL::BN - 1) / TL::BN;
   a.tiles = EPI <= kEpiSymAdd ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
-  constexpr auto kernel = k_muon_product<AKM, BKM, BM, BN, WM, WN, LO, EPI, TW>;
-  HG_TRY(allow_lds<kernel>(bytes));
-  HG_LAUNCH(name, kernel, dim3((unsigned)(a.tiles * count)), dim3((BM / WM) * (BN / WN) * 64), bytes, s, a);
+  constexpr auto kernel = k_muon_product<TL, AKM, BKM, LO, EPI, T>;
+  HG_TRY(allow_lds<kernel>(TL::kLds));
+  // one block a tile in whole rounds of the chip; the rest in parts, if that helps
+  const int64_t tiles = (int64_t)a.tiles * count, slots = (int64_t)num_cus() * std::max<int64_t>(1, 160 * 1024 / (int64_t)TL::kLds);
+  const int64_t rest = tiles % slots, steps = cdiv(a.K, LO ? 32 : 64);
+  a.pieces = 1;
+  if (TL::BM * TL::BN <= 128 * 128 && rest)
+    a.pieces = (int32_t)std::max<int64_t>(1, std::min(std::min<int64_t>(slots, kParts) / rest, steps / kLeastSteps));
+  a.full = (uint32_t)(a.pieces > 1 ? tiles - rest : tiles);
+  HG_LAUNCH(name, kernel, dim3((unsigned)(a.full + (tiles - a.full) * a.pieces)), dim3(TL::NT), TL::kLds, s, a);
+  if (a.pieces > 1)
+    HG_LAUNCH("muon_join", (k_muon_join<TL, LO, EPI, T>), dim3((unsigned)(rest * TL::MI * TL::NI)), dim3(TL::NT), 0, s, a);
   return HG_OK;
+}
+
+typedef Tile<64, 64, 32, 32, 4> T64;
+typedef Tile<64, 128, 32, 64, 2> T64x128;
+typedef Tile<128, 128, 64, 64, 2> T128;
+typedef Tile<256, 256, 128, 64, 2> T256;
+
+// Symmetric products.
+template <bool AKM, bool LO, int EPI, class T>
+int symmetric(const char* name, const MuonArgs& a, int count, hipStream_t s) {
+  if (a.M >= kSym128) return product<T128, AKM, AKM, LO, EPI, T>(name, a, count, s);
+  return product<T64, AKM, AKM, LO, EPI, T>(name, a, count, s);
+}
+
+// Products with X.
+template <bool BKM, bool LO, int EPI, class T>
+int apply(const char* name, const MuonArgs& a, int count, hipStream_t s) {
+  const auto tiles = [&](int bm, int bn) { return cdiv(a.M, bm) * cdiv(a.N, bn) * count; };
+  if constexpr (!LO)
+    if (tiles(256, 256) >= 192) return product<T256, true, BKM, LO, EPI, T>(name, a, count, s);
+  if (tiles(128, 128) >= 512) return product<T128, true, BKM, LO, EPI, T>(name, a, count, s);
+  if (tiles(64, 128) >= 256) return product<T64x128, true, BKM, LO, EPI, T>(name, a, count, s);
+  return product<T64, true, BKM, LO, EPI, T>(name, a, count, s);
 }
 
 template <bool TALL, bool LO, class TW>
 int steps(const hg_muon_desc* A, const Bufs& b, void* W, hipStream_t s) {
-  Planes x = b.x0, next = b.x1;
+  Stored x = b.x0, next = b.x1;
   const int32_t k = std::min(A->rows, A->cols), len = std::max(A->rows, A->cols);
   for (int i = 0; i < A->steps; ++i) {
     MuonArgs g{};
+    g.part = b.sums;
     g.a = g.b = x;
     g.o = b.a;
     g.M = g.N = k;
     g.K = len;
     g.zs = pow2(kAe - 2 * kXe);
-    HG_TRY((product<!TALL, !TALL, 64, 64, 32, 32, LO, kEpiSym, TW>("muon_gram", g, A->count, s)));
+    HG_TRY((symmetric<!TALL, LO, kEpiSym, TW>("muon_gram", g, A->count, s)));
     g.a = g.b = g.c = b.a;
     g.o = b.b;
     g.K = k;
     g.zs = kS * pow2(kBe - 2 * kAe);
     g.cs = kQ * pow2(kBe - kAe);
-    HG_TRY((product<true, true, 64, 64, 32, 32, LO, kEpiSymAdd, TW>("muon_square", g, A->count, s)));
+    HG_TRY((symmetric<true, LO, kEpiSymAdd, TW>("muon_square", g, A->count, s)));
     g.a = TALL ? x : b.b;
     g.b = TALL ? b.b : x;
     g.c = x;
@@ -408,21 +944,51 @@ int steps(const hg_muon_desc* A, const Bufs& b, void* W, hipStream_t s) {
     g.zs = pow2(-kBe);
     g.cs = kP;
     if (i + 1 < A->steps) {
-      HG_TRY((product<true, TALL, 64, 64, 32, 32, LO, kEpiAdd, TW>("muon_apply", g, A->count, s)));
+      HG_TRY((apply<TALL, LO, kEpiAdd, TW>("muon_apply", g, A->count, s)));
       std::swap(x, next);
     } else {
       g.W = W;
       g.ws = 1.f - A->lr * A->weight_decay;
       g.us = A->lr * A->scale * pow2(-kXe);
-      HG_TRY((product<true, TALL, 64, 64, 32, 32, LO, kEpiUpdate, TW>("muon_update", g, A->count, s)));
+      HG_TRY((apply<TALL, LO, kEpiUpdate, TW>("muon_update", g, A->count, s)));
     }
   }
+  return HG_OK;
+}
+
+template <class T, int MP>
+int small(const hg_muon_desc* A, size_t bytes, T* W, const T* G, float* M, hipStream_t s) {
+  SmallArgs a{};
+  a.G = G;
+  a.M = M;
+  a.W = W;
+  a.rows = A->rows;
+  a.cols = A->cols;
+  a.m = std::min(A->rows, A->cols);
+  a.n = std::max(A->rows, A->cols);
+  a.panels = (int32_t)cdiv(a.n, sizeof(T) == 4 ? 32 : 64);
+  a.steps = A->steps;
+  a.nesterov = A->nesterov;
+  a.mu = A->mu;
+  a.eps = A->eps;
+  a.ws = 1.f - A->lr * A->weight_decay;
+  a.us = A->lr * A->scale * pow2(-kXe);
+  constexpr auto kernel = k_muon_small<T, MP>;
+  HG_TRY(allow_lds<kernel>(bytes));
+  HG_LAUNCH("muon_small", kernel, dim3((unsigned)A->count), dim3(kSmallWaves * 64), bytes, s, a);
   return HG_OK;
 }
 
 template <class T>
 int run(const hg_muon_desc* A, const Bufs& b, T* W, const T* G, float* M, hipStream_t s) {
   constexpr bool LO = sizeof(T) == 4;
+  size_t bytes = 0;
+  switch (small_of(A, &bytes)) {
+    case 32: return small<T, 32>(A, bytes, W, G, M, s);
+    case 64: return small<T, 64>(A, bytes, W, G, M, s);
+    case 128: return small<T, 128>(A, bytes, W, G, M, s);
+    default: break;
+  }
   const int64_t n = (int64_t)A->rows * A->cols;
   const dim3 grid((unsigned)b.parts, (unsigned)A->count);
   HG_LAUNCH("muon_momentum", k_muon_momentum<T>, grid, dim3(256), 0, s, G, M, n, A->mu, A->nesterov, b.part);

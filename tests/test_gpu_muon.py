@@ -43,7 +43,8 @@ def directions(seed, m, n, dtype):
 
 
 SIZES = [(1, 1), (1, 50), (50, 1), (3, 5), (16, 16), (17, 64), (64, 64), (65, 63), (63, 200), (128, 128), (129, 257), (200, 517),
-         (517, 200), (256, 1000), (1030, 70), (300, 300), (640, 1111)]
+         (517, 200), (256, 1000), (1030, 70), (300, 300), (640, 1111), (32, 900), (31, 33), (64, 700), (128, 350), (100, 97),
+         (1100, 90), (33, 1400), (1500, 140)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

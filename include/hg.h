@@ -693,8 +693,8 @@ int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, const hg_heads*
  *   rows' = rows + hg_linear(y);   W = hg_muon_step(W, dW)
  * Rows of these operators need no alignment but their values' own: an element
  * (sequence b, token t, channel c) lies at p[b * batch + t * token + c] of an
- * hg_heads whose head stride is not used.  Strides are at least 0 and below 2^40,
- * those of outputs keep the rows apart.  Outputs must not overlap inputs or each
+ * hg_heads whose head stride is not used.  Strides are at least 0 and at most 2^40
+ * (a token's of the recurrence 2^21), those of outputs keep the rows apart.  Outputs must not overlap inputs or each
  * other; views of one packed buffer may interleave.  Workspaces are 16-byte
  * aligned.  Asynchronous and deterministic.
  *

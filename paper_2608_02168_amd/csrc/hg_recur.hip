@@ -22,6 +22,7 @@
 // by a thread that starts earlier: two threads then compute and write the same
 // values of the same addresses.
 #include <cmath>
+#include <type_traits>
 
 #include "hg_rows4.h"
 
@@ -32,7 +33,7 @@ constexpr int V = 4;             // channels of a thread
 constexpr int CL = 16;           // threads side by side
 constexpr int TW = 64 / CL;      // runs of tokens in a wave
 constexpr int kSlab = CL * V;    // channels of a block
-constexpr int kNW = 8;           // waves of a block
+constexpr int kNW = 4;           // waves of a block
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct RecurArgs {
@@ -60,16 +61,17 @@ __device__ __forceinline__ float slope_of(float decay, float rate) {
   return rate * kLog2e * (fmaxf(decay, 0.f) + log1pf(expf(-fabsf(decay))));
 }
 
-// 1 - a^2 for a = 2^l: near a = 1 by the series of -(e^y - 1), y = 2 l ln 2, to y^6
-// (relative error 5e-8 at y = -1/4, where 1 - a a has 4e-7).
+// 1 - a^2 for a = 2^l: near a = 1 by the series of 1 - e^y, y = 2 l ln 2, to y^6
+// (relative error 5e-8 at y = -1/4, where 1 - a a has 4e-7).  bfloat16 rows take it
+// too: the states are float32.
 __device__ __forceinline__ float rest_of(float l, float a) {
-  const float y = l * 1.3862943611198906f;
-  float p = fmaf(y, 1.f / 720.f, 1.f / 120.f);
-  p = fmaf(y, p, 1.f / 24.f);
-  p = fmaf(y, p, 1.f / 6.f);
-  p = fmaf(y, p, 0.5f);
-  p = fmaf(y, p, 1.f);
-  return y > -0.25f ? -y * p : fmaf(-a, a, 1.f);
+  constexpr float y = 1.3862943611198906f;  // y / l
+  float p = fmaf(l, -y * y * y * y * y * y / 720.f, -y * y * y * y * y / 120.f);
+  p = fmaf(l, p, -y * y * y * y / 24.f);
+  p = fmaf(l, p, -y * y * y / 6.f);
+  p = fmaf(l, p, -y * y / 2.f);
+  p = fmaf(l, p, -y);
+  return l > -0.25f / y ? l * p : fmaf(-a, a, 1.f);
 }
 
 // The steps of the runs before this thread's in its wave (sign 1: the ranks below), and
@@ -131,12 +133,17 @@ __device__ __forceinline__ void compose(Step& s, float (&y)[V], float (&at)[V], 
   }
 }
 
-// What a block (WAVE: a wave) works on.
+// What a block (WAVE: a wave) works on.  All but the channels is the same in a wave.
 struct Place {
   int64_t b, t_beg, t_end, out_end;  // tokens of the segment: inside the sequence, and with the rows past it
   int32_t seg, c0;                   // first channel of the thread
-  bool on;                           // the thread has channels
+  bool on;                           // no thread before has the same channels
 };
+__device__ __forceinline__ int64_t len_of(const RecurArgs& a, int64_t b) {
+  if (!a.lens) return a.t;
+  const int32_t n = a.lens[b];
+  return n < 0 ? 0 : (n < a.t ? n : a.t);
+}
 template <bool WAVE>
 __device__ __forceinline__ Place place_of(const RecurArgs& a, int wave, int col) {
   Place p;
@@ -151,11 +158,7 @@ __device__ __forceinline__ Place place_of(const RecurArgs& a, int wave, int col)
   const int c = (int)slab * kSlab + col * V;
   p.on = c < a.width;
   p.c0 = c < a.width - V ? c : a.width - V;
-  int64_t len = a.t;
-  if (a.lens && p.b < a.batch) {
-    const int32_t n = a.lens[p.b];
-    len = n < 0 ? 0 : (n < a.t ? n : a.t);
-  }
+  const int64_t len = p.b < a.batch ? len_of(a, p.b) : 0;
   p.t_beg = p.seg * a.seg_len;
   p.out_end = p.t_beg + a.seg_len < a.t ? p.t_beg + a.seg_len : a.t;
   p.t_end = len < p.out_end ? len : p.out_end;
@@ -163,41 +166,52 @@ __device__ __forceinline__ Place place_of(const RecurArgs& a, int wave, int col)
   return p;
 }
 
-template <class T>
-__device__ __forceinline__ T* row(const Rows& x, const Place& p, int64_t t) {
-  return static_cast<T*>(x.p) + p.b * x.sb + t * x.st + p.c0;
-}
-
-// K rows of one operand from token t on, of which those in [lo, hi) are read.
-template <class T, int K>
-__device__ __forceinline__ void load(typename Quad<T>::raw (&w)[K], const Rows& x, const Place& p, int64_t t, int64_t lo,
-                                     int64_t hi) {
-  const T* q = row<T>(x, p, t);
-  if (p.on && t >= lo && t + K <= hi) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) w[k] = Quad<T>::load(q + k * x.st);
-  } else {
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (p.on && t + k >= lo && t + k < hi) w[k] = Quad<T>::load(q + k * x.st);
+// One operand's rows of a sequence: an address that is the same in a wave and a
+// thread's 32-bit offset from it, so that a row costs no vector instruction but its
+// load (Off 32 bits: a block's tile is below 2^32 bytes, kMaxToken).
+template <class T, class Off = uint32_t>
+struct Stream {
+  const char* base;  // token 0
+  int64_t row;       // bytes between tokens
+  Off off;           // of the thread, from the tile's first token
+  __device__ __forceinline__ Stream(const Rows& x, const Place& p, Off skip)
+      : base(static_cast<const char*>(x.p) + p.b * x.sb * (int64_t)sizeof(T)), row(x.st * (int64_t)sizeof(T)),
+        off(skip * (Off)(x.st * (int64_t)sizeof(T)) + (Off)p.c0 * (Off)sizeof(T)) {}
+  // the thread's token k of the tile from token ts on
+  __device__ __forceinline__ T* at(int64_t ts, int k) const {
+    return reinterpret_cast<T*>(const_cast<char*>(base + (ts + k) * row + off));
   }
+};
+
+// K rows of one operand, the thread's tokens t .. of the tile from ts on; FULL: all
+// are inside, else those in [lo, hi) are read.
+template <class T, int K, bool FULL, class Off>
+__device__ __forceinline__ void load(typename Quad<T>::raw (&w)[K], const Stream<T, Off>& x, int64_t ts, int64_t t, int64_t lo,
+                                     int64_t hi) {
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if (FULL || (t + k >= lo && t + k < hi)) w[k] = Quad<T>::load(x.at(ts, k));
 }
 
+// The rows past a sequence's end as zeros.
 template <class T>
 __device__ __forceinline__ void zero_rows(const Rows& x, const Place& p, int rank, int ranks) {
   const float z[V] = {0.f, 0.f, 0.f, 0.f};
+  T* o = static_cast<T*>(x.p) + p.b * x.sb + p.c0;
   if (p.on)
-    for (int64_t t = p.t_end + rank; t < p.out_end; t += ranks) Quad<T>::put(row<T>(x, p, t), z);
+    for (int64_t t = p.t_end + rank; t < p.out_end; t += ranks) Quad<T>::put(o + t * x.st, z);
 }
+
+template <bool B>
+using Bool = std::integral_constant<bool, B>;
 
 __device__ __forceinline__ void load_state(const float* s, const RecurArgs& a, const Place& p, float (&y)[V]) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) y[j] = s && p.on ? s[p.b * a.width + p.c0 + j] : 0.f;
+  for (int j = 0; j < V; ++j) y[j] = s ? s[p.b * a.width + p.c0 + j] : 0.f;
 }
 
 // The steps of the segments [from, to) in their order, on y.
 __device__ __forceinline__ void run_segments(const RecurArgs& a, const Place& p, int from, int to, int dir, float (&y)[V]) {
-  if (!p.on) return;
   const float* s = a.sums + p.b * a.segs * 2 * (int64_t)a.width + p.c0;
   for (int q = from; q != to; q += dir) {
     const float* f = s + q * 2 * (int64_t)a.width;
@@ -209,25 +223,27 @@ __device__ __forceinline__ void run_segments(const RecurArgs& a, const Place& p,
 template <class T, int K, bool WAVE>
 __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
   __shared__ __align__(16) float lds[WAVE ? 4 : 2 * kNW * 2 * kSlab];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % CL, rank = lane / CL;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
   constexpr int kTile = (WAVE ? 1 : kNW) * TW * K;
   const Place p = place_of<WAVE>(a, wave, col);
   if (WAVE && p.b >= a.batch) return;
   const int run = WAVE ? rank : wave * TW + rank;
   float slope[V], y[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) slope[j] = p.on ? -slope_of(a.decay[p.c0 + j], a.rate) : 0.f;
+  for (int j = 0; j < V; ++j) slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
   load_state(a.s_in, a, p, y);
   if (!WAVE && p.seg) run_segments(a, p, 0, p.seg, 1, y);
+  const Stream<T> sx(a.x, p, run * K), sr(a.r, p, run * K), si(a.i, p, run * K), sh(a.h, p, run * K);
   typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {};
-  auto fetch = [&](int64_t t) {
-    load<T, K>(rr, a.r, p, t, p.t_beg, p.t_end);
-    load<T, K>(ri, a.i, p, t, p.t_beg, p.t_end);
-    load<T, K>(rx, a.x, p, t, p.t_beg, p.t_end);
+  auto fetch = [&](auto full, int64_t ts) {
+    constexpr bool FULL = decltype(full)::value;
+    load<T, K, FULL>(rr, sr, ts, ts + run * K, p.t_beg, p.t_end);
+    load<T, K, FULL>(ri, si, ts, ts + run * K, p.t_beg, p.t_end);
+    load<T, K, FULL>(rx, sx, ts, ts + run * K, p.t_beg, p.t_end);
   };
-  fetch(p.t_beg + run * K);
   int odd = 0;
-  for (int64_t ts = p.t_beg; ts < p.t_end; ts += kTile, odd ^= 1) {
+  auto tile = [&](auto full, int64_t ts) {
+    constexpr bool FULL = decltype(full)::value;
     const int64_t t0 = ts + run * K;
     float fa[K][V], fu[K][V];
     Step s;
@@ -235,7 +251,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
     for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool in = t0 + k < p.t_end;
+      const bool in = FULL || t0 + k < p.t_end;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float l = slope[j] * sigm(Quad<T>::get(rr[k], j));
@@ -247,16 +263,31 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
         s.b[j] = fmaf(fa[k][j], s.b[j], fu[k][j]);
       }
     }
-    if (ts + kTile < p.t_end) fetch(t0 + kTile);
+    if (ts + 2 * kTile <= p.t_end) {
+      fetch(Bool<true>{}, ts + kTile);
+    } else if (ts + kTile < p.t_end) {
+      fetch(Bool<false>{}, ts + kTile);
+    }
     float at[V];
     compose<WAVE>(s, y, at, lds + (WAVE ? 0 : odd * kNW * 2 * kSlab), wave, rank, col);
+    odd ^= 1;
+    if (p.on) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+      for (int k = 0; k < K; ++k) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) at[j] = fmaf(fa[k][j], at[j], fu[k][j]);
-      if (p.on && t0 + k < p.t_end) Quad<T>::put(row<T>(a.h, p, t0 + k), at);
+        for (int j = 0; j < V; ++j) at[j] = fmaf(fa[k][j], at[j], fu[k][j]);
+        if (FULL || t0 + k < p.t_end) Quad<T>::put(sh.at(ts, k), at);
+      }
     }
+  };
+  int64_t ts = p.t_beg;
+  if (ts + kTile <= p.t_end) {
+    fetch(Bool<true>{}, ts);
+  } else {
+    fetch(Bool<false>{}, ts);
   }
+  for (; ts + kTile <= p.t_end; ts += kTile) tile(Bool<true>{}, ts);
+  if (ts < p.t_end) tile(Bool<false>{}, ts);
   zero_rows<T>(a.h, p, run, WAVE ? TW : kNW * TW);
   if (a.s_out && p.on && run == 0 && p.seg == a.segs - 1) {
 #pragma unroll
@@ -270,67 +301,74 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
 template <class T, int K, bool BACK>
 __global__ void __launch_bounds__(kNW * 64) k_recur_sums(const RecurArgs a) {
   __shared__ __align__(16) float lds[kNW * 2 * kSlab];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % CL, rank = lane / CL;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
   const Place p = place_of<false>(a, wave, col);
   // (the steps of the last segment of a walk lead nowhere)
   if (p.seg == (BACK ? 0 : a.segs - 1)) return;
-  const int run = wave * TW + rank;
+  // run q of the segment in the walk's order: tokens [beg + q per, ..) forward, backward down from end - q per
+  const int q = wave * TW + rank;
   const int64_t n = p.t_end - p.t_beg, per = ((n + kNW * TW - 1) / (kNW * TW) + K - 1) / K * K;
-  int64_t lo, hi;
-  if constexpr (BACK) {
-    hi = p.t_end - run * per;
-    lo = hi - per;
-  } else {
-    lo = p.t_beg + run * per;
-    hi = lo + per;
-  }
-  lo = lo < p.t_beg ? p.t_beg : lo;
-  hi = hi > p.t_end ? p.t_end : hi;
+  const int64_t first = BACK ? p.t_end - kNW * TW * per : p.t_beg;  // (may be before the segment)
+  const int64_t skip = (BACK ? kNW * TW - 1 - q : q) * per;
+  const Stream<T, int64_t> sx(BACK ? a.dh : a.x, p, skip), sr(a.r, p, skip), si(a.i, p, skip);
   float slope[V];
   Step s;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    slope[j] = p.on ? -slope_of(a.decay[p.c0 + j], a.rate) : 0.f;
+    slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
     s.a[j] = 1.f;
     s.b[j] = 0.f;
   }
   typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {};
-  auto fetch = [&](int64_t t) {
-    load<T, K>(rr, a.r, p, t, lo, hi);
-    if constexpr (!BACK) load<T, K>(ri, a.i, p, t, lo, hi);
-    load<T, K>(rx, BACK ? a.dh : a.x, p, t, lo, hi);
+  auto fetch = [&](auto full, int64_t ts) {
+    constexpr bool FULL = decltype(full)::value;
+    load<T, K, FULL>(rr, sr, ts, ts + skip, p.t_beg, p.t_end);
+    if constexpr (!BACK) load<T, K, FULL>(ri, si, ts, ts + skip, p.t_beg, p.t_end);
+    load<T, K, FULL>(rx, sx, ts, ts + skip, p.t_beg, p.t_end);
   };
-  const int64_t first = BACK ? hi - K : lo, step = BACK ? -K : K;
-  fetch(first);
-  for (int64_t t = first; BACK ? t + K > lo : t < hi; t += step) {
-    float fa[K][V], fu[K][V];
+  // whether all runs' tokens of a round lie inside: only the last run forward, backward the first, may not
+  const bool whole = per * kNW * TW == n;
+  const auto walk = [&](auto full) {
+    constexpr bool FULL = decltype(full)::value;
+    const int64_t step = BACK ? -K : K;
+    int64_t ts = BACK ? first + per - K : first;
+    if (per > 0) fetch(full, ts);
+    for (int64_t i = 0; i < per; i += K, ts += step) {
+      float fa[K][V], fu[K][V];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const bool in = t + k >= lo && t + k < hi;
+      for (int k = 0; k < K; ++k) {
+        const int64_t t = ts + skip + k;
+        const bool in = FULL || (t >= p.t_beg && t < p.t_end);
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float l = slope[j] * sigm(Quad<T>::get(rr[k], j));
-        const float f = __builtin_amdgcn_exp2f(l);
-        float u = Quad<T>::get(rx[k], j);
-        if constexpr (BACK) {
-          u *= f;
-        } else {
-          u *= __builtin_amdgcn_sqrtf(rest_of(l, f)) * sigm(Quad<T>::get(ri[k], j));
+        for (int j = 0; j < V; ++j) {
+          const float l = slope[j] * sigm(Quad<T>::get(rr[k], j));
+          const float f = __builtin_amdgcn_exp2f(l);
+          float u = Quad<T>::get(rx[k], j);
+          if constexpr (BACK) {
+            u *= f;
+          } else {
+            u *= __builtin_amdgcn_sqrtf(rest_of(l, f)) * sigm(Quad<T>::get(ri[k], j));
+          }
+          fa[k][j] = in ? f : 1.f;
+          fu[k][j] = in ? u : 0.f;
         }
-        fa[k][j] = in ? f : 1.f;
-        fu[k][j] = in ? u : 0.f;
+      }
+      if (i + K < per) fetch(full, ts + step);
+#pragma unroll
+      for (int o = 0; o < K; ++o) {
+        const int k = BACK ? K - 1 - o : o;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          s.a[j] *= fa[k][j];
+          s.b[j] = fmaf(fa[k][j], s.b[j], fu[k][j]);
+        }
       }
     }
-    fetch(t + step);
-#pragma unroll
-    for (int q = 0; q < K; ++q) {
-      const int k = BACK ? K - 1 - q : q;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        s.a[j] *= fa[k][j];
-        s.b[j] = fmaf(fa[k][j], s.b[j], fu[k][j]);
-      }
-    }
+  };
+  if (whole) {
+    walk(Bool<true>{});
+  } else {
+    walk(Bool<false>{});
   }
   // the whole segment's step: the value that leaves it from 0, and the product of its factors
   Step before;
@@ -340,12 +378,12 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_sums(const RecurArgs a) {
     *reinterpret_cast<f32x4*>(lds + wave * 2 * kSlab + kSlab + col * V) = f32x4{s.b[0], s.b[1], s.b[2], s.b[3]};
   }
   __syncthreads();
-  if (run == 0 && p.on) {
+  if (q == 0 && p.on) {
     f32x4 ya = f32x4{1.f, 1.f, 1.f, 1.f}, yb = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int q = 0; q < kNW; ++q) {
-      const f32x4 qa = *reinterpret_cast<const f32x4*>(lds + q * 2 * kSlab + col * V);
-      const f32x4 qb = *reinterpret_cast<const f32x4*>(lds + q * 2 * kSlab + kSlab + col * V);
+    for (int w = 0; w < kNW; ++w) {
+      const f32x4 qa = *reinterpret_cast<const f32x4*>(lds + w * 2 * kSlab + col * V);
+      const f32x4 qb = *reinterpret_cast<const f32x4*>(lds + w * 2 * kSlab + kSlab + col * V);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         yb[j] = fmaf(qa[j], yb[j], qb[j]);
@@ -363,49 +401,48 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_sums(const RecurArgs a) {
 template <class T, int K, bool WAVE>
 __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32_t stride) {
   __shared__ __align__(16) float lds[2 * kNW * 2 * kSlab];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane % CL, rank = lane / CL;
-  constexpr int kTile = (WAVE ? 1 : kNW) * TW * K;
-  const int run = WAVE ? rank : wave * TW + rank;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
+  constexpr int kRuns = (WAVE ? 1 : kNW) * TW, kTile = kRuns * K;
+  const int run = WAVE ? rank : wave * TW + rank, skip = (kRuns - 1 - run) * K;  // the first run is the tile's last
   Place p = place_of<WAVE>(a, wave, col);
   float slope[V], sum[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    slope[j] = p.on ? -slope_of(a.decay[p.c0 + j], a.rate) : 0.f;
+    slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
     sum[j] = 0.f;
   }
   for (; p.b < a.batch; p.b += stride) {
-    if (WAVE && a.lens) {
-      const int32_t n = a.lens[p.b];
-      p.t_end = n < 0 ? 0 : (n < a.t ? n : a.t);
-    }
+    if (WAVE) p.t_end = len_of(a, p.b);
     float y[V];
     load_state(a.s_in, a, p, y);
     if (!WAVE && p.seg < a.segs - 1) run_segments(a, p, a.segs - 1, p.seg, -1, y);
+    const Stream<T> sx(a.x, p, skip), sr(a.r, p, skip), si(a.i, p, skip), sh(a.h, p, skip), sg(a.dh, p, skip), ox(a.dx, p, skip),
+        orr(a.dr, p, skip), oi(a.di, p, skip);
     typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {}, rh[K] = {}, rg[K] = {};
-    auto fetch = [&](int64_t t) {
-      load<T, K>(rr, a.r, p, t, p.t_beg, p.t_end);
-      load<T, K>(rg, a.dh, p, t, p.t_beg, p.t_end);
-      load<T, K>(ri, a.i, p, t, p.t_beg, p.t_end);
-      load<T, K>(rx, a.x, p, t, p.t_beg, p.t_end);
-      // row k: h before token t + k
-      load<T, K>(rh, a.h, p, t - 1, p.t_beg ? p.t_beg - 1 : 0, p.t_end - 1);
+    // the tile of tokens ts .. ts + kTile - 1 (row k of rh: h before the thread's token k); FULL: it begins after t_beg
+    auto fetch = [&](auto full, int64_t ts) {
+      constexpr bool FULL = decltype(full)::value;
+      load<T, K, FULL>(rr, sr, ts, ts + skip, p.t_beg, p.t_end);
+      load<T, K, FULL>(rg, sg, ts, ts + skip, p.t_beg, p.t_end);
+      load<T, K, FULL>(ri, si, ts, ts + skip, p.t_beg, p.t_end);
+      load<T, K, FULL>(rx, sx, ts, ts + skip, p.t_beg, p.t_end);
+      load<T, K, FULL>(rh, sh, ts - 1, ts - 1 + skip, p.t_beg ? p.t_beg - 1 : 0, p.t_end);
     };
-    // the tiles from the last token down, each run below the one before
-    fetch(p.t_end - (run + 1) * K);
     int odd = 0;
-    for (int64_t te = p.t_end; te > p.t_beg; te -= kTile, odd ^= 1) {
-      const int64_t t0 = te - (run + 1) * K;
-      float sr[K][V], fa[K][V], gh[K][V];
+    auto tile = [&](auto full, int64_t ts) {
+      constexpr bool FULL = decltype(full)::value;
+      const int64_t t0 = ts + skip;
+      float fs[K][V], fa[K][V], gh[K][V];
       Step s;
 #pragma unroll
       for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
 #pragma unroll
       for (int k = K - 1; k >= 0; --k) {
-        const bool in = t0 + k >= p.t_beg;
+        const bool in = FULL || t0 + k >= p.t_beg;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          sr[k][j] = sigm(Quad<T>::get(rr[k], j));
-          const float f = __builtin_amdgcn_exp2f(slope[j] * sr[k][j]);
+          fs[k][j] = sigm(Quad<T>::get(rr[k], j));
+          const float f = __builtin_amdgcn_exp2f(slope[j] * fs[k][j]);
           fa[k][j] = in ? f : 1.f;
           gh[k][j] = in ? Quad<T>::get(rg[k], j) : 0.f;
           s.b[j] = fa[k][j] * (s.b[j] + gh[k][j]);
@@ -414,32 +451,48 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
       }
       float at[V];
       compose<WAVE>(s, y, at, lds + (WAVE ? 0 : odd * kNW * 2 * kSlab), wave, rank, col);
+      odd ^= 1;
 #pragma unroll
       for (int k = K - 1; k >= 0; --k) {
-        if (!p.on || t0 + k < p.t_beg) continue;
-        float hb[V], ox[V], oi[V], orr[V];
+        if (!FULL && t0 + k < p.t_beg) continue;
+        float hb[V], vx[V], vi[V], vr[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) hb[j] = Quad<T>::get(rh[k], j);
-        if (t0 + k == 0) load_state(a.s_first, a, p, hb);
+        if (!FULL && t0 + k == 0) load_state(a.s_first, a, p, hb);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float f = fa[k][j], l = slope[j] * sr[k][j], g = gh[k][j] + at[j];
+          const float f = fa[k][j], l = slope[j] * fs[k][j], g = gh[k][j] + at[j];
           at[j] = f * g;
-          // (1 - a^2 below 2^-120, where l = 0, so that its root's inverse is finite)
+          // (1 - a^2 at least 2^-120, below which l = 0, so that its root's inverse is finite)
           const float m = rest_of(l, f), iq = __builtin_amdgcn_rsqf(fmaxf(m, 7.5e-37f)), q = m * iq;
-          const float si = sigm(Quad<T>::get(ri[k], j)), x = Quad<T>::get(rx[k], j), gs = g * si;
-          ox[j] = gs * q;
-          oi[j] = ox[j] * x * (1.f - si);
-          const float dl = f * (g * hb[j] - gs * x * f * iq);
-          sum[j] = fmaf(dl, sr[k][j], sum[j]);
-          orr[j] = dl * (l * 0.69314718055994531f) * (1.f - sr[k][j]);
+          const float sg1 = sigm(Quad<T>::get(ri[k], j)), x = Quad<T>::get(rx[k], j), gs = g * sg1;
+          vx[j] = gs * q;
+          vi[j] = vx[j] * x * (1.f - sg1);
+          const float dl = f * fmaf(g, hb[j], -gs * x * f * iq);
+          sum[j] = fmaf(dl, fs[k][j], sum[j]);
+          vr[j] = dl * (l * 0.69314718055994531f) * (1.f - fs[k][j]);
         }
-        Quad<T>::put(row<T>(a.dx, p, t0 + k), ox);
-        Quad<T>::put(row<T>(a.di, p, t0 + k), oi);
-        Quad<T>::put(row<T>(a.dr, p, t0 + k), orr);
+        if (p.on) {
+          Quad<T>::put(ox.at(ts, k), vx);
+          Quad<T>::put(oi.at(ts, k), vi);
+          Quad<T>::put(orr.at(ts, k), vr);
+        }
       }
-      if (te - kTile > p.t_beg) fetch(t0 - kTile);
+      // the tile before; one that holds token 0 is not full (its h before comes from the state)
+      if (ts - kTile > p.t_beg) {
+        fetch(Bool<true>{}, ts - kTile);
+      } else if (ts > p.t_beg) {
+        fetch(Bool<false>{}, ts - kTile);
+      }
+    };
+    int64_t ts = p.t_end - kTile;
+    if (ts > p.t_beg) {
+      fetch(Bool<true>{}, ts);
+    } else {
+      fetch(Bool<false>{}, ts);
     }
+    for (; ts > p.t_beg; ts -= kTile) tile(Bool<true>{}, ts);
+    if (ts + kTile > p.t_beg) tile(Bool<false>{}, ts);
     const int ranks = WAVE ? TW : kNW * TW;
     zero_rows<T>(a.dx, p, run, ranks);
     zero_rows<T>(a.di, p, run, ranks);
@@ -453,10 +506,10 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
   if (!a.part) return;
   // the block's sums of its runs, in order
   __syncthreads();
-  float* sh = lds;  // [NW * TW][slab]
+  float* all = lds;  // [NW * TW][slab]
   static_assert(kNW * TW * kSlab <= 2 * kNW * 2 * kSlab, "the sums fit the block's LDS");
 #pragma unroll
-  for (int j = 0; j < V; ++j) sh[(wave * TW + rank) * kSlab + col * V + j] = sum[j];
+  for (int j = 0; j < V; ++j) all[(wave * TW + rank) * kSlab + col * V + j] = sum[j];
   __syncthreads();
   const uint32_t rest = blockIdx.x / (uint32_t)a.slabs, slab = blockIdx.x - rest * (uint32_t)a.slabs;
   for (int c = threadIdx.x; c < kSlab; c += kNW * 64) {
@@ -465,7 +518,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
     // the thread that has channel ch: the last ones start at width - V
     const int own = c / V, c0 = (int)slab * kSlab + own * V, shift = c0 < a.width - V ? 0 : c0 - (a.width - V);
     float s = 0.f;
-    for (int q = 0; q < kNW * TW; ++q) s += sh[q * kSlab + c + shift];
+    for (int q = 0; q < kNW * TW; ++q) s += all[q * kSlab + c + shift];
     a.part[(int64_t)rest * a.width + ch] = s;
   }
 }
@@ -517,9 +570,13 @@ __global__ void __launch_bounds__(256)
 }
 
 // ---- host ---------------------------------------------------------------------------
-template <class T>
-constexpr int fwd_run() { return sizeof(T) == 4 ? 4 : 8; }
-constexpr int kBwdRun = 4;
+constexpr int64_t kMaxToken = (int64_t)1 << 21;  // (a tile has at most 2^8 tokens of 4-byte values)
+// Tokens of a thread's run.  Fewer registers and more waves against the shuffles and
+// LDS of a tile: one history of 65521 tokens of 1024 channels, bfloat16, 219 us with 4,
+// 236 with 8; backward of 8 x 2048 tokens of 2048 channels 121 us with 2, 127 with 4; a
+// wave for each of 8192 histories of 24 tokens, float32, 62 us with 1, 67 with 2.
+constexpr int fwd_run(bool wave) { return wave ? 2 : 4; }
+constexpr int bwd_run(bool wave) { return wave ? 1 : 2; }
 
 struct Split {
   bool wave;         // a wave for each sequence
@@ -542,8 +599,8 @@ Split split_of(const hg_recur_desc* A, bool bwd) {
     s.stride = (int32_t)(s.rows * kNW);
     return s;
   }
-  const int64_t tile = (int64_t)kNW * TW * (bwd ? kBwdRun : A->dtype == HG_DTYPE_F32 ? fwd_run<float>() : fwd_run<bf16_t>());
-  const int64_t n = std::min<int64_t>(512 / std::max<int64_t>(pairs, 1), A->t / (4 * tile));
+  const int64_t tile = (int64_t)kNW * TW * (bwd ? bwd_run(false) : fwd_run(false));
+  const int64_t n = std::min<int64_t>(1024 / std::max<int64_t>(pairs, 1), A->t / (4 * tile));
   if (n > 1) {
     s.seg_len = cdiv(cdiv(A->t, n), tile) * tile;
     s.segs = (int32_t)cdiv(A->t, s.seg_len);
@@ -578,6 +635,15 @@ int check(const hg_recur_desc* A, const char* what) {
   return HG_OK;
 }
 
+// The rows of a call; a single token's stride is never walked.
+int rows_in(const hg_recur_desc* A, const char* what, const hg_heads* x, const char* name, bool out, Rows* r) {
+  HG_TRY(check_rows(what, x, name, out, A->batch, A->t, A->width, A->dtype));
+  if (A->t > 1 && x->token > kMaxToken)
+    return fail(HG_ERR_UNSUPPORTED, "%s: tokens of %s are %lld apart", what, name, (long long)x->token);
+  *r = Rows{x->p, x->batch, A->t > 1 ? x->token : 0};
+  return HG_OK;
+}
+
 RecurArgs args_of(const hg_recur_desc* A, const Split& s, const float* decay, const int32_t* lens) {
   RecurArgs a{};
   a.decay = decay;
@@ -594,13 +660,12 @@ RecurArgs args_of(const hg_recur_desc* A, const Split& s, const float* decay, co
 
 template <class T>
 int launch_fwd(const RecurArgs& a, const Split& s, hipStream_t st) {
-  constexpr int K = fwd_run<T>();
   const dim3 grid((unsigned)(s.rows * s.slabs)), block(kNW * 64);
-  if (s.segs > 1) HG_LAUNCH("recur_sums", (k_recur_sums<T, K, false>), grid, block, 0, st, a);
+  if (s.segs > 1) HG_LAUNCH("recur_sums", (k_recur_sums<T, fwd_run(false), false>), grid, block, 0, st, a);
   if (s.wave) {
-    HG_LAUNCH("recur", (k_recur_fwd<T, K, true>), grid, block, 0, st, a);
+    HG_LAUNCH("recur", (k_recur_fwd<T, fwd_run(true), true>), grid, block, 0, st, a);
   } else {
-    HG_LAUNCH("recur", (k_recur_fwd<T, K, false>), grid, block, 0, st, a);
+    HG_LAUNCH("recur", (k_recur_fwd<T, fwd_run(false), false>), grid, block, 0, st, a);
   }
   return HG_OK;
 }
@@ -608,11 +673,11 @@ int launch_fwd(const RecurArgs& a, const Split& s, hipStream_t st) {
 template <class T>
 int launch_bwd(const RecurArgs& a, const Split& s, hipStream_t st) {
   const dim3 grid((unsigned)(s.rows * s.slabs)), block(kNW * 64);
-  if (s.segs > 1) HG_LAUNCH("recur_bwd_sums", (k_recur_sums<T, kBwdRun, true>), grid, block, 0, st, a);
+  if (s.segs > 1) HG_LAUNCH("recur_bwd_sums", (k_recur_sums<T, bwd_run(false), true>), grid, block, 0, st, a);
   if (s.wave) {
-    HG_LAUNCH("recur_bwd", (k_recur_bwd<T, kBwdRun, true>), grid, block, 0, st, a, s.stride);
+    HG_LAUNCH("recur_bwd", (k_recur_bwd<T, bwd_run(true), true>), grid, block, 0, st, a, s.stride);
   } else {
-    HG_LAUNCH("recur_bwd", (k_recur_bwd<T, kBwdRun, false>), grid, block, 0, st, a, 1);
+    HG_LAUNCH("recur_bwd", (k_recur_bwd<T, bwd_run(false), false>), grid, block, 0, st, a, 1);
   }
   return HG_OK;
 }
@@ -641,10 +706,11 @@ extern "C" int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_
                             float* state_out, void* ws, size_t ws_bytes, void* stream) {
   const char* what = "hg_recur_fwd";
   HG_TRY(check(A, what));
-  HG_TRY(check_rows(what, x, "x", false, A->batch, A->t, A->width, A->dtype));
-  HG_TRY(check_rows(what, r, "r", false, A->batch, A->t, A->width, A->dtype));
-  HG_TRY(check_rows(what, i, "i", false, A->batch, A->t, A->width, A->dtype));
-  HG_TRY(check_rows(what, h, "h", true, A->batch, A->t, A->width, A->dtype));
+  Rows rx, rr, ri, rh;
+  HG_TRY(rows_in(A, what, x, "x", false, &rx));
+  HG_TRY(rows_in(A, what, r, "r", false, &rr));
+  HG_TRY(rows_in(A, what, i, "i", false, &ri));
+  HG_TRY(rows_in(A, what, h, "h", true, &rh));
   if (A->batch == 0) return HG_OK;
   if (!decay) return fail(HG_ERR_ARG, "%s: null decay", what);
   for (const hg_heads* v : {x, r, i})
@@ -657,10 +723,10 @@ extern "C" int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   const Split s = split_of(A, false);
   RecurArgs a = args_of(A, s, decay, lens);
   a.sums = take(A, false, m).sums;
-  a.x = rows_of(x);
-  a.r = rows_of(r);
-  a.i = rows_of(i);
-  a.h = rows_of(h);
+  a.x = rx;
+  a.r = rr;
+  a.i = ri;
+  a.h = rh;
   a.s_in = state;
   a.s_out = state_out;
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -677,7 +743,8 @@ extern "C" int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   if (accumulate != 0 && accumulate != 1) return fail(HG_ERR_ARG, "%s: accumulate %d", what, accumulate);
   const hg_heads* all[8] = {x, r, i, h, dh, dx, dr, di};
   const char* names[8] = {"x", "r", "i", "h", "dh", "dx", "dr", "di"};
-  for (int k = 0; k < 8; ++k) HG_TRY(check_rows(what, all[k], names[k], k >= 5, A->batch, A->t, A->width, A->dtype));
+  Rows in[8];
+  for (int k = 0; k < 8; ++k) HG_TRY(rows_in(A, what, all[k], names[k], k >= 5, &in[k]));
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (A->batch == 0) return ddecay && !accumulate ? fill_f32(ddecay, 0.f, A->width, st) : HG_OK;
   if (!decay) return fail(HG_ERR_ARG, "%s: null decay", what);
@@ -696,14 +763,14 @@ extern "C" int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   RecurArgs a = args_of(A, s, decay, lens);
   a.sums = b.sums;
   a.part = ddecay ? b.part : nullptr;
-  a.x = rows_of(x);
-  a.r = rows_of(r);
-  a.i = rows_of(i);
-  a.h = rows_of(h);
-  a.dh = rows_of(dh);
-  a.dx = rows_of(dx);
-  a.dr = rows_of(dr);
-  a.di = rows_of(di);
+  a.x = in[0];
+  a.r = in[1];
+  a.i = in[2];
+  a.h = in[3];
+  a.dh = in[4];
+  a.dx = in[5];
+  a.dr = in[6];
+  a.di = in[7];
   a.s_first = state;
   a.s_in = dstate_out;
   a.s_out = dstate;
@@ -720,10 +787,11 @@ extern "C" int hg_recur_step(const hg_recur_desc* A, const hg_heads* x, const hg
   const char* what = "hg_recur_step";
   HG_TRY(check(A, what));
   if (A->t != 1) return fail(HG_ERR_ARG, "%s: t=%lld, one token a row", what, (long long)A->t);
-  HG_TRY(check_rows(what, x, "x", false, A->batch, A->t, A->width, A->dtype));
-  HG_TRY(check_rows(what, r, "r", false, A->batch, A->t, A->width, A->dtype));
-  HG_TRY(check_rows(what, i, "i", false, A->batch, A->t, A->width, A->dtype));
-  HG_TRY(check_rows(what, h, "h", true, A->batch, A->t, A->width, A->dtype));
+  Rows rx, rr, ri, rh;
+  HG_TRY(rows_in(A, what, x, "x", false, &rx));
+  HG_TRY(rows_in(A, what, r, "r", false, &rr));
+  HG_TRY(rows_in(A, what, i, "i", false, &ri));
+  HG_TRY(rows_in(A, what, h, "h", true, &rh));
   if (n_slots < 0 || (!slots && n_slots < A->batch))
     return fail(HG_ERR_ARG, "%s: %lld states for %d rows", what, (long long)n_slots, A->batch);
   if (A->batch == 0) return HG_OK;
@@ -735,10 +803,10 @@ extern "C" int hg_recur_step(const hg_recur_desc* A, const hg_heads* x, const hg
   a.batch = A->batch;
   a.width = A->width;
   a.rate = A->rate;
-  a.x = rows_of(x);
-  a.r = rows_of(r);
-  a.i = rows_of(i);
-  a.h = rows_of(h);
+  a.x = rx;
+  a.r = rr;
+  a.i = ri;
+  a.h = rh;
   const dim3 grid((unsigned)cdiv((int64_t)A->batch * A->width, 256));
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (A->dtype == HG_DTYPE_F32) {

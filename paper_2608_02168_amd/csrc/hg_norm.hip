@@ -202,21 +202,41 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
   affine<V>(a, s, w, bias);
 #pragma unroll
   for (int j = 0; j < V; ++j) dw[j] = db[j] = 0.f;
-  int odd = 0;
-  for (int64_t i0 = (int64_t)s.rb * a.rper; i0 < a.rows; i0 += (int64_t)a.row_blocks * a.rper, odd ^= 1) {
-    const int64_t b = i0 + s.row;
+  // the next item's rows are under way while one is worked on, where they are few
+  constexpr int AHEAD = V > 1 && R <= 2 && BT <= 256 ? 2 : 1;
+  typename Vec<T, V>::raw xs[AHEAD][R], ys[AHEAD][R];
+  typename Vec<float, 2>::raw st[AHEAD];
+  int64_t ns[AHEAD];
+  const int64_t step = (int64_t)a.row_blocks * a.rper;
+  auto fetch = [&](int to, int64_t b) {
     const bool in = s.on && b < a.rows;
     const int64_t n = in ? len_of(a, b) : 0;
-    typename Vec<T, V>::raw x[R], y[R];
+    ns[to] = n;
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int64_t t = s.r + k * s.nr;
       if (t < n) {
-        x[k] = Vec<T, V>::load(at<T, V>(a.x, b, t, s.c));
-        y[k] = Vec<T, V>::load(at<T, V>(a.dy, b, t, s.c));
+        xs[to][k] = Vec<T, V>::load(at<T, V>(a.x, b, t, s.c));
+        ys[to][k] = Vec<T, V>::load(at<T, V>(a.dy, b, t, s.c));
       }
     }
-    const float mean = in ? a.stats[(b * a.groups + s.g) * 2] : 0.f, rstd = in ? a.stats[(b * a.groups + s.g) * 2 + 1] : 0.f;
+    st[to] = in ? Vec<float, 2>::load(a.stats + (b * a.groups + s.g) * 2) : Vec<float, 2>::raw{0.f, 0.f};
+  };
+  const int64_t first = (int64_t)s.rb * a.rper;
+  if (AHEAD > 1) fetch(0, first + s.row);
+  int odd = 0;
+  auto item = [&](auto now, int64_t i0) {
+    constexpr int NOW = decltype(now)::value;
+    const int64_t b = i0 + s.row;
+    const bool in = s.on && b < a.rows;
+    if (AHEAD > 1) {
+      if (i0 + step < a.rows) fetch(NOW ^ 1, b + step);
+    } else {
+      fetch(0, b);
+    }
+    const int64_t n = ns[NOW];
+    typename Vec<T, V>::raw(&x)[R] = xs[NOW], (&y)[R] = ys[NOW];
+    const float mean = st[NOW][0], rstd = st[NOW][1];
     float e[R][V], sum[2] = {0.f, 0.f};
     g_by_act<true>(a.act, [&](auto act) {
       constexpr int ACT = decltype(act)::value;
@@ -242,6 +262,7 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
         }
     });
     item_sum<2>(sum, a.lp, sh[odd]);
+    odd ^= 1;
     const float inv = n > 0 ? 1.f / (float)(n * a.cg) : 0.f, m0 = sum[0] * inv, m1 = sum[1] * inv;
     if (in)
 #pragma unroll
@@ -256,6 +277,10 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
         }
         Vec<T, V>::put(at<T, V>(a.y, b, t, s.c), o);
       }
+  };
+  for (int64_t i0 = first; i0 < a.rows; i0 += AHEAD * step) {
+    item(std::integral_constant<int, 0>{}, i0);
+    if (AHEAD > 1 && i0 + step < a.rows) item(std::integral_constant<int, AHEAD - 1>{}, i0 + step);
   }
   if (!a.part) return;
   // the block's sums of each channel: over its rows and row lanes, in order
@@ -559,18 +584,23 @@ Plan plan_of(const hg_group_norm_desc* A, bool bwd) {
   p.v = vec_of(A);
   a.nv = a.cg / p.v;
   a.lc = log2_up(a.nv);
-  // an item's threads: as few as hold it at four tokens each, or eight
+  // An item's threads: up to 256 of four or eight tokens each, else up to 1024 of eight
+  // (in the backward, which holds three times as much, of one or two); else chunks.
   const int64_t t = std::max<int64_t>(A->t, 1);
-  const int lr4 = log2_up(cdiv(t, 4)), lr8 = log2_up(cdiv(t, kMostRows));
-  const int lr = a.lc + lr4 <= 8 ? lr4 : lr8;
+  const int lr4 = log2_up(cdiv(t, 4)), lr8 = log2_up(cdiv(t, kMostRows)), lrb = log2_up(cdiv(t, p.v == 8 ? 1 : 2));
+  const int lr = a.lc + lr4 <= 8 ? lr4 : a.lc + lr8 <= 8 || !bwd ? lr8 : lrb;
   p.chunked = a.lc + lr > 10 ||
               // items that leave most of the chip without a block are better cut, once they are long
               (lr >= 3 && a.lc + lr > 8 && (int64_t)A->batch * A->groups < 64);
   if (!p.chunked) {
     a.lp = a.lc + lr;
     p.r = 1 << std::min(3, log2_up(cdiv(t, (int64_t)1 << lr)));
-    p.bt = a.lp <= 8 && !bwd ? 256 : 1024;
-    lay_out(p, A->batch, bwd ? 512 : (int64_t)1 << 21);
+    p.bt = a.lp <= 8 ? 256 : 1024;
+    // A row of partial sums of dw and db for each block of the backward: few blocks
+    // (16384 rows of 16 x 64 channels 38 us with 1024, 46 with 1536), but single channels
+    // a thread are few bytes in flight and take more (20000 rows of 32 x 25 channels 95
+    // us with 4096, 115 with 2048).
+    lay_out(p, A->batch, !bwd ? (int64_t)1 << 21 : p.bt == 256 ? (p.v == 1 ? 4096 : 1024) : 512);
     return p;
   }
   p.r = kMostRows;
@@ -631,15 +661,6 @@ int check(const hg_group_norm_desc* A, const char* what) {
   return HG_OK;
 }
 
-#define HG_NORM_R(NAME_, K_, V_, BT_, ...)                                                                       \
-  switch (p.r) {                                                                                                 \
-    case 1: HG_LAUNCH(NAME_, (K_<T, V_, 1, BT_ __VA_ARGS__>), grid, dim3(BT_), 0, s, a); break;                  \
-    case 2: HG_LAUNCH(NAME_, (K_<T, V_, 2, BT_ __VA_ARGS__>), grid, dim3(BT_), 0, s, a); break;                  \
-    case 4: HG_LAUNCH(NAME_, (K_<T, V_, 4, BT_ __VA_ARGS__>), grid, dim3(BT_), 0, s, a); break;                  \
-    default: HG_LAUNCH(NAME_, (K_<T, V_, 8, BT_ __VA_ARGS__>), grid, dim3(BT_), 0, s, a);                        \
-  }
-#define HG_COMMA ,
-
 unsigned apply_blocks(const NormArgs& a, int v) {
   return (unsigned)cdiv((int64_t)a.batch * cdiv(a.t, kApply) * (a.width / v), 256);
 }
@@ -648,12 +669,18 @@ template <class T, int V>
 int launch_fwd(const Plan& p, const NormArgs& a, const Bufs& b, hipStream_t s) {
   const dim3 grid((unsigned)p.blocks);
   if (!p.chunked) {
-    if (p.bt == 256) {
-      HG_NORM_R("group_norm", k_norm_fwd, V, 256, HG_COMMA false);
-    } else {
-      HG_NORM_R("group_norm", k_norm_fwd, V, 1024, HG_COMMA false);
-    }
-    return HG_OK;
+    const auto by_r = [&](auto bt) {
+      constexpr int BT = decltype(bt)::value;
+      const char* name = "group_norm";
+      switch (p.r) {
+        case 1: HG_LAUNCH(name, (k_norm_fwd<T, V, 1, BT, false>), grid, dim3(BT), 0, s, a); break;
+        case 2: HG_LAUNCH(name, (k_norm_fwd<T, V, 2, BT, false>), grid, dim3(BT), 0, s, a); break;
+        case 4: HG_LAUNCH(name, (k_norm_fwd<T, V, 4, BT, false>), grid, dim3(BT), 0, s, a); break;
+        default: HG_LAUNCH(name, (k_norm_fwd<T, V, 8, BT, false>), grid, dim3(BT), 0, s, a);
+      }
+      return HG_OK;
+    };
+    return p.bt == 256 ? by_r(std::integral_constant<int, 256>{}) : by_r(std::integral_constant<int, 1024>{});
   }
   if (p.bt == 256) {
     HG_LAUNCH("group_norm_chunks", (k_norm_fwd<T, V, kMostRows, 256, true>), grid, dim3(256), 0, s, a);
@@ -672,7 +699,23 @@ int launch_bwd(const Plan& p, NormArgs a, const Bufs& b, float* dw, float* db, i
   const unsigned first = (unsigned)cdiv(2 * (int64_t)a.width, 16);
   if (!p.chunked) {
     if (!dw && !db) a.part = nullptr;
-    HG_NORM_R("group_norm_bwd", k_norm_bwd, V, 1024, );
+    const char* name = "group_norm_bwd";
+    if (p.bt == 256) {
+      switch (p.r) {
+        case 1: HG_LAUNCH(name, (k_norm_bwd<T, V, 1, 256>), grid, dim3(256), 0, s, a); break;
+        case 2: HG_LAUNCH(name, (k_norm_bwd<T, V, 2, 256>), grid, dim3(256), 0, s, a); break;
+        case 4: HG_LAUNCH(name, (k_norm_bwd<T, V, 4, 256>), grid, dim3(256), 0, s, a); break;
+        default: HG_LAUNCH(name, (k_norm_bwd<T, V, 8, 256>), grid, dim3(256), 0, s, a);
+      }
+    } else if (p.r == 1) {
+      HG_LAUNCH(name, (k_norm_bwd<T, V, 1, 1024>), grid, dim3(1024), 0, s, a);
+    } else if (p.r == 2) {
+      HG_LAUNCH(name, (k_norm_bwd<T, V, 2, 1024>), grid, dim3(1024), 0, s, a);
+    } else if (V < 8 && p.r == 4) {
+      HG_LAUNCH(name, (k_norm_bwd<T, V < 8 ? V : 4, 4, 1024>), grid, dim3(1024), 0, s, a);
+    } else {
+      HG_LAUNCH(name, (k_norm_bwd<T, V == 1 ? 1 : 4, 8, 1024>), grid, dim3(1024), 0, s, a);
+    }
     if (dw || db)
       HG_LAUNCH("group_norm_grads", k_norm_grads, dim3(first), dim3(1024), 0, s, b.part, (int64_t)a.row_blocks, a.width,
                 a.groups, a.w, dw, db, accumulate, nullptr);

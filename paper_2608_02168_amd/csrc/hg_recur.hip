@@ -11,12 +11,14 @@
 // A thread has four channels and K tokens in a row.  It composes its tokens' steps
 // in registers, the four runs of a wave (16 threads side by side) compose by
 // shuffles, the waves of a block through LDS; then each thread walks its tokens
-// again from the value that reaches it.  So a block takes 4 NW K tokens of 64
-// channels at a time with one barrier, every value is read and written once, and
-// what is serial is a sequence's tiles.  One wave does so alone where sequences
-// are many (WAVE: no barrier).  Where there are few, the history is cut into
-// segments: a first pass composes each segment's step (k_recur_sums), and the
-// segments' blocks start from the steps before theirs.
+// again from the value that reaches it.  So a block takes 16 K tokens of 64 channels
+// at a time, and every value is read and written once.  Many sequences: a wave
+// (WAVE: no barrier) or a block walks each.  Few: a block for each tile, all at once,
+// and the tiles' steps compose through memory (k_recur_chain_*).
+//
+// Bound by HBM and by the vector instructions at once: some 55 a value forward, six of
+// them transcendental, are 95 us for 67M values on this chip, their 8 bytes 103 us at
+// the 5.2 TB/s of a large copy.
 //
 // The last four channels of a row whose width is no multiple of four are taken
 // by a thread that starts earlier: two threads then compute and write the same
@@ -44,10 +46,9 @@ struct RecurArgs {
   const float* s_in;     // state, in the backward dstate_out
   const float* s_first;  // backward: the forward's state
   float* s_out;
-  float* sums;           // [batch][segs][2][width] steps of the segments
   float* part;           // [blocks of a slab][width] sums of dlog sigmoid(r), or null
-  int64_t t, seg_len;
-  int32_t batch, width, slabs, segs;
+  int64_t t;
+  int32_t batch, width, slabs;
   float rate;
 };
 
@@ -135,34 +136,29 @@ __device__ __forceinline__ void compose(Step& s, float (&y)[V], float (&at)[V], 
 
 // What a block (WAVE: a wave) works on.  All but the channels is the same in a wave.
 struct Place {
-  int64_t b, t_beg, t_end, out_end;  // tokens of the segment: inside the sequence, and with the rows past it
-  int32_t seg, c0;                   // first channel of the thread
-  bool on;                           // no thread before has the same channels
+  int64_t b, t_end, out_end;  // its sequence, whose rows past t_end are zeros up to out_end
+  int32_t c0;                 // first channel of the thread
+  bool on;                    // no thread before has the same channels
 };
 __device__ __forceinline__ int64_t len_of(const RecurArgs& a, int64_t b) {
   if (!a.lens) return a.t;
   const int32_t n = a.lens[b];
   return n < 0 ? 0 : (n < a.t ? n : a.t);
 }
+// A thread's channels: the last ones of a row start at width - V.
+__device__ __forceinline__ void channels_of(const RecurArgs& a, int slab, int col, Place& p) {
+  const int c = slab * kSlab + col * V;
+  p.on = c < a.width;
+  p.c0 = c < a.width - V ? c : a.width - V;
+}
 template <bool WAVE>
 __device__ __forceinline__ Place place_of(const RecurArgs& a, int wave, int col) {
   Place p;
-  const uint32_t id = blockIdx.x, rest = id / (uint32_t)a.slabs, slab = id - rest * (uint32_t)a.slabs;
-  if constexpr (WAVE) {
-    p.b = (int64_t)rest * kNW + wave;
-    p.seg = 0;
-  } else {
-    p.b = rest / (uint32_t)a.segs;
-    p.seg = (int32_t)(rest - (uint32_t)p.b * (uint32_t)a.segs);
-  }
-  const int c = (int)slab * kSlab + col * V;
-  p.on = c < a.width;
-  p.c0 = c < a.width - V ? c : a.width - V;
-  const int64_t len = p.b < a.batch ? len_of(a, p.b) : 0;
-  p.t_beg = p.seg * a.seg_len;
-  p.out_end = p.t_beg + a.seg_len < a.t ? p.t_beg + a.seg_len : a.t;
-  p.t_end = len < p.out_end ? len : p.out_end;
-  if (p.t_end < p.t_beg) p.t_end = p.t_beg;
+  const uint32_t id = blockIdx.x, rest = id / (uint32_t)a.slabs;
+  p.b = WAVE ? (int64_t)rest * kNW + wave : rest;
+  channels_of(a, (int)(id - rest * (uint32_t)a.slabs), col, p);
+  p.t_end = p.b < a.batch ? len_of(a, p.b) : 0;
+  p.out_end = a.t;
   return p;
 }
 
@@ -210,16 +206,6 @@ __device__ __forceinline__ void load_state(const float* s, const RecurArgs& a, c
   for (int j = 0; j < V; ++j) y[j] = s ? s[p.b * a.width + p.c0 + j] : 0.f;
 }
 
-// The steps of the segments [from, to) in their order, on y.
-__device__ __forceinline__ void run_segments(const RecurArgs& a, const Place& p, int from, int to, int dir, float (&y)[V]) {
-  const float* s = a.sums + p.b * a.segs * 2 * (int64_t)a.width + p.c0;
-  for (int q = from; q != to; q += dir) {
-    const float* f = s + q * 2 * (int64_t)a.width;
-#pragma unroll
-    for (int j = 0; j < V; ++j) y[j] = fmaf(f[j], y[j], f[a.width + j]);
-  }
-}
-
 template <class T, int K, bool WAVE>
 __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
   __shared__ __align__(16) float lds[WAVE ? 4 : 2 * kNW * 2 * kSlab];
@@ -232,14 +218,13 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
 #pragma unroll
   for (int j = 0; j < V; ++j) slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
   load_state(a.s_in, a, p, y);
-  if (!WAVE && p.seg) run_segments(a, p, 0, p.seg, 1, y);
   const Stream<T> sx(a.x, p, run * K), sr(a.r, p, run * K), si(a.i, p, run * K), sh(a.h, p, run * K);
   typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {};
   auto fetch = [&](auto full, int64_t ts) {
     constexpr bool FULL = decltype(full)::value;
-    load<T, K, FULL>(rr, sr, ts, ts + run * K, p.t_beg, p.t_end);
-    load<T, K, FULL>(ri, si, ts, ts + run * K, p.t_beg, p.t_end);
-    load<T, K, FULL>(rx, sx, ts, ts + run * K, p.t_beg, p.t_end);
+    load<T, K, FULL>(rr, sr, ts, ts + run * K, 0, p.t_end);
+    load<T, K, FULL>(ri, si, ts, ts + run * K, 0, p.t_end);
+    load<T, K, FULL>(rx, sx, ts, ts + run * K, 0, p.t_end);
   };
   int odd = 0;
   auto tile = [&](auto full, int64_t ts) {
@@ -280,7 +265,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
       }
     }
   };
-  int64_t ts = p.t_beg;
+  int64_t ts = 0;
   if (ts + kTile <= p.t_end) {
     fetch(Bool<true>{}, ts);
   } else {
@@ -289,110 +274,47 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
   for (; ts + kTile <= p.t_end; ts += kTile) tile(Bool<true>{}, ts);
   if (ts < p.t_end) tile(Bool<false>{}, ts);
   zero_rows<T>(a.h, p, run, WAVE ? TW : kNW * TW);
-  if (a.s_out && p.on && run == 0 && p.seg == a.segs - 1) {
+  if (a.s_out && p.on && run == 0) {
 #pragma unroll
     for (int j = 0; j < V; ++j) a.s_out[p.b * a.width + p.c0 + j] = y[j];
   }
 }
 
-// The step of each segment.  A thread takes one run of the segment's tokens and
-// walks it K at a time; the block composes the runs at the end.  BACK: the
-// backward's, from the last token.
-template <class T, int K, bool BACK>
-__global__ void __launch_bounds__(kNW * 64) k_recur_sums(const RecurArgs a) {
-  __shared__ __align__(16) float lds[kNW * 2 * kSlab];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
-  const Place p = place_of<false>(a, wave, col);
-  // (the steps of the last segment of a walk lead nowhere)
-  if (p.seg == (BACK ? 0 : a.segs - 1)) return;
-  // run q of the segment in the walk's order: tokens [beg + q per, ..) forward, backward down from end - q per
-  const int q = wave * TW + rank;
-  const int64_t n = p.t_end - p.t_beg, per = ((n + kNW * TW - 1) / (kNW * TW) + K - 1) / K * K;
-  const int64_t first = BACK ? p.t_end - kNW * TW * per : p.t_beg;  // (may be before the segment)
-  const int64_t skip = (BACK ? kNW * TW - 1 - q : q) * per;
-  const Stream<T, int64_t> sx(BACK ? a.dh : a.x, p, skip), sr(a.r, p, skip), si(a.i, p, skip);
-  float slope[V];
-  Step s;
+// The gradients at one token, and what it adds to the sums; at: the gradient that
+// reaches h from the token after, becomes the one that this token passes on.
+template <class T>
+__device__ __forceinline__ void grads_of(const float (&slope)[V], const float (&fs)[V], const float (&fa)[V], const float (&gh)[V],
+                                         const typename Quad<T>::raw& ri, const typename Quad<T>::raw& rx, const float (&hb)[V],
+                                         float (&at)[V], float (&sum)[V], float (&vx)[V], float (&vi)[V], float (&vr)[V]) {
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
-    s.a[j] = 1.f;
-    s.b[j] = 0.f;
+    const float f = fa[j], l = slope[j] * fs[j], g = gh[j] + at[j];
+    at[j] = f * g;
+    // (1 - a^2 at least 2^-120, below which l = 0, so that its root's inverse is finite)
+    const float m = rest_of(l, f), iq = __builtin_amdgcn_rsqf(fmaxf(m, 7.5e-37f)), q = m * iq;
+    const float sg = sigm(Quad<T>::get(ri, j)), x = Quad<T>::get(rx, j), gs = g * sg;
+    vx[j] = gs * q;
+    vi[j] = vx[j] * x * (1.f - sg);
+    const float dl = f * fmaf(g, hb[j], -gs * x * f * iq);
+    sum[j] = fmaf(dl, fs[j], sum[j]);
+    vr[j] = dl * (l * 0.69314718055994531f) * (1.f - fs[j]);
   }
-  typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {};
-  auto fetch = [&](auto full, int64_t ts) {
-    constexpr bool FULL = decltype(full)::value;
-    load<T, K, FULL>(rr, sr, ts, ts + skip, p.t_beg, p.t_end);
-    if constexpr (!BACK) load<T, K, FULL>(ri, si, ts, ts + skip, p.t_beg, p.t_end);
-    load<T, K, FULL>(rx, sx, ts, ts + skip, p.t_beg, p.t_end);
-  };
-  // whether all runs' tokens of a round lie inside: only the last run forward, backward the first, may not
-  const bool whole = per * kNW * TW == n;
-  const auto walk = [&](auto full) {
-    constexpr bool FULL = decltype(full)::value;
-    const int64_t step = BACK ? -K : K;
-    int64_t ts = BACK ? first + per - K : first;
-    if (per > 0) fetch(full, ts);
-    for (int64_t i = 0; i < per; i += K, ts += step) {
-      float fa[K][V], fu[K][V];
+}
+
+// A block's sums of its runs, in order, as row `at` of the partial sums.
+__device__ __forceinline__ void block_sums(const RecurArgs& a, const float (&sum)[V], float* all, int run, int col, int slab,
+                                           int64_t at) {
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int64_t t = ts + skip + k;
-        const bool in = FULL || (t >= p.t_beg && t < p.t_end);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float l = slope[j] * sigm(Quad<T>::get(rr[k], j));
-          const float f = __builtin_amdgcn_exp2f(l);
-          float u = Quad<T>::get(rx[k], j);
-          if constexpr (BACK) {
-            u *= f;
-          } else {
-            u *= __builtin_amdgcn_sqrtf(rest_of(l, f)) * sigm(Quad<T>::get(ri[k], j));
-          }
-          fa[k][j] = in ? f : 1.f;
-          fu[k][j] = in ? u : 0.f;
-        }
-      }
-      if (i + K < per) fetch(full, ts + step);
-#pragma unroll
-      for (int o = 0; o < K; ++o) {
-        const int k = BACK ? K - 1 - o : o;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          s.a[j] *= fa[k][j];
-          s.b[j] = fmaf(fa[k][j], s.b[j], fu[k][j]);
-        }
-      }
-    }
-  };
-  if (whole) {
-    walk(Bool<true>{});
-  } else {
-    walk(Bool<false>{});
-  }
-  // the whole segment's step: the value that leaves it from 0, and the product of its factors
-  Step before;
-  compose_wave(s, before, rank);
-  if (rank == TW - 1) {
-    *reinterpret_cast<f32x4*>(lds + wave * 2 * kSlab + col * V) = f32x4{s.a[0], s.a[1], s.a[2], s.a[3]};
-    *reinterpret_cast<f32x4*>(lds + wave * 2 * kSlab + kSlab + col * V) = f32x4{s.b[0], s.b[1], s.b[2], s.b[3]};
-  }
+  for (int j = 0; j < V; ++j) all[run * kSlab + col * V + j] = sum[j];
   __syncthreads();
-  if (q == 0 && p.on) {
-    f32x4 ya = f32x4{1.f, 1.f, 1.f, 1.f}, yb = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < kNW; ++w) {
-      const f32x4 qa = *reinterpret_cast<const f32x4*>(lds + w * 2 * kSlab + col * V);
-      const f32x4 qb = *reinterpret_cast<const f32x4*>(lds + w * 2 * kSlab + kSlab + col * V);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        yb[j] = fmaf(qa[j], yb[j], qb[j]);
-        ya[j] *= qa[j];
-      }
-    }
-    float* o = a.sums + (p.b * a.segs + p.seg) * 2 * (int64_t)a.width + p.c0;
-#pragma unroll
-    for (int j = 0; j < V; ++j) o[j] = ya[j], o[a.width + j] = yb[j];
+  for (int c = threadIdx.x; c < kSlab; c += kNW * 64) {
+    const int ch = slab * kSlab + c;
+    if (ch >= a.width) continue;
+    // the thread that has channel ch: the last ones start at width - V
+    const int own = c / V, c0 = slab * kSlab + own * V, shift = c0 < a.width - V ? 0 : c0 - (a.width - V);
+    float s = 0.f;
+    for (int q = 0; q < kNW * TW; ++q) s += all[q * kSlab + c + shift];
+    a.part[at * a.width + ch] = s;
   }
 }
 
@@ -415,18 +337,17 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
     if (WAVE) p.t_end = len_of(a, p.b);
     float y[V];
     load_state(a.s_in, a, p, y);
-    if (!WAVE && p.seg < a.segs - 1) run_segments(a, p, a.segs - 1, p.seg, -1, y);
     const Stream<T> sx(a.x, p, skip), sr(a.r, p, skip), si(a.i, p, skip), sh(a.h, p, skip), sg(a.dh, p, skip), ox(a.dx, p, skip),
         orr(a.dr, p, skip), oi(a.di, p, skip);
     typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {}, rh[K] = {}, rg[K] = {};
-    // the tile of tokens ts .. ts + kTile - 1 (row k of rh: h before the thread's token k); FULL: it begins after t_beg
+    // the tile of tokens ts .. ts + kTile - 1 (row k of rh: h before the thread's token k); FULL: it begins after token 0
     auto fetch = [&](auto full, int64_t ts) {
       constexpr bool FULL = decltype(full)::value;
-      load<T, K, FULL>(rr, sr, ts, ts + skip, p.t_beg, p.t_end);
-      load<T, K, FULL>(rg, sg, ts, ts + skip, p.t_beg, p.t_end);
-      load<T, K, FULL>(ri, si, ts, ts + skip, p.t_beg, p.t_end);
-      load<T, K, FULL>(rx, sx, ts, ts + skip, p.t_beg, p.t_end);
-      load<T, K, FULL>(rh, sh, ts - 1, ts - 1 + skip, p.t_beg ? p.t_beg - 1 : 0, p.t_end);
+      load<T, K, FULL>(rr, sr, ts, ts + skip, 0, p.t_end);
+      load<T, K, FULL>(rg, sg, ts, ts + skip, 0, p.t_end);
+      load<T, K, FULL>(ri, si, ts, ts + skip, 0, p.t_end);
+      load<T, K, FULL>(rx, sx, ts, ts + skip, 0, p.t_end);
+      load<T, K, FULL>(rh, sh, ts - 1, ts - 1 + skip, 0, p.t_end);
     };
     int odd = 0;
     auto tile = [&](auto full, int64_t ts) {
@@ -438,7 +359,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
       for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
 #pragma unroll
       for (int k = K - 1; k >= 0; --k) {
-        const bool in = FULL || t0 + k >= p.t_beg;
+        const bool in = FULL || t0 + k >= 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
           fs[k][j] = sigm(Quad<T>::get(rr[k], j));
@@ -454,24 +375,12 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
       odd ^= 1;
 #pragma unroll
       for (int k = K - 1; k >= 0; --k) {
-        if (!FULL && t0 + k < p.t_beg) continue;
+        if (!FULL && t0 + k < 0) continue;
         float hb[V], vx[V], vi[V], vr[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) hb[j] = Quad<T>::get(rh[k], j);
         if (!FULL && t0 + k == 0) load_state(a.s_first, a, p, hb);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float f = fa[k][j], l = slope[j] * fs[k][j], g = gh[k][j] + at[j];
-          at[j] = f * g;
-          // (1 - a^2 at least 2^-120, below which l = 0, so that its root's inverse is finite)
-          const float m = rest_of(l, f), iq = __builtin_amdgcn_rsqf(fmaxf(m, 7.5e-37f)), q = m * iq;
-          const float sg1 = sigm(Quad<T>::get(ri[k], j)), x = Quad<T>::get(rx[k], j), gs = g * sg1;
-          vx[j] = gs * q;
-          vi[j] = vx[j] * x * (1.f - sg1);
-          const float dl = f * fmaf(g, hb[j], -gs * x * f * iq);
-          sum[j] = fmaf(dl, fs[k][j], sum[j]);
-          vr[j] = dl * (l * 0.69314718055994531f) * (1.f - fs[k][j]);
-        }
+        grads_of<T>(slope, fs[k], fa[k], gh[k], ri[k], rx[k], hb, at, sum, vx, vi, vr);
         if (p.on) {
           Quad<T>::put(ox.at(ts, k), vx);
           Quad<T>::put(oi.at(ts, k), vi);
@@ -479,48 +388,321 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
         }
       }
       // the tile before; one that holds token 0 is not full (its h before comes from the state)
-      if (ts - kTile > p.t_beg) {
+      if (ts - kTile > 0) {
         fetch(Bool<true>{}, ts - kTile);
-      } else if (ts > p.t_beg) {
+      } else if (ts > 0) {
         fetch(Bool<false>{}, ts - kTile);
       }
     };
     int64_t ts = p.t_end - kTile;
-    if (ts > p.t_beg) {
+    if (ts > 0) {
       fetch(Bool<true>{}, ts);
     } else {
       fetch(Bool<false>{}, ts);
     }
-    for (; ts > p.t_beg; ts -= kTile) tile(Bool<true>{}, ts);
-    if (ts + kTile > p.t_beg) tile(Bool<false>{}, ts);
+    for (; ts > 0; ts -= kTile) tile(Bool<true>{}, ts);
+    if (ts + kTile > 0) tile(Bool<false>{}, ts);
     const int ranks = WAVE ? TW : kNW * TW;
     zero_rows<T>(a.dx, p, run, ranks);
     zero_rows<T>(a.di, p, run, ranks);
     zero_rows<T>(a.dr, p, run, ranks);
-    if (a.s_out && p.on && run == 0 && p.seg == 0) {
+    if (a.s_out && p.on && run == 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) a.s_out[p.b * a.width + p.c0 + j] = y[j];
     }
     if (!WAVE) break;
   }
   if (!a.part) return;
-  // the block's sums of its runs, in order
   __syncthreads();
-  float* all = lds;  // [NW * TW][slab]
   static_assert(kNW * TW * kSlab <= 2 * kNW * 2 * kSlab, "the sums fit the block's LDS");
-#pragma unroll
-  for (int j = 0; j < V; ++j) all[(wave * TW + rank) * kSlab + col * V + j] = sum[j];
+  const uint32_t rest = blockIdx.x / (uint32_t)a.slabs;
+  block_sums(a, sum, lds, wave * TW + rank, col, (int)(blockIdx.x - rest * (uint32_t)a.slabs), rest);
+}
+
+// ---- one pass over few long histories ------------------------------------------------
+// A block has one tile of 64 channels.  Blocks take tickets, tile by tile of all
+// sequences, publish their tile's composed step (A, B) and form the value y that
+// reaches it from the steps of the tiles before in its group of kGroup and the value
+// that reaches the group, which the last block of the group before publishes.  The
+// order of every product is fixed, so results do not depend on timing.
+//
+// A published word is its own flag: the words are all ones (a NaN that no step is
+// stored as) before the launch, and are stored and read whole, at device scope.  A
+// block waits for blocks of lower tickets only, which have started, and which publish
+// their step before they wait for anything: every wait ends.
+constexpr int kGroup = 32;  // (16 and 64: within 1 %)
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+struct Chain {
+  uint64_t* step;    // [pairs][tiles][64]: A, B
+  uint32_t* value;   // [pairs][groups][64]: y that reaches a group (of group 0: not used)
+  uint32_t* ticket;
+  int32_t tiles, groups;
+  uint32_t pairs;
+};
+
+__device__ __forceinline__ uint32_t word_of(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return u == kNone ? 0x7FC00000u : u;
+}
+__device__ __forceinline__ uint64_t peek(const uint64_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint32_t peek(const uint32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+struct ChainLds {
+  float wave[kNW][2][kSlab];  // the waves' steps
+  float far[kNW][2][kSlab];   // steps of the tiles before, by wave
+  float y[kSlab];             // the value that reaches the tile
+  uint32_t ticket;
+};
+
+// The block's tile: its ticket's place, n counted in the walk's order.
+__device__ __forceinline__ uint32_t take_ticket(const Chain& q, ChainLds& sh) {
+  if (threadIdx.x == 0) sh.ticket = atomicAdd(q.ticket, 1u);
   __syncthreads();
-  const uint32_t rest = blockIdx.x / (uint32_t)a.slabs, slab = blockIdx.x - rest * (uint32_t)a.slabs;
-  for (int c = threadIdx.x; c < kSlab; c += kNW * 64) {
-    const int ch = (int)slab * kSlab + c;
-    if (ch >= a.width) continue;
-    // the thread that has channel ch: the last ones start at width - V
-    const int own = c / V, c0 = (int)slab * kSlab + own * V, shift = c0 < a.width - V ? 0 : c0 - (a.width - V);
-    float s = 0.f;
-    for (int q = 0; q < kNW * TW; ++q) s += all[q * kSlab + c + shift];
-    a.part[(int64_t)rest * a.width + ch] = s;
+  return __builtin_amdgcn_readfirstlane(sh.ticket);
+}
+
+// From the threads' steps s: `at`, the value that reaches this thread's run.  Lane l of
+// a wave has channel l of the slab in between; y0: the value that reaches the first
+// tile, of that channel; last: no tile after this one needs its value, which `out` has.
+__device__ __forceinline__ void chain(Step& s, float (&at)[V], float& out, const Chain& q, ChainLds& sh, uint32_t pair, int n,
+                                      bool last, float y0, int wave, int rank, int col) {
+  const int lane = threadIdx.x & 63;
+  Step before;
+  compose_wave(s, before, rank);
+  if (rank == TW - 1) {
+    *reinterpret_cast<f32x4*>(&sh.wave[wave][0][col * V]) = f32x4{s.a[0], s.a[1], s.a[2], s.a[3]};
+    *reinterpret_cast<f32x4*>(&sh.wave[wave][1][col * V]) = f32x4{s.b[0], s.b[1], s.b[2], s.b[3]};
   }
+  __syncthreads();
+  float ta = 1.f, tb = 0.f;  // the tile's step
+#pragma unroll
+  for (int w = 0; w < kNW; ++w) {
+    const float a = sh.wave[w][0][lane], b = sh.wave[w][1][lane];
+    tb = fmaf(a, tb, b);
+    ta *= a;
+  }
+  const int group = n / kGroup, r = n - group * kGroup;
+  uint64_t* steps = q.step + ((int64_t)pair * q.tiles + (n - r)) * kSlab + lane;
+  if (wave == 0 && r != kGroup - 1 && !last)
+    __hip_atomic_store(steps + (int64_t)r * kSlab, (uint64_t)__float_as_uint(tb) << 32 | word_of(ta), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+  // this wave's share of the tiles before in the group, then the value that reaches the group
+  constexpr int PER = kGroup / kNW;
+  float fa = 1.f, fb = 0.f;
+  {
+    uint64_t w[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (wave * PER + k < r) w[k] = peek(steps + (int64_t)(wave * PER + k) * kSlab);
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      if (wave * PER + k < r) {
+        while ((uint32_t)w[k] == kNone) {
+          __builtin_amdgcn_s_sleep(1);
+          w[k] = peek(steps + (int64_t)(wave * PER + k) * kSlab);
+        }
+        const float a = __uint_as_float((uint32_t)w[k]), b = __uint_as_float((uint32_t)(w[k] >> 32));
+        fb = fmaf(a, fb, b);
+        fa *= a;
+      }
+  }
+  sh.far[wave][0][lane] = fa;
+  sh.far[wave][1][lane] = fb;
+  __syncthreads();
+  if (wave == 0) {
+    float y = y0;
+    if (group > 0) {
+      const uint32_t* v = q.value + ((int64_t)pair * q.groups + group) * kSlab + lane;
+      uint32_t u = peek(v);
+      while (u == kNone) {
+        __builtin_amdgcn_s_sleep(1);
+        u = peek(v);
+      }
+      y = __uint_as_float(u);
+    }
+#pragma unroll
+    for (int w = 0; w < kNW; ++w) y = fmaf(sh.far[w][0][lane], y, sh.far[w][1][lane]);
+    out = fmaf(ta, y, tb);
+    if (r == kGroup - 1 && !last)
+      __hip_atomic_store(q.value + ((int64_t)pair * q.groups + group + 1) * kSlab + lane, word_of(out), __ATOMIC_RELAXED,
+                         __HIP_MEMORY_SCOPE_AGENT);
+    sh.y[lane] = y;
+  }
+  __syncthreads();
+  f32x4 y = *reinterpret_cast<const f32x4*>(&sh.y[col * V]);
+  for (int w = 0; w < wave; ++w) {
+    const f32x4 qa = *reinterpret_cast<const f32x4*>(&sh.wave[w][0][col * V]);
+    const f32x4 qb = *reinterpret_cast<const f32x4*>(&sh.wave[w][1][col * V]);
+#pragma unroll
+    for (int j = 0; j < V; ++j) y[j] = fmaf(qa[j], y[j], qb[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) at[j] = fmaf(before.a[j], y[j], before.b[j]);
+}
+
+// The channel that lane l has in chain().
+__device__ __forceinline__ int channel_of(const RecurArgs& a, int slab, int lane) {
+  const int c = slab * kSlab + (lane & ~(V - 1));
+  return (c < a.width - V ? c : a.width - V) + (lane & (V - 1));
+}
+
+// A block's rows past the sequence's end, of its own stretch of the t tokens.
+template <class T, int TILE>
+__device__ __forceinline__ void zero_stretch(const RecurArgs& a, const Rows& x, Place p, int64_t len, int n, int run) {
+  p.t_end = (int64_t)n * TILE > len ? (int64_t)n * TILE : len;
+  p.out_end = (int64_t)(n + 1) * TILE < a.t ? (int64_t)(n + 1) * TILE : a.t;
+  zero_rows<T>(x, p, run, kNW * TW);
+}
+
+template <class T, int K>
+__global__ void __launch_bounds__(kNW * 64) k_recur_chain_fwd(const RecurArgs a, const Chain q) {
+  __shared__ ChainLds sh;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
+  constexpr int kTile = kNW * TW * K;
+  const uint32_t ticket = take_ticket(q, sh), n = ticket / q.pairs, pair = ticket - n * q.pairs;
+  const int slab = (int)(pair % (uint32_t)a.slabs), run = wave * TW + rank;
+  Place p;
+  p.b = pair / (uint32_t)a.slabs;
+  channels_of(a, slab, col, p);
+  const int64_t len = len_of(a, p.b), ts = (int64_t)n * kTile, t0 = ts + run * K;
+  const int64_t state_at = p.b * a.width + channel_of(a, slab, lane);
+  if (ts < len) {
+    const Stream<T> sx(a.x, p, run * K), sr(a.r, p, run * K), si(a.i, p, run * K), so(a.h, p, run * K);
+    typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {};
+    const bool whole = ts + kTile <= len;
+    if (whole) {
+      load<T, K, true>(rr, sr, ts, t0, 0, len);
+      load<T, K, true>(ri, si, ts, t0, 0, len);
+      load<T, K, true>(rx, sx, ts, t0, 0, len);
+    } else {
+      load<T, K, false>(rr, sr, ts, t0, 0, len);
+      load<T, K, false>(ri, si, ts, t0, 0, len);
+      load<T, K, false>(rx, sx, ts, t0, 0, len);
+    }
+    float slope[V], fa[K][V], fu[K][V], at[V], y0 = 0.f, out = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
+    if (n < kGroup && a.s_in) y0 = a.s_in[state_at];  // (it reaches group 0)
+    Step s;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const bool in = t0 + k < len;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float l = slope[j] * sigm(Quad<T>::get(rr[k], j));
+        const float f = __builtin_amdgcn_exp2f(l);
+        const float u = __builtin_amdgcn_sqrtf(rest_of(l, f)) * sigm(Quad<T>::get(ri[k], j)) * Quad<T>::get(rx[k], j);
+        fa[k][j] = in ? f : 1.f;
+        fu[k][j] = in ? u : 0.f;
+        s.a[j] *= fa[k][j];
+        s.b[j] = fmaf(fa[k][j], s.b[j], fu[k][j]);
+      }
+    }
+    const bool last = ts + kTile >= len;
+    chain(s, at, out, q, sh, pair, (int)n, last, y0, wave, rank, col);
+    if (p.on) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) at[j] = fmaf(fa[k][j], at[j], fu[k][j]);
+        if (whole || t0 + k < len) Quad<T>::put(so.at(ts, k), at);
+      }
+    }
+    if (last && a.s_out && wave == 0) a.s_out[state_at] = out;
+  } else if (n == 0 && a.s_out && wave == 0) {
+    a.s_out[state_at] = a.s_in ? a.s_in[state_at] : 0.f;  // no tokens
+  }
+  zero_stretch<T, kTile>(a, a.h, p, len, (int)n, run);
+}
+
+template <class T, int K>
+__global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a, const Chain q) {
+  __shared__ ChainLds sh;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
+  constexpr int kRuns = kNW * TW, kTile = kRuns * K;
+  const uint32_t ticket = take_ticket(q, sh), n = ticket / q.pairs, pair = ticket - n * q.pairs;
+  const int slab = (int)(pair % (uint32_t)a.slabs), run = wave * TW + rank, skip = (kRuns - 1 - run) * K;
+  Place p;
+  p.b = pair / (uint32_t)a.slabs;
+  channels_of(a, slab, col, p);
+  const int64_t len = len_of(a, p.b), ts = len - (int64_t)(n + 1) * kTile, t0 = ts + skip;  // the tiles end at the last token
+  const int64_t state_at = p.b * a.width + channel_of(a, slab, lane);
+  float sum[V] = {0.f, 0.f, 0.f, 0.f};
+  if (ts + kTile > 0) {
+    const Stream<T> sx(a.x, p, skip), sr(a.r, p, skip), si(a.i, p, skip), sh1(a.h, p, skip), sg(a.dh, p, skip), ox(a.dx, p, skip),
+        orr(a.dr, p, skip), oi(a.di, p, skip);
+    typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {}, rh[K] = {}, rg[K] = {};
+    const bool whole = ts > 0;  // (token 0's h before comes from the state)
+    const auto fetch = [&](auto full) {
+      constexpr bool FULL = decltype(full)::value;
+      load<T, K, FULL>(rr, sr, ts, t0, 0, len);
+      load<T, K, FULL>(rg, sg, ts, t0, 0, len);
+      load<T, K, FULL>(ri, si, ts, t0, 0, len);
+      load<T, K, FULL>(rx, sx, ts, t0, 0, len);
+      load<T, K, FULL>(rh, sh1, ts - 1, t0 - 1, 0, len);
+    };
+    if (whole) {
+      fetch(Bool<true>{});
+    } else {
+      fetch(Bool<false>{});
+    }
+    float slope[V], fs[K][V], fa[K][V], gh[K][V], at[V], y0 = 0.f, out = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
+    if (n < kGroup && a.s_in) y0 = a.s_in[state_at];  // (it reaches group 0)
+    Step s;
+#pragma unroll
+    for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
+#pragma unroll
+    for (int k = K - 1; k >= 0; --k) {
+      const bool in = t0 + k >= 0;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        fs[k][j] = sigm(Quad<T>::get(rr[k], j));
+        const float f = __builtin_amdgcn_exp2f(slope[j] * fs[k][j]);
+        fa[k][j] = in ? f : 1.f;
+        gh[k][j] = in ? Quad<T>::get(rg[k], j) : 0.f;
+        s.b[j] = fa[k][j] * (s.b[j] + gh[k][j]);
+        s.a[j] *= fa[k][j];
+      }
+    }
+    const bool last = ts <= 0;
+    chain(s, at, out, q, sh, pair, (int)n, last, y0, wave, rank, col);
+#pragma unroll
+    for (int k = K - 1; k >= 0; --k) {
+      if (t0 + k < 0) continue;
+      float hb[V], vx[V], vi[V], vr[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) hb[j] = Quad<T>::get(rh[k], j);
+      if (t0 + k == 0) load_state(a.s_first, a, p, hb);
+      grads_of<T>(slope, fs[k], fa[k], gh[k], ri[k], rx[k], hb, at, sum, vx, vi, vr);
+      if (p.on) {
+        Quad<T>::put(ox.at(ts, k), vx);
+        Quad<T>::put(oi.at(ts, k), vi);
+        Quad<T>::put(orr.at(ts, k), vr);
+      }
+    }
+    if (last && a.s_out && wave == 0) a.s_out[state_at] = out;
+  } else if (n == 0 && a.s_out && wave == 0) {
+    a.s_out[state_at] = a.s_in ? a.s_in[state_at] : 0.f;
+  }
+  zero_stretch<T, kTile>(a, a.dx, p, len, (int)n, run);
+  zero_stretch<T, kTile>(a, a.di, p, len, (int)n, run);
+  zero_stretch<T, kTile>(a, a.dr, p, len, (int)n, run);
+  if (a.part) {
+    __shared__ __align__(16) float all[kRuns * kSlab];
+    block_sums(a, sum, all, wave * TW + rank, col, slab, p.b * q.tiles + n);
+  }
+}
+
+// The words before a launch, and its ticket.
+__global__ void __launch_bounds__(256) k_recur_clear(uint4* __restrict__ p, int64_t n, uint32_t* __restrict__ ticket) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = uint4{kNone, kNone, kNone, kNone};
+  if (i == 0) *ticket = 0;
 }
 
 // ddecay from the blocks' sums: 16 channels a block, 64 threads a channel (every
@@ -571,17 +753,22 @@ __global__ void __launch_bounds__(256)
 
 // ---- host ---------------------------------------------------------------------------
 constexpr int64_t kMaxToken = (int64_t)1 << 21;  // (a tile has at most 2^8 tokens of 4-byte values)
-// Tokens of a thread's run.  Fewer registers and more waves against the shuffles and
-// LDS of a tile: one history of 65521 tokens of 1024 channels, bfloat16, 219 us with 4,
-// 236 with 8; backward of 8 x 2048 tokens of 2048 channels 121 us with 2, 127 with 4; a
-// wave for each of 8192 histories of 24 tokens, float32, 62 us with 1, 67 with 2.
+// Tokens of a thread's run.  Where a block walks a sequence, fewer registers and more
+// waves against the shuffles and LDS of a tile: backward of 8 x 2048 tokens of 2048
+// channels, bfloat16, 102 us with 2, 108 with 4; a wave for each of 8192 float32
+// histories of 24 tokens 62 us with 1, 67 with 2.
 constexpr int fwd_run(bool wave) { return wave ? 2 : 4; }
 constexpr int bwd_run(bool wave) { return wave ? 1 : 2; }
+// In a chain the whole tile is in flight at once: one history of 65521 tokens of 1024
+// channels, bfloat16, 148 us with 12, 154 with 8, 158 with 16, 233 with 4; 8 x 2048
+// tokens of 1024 channels, float32, 64 us with 8, 77 with 4; their backward 124 us with
+// 5, 130 with 4, 147 with 6; in bfloat16, 2048 channels, 105 us with 8, 126 with 12.
+constexpr int chain_run(bool bwd, bool f32) { return bwd ? (f32 ? 5 : 8) : (f32 ? 8 : 12); }
 
 struct Split {
   bool wave;         // a wave for each sequence
-  int32_t slabs, segs;
-  int64_t seg_len;
+  bool chain;        // a block for each tile, in one pass
+  int32_t slabs, tiles;
   int64_t rows;      // blocks of a slab
   int32_t stride;    // WAVE backward: sequences between two of one wave
 };
@@ -591,33 +778,37 @@ Split split_of(const hg_recur_desc* A, bool bwd) {
   s.slabs = (int32_t)cdiv(A->width, kSlab);
   const int64_t pairs = (int64_t)A->batch * s.slabs;
   s.wave = pairs >= 4096 || A->t <= 64;
-  s.segs = 1;
-  s.seg_len = std::max<int64_t>(A->t, 1);
   if (s.wave) {
     s.rows = cdiv(A->batch, kNW);
     if (bwd) s.rows = std::min<int64_t>(s.rows, std::max<int64_t>(1, cdiv(2048, s.slabs)));
     s.stride = (int32_t)(s.rows * kNW);
     return s;
   }
-  const int64_t tile = (int64_t)kNW * TW * (bwd ? bwd_run(false) : fwd_run(false));
-  const int64_t n = std::min<int64_t>(1024 / std::max<int64_t>(pairs, 1), A->t / (4 * tile));
-  if (n > 1) {
-    s.seg_len = cdiv(cdiv(A->t, n), tile) * tile;
-    s.segs = (int32_t)cdiv(A->t, s.seg_len);
-  }
-  s.rows = (int64_t)A->batch * s.segs;
+  // Few sequences: one pass, a block a tile.  Walked in segments by a block each, after
+  // a pass that composes the segments' steps, the long history above took 219 us.
+  const int64_t tile = (int64_t)kNW * TW * chain_run(bwd, A->dtype == HG_DTYPE_F32);
+  s.chain = pairs < 1024 && pairs * cdiv(A->t, tile) < (int64_t)1 << 24;  // (a grid has fewer than 2^32 threads)
+  s.tiles = s.chain ? (int32_t)cdiv(A->t, tile) : 1;
+  s.rows = (int64_t)A->batch * s.tiles;
   return s;
 }
 
 struct Bufs {
-  float *sums = nullptr, *part = nullptr;
+  float* part = nullptr;
+  uint32_t* words = nullptr;  // a chain's steps, then its values, then the ticket
+  int64_t clear = 0;          // of them before the ticket
 };
+int64_t chain_groups(const Split& s) { return cdiv(s.tiles, kGroup); }
 template <class Mem>
 Bufs take(const hg_recur_desc* A, bool bwd, Mem& m) {
   const Split s = split_of(A, bwd);
+  const int64_t pairs = (int64_t)A->batch * s.slabs;
   Bufs b;
-  b.sums = m.template take<float>(s.segs > 1 ? (int64_t)A->batch * s.segs * 2 * A->width : 0);
   b.part = m.template take<float>(bwd ? s.rows * A->width : 0);
+  if (s.chain) {
+    b.clear = pairs * (2 * s.tiles + chain_groups(s)) * kSlab;
+    b.words = m.template take<uint32_t>(b.clear + 4);
+  }
   return b;
 }
 
@@ -627,7 +818,7 @@ int check(const hg_recur_desc* A, const char* what) {
     return fail(HG_ERR_ARG, "%s: batch=%d t=%lld width=%d rate=%g", what, A->batch, (long long)A->t, A->width, (double)A->rate);
   if (A->dtype != HG_DTYPE_F32 && A->dtype != HG_DTYPE_BF16) return fail(HG_ERR_ARG, "%s: dtype %d", what, A->dtype);
   if (A->width < V) return fail(HG_ERR_UNSUPPORTED, "%s: width %d is below %d", what, A->width, V);
-  // (a grid has fewer than 2^32 threads: 512 for each slab of a sequence's segment)
+  // (a grid has fewer than 2^32 threads: 256 for each slab of a sequence)
   if (A->width > 1 << 20 || A->t > (int64_t)1 << 40 || (int64_t)A->batch * cdiv(A->width, kSlab) >= (int64_t)1 << 22 ||
       (int64_t)A->batch * A->width >= ((int64_t)1 << 32) - 256)
     return fail(HG_ERR_UNSUPPORTED, "%s: %d sequences of %lld tokens and %d channels are too many", what, A->batch,
@@ -649,19 +840,37 @@ RecurArgs args_of(const hg_recur_desc* A, const Split& s, const float* decay, co
   a.decay = decay;
   a.lens = lens;
   a.t = A->t;
-  a.seg_len = s.seg_len;
   a.batch = A->batch;
   a.width = A->width;
   a.slabs = s.slabs;
-  a.segs = s.segs;
   a.rate = A->rate;
   return a;
 }
 
+// A chain's words set, and where they are.
+int clear_chain(const RecurArgs& a, const Split& s, const Bufs& b, Chain* q, hipStream_t st) {
+  const int64_t pairs = (int64_t)a.batch * a.slabs;
+  q->step = reinterpret_cast<uint64_t*>(b.words);
+  q->value = b.words + pairs * 2 * s.tiles * kSlab;
+  q->ticket = b.words + b.clear;
+  q->tiles = s.tiles;
+  q->groups = (int32_t)chain_groups(s);
+  q->pairs = (uint32_t)pairs;
+  HG_LAUNCH("recur_clear", k_recur_clear, dim3((unsigned)cdiv(b.clear / 4, 256)), dim3(256), 0, st, reinterpret_cast<uint4*>(b.words),
+            b.clear / 4, q->ticket);
+  return HG_OK;
+}
+
 template <class T>
-int launch_fwd(const RecurArgs& a, const Split& s, hipStream_t st) {
+int launch_fwd(const RecurArgs& a, const Split& s, const Bufs& b, hipStream_t st) {
+  if (s.chain) {
+    Chain q{};
+    HG_TRY(clear_chain(a, s, b, &q, st));
+    HG_LAUNCH("recur_chain", (k_recur_chain_fwd<T, chain_run(false, sizeof(T) == 4)>), dim3((unsigned)(s.rows * s.slabs)),
+              dim3(kNW * 64), 0, st, a, q);
+    return HG_OK;
+  }
   const dim3 grid((unsigned)(s.rows * s.slabs)), block(kNW * 64);
-  if (s.segs > 1) HG_LAUNCH("recur_sums", (k_recur_sums<T, fwd_run(false), false>), grid, block, 0, st, a);
   if (s.wave) {
     HG_LAUNCH("recur", (k_recur_fwd<T, fwd_run(true), true>), grid, block, 0, st, a);
   } else {
@@ -671,9 +880,15 @@ int launch_fwd(const RecurArgs& a, const Split& s, hipStream_t st) {
 }
 
 template <class T>
-int launch_bwd(const RecurArgs& a, const Split& s, hipStream_t st) {
+int launch_bwd(const RecurArgs& a, const Split& s, const Bufs& b, hipStream_t st) {
+  if (s.chain) {
+    Chain q{};
+    HG_TRY(clear_chain(a, s, b, &q, st));
+    HG_LAUNCH("recur_bwd_chain", (k_recur_chain_bwd<T, chain_run(true, sizeof(T) == 4)>), dim3((unsigned)(s.rows * s.slabs)),
+              dim3(kNW * 64), 0, st, a, q);
+    return HG_OK;
+  }
   const dim3 grid((unsigned)(s.rows * s.slabs)), block(kNW * 64);
-  if (s.segs > 1) HG_LAUNCH("recur_bwd_sums", (k_recur_sums<T, bwd_run(false), true>), grid, block, 0, st, a);
   if (s.wave) {
     HG_LAUNCH("recur_bwd", (k_recur_bwd<T, bwd_run(true), true>), grid, block, 0, st, a, s.stride);
   } else {
@@ -722,7 +937,7 @@ extern "C" int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   Arena m(ws, ws_bytes);
   const Split s = split_of(A, false);
   RecurArgs a = args_of(A, s, decay, lens);
-  a.sums = take(A, false, m).sums;
+  const Bufs b = take(A, false, m);
   a.x = rx;
   a.r = rr;
   a.i = ri;
@@ -730,7 +945,7 @@ extern "C" int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   a.s_in = state;
   a.s_out = state_out;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  return A->dtype == HG_DTYPE_F32 ? launch_fwd<float>(a, s, st) : launch_fwd<bf16_t>(a, s, st);
+  return A->dtype == HG_DTYPE_F32 ? launch_fwd<float>(a, s, b, st) : launch_fwd<bf16_t>(a, s, b, st);
 }
 
 extern "C" int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_heads* r, const hg_heads* i,
@@ -761,7 +976,6 @@ extern "C" int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   const Split s = split_of(A, true);
   const Bufs b = take(A, true, m);
   RecurArgs a = args_of(A, s, decay, lens);
-  a.sums = b.sums;
   a.part = ddecay ? b.part : nullptr;
   a.x = in[0];
   a.r = in[1];
@@ -774,7 +988,7 @@ extern "C" int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   a.s_first = state;
   a.s_in = dstate_out;
   a.s_out = dstate;
-  HG_TRY(A->dtype == HG_DTYPE_F32 ? launch_bwd<float>(a, s, st) : launch_bwd<bf16_t>(a, s, st));
+  HG_TRY(A->dtype == HG_DTYPE_F32 ? launch_bwd<float>(a, s, b, st) : launch_bwd<bf16_t>(a, s, b, st));
   if (ddecay)
     HG_LAUNCH("recur_ddecay", k_recur_ddecay, dim3((unsigned)cdiv(A->width, 16)), dim3(1024), 0, st, a.part, s.rows, A->width,
               decay, A->rate, ddecay, accumulate);

@@ -151,8 +151,10 @@ def test_muon_refusals(L):
     assert step(None) == step(d(), W=None) == step(d(), G=None) == step(d(), M=None) == ARG
     assert step(d(), W=P + 2) == step(d(), G=2 * P + 1) == step(d(), M=3 * P + 2) == step(d(), ws=4 * P + 8) == ARG
     assert step(d(), G=P) == step(d(), M=P + 1024) == step(d(), M=2 * P - 16) == ARG
-    need = L.hg_muon_workspace_size(d())
-    assert need > 0 and step(d(), n=need - 1) == step(d(), ws=None) == CAPACITY
+    large = d(m=200, n=300)  # small matrices need no workspace
+    need = L.hg_muon_workspace_size(large)
+    assert L.hg_muon_workspace_size(d()) == 0 < need
+    assert step(large, M=9 * P, n=need - 1) == step(large, M=9 * P, ws=None) == CAPACITY
     assert step(d(c=0)) == OK
 
 

@@ -61,7 +61,7 @@ def lens_of(kind, b, t):
 CASES = [(2, 1, 8, None, True), (3, 3, 5, "ragged", False), (2, 9, 64, "ragged", True), (2, 64, 67, "wild", True),
          (1, 65, 4, None, False), (2, 130, 30, "empty", True), (3, 257, 64, "ragged", True), (1, 700, 129, None, True),
          (1, 2100, 66, None, False), (2, 2500, 33, "wild", True), (130, 40, 16, "ragged", False),
-         (70, 70, 4200, "ragged", True)]
+         (70, 70, 4200, "ragged", True), (1030, 70, 16, "ragged", True), (1, 9000, 70, None, True)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -74,7 +74,7 @@ def test_forward_and_backward(b, t, w, lens, state, dtype):
     h, s1 = api.hg_recur_fwd(x, r, i, g, lens=n, state=s0, want_state=True)
     dh = normal(9, b, t, w, dtype=dtype)
     got = api.hg_recur_bwd(x, r, i, g, h, dh, lens=n, state=s0, dstate_out=ds)
-    if b * t * w > 10 ** 7:  # the oracle on some sequences; all of the sum by linearity is another case's
+    if b > 64:  # the oracle on some sequences
         keep = [0, 1, b - 1]
         x, r, i, h, dh = (v[keep] for v in (x, r, i, h, dh))
         s0, ds, s1, n = (None if v is None else v[keep] for v in (s0, ds, s1, n))
@@ -93,10 +93,41 @@ def test_forward_and_backward(b, t, w, lens, state, dtype):
             assert not h[k, m:].any() and not any(v[k, m:].any() for v in got[:3])
 
 
-def test_segments_and_waves_are_exercised():
-    """The sizes above reach the paths that they are there for."""
-    assert api.hg_recur_fwd_workspace_size(1, 2100, 66) > 0 and api.hg_recur_fwd_workspace_size(2, 130, 64) == 0
-    assert api.hg_recur_bwd_workspace_size(1, 2100, 66) > api.hg_recur_bwd_workspace_size(1, 64, 66)
+def test_the_paths_are_exercised():
+    """The sizes above reach the paths that they are there for: waves and blocks that walk a sequence need no
+    workspace forward, tiles that compose through memory do."""
+    size = api.hg_recur_fwd_workspace_size
+    assert size(130, 40, 16) == size(1030, 70, 16) == size(70, 70, 4200) == 0
+    assert min(size(1, 65, 4), size(2, 2500, 33), size(1, 9000, 70)) > 0
+
+
+def test_results_do_not_depend_on_timing():
+    """Tiles that compose through memory: the same bits each time, with other work beside them too."""
+    b, t, w = 2, 9000, 100
+    x, r, i = problem(b, t, w, F32)
+    g, dh, n = decays(w), normal(4, b, t, w), lens_of("ragged", b, t)
+    first = None
+    other, side = torch.randn(4096, 4096).cuda(), torch.cuda.Stream()
+    for k in range(6):
+        if k % 2:
+            with torch.cuda.stream(side):
+                other @ other
+        h, s = api.hg_recur_fwd(x, r, i, g, lens=n, want_state=True)
+        out = [h, s] + [v for v in api.hg_recur_bwd(x, r, i, g, h, dh, lens=n) if v is not None]
+        first = first or out
+        assert all(torch.equal(p, q) for p, q in zip(first, out))
+    torch.cuda.synchronize()
+
+
+def test_two_calls_at_once():
+    b, t, w = 1, 20000, 80
+    x, r, i = problem(b, t, w, BF16)
+    want, _ = api.hg_recur_fwd(x, r, i, decays(w))
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = [api.hg_recur_fwd(x, r, i, decays(w), stream=s)[0] for s in streams for _ in range(3)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(v, want) for v in got)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

@@ -819,7 +819,7 @@ int small_of(const hg_muon_desc* A, size_t* bytes) {
   if (A->steps == 0 || m > 128) return 0;
   const int mp = m <= 32 ? 32 : m <= 64 ? 64 : 128, cp = lo ? 32 : 64;
   const size_t panels = (size_t)(cdiv(n, cp) + cdiv(mp, cp)), need = panels * mp * 128;
-  if (need > 152 * 1024) return 0;  // (and 4 KB for the norm)
+  if (need > 152 * 1024) return 0;  // (and 8 KB for the norm)
   *bytes = need;
   return mp;
 }

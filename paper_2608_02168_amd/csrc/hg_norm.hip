@@ -709,12 +709,8 @@ int launch_bwd(const Plan& p, NormArgs a, const Bufs& b, float* dw, float* db, i
       }
     } else if (p.r == 1) {
       HG_LAUNCH(name, (k_norm_bwd<T, V, 1, 1024>), grid, dim3(1024), 0, s, a);
-    } else if (p.r == 2) {
-      HG_LAUNCH(name, (k_norm_bwd<T, V, 2, 1024>), grid, dim3(1024), 0, s, a);
-    } else if (V < 8 && p.r == 4) {
-      HG_LAUNCH(name, (k_norm_bwd<T, V < 8 ? V : 4, 4, 1024>), grid, dim3(1024), 0, s, a);
     } else {
-      HG_LAUNCH(name, (k_norm_bwd<T, V == 1 ? 1 : 4, 8, 1024>), grid, dim3(1024), 0, s, a);
+      HG_LAUNCH(name, (k_norm_bwd<T, V < 8 ? V : 4, 2, 1024>), grid, dim3(1024), 0, s, a);  // (never with eight channels)
     }
     if (dw || db)
       HG_LAUNCH("group_norm_grads", k_norm_grads, dim3(first), dim3(1024), 0, s, b.part, (int64_t)a.row_blocks, a.width,

@@ -76,6 +76,7 @@ def test_recur_refusals(L):
     assert fwd(d(), x=None) == fwd(d(), r=rows(0)) == fwd(d(), g=None) == fwd(d(), h=None) == ARG
     assert fwd(d(), x=rows(1, shift=1)) == fwd(d(), x=rows(1, token=-1)) == fwd(d(), x=rows(1, batch=1 << 41)) == ARG
     assert fwd(d(), h=rows(1)) == fwd(d(), h=rows(2, shift=2)) == fwd(d(), h=rows(3, token=17)) == ARG   # overlap inputs
+    assert fwd(d(), x=rows(1, batch=1 << 30, token=(1 << 21) + 1)) == UNSUPPORTED
     assert fwd(d(), h=rows(6, token=15)) == fwd(d(), h=rows(6, batch=300)) == fwd(d(), so=5 * P) == ARG
     assert bwd(d(), dx=rows(9), dr=rows(9)) == bwd(d(), di=rows(6)) == bwd(d(), dx=rows(8)) == ARG
     assert bwd(d(), ds=13 * P) == bwd(d(), ds=5 * P) == bwd(d(), dg=4 * P) == bwd(d(), acc=2) == ARG

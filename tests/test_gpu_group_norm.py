@@ -54,7 +54,8 @@ CASES = [(1, 1, 1, 1, None), (7, 1, 64, 4, None), (300, 1, 96, 12, None), (5, 1,
          (3, 1, 2048, 1, None), (2, 1, 8192, 2, None), (9, 1, 40, 40, None), (4, 1, 1000, 1, None), (17, 1, 60, 5, "ragged"),
          (6, 5, 32, 4, "ragged"), (64, 24, 64, 4, "ragged"), (5, 96, 200, 5, "wild"), (2, 100, 24, 3, "empty"),
          (3, 333, 48, 2, "ragged"), (40, 700, 16, 2, None), (1, 5000, 128, 8, None), (2, 9001, 40, 5, "ragged"),
-         (1, 4000, 25, 1, None), (2, 3000, 1100, 11, "wild"), (1, 70000, 16, 16, None)]
+         (1, 4000, 25, 1, None), (2, 3000, 1100, 11, "wild"), (1, 70000, 16, 16, None), (2, 20, 512, 2, "ragged"), (3, 7, 2048, 1, None),
+         (2, 60, 300, 3, "wild"), (9, 3, 1000, 1, None), (1, 300, 1024, 1, None)]
 
 
 def clear_of_kinks(x, w, b, groups, lens):
@@ -146,6 +147,22 @@ def test_rows_where_they_lie(t, dtype):
     mask = torch.zeros_like(out, dtype=torch.bool)
     mask[:, :, :t, 1:1 + width] = True
     assert (out[~mask] == 7.0).all()
+
+
+@pytest.mark.parametrize("t", [9, 2100])
+def test_offsets_beyond_32_bits(t):
+    """Rows up to 8.8 GB behind the first (a row past 2^32 bytes, in the same and in chunks of a sequence)."""
+    width, far = 16, 1 << (21 if t > 1000 else 29)
+    mem = torch.empty((t - 1) * far + 3 * width, dtype=BF16, device="cuda")
+    x, y, dx = (mem.as_strided((1, t, width), (0, far, 1), k * width) for k in range(3))
+    x.copy_(normal(1, 1, t, width))
+    w, b, dy = 1 + 0.1 * normal(2, width), normal(3, width), normal(4, 1, t, width, dtype=BF16)
+    want, st = api.hg_group_norm_fwd(x.contiguous(), 2, w, b, act=2, want_stats=True)
+    api.hg_group_norm_fwd(x, 2, w, b, act=2, y=y)
+    assert torch.equal(y, want)
+    ref = api.hg_group_norm_bwd(x.contiguous(), 2, w, b, st, dy, act=2)
+    got = api.hg_group_norm_bwd(x, 2, w, b, st, dy, act=2, dx=dx)
+    assert all(torch.equal(p, q) for p, q in zip(got, ref)) and torch.equal(y, want)
 
 
 @pytest.mark.parametrize("t", [1, 40, 6000])

@@ -44,7 +44,7 @@ def directions(seed, m, n, dtype):
 
 SIZES = [(1, 1), (1, 50), (50, 1), (3, 5), (16, 16), (17, 64), (64, 64), (65, 63), (63, 200), (128, 128), (129, 257), (200, 517),
          (517, 200), (256, 1000), (1030, 70), (300, 300), (640, 1111), (32, 900), (31, 33), (64, 700), (128, 350), (100, 97),
-         (1100, 90), (33, 1400), (1500, 140)]
+         (1100, 90), (33, 1400), (1500, 140), (64, 544), (64, 545), (32, 1184), (448, 128), (449, 128), (129, 128), (2100, 130)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -148,3 +148,30 @@ def test_replayed_graph(m, n, dtype):
         torch.cuda.synchronize()
         api.hg_muon_step(w, G, mom, lr=0.1)
         assert torch.equal(W, w) and torch.equal(M, mom)
+
+
+# tiles of 256 x 256 and 128 x 128, symmetric products of 128 x 128 with and without parts of k, several rounds of tiles
+LARGE = [(2048, 6400, BF16), (6403, 2050, BF16), (1024, 8192, F32), (8190, 1030, F32), (2100, 2100, F32), (1500, 3001, BF16),
+         (520, 4100, F32), (1037, 1041, F32)]
+
+
+@pytest.mark.parametrize("m,n,dtype", LARGE)
+def test_large_tiles(m, n, dtype):
+    """Against the same formula by torch in float64 on the device; the whole matrix and its worst 64 x 64 block, so
+    that no single tile is off."""
+    G = normal(1, m, n, dtype=dtype)
+    W = torch.zeros_like(G)
+    api.hg_muon_step(W, G, torch.zeros(m, n).cuda(), lr=1.0, mu=0.0, scale=1.0)
+    p, q, s = rec.COEF
+    X = G.double()
+    X /= X.norm()
+    for _ in range(5):
+        A = X @ X.T if m <= n else X.T @ X
+        B = q * A + s * (A @ A)
+        X = p * X + (B @ X if m <= n else X @ B)
+    bar = 3e-5 if dtype is F32 else 5e-3
+    d = -W.double() - X
+    assert float(d.norm() / X.norm()) < bar
+    pad = torch.nn.functional.pad(d.square(), (0, -n % 64, 0, -m % 64))
+    blocks = pad.view(-(-m // 64), 64, -(-n // 64), 64).sum((1, 3))
+    assert float(blocks.max().sqrt()) < 4 * bar * 64 * float(X.square().mean().sqrt())

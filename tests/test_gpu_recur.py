@@ -231,6 +231,25 @@ def test_rows_where_they_lie(dtype):
     assert (out[~mask] == 7.0).all()
 
 
+@pytest.mark.parametrize("b", [1, 300])
+def test_offsets_beyond_32_bits(b):
+    """Tokens (or sequences) up to 8.8 GB behind the first."""
+    t, w, far = (2100, 16, 1 << 21) if b == 1 else (16, 16, 1 << 24)
+    strides = (0, far, 1) if b == 1 else (far, 8 * w, 1)
+    mem = torch.empty((2100 if b == 1 else 300) * far, dtype=BF16, device="cuda")
+    x, r, i, h, dx, dr, di = (mem.as_strided((b, t, w), strides, k * w) for k in range(7))
+    for k, v in enumerate((x, r, i)):
+        v.copy_(normal(k, b, t, w))
+    g, dh = decays(w), normal(4, b, t, w, dtype=BF16)
+    near = [v.contiguous() for v in (x, r, i)]
+    want, s1 = api.hg_recur_fwd(*near, g, want_state=True)
+    _, s2 = api.hg_recur_fwd(x, r, i, g, h=h, want_state=True)
+    assert torch.equal(h, want) and torch.equal(s1, s2)
+    ref = api.hg_recur_bwd(*near, g, want, dh)
+    got = api.hg_recur_bwd(x, r, i, g, h, dh, dx=dx, dr=dr, di=di)
+    assert all(torch.equal(p, q) for p, q in zip(got[:4], ref[:4])) and torch.equal(h, want)
+
+
 def test_accumulated_decay_gradient():
     x, r, i = problem(5, 33, 10, F32)
     h, _ = api.hg_recur_fwd(x, r, i, decays(10))

@@ -202,41 +202,21 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
   affine<V>(a, s, w, bias);
 #pragma unroll
   for (int j = 0; j < V; ++j) dw[j] = db[j] = 0.f;
-  // the next item's rows are under way while one is worked on, where they are few
-  constexpr int AHEAD = V > 1 && R <= 2 && BT <= 256 ? 2 : 1;
-  typename Vec<T, V>::raw xs[AHEAD][R], ys[AHEAD][R];
-  typename Vec<float, 2>::raw st[AHEAD];
-  int64_t ns[AHEAD];
-  const int64_t step = (int64_t)a.row_blocks * a.rper;
-  auto fetch = [&](int to, int64_t b) {
+  int odd = 0;
+  for (int64_t i0 = (int64_t)s.rb * a.rper; i0 < a.rows; i0 += (int64_t)a.row_blocks * a.rper, odd ^= 1) {
+    const int64_t b = i0 + s.row;
     const bool in = s.on && b < a.rows;
     const int64_t n = in ? len_of(a, b) : 0;
-    ns[to] = n;
+    typename Vec<T, V>::raw x[R], y[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const int64_t t = s.r + k * s.nr;
       if (t < n) {
-        xs[to][k] = Vec<T, V>::load(at<T, V>(a.x, b, t, s.c));
-        ys[to][k] = Vec<T, V>::load(at<T, V>(a.dy, b, t, s.c));
+        x[k] = Vec<T, V>::load(at<T, V>(a.x, b, t, s.c));
+        y[k] = Vec<T, V>::load(at<T, V>(a.dy, b, t, s.c));
       }
     }
-    st[to] = in ? Vec<float, 2>::load(a.stats + (b * a.groups + s.g) * 2) : Vec<float, 2>::raw{0.f, 0.f};
-  };
-  const int64_t first = (int64_t)s.rb * a.rper;
-  if (AHEAD > 1) fetch(0, first + s.row);
-  int odd = 0;
-  auto item = [&](auto now, int64_t i0) {
-    constexpr int NOW = decltype(now)::value;
-    const int64_t b = i0 + s.row;
-    const bool in = s.on && b < a.rows;
-    if (AHEAD > 1) {
-      if (i0 + step < a.rows) fetch(NOW ^ 1, b + step);
-    } else {
-      fetch(0, b);
-    }
-    const int64_t n = ns[NOW];
-    typename Vec<T, V>::raw(&x)[R] = xs[NOW], (&y)[R] = ys[NOW];
-    const float mean = st[NOW][0], rstd = st[NOW][1];
+    const float mean = in ? a.stats[(b * a.groups + s.g) * 2] : 0.f, rstd = in ? a.stats[(b * a.groups + s.g) * 2 + 1] : 0.f;
     float e[R][V], sum[2] = {0.f, 0.f};
     g_by_act<true>(a.act, [&](auto act) {
       constexpr int ACT = decltype(act)::value;
@@ -262,7 +242,6 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
         }
     });
     item_sum<2>(sum, a.lp, sh[odd]);
-    odd ^= 1;
     const float inv = n > 0 ? 1.f / (float)(n * a.cg) : 0.f, m0 = sum[0] * inv, m1 = sum[1] * inv;
     if (in)
 #pragma unroll
@@ -277,10 +256,6 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
         }
         Vec<T, V>::put(at<T, V>(a.y, b, t, s.c), o);
       }
-  };
-  for (int64_t i0 = first; i0 < a.rows; i0 += AHEAD * step) {
-    item(std::integral_constant<int, 0>{}, i0);
-    if (AHEAD > 1 && i0 + step < a.rows) item(std::integral_constant<int, AHEAD - 1>{}, i0 + step);
   }
   if (!a.part) return;
   // the block's sums of each channel: over its rows and row lanes, in order
@@ -597,8 +572,8 @@ Plan plan_of(const hg_group_norm_desc* A, bool bwd) {
     p.r = 1 << std::min(3, log2_up(cdiv(t, (int64_t)1 << lr)));
     p.bt = a.lp <= 8 ? 256 : 1024;
     // A row of partial sums of dw and db for each block of the backward: few blocks
-    // (16384 rows of 16 x 64 channels 38 us with 1024, 46 with 1536), but single channels
-    // a thread are few bytes in flight and take more (20000 rows of 32 x 25 channels 95
+    // (16384 rows of 16 x 64 channels 40 us with 1024, 45 with 1536), but single channels
+    // a thread are few bytes in flight and take more (20000 rows of 32 x 25 channels 81
     // us with 4096, 115 with 2048).
     lay_out(p, A->batch, !bwd ? (int64_t)1 << 21 : p.bt == 256 ? (p.v == 1 ? 4096 : 1024) : 512);
     return p;

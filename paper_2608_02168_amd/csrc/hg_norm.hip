@@ -14,6 +14,11 @@
 // means and squares of the chunks by the same kernel, joined (k_norm_join), and a
 // pass that forms the output (k_norm_apply); in the backward sums of the columns,
 // joined, and a pass.
+//
+// Bound by HBM, the backward with an activation by the vector unit as well (53% of the
+// cycles: 16384 rows of 16 x 64 bfloat16 channels 37 us, 2.7 TB/s).  A float32 backward
+// of 200003 rows of 128 channels: 51 us for the columns (4.1 TB/s), 48 for the pass
+// (6.4); a forward of 512 x 96 tokens of 200 float32 channels 18 us (3.9).
 #include <cmath>
 
 #include "hg_gemm.h"
@@ -636,6 +641,13 @@ int check(const hg_group_norm_desc* A, const char* what) {
   return HG_OK;
 }
 
+int check_grid(const Plan& p, const hg_group_norm_desc* A, const char* what) {
+  if (p.blocks * p.bt >= (int64_t)1 << 32)
+    return fail(HG_ERR_UNSUPPORTED, "%s: %d sequences of %lld tokens and %d channels are too many", what, A->batch,
+                (long long)A->t, A->width);
+  return HG_OK;
+}
+
 unsigned apply_blocks(const NormArgs& a, int v) {
   return (unsigned)cdiv((int64_t)a.batch * cdiv(a.t, kApply) * (a.width / v), 256);
 }
@@ -737,6 +749,7 @@ extern "C" int hg_group_norm_fwd(const hg_group_norm_desc* A, const hg_heads* x,
   if (A->t == 0) return stats ? fill_f32(stats, 0.f, (int64_t)A->batch * A->groups * 2, s) : HG_OK;
   if (rows_meet(y, x, A->batch, A->t, A->width, A->dtype)) return fail(HG_ERR_ARG, "%s: y overlaps x", what);
   const Plan p = plan_of(A, false);
+  HG_TRY(check_grid(p, A, what));
   Sizer need;
   take(p, false, need);
   HG_TRY(check_workspace(what, ws, ws_bytes, need.used));
@@ -774,9 +787,12 @@ extern "C" int hg_group_norm_bwd(const hg_group_norm_desc* A, const hg_heads* x,
   if (!stats) return fail(HG_ERR_ARG, "%s: null stats", what);
   for (const hg_heads* v : {x, dy})
     if (rows_meet(dx, v, A->batch, A->t, A->width, A->dtype)) return fail(HG_ERR_ARG, "%s: dx overlaps an input", what);
-  if ((dw && (dw == w || dw == b || dw == db)) || (db && (db == w || db == b)))
+  const size_t vec = (size_t)A->width * 4;
+  if (ranges_meet(dw, vec, w, vec) || ranges_meet(dw, vec, b, vec) || ranges_meet(dw, vec, db, vec) || ranges_meet(db, vec, w, vec) ||
+      ranges_meet(db, vec, b, vec))
     return fail(HG_ERR_ARG, "%s: a gradient's buffer is another of the call's", what);
   const Plan p = plan_of(A, true);
+  HG_TRY(check_grid(p, A, what));
   Sizer need;
   take(p, true, need);
   HG_TRY(check_workspace(what, ws, ws_bytes, need.used));

@@ -429,7 +429,10 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
 // A published word is its own flag: the words are all ones (a NaN that no step is
 // stored as) before the launch, and are stored and read whole, at device scope.  A
 // block waits for blocks of lower tickets only, which have started, and which publish
-// their step before they wait for anything: every wait ends.
+// their step before they wait for anything: every wait ends.  (Two calls at once on one
+// workspace clear each other's words.  A wait that has looked kTries times, seconds,
+// writes NaN for its word, so that such calls end too, with NaN; a ticket past the last
+// tile ends its block.)
 constexpr int kGroup = 32;  // (16 and 64: within 1 %)
 constexpr uint32_t kNone = 0xFFFFFFFFu;
 
@@ -447,6 +450,24 @@ __device__ __forceinline__ uint32_t word_of(float v) {
 }
 __device__ __forceinline__ uint64_t peek(const uint64_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ uint32_t peek(const uint32_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+constexpr int kTries = 1 << 22;
+__device__ __forceinline__ uint32_t flag_of(uint64_t w) { return (uint32_t)w; }
+__device__ __forceinline__ uint32_t flag_of(uint32_t w) { return w; }
+// The word at p once it is there; w: as it was read before.
+template <class W>
+__device__ __forceinline__ W await(W* p, W w) {
+  for (int n = 0; flag_of(w) == kNone; ++n) {
+    if (n == kTries) {
+      w = sizeof(W) == 8 ? (W)0x7FC000007FC00000ull : (W)0x7FC00000u;
+      __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      break;
+    }
+    __builtin_amdgcn_s_sleep(1);
+    w = peek(p);
+  }
+  return w;
+}
 
 struct ChainLds {
   float wave[kNW][2][kSlab];  // the waves' steps
@@ -498,10 +519,7 @@ __device__ __forceinline__ void chain(Step& s, float (&at)[V], float& out, const
 #pragma unroll
     for (int k = 0; k < PER; ++k)
       if (wave * PER + k < r) {
-        while ((uint32_t)w[k] == kNone) {
-          __builtin_amdgcn_s_sleep(1);
-          w[k] = peek(steps + (int64_t)(wave * PER + k) * kSlab);
-        }
+        w[k] = await(steps + (int64_t)(wave * PER + k) * kSlab, w[k]);
         const float a = __uint_as_float((uint32_t)w[k]), b = __uint_as_float((uint32_t)(w[k] >> 32));
         fb = fmaf(a, fb, b);
         fa *= a;
@@ -513,13 +531,8 @@ __device__ __forceinline__ void chain(Step& s, float (&at)[V], float& out, const
   if (wave == 0) {
     float y = y0;
     if (group > 0) {
-      const uint32_t* v = q.value + ((int64_t)pair * q.groups + group) * kSlab + lane;
-      uint32_t u = peek(v);
-      while (u == kNone) {
-        __builtin_amdgcn_s_sleep(1);
-        u = peek(v);
-      }
-      y = __uint_as_float(u);
+      uint32_t* v = q.value + ((int64_t)pair * q.groups + group) * kSlab + lane;
+      y = __uint_as_float(await(v, peek(v)));
     }
 #pragma unroll
     for (int w = 0; w < kNW; ++w) y = fmaf(sh.far[w][0][lane], y, sh.far[w][1][lane]);
@@ -561,6 +574,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_fwd(const RecurArgs a,
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
   constexpr int kTile = kNW * TW * K;
   const uint32_t ticket = take_ticket(q, sh), n = ticket / q.pairs, pair = ticket - n * q.pairs;
+  if (n >= (uint32_t)q.tiles) return;
   const int slab = (int)(pair % (uint32_t)a.slabs), run = wave * TW + rank;
   Place p;
   p.b = pair / (uint32_t)a.slabs;
@@ -624,6 +638,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a,
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane % CL, rank = lane / CL;
   constexpr int kRuns = kNW * TW, kTile = kRuns * K;
   const uint32_t ticket = take_ticket(q, sh), n = ticket / q.pairs, pair = ticket - n * q.pairs;
+  if (n >= (uint32_t)q.tiles) return;
   const int slab = (int)(pair % (uint32_t)a.slabs), run = wave * TW + rank, skip = (kRuns - 1 - run) * K;
   Place p;
   p.b = pair / (uint32_t)a.slabs;
@@ -930,7 +945,8 @@ extern "C" int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_
   if (!decay) return fail(HG_ERR_ARG, "%s: null decay", what);
   for (const hg_heads* v : {x, r, i})
     if (rows_meet(h, v, A->batch, A->t, A->width, A->dtype)) return fail(HG_ERR_ARG, "%s: h overlaps an input", what);
-  if (state && state == state_out) return fail(HG_ERR_ARG, "%s: state_out is state", what);
+  const size_t states = (size_t)A->batch * A->width * 4;
+  if (ranges_meet(state, states, state_out, states)) return fail(HG_ERR_ARG, "%s: state_out overlaps state", what);
   Sizer need;
   take(A, false, need);
   HG_TRY(check_workspace(what, ws, ws_bytes, need.used));
@@ -967,8 +983,10 @@ extern "C" int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_
     for (int q = 0; q < k; ++q)
       if (rows_meet(all[k], all[q], A->batch, A->t, A->width, A->dtype))
         return fail(HG_ERR_ARG, "%s: %s overlaps %s", what, names[k], names[q]);
-  if (dstate && (dstate == state || dstate == dstate_out)) return fail(HG_ERR_ARG, "%s: dstate is an input", what);
-  if (ddecay && ddecay == decay) return fail(HG_ERR_ARG, "%s: ddecay is decay", what);
+  const size_t states = (size_t)A->batch * A->width * 4, vec = (size_t)A->width * 4;
+  if (ranges_meet(dstate, states, state, states) || ranges_meet(dstate, states, dstate_out, states))
+    return fail(HG_ERR_ARG, "%s: dstate overlaps an input", what);
+  if (ranges_meet(ddecay, vec, decay, vec)) return fail(HG_ERR_ARG, "%s: ddecay overlaps decay", what);
   Sizer need;
   take(A, true, need);
   HG_TRY(check_workspace(what, ws, ws_bytes, need.used));

@@ -97,6 +97,12 @@ inline bool rows_meet(const hg_heads* o, const hg_heads* x, int64_t batch, int64
   return t > 1 && batch > 1 && o->batch % o->token != 0 && o->batch < t * o->token;
 }
 
+// Whether two stretches of memory share an address (not if either is null or empty).
+inline bool ranges_meet(const void* p, size_t a, const void* q, size_t b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+  return p && q && a && b && x < y + b && y < x + a;
+}
+
 inline Rows rows_of(const hg_heads* x) { return Rows{x->p, x->batch, x->token}; }
 
 inline int check_workspace(const char* what, const void* ws, size_t ws_bytes, size_t need) {

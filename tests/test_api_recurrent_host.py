@@ -135,6 +135,42 @@ def test_group_norm_refusals(L):
     assert fwd(d(b=0)) == OK
 
 
+def test_states_and_gradients_that_share_part_of_a_buffer(L):
+    """Refused as well as the same buffer: another block may read what one wrote."""
+    d = api._pack_recur(20, 2, 16, 1, 8.0)
+    state = 2 * 16 * 4
+
+    def fwd(so, ws):
+        return L.hg_recur_fwd(d, rows(1), rows(2), rows(3), 4 * P, None, 5 * P, rows(6), so, ws, BIG, None)
+
+    def bwd(dg, ds):  # (refused for its workspace alone where nothing overlaps)
+        return L.hg_recur_bwd(d, rows(1), rows(2), rows(3), 4 * P, None, 5 * P, rows(6), rows(8), 13 * P, rows(9), rows(10),
+                              rows(11), dg, ds, 0, None, 0, None)
+
+    assert fwd(5 * P + state - 4, None) == fwd(5 * P - state + 4, None) == ARG
+    assert bwd(12 * P, 5 * P + state) == bwd(4 * P + 64, 14 * P) == CAPACITY
+    assert bwd(12 * P, 5 * P + state - 4) == bwd(12 * P, 13 * P - 4) == bwd(4 * P + 60, 14 * P) == ARG
+    g = api._pack_group_norm(20, 2, 16, 4, 1, 2, 1e-5)
+
+    def norm(dw, db):
+        return L.hg_group_norm_bwd(g, rows(1), 3 * P, 4 * P, None, 5 * P, rows(2), rows(6), dw, db, 0, None, 0, None)
+
+    assert norm(7 * P, 7 * P + 64) == norm(3 * P + 64, 9 * P) == CAPACITY
+    assert norm(7 * P, 7 * P + 60) == norm(3 * P + 60, 9 * P) == norm(7 * P, 4 * P - 60) == ARG
+
+
+def test_grids_stay_launchable(L):
+    """Single channels a thread in slabs of 64, 256 threads each: fewer than 2^32 threads a launch."""
+    def bwd(batch):
+        w = 1021 * 1024  # 16336 slabs
+        d = api._pack_group_norm(3, batch, w, 1024, 0, 0, 1e-5)
+        x = [api._pack_heads(k << 42, 3 * w, w, 0) for k in (1, 2, 3)]
+        return L.hg_group_norm_bwd(d, x[0], None, None, None, 5 * P, x[1], x[2], None, None, 0, None, 0, None)
+
+    assert bwd(1) == bwd(1027) == CAPACITY
+    assert bwd(1028) == bwd(4000) == UNSUPPORTED
+
+
 def test_muon_refusals(L):
     def d(c=2, m=16, n=24, dtype=0, steps=5, nes=1, lr=0.1, mu=0.9, wd=0.0, scale=1.0, eps=1e-7):
         return api._pack_muon(c, m, n, dtype, steps, nes, lr, mu, wd, scale, eps, 0)

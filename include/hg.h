@@ -26,6 +26,10 @@
  *                           decorrelation and CCA-loss equations; the lambda_CCA
  *                           weight of the joint objective)
  *
+ * and, next to the paper's encoder, the operators of a sequence encoder over node
+ * histories: hg_linear_*, hg_glu_*, hg_qk_norm_rope_*, hg_linattn_*, of its
+ * recurrent block: hg_recur_*, hg_group_norm_*, and hg_muon_step, its optimiser.
+ *
  * Conventions (all entry points):
  *  - Pointers named in a struct or argument list are DEVICE pointers unless
  *    the comment says "host".  Matrices are row-major and contiguous.
@@ -694,9 +698,10 @@ int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, const hg_heads*
  * Rows of these operators need no alignment but their values' own: an element
  * (sequence b, token t, channel c) lies at p[b * batch + t * token + c] of an
  * hg_heads whose head stride is not used.  Strides are at least 0 and at most 2^40
- * (a token's of the recurrence 2^21), those of outputs keep the rows apart.  Outputs must not overlap inputs or each
- * other; views of one packed buffer may interleave.  Workspaces are 16-byte
- * aligned.  Asynchronous and deterministic.
+ * (a token's of the recurrence 2^21), those of outputs keep the rows apart.
+ * Outputs must not overlap inputs or each other; views of one packed buffer may
+ * interleave.  Workspaces are 16-byte aligned; two calls that may run at the same
+ * time need one each.  Asynchronous and deterministic.
  *
  * Gated linear recurrence: the GRU of E13 without its products with the state,
  * so that a history is a scan.  Per channel c with l_c = -rate softplus(decay[c]),

@@ -15,8 +15,8 @@
 // pass that forms the output (k_norm_apply); in the backward sums of the columns,
 // joined, and a pass.
 //
-// Bound by HBM, the backward with an activation by the vector unit as well (53% of the
-// cycles: 16384 rows of 16 x 64 bfloat16 channels 37 us, 2.7 TB/s).  A float32 backward
+// Bound by HBM, the backward with an activation by the vector unit as well (56% of the
+// cycles: 16384 rows of 16 x 64 bfloat16 channels 34 us, 3.0 TB/s).  A float32 backward
 // of 200003 rows of 128 channels: 51 us for the columns (4.1 TB/s), 48 for the pass
 // (6.4); a forward of 512 x 96 tokens of 200 float32 channels 18 us (3.9).
 #include <cmath>
@@ -200,6 +200,10 @@ __global__ void __launch_bounds__(BT) k_norm_fwd(const NormArgs a) {
 
 template <class T, int V, int R, int BT>
 __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
+  // u stays in registers for the second pass where they last (float32, SiLU: 16384 rows of
+  // 16 x 64 channels 43 us, 53 where it is formed again; 512 x 96 tokens of 5 x 40
+  // channels, eight of a thread, 55 and 30)
+  constexpr bool KEEP = R * V <= 16;
   __shared__ float sh[2][BT / 64][2];
   __shared__ float col[BT * V];
   const Spot s = spot_of<V>(a);
@@ -222,32 +226,32 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
       }
     }
     const float mean = in ? a.stats[(b * a.groups + s.g) * 2] : 0.f, rstd = in ? a.stats[(b * a.groups + s.g) * 2 + 1] : 0.f;
-    float e[R][V], sum[2] = {0.f, 0.f};
+    float e[R][V], u[KEEP ? R : 1][V], sum[2] = {0.f, 0.f};
     g_by_act<true>(a.act, [&](auto act) {
       constexpr int ACT = decltype(act)::value;
 #pragma unroll
       for (int k = 0; k < R; ++k)
         if (s.r + k * s.nr < n) {
-          float z[V], u[V], f[V], d[V];
+          float z[V], f[V], d[V];
 #pragma unroll
           for (int j = 0; j < V; ++j) {
-            u[j] = (Vec<T, V>::get(x[k], j) - mean) * rstd;
-            z[j] = fmaf(u[j], w[j], bias[j]);
+            u[KEEP ? k : 0][j] = (Vec<T, V>::get(x[k], j) - mean) * rstd;
+            z[j] = fmaf(u[KEEP ? k : 0][j], w[j], bias[j]);
           }
           act_of<ACT, true, V>(z, f, d);
 #pragma unroll
           for (int j = 0; j < V; ++j) {
             const float dz = Vec<T, V>::get(y[k], j) * d[j];
-            dw[j] = fmaf(dz, u[j], dw[j]);
+            dw[j] = fmaf(dz, u[KEEP ? k : 0][j], dw[j]);
             db[j] += dz;
             e[k][j] = dz * w[j];
             sum[0] += e[k][j];
-            sum[1] = fmaf(e[k][j], u[j], sum[1]);
+            sum[1] = fmaf(e[k][j], u[KEEP ? k : 0][j], sum[1]);
           }
         }
     });
     item_sum<2>(sum, a.lp, sh[odd]);
-    const float inv = n > 0 ? 1.f / (float)(n * a.cg) : 0.f, m0 = sum[0] * inv, m1 = sum[1] * inv;
+    const float inv = n > 0 ? 1.f / (float)(n * a.cg) : 0.f, c0 = sum[0] * inv * rstd, c1 = sum[1] * inv * rstd;
     if (in)
 #pragma unroll
       for (int k = 0; k < R; ++k) {
@@ -256,8 +260,8 @@ __global__ void __launch_bounds__(BT) k_norm_bwd(const NormArgs a) {
         float o[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float u = (Vec<T, V>::get(x[k], j) - mean) * rstd;
-          o[j] = t < n ? rstd * (e[k][j] - m0 - u * m1) : 0.f;
+          const float v = KEEP ? u[KEEP ? k : 0][j] : (Vec<T, V>::get(x[k], j) - mean) * rstd;
+          o[j] = t < n ? fmaf(rstd, e[k][j], fmaf(-c1, v, -c0)) : 0.f;
         }
         Vec<T, V>::put(at<T, V>(a.y, b, t, s.c), o);
       }
@@ -331,11 +335,11 @@ __global__ void __launch_bounds__(256) k_norm_apply(const NormArgs a, const floa
   const int64_t t0 = (tile - b * per) * kApply, n = len_of(a, b);
   const int g = c / a.cg;
   const float mean = stats[(b * a.groups + g) * 2], rstd = stats[(b * a.groups + g) * 2 + 1];
-  float m0 = 0.f, m1 = 0.f;
+  float c0 = 0.f, c1 = 0.f;
   if (BACK) {
     const float inv = n > 0 ? (float)(1.0 / (double)(n * a.cg)) : 0.f;
-    m0 = a.gsum[(b * a.groups + g) * 2] * inv;
-    m1 = a.gsum[(b * a.groups + g) * 2 + 1] * inv;
+    c0 = a.gsum[(b * a.groups + g) * 2] * inv * rstd;
+    c1 = a.gsum[(b * a.groups + g) * 2 + 1] * inv * rstd;
   }
   float w[V], bias[V];
 #pragma unroll
@@ -368,7 +372,7 @@ __global__ void __launch_bounds__(256) k_norm_apply(const NormArgs a, const floa
         act_of<ACT, BACK, V>(z, f, d);
 #pragma unroll
         for (int j = 0; j < V; ++j)
-          o[j] = BACK ? rstd * (Vec<T, V>::get(dy[k], j) * d[j] * w[j] - m0 - u[j] * m1) : f[j];
+          o[j] = BACK ? fmaf(rstd, Vec<T, V>::get(dy[k], j) * d[j] * w[j], fmaf(-c1, u[j], -c0)) : f[j];
       }
       Vec<T, V>::put(at<T, V>(a.y, b, t0 + k, c), o);
     }
@@ -577,9 +581,9 @@ Plan plan_of(const hg_group_norm_desc* A, bool bwd) {
     p.r = 1 << std::min(3, log2_up(cdiv(t, (int64_t)1 << lr)));
     p.bt = a.lp <= 8 ? 256 : 1024;
     // A row of partial sums of dw and db for each block of the backward: few blocks
-    // (16384 rows of 16 x 64 channels 40 us with 1024, 45 with 1536), but single channels
-    // a thread are few bytes in flight and take more (20000 rows of 32 x 25 channels 81
-    // us with 4096, 115 with 2048).
+    // (16384 rows of 16 x 64 channels 37 us with 1024, 42 with 1536), but single channels
+    // a thread are few bytes in flight and take more (20000 rows of 32 x 25 channels 73
+    // us with 4096, 77 with 2048).
     lay_out(p, A->batch, !bwd ? (int64_t)1 << 21 : p.bt == 256 ? (p.v == 1 ? 4096 : 1024) : 512);
     return p;
   }

@@ -16,9 +16,9 @@
 // (WAVE: no barrier) or a block walks each.  Few: a block for each tile, all at once,
 // and the tiles' steps compose through memory (k_recur_chain_*).
 //
-// Bound by HBM and by the vector instructions at once: some 55 a value forward, six of
-// them transcendental, are 95 us for 67M values on this chip, their 8 bytes 103 us at
-// the 5.2 TB/s of a large copy.
+// Bound by HBM and by the vector instructions at once: 49 issue slots a value forward, six
+// instructions of them transcendental, are 83 us for 67M values on this chip, their 8
+// bytes 103 us at the 5.2 TB/s of a large copy (one pass over both: 128 us).
 //
 // The last four channels of a row whose width is no multiple of four are taken
 // by a thread that starts earlier: two threads then compute and write the same
@@ -57,9 +57,11 @@ using Quad = Vec<T, V>;
 
 __device__ __forceinline__ float sigm(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
 
-// rate softplus(decay) log2 e: the factor is 2^(-that sigmoid(r))
+// rate softplus(decay) log2 e: the factor is 2^(-that sigmoid(r)).  Finite, so that it is
+// 0 times sigmoid(r) = 0.
 __device__ __forceinline__ float slope_of(float decay, float rate) {
-  return rate * kLog2e * (fmaxf(decay, 0.f) + log1pf(expf(-fabsf(decay))));
+  const float v = rate * kLog2e * (fmaxf(decay, 0.f) + log1pf(expf(-fabsf(decay))));
+  return v == INFINITY ? 3.4e38f : v;
 }
 
 // 1 - a^2 for a = 2^l: near a = 1 by the series of 1 - e^y, y = 2 l ln 2, to y^6
@@ -568,6 +570,19 @@ __device__ __forceinline__ void zero_stretch(const RecurArgs& a, const Rows& x, 
   zero_rows<T>(x, p, run, kNW * TW);
 }
 
+// Gates r of rows that no token has: sigmoid(-inf) = 0, so that their factor is 1 and,
+// with x = 0 or dh = 0, their step leaves the value as it is, with no select a value
+// (65521 bfloat16 tokens of 1024 channels 137 us, 143 with selects, both 12 tokens a thread).
+template <class T, int K>
+__device__ __forceinline__ void no_token(typename Quad<T>::raw (&r)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    if constexpr (sizeof(T) == 4) {
+      r[k] = -INFINITY;
+    } else {
+      r[k] = 0xFF80FF80u;
+    }
+}
 template <class T, int K>
 __global__ void __launch_bounds__(kNW * 64) k_recur_chain_fwd(const RecurArgs a, const Chain q) {
   __shared__ ChainLds sh;
@@ -583,7 +598,8 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_fwd(const RecurArgs a,
   const int64_t state_at = p.b * a.width + channel_of(a, slab, lane);
   if (ts < len) {
     const Stream<T> sx(a.x, p, run * K), sr(a.r, p, run * K), si(a.i, p, run * K), so(a.h, p, run * K);
-    typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {};
+    typename Quad<T>::raw rx[K] = {}, rr[K], ri[K] = {};
+    no_token<T>(rr);
     const bool whole = ts + kTile <= len;
     if (whole) {
       load<T, K, true>(rr, sr, ts, t0, 0, len);
@@ -603,14 +619,13 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_fwd(const RecurArgs a,
     for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool in = t0 + k < len;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float l = slope[j] * sigm(Quad<T>::get(rr[k], j));
         const float f = __builtin_amdgcn_exp2f(l);
         const float u = __builtin_amdgcn_sqrtf(rest_of(l, f)) * sigm(Quad<T>::get(ri[k], j)) * Quad<T>::get(rx[k], j);
-        fa[k][j] = in ? f : 1.f;
-        fu[k][j] = in ? u : 0.f;
+        fa[k][j] = f;
+        fu[k][j] = u;
         s.a[j] *= fa[k][j];
         s.b[j] = fmaf(fa[k][j], s.b[j], fu[k][j]);
       }
@@ -649,7 +664,8 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a,
   if (ts + kTile > 0) {
     const Stream<T> sx(a.x, p, skip), sr(a.r, p, skip), si(a.i, p, skip), sh1(a.h, p, skip), sg(a.dh, p, skip), ox(a.dx, p, skip),
         orr(a.dr, p, skip), oi(a.di, p, skip);
-    typename Quad<T>::raw rx[K] = {}, rr[K] = {}, ri[K] = {}, rh[K] = {}, rg[K] = {};
+    typename Quad<T>::raw rx[K] = {}, rr[K], ri[K] = {}, rh[K] = {}, rg[K] = {};
+    no_token<T>(rr);
     const bool whole = ts > 0;  // (token 0's h before comes from the state)
     const auto fetch = [&](auto full) {
       constexpr bool FULL = decltype(full)::value;
@@ -673,13 +689,12 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a,
     for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
 #pragma unroll
     for (int k = K - 1; k >= 0; --k) {
-      const bool in = t0 + k >= 0;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         fs[k][j] = sigm(Quad<T>::get(rr[k], j));
         const float f = __builtin_amdgcn_exp2f(slope[j] * fs[k][j]);
-        fa[k][j] = in ? f : 1.f;
-        gh[k][j] = in ? Quad<T>::get(rg[k], j) : 0.f;
+        fa[k][j] = f;
+        gh[k][j] = Quad<T>::get(rg[k], j);
         s.b[j] = fa[k][j] * (s.b[j] + gh[k][j]);
         s.a[j] *= fa[k][j];
       }
@@ -775,10 +790,11 @@ constexpr int64_t kMaxToken = (int64_t)1 << 21;  // (a tile has at most 2^8 toke
 constexpr int fwd_run(bool wave) { return wave ? 2 : 4; }
 constexpr int bwd_run(bool wave) { return wave ? 1 : 2; }
 // In a chain the whole tile is in flight at once: one history of 65521 tokens of 1024
-// channels, bfloat16, 148 us with 12, 154 with 8, 158 with 16, 233 with 4; 8 x 2048
-// tokens of 1024 channels, float32, 64 us with 8, 77 with 4; their backward 124 us with
-// 5, 130 with 4, 147 with 6; in bfloat16, 2048 channels, 105 us with 8, 126 with 12.
-constexpr int chain_run(bool bwd, bool f32) { return bwd ? (f32 ? 5 : 8) : (f32 ? 8 : 12); }
+// channels, bfloat16, 132 us with 14, 137 with 10 or 12, 142 with 16; 8 x 2048 tokens of
+// 1024 channels, float32, 64 us with 8, 67 with 10, 69 with 6, their backward 125 us with
+// 5, 128 with 4, 148 with 6; ragged in bfloat16, 2048 channels, 105 us with 9, 107 with
+// 8, 132 with 10.
+constexpr int chain_run(bool bwd, bool f32) { return bwd ? (f32 ? 5 : 9) : (f32 ? 8 : 14); }
 
 struct Split {
   bool wave;         // a wave for each sequence

@@ -182,6 +182,26 @@ def test_gates_at_their_ends(dtype):
         assert parity_err(host(got[k]), ref[k]) < bar(dtype if k < 3 else F32, t), k
 
 
+@pytest.mark.parametrize("b,t", [(3, 600), (1200, 100), (3, 20)])
+def test_slopes_past_the_largest_number(b, t):
+    """rate softplus(decay) beyond float32: a = 0, but 1 where sigmoid(r) = 0, and nothing from rows past the end."""
+    w = 8
+    x, r, i = (v.clone() for v in problem(b, t, w, F32, packed=False))
+    r[:, 3] = float("-inf")
+    g = decays(w)
+    g[1] = 3e38
+    lens = torch.full((b,), t - 7, dtype=torch.int32, device="cuda")
+    s0, dh = normal(5, b, w), normal(6, b, t, w)
+    h, s1 = api.hg_recur_fwd(x, r, i, g, lens=lens, state=s0, want_state=True)
+    gated = (torch.sigmoid(i.double()) * x.double())[:, :, 1]
+    want = gated.clone()
+    want[:, 3] = gated[:, 2]
+    want[:, t - 7:] = 0
+    assert parity_err(host(h)[..., 1], host(want)) < bar(F32, 1) and parity_err(host(s1)[:, 1], host(want[:, t - 8])) < bar(F32, 1)
+    for v in api.hg_recur_bwd(x, r, i, g, h, dh, lens=lens, state=s0):
+        assert torch.isfinite(v).all()
+
+
 def test_factors_next_to_one():
     """1 - a^2 far below 2^-24: the input's share keeps its digits."""
     b, t, w = 1, 400, 16

@@ -788,14 +788,15 @@ int hg_group_norm_bwd(const hg_group_norm_desc* A, const hg_heads* x, const floa
  *   W = (1 - lr weight_decay) W - lr scale X
  * W and G [count, rows, cols] in dtype, M float32, contiguous; W, G and M do not
  * overlap.  M = 0 before the first update.
- * Precision: |U| is summed in float64 and every product in float32.  float32
- * matrices enter the products as two fp16 parts of each value, three part
+ * Precision: |U| is summed in float64 and every product in float32.  Matrices of
+ * both types enter the products as two fp16 parts of each value, three part
  * products (the row transforms' rule stated at the top, with one scale for the
- * whole of X, whose entries are at most 1.21): float32 accuracy.  bfloat16 matrices
- * enter as the fp16 high part alone (X, A and B are rounded to 11 bits a step: X is
- * off by some 2^-9 of its norm, up to 2^-7 where noise lies far below a gradient's
- * strong directions).  A matrix whose U holds a value
- * that is not finite becomes NaN as a whole; the others of the call do not.
+ * whole of X, whose entries are at most 1.21): float32 accuracy, X is off by some
+ * 2^-20 of its norm.  A rounding of 2^-22 in directions that U leaves empty grows
+ * by up to 3.4445 a step: where few directions hold all of U, X is off by up to
+ * 1e-4 of its norm after five steps (485 2^-22, a matrix of rank one).  W is rounded
+ * once.  A matrix whose U holds a value that is not finite becomes NaN as a whole;
+ * the others of the call do not.
  * rows and cols are at most 2^15, count rows cols is below 2^32 and count times the
  * 64 x 64 tiles of a matrix below 2^22. */
 typedef struct hg_muon_desc {

@@ -7,20 +7,23 @@
 // singular values go through x (p + q x^2 + s x^4), which keeps [0, 1.21] in
 // [0, 1.21] and takes small ones up by p a step.
 //
-// X, A and B are held in fp16 parts: the high part, and for float32 matrices what
-// its rounding left (a float32 product is then hi hi + hi lo + lo hi, as in the
-// row transforms).  Since no entry of X exceeds 1.21, of A 1.47 and of B 2.81,
-// fixed powers of two take them to the top of fp16's range, exactly; a high part
-// alone is off by 2^-12 of an entry down to 2^-28.  Sums are float32.
+// X, A and B are held in two fp16 parts, the high part and what its rounding left (a
+// product is then hi hi + hi lo + lo hi, as in the row transforms).  Since no entry
+// of X exceeds 1.21, of A 1.47 and of B 2.81, fixed powers of two take them to the
+// top of fp16's range, exactly.  Sums are float32.  bfloat16 matrices too: with the
+// high part alone, off by 2^-12 of an entry, a step's noise in directions that a
+// gradient leaves empty grows by p with each step after it, to 0.03 of X's norm
+// where min / 8 directions hold it and 0.1 for rank one (a third of the products:
+// 4096 x 8192 in 2.5 ms, 6.2 so).
 //
 // Each product runs on the fp16 MFMA in tiles, with the tile loads of the linear
 // map's products (hg_gemm.h): X is read as it lies, by rows or with k as the row
 // index.  A and A A are symmetric: only tiles on and below the diagonal are
 // formed, and written twice.  The sums q A + s A A and p X + B X and the update of
 // W are the products' epilogues, so a step is three launches (and where the last tiles'
-// k is cut, the sums of the parts).  Bound by the MFMA: a step of 4096 x 8192 bfloat16
-// is 136 us for A, 79 for B and 258 for B X (1.0, 0.9 and 1.1 PFLOP/s), of 1024 x 5632
-// float32 24, 17 and 48 (0.74 PFLOP/s of fp16 products; the tiles are few).
+// k is cut, the sums of the parts).  Bound by the MFMA: a step of 4096 x 8192 is 362 us
+// for A, 186 for B and 670 for B X (1.1, 1.1 and 1.2 PFLOP/s of fp16 products; a large
+// library product 1.2), of 1024 x 5632 27, 20 and 50 (0.7 PFLOP/s; the tiles are few).
 #include <cmath>
 
 #include "hg_gemm.h"
@@ -37,9 +40,9 @@ constexpr float pow2(int e) { return e >= 0 ? (float)(1ll << e) : 1.f / (float)(
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
 // One stored matrix of rows x cols values, `step` 16-bit values from one matrix of
-// the call to the next.  A row holds its columns up to a multiple of 8 (with LO of
-// 32), zeros from cols on; with LO each 32 high parts are followed by their low
-// parts, so that a tile's 128-byte rows are 32 columns in two parts, or 64 in one.
+// the call to the next.  A row holds its columns up to a multiple of 32, zeros from
+// cols on; each 32 high parts are followed by their low parts, so that a tile's
+// 128-byte rows are 32 columns in two parts.
 struct Stored {
   uint16_t* p;
   int64_t step;
@@ -47,9 +50,8 @@ struct Stored {
   int32_t pad;  // columns with their padding
   int32_t ld;   // values of a row
 };
-template <bool LO>
 __device__ __forceinline__ int64_t spot(const Stored& o, int r, int c) {
-  return (int64_t)r * o.ld + (LO ? (c >> 5) * 64 + (c & 31) : c);
+  return (int64_t)r * o.ld + (c >> 5) * 64 + (c & 31);
 }
 
 struct MuonArgs {
@@ -69,7 +71,6 @@ struct MuonArgs {
 enum { kEpiSym = 0, kEpiSymAdd = 1, kEpiAdd = 2, kEpiUpdate = 3 };
 
 // The parts of four adjacent values (of the first of them) of a row.
-template <bool LO>
 __device__ __forceinline__ void put4(uint16_t* p, const float (&v)[4]) {
   f16x4 h, l;
 #pragma unroll
@@ -78,13 +79,12 @@ __device__ __forceinline__ void put4(uint16_t* p, const float (&v)[4]) {
     l[q] = (_Float16)(v[q] - (float)h[q]);
   }
   *reinterpret_cast<f16x4*>(p) = h;
-  if (LO) *reinterpret_cast<f16x4*>(p + 32) = l;
+  *reinterpret_cast<f16x4*>(p + 32) = l;
 }
-template <bool LO>
 __device__ __forceinline__ void put1(uint16_t* p, float v) {
   const _Float16 h = (_Float16)v;
   *p = __builtin_bit_cast(uint16_t, h);
-  if (LO) p[32] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
+  p[32] = __builtin_bit_cast(uint16_t, (_Float16)(v - (float)h));
 }
 // Tile (row, column) of tile id of the lower triangle of tm tile rows, in the order
 // of g_tile_of: each XCD takes one contiguous share of a walk that goes down eight
@@ -128,16 +128,16 @@ __device__ __forceinline__ void tile_of(const MuonArgs& p, uint32_t tile, uint32
 // What the epilogue of columns n .. n + 3 of row m reads: of X or A, and of W.  All
 // of a row of blocks is loaded before the first is written: the compiler keeps loads
 // behind stores that may be to the same place, and would wait for each.
-template <bool LO, int EPI, class T>
+template <int EPI, class T>
 struct Beside {
   f16x4 h, l;
   typename Vec<T, 4>::raw w;
   __device__ __forceinline__ void load(const MuonArgs& p, uint32_t mat, int m, int n) {
     if constexpr (EPI != kEpiSym) {
       if (m < p.M && n < p.c.pad) {
-        const uint16_t* x = p.c.p + mat * p.c.step + spot<LO>(p.c, m, n);
+        const uint16_t* x = p.c.p + mat * p.c.step + spot(p.c, m, n);
         h = *reinterpret_cast<const f16x4*>(x);
-        if (LO) l = *reinterpret_cast<const f16x4*>(x + 32);
+        l = *reinterpret_cast<const f16x4*>(x + 32);
       }
     }
     if constexpr (EPI == kEpiUpdate)
@@ -147,9 +147,9 @@ struct Beside {
 
 // The epilogue of columns n .. n + 3 of row m; mirror: below the diagonal of a
 // symmetric result, whose transpose is written too.
-template <bool LO, int EPI, class T>
+template <int EPI, class T>
 __device__ __forceinline__ void finish(const MuonArgs& p, uint32_t mat, int m, int n, bool mirror, const f32x4& z,
-                                       const Beside<LO, EPI, T>& x) {
+                                       const Beside<EPI, T>& x) {
   constexpr bool SYM = EPI <= kEpiSymAdd;
   const bool row = m < p.M;
   const int left = p.N - n;
@@ -160,7 +160,7 @@ __device__ __forceinline__ void finish(const MuonArgs& p, uint32_t mat, int m, i
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     v[q] = row ? p.zs * z[q] : 0.f;
-    if (EPI != kEpiSym && row) v[q] = fmaf(p.cs, LO ? (float)x.h[q] + (float)x.l[q] : (float)x.h[q], v[q]);
+    if (EPI != kEpiSym && row) v[q] = fmaf(p.cs, (float)x.h[q] + (float)x.l[q], v[q]);
   }
   if constexpr (EPI == kEpiUpdate) {
     T* w = static_cast<T*>(p.W) + ((int64_t)mat * p.M + m) * p.N + n;
@@ -178,11 +178,11 @@ __device__ __forceinline__ void finish(const MuonArgs& p, uint32_t mat, int m, i
     }
   } else {
     uint16_t* o = p.o.p + mat * p.o.step;
-    if (row) put4<LO>(o + spot<LO>(p.o, m, n), v);
+    if (row) put4(o + spot(p.o, m, n), v);
     if (SYM && mirror) {
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (q < left) put1<LO>(o + spot<LO>(p.o, n + q, m), v[q]);
+        if (q < left) put1(o + spot(p.o, n + q, m), v[q]);
     }
   }
 }
@@ -201,11 +201,11 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <class TL, bool AKM, bool BKM, bool LO, int EPI, class T>
+template <class TL, bool AKM, bool BKM, int EPI, class T>
 __global__ void __launch_bounds__(TL::NT) k_muon_product(const MuonArgs p) {
   constexpr int BM = TL::BM, BN = TL::BN, MI = TL::MI, NI = TL::NI, NW = TL::NW, ST = TL::ST;
-  constexpr int PL = LO ? 2 : 1, BK = 64 / PL;  // k of a stage
-  // by rows of k: 64 values, in two parts those of 32; with k as the row: BK rows of the tile's columns in their parts
+  constexpr int PL = 2, BK = 32;  // parts of a value, k of a stage
+  // by rows of k: 32 values in two parts; with k as the row: 32 rows of the tile's columns in theirs
   typedef GTile<AKM ? BM : BM * PL, AKM ? 64 : BK, AKM, NW, false> TA;
   typedef GTile<BKM ? BN : BN * PL, BKM ? 64 : BK, BKM, NW, false> TB;
   constexpr int kStage = TA::kBytes + TB::kBytes, kLoads = TA::PER + TB::PER;
@@ -268,38 +268,23 @@ __global__ void __launch_bounds__(TL::NT) k_muon_product(const MuonArgs p) {
     if (t + ST - 1 < to) issue(t + ST - 1);
     const char* sa = lds + (t % ST) * kStage;
     const char* sb = sa + TA::kBytes;
-    // fragment (i, part or half of the stage's k)
-    auto fa_of = [&](int i, int h) { return AKM || !LO ? TA::frag(sa, i, h, c, g) : TA::frag(sa, (i >> 1) * 4 + (i & 1) + 2 * h, 0, c, g); };
-    auto fb_of = [&](int i, int h) { return BKM || !LO ? TB::frag(sb, i, h, c, g) : TB::frag(sb, (i >> 1) * 4 + (i & 1) + 2 * h, 0, c, g); };
-    if constexpr (LO) {
-      uint4 fa[2][MI], fb[2][NI];
+    // fragment (i, part)
+    auto fa_of = [&](int i, int h) { return AKM ? TA::frag(sa, i, h, c, g) : TA::frag(sa, (i >> 1) * 4 + (i & 1) + 2 * h, 0, c, g); };
+    auto fb_of = [&](int i, int h) { return BKM ? TB::frag(sb, i, h, c, g) : TB::frag(sb, (i >> 1) * 4 + (i & 1) + 2 * h, 0, c, g); };
+    uint4 fa[2][MI], fb[2][NI];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) fb[h][j] = fb_of(wn * NI + j, h);
+      for (int j = 0; j < NI; ++j) fb[h][j] = fb_of(wn * NI + j, h);
 #pragma unroll
-        for (int i = 0; i < MI; ++i) fa[h][i] = fa_of(wm * MI + i, h);
-      }
-#pragma unroll
-      for (int h = 0; h < 3; ++h)
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-          for (int j = 0; j < NI; ++j) acc[i][j] = mfma_f16(fb[h == 1][j], fa[h == 2][i], acc[i][j]);
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint4 fa[MI], fb[NI];
-#pragma unroll
-        for (int j = 0; j < NI; ++j) fb[j] = fb_of(wn * NI + j, h);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) fa[i] = fa_of(wm * MI + i, h);
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-          for (int j = 0; j < NI; ++j) acc[i][j] = mfma_f16(fb[j], fa[i], acc[i][j]);
-      }
+      for (int i = 0; i < MI; ++i) fa[h][i] = fa_of(wm * MI + i, h);
     }
+#pragma unroll
+    for (int h = 0; h < 3; ++h)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = mfma_f16(fb[h == 1][j], fa[h == 2][i], acc[i][j]);
   }
 
   if (pieces > 1) {
@@ -312,7 +297,7 @@ __global__ void __launch_bounds__(TL::NT) k_muon_product(const MuonArgs p) {
   }
   // lane (c, g) holds columns 16 j + 4 g .. + 3 of row 16 i + c
   const int mr = m0 + wm * TL::WM + c, nc = n0 + wn * TL::WN + 4 * g;
-  Beside<LO, EPI, T> x[2][NI];
+  Beside<EPI, T> x[2][NI];
 #pragma unroll
   for (int j = 0; j < NI; ++j) x[0][j].load(p, mat, mr, nc + 16 * j);
 #pragma unroll
@@ -321,13 +306,13 @@ __global__ void __launch_bounds__(TL::NT) k_muon_product(const MuonArgs p) {
 #pragma unroll
       for (int j = 0; j < NI; ++j) x[(i + 1) & 1][j].load(p, mat, mr + 16 * (i + 1), nc + 16 * j);
 #pragma unroll
-    for (int j = 0; j < NI; ++j) finish<LO, EPI, T>(p, mat, mr + 16 * i, nc + 16 * j, im != in, acc[i][j], x[i & 1][j]);
+    for (int j = 0; j < NI; ++j) finish<EPI, T>(p, mat, mr + 16 * i, nc + 16 * j, im != in, acc[i][j], x[i & 1][j]);
   }
 }
 
 // Tiles whose k was cut: their parts added in order, then the epilogue.  A block has
 // one of the MI NI groups of 16 x 16 of each of a tile's waves.
-template <class TL, bool LO, int EPI, class T>
+template <class TL, int EPI, class T>
 __global__ void __launch_bounds__(TL::NT) k_muon_join(const MuonArgs p) {
   constexpr int G = TL::MI * TL::NI;
   const uint32_t cut = blockIdx.x / G, ij = blockIdx.x - cut * G;
@@ -337,7 +322,7 @@ __global__ void __launch_bounds__(TL::NT) k_muon_join(const MuonArgs p) {
   const float* all = p.part + (int64_t)cut * p.pieces * TL::BM * TL::BN + (int64_t)ij * TL::NT * 4 + threadIdx.x * 4;
   const int m = (int)im * TL::BM + (wave / TL::NWN) * TL::WM + 16 * i + c;
   const int n = (int)in * TL::BN + (wave % TL::NWN) * TL::WN + 16 * j + 4 * g;
-  Beside<LO, EPI, T> x;
+  Beside<EPI, T> x;
   x.load(p, mat, m, n);
   f32x4 z{0.f, 0.f, 0.f, 0.f};
   for (int q0 = 0; q0 < p.pieces; q0 += 8) {
@@ -351,7 +336,7 @@ __global__ void __launch_bounds__(TL::NT) k_muon_join(const MuonArgs p) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) z[v] += y[q][v];
   }
-  finish<LO, EPI, T>(p, mat, m, n, im != in, z, x);
+  finish<EPI, T>(p, mat, m, n, im != in, z, x);
 }
 
 // ---- momentum, norm, first X ------------------------------------------------------
@@ -426,7 +411,7 @@ __device__ __forceinline__ float scaled(float u, const Inverse& i, int more) {
 }
 
 // X = U / max(|U|, eps) in its parts, or with steps = 0 the update of W.
-template <class T, bool LO, bool UPDATE>
+template <class T, bool UPDATE>
 __global__ void __launch_bounds__(256)
     k_muon_first(const T* __restrict__ G, const float* __restrict__ M, int32_t rows, int32_t cols, float mu, int nesterov,
                  const double* __restrict__ part, int parts, float eps, Stored o, T* __restrict__ W, float ws, float us) {
@@ -475,7 +460,7 @@ __global__ void __launch_bounds__(256)
       v[q] = UPDATE ? fmaf(-us, x, ws * w[q]) : x;
     }
     if constexpr (!UPDATE) {
-      put4<LO>(o.p + mat * o.step + spot<LO>(o, r, c), v);
+      put4(o.p + mat * o.step + spot(o, r, c), v);
     } else if (left >= 4) {
       Vec<T, 4>::put(W + at, v);
     } else {
@@ -523,13 +508,13 @@ __device__ __forceinline__ uint4 panel_cols(const char* panel, int j, int kb, in
   return uint4{x.x, x.y, y.x, y.y};
 }
 // the high part of value (r, col) of panels of MP rows
-template <bool LO, int MP>
+template <int MP>
 __device__ __forceinline__ uint16_t* panel_at(char* panels, int r, int col) {
-  const int panel = LO ? col >> 5 : col >> 6, v = LO ? col & 31 : col & 63;
+  const int panel = col >> 5, v = col & 31;
   return reinterpret_cast<uint16_t*>(panels + panel * MP * 128 + r * 128 + (((v >> 3) ^ (r & 7)) * 16)) + (v & 7);
 }
 // (the low part's chunk is four from the high part's, before the exchange by r & 7)
-template <bool LO, int MP>
+template <int MP>
 __device__ __forceinline__ void panel_put4(char* panels, int r, int col, const float (&v)[4]) {
   f16x4 h, l;
 #pragma unroll
@@ -537,25 +522,21 @@ __device__ __forceinline__ void panel_put4(char* panels, int r, int col, const f
     h[q] = (_Float16)v[q];
     l[q] = (_Float16)(v[q] - (float)h[q]);
   }
-  uint16_t* p = panel_at<LO, MP>(panels, r, col);
+  uint16_t* p = panel_at<MP>(panels, r, col);
   *reinterpret_cast<f16x4*>(p) = h;
-  if (LO) *reinterpret_cast<f16x4*>(reinterpret_cast<uint16_t*>(reinterpret_cast<uintptr_t>(p) ^ 64)) = l;
+  *reinterpret_cast<f16x4*>(reinterpret_cast<uint16_t*>(reinterpret_cast<uintptr_t>(p) ^ 64)) = l;
 }
-template <bool LO, int MP>
+template <int MP>
 __device__ __forceinline__ void panel_get4(const char* panels, int r, int col, float (&v)[4]) {
-  const uint16_t* p = panel_at<LO, MP>(const_cast<char*>(panels), r, col);
+  const uint16_t* p = panel_at<MP>(const_cast<char*>(panels), r, col);
   const f16x4 h = *reinterpret_cast<const f16x4*>(p);
+  const f16x4 l = *reinterpret_cast<const f16x4*>(reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(p) ^ 64));
 #pragma unroll
-  for (int q = 0; q < 4; ++q) v[q] = (float)h[q];
-  if (LO) {
-    const f16x4 l = *reinterpret_cast<const f16x4*>(reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(p) ^ 64));
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] += (float)l[q];
-  }
+  for (int q = 0; q < 4; ++q) v[q] = (float)h[q] + (float)l[q];
 }
 
-// One stage of k (a panel's 128-byte rows) into acc: hi hi and, with LO, the cross products.
-template <bool LO, int MI, int NI, class FA, class FB>
+// One stage of k (a panel's 128-byte rows) into acc: hi hi and the cross products.
+template <int MI, int NI, class FA, class FB>
 __device__ __forceinline__ void stage(f32x4 (&acc)[MI][NI], FA fa_of, FB fb_of) {
   uint4 fa[2][MI], fb[2][NI];
 #pragma unroll
@@ -566,12 +547,11 @@ __device__ __forceinline__ void stage(f32x4 (&acc)[MI][NI], FA fa_of, FB fb_of) 
     for (int i = 0; i < MI; ++i) fa[h][i] = fa_of(i, h);
   }
 #pragma unroll
-  for (int h = 0; h < (LO ? 3 : 2); ++h)
+  for (int h = 0; h < 3; ++h)
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
-        acc[i][j] = mfma_f16(fb[LO ? h == 1 : h][j], fa[LO ? h == 2 : h][i], acc[i][j]);
+      for (int j = 0; j < NI; ++j) acc[i][j] = mfma_f16(fb[h == 1][j], fa[h == 2][i], acc[i][j]);
 }
 template <int MI, int NI>
 __device__ __forceinline__ void clear(f32x4 (&acc)[MI][NI]) {
@@ -583,9 +563,8 @@ __device__ __forceinline__ void clear(f32x4 (&acc)[MI][NI]) {
 
 template <class T, int MP>
 __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs p) {
-  constexpr bool LO = sizeof(T) == 4;
-  constexpr int NT = kSmallWaves * 64, kPanel = MP * 128, AP = (LO ? 2 : 1) * MP / 64 > 0 ? (LO ? 2 : 1) * MP / 64 : 1;
-  constexpr int CP = LO ? 32 : 64;                 // columns of a panel
+  constexpr int CP = 32;                           // columns of a panel
+  constexpr int NT = kSmallWaves * 64, kPanel = MP * 128, AP = MP / CP;
   constexpr int WR = MP / 16 < 4 ? MP / 16 : 4, WC = WR;  // waves of A
   constexpr int MI = MP / 16 / WR, NI = MP / 16 / WC;
   constexpr int XR = MP / 32, XI = MP / 16 / XR;  // row parts of a panel of X, their 16-row blocks
@@ -656,10 +635,10 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
     for (int k = 0; k < 4; ++k) {
       if (k >= n) break;
       const float y = scaled(p.nesterov ? fmaf(p.mu, m[k], x[k]) : m[k], inv, kXe);
-      uint16_t* o = panel_at<LO, MP>(xs, tall ? q : r, tall ? r : q);
+      uint16_t* o = panel_at<MP>(xs, tall ? q : r, tall ? r : q);
       const _Float16 h = (_Float16)y;
       *o = __builtin_bit_cast(uint16_t, h);
-      if (LO) *reinterpret_cast<uint16_t*>(reinterpret_cast<uintptr_t>(o) ^ 64) = __builtin_bit_cast(uint16_t, (_Float16)(y - (float)h));
+      *reinterpret_cast<uint16_t*>(reinterpret_cast<uintptr_t>(o) ^ 64) = __builtin_bit_cast(uint16_t, (_Float16)(y - (float)h));
       if (++q == p.cols) q = 0, ++r;
     }
   });
@@ -675,7 +654,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
     if (mine)
       for (int q = 0; q < p.panels; ++q) {
         const char* x = xs + q * kPanel;
-        stage<LO>(acc, [&](int i, int h) { return panel_rows(x, wr * MI + i, h, c, g); },
+        stage(acc, [&](int i, int h) { return panel_rows(x, wr * MI + i, h, c, g); },
                   [&](int j, int h) { return panel_rows(x, wc * NI + j, h, c, g); });
       }
     auto store = [&](float zs) {
@@ -687,7 +666,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
           float v[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[k] = zs * acc[i][j][k];
-          panel_put4<LO, MP>(as, r, col, v);
+          panel_put4<MP>(as, r, col, v);
         }
     };
     if (mine) store(pow2(kAe - 2 * kXe));
@@ -698,7 +677,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
 #pragma unroll
       for (int q = 0; q < AP; ++q) {
         const char* x = as + q * kPanel;
-        stage<LO>(acc, [&](int i, int h) { return panel_rows(x, wr * MI + i, h, c, g); },
+        stage(acc, [&](int i, int h) { return panel_rows(x, wr * MI + i, h, c, g); },
                   [&](int j, int h) { return panel_rows(x, wc * NI + j, h, c, g); });
       }
 #pragma unroll
@@ -706,7 +685,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
           float v[4];
-          panel_get4<LO, MP>(as, 16 * (wr * MI + i) + c, 16 * (wc * NI + j) + 4 * g, v);
+          panel_get4<MP>(as, 16 * (wr * MI + i) + c, 16 * (wc * NI + j) + 4 * g, v);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             acc[i][j][k] = fmaf(kQ * pow2(kBe - kAe), v[k], kS * pow2(kBe - 2 * kAe) * acc[i][j][k]);
@@ -724,18 +703,18 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
       if (u < units) {
 #pragma unroll
         for (int q = 0; q < MP / 32; ++q) {
-          // rows of B: 32 of its columns in two parts, or one half of a panel's 64
-          const char* bq = as + (LO ? q : q / 2) * kPanel;
+          // rows of B: 32 of its columns in two parts
+          const char* bq = as + q * kPanel;
           uint4 fa[2][XI], fb[2][XJ];
 #pragma unroll
-          for (int h = 0; h < (LO ? 2 : 1); ++h) {
+          for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int i = 0; i < XI; ++i) fa[h][i] = panel_rows(bq, part * XI + i, LO ? h : q & 1, c, g);
+            for (int i = 0; i < XI; ++i) fa[h][i] = panel_rows(bq, part * XI + i, h, c, g);
 #pragma unroll
-            for (int j = 0; j < XJ; ++j) fb[h][j] = panel_cols(x, LO ? j + 2 * h : j, q, c, g);
+            for (int j = 0; j < XJ; ++j) fb[h][j] = panel_cols(x, j + 2 * h, q, c, g);
           }
 #pragma unroll
-          for (int h = 0; h < (LO ? 3 : 1); ++h)
+          for (int h = 0; h < 3; ++h)
 #pragma unroll
             for (int i = 0; i < XI; ++i)
 #pragma unroll
@@ -746,7 +725,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
 #pragma unroll
           for (int j = 0; j < XJ; ++j) {
             float v[4];
-            panel_get4<LO, MP>(x, 16 * (part * XI + i) + c, 16 * j + 4 * g, v);
+            panel_get4<MP>(x, 16 * (part * XI + i) + c, 16 * j + 4 * g, v);
 #pragma unroll
             for (int k = 0; k < 4; ++k) z[i][j][k] = fmaf(kP, v[k], pow2(-kBe) * z[i][j][k]);
           }
@@ -758,7 +737,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
 #pragma unroll
           for (int j = 0; j < XJ; ++j) {
             const float v[4] = {z[i][j][0], z[i][j][1], z[i][j][2], z[i][j][3]};
-            panel_put4<LO, MP>(xs, 16 * (part * XI + i) + c, panel * CP + 16 * j + 4 * g, v);
+            panel_put4<MP>(xs, 16 * (part * XI + i) + c, panel * CP + 16 * j + 4 * g, v);
           }
     }
     __syncthreads();
@@ -767,10 +746,9 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
   // W along X, in W's order (a lane's values of the last product lie in 16 rows: 13 us
   // more for 128 x 128 float32)
   const auto x_at = [&](int r, int q) {
-    const uint16_t* o = panel_at<LO, MP>(xs, tall ? q : r, tall ? r : q);
-    float v = (float)__builtin_bit_cast(_Float16, *o);
-    if (LO) v += (float)__builtin_bit_cast(_Float16, *reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(o) ^ 64));
-    return v;
+    const uint16_t* o = panel_at<MP>(xs, tall ? q : r, tall ? r : q);
+    return (float)__builtin_bit_cast(_Float16, *o) +
+           (float)__builtin_bit_cast(_Float16, *reinterpret_cast<const uint16_t*>(reinterpret_cast<uintptr_t>(o) ^ 64));
   };
   for (int i0 = threadIdx.x * 4; i0 < n4; i0 += NT * 4 * kFlight) {
     typename Vec<T, 4>::raw w[kFlight];
@@ -801,8 +779,8 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
 // ---- host ---------------------------------------------------------------------------
 // Blocks of a launch's last round whose tiles are cut along k, and their parts.
 constexpr int kParts = 512;       // blocks of parts at most
-// Stages of k of a part at least (1024 x 5632 float32: 507 us with 8, 522 with 4, 519 with
-// 16; 1024 x 1024 bfloat16 222, 233, 243; 512 x 2048 float32 203, 197, 192).
+// Stages of k of a part at least (3 of 517 x 200 bfloat16: 133 us with 8, 139 with 16; 1024 x
+// 1024 float32 265, 283, 335 with 24; 512 x 2048 184, 195, 219; 1024 x 5632 520, 517, 499).
 constexpr int kLeastSteps = 8;
 // Sides from which symmetric products take 128 x 128 tiles (512 x 2048 float32: 203 us
 // with 64 x 64, 229 with 128; 1024 x 5632: 315 of 510 us with 64, 302 of 523 with 128).
@@ -817,11 +795,10 @@ struct Bufs {
 
 // The rows that a block holds a small matrix in, or 0; its LDS.
 int small_of(const hg_muon_desc* A, size_t* bytes) {
-  const bool lo = A->dtype == HG_DTYPE_F32;
   const int32_t m = std::min(A->rows, A->cols), n = std::max(A->rows, A->cols);
   if (A->steps == 0 || m > 128) return 0;
-  const int mp = m <= 32 ? 32 : m <= 64 ? 64 : 128, cp = lo ? 32 : 64;
-  const size_t panels = (size_t)(cdiv(n, cp) + cdiv(mp, cp)), need = panels * mp * 128;
+  const int mp = m <= 32 ? 32 : m <= 64 ? 64 : 128;
+  const size_t panels = (size_t)(cdiv(n, 32) + mp / 32), need = panels * mp * 128;
   if (need > 152 * 1024) return 0;  // (and 8 KB for the norm)
   *bytes = need;
   return mp;
@@ -830,11 +807,10 @@ int small_of(const hg_muon_desc* A, size_t* bytes) {
 template <class Mem>
 Stored stored(const hg_muon_desc* A, int32_t rows, int32_t cols, bool memory, Mem& m) {
   Stored p{};
-  const bool lo = A->dtype == HG_DTYPE_F32;
   p.rows = rows;
   p.cols = cols;
-  p.pad = lo ? (cols + 31) / 32 * 32 : (cols + 7) / 8 * 8;
-  p.ld = lo ? 2 * p.pad : p.pad;
+  p.pad = (cols + 31) / 32 * 32;
+  p.ld = 2 * p.pad;
   p.step = (int64_t)rows * p.ld;
   if (memory) p.p = m.template take<uint16_t>(p.step * A->count);
   return p;
@@ -877,16 +853,16 @@ int check(const hg_muon_desc* A, const char* what) {
 
 // CUT: tiles of the last round may be cut along k.  Not those of the products with X,
 // whose sums are larger than what the cut saves (1024 x 1024 float32 266 us, 294 with).
-template <class TL, bool AKM, bool BKM, bool LO, int EPI, class T, bool CUT = EPI <= kEpiSymAdd>
+template <class TL, bool AKM, bool BKM, int EPI, class T, bool CUT = EPI <= kEpiSymAdd>
 int product(const char* name, MuonArgs a, int count, hipStream_t s) {
   a.tiles_m = (a.M + TL::BM - 1) / TL::BM;
   a.tiles_n = (a.N + TL::BN - 1) / TL::BN;
   a.tiles = EPI <= kEpiSymAdd ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
-  constexpr auto kernel = k_muon_product<TL, AKM, BKM, LO, EPI, T>;
+  constexpr auto kernel = k_muon_product<TL, AKM, BKM, EPI, T>;
   HG_TRY(allow_lds<kernel>(TL::kLds));
   // one block a tile in whole rounds of the chip; the rest in parts, if that helps
   const int64_t tiles = (int64_t)a.tiles * count, slots = (int64_t)num_cus() * std::max<int64_t>(1, 160 * 1024 / (int64_t)TL::kLds);
-  const int64_t rest = tiles % slots, steps = cdiv(a.K, LO ? 32 : 64);
+  const int64_t rest = tiles % slots, steps = cdiv(a.K, 32);
   a.pieces = 1;
   if (CUT && rest)
     a.pieces = (int32_t)std::max<int64_t>(1, std::min(std::min<int64_t>(slots, kParts) / rest, steps / kLeastSteps));
@@ -894,7 +870,7 @@ int product(const char* name, MuonArgs a, int count, hipStream_t s) {
   HG_LAUNCH(name, kernel, dim3((unsigned)(a.full + (tiles - a.full) * a.pieces)), dim3(TL::NT), TL::kLds, s, a);
   if constexpr (CUT) {
     if (a.pieces > 1)
-      HG_LAUNCH("muon_join", (k_muon_join<TL, LO, EPI, T>), dim3((unsigned)(rest * TL::MI * TL::NI)), dim3(TL::NT), 0, s, a);
+      HG_LAUNCH("muon_join", (k_muon_join<TL, EPI, T>), dim3((unsigned)(rest * TL::MI * TL::NI)), dim3(TL::NT), 0, s, a);
   }
   return HG_OK;
 }
@@ -905,27 +881,26 @@ typedef Tile<128, 128, 64, 64, 2> T128;
 typedef Tile<256, 256, 128, 64, 2> T256;
 
 // Symmetric products.  A A has k as short as its sides: from 1024 to 2048 one launch of
-// small tiles beats large ones in parts and their sum (1024 x 1024 float32: 277 us, 294;
-// 1024 x 4096 bfloat16: 238, 258; 512 x 2048 float32: 210, 206).
-template <bool AKM, bool LO, int EPI, class T>
+// small tiles beats large ones in parts and their sum (1024 x 1024 float32: 277 us, 294).
+template <bool AKM, int EPI, class T>
 int symmetric(const char* name, const MuonArgs& a, int count, hipStream_t s) {
-  if (EPI == kEpiSymAdd && a.M >= 1024 && a.M < 2048) return product<T64, AKM, AKM, LO, EPI, T, false>(name, a, count, s);
-  if (a.M >= kSym128) return product<T128, AKM, AKM, LO, EPI, T>(name, a, count, s);
-  return product<T64, AKM, AKM, LO, EPI, T>(name, a, count, s);
+  if (EPI == kEpiSymAdd && a.M >= 1024 && a.M < 2048) return product<T64, AKM, AKM, EPI, T, false>(name, a, count, s);
+  if (a.M >= kSym128) return product<T128, AKM, AKM, EPI, T>(name, a, count, s);
+  return product<T64, AKM, AKM, EPI, T>(name, a, count, s);
 }
 
-// Products with X.
-template <bool BKM, bool LO, int EPI, class T>
+// Products with X (4096 x 8192: 6.17 ms with 256 x 256 tiles, 6.43 with 128 x 128; 6403 x
+// 2050: 1.64 with either).
+template <bool BKM, int EPI, class T>
 int apply(const char* name, const MuonArgs& a, int count, hipStream_t s) {
   const auto tiles = [&](int bm, int bn) { return cdiv(a.M, bm) * cdiv(a.N, bn) * count; };
-  if constexpr (!LO)
-    if (tiles(256, 256) >= 192) return product<T256, true, BKM, LO, EPI, T>(name, a, count, s);
-  if (tiles(128, 128) >= 512) return product<T128, true, BKM, LO, EPI, T>(name, a, count, s);
-  if (tiles(64, 128) >= 256) return product<T64x128, true, BKM, LO, EPI, T>(name, a, count, s);
-  return product<T64, true, BKM, LO, EPI, T>(name, a, count, s);
+  if (tiles(256, 256) >= 192) return product<T256, true, BKM, EPI, T>(name, a, count, s);
+  if (tiles(128, 128) >= 512) return product<T128, true, BKM, EPI, T>(name, a, count, s);
+  if (tiles(64, 128) >= 256) return product<T64x128, true, BKM, EPI, T>(name, a, count, s);
+  return product<T64, true, BKM, EPI, T>(name, a, count, s);
 }
 
-template <bool TALL, bool LO, class TW>
+template <bool TALL, class TW>
 int steps(const hg_muon_desc* A, const Bufs& b, void* W, hipStream_t s) {
   Stored x = b.x0, next = b.x1;
   const int32_t k = std::min(A->rows, A->cols), len = std::max(A->rows, A->cols);
@@ -937,13 +912,13 @@ int steps(const hg_muon_desc* A, const Bufs& b, void* W, hipStream_t s) {
     g.M = g.N = k;
     g.K = len;
     g.zs = pow2(kAe - 2 * kXe);
-    HG_TRY((symmetric<!TALL, LO, kEpiSym, TW>("muon_gram", g, A->count, s)));
+    HG_TRY((symmetric<!TALL, kEpiSym, TW>("muon_gram", g, A->count, s)));
     g.a = g.b = g.c = b.a;
     g.o = b.b;
     g.K = k;
     g.zs = kS * pow2(kBe - 2 * kAe);
     g.cs = kQ * pow2(kBe - kAe);
-    HG_TRY((symmetric<true, LO, kEpiSymAdd, TW>("muon_square", g, A->count, s)));
+    HG_TRY((symmetric<true, kEpiSymAdd, TW>("muon_square", g, A->count, s)));
     g.a = TALL ? x : b.b;
     g.b = TALL ? b.b : x;
     g.c = x;
@@ -954,13 +929,13 @@ int steps(const hg_muon_desc* A, const Bufs& b, void* W, hipStream_t s) {
     g.zs = pow2(-kBe);
     g.cs = kP;
     if (i + 1 < A->steps) {
-      HG_TRY((apply<TALL, LO, kEpiAdd, TW>("muon_apply", g, A->count, s)));
+      HG_TRY((apply<TALL, kEpiAdd, TW>("muon_apply", g, A->count, s)));
       std::swap(x, next);
     } else {
       g.W = W;
       g.ws = 1.f - A->lr * A->weight_decay;
       g.us = A->lr * A->scale * pow2(-kXe);
-      HG_TRY((apply<TALL, LO, kEpiUpdate, TW>("muon_update", g, A->count, s)));
+      HG_TRY((apply<TALL, kEpiUpdate, TW>("muon_update", g, A->count, s)));
     }
   }
   return HG_OK;
@@ -976,7 +951,7 @@ int small(const hg_muon_desc* A, size_t bytes, T* W, const T* G, float* M, hipSt
   a.cols = A->cols;
   a.m = std::min(A->rows, A->cols);
   a.n = std::max(A->rows, A->cols);
-  a.panels = (int32_t)cdiv(a.n, sizeof(T) == 4 ? 32 : 64);
+  a.panels = (int32_t)cdiv(a.n, 32);
   a.steps = A->steps;
   a.nesterov = A->nesterov;
   a.mu = A->mu;
@@ -991,7 +966,6 @@ int small(const hg_muon_desc* A, size_t bytes, T* W, const T* G, float* M, hipSt
 
 template <class T>
 int run(const hg_muon_desc* A, const Bufs& b, T* W, const T* G, float* M, hipStream_t s) {
-  constexpr bool LO = sizeof(T) == 4;
   size_t bytes = 0;
   switch (small_of(A, &bytes)) {
     case 32: return small<T, 32>(A, bytes, W, G, M, s);
@@ -1003,13 +977,13 @@ int run(const hg_muon_desc* A, const Bufs& b, T* W, const T* G, float* M, hipStr
   const dim3 grid((unsigned)b.parts, (unsigned)A->count);
   HG_LAUNCH("muon_momentum", k_muon_momentum<T>, grid, dim3(256), 0, s, G, M, n, A->mu, A->nesterov, b.part);
   if (A->steps == 0) {
-    HG_LAUNCH("muon_first", (k_muon_first<T, LO, true>), grid, dim3(256), 0, s, G, M, A->rows, A->cols, A->mu, A->nesterov,
+    HG_LAUNCH("muon_first", (k_muon_first<T, true>), grid, dim3(256), 0, s, G, M, A->rows, A->cols, A->mu, A->nesterov,
               b.part, b.parts, A->eps, b.x0, W, 1.f - A->lr * A->weight_decay, A->lr * A->scale);
     return HG_OK;
   }
-  HG_LAUNCH("muon_first", (k_muon_first<T, LO, false>), grid, dim3(256), 0, s, G, M, A->rows, A->cols, A->mu, A->nesterov, b.part,
+  HG_LAUNCH("muon_first", (k_muon_first<T, false>), grid, dim3(256), 0, s, G, M, A->rows, A->cols, A->mu, A->nesterov, b.part,
             b.parts, A->eps, b.x0, W, 0.f, 0.f);
-  return A->rows > A->cols ? steps<true, LO, T>(A, b, W, s) : steps<false, LO, T>(A, b, W, s);
+  return A->rows > A->cols ? steps<true, T>(A, b, W, s) : steps<false, T>(A, b, W, s);
 }
 
 }  // namespace

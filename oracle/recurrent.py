@@ -80,12 +80,12 @@ def recur_bwd(x, r, i, decay, rate, h, dh, lens=None, state=None, dstate_out=Non
             before = h[s, k - 1] if k else (np.zeros(w) if state is None else np.asarray(state, F64)[s])
             g = dh[s, k] + c
             dx[s, k] = g * q * si
-            di[s, k] = g * q * x[s, k] * si * (1 - si)
+            di[s, k] = g * q * x[s, k] * si * sigmoid(-i[s, k])
             # dq/dl = -a^2 / q; times l or sr it goes to 0 where l does
             with np.errstate(divide="ignore", invalid="ignore"):
                 slope = np.where(q > 0, a * a / q, 0.0)
             dlog = g * (a * before - si * x[s, k] * slope)
-            dr[s, k] = dlog * l * (1 - sr)
+            dr[s, k] = dlog * l * sigmoid(-r[s, k])
             ddecay += -rate * sigmoid(decay) * dlog * sr
             c = a * g
         dstate[s] = c

@@ -55,7 +55,13 @@ struct RecurArgs {
 template <class T>
 using Quad = Vec<T, V>;
 
-__device__ __forceinline__ float sigm(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * z)); }
+// sigmoid(z) from e = 2^(-z log2 e), and sigmoid(-z) by its own size: 1 - sigmoid(z) has
+// no digits left from z = 17 on.  (Where e is infinite the sigmoid is 0, and so is
+// what the backward multiplies the other with: any finite value will do.)
+__device__ __forceinline__ float exp_of(float z) { return __builtin_amdgcn_exp2f(-kLog2e * z); }
+__device__ __forceinline__ float sigm_of(float e) { return __builtin_amdgcn_rcpf(1.f + e); }
+__device__ __forceinline__ float rest_of_sigm(float e, float s) { return fminf(e, 3.4e38f) * s; }
+__device__ __forceinline__ float sigm(float z) { return sigm_of(exp_of(z)); }
 
 // rate softplus(decay) log2 e: the factor is 2^(-that sigmoid(r)).  Finite, so that it is
 // 0 times sigmoid(r) = 0.
@@ -283,23 +289,31 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_fwd(const RecurArgs a) {
 }
 
 // The gradients at one token, and what it adds to the sums; at: the gradient that
-// reaches h from the token after, becomes the one that this token passes on.
+// reaches h from the token after, becomes the one that this token passes on.  fe: the
+// exponential of the gate r, from which its sigmoid is formed again (as many registers
+// as the sigmoid, and the derivative keeps its digits).  The empty asm keeps the compiler
+// from holding the sigmoids and the unpacked dh as well (bfloat16 tiles 240 registers, 283
+// and one wave a SIMD without).
 template <class T>
-__device__ __forceinline__ void grads_of(const float (&slope)[V], const float (&fs)[V], const float (&fa)[V], const float (&gh)[V],
-                                         const typename Quad<T>::raw& ri, const typename Quad<T>::raw& rx, const float (&hb)[V],
-                                         float (&at)[V], float (&sum)[V], float (&vx)[V], float (&vi)[V], float (&vr)[V]) {
+__device__ __forceinline__ void grads_of(const float (&slope)[V], const float (&fe)[V], const float (&fa)[V],
+                                         typename Quad<T>::raw rg, const typename Quad<T>::raw& ri,
+                                         const typename Quad<T>::raw& rx, const float (&hb)[V], float (&at)[V], float (&sum)[V],
+                                         float (&vx)[V], float (&vi)[V], float (&vr)[V]) {
+  asm("" : "+v"(rg));
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const float f = fa[j], l = slope[j] * fs[j], g = gh[j] + at[j];
+    float er = fe[j];
+    asm("" : "+v"(er));
+    const float s = sigm_of(er), f = fa[j], l = slope[j] * s, g = Quad<T>::get(rg, j) + at[j];
     at[j] = f * g;
     // (1 - a^2 at least 2^-120, below which l = 0, so that its root's inverse is finite)
     const float m = rest_of(l, f), iq = __builtin_amdgcn_rsqf(fmaxf(m, 7.5e-37f)), q = m * iq;
-    const float sg = sigm(Quad<T>::get(ri, j)), x = Quad<T>::get(rx, j), gs = g * sg;
+    const float ei = exp_of(Quad<T>::get(ri, j)), sg = sigm_of(ei), x = Quad<T>::get(rx, j), gs = g * sg;
     vx[j] = gs * q;
-    vi[j] = vx[j] * x * (1.f - sg);
+    vi[j] = vx[j] * x * rest_of_sigm(ei, sg);
     const float dl = f * fmaf(g, hb[j], -gs * x * f * iq);
-    sum[j] = fmaf(dl, fs[j], sum[j]);
-    vr[j] = dl * (l * 0.69314718055994531f) * (1.f - fs[j]);
+    sum[j] = fmaf(dl, s, sum[j]);
+    vr[j] = dl * (l * 0.69314718055994531f) * rest_of_sigm(er, s);
   }
 }
 
@@ -355,7 +369,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
     auto tile = [&](auto full, int64_t ts) {
       constexpr bool FULL = decltype(full)::value;
       const int64_t t0 = ts + skip;
-      float fs[K][V], fa[K][V], gh[K][V];
+      float fe[K][V], fa[K][V];
       Step s;
 #pragma unroll
       for (int j = 0; j < V; ++j) s.a[j] = 1.f, s.b[j] = 0.f;
@@ -364,11 +378,10 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
         const bool in = FULL || t0 + k >= 0;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          fs[k][j] = sigm(Quad<T>::get(rr[k], j));
-          const float f = __builtin_amdgcn_exp2f(slope[j] * fs[k][j]);
+          fe[k][j] = exp_of(Quad<T>::get(rr[k], j));
+          const float f = __builtin_amdgcn_exp2f(slope[j] * sigm_of(fe[k][j]));
           fa[k][j] = in ? f : 1.f;
-          gh[k][j] = in ? Quad<T>::get(rg[k], j) : 0.f;
-          s.b[j] = fa[k][j] * (s.b[j] + gh[k][j]);
+          s.b[j] = fa[k][j] * (s.b[j] + (in ? Quad<T>::get(rg[k], j) : 0.f));
           s.a[j] *= fa[k][j];
         }
       }
@@ -382,7 +395,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_bwd(const RecurArgs a, int32
 #pragma unroll
         for (int j = 0; j < V; ++j) hb[j] = Quad<T>::get(rh[k], j);
         if (!FULL && t0 + k == 0) load_state(a.s_first, a, p, hb);
-        grads_of<T>(slope, fs[k], fa[k], gh[k], ri[k], rx[k], hb, at, sum, vx, vi, vr);
+        grads_of<T>(slope, fe[k], fa[k], rg[k], ri[k], rx[k], hb, at, sum, vx, vi, vr);
         if (p.on) {
           Quad<T>::put(ox.at(ts, k), vx);
           Quad<T>::put(oi.at(ts, k), vi);
@@ -680,7 +693,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a,
     } else {
       fetch(Bool<false>{});
     }
-    float slope[V], fs[K][V], fa[K][V], gh[K][V], at[V], y0 = 0.f, out = 0.f;
+    float slope[V], fe[K][V], fa[K][V], at[V], y0 = 0.f, out = 0.f;
 #pragma unroll
     for (int j = 0; j < V; ++j) slope[j] = -slope_of(a.decay[p.c0 + j], a.rate);
     if (n < kGroup && a.s_in) y0 = a.s_in[state_at];  // (it reaches group 0)
@@ -691,11 +704,10 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a,
     for (int k = K - 1; k >= 0; --k) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        fs[k][j] = sigm(Quad<T>::get(rr[k], j));
-        const float f = __builtin_amdgcn_exp2f(slope[j] * fs[k][j]);
+        fe[k][j] = exp_of(Quad<T>::get(rr[k], j));
+        const float f = __builtin_amdgcn_exp2f(slope[j] * sigm_of(fe[k][j]));
         fa[k][j] = f;
-        gh[k][j] = Quad<T>::get(rg[k], j);
-        s.b[j] = fa[k][j] * (s.b[j] + gh[k][j]);
+        s.b[j] = fa[k][j] * (s.b[j] + Quad<T>::get(rg[k], j));
         s.a[j] *= fa[k][j];
       }
     }
@@ -708,7 +720,7 @@ __global__ void __launch_bounds__(kNW * 64) k_recur_chain_bwd(const RecurArgs a,
 #pragma unroll
       for (int j = 0; j < V; ++j) hb[j] = Quad<T>::get(rh[k], j);
       if (t0 + k == 0) load_state(a.s_first, a, p, hb);
-      grads_of<T>(slope, fs[k], fa[k], gh[k], ri[k], rx[k], hb, at, sum, vx, vi, vr);
+      grads_of<T>(slope, fe[k], fa[k], rg[k], ri[k], rx[k], hb, at, sum, vx, vi, vr);
       if (p.on) {
         Quad<T>::put(ox.at(ts, k), vx);
         Quad<T>::put(oi.at(ts, k), vi);

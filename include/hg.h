@@ -732,7 +732,7 @@ int hg_recur_fwd(const hg_recur_desc* A, const hg_heads* x, const hg_heads* r, c
  *   dlog_t = g_t (a_t h_{t-1} - sigmoid(i_t) x_t a_t^2 / q_t),
  *   dr_t = dlog_t l_c sigmoid'(r_t),  ddecay[c] = -rate softplus'(decay[c]) sum dlog_t sigmoid(r_t),
  *   dstate = a_0 g_0
- * (dr and ddecay's term are 0, their limit, where l_c sigmoid(r_t) = 0).  dx, dr, di
+ * (dx, di and what x adds to dlog_t are 0 where q_t^2 is below 2^-126).  dx, dr, di
  * and dstate [batch, width] (may be NULL) are OVERWRITTEN; ddecay [width] (may be
  * NULL) is OVERWRITTEN when accumulate = 0 and added into when accumulate = 1. */
 int hg_recur_bwd(const hg_recur_desc* A, const hg_heads* x, const hg_heads* r, const hg_heads* i, const float* decay,

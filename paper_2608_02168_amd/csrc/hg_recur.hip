@@ -306,12 +306,12 @@ __device__ __forceinline__ void grads_of(const float (&slope)[V], const float (&
     asm("" : "+v"(er));
     const float s = sigm_of(er), f = fa[j], l = slope[j] * s, g = Quad<T>::get(rg, j) + at[j];
     at[j] = f * g;
-    // (1 - a^2 at least 2^-120, below which l = 0, so that its root's inverse is finite)
-    const float m = rest_of(l, f), iq = __builtin_amdgcn_rsqf(fmaxf(m, 7.5e-37f)), q = m * iq;
+    // (1 - a^2 below the smallest normal number, whose root the hardware does not take, is zero)
+    const float m = rest_of(l, f), iq = m >= 0x1p-126f ? __builtin_amdgcn_rsqf(m) : 0.f, q = m * iq;
     const float ei = exp_of(Quad<T>::get(ri, j)), sg = sigm_of(ei), x = Quad<T>::get(rx, j), gs = g * sg;
     vx[j] = gs * q;
     vi[j] = vx[j] * x * rest_of_sigm(ei, sg);
-    const float dl = f * fmaf(g, hb[j], -gs * x * f * iq);
+    const float dl = f * fmaf(g, hb[j], -gs * iq * f * x);  // (iq first: where it is zero, no product of g and x)
     sum[j] = fmaf(dl, s, sum[j]);
     vr[j] = dl * (l * 0.69314718055994531f) * rest_of_sigm(er, s);
   }

@@ -699,9 +699,10 @@ int hg_linattn_step(const hg_linattn_desc* A, const hg_heads* q, const hg_heads*
  * (sequence b, token t, channel c) lies at p[b * batch + t * token + c] of an
  * hg_heads whose head stride is not used.  Strides are at least 0 and at most 2^40
  * (a token's of the recurrence 2^21), those of outputs keep the rows apart.
- * Outputs must not overlap inputs or each other; views of one packed buffer may
- * interleave.  Workspaces are 16-byte aligned; two calls that may run at the same
- * time need one each.  Asynchronous and deterministic.
+ * Outputs must not overlap inputs or each other; views of one packed buffer that
+ * have the same strides may interleave, in any order of its dimensions.  Workspaces
+ * are 16-byte aligned; two calls that may run at the same time need one each.
+ * Asynchronous and deterministic.
  *
  * Gated linear recurrence: the GRU of E13 without its products with the state,
  * so that a history is a scan.  Per channel c with l_c = -rate softplus(decay[c]),

@@ -5,6 +5,8 @@
 // value's size).
 #pragma once
 
+#include <algorithm>
+
 #include "hg_mfma.h"
 
 namespace hg {
@@ -81,8 +83,9 @@ inline int check_rows(const char* what, const hg_heads* x, const char* name, boo
   return HG_OK;
 }
 
-// Whether an output's rows o may share an address with the rows x: not if they lie
-// in different stretches of memory, nor if they are different columns of one buffer.
+// Whether an output's rows o may share an address with the rows x: not if they lie in
+// different stretches of memory; with the same strides (views of one buffer) exactly if
+// some two rows are less than a row's width apart.
 inline bool rows_meet(const hg_heads* o, const hg_heads* x, int64_t batch, int64_t t, int32_t width, int32_t dtype) {
   if (t < 1 || batch < 1) return false;
   const int64_t e = dtype == HG_DTYPE_F32 ? 4 : 2;
@@ -90,11 +93,25 @@ inline bool rows_meet(const hg_heads* o, const hg_heads* x, int64_t batch, int64
   const intptr_t po = reinterpret_cast<intptr_t>(o->p), px = reinterpret_cast<intptr_t>(x->p);
   if (po + bytes(o) <= px || px + bytes(x) <= po) return false;
   if ((t > 1 && o->token != x->token) || (batch > 1 && o->batch != x->batch)) return true;
-  const int64_t row = t > 1 ? o->token : o->batch, d = (po < px ? px - po : po - px);
-  if (t == 1 && batch == 1) return true;
-  if (d % e || d / e >= row || d / e < width || row - d / e < width) return true;
-  // the last row of a sequence and the first of the next
-  return t > 1 && batch > 1 && o->batch % o->token != 0 && o->batch < t * o->token;
+  if ((px - po) % e) return true;
+  // Rows (b, t) of o and (b', t') of x start d - k2 outer - k1 inner values apart, k1 and k2 any
+  // differences of their indexes.  An outer step is longer than all inner ones with a row
+  // (check_rows), so only the two k2 next to d matter, and for each the two k1 next to what is left.
+  struct Step {
+    int64_t stride, most;
+  } inner{t > 1 ? o->token : 1, t - 1}, outer{batch > 1 ? o->batch : 1, batch - 1};
+  if (inner.stride > outer.stride) std::swap(inner, outer);
+  const auto near = [](int64_t d, const Step& s, int up) {
+    const int64_t k = d / s.stride - (d % s.stride < 0) + up;
+    return d - std::min(std::max(k, -s.most), s.most) * s.stride;
+  };
+  const int64_t d = (px - po) / e;
+  for (int a = 0; a < 2; ++a)
+    for (int b = 0; b < 2; ++b) {
+      const int64_t apart = near(near(d, outer, a), inner, b);
+      if (apart > -width && apart < width) return true;
+    }
+  return false;
 }
 
 // Whether two stretches of memory share an address (not if either is null or empty).

@@ -1153,17 +1153,19 @@ __global__ void __launch_bounds__(256) k_product_join(const GShape p, int splits
 }
 
 // More than 64 KB of LDS for a kernel: an attribute of its copy on each device, set
-// before its first launch there (a device past the 64th sets it every time).
-template <auto kern>
-int allow_lds(size_t lds) {
-  if (lds > 65536) {
+// before its first launch there (a device past the 64th sets it every time).  MOST:
+// the most dynamic LDS that any launch of the kernel asks for, STATIC: what it has
+// beside that.
+template <auto kern, size_t MOST, size_t STATIC = 0>
+int allow_lds() {
+  if constexpr (MOST + STATIC > 65536) {
     static std::atomic<uint64_t> set_on{0};
     int dev = 0;
     HG_HIP_TRY(hipGetDevice(&dev));
     const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
     if (!(set_on.load(std::memory_order_relaxed) & bit)) {
       HG_HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                     (int)lds));
+                                     (int)MOST));
       set_on.fetch_or(bit, std::memory_order_relaxed);
     }
   }

@@ -296,7 +296,7 @@ int launch_tiles(const char* name, const GArgs<uint16_t>& a, const Tiling& t, hi
   constexpr size_t lds = g_lds_bytes(2, TILE, TILE, 64);
   constexpr int WN = TILE == 256 ? 64 : TILE / 2, NT = 2 * (TILE / WN) * 64;
   constexpr auto kern = k_gemm16<AKM, BKM, TILE, TILE, 64, TILE / 2, WN, Epi, SPLIT>;
-  HG_TRY((allow_lds<kern>(lds)));
+  HG_TRY((allow_lds<kern, lds>()));
   HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(NT), lds, s, a);
   return HG_OK;
 }
@@ -305,7 +305,7 @@ template <bool AKM, bool BKM, int TILE, class Epi, bool SPLIT, bool VEC>
 int launch_tiles32(const char* name, const GArgs<float>& a, const Tiling& t, hipStream_t s) {
   constexpr size_t lds = g_lds_bytes(3, TILE, TILE, kG32K);
   constexpr auto kern = k_gemm32<AKM, BKM, TILE, TILE, TILE / 2, TILE / 2, Epi, SPLIT, VEC>;
-  HG_TRY((allow_lds<kern>(lds)));
+  HG_TRY((allow_lds<kern, lds>()));
   HG_LAUNCH(name, kern, dim3((unsigned)(t.tiles_m * t.tiles_n), SPLIT ? t.splits : 1), dim3(256), lds, s, a);
   return HG_OK;
 }
@@ -581,10 +581,10 @@ int narrow_bwd(const Prob& p, const float* X, const float* W, const float* bias,
   const GNarrow a{X,     W,       dY,  bias, dX,    p.ld_x, p.ld_y, p.ld_r, p.n, p.d, p.f,
                   p.act, b.part, dbias ? b.colsum : nullptr, p.f};
   if (p.d <= 64 && p.f <= 64) {
-    HG_TRY((allow_lds<k_narrow_bwd<2>>(kNarrowLds)));
+    HG_TRY((allow_lds<k_narrow_bwd<2>, kNarrowLds>()));
     HG_LAUNCH("linear_narrow_bwd", k_narrow_bwd<2>, dim3(kNarrowBlocks), dim3(kNarrowThreads), kNarrowLds, s, a);
   } else {
-    HG_TRY((allow_lds<k_narrow_bwd<4>>(kNarrowLds)));
+    HG_TRY((allow_lds<k_narrow_bwd<4>, kNarrowLds>()));
     HG_LAUNCH("linear_narrow_bwd", k_narrow_bwd<4>, dim3(kNarrowBlocks), dim3(kNarrowThreads), kNarrowLds, s, a);
   }
   GShape j{};

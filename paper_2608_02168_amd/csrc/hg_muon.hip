@@ -491,6 +491,8 @@ struct SmallArgs {
 };
 
 constexpr int kSmallWaves = 16;
+constexpr size_t kSmallStatic = (size_t)kSmallWaves * 64 * sizeof(double);  // the norm's sums
+constexpr size_t kSmallLds = 160 * 1024 - kSmallStatic;                    // X and A at most
 constexpr int kFlight = 4;  // times four values of a thread in flight
 
 // fragment of rows 16 i + c of a panel, k = 32 kb + 8 g ..
@@ -571,6 +573,7 @@ __global__ void __launch_bounds__(kSmallWaves * 64) k_muon_small(const SmallArgs
   constexpr int XJ = CP / 16;
   extern __shared__ __align__(1024) char lds[];
   __shared__ double sh[NT];
+  static_assert(sizeof(sh) == kSmallStatic, "the LDS beside the panels");
   char *xs = lds, *as = lds + p.panels * kPanel;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, g = lane >> 4;
   const int64_t size = (int64_t)p.rows * p.cols, base = blockIdx.x * size;
@@ -799,7 +802,7 @@ int small_of(const hg_muon_desc* A, size_t* bytes) {
   if (A->steps == 0 || m > 128) return 0;
   const int mp = m <= 32 ? 32 : m <= 64 ? 64 : 128;
   const size_t panels = (size_t)(cdiv(n, 32) + mp / 32), need = panels * mp * 128;
-  if (need > 152 * 1024) return 0;  // (and 8 KB for the norm)
+  if (need > kSmallLds) return 0;
   *bytes = need;
   return mp;
 }
@@ -859,7 +862,7 @@ int product(const char* name, MuonArgs a, int count, hipStream_t s) {
   a.tiles_n = (a.N + TL::BN - 1) / TL::BN;
   a.tiles = EPI <= kEpiSymAdd ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
   constexpr auto kernel = k_muon_product<TL, AKM, BKM, EPI, T>;
-  HG_TRY(allow_lds<kernel>(TL::kLds));
+  HG_TRY((allow_lds<kernel, TL::kLds>()));
   // one block a tile in whole rounds of the chip; the rest in parts, if that helps
   const int64_t tiles = (int64_t)a.tiles * count, slots = (int64_t)num_cus() * std::max<int64_t>(1, 160 * 1024 / (int64_t)TL::kLds);
   const int64_t rest = tiles % slots, steps = cdiv(a.K, 32);
@@ -959,7 +962,7 @@ int small(const hg_muon_desc* A, size_t bytes, T* W, const T* G, float* M, hipSt
   a.ws = 1.f - A->lr * A->weight_decay;
   a.us = A->lr * A->scale * pow2(-kXe);
   constexpr auto kernel = k_muon_small<T, MP>;
-  HG_TRY(allow_lds<kernel>(bytes));
+  HG_TRY((allow_lds<kernel, kSmallLds, kSmallStatic>()));
   HG_LAUNCH("muon_small", kernel, dim3((unsigned)A->count), dim3(kSmallWaves * 64), bytes, s, a);
   return HG_OK;
 }

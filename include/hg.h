@@ -788,7 +788,8 @@ int hg_group_norm_bwd(const hg_group_norm_desc* A, const hg_heads* x, const floa
  * which brings every singular value of X near 1, and
  *   W = (1 - lr weight_decay) W - lr scale X
  * W and G [count, rows, cols] in dtype, M float32, contiguous; W, G and M do not
- * overlap.  M = 0 before the first update.
+ * overlap.  M = 0 before the first update.  A usual scale is
+ * sqrt(max(1, outputs / inputs)): of hg_linear's W [d_in, d_out], cols / rows.
  * Precision: |U| is summed in float64 and every product in float32.  Matrices of
  * both types enter the products as two fp16 parts of each value, three part
  * products (the row transforms' rule stated at the top, with one scale for the

@@ -1329,7 +1329,10 @@ def hg_muon_step(param, grad, momentum, lr: float, mu: float = 0.95, weight_deca
                  steps: int = 5, scale: Optional[float] = None, eps: float = 1e-7, ws=None, stream=None):
     """One update of matrices along their orthogonalised momentum, in place on
     param and momentum: param and grad [rows, cols] or [count, rows, cols],
-    float32 or bfloat16, momentum float32.  scale None: sqrt(max(1, rows / cols))."""
+    float32 or bfloat16, momentum float32.  scale None: sqrt(max(1, rows / cols)), the
+    published factor for weights stored [outputs, inputs]; the weights of
+    hg_linear_fwd and hg_glu_fwd are [inputs, outputs], for which it is
+    sqrt(max(1, cols / rows)): give it as scale (as encoder.train does)."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return hg_muon_step(param, grad, momentum, lr, mu, weight_decay, nesterov, steps, scale, eps, ws)

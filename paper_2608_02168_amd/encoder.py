@@ -280,7 +280,8 @@ def train(cfg: EncoderConfig, steps: int, batch: int = 512, t: int = 96, seed: i
         flat = [g[n] for g in grads for n in cfg.params] + [hg[n] for n in head]
         for k, (w, g, (m, v)) in enumerate(zip(tensors, flat, moments)):
             if optimizer == "muon" and k < of_blocks and w.dim() == 2:
-                api.hg_muon_step(w, g, m, lr=lr)
+                # weights are [inputs, outputs]: the published factor, for outputs over inputs
+                api.hg_muon_step(w, g, m, lr=lr, scale=max(1.0, w.shape[1] / w.shape[0]) ** 0.5)
             else:
                 api.hg_adam_step(w, g, m, v, i, lr=lr)
         losses.append(loss)

@@ -60,6 +60,9 @@ class EncoderConfig:
             raise ValueError(f"{self}: {self.heads} heads on {self.kv_heads} key heads")
         if self.d % self.heads or self.d_head % 8 or not 8 <= self.d_head <= 128:
             raise ValueError(f"{self}: d is not heads of a multiple of 8 up to 128 columns")
+        # (the first decays are logarithms of exponentials of 0.2 / rate)
+        if not 1e-3 <= self.rate < float("inf"):
+            raise ValueError(f"{self}: a rate is finite and at least 0.001")
 
     @property
     def params(self) -> tuple:

@@ -795,10 +795,12 @@ __global__ void __launch_bounds__(256)
 
 // ---- host ---------------------------------------------------------------------------
 constexpr int64_t kMaxToken = (int64_t)1 << 21;  // (a tile has at most 2^8 tokens of 4-byte values)
-// Tokens of a thread's run.  Where a block walks a sequence, fewer registers and more
-// waves against the shuffles and LDS of a tile: backward of 8 x 2048 tokens of 2048
-// channels, bfloat16, 102 us with 2, 108 with 4; a wave for each of 8192 float32
-// histories of 24 tokens 62 us with 1, 67 with 2.
+// Tokens of a thread's run: fewer registers and more waves against the shuffles and LDS
+// of a tile.  Where a block walks a sequence, bfloat16: backward of 64 x 512 tokens of
+// 2048 channels 251 us with 2, 257 with 1, 248 with 4, of 2048 x 96 tokens of 64 channels
+// 54, 52 and 62; forward of the former 119 with 4, 117 with 2, 127 with 8, of 2048 x 1024
+// tokens of 64 channels 217, 222 and 224.  A wave for each of 8192 float32 histories of 24
+// tokens, backward: 62 us with 1, 67 with 2.
 constexpr int fwd_run(bool wave) { return wave ? 2 : 4; }
 constexpr int bwd_run(bool wave) { return wave ? 1 : 2; }
 // In a chain the whole tile is in flight at once: one history of 65521 tokens of 1024
@@ -820,17 +822,23 @@ Split split_of(const hg_recur_desc* A, bool bwd) {
   Split s{};
   s.slabs = (int32_t)cdiv(A->width, kSlab);
   const int64_t pairs = (int64_t)A->batch * s.slabs;
-  s.wave = pairs >= 4096 || A->t <= 64;
+  // Up to a tile of 64 tokens, a wave each (8192 histories of 64 bfloat16 channels: of 24
+  // tokens forward 23 us, 61 in blocks, backward 57, 86; of 64 tokens 55, 65 and 123, 140; of
+  // 128 tokens 116, 113 and 230, 236).
+  s.wave = A->t <= 64;
   if (s.wave) {
     s.rows = cdiv(A->batch, kNW);
     if (bwd) s.rows = std::min<int64_t>(s.rows, std::max<int64_t>(1, cdiv(2048, s.slabs)));
     s.stride = (int32_t)(s.rows * kNW);
     return s;
   }
-  // Few sequences: one pass, a block a tile.  Walked in segments by a block each, after
-  // a pass that composes the segments' steps, the long history above took 219 us.
+  // Few sequences, up to three blocks for two CUs: one pass, a block a tile (64 bfloat16
+  // channels, 256 of 4096 tokens: forward 129 us, 137 where a block walks each, backward 287,
+  // 346; 384 of 2048: 104, 99 and 227, 224; 512 of 2048: 132, 115 and 289, 232).  Walked in
+  // segments by a block each, after a pass that composes the segments' steps, the long history
+  // above took 219 us.
   const int64_t tile = (int64_t)kNW * TW * chain_run(bwd, A->dtype == HG_DTYPE_F32);
-  s.chain = pairs < 1024 && pairs * cdiv(A->t, tile) < (int64_t)1 << 24;  // (a grid has fewer than 2^32 threads)
+  s.chain = pairs < 384 && pairs * cdiv(A->t, tile) < (int64_t)1 << 24;  // (a grid has fewer than 2^32 threads)
   s.tiles = s.chain ? (int32_t)cdiv(A->t, tile) : 1;
   s.rows = (int64_t)A->batch * s.tiles;
   return s;

@@ -785,9 +785,6 @@ constexpr int kParts = 512;       // blocks of parts at most
 // Stages of k of a part at least (3 of 517 x 200 bfloat16: 133 us with 8, 139 with 16; 1024 x
 // 1024 float32 265, 283, 335 with 24; 512 x 2048 184, 195, 219; 1024 x 5632 520, 517, 499).
 constexpr int kLeastSteps = 8;
-// Sides from which symmetric products take 128 x 128 tiles (512 x 2048 float32: 203 us
-// with 64 x 64, 229 with 128; 1024 x 5632: 315 of 510 us with 64, 302 of 523 with 128).
-constexpr int kSym128 = 1024;
 
 struct Bufs {
   double* part = nullptr;
@@ -854,10 +851,11 @@ int check(const hg_muon_desc* A, const char* what) {
   return HG_OK;
 }
 
-// CUT: tiles of the last round may be cut along k.  Not those of the products with X,
-// whose sums are larger than what the cut saves (1024 x 1024 float32 266 us, 294 with).
-template <class TL, bool AKM, bool BKM, int EPI, class T, bool CUT = EPI <= kEpiSymAdd>
+// Tiles of the last round may be cut along k.  Not those of the products with X, whose
+// sums are larger than what the cut saves (1024 x 1024 float32 266 us, 294 with).
+template <class TL, bool AKM, bool BKM, int EPI, class T>
 int product(const char* name, MuonArgs a, int count, hipStream_t s) {
+  constexpr bool CUT = EPI <= kEpiSymAdd;
   a.tiles_m = (a.M + TL::BM - 1) / TL::BM;
   a.tiles_n = (a.N + TL::BN - 1) / TL::BN;
   a.tiles = EPI <= kEpiSymAdd ? a.tiles_m * (a.tiles_m + 1) / 2 : a.tiles_m * a.tiles_n;
@@ -883,23 +881,27 @@ typedef Tile<64, 128, 32, 64, 2> T64x128;
 typedef Tile<128, 128, 64, 64, 2> T128;
 typedef Tile<256, 256, 128, 64, 2> T256;
 
-// Symmetric products.  A A has k as short as its sides: from 1024 to 2048 one launch of
-// small tiles beats large ones in parts and their sum (1024 x 1024 float32: 277 us, 294).
+// Symmetric products: tiles of 64 x 64 up to sides of 2048 (1024 x 1024: 246 us, 262 with 128
+// x 128 for A; 2000 x 2500: 862, 930; the square of 2048 x 4096 with 128 x 128: 1.07 ms in
+// all, 1.15 with 64 x 64), unless k is five times the side or more (A of 1024 x 5632: 509 us
+// with 128 x 128, 522 with 64 x 64; of 1024 x 4096: 427, 416).
 template <bool AKM, int EPI, class T>
 int symmetric(const char* name, const MuonArgs& a, int count, hipStream_t s) {
-  if (EPI == kEpiSymAdd && a.M >= 1024 && a.M < 2048) return product<T64, AKM, AKM, EPI, T, false>(name, a, count, s);
-  if (a.M >= kSym128) return product<T128, AKM, AKM, EPI, T>(name, a, count, s);
+  if (a.M >= 2048 || (a.M >= 1024 && a.K >= 5 * a.M)) return product<T128, AKM, AKM, EPI, T>(name, a, count, s);
   return product<T64, AKM, AKM, EPI, T>(name, a, count, s);
 }
 
-// Products with X (4096 x 8192: 6.17 ms with 256 x 256 tiles, 6.43 with 128 x 128; 6403 x
-// 2050: 1.64 with either).
+// Products with X: the largest tiles of which there are some for every CU.  A product of 2560 x
+// 5120 (200 tiles of 256 x 256) takes 208 us with them, 222 with 128 x 128, of 2304 x 5376 (189)
+// 185 and 167; of 2500 x 2500 (400 of 128 x 128) 115 with them, 132 with 64 x 128, of 2048 x 2048
+// (256) 65 and 61; of 1536 x 1536 (288 of 64 x 128) 45 with them, 54 with 64 x 64, of 1024 x
+// 2048 (256) 30 and 26.
 template <bool BKM, int EPI, class T>
 int apply(const char* name, const MuonArgs& a, int count, hipStream_t s) {
   const auto tiles = [&](int bm, int bn) { return cdiv(a.M, bm) * cdiv(a.N, bn) * count; };
   if (tiles(256, 256) >= 192) return product<T256, true, BKM, EPI, T>(name, a, count, s);
-  if (tiles(128, 128) >= 512) return product<T128, true, BKM, EPI, T>(name, a, count, s);
-  if (tiles(64, 128) >= 256) return product<T64x128, true, BKM, EPI, T>(name, a, count, s);
+  if (tiles(128, 128) > 384) return product<T128, true, BKM, EPI, T>(name, a, count, s);
+  if (tiles(64, 128) > 256) return product<T64x128, true, BKM, EPI, T>(name, a, count, s);
   return product<T64, true, BKM, EPI, T>(name, a, count, s);
 }
 

@@ -569,28 +569,31 @@ Plan plan_of(const hg_group_norm_desc* A, bool bwd) {
   a.nv = a.cg / p.v;
   a.lc = log2_up(a.nv);
   // An item's threads: up to 256 of four or eight tokens each, else up to 1024 of eight
-  // (in the backward, which holds three times as much, of one or two); else chunks.
+  // (in the backward, which holds three times as much, of one or two); else chunks.  Few
+  // such items too: one of 1000 float32 tokens of 16 channels takes 12 us, 18 in chunks.
   const int64_t t = std::max<int64_t>(A->t, 1);
   const int lr4 = log2_up(cdiv(t, 4)), lr8 = log2_up(cdiv(t, kMostRows)), lrb = log2_up(cdiv(t, p.v == 8 ? 1 : 2));
   const int lr = a.lc + lr4 <= 8 ? lr4 : a.lc + lr8 <= 8 || !bwd ? lr8 : lrb;
-  p.chunked = a.lc + lr > 10 ||
-              // items that leave most of the chip without a block are better cut, once they are long
-              (lr >= 3 && a.lc + lr > 8 && (int64_t)A->batch * A->groups < 64);
+  p.chunked = a.lc + lr > 10;
   if (!p.chunked) {
     a.lp = a.lc + lr;
     p.r = 1 << std::min(3, log2_up(cdiv(t, (int64_t)1 << lr)));
     p.bt = a.lp <= 8 ? 256 : 1024;
     // A row of partial sums of dw and db for each block of the backward: few blocks
-    // (16384 rows of 16 x 64 channels 37 us with 1024, 42 with 1536), but single channels
-    // a thread are few bytes in flight and take more (20000 rows of 32 x 25 channels 73
-    // us with 4096, 77 with 2048).
-    lay_out(p, A->batch, !bwd ? (int64_t)1 << 21 : p.bt == 256 ? (p.v == 1 ? 4096 : 1024) : 512);
+    // (16384 bfloat16 rows of 16 x 64 channels 37 us with 1024, 36 with 512, 44 with 2048,
+    // float32 44, 57 and 52; of 1024 threads, 4096 rows of 8192 bfloat16 channels 74 us with
+    // 256, 90 with 512, 118 with 128), but single channels a thread are few bytes in flight
+    // and take more (20000 bfloat16 rows of 32 x 25 channels 71 us with 2048, 90 with 1024, 69
+    // with 4096, 100000 float32 ones of 5 x 25 87, 125 and 93).
+    lay_out(p, A->batch, !bwd ? (int64_t)1 << 21 : p.bt == 256 ? (p.v == 1 ? 2048 : 1024) : 256);
     return p;
   }
   p.r = kMostRows;
   p.bt = 256;
   if (bwd) {
-    // columns: a slab of 2^lc threads, chunks so that the blocks fill the chip
+    // columns: a slab of 2^lc threads, chunks so that the blocks fill the chip (200003 rows of
+    // 128 float32 channels 110 us with 1024 blocks, 108 with 512, 111 with 2048; 64 x 5000 of
+    // 128 bfloat16 channels 97, 96 and 93)
     const int64_t cols = A->width / p.v;
     a.lc = std::min(6, log2_up(cols));
     a.slabs = (int32_t)cdiv(cols, (int64_t)1 << a.lc);

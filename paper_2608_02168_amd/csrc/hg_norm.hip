@@ -579,13 +579,21 @@ Plan plan_of(const hg_group_norm_desc* A, bool bwd) {
     a.lp = a.lc + lr;
     p.r = 1 << std::min(3, log2_up(cdiv(t, (int64_t)1 << lr)));
     p.bt = a.lp <= 8 ? 256 : 1024;
-    // A row of partial sums of dw and db for each block of the backward: few blocks
-    // (16384 bfloat16 rows of 16 x 64 channels 37 us with 1024, 36 with 512, 44 with 2048,
-    // float32 44, 57 and 52; of 1024 threads, 4096 rows of 8192 bfloat16 channels 74 us with
-    // 256, 90 with 512, 118 with 128), but single channels a thread are few bytes in flight
-    // and take more (20000 bfloat16 rows of 32 x 25 channels 71 us with 2048, 90 with 1024, 69
-    // with 4096, 100000 float32 ones of 5 x 25 87, 125 and 93).
-    lay_out(p, A->batch, !bwd ? (int64_t)1 << 21 : p.bt == 256 ? (p.v == 1 ? 2048 : 1024) : 256);
+    // A block fetches w and b once, and each block of the backward has a row of partial sums
+    // of dw and db: few blocks, but enough to fill the chip.  Forward, 16384 rows of 16 x 64
+    // channels: bfloat16 30 us with 2048, 28 with 1024, 37 with 4096, 62 with one for every two
+    // rows, float32 29, 33, 29 and 37; of 1024 threads, 4096 bfloat16 rows of 4096 channels 34 us
+    // with 512, 42 with 1024, 63 with one for each.  Backward, the same rows: bfloat16 37 us with
+    // 1024, 36 with 512, 44 with 2048, float32 44, 57 and 52; of 1024 threads, 4096 rows of 8192
+    // bfloat16 channels 74 us with 256, 90 with 512, 118 with 128.  Single channels a thread are
+    // few bytes in flight and take more: 30000 bfloat16 rows of 32 x 25 channels forward 124 us
+    // with 4096, 133 with 2048, 161 with one for each; backward, 20000 such rows 71 us with 2048,
+    // 90 with 1024, 69 with 4096, 100000 float32 ones of 5 x 25 87, 125 and 93.
+    if (bwd) {
+      lay_out(p, A->batch, p.bt > 256 ? 256 : p.v == 1 ? 2048 : 1024);
+    } else {
+      lay_out(p, A->batch, p.bt > 256 ? 512 : p.v == 1 ? 4096 : 2048);
+    }
     return p;
   }
   p.r = kMostRows;

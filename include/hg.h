@@ -799,8 +799,8 @@ int hg_group_norm_bwd(const hg_group_norm_desc* A, const hg_heads* x, const floa
  * 1e-4 of its norm after five steps (485 2^-22, a matrix of rank one).  W is rounded
  * once.  A matrix whose U holds a value that is not finite becomes NaN as a whole;
  * the others of the call do not.
- * rows and cols are at most 2^15, count rows cols is below 2^32 and count times the
- * 64 x 64 tiles of a matrix below 2^22. */
+ * rows and cols are at most 2^15, count at most 65535, count rows cols is below
+ * 2^32 and count times the 64 x 64 tiles of a matrix below 2^22. */
 typedef struct hg_muon_desc {
   int32_t count, rows, cols;
   int32_t dtype;      /* of W and G */

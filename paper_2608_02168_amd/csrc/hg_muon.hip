@@ -23,7 +23,11 @@
 // W are the products' epilogues, so a step is three launches (and where the last tiles'
 // k is cut, the sums of the parts).  Bound by the MFMA: a step of 4096 x 8192 is 362 us
 // for A, 186 for B and 670 for B X (1.1, 1.1 and 1.2 PFLOP/s of fp16 products; a large
-// library product 1.2), of 1024 x 5632 27, 20 and 50 (0.7 PFLOP/s; the tiles are few).
+// library product 1.2), of 1024 x 5632 34, 16 and 50 (0.5, 0.2 and 0.7 PFLOP/s; the
+// tiles are few, and 9 and 6 of it add parts of k).
+//
+// The iteration with these three coefficients and five steps is a published method (K.
+// Jordan and others, 2024: an optimizer for hidden layers).
 #include <cmath>
 
 #include "hg_gemm.h"

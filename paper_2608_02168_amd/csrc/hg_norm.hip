@@ -15,10 +15,10 @@
 // pass that forms the output (k_norm_apply); in the backward sums of the columns,
 // joined, and a pass.
 //
-// Bound by HBM, the backward with an activation by the vector unit as well (56% of the
+// Bound by HBM, the backward with an activation by the vector unit as well (55% of the
 // cycles: 16384 rows of 16 x 64 bfloat16 channels 34 us, 3.0 TB/s).  A float32 backward
 // of 200003 rows of 128 channels: 51 us for the columns (4.1 TB/s), 48 for the pass
-// (6.4); a forward of 512 x 96 tokens of 200 float32 channels 18 us (3.9).
+// (6.4); a forward of 512 x 96 tokens of 200 float32 channels 16 us (4.3).
 #include <cmath>
 
 #include "hg_gemm.h"

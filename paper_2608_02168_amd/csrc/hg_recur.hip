@@ -16,6 +16,10 @@
 // (WAVE: no barrier) or a block walks each.  Few: a block for each tile, all at once,
 // and the tiles' steps compose through memory (k_recur_chain_*).
 //
+// The gates are a published recurrence's (S. De and others, 2024, arXiv 2402.19427); that
+// tiles publish their composed steps and form their prefix from those before is the
+// one-pass scan of D. Merrill and M. Garland, 2016.
+//
 // Bound by HBM and by the vector instructions at once: 49 issue slots a value forward, six
 // instructions of them transcendental, are 83 us for 67M values on this chip, their 8
 // bytes 103 us at the 5.2 TB/s of a large copy (one pass over both: 128 us).
@@ -805,9 +809,9 @@ constexpr int fwd_run(bool wave) { return wave ? 2 : 4; }
 constexpr int bwd_run(bool wave) { return wave ? 1 : 2; }
 // In a chain the whole tile is in flight at once: one history of 65521 tokens of 1024
 // channels, bfloat16, 132 us with 14, 137 with 10 or 12, 142 with 16; 8 x 2048 tokens of
-// 1024 channels, float32, 64 us with 8, 67 with 10, 69 with 6, their backward 125 us with
-// 5, 128 with 4, 148 with 6; ragged in bfloat16, 2048 channels, 105 us with 9, 107 with
-// 8, 132 with 10.
+// 1024 channels, float32, 64 us with 8, 67 with 10, 69 with 6, their backward 128 us with
+// 5, 127 with 4 or 6; ragged in bfloat16, 2048 channels, 108 us with 9, 110 with 8, 136
+// with 10.
 constexpr int chain_run(bool bwd, bool f32) { return bwd ? (f32 ? 5 : 9) : (f32 ? 8 : 14); }
 
 struct Split {

@@ -885,10 +885,10 @@ typedef Tile<64, 128, 32, 64, 2> T64x128;
 typedef Tile<128, 128, 64, 64, 2> T128;
 typedef Tile<256, 256, 128, 64, 2> T256;
 
-// Symmetric products: tiles of 64 x 64 up to sides of 2048 (1024 x 1024: 246 us, 262 with 128
-// x 128 for A; 2000 x 2500: 862, 930; the square of 2048 x 4096 with 128 x 128: 1.07 ms in
-// all, 1.15 with 64 x 64), unless k is five times the side or more (A of 1024 x 5632: 509 us
-// with 128 x 128, 522 with 64 x 64; of 1024 x 4096: 427, 416).
+// Symmetric products: tiles of 64 x 64 up to sides of 2048 (whole updates: 1024 x 1024 246 us,
+// 262 with 128 x 128 for A; 2000 x 2500 862, 930; 2048 x 4096 1.15 ms, 1.07 with 128 x 128),
+// unless k is five times the side or more (1024 x 8192: 667 us, 630 with 128 x 128 for A; 1024 x
+// 5120: 499, 491; 1024 x 4096: 416, 427).
 template <bool AKM, int EPI, class T>
 int symmetric(const char* name, const MuonArgs& a, int count, hipStream_t s) {
   if (a.M >= 2048 || (a.M >= 1024 && a.K >= 5 * a.M)) return product<T128, AKM, AKM, EPI, T>(name, a, count, s);

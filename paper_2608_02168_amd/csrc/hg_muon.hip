@@ -885,26 +885,34 @@ typedef Tile<64, 128, 32, 64, 2> T64x128;
 typedef Tile<128, 128, 64, 64, 2> T128;
 typedef Tile<256, 256, 128, 64, 2> T256;
 
-// Symmetric products: tiles of 64 x 64 up to sides of 2048 (whole updates: 1024 x 1024 246 us,
-// 262 with 128 x 128 for A; 2000 x 2500 862, 930; 2048 x 4096 1.15 ms, 1.07 with 128 x 128),
-// unless k is five times the side or more (1024 x 8192: 667 us, 630 with 128 x 128 for A; 1024 x
-// 5120: 499, 491; 1024 x 4096: 416, 427).
+// Symmetric products: tiles of 128 x 128 where there are many, or k is long, and they cover
+// little more than tiles of 64 x 64, whose sums of cut tiles are smaller.  Whole updates with
+// either for A, by tiles of 128 x 128 times k: 1024 x 4096 (36 x 4096) 427 us, 416 with 64 x 64;
+// 1024 x 5120 491, 499; 4 of 1024 x 1024 (144 x 1024) 486, 463; 16 of 600 x 2400 (240 x 2400)
+// 1.17 ms, 1.25; 2048 x 4096 (136 x 4096) 1.07 ms, 1.15.  Rows that fill no tile: 64 of 300 x
+// 2000 (60% more covered) 1.41 ms, 1.49; 64 of 130 x 2000 (twice as much) 622 us, 572.
 template <bool AKM, int EPI, class T>
 int symmetric(const char* name, const MuonArgs& a, int count, hipStream_t s) {
-  if (a.M >= 2048 || (a.M >= 1024 && a.K >= 5 * a.M)) return product<T128, AKM, AKM, EPI, T>(name, a, count, s);
+  const auto tiles = [&](int64_t side) { return cdiv(a.M, side) * (cdiv(a.M, side) + 1) / 2; };
+  const bool few128 = 4 * (double)tiles(128) <= 1.65 * (double)tiles(64);
+  if (tiles(128) * count * a.K >= 160 * 1024 && few128) return product<T128, AKM, AKM, EPI, T>(name, a, count, s);
   return product<T64, AKM, AKM, EPI, T>(name, a, count, s);
 }
 
-// Products with X: the largest tiles of which there are some for every CU.  A product of 2560 x
-// 5120 (200 tiles of 256 x 256) takes 208 us with them, 222 with 128 x 128, of 2304 x 5376 (189)
-// 185 and 167; of 2500 x 2500 (400 of 128 x 128) 115 with them, 132 with 64 x 128, of 2048 x 2048
-// (256) 65 and 61; of 1536 x 1536 (288 of 64 x 128) 45 with them, 54 with 64 x 64, of 1024 x
-// 2048 (256) 30 and 26.
+// Products with X: the largest tiles of which there are some for every CU, unless they
+// cover much more than smaller ones would.  A product of 2560 x 5120 (200 tiles of 256 x 256)
+// takes 208 us with them, 222 with 128 x 128, of 2304 x 5376 (189) 185 and 167; of 2500 x 2500
+// (400 of 128 x 128) 115 with them, 132 with 64 x 128, of 2048 x 2048 (256) 65 and 61; of 1536 x
+// 1536 (288 of 64 x 128) 45 with them, 54 with 64 x 64, of 1024 x 2048 (256) 30 and 26.  Rows
+// that fill no tile: 4 of 1100 x 5000 (11% more in 256 x 256 than in 128 x 128) 203 us, 171, 64 of
+// 300 x 2000 (20% more in 128 x 128 than in 64 x 128) 164, 154, 20 of 700 x 2100 (9%) 169, 173.
 template <bool BKM, int EPI, class T>
 int apply(const char* name, const MuonArgs& a, int count, hipStream_t s) {
   const auto tiles = [&](int bm, int bn) { return cdiv(a.M, bm) * cdiv(a.N, bn) * count; };
-  if (tiles(256, 256) >= 192) return product<T256, true, BKM, EPI, T>(name, a, count, s);
-  if (tiles(128, 128) > 384) return product<T128, true, BKM, EPI, T>(name, a, count, s);
+  const auto covered = [&](int bm, int bn) { return (double)(cdiv(a.M, bm) * bm * cdiv(a.N, bn) * bn); };
+  const bool few256 = covered(256, 256) <= 1.05 * covered(128, 128) && covered(256, 256) <= 1.1 * covered(64, 128);
+  if (tiles(256, 256) >= 192 && few256) return product<T256, true, BKM, EPI, T>(name, a, count, s);
+  if (tiles(128, 128) > 384 && covered(128, 128) <= 1.1 * covered(64, 128)) return product<T128, true, BKM, EPI, T>(name, a, count, s);
   if (tiles(64, 128) > 256) return product<T64x128, true, BKM, EPI, T>(name, a, count, s);
   return product<T64, true, BKM, EPI, T>(name, a, count, s);
 }

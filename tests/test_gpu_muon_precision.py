@@ -86,3 +86,25 @@ def test_both_types_alike(kind, bar, m, n):
     assert torch.equal(M, M32)
     # either is off by its bar of the norm of X, whose singular values are at most 1.21
     assert excess(W.double().cpu().numpy(), W32.double().cpu().numpy()) < 2 * bar * 1.21 * min(m, n) ** 0.5
+
+
+# many matrices of a size between: tiles of 64, 128 and 256, tall ones, sides that fill no tile, cut tiles of several
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("count,m,n", [(16, 200, 4000), (16, 1000, 200), (64, 300, 700), (6, 640, 2500), (12, 700, 600),
+                                       (33, 130, 900), (4, 1100, 2050), (16, 256, 3000), (3, 1500, 1400)])
+def test_batches(count, m, n, dtype):
+    G = torch.stack([gradient(("independent", 0.1, 1 / 30)[k % 3], m, n, 20 + 3 * k) for k in range(count)]).to(dtype).cuda()
+    W, M = torch.zeros_like(G), torch.zeros(count, m, n).cuda()
+    api.hg_muon_step(W, G, M, lr=1.0, mu=0.0, nesterov=False, scale=1.0)
+    p, q, s = rec.COEF
+    for k in range(count):
+        X = G[k].double()
+        X /= X.norm()
+        for _ in range(5):
+            A = X @ X.T if m <= n else X.T @ X
+            B = q * A + s * (A @ A)
+            X = p * X + (B @ X if m <= n else X @ B)
+        d = (-W[k].double() - X).abs()
+        if dtype is BF16:
+            d = (d - 2.0 ** -8 * X.abs()).clamp(min=0)
+        assert float(d.norm() / X.norm()) < 3e-5, k

@@ -899,21 +899,26 @@ int symmetric(const char* name, const MuonArgs& a, int count, hipStream_t s) {
   return product<T64, AKM, AKM, EPI, T>(name, a, count, s);
 }
 
-// Products with X: the largest tiles of which there are some for every CU, unless they
-// cover much more than smaller ones would.  A product of 2560 x 5120 (200 tiles of 256 x 256)
-// takes 208 us with them, 222 with 128 x 128, of 2304 x 5376 (189) 185 and 167; of 2500 x 2500
-// (400 of 128 x 128) 115 with them, 132 with 64 x 128, of 2048 x 2048 (256) 65 and 61; of 1536 x
-// 1536 (288 of 64 x 128) 45 with them, 54 with 64 x 64, of 1024 x 2048 (256) 30 and 26.  Rows
-// that fill no tile: 4 of 1100 x 5000 (11% more in 256 x 256 than in 128 x 128) 203 us, 171, 64 of
-// 300 x 2000 (20% more in 128 x 128 than in 64 x 128) 164, 154, 20 of 700 x 2100 (9%) 169, 173.
+// Products with X: of the tiles of which there are some for every CU, those that give the
+// CU with the most of them the least work; the same work takes 5% longer in tiles of 128 x 128
+// than of 256 x 256, 20% in 64 x 128.  A product of 2560 x 5120 (200 tiles of 256 x 256) takes 208
+// us with them, 222 with 128 x 128, of 2304 x 5376 (189) 185 and 167; of 2500 x 2500 (400 of 128 x
+// 128) 115 with them, 132 with 64 x 128, of 2048 x 2048 (256) 65 and 61; of 1536 x 1536 (288 of
+// 64 x 128) 45 with them, 54 with 64 x 64, of 1024 x 2048 (256) 30 and 26.  Tiles that are partly
+// empty, or leave CUs without one at the end: 3432 x 5264 (294 of 256 x 256, a whole update) 4.27
+// ms, 3.54 with 128 x 128; 4 of 1100 x 5000 203 us, 171; 64 of 300 x 2000 164 us with 128 x 128,
+// 154 with 64 x 128.
 template <bool BKM, int EPI, class T>
 int apply(const char* name, const MuonArgs& a, int count, hipStream_t s) {
+  const int64_t cus = num_cus();
   const auto tiles = [&](int bm, int bn) { return cdiv(a.M, bm) * cdiv(a.N, bn) * count; };
-  const auto covered = [&](int bm, int bn) { return (double)(cdiv(a.M, bm) * bm * cdiv(a.N, bn) * bn); };
-  const bool few256 = covered(256, 256) <= 1.05 * covered(128, 128) && covered(256, 256) <= 1.1 * covered(64, 128);
-  if (tiles(256, 256) >= 192 && few256) return product<T256, true, BKM, EPI, T>(name, a, count, s);
-  if (tiles(128, 128) > 384 && covered(128, 128) <= 1.1 * covered(64, 128)) return product<T128, true, BKM, EPI, T>(name, a, count, s);
-  if (tiles(64, 128) > 256) return product<T64x128, true, BKM, EPI, T>(name, a, count, s);
+  const auto most = [&](int bm, int bn, int64_t least, double slow) {
+    return tiles(bm, bn) < least ? INFINITY : slow * (double)(cdiv(tiles(bm, bn), cus) * bm * bn);
+  };
+  const double w256 = most(256, 256, 192, 1.0), w128 = most(128, 128, 385, 1.05), w64 = most(64, 128, 257, 1.2);
+  if (w256 <= std::min(w128, w64) && w256 < INFINITY) return product<T256, true, BKM, EPI, T>(name, a, count, s);
+  if (w128 <= w64 && w128 < INFINITY) return product<T128, true, BKM, EPI, T>(name, a, count, s);
+  if (w64 < INFINITY) return product<T64x128, true, BKM, EPI, T>(name, a, count, s);
   return product<T64, true, BKM, EPI, T>(name, a, count, s);
 }
 
